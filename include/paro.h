@@ -330,6 +330,58 @@ int paro_cost(const char *strategy, double psi, double psi_trainable, int N, int
  * per mini-batch: Psi * (s - 1) * (g - 1) / N. */
 double paro_two_step_saving(double psi, int N, int M, int s);
 
+/* ---- operators beside the Update stage ----------------------------------------
+ * Where the contributions come from: the largest tensors of a language model get their
+ * gradients from the embedding, the feed-forward blocks and the loss.  These calls need no
+ * plan and no device memory of the library's; they enqueue kernels on `stream` and can be
+ * captured.  dtype: PARO_BF16, PARO_F32 or PARO_F16.  Arrays are DEVICE memory, aligned to their
+ * elements (16-byte aligned rows are the fast case); rows of activations lie ld elements
+ * apart (0 = dense), weights and their gradients are dense, as the layout above has them.  Outputs do not overlap inputs, but where said.
+ * A workspace is DEVICE memory of at least the bytes that the matching query returns, 16-byte
+ * aligned; its contents are of no account before and after the call, and calls that overlap in time
+ * need one each.  Sums run in fp32 in an order that the arguments fix: the same call gives
+ * the same bits.  Results are rounded once, to nearest even. */
+enum { PARO_I32 = 8, PARO_I64 = 9 }; /* dtype of token numbers */
+
+/* out[i] = scale * table[tokens[i] - first_token], 0 <= i < n.  table: [rows][dim]; it holds the tokens
+ * [first_token, first_token + rows) - a part of the vocabulary, where that is split.  Any other token (padding, -1)
+ * gives zeros. */
+int paro_embed(const void *table, int dtype, int64_t rows, int64_t dim, const void *tokens, int token_dtype,
+               int64_t n, int64_t first_token, float scale, void *out, int64_t ld_out, void *stream);
+
+/* grad[v] = scale * the sum of dout[i] over the tokens with tokens[i] - first_token == v, in the order of i
+ * (parts of long runs are summed apart); zeros for a row that no token names.  grad: [rows][dim], all of it
+ * written, of dout's dtype or fp32. */
+int64_t paro_embed_grad_workspace(int64_t n, int64_t rows, int64_t dim);
+int paro_embed_grad(const void *dout, int dtype, int64_t ld_dout, const void *tokens, int token_dtype, int64_t n,
+                    int64_t first_token, float scale, void *grad, int grad_dtype, int64_t rows, int64_t dim,
+                    void *workspace, int64_t workspace_bytes, void *stream);
+
+/* Distillation from a teacher's k largest logits at temperature T.  For each of n rows, with
+ *   p = softmax(teacher / T) over the row's held entries, q = softmax(logits / T) over the vocabulary:
+ *   loss = T^2 * sum_j p_j * (log p_j - log q[ids_j])
+ *   d loss / d logits[v] = T * (q[v] - the sum of p_j over the entries with ids_j == v)
+ * An entry is held when its id lies in [0, vocab) and its logit is not -inf; ids may repeat.  A row that holds none
+ * has loss 0 (and lse 0) and gradient 0, and its logits are not read.  A logit of -inf has q = 0. */
+enum { PARO_DISTILL_MAX_K = 1024 };
+typedef struct {
+    int64_t n, vocab, k;
+    int64_t ld_logits, ld_teacher, ld_dlogits;  /* elements from row to row, 0 = dense; ld_teacher: teacher and ids */
+    float temperature;
+    int32_t dtype, teacher_dtype;               /* of logits and dlogits; of teacher */
+    int32_t reserved_;                          /* 0 */
+} paro_distill_t;
+
+/* loss: fp32 [n].  lse: NULL, or fp32 [n] = log of the sum of exp(logits / T), for paro_distill_grad. */
+int paro_distill_loss(const paro_distill_t *d, const void *logits, const void *teacher, const int32_t *ids, float *loss,
+                      float *lse, void *stream);
+/* dlogits = dloss[row] * the gradient above.  dloss: fp32 [n], NULL = ones.  dlogits may be logits. */
+int paro_distill_grad(const paro_distill_t *d, const void *logits, const void *teacher, const int32_t *ids,
+                      const float *lse, const float *dloss, void *dlogits, void *stream);
+/* Both in one pass over the logits. */
+int paro_distill_step(const paro_distill_t *d, const void *logits, const void *teacher, const int32_t *ids,
+                      const float *dloss, float *loss, void *dlogits, void *stream);
+
 /* text of the calling thread's last error ("" if none); valid until that
  * thread's next failing call */
 const char *paro_last_error(void);

@@ -31,6 +31,8 @@ PARO_CHUNK, PARO_TENSORS = 0, 1
 PARO_RS, PARO_AG = 0, 1
 PARO_MAX_RANKS = 256
 PARO_STATIC_MAX_CHUNK = 1 << 30
+PARO_I32, PARO_I64 = 8, 9
+PARO_DISTILL_MAX_K = 1024
 
 for _f in (_SO, os.path.join(_HERE, "_marshal" + sysconfig.get_config_var("EXT_SUFFIX"))):
     if not os.path.exists(_f):
@@ -74,6 +76,12 @@ class paro_cost_t(Structure):
                [("recommended", c_int32 * 4), ("derived", c_int32)]
 
 
+class paro_distill_t(Structure):
+    _fields_ = [("n", c_int64), ("vocab", c_int64), ("k", c_int64), ("ld_logits", c_int64), ("ld_teacher", c_int64),
+                ("ld_dlogits", c_int64), ("temperature", c_float), ("dtype", c_int32), ("teacher_dtype", c_int32),
+                ("reserved_", c_int32)]
+
+
 EXPORTS = {
     "paro_strategy_legal": (c_int, [c_char_p]),
     "paro_plan": (c_int, [c_int, c_int, c_char_p, POINTER(c_int64), c_int64, POINTER(paro_plan_opts_t),
@@ -103,6 +111,14 @@ EXPORTS = {
                                        c_void_p]),
     "paro_cost": (c_int, [c_char_p, c_double, c_double, c_int, c_int, c_int, c_int, c_int, POINTER(paro_cost_t)]),
     "paro_two_step_saving": (c_double, [c_double, c_int, c_int, c_int]),
+    "paro_embed": (c_int, [c_void_p, c_int, c_int64, c_int64, c_void_p, c_int, c_int64, c_int64, c_float, c_void_p, c_int64,
+                           c_void_p]),
+    "paro_embed_grad_workspace": (c_int64, [c_int64, c_int64, c_int64]),
+    "paro_embed_grad": (c_int, [c_void_p, c_int, c_int64, c_void_p, c_int, c_int64, c_int64, c_float, c_void_p, c_int, c_int64,
+                                c_int64, c_void_p, c_int64, c_void_p]),
+    "paro_distill_loss": (c_int, [POINTER(paro_distill_t)] + [c_void_p] * 6),
+    "paro_distill_grad": (c_int, [POINTER(paro_distill_t)] + [c_void_p] * 7),
+    "paro_distill_step": (c_int, [POINTER(paro_distill_t)] + [c_void_p] * 7),
     "paro_last_error": (c_char_p, []),
 }
 for _name, (_res, _args) in EXPORTS.items():
@@ -278,6 +294,42 @@ def paro_cost(strategy: str, psi: float, psi_trainable: float, N: int, M: int, s
 
 def paro_two_step_saving(psi: float, N: int, M: int, s: int) -> float:
     return float(_lib.paro_two_step_saving(psi, N, M, s))
+
+
+# ---- operators beside the Update stage: where the contributions come from
+def paro_embed(table: int, dtype: int, rows: int, dim: int, tokens: int, token_dtype: int, n: int, first_token: int, scale: float,
+               out: int, ld_out: int = 0, stream: int = 0) -> None:
+    _check(_lib.paro_embed(table, dtype, rows, dim, tokens, token_dtype, n, first_token, scale, out, ld_out, stream))
+
+
+def paro_embed_grad_workspace(n: int, rows: int, dim: int) -> int:
+    """Bytes."""
+    rc = _lib.paro_embed_grad_workspace(n, rows, dim)
+    return rc if rc >= 0 else _check(rc)
+
+
+def paro_embed_grad(dout: int, dtype: int, ld_dout: int, tokens: int, token_dtype: int, n: int, first_token: int, scale: float,
+                    grad: int, grad_dtype: int, rows: int, dim: int, workspace: int, workspace_bytes: int, stream: int = 0) -> None:
+    _check(_lib.paro_embed_grad(dout, dtype, ld_dout, tokens, token_dtype, n, first_token, scale, grad, grad_dtype, rows, dim,
+                                workspace, workspace_bytes, stream))
+
+
+def make_distill(*, n, vocab, k, temperature, dtype, teacher_dtype, ld_logits=0, ld_teacher=0, ld_dlogits=0) -> paro_distill_t:
+    return paro_distill_t(n, vocab, k, ld_logits, ld_teacher, ld_dlogits, temperature, dtype, teacher_dtype, 0)
+
+
+def paro_distill_loss(d: paro_distill_t, logits: int, teacher: int, ids: int, loss: int, lse: int = 0, stream: int = 0) -> None:
+    _check(_lib.paro_distill_loss(byref(d), logits, teacher, ids, loss, lse, stream))
+
+
+def paro_distill_grad(d: paro_distill_t, logits: int, teacher: int, ids: int, lse: int, dloss: int, dlogits: int,
+                      stream: int = 0) -> None:
+    _check(_lib.paro_distill_grad(byref(d), logits, teacher, ids, lse, dloss, dlogits, stream))
+
+
+def paro_distill_step(d: paro_distill_t, logits: int, teacher: int, ids: int, dloss: int, loss: int, dlogits: int,
+                      stream: int = 0) -> None:
+    _check(_lib.paro_distill_step(byref(d), logits, teacher, ids, dloss, loss, dlogits, stream))
 
 
 # The device calls and make_adam, which a training program makes every step, take their usual arguments through

@@ -5,15 +5,17 @@ import hashlib
 import os
 import subprocess
 import sysconfig
+import tempfile
+from concurrent.futures import ThreadPoolExecutor
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(HERE)
 SO = os.path.join(HERE, "libparo.so")
-SOURCES = [os.path.join(HERE, "csrc", "plan.cpp"), os.path.join(HERE, "csrc", "kernels.hip")]
+SOURCES = [os.path.join(HERE, "csrc", f) for f in ("plan.cpp", "kernels.hip", "embed.hip", "distill.hip")]
 # the extension reads CPython's own structures: its name carries the interpreter that it was built for, so that no other loads it
 MARSHAL_SO = os.path.join(HERE, "_marshal" + sysconfig.get_config_var("EXT_SUFFIX"))
 MARSHAL_SOURCE = os.path.join(HERE, "csrc", "marshal.cpp")
-HEADERS = [os.path.join(HERE, "csrc", h) for h in ("plan.hpp", "device_util.hpp", "loaders.hpp")] + \
+HEADERS = [os.path.join(HERE, "csrc", h) for h in ("plan.hpp", "device_util.hpp", "loaders.hpp", "operators.hpp")] + \
           [os.path.join(ROOT, "include", "paro.h")]
 
 # -ffp-contract=off: every fp32 operation of the fold and of Adam is rounded on its own, so
@@ -59,11 +61,18 @@ def build(verbose: bool = False) -> str:
     hipcc = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
     if os.path.exists(STAMP):
         os.remove(STAMP)
-    for cmd in ([hipcc] + FLAGS + SOURCES + ["-o", SO],
-                [os.environ.get("CXX", "g++")] + MARSHAL_FLAGS + [MARSHAL_SOURCE, "-o", MARSHAL_SO]):
+
+    def run(cmd):
         if verbose:
-            print(" ".join(cmd))
+            print(" ".join(cmd), flush=True)
         subprocess.run(cmd, check=True)
+
+    with tempfile.TemporaryDirectory(prefix="paro_build_") as objects, ThreadPoolExecutor(max_workers=4) as pool:
+        compiled = [os.path.join(objects, os.path.basename(f) + ".o") for f in SOURCES]
+        jobs = [[hipcc] + [f for f in FLAGS if f != "-shared"] + ["-c", f, "-o", o] for f, o in zip(SOURCES, compiled)] + \
+               [[os.environ.get("CXX", "g++")] + MARSHAL_FLAGS + [MARSHAL_SOURCE, "-o", MARSHAL_SO]]
+        list(pool.map(run, jobs))
+        run([hipcc, "--offload-arch=gfx950", "-shared", "-fPIC"] + compiled + ["-o", SO])
     with open(STAMP, "w") as fh:
         fh.write(source_hash() + "\n")
     return SO
