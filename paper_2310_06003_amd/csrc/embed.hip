@@ -60,12 +60,16 @@ __global__ __launch_bounds__(THREADS) void k_embed(const void *table, const Toke
 }
 
 // ---------------------------------------------------------------- tokens sorted by row, in order
-// A block takes SORT_ROWS rows of the table and reads all tokens: its sixteen waves take consecutive parts of them, count
-// theirs for each row in counters of their own, and - after a scan over rows and waves - write them to their places in a second
-// walk.  Tokens of one row keep their order, nothing is atomic, no block waits for another: one launch.
+// A block takes SORT_ROWS rows of the table and reads a slice of the tokens: its sixteen waves walk consecutive parts of it twice - to
+// count theirs for each row in counters of their own and, after a scan over rows, slices and waves, to write them to their places.
+// Tokens of one row keep their order, nothing is atomic, no block waits for another.  A wave collects its block's tokens, one in many, in
+// a ring and works on 64 at a time.  Up to SLICE tokens are one slice and one launch; of more, a launch before counts every slice's.
 constexpr int SORT_BITS = 9, SORT_ROWS = 1 << SORT_BITS, SORT_WAVES = 16, SORT_THREADS = 64 * SORT_WAVES;
+constexpr int SORT_RING = 128, SORT_AHEAD = 8;     // tokens a lane loads ahead
+constexpr int64_t SLICE = SORT_AHEAD * SORT_THREADS;  // 32768 tokens in one slice 30 us, in slices of 4096 25, of 8192 18
+constexpr int64_t MAX_SLICES = 16;
 
-// Lanes with the same value as this one, among `in`.
+// Lanes with the same row as this one, among `in`.
 __device__ __forceinline__ uint64_t same_row(int row, uint64_t in) {
 #pragma unroll
     for (int b = 0; b < SORT_BITS; ++b) {
@@ -75,63 +79,129 @@ __device__ __forceinline__ uint64_t same_row(int row, uint64_t in) {
     return in;
 }
 
-template <class Token>
-__global__ __launch_bounds__(SORT_THREADS) void k_sort_tokens(const Token *tokens, int64_t n, int64_t first, int64_t rows, int *start,
-                                                              int *order, int *row_at) {
+// The slices' counts: of each row [slices][rows], and of the tokens in rows before a block's [slices][blocks].
+struct SliceCounts {
+    int *of_row, *below;
+};
+
+template <class Token, bool COUNT>
+__global__ __launch_bounds__(SORT_THREADS) void k_sort_tokens(const Token *tokens, int64_t n, int64_t first, int64_t rows, int64_t slice,
+                                                              SliceCounts counts, int *start, int *order, int *row_at) {
     __shared__ int count[SORT_WAVES][SORT_ROWS];
-    __shared__ int scan[SORT_ROWS];
+    __shared__ int ring_row[SORT_WAVES][SORT_RING], ring_at[SORT_WAVES][SORT_RING];
+    __shared__ int wave_total[SORT_ROWS / 64];
     __shared__ int below_of[SORT_WAVES];
     const int w = wave_of(), lane = lane_of();
-    const int64_t lo = (int64_t)blockIdx.x * SORT_ROWS, hi = lo + SORT_ROWS < rows ? lo + SORT_ROWS : rows;
-    const int64_t part = (n + SORT_THREADS - 1) / SORT_THREADS * 64;
-    const int64_t begin = w * part, end = begin + part < n ? begin + part : n;
-    for (int r = threadIdx.x; r < SORT_WAVES * SORT_ROWS; r += SORT_THREADS) (&count[0][0])[r] = 0;
-    __syncthreads();
-
+    const int64_t lo = (int64_t)blockIdx.x * SORT_ROWS;
+    const int in_range = (int)(lo + SORT_ROWS < rows ? SORT_ROWS : rows - lo);
+    const int64_t from_token = blockIdx.y * slice, to_token = from_token + slice < n ? from_token + slice : n;
+    const int64_t part = (slice + SORT_THREADS - 1) / SORT_THREADS * 64;
+    const int64_t begin = from_token + w * part, end = begin + part < to_token ? begin + part : to_token;
     const uint64_t before = ((uint64_t)1 << lane) - 1;
-    int below = 0;
+
+    // visit(row, i, place) for the tokens of the block's rows, in order; place counts on from what the wave's counter of the row holds.
+    // Returns how many tokens lie in rows before the block's.
     const auto walk = [&](auto &&visit) {
-        for (int64_t i0 = begin; i0 < end; i0 += 256) {          // four loads in flight
-            int64_t r[4];
-#pragma unroll
-            for (int u = 0; u < 4; ++u) {
-                const int64_t i = i0 + u * 64 + lane;
-                r[u] = i < end ? row_of(tokens, i, first, rows) : -1;
+        int below = 0, held = 0, head = 0;
+        const auto number = [&](int of) {
+            __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+            const int row = ring_row[w][(head + lane) & (SORT_RING - 1)], at = ring_at[w][(head + lane) & (SORT_RING - 1)];
+            const uint64_t same = same_row(row, of == 64 ? ~(uint64_t)0 : ((uint64_t)1 << of) - 1);
+            if (lane < of) {
+                const int place = count[w][row], rank = __popcll(same & before);
+                if (rank == 0) count[w][row] = place + __popcll(same);
+                visit(row, at, place + rank);
             }
+            head += of;
+            held -= of;
+        };
+        uint64_t next[SORT_AHEAD];
+        const auto load = [&](int64_t from) {
 #pragma unroll
-            for (int u = 0; u < 4; ++u) visit(i0 + u * 64 + lane, r[u]);
+            for (int u = 0; u < SORT_AHEAD; ++u) {
+                const int64_t i = from + u * 64 + lane;
+                next[u] = i < end ? (uint64_t)(int64_t)tokens[i] - (uint64_t)first : ~(uint64_t)0;
+            }
+        };
+        load(begin);
+        for (int64_t from = begin; from < end; from += SORT_AHEAD * 64) {
+            uint64_t now[SORT_AHEAD];
+#pragma unroll
+            for (int u = 0; u < SORT_AHEAD; ++u) now[u] = next[u];
+            load(from + SORT_AHEAD * 64);
+#pragma unroll
+            for (int u = 0; u < SORT_AHEAD; ++u) {
+                below += __popcll(__ballot(now[u] < (uint64_t)lo));
+                const bool mine = now[u] - (uint64_t)lo < (uint64_t)in_range;
+                const uint64_t in = __ballot(mine);
+                if (!in) continue;
+                if (mine) {
+                    const int to = (head + held + __popcll(in & before)) & (SORT_RING - 1);
+                    ring_row[w][to] = (int)(now[u] - (uint64_t)lo);
+                    ring_at[w][to] = (int)(from + u * 64 + lane);
+                }
+                held += __popcll(in);
+                if (held >= 64) number(64);
+            }
         }
+        if (held) number(held);
+        return below;
     };
-    walk([&](int64_t, int64_t r) {
-        below += __popcll(__ballot(r >= 0 && r < lo));
-        const uint64_t in = __ballot(r >= lo && r < hi);
-        if (!in) return;
-        const int row = (int)(r - lo) & (SORT_ROWS - 1);
-        const uint64_t same = same_row(row, in);
-        if (r >= lo && r < hi && !(same & before)) count[w][row] += __popcll(same);
-    });
+
+    for (int r = lane; r < SORT_ROWS; r += 64) count[w][r] = 0;
+    const int below = walk([](int, int, int) {});
     if (lane == 0) below_of[w] = below;
     __syncthreads();
 
-    int base = 0;
-    for (int k = 0; k < SORT_WAVES; ++k) base += below_of[k];
-    int total = 0;
+    // The row of each of the first threads: tokens before it in the block's range, then where each wave's begin.
     const int mine = threadIdx.x;
+    int total = 0, sum = 0, before_slice = 0;
     if (mine < SORT_ROWS) {
+#pragma unroll
         for (int k = 0; k < SORT_WAVES; ++k) total += count[k][mine];
-        scan[mine] = total;
+        if constexpr (COUNT) {
+            if (mine < in_range) counts.of_row[blockIdx.y * rows + lo + mine] = total;
+            if (mine == 0) {
+                int all = 0;
+                for (int k = 0; k < SORT_WAVES; ++k) all += below_of[k];
+                counts.below[blockIdx.y * gridDim.x + blockIdx.x] = all;
+            }
+            return;
+        }
+        if (gridDim.y > 1) {
+            total = 0;
+            if (mine < in_range)
+                for (unsigned s = 0; s < gridDim.y; ++s) {
+                    const int c = counts.of_row[s * rows + lo + mine];
+                    total += c;
+                    if (s < blockIdx.y) before_slice += c;
+                }
+        }
+        sum = total;
+#pragma unroll
+        for (int step = 1; step < 64; step *= 2) {
+            const int other = __shfl_up(sum, step);
+            if (lane >= step) sum += other;
+        }
+        if (lane == 63) wave_total[w] = sum;
     }
+    if constexpr (COUNT) return;
     __syncthreads();
-    for (int step = 1; step < SORT_ROWS; step *= 2) {
-        const int other = mine < SORT_ROWS && mine >= step ? scan[mine - step] : 0;
-        __syncthreads();
-        if (mine < SORT_ROWS) scan[mine] += other;
-        __syncthreads();
-    }
     if (mine < SORT_ROWS) {
-        int at = base + scan[mine] - total;
-        if (lo + mine < hi) start[lo + mine] = at;
-        if (lo + mine == rows - 1) start[rows] = at + total;
+        int at = sum - total;
+        for (int k = 0; k < w; ++k) at += wave_total[k];
+        if (gridDim.y > 1) {
+            for (unsigned s = 0; s < gridDim.y; ++s) at += counts.below[s * gridDim.x + blockIdx.x];
+        } else {
+#pragma unroll
+            for (int k = 0; k < SORT_WAVES; ++k) at += below_of[k];
+        }
+        if (blockIdx.y == 0 && mine < in_range) {
+            start[lo + mine] = at;
+            if (lo + mine == rows - 1) start[rows] = at + total;
+        }
+        at += before_slice;
+#pragma unroll
         for (int k = 0; k < SORT_WAVES; ++k) {
             const int c = count[k][mine];
             count[k][mine] = at;
@@ -140,123 +210,149 @@ __global__ __launch_bounds__(SORT_THREADS) void k_sort_tokens(const Token *token
     }
     __syncthreads();
 
-    walk([&](int64_t i, int64_t r) {
-        const uint64_t in = __ballot(r >= lo && r < hi);
-        if (!in) return;
-        const int row = (int)(r - lo) & (SORT_ROWS - 1);
-        const uint64_t same = same_row(row, in);
-        if (r >= lo && r < hi) {
-            const int at = count[w][row], rank = __popcll(same & before);
-            order[at + rank] = (int)i;
-            row_at[at + rank] = (int)r;
-            if (rank == 0) count[w][row] = at + __popcll(same);
-        }
+    walk([&](int row, int i, int place) {
+        order[place] = i;
+        row_at[place] = (int)lo + row;
     });
 }
 
 // ---------------------------------------------------------------- sums over the sorted tokens
+// What a lane loads of a row of dout: as many elements as a piece of the gradient has, so that every store instruction of a wave covers
+// whole cache lines (fp32 gradients of two-byte rows in pieces of dout, 32 bytes a lane: GPT-2's table 56 us, so 40).
+template <int DT, int GT>
+struct RowPiece {
+    static constexpr int N = Elem<GT>::E;
+    static constexpr bool HALF = N < Elem<DT>::E;
+    u32x4 raw;
+    __device__ __forceinline__ void load(const void *dout, int64_t elem) {
+        if constexpr (HALF) {
+            const u32x2 r = load_half_piece_stream(dout, elem);
+            raw[0] = r[0];
+            raw[1] = r[1];
+        } else {
+            raw = load_stream<DT>(dout, elem);
+        }
+    }
+    __device__ __forceinline__ void add_to(float (&acc)[N]) const {
+        float x[Elem<DT>::E];
+        unpack<DT>(raw, x);
+#pragma unroll
+        for (int j = 0; j < N; ++j) acc[j] += x[j];
+    }
+};
+
 // acc += dout[order[a .. b)], in order, for the lane's pieces of a tile of columns.
-template <int DT, int C>
-__device__ __forceinline__ void add_rows(float (&acc)[C][Elem<DT>::E], const void *dout, int64_t ld, const int *order, int a, int b,
+template <int DT, int GT, int C>
+__device__ __forceinline__ void add_rows(float (&acc)[C][Elem<GT>::E], const void *dout, int64_t ld, const int *order, int a, int b,
                                          const int64_t (&col)[C], int64_t dim) {
-    constexpr int E = Elem<DT>::E, U = 4;
+    constexpr int U = C >= 8 ? 1 : 8 / C;           // 8 loads in flight
     for (int k = a; k < b; k += U) {
-        u32x4 raw[U][C];
+        RowPiece<DT, GT> piece[U][C];
 #pragma unroll
         for (int u = 0; u < U; ++u) {
             const int64_t row = (int64_t)order[k + u < b ? k + u : b - 1] * ld;
 #pragma unroll
             for (int c = 0; c < C; ++c)
-                if (k + u < b && col[c] < dim) raw[u][c] = load_piece<DT>(dout, row + col[c]);
+                if (k + u < b && col[c] < dim) piece[u][c].load(dout, row + col[c]);
         }
 #pragma unroll
         for (int u = 0; u < U; ++u)
 #pragma unroll
             for (int c = 0; c < C; ++c)
-                if (k + u < b && col[c] < dim) {
-                    float x[E];
-                    unpack<DT>(raw[u][c], x);
-#pragma unroll
-                    for (int j = 0; j < E; ++j) acc[c][j] += x[j];
-                }
+                if (k + u < b && col[c] < dim) piece[u][c].add_to(acc[c]);
     }
 }
 
 // Columns of a lane's pieces; the last piece of a row starts early, past the row: dim.
 template <int E, int C>
-__device__ __forceinline__ void columns(int64_t (&col)[C], int64_t tile, int64_t dim) {
+__device__ __forceinline__ void columns(int64_t (&col)[C], int64_t dim) {
 #pragma unroll
     for (int c = 0; c < C; ++c) {
-        const int64_t e = tile * (64 * C * E) + c * 64 * E + lane_of() * E;
+        const int64_t e = (int64_t)blockIdx.y * (64 * C * E) + c * 64 * E + lane_of() * E;
         col[c] = e >= dim ? dim : e < dim - E ? e : dim - E;
     }
 }
 
-// Runs of more than `seg` tokens are summed segment by segment of the sorted order, in parallel.  Of one segment such a run
-// holds the beginning (slot 0), or the end and not the beginning (slot 1).
-template <int DT, int C>
-__global__ __launch_bounds__(THREADS) void k_segment_sums(const void *dout, int64_t ld, const int *start, const int *order, const int *row_at,
-                                                          int64_t rows, int64_t dim, int seg, float *partial) {
-    constexpr int E = Elem<DT>::E;
-    const int64_t s = (int64_t)blockIdx.x * WAVES + wave_of();
-    const int held = start[rows], a = (int)(s * seg), b = a + seg < held ? a + seg : held;
-    if (a >= b) return;
-    int64_t col[C];
-    columns<E>(col, blockIdx.y, dim);
-    const int rows_of[2] = {row_at[a], row_at[b - 1]};
-    for (int slot = 0; slot < 2; ++slot) {
-        if (slot == 1 && rows_of[1] == rows_of[0]) break;
-        const int from = start[rows_of[slot]], to = start[rows_of[slot] + 1];
-        if (to - from <= seg) continue;
-        float acc[C][E] = {};
-        add_rows<DT>(acc, dout, ld, order, from > a ? from : a, to < b ? to : b, col, dim);
+template <int GT, int C>
+__device__ __forceinline__ void store_row(float (&acc)[C][Elem<GT>::E], void *grad, int64_t v, const int64_t (&col)[C], int64_t dim, float scale) {
 #pragma unroll
-        for (int c = 0; c < C; ++c)
-            if (col[c] < dim)
+    for (int c = 0; c < C; ++c) {
+        if (col[c] >= dim) continue;
 #pragma unroll
-                for (int j = 0; j < E; j += 4)
-                    store_piece<PARO_F32>(partial, (2 * s + slot) * dim + col[c] + j, pack<PARO_F32>(&acc[c][j]));
+        for (int j = 0; j < Elem<GT>::E; ++j) acc[c][j] *= scale;
+        store_stream<GT>(grad, v * dim + col[c], pack<GT>(acc[c]));
     }
 }
 
-// A wave writes a tile of a row of the table's gradient: of a short run its tokens' sum, of a long one its segments', and
-// zeros where no token is.
+// A wave of the first blocks takes a segment of the sorted tokens: runs of more than `seg` are summed segment by segment, in parallel.
+// Of one segment such a run holds the beginning (slot 0), or the end and not the beginning (slot 1).  A wave of the others takes a
+// row of the table's gradient: it writes a short run's sum, or zeros where no token is.
 template <int DT, int GT, int C>
-__global__ __launch_bounds__(THREADS) void k_row_sums(const void *dout, int64_t ld, const int *start, const int *order, int64_t rows,
-                                                      int64_t dim, int seg, const float *partial, float scale, void *grad) {
-    constexpr int E = Elem<DT>::E, G = Elem<GT>::E;
-    static_assert(G <= E, "the gradient is at least as wide as what is summed");
-    for (int64_t v = (int64_t)blockIdx.x * WAVES + wave_of(); v < rows; v += (int64_t)gridDim.x * WAVES) {
-        const int a = start[v], b = start[v + 1];
-        int64_t col[C];
-        columns<E>(col, blockIdx.y, dim);
-        float acc[C][E] = {};
-        if (b - a <= seg) {
-            add_rows<DT>(acc, dout, ld, order, a, b, col, dim);
-        } else {
-            for (int64_t s = a / seg; s * seg < b; ++s) {
-                const int slot = s * seg < a ? 1 : 0;
+__global__ __launch_bounds__(THREADS) void k_sums(const void *dout, int64_t ld, const int *start, const int *order, const int *row_at, int64_t rows,
+                                                  int64_t dim, int seg, unsigned seg_blocks, float scale, float *partial, void *grad) {
+    constexpr int E = Elem<GT>::E;
+    int64_t col[C];
+    columns<E>(col, dim);
+    if (blockIdx.x < seg_blocks) {
+        const int64_t s = (int64_t)blockIdx.x * WAVES + wave_of();
+        const int held = start[rows], a = (int)(s * seg), b = a + seg < held ? a + seg : held;
+        if (a >= b) return;
+        const int rows_of[2] = {row_at[a], row_at[b - 1]};
+        for (int slot = 0; slot < 2; ++slot) {
+            if (slot == 1 && rows_of[1] == rows_of[0]) break;
+            const int from = start[rows_of[slot]], to = start[rows_of[slot] + 1];
+            if (to - from <= seg) continue;
+            float acc[C][E] = {};
+            add_rows<DT, GT>(acc, dout, ld, order, from > a ? from : a, to < b ? to : b, col, dim);
 #pragma unroll
-                for (int c = 0; c < C; ++c)
-                    if (col[c] < dim)
+            for (int c = 0; c < C; ++c)
+                if (col[c] < dim)
 #pragma unroll
-                        for (int j = 0; j < E; j += 4) {
-                            float x[4];
-                            unpack<PARO_F32>(load_piece<PARO_F32>(partial, (2 * s + slot) * dim + col[c] + j), x);
-#pragma unroll
-                            for (int q = 0; q < 4; ++q) acc[c][j + q] += x[q];
-                        }
-            }
+                    for (int j = 0; j < E; j += 4) store_piece<PARO_F32>(partial, (2 * s + slot) * dim + col[c] + j, pack<PARO_F32>(&acc[c][j]));
         }
-#pragma unroll
-        for (int c = 0; c < C; ++c) {
-            if (col[c] >= dim) continue;
-#pragma unroll
-            for (int j = 0; j < E; ++j) acc[c][j] *= scale;
-#pragma unroll
-            for (int j = 0; j < E; j += G) store_piece<GT>(grad, v * dim + col[c] + j, pack<GT>(&acc[c][j]));
-        }
+        return;
     }
+    for (int64_t v = (int64_t)(blockIdx.x - seg_blocks) * WAVES + wave_of(); v < rows; v += (int64_t)(gridDim.x - seg_blocks) * WAVES) {
+        const int a = start[v], b = start[v + 1];
+        if (b - a > seg) continue;
+        float acc[C][E] = {};
+        add_rows<DT, GT>(acc, dout, ld, order, a, b, col, dim);
+        store_row<GT>(acc, grad, v, col, dim, scale);
+    }
+}
+
+// A wave adds up the segments of the long run that begins in its segment, if one does: the last one there.
+template <int GT>
+__global__ __launch_bounds__(THREADS) void k_join(const int *start, const int *row_at, int64_t rows, int64_t dim, int seg, float scale,
+                                                  const float *partial, void *grad) {
+    constexpr int E = Elem<GT>::E, U = 8;
+    int64_t col[1];
+    columns<E>(col, dim);
+    const int64_t s0 = (int64_t)blockIdx.x * WAVES + wave_of();
+    const int held = start[rows], a = (int)(s0 * seg), end = a + seg < held ? a + seg : held;
+    if (a >= end) return;
+    const int v = row_at[end - 1], from = start[v], to = start[v + 1];
+    if (from < a || to - from <= seg || col[0] >= dim) return;
+    float acc[1][E] = {};
+    for (int64_t s = s0; s * seg < to; s += U) {
+        u32x4 raw[U][E / 4];
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+#pragma unroll
+            for (int j = 0; j < E / 4; ++j)
+                if ((s + u) * seg < to) raw[u][j] = load_piece<PARO_F32>(partial, (2 * (s + u) + ((s + u) * seg < from ? 1 : 0)) * dim + col[0] + 4 * j);
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+#pragma unroll
+            for (int j = 0; j < E / 4; ++j)
+                if ((s + u) * seg < to) {
+                    float x[4];
+                    unpack<PARO_F32>(raw[u][j], x);
+#pragma unroll
+                    for (int q = 0; q < 4; ++q) acc[0][4 * j + q] += x[q];
+                }
+    }
+    store_row<GT>(acc, grad, v, col, dim, scale);
 }
 
 // Rows narrower than a piece: a thread for each element.
@@ -266,6 +362,7 @@ __global__ __launch_bounds__(THREADS) void k_narrow_sums(const void *dout, int64
     for (int64_t e = (int64_t)blockIdx.x * THREADS + threadIdx.x; e < rows * dim; e += (int64_t)gridDim.x * THREADS) {
         const int64_t v = e / dim, c = e - v * dim;
         float sum = 0.0f;
+#pragma unroll 4
         for (int k = start[v]; k < start[v + 1]; ++k) sum += load_one<DT>(dout, order[k] * ld + c);
         store_one<GT>(grad, e, sum * scale);
     }
@@ -278,25 +375,33 @@ dim3 grid_for(int64_t rows, int64_t tiles) {
     return dim3((unsigned)std::max<int64_t>(1, std::min(MAX_BLOCKS / tiles, ceil_div(rows, WAVES))), (unsigned)tiles);
 }
 
-// Tokens of a segment: what a long run's parts and their number cost in a row are alike near the square root.
+// Tokens of a segment: short, so that many waves share a long run; and no more than MAX_SEGMENTS, which one wave adds up where all
+// tokens are of one row.
+constexpr int64_t MAX_SEGMENTS = 2048;
 int segment_of(int64_t n) {
-    int seg = 64;
-    while ((int64_t)seg * seg < n) seg *= 2;
+    int seg = 32;
+    while (n / seg > MAX_SEGMENTS) seg *= 2;
     return seg;
 }
-constexpr int GRAD_PIECES = 2;           // pieces a lane of the gradient's kernels
+constexpr int GRAD_PIECES = 4;           // pieces a lane of the sums: 32768 tokens of 4096, 139 us with one, 133 with two, 114
+
+// Tokens of a slice of the sort.
+int64_t slice_of(int64_t n) { return std::max(SLICE, ceil_div(ceil_div(n, MAX_SLICES), SORT_THREADS) * SORT_THREADS); }
 
 struct GradRoom {                        // parts of the workspace, in bytes
-    int64_t start, order, row_at, partial, all;
+    int64_t start, order, row_at, of_row, below, partial, all;
 };
 GradRoom grad_room(int64_t n, int64_t rows, int64_t dim) {
     const auto up = [](int64_t x) { return (x + 255) / 256 * 256; };
+    const int64_t slices = n > SLICE ? ceil_div(n, slice_of(n)) : 0;
     GradRoom g;
     g.start = 0;
     g.order = up((rows + 1) * 4);
     g.row_at = g.order + up(n * 4);
-    g.partial = g.row_at + up(n * 4);
-    g.all = g.partial + up(2 * ceil_div(n, segment_of(n)) * dim * 4);
+    g.of_row = g.row_at + up(n * 4);
+    g.below = g.of_row + up(slices * rows * 4);
+    g.partial = g.below + up(slices * ceil_div(rows, SORT_ROWS) * 4);
+    g.all = g.partial + (n > segment_of(n) ? up(2 * ceil_div(n, segment_of(n)) * dim * 4) : 0);
     return g;
 }
 
@@ -327,14 +432,16 @@ void launch_sums(const void *dout, int64_t ld, int64_t n, float scale, void *gra
                            ld, start, order, rows, dim, scale, grad);
         return;
     }
-    const int seg = segment_of(n);
-    const int64_t tiles = ceil_div(dim, 64 * GRAD_PIECES * Elem<DT>::E);
+    const int seg = segment_of(n), *row_at = reinterpret_cast<int *>(ws + g.row_at);
     float *partial = reinterpret_cast<float *>(ws + g.partial);
-    if (n > seg)
-        hipLaunchKernelGGL((k_segment_sums<DT, GRAD_PIECES>), dim3((unsigned)ceil_div(ceil_div(n, seg), WAVES), (unsigned)tiles), dim3(THREADS), 0,
-                           st, dout, ld, start, order, reinterpret_cast<int *>(ws + g.row_at), rows, dim, seg, partial);
-    hipLaunchKernelGGL((k_row_sums<DT, GT, GRAD_PIECES>), grid_for(rows, tiles), dim3(THREADS), 0, st, dout, ld, start, order, rows, dim, seg,
-                       partial, scale, grad);
+    const unsigned seg_blocks = n > seg ? (unsigned)ceil_div(ceil_div(n, seg), WAVES) : 0;
+    dim3 grid = grid_for(rows, ceil_div(dim, 64 * GRAD_PIECES * Elem<GT>::E));
+    grid.x += seg_blocks;
+    hipLaunchKernelGGL((k_sums<DT, GT, GRAD_PIECES>), grid, dim3(THREADS), 0, st, dout, ld, start, order, row_at, rows, dim, seg, seg_blocks, scale,
+                       partial, grad);
+    if (seg_blocks)
+        hipLaunchKernelGGL((k_join<GT>), dim3(seg_blocks, (unsigned)ceil_div(dim, 64 * Elem<GT>::E)), dim3(THREADS), 0, st, start, row_at, rows, dim, seg,
+                           scale, partial, grad);
 }
 
 }  // namespace
@@ -400,13 +507,20 @@ int paro_embed_grad(const void *dout, int dtype, int64_t ld_dout, const void *to
         char *ws = static_cast<char *>(workspace);
         int *start = reinterpret_cast<int *>(ws + g.start), *order = reinterpret_cast<int *>(ws + g.order);
         int *row_at = reinterpret_cast<int *>(ws + g.row_at);
-        const dim3 sort_grid((unsigned)ceil_div(rows, SORT_ROWS));
-        if (token_dtype == PARO_I64)
-            hipLaunchKernelGGL((k_sort_tokens<int64_t>), sort_grid, dim3(SORT_THREADS), 0, st, static_cast<const int64_t *>(tokens), n, first_token,
-                               rows, start, order, row_at);
-        else
-            hipLaunchKernelGGL((k_sort_tokens<int32_t>), sort_grid, dim3(SORT_THREADS), 0, st, static_cast<const int32_t *>(tokens), n, first_token,
-                               rows, start, order, row_at);
+        const int64_t slice = slice_of(n);
+        const dim3 sort_grid((unsigned)ceil_div(rows, SORT_ROWS), (unsigned)std::max<int64_t>(1, ceil_div(n, slice)));
+        const SliceCounts counts{reinterpret_cast<int *>(ws + g.of_row), reinterpret_cast<int *>(ws + g.below)};
+#define PARO_SORT(TOKEN, COUNT)                                                                                                        \
+    hipLaunchKernelGGL((k_sort_tokens<TOKEN, COUNT>), sort_grid, dim3(SORT_THREADS), 0, st, static_cast<const TOKEN *>(tokens), n, first_token, \
+                       rows, slice, counts, start, order, row_at)
+        if (token_dtype == PARO_I64) {
+            if (sort_grid.y > 1) PARO_SORT(int64_t, true);
+            PARO_SORT(int64_t, false);
+        } else {
+            if (sort_grid.y > 1) PARO_SORT(int32_t, true);
+            PARO_SORT(int32_t, false);
+        }
+#undef PARO_SORT
         PARO_LAUNCHED("paro_embed_grad");
 #define PARO_SUMS(DT, GT) launch_sums<DT, GT>(dout, ld_dout, n, scale, grad, rows, dim, ws, g, st)
         if (dtype == PARO_F32) PARO_SUMS(PARO_F32, PARO_F32);

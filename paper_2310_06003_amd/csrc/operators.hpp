@@ -112,6 +112,25 @@ __device__ __forceinline__ void store_piece(void *base, int64_t elem, u32x4 v) {
     if constexpr (DT == PARO_F32) *reinterpret_cast<piece_at4 *>(at) = v;
     else *reinterpret_cast<piece_at2 *>(at) = v;
 }
+// ... of what is touched once and larger than the caches.
+template <int DT>
+__device__ __forceinline__ u32x4 load_stream(const void *base, int64_t elem) {
+    const char *at = static_cast<const char *>(base) + elem * Elem<DT>::BYTES;
+    if constexpr (DT == PARO_F32) return __builtin_nontemporal_load(reinterpret_cast<const piece_at4 *>(at));
+    else return __builtin_nontemporal_load(reinterpret_cast<const piece_at2 *>(at));
+}
+template <int DT>
+__device__ __forceinline__ void store_stream(void *base, int64_t elem, u32x4 v) {
+    char *at = static_cast<char *>(base) + elem * Elem<DT>::BYTES;
+    if constexpr (DT == PARO_F32) __builtin_nontemporal_store(v, reinterpret_cast<piece_at4 *>(at));
+    else __builtin_nontemporal_store(v, reinterpret_cast<piece_at2 *>(at));
+}
+// Four elements of a two-byte type.
+typedef unsigned int u32x2 __attribute__((ext_vector_type(2)));
+typedef u32x2 half_piece_at2 __attribute__((aligned(2)));
+__device__ __forceinline__ u32x2 load_half_piece_stream(const void *base, int64_t elem) {
+    return __builtin_nontemporal_load(reinterpret_cast<const half_piece_at2 *>(static_cast<const char *>(base) + elem * 2));
+}
 template <int DT>
 __device__ __forceinline__ float load_one(const void *base, int64_t elem) {
     if constexpr (DT == PARO_F32) return static_cast<const float *>(base)[elem];
