@@ -382,6 +382,26 @@ int paro_distill_grad(const paro_distill_t *d, const void *logits, const void *t
 int paro_distill_step(const paro_distill_t *d, const void *logits, const void *teacher, const int32_t *ids,
                       const float *dloss, float *loss, void *dlogits, void *stream);
 
+/* The gated projections of a feed-forward block (the product that follows, with the down projection, is a plain one):
+ *   g = x Wg', u = x Wu', h = act(g) * u        act: silu(g) = g / (1 + exp(-g)), or gelu(g) = g/2 (1 + erf(g / sqrt 2))
+ * x: [n][dim], ld_x apart; Wg, Wu: [hidden][dim]; h, g, u: [n][hidden], ld_h apart.  dtype: PARO_BF16 or PARO_F16.  g and u are
+ * stored for the backward pass, or NULL both; h is formed from their fp32 values.  n == 0 is nothing to do. */
+enum { PARO_SILU = 0, PARO_GELU = 1 };
+typedef struct {
+    int64_t n, dim, hidden;
+    int64_t ld_x, ld_h;         /* elements from row to row, 0 = dense */
+    int32_t dtype, act;
+} paro_gated_t;
+int64_t paro_gated_workspace(const paro_gated_t *d, int grad); /* bytes: of paro_gated, or of paro_gated_grad */
+int paro_gated(const paro_gated_t *d, const void *x, const void *w_gate, const void *w_up, void *h, void *gate, void *up,
+               void *workspace, int64_t workspace_bytes, void *stream);
+/* From dh (as h) and the stored projections: dg = dh * u * act'(g), du = dh * act(g), each rounded to dtype - what the
+ * matrix cores take - and
+ *   dx = dg Wg + du Wu  (as x),   dWg = dg' x,   dWu = du' x  (dense; zeros for n == 0). */
+int paro_gated_grad(const paro_gated_t *d, const void *dh, const void *gate, const void *up, const void *x,
+                    const void *w_gate, const void *w_up, void *dx, void *dw_gate, void *dw_up, void *workspace,
+                    int64_t workspace_bytes, void *stream);
+
 /* text of the calling thread's last error ("" if none); valid until that
  * thread's next failing call */
 const char *paro_last_error(void);

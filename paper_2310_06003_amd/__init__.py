@@ -33,6 +33,7 @@ PARO_MAX_RANKS = 256
 PARO_STATIC_MAX_CHUNK = 1 << 30
 PARO_I32, PARO_I64 = 8, 9
 PARO_DISTILL_MAX_K = 1024
+PARO_SILU, PARO_GELU = 0, 1
 
 for _f in (_SO, os.path.join(_HERE, "_marshal" + sysconfig.get_config_var("EXT_SUFFIX"))):
     if not os.path.exists(_f):
@@ -82,6 +83,11 @@ class paro_distill_t(Structure):
                 ("reserved_", c_int32)]
 
 
+class paro_gated_t(Structure):
+    _fields_ = [("n", c_int64), ("dim", c_int64), ("hidden", c_int64), ("ld_x", c_int64), ("ld_h", c_int64), ("dtype", c_int32),
+                ("act", c_int32)]
+
+
 EXPORTS = {
     "paro_strategy_legal": (c_int, [c_char_p]),
     "paro_plan": (c_int, [c_int, c_int, c_char_p, POINTER(c_int64), c_int64, POINTER(paro_plan_opts_t),
@@ -119,6 +125,9 @@ EXPORTS = {
     "paro_distill_loss": (c_int, [POINTER(paro_distill_t)] + [c_void_p] * 6),
     "paro_distill_grad": (c_int, [POINTER(paro_distill_t)] + [c_void_p] * 7),
     "paro_distill_step": (c_int, [POINTER(paro_distill_t)] + [c_void_p] * 7),
+    "paro_gated_workspace": (c_int64, [POINTER(paro_gated_t), c_int]),
+    "paro_gated": (c_int, [POINTER(paro_gated_t)] + [c_void_p] * 7 + [c_int64, c_void_p]),
+    "paro_gated_grad": (c_int, [POINTER(paro_gated_t)] + [c_void_p] * 10 + [c_int64, c_void_p]),
     "paro_last_error": (c_char_p, []),
 }
 for _name, (_res, _args) in EXPORTS.items():
@@ -330,6 +339,26 @@ def paro_distill_grad(d: paro_distill_t, logits: int, teacher: int, ids: int, ls
 def paro_distill_step(d: paro_distill_t, logits: int, teacher: int, ids: int, dloss: int, loss: int, dlogits: int,
                       stream: int = 0) -> None:
     _check(_lib.paro_distill_step(byref(d), logits, teacher, ids, dloss, loss, dlogits, stream))
+
+
+def make_gated(*, n, dim, hidden, dtype, act=PARO_SILU, ld_x=0, ld_h=0) -> paro_gated_t:
+    return paro_gated_t(n, dim, hidden, ld_x, ld_h, dtype, act)
+
+
+def paro_gated_workspace(d: paro_gated_t, grad: bool) -> int:
+    """Bytes."""
+    rc = _lib.paro_gated_workspace(byref(d), 1 if grad else 0)
+    return rc if rc >= 0 else _check(rc)
+
+
+def paro_gated(d: paro_gated_t, x: int, w_gate: int, w_up: int, h: int, gate: int, up: int, workspace: int, workspace_bytes: int,
+               stream: int = 0) -> None:
+    _check(_lib.paro_gated(byref(d), x, w_gate, w_up, h, gate, up, workspace, workspace_bytes, stream))
+
+
+def paro_gated_grad(d: paro_gated_t, dh: int, gate: int, up: int, x: int, w_gate: int, w_up: int, dx: int, dw_gate: int, dw_up: int,
+                    workspace: int, workspace_bytes: int, stream: int = 0) -> None:
+    _check(_lib.paro_gated_grad(byref(d), dh, gate, up, x, w_gate, w_up, dx, dw_gate, dw_up, workspace, workspace_bytes, stream))
 
 
 # The device calls and make_adam, which a training program makes every step, take their usual arguments through

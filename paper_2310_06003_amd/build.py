@@ -11,7 +11,7 @@ from concurrent.futures import ThreadPoolExecutor
 HERE = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(HERE)
 SO = os.path.join(HERE, "libparo.so")
-SOURCES = [os.path.join(HERE, "csrc", f) for f in ("plan.cpp", "kernels.hip", "embed.hip", "distill.hip")]
+SOURCES = [os.path.join(HERE, "csrc", f) for f in ("plan.cpp", "kernels.hip", "embed.hip", "distill.hip", "gated.hip")]
 # the extension reads CPython's own structures: its name carries the interpreter that it was built for, so that no other loads it
 MARSHAL_SO = os.path.join(HERE, "_marshal" + sysconfig.get_config_var("EXT_SUFFIX"))
 MARSHAL_SOURCE = os.path.join(HERE, "csrc", "marshal.cpp")

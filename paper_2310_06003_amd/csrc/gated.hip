@@ -1,0 +1,634 @@
+// The gated projections of a feed-forward block and their gradient (gfx950):
+//
+//   g = x Wg',  u = x Wu',  h = act(g) * u
+//   dg = dh u act'(g),  du = dh act(g);   dx = dg Wg + du Wu,  dWg = dg' x,  dWu = du' x
+//
+// Bound by the matrix cores for many tokens, by reading the weights for few.  Three products of one kernel: a block computes
+// a tile of the result with 16x16x32 matrix instructions in fp32, its waves side by side on it, from two stages of 64 steps of the inner
+// dimension in shared memory that are filled past the registers.  Forward, a tile holds the gate's and the up projection's columns of
+// the same hidden elements, so that one wave has both and the activation and the product happen in its registers.
+// An operand whose inner dimension lies along memory (x, W forward; dg | du of dx) is read from shared memory in pieces of eight steps; one
+// whose inner dimension goes from row to row (W of dx; both of dW) is staged as it lies and transposed by the reading instruction.
+#include "operators.hpp"
+
+namespace {
+
+constexpr int STEPS = 64;                // of the inner dimension, a stage
+constexpr int ROW_BYTES = STEPS * 2;     // of an operand that lies along it
+enum { FORWARD = 0, INPUT_GRAD = 1, WEIGHT_GRAD = 2 };
+
+typedef short short4_t __attribute__((ext_vector_type(4)));
+typedef short short8_t __attribute__((ext_vector_type(8)));
+typedef __bf16 bf16x8_t __attribute__((ext_vector_type(8)));
+typedef _Float16 f16x8_t __attribute__((ext_vector_type(8)));
+typedef unsigned int u32x2_t __attribute__((ext_vector_type(2)));
+typedef __attribute__((address_space(3))) char lds_char;
+
+template <int DT>
+__device__ __forceinline__ f32x4 mfma(short8_t a, short8_t b, f32x4 c) {
+    if constexpr (DT == PARO_F16)
+        return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8_t, a), __builtin_bit_cast(f16x8_t, b), c, 0, 0, 0);
+    else
+        return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, a), __builtin_bit_cast(bf16x8_t, b), c, 0, 0, 0);
+}
+
+// The activation and its derivative.
+template <int ACT>
+__device__ __forceinline__ float act(float g) {
+    if constexpr (ACT == PARO_SILU) return g / (1.0f + __expf(-g));
+    else return 0.5f * g * (1.0f + erff(g * 0.70710678118654752440f));
+}
+template <int ACT>
+__device__ __forceinline__ void act_and_slope(float g, float &a, float &da) {
+    if constexpr (ACT == PARO_SILU) {
+        const float y = 1.0f / (1.0f + __expf(-g));
+        a = g * y;
+        da = y * (1.0f + g * (1.0f - y));
+    } else {
+        const float y = 0.5f * (1.0f + erff(g * 0.70710678118654752440f));
+        a = g * y;
+        da = y + g * __expf(-0.5f * g * g) * 0.39894228040143267794f;
+    }
+}
+
+__device__ __forceinline__ int wave_of() { return __builtin_amdgcn_readfirstlane(threadIdx.x >> 6); }
+
+// 16 bytes a lane from memory to shared memory at `to` + 16 * lane, past the registers; out of range: zeros.  In assembly because
+// the compiler, which cannot tell the stages apart, would wait for it before every read of shared memory; end_stage() waits.
+// There is no register that it writes.
+__device__ __forceinline__ void fill(u32x4 from, unsigned offset, unsigned to) {
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(to), "v"(offset), "s"(from) : "memory");
+}
+// All of the wave's fills have arrived, all its reads are done; then those of all waves.
+__device__ __forceinline__ void end_stage() { asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory"); }
+
+// A buffer descriptor of the bytes from `base` on; beyond them the hardware reads zeros.
+__device__ __forceinline__ u32x4 range(const char *base, int64_t bytes) {
+    const uint64_t at = (uint64_t)(uintptr_t)base;
+    return u32x4{(unsigned)at, (unsigned)(at >> 32) & 0xFFFFu, bytes < 0 ? 0u : bytes > 0x7FFFFFF0 ? 0x7FFFFFF0u : (unsigned)bytes, 0x00020000u};
+}
+constexpr unsigned NOWHERE = 0x80000000u;
+
+struct Product {
+    // Operand a: [rows][inner] (along) or [inner][rows] (across), operand b: [cols][inner] or [inner][cols].  Two parts: forward, the
+    // columns of b (gate, up); of dx, the inner dimension (of a the left and the right half, of b two matrices).
+    const char *a[2], *b[2];
+    int64_t lda, ldb;                    // bytes
+    int64_t rows, cols, inner;           // inner: of one part, in whole pieces where an operand lies along it
+    int64_t inner_b;                     // across: rows that b has
+    char *out[3];                        // h, g, u; dx; dWg, dWu
+    int64_t ldo;                         // elements
+    float *partial;                      // splits > 1: [split][rows][cols of all parts], fp32
+    int64_t ldp;
+    int tiles_m, tiles_n, splits;
+};
+
+// Which tile a block computes.  Blocks go to the eight XCDs in turn: each takes a run of tiles of its own, eight tiles of rows
+// wide, so that what its blocks read at a time stays in its L2.
+__device__ __forceinline__ void tile_of(unsigned block, int tiles_m, int tiles_n, int &tm, int &tn) {
+    const unsigned all = tiles_m * tiles_n, each = all / 8, more = all % 8, xcd = block % 8;
+    const unsigned t = xcd * each + (xcd < more ? xcd : more) + block / 8;
+    constexpr unsigned WIDE = 8;
+    const unsigned band = t / (WIDE * tiles_n), first = band * WIDE, in = t - band * WIDE * tiles_n;
+    const unsigned high = tiles_m - first < WIDE ? tiles_m - first : WIDE;
+    tm = first + in % high;
+    tn = in / high;
+}
+
+template <int DT, int MODE, int ACT, int BM, int BN, int WAVES_M, int WAVES_N>
+__global__ __launch_bounds__(64 * WAVES_M * WAVES_N) void k_product(Product p) {
+    constexpr int THREADS_ = 64 * WAVES_M * WAVES_N;
+    constexpr int TM = BM / WAVES_M / 16, TN = BN / WAVES_N / 16;             // 16x16 tiles of a wave
+    constexpr int A_BYTES = BM * ROW_BYTES, B_BYTES = BN * ROW_BYTES, STAGE = A_BYTES + B_BYTES;
+    constexpr int A_FILLS = A_BYTES / (THREADS_ * 16), B_FILLS = B_BYTES / (THREADS_ * 16);
+    constexpr bool A_ACROSS = MODE == WEIGHT_GRAD, B_ACROSS = MODE != FORWARD;
+    static_assert(TN == 4, "a wave's columns are two pairs of tiles");
+    extern __shared__ __attribute__((aligned(1024))) char stages[];
+    const unsigned lds0 = (unsigned)(uintptr_t)(lds_char *)stages;
+    const int w = wave_of(), lane = threadIdx.x & 63, wm = w / WAVES_N, wn = w % WAVES_N;
+    int tm, tn;
+    tile_of(blockIdx.x, p.tiles_m, p.tiles_n, tm, tn);
+    const int64_t m0 = (int64_t)tm * BM;
+
+    // The tile's operands: where they begin, and how many bytes from there may be read at step 0.
+    constexpr int HALF_N = BN / 2;
+    const int64_t n_tiles_part = MODE == WEIGHT_GRAD ? p.tiles_m / 2 : 0;     // dW: the first half of the tiles of rows is dWg
+    const int out_part = MODE == WEIGHT_GRAD ? tm >= n_tiles_part : 0;
+    const int64_t row0 = MODE == WEIGHT_GRAD ? m0 - out_part * n_tiles_part * BM : m0;
+    const int64_t col0 = (int64_t)tn * (MODE == FORWARD ? HALF_N : BN);
+    const int64_t rows_left = p.rows - row0 < BM ? p.rows - row0 : BM;
+
+    unsigned a_at[A_FILLS], b_at[B_FILLS];          // a lane's offsets from the operand's beginning
+    int a_step[A_FILLS], b_step[B_FILLS];           // along: the step that its piece begins with
+    const auto along = [&](int row, unsigned &at, int &step, int64_t memory_row, int64_t ld) {
+        const int piece = (lane & 7) ^ ((row >> 1) & 7);
+        at = (unsigned)(memory_row * ld) + piece * 16;
+        step = piece * 8;
+    };
+    const auto across = [&](int k, int piece, unsigned &at, int64_t ld) {
+        const int block = (piece >> 1) ^ ((k & 3) | ((k >> 1) & 4));
+        at = (unsigned)(k * ld) + (block * 2 + (piece & 1)) * 16;
+    };
+#pragma unroll
+    for (int i = 0; i < A_FILLS; ++i) {
+        if constexpr (A_ACROSS) {
+            constexpr int PIECES = BM / 8;
+            across((w * A_FILLS + i) * (64 / PIECES) + lane / PIECES, lane % PIECES, a_at[i], p.lda);
+        } else {
+            const int r = (w * A_FILLS + i) * 8 + lane / 8;
+            along(r, a_at[i], a_step[i], r, p.lda);
+        }
+    }
+#pragma unroll
+    for (int i = 0; i < B_FILLS; ++i) {
+        if constexpr (B_ACROSS) {
+            constexpr int PIECES = BN / 8;
+            across((w * B_FILLS + i) * (64 / PIECES) + lane / PIECES, lane % PIECES, b_at[i], p.ldb);
+        } else {                                    // 32 rows of the gate's, then 32 of the up projection's, for each wave's 64 columns
+            static_assert(B_ACROSS || B_FILLS == 4, "a wave fills 32 rows of b");
+            const int r = (w * B_FILLS + i) * 8 + lane / 8;
+            along(r, b_at[i], b_step[i], i * 8 + lane / 8, p.ldb);
+        }
+    }
+    // Forward: this wave's rows of b are the gate's (even waves) or the up projection's, from this row on.
+    const int b_part = MODE == FORWARD ? w & 1 : 0;
+    const int64_t b_row0 = MODE == FORWARD ? col0 + (w >> 1) * 32 : 0;
+
+    const int per_part = (int)((p.inner + STEPS - 1) / STEPS), parts = MODE == INPUT_GRAD ? 2 : 1;
+    const int stages_all = per_part * parts;
+    const int from = (int)((int64_t)stages_all * blockIdx.y / p.splits), to = (int)((int64_t)stages_all * (blockIdx.y + 1) / p.splits);
+
+    const auto fill_stage = [&](int t, unsigned lds) {
+        const int part = parts == 2 && t >= per_part, k0 = (t - part * per_part) * STEPS;
+        const bool tail = k0 + STEPS > p.inner;
+        u32x4 ra, rb;
+        if constexpr (A_ACROSS) {
+            const int64_t shift = k0 * p.lda + row0 * 2;
+            ra = range(p.a[out_part] + shift, p.inner * p.lda - out_part * (p.lda / 2) - shift);
+        } else {
+            const char *base = p.a[part] + row0 * p.lda + k0 * 2;
+            ra = range(base, (rows_left - 1) * p.lda + (p.inner - k0) * 2);
+        }
+        if constexpr (B_ACROSS) {
+            const int64_t shift = k0 * p.ldb + col0 * 2;
+            rb = range(p.b[part] + shift, (p.inner_b - 1) * p.ldb + (p.cols + 7) / 8 * 16 - shift);       // whole pieces: the rows have them, or their copy
+        } else {
+            const int64_t left = p.cols - b_row0 < 32 ? p.cols - b_row0 : 32;
+            rb = range(p.b[b_part] + b_row0 * p.ldb + k0 * 2, left <= 0 ? 0 : (left - 1) * p.ldb + (p.inner - k0) * 2);
+        }
+#pragma unroll
+        for (int i = 0; i < A_FILLS; ++i) {
+            unsigned at = a_at[i];
+            if (!A_ACROSS && tail) at = k0 + a_step[i] < p.inner ? at : NOWHERE;
+            fill(ra, at, lds + (w * A_FILLS + i) * 1024);
+        }
+#pragma unroll
+        for (int i = 0; i < B_FILLS; ++i) {
+            unsigned at = b_at[i];
+            if (!B_ACROSS && tail) at = k0 + b_step[i] < p.inner ? at : NOWHERE;
+            fill(rb, at, lds + A_BYTES + (w * B_FILLS + i) * 1024);
+        }
+    };
+
+    // Where a lane reads a fragment: rows lane % 16 of a tile, steps 8 * (lane / 16) on.
+    const int quad = lane >> 4, of16 = lane & 15;
+    const int along_row = of16 * ROW_BYTES, along_key = (of16 >> 1);
+    const int across_key = (of16 >> 2) | ((quad & 1) << 2);
+    const auto read_along = [&](const char *at, int tile, int half) {
+        return *reinterpret_cast<const short8_t *>(at + tile * 16 * ROW_BYTES + along_row + (((half * 4 + quad) ^ along_key) << 4));
+    };
+    const auto read_across = [&](const char *at, int tile, int half, int width) {     // tile: of 16 rows (or columns) of `width` in all
+        const char *where = at + (half * 32 + quad * 8 + (of16 >> 2)) * (width * 2) + ((tile ^ across_key) << 5) + (of16 & 3) * 8;
+        const short4_t lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) short4_t *)where);
+        const short4_t hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) short4_t *)(where + 4 * width * 2));
+        return __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
+    };
+
+    f32x4 acc[TM][TN] = {};
+    const auto compute = [&](const char *stage) {
+#pragma unroll
+        for (int half = 0; half < 2; ++half) {
+            short8_t fa[TM], fb[TN];
+#pragma unroll
+            for (int j = 0; j < TN; ++j) {
+                if constexpr (B_ACROSS) fb[j] = read_across(stage + A_BYTES, wn * TN + j, half, BN);
+                else fb[j] = read_along(stage + A_BYTES + wn * TN * 16 * ROW_BYTES, j, half);
+            }
+#pragma unroll
+            for (int i = 0; i < TM; ++i) {
+                if constexpr (A_ACROSS) fa[i] = read_across(stage, wm * TM + i, half, BM);
+                else fa[i] = read_along(stage + wm * TM * 16 * ROW_BYTES, i, half);
+            }
+#pragma unroll
+            for (int i = 0; i < TM; ++i)
+#pragma unroll
+                for (int j = 0; j < TN; ++j) acc[i][j] = mfma<DT>(fb[j], fa[i], acc[i][j]);
+        }
+    };
+
+    if (from < to) fill_stage(from, lds0);
+    for (int t = from; t < to; ++t) {
+        const int which = (t - from) & 1;
+        end_stage();
+        if (t + 1 < to) fill_stage(t + 1, lds0 + (which ^ 1) * STAGE);
+        compute(stages + which * STAGE);
+    }
+
+    // Of each 16x16 tile a lane holds four columns, 4 * (lane / 16) on, of row lane % 16.
+    if (p.splits > 1) {
+        float *to_part = p.partial + (int64_t)blockIdx.y * (MODE == WEIGHT_GRAD ? 2 : 1) * p.rows * p.ldp;
+#pragma unroll
+        for (int i = 0; i < TM; ++i) {
+            const int64_t m = row0 + (wm * TM + i) * 16 + of16;
+            if (m >= p.rows) continue;
+#pragma unroll
+            for (int j = 0; j < TN; ++j) {
+                const int64_t in = MODE == FORWARD ? wn * 32 + (j & 1) * 16 + quad * 4 : (wn * TN + j) * 16 + quad * 4;
+                const int64_t n = col0 + in, width = p.ldp / (MODE == FORWARD ? 2 : 1);
+                if (n < width) *reinterpret_cast<f32x4 *>(to_part + (out_part * p.rows + m) * p.ldp + (MODE == FORWARD ? (j >> 1) * width : 0) + n) = acc[i][j];
+            }
+        }
+        return;
+    }
+    // Two tiles of columns side by side: quads exchange halves, so that each lane has eight columns in a row.
+    const auto store8 = [&](char *out, int64_t m, int64_t n, const f32x4 &left, const f32x4 &right) {
+        u32x2_t a{pack2<DT>(left[0], left[1]), pack2<DT>(left[2], left[3])}, b{pack2<DT>(right[0], right[1]), pack2<DT>(right[2], right[3])};
+        const auto s0 = __builtin_amdgcn_permlane16_swap(a[0], b[0], false, false);
+        const auto s1 = __builtin_amdgcn_permlane16_swap(a[1], b[1], false, false);
+        const u32x4 v{s0[0], s1[0], s0[1], s1[1]};
+        n += (quad & 1) * 16 + (quad >> 1) * 8;
+        if (m >= p.rows || n >= p.cols) return;
+        if (n + 8 <= p.cols) {
+            store_piece<DT>(out, m * p.ldo + n, v);
+        } else {
+#pragma unroll
+            for (int e = 0; e < 8; ++e)
+                if (n + e < p.cols) reinterpret_cast<unsigned short *>(out)[m * p.ldo + n + e] = (unsigned short)(v[e / 2] >> (16 * (e & 1)));
+        }
+    };
+#pragma unroll
+    for (int i = 0; i < TM; ++i) {
+        const int64_t m = row0 + (wm * TM + i) * 16 + of16;
+        if constexpr (MODE == FORWARD) {
+            f32x4 h[2];
+#pragma unroll
+            for (int j = 0; j < 2; ++j)
+#pragma unroll
+                for (int q = 0; q < 4; ++q) h[j][q] = act<ACT>(acc[i][j][q]) * acc[i][j + 2][q];
+            const int64_t n = col0 + wn * 32;
+            store8(p.out[0], m, n, h[0], h[1]);
+            if (p.out[1]) {
+                store8(p.out[1], m, n, acc[i][0], acc[i][1]);
+                store8(p.out[2], m, n, acc[i][2], acc[i][3]);
+            }
+        } else {
+#pragma unroll
+            for (int j = 0; j < TN; j += 2) store8(p.out[out_part], m, col0 + (wn * TN + j) * 16, acc[i][j], acc[i][j + 1]);
+        }
+    }
+}
+
+// Sums of a split product's parts, in order, and what its epilogue does.  A thread for four columns.
+template <int DT, int MODE, int ACT>
+__global__ __launch_bounds__(256) void k_join_splits(Product p) {
+    const int parts = MODE == WEIGHT_GRAD ? 2 : 1;
+    const int64_t width = p.ldp / (MODE == FORWARD ? 2 : 1), per_row = width / 4, all = parts * p.rows * per_row;
+    const int64_t stride = (int64_t)parts * p.rows * p.ldp;
+    for (int64_t e = (int64_t)blockIdx.x * 256 + threadIdx.x; e < all; e += (int64_t)gridDim.x * 256) {
+        const int64_t row = e / per_row, n = (e - row * per_row) * 4;
+        f32x4 sum[2] = {};
+        for (int s = 0; s < p.splits; ++s) {
+            const float *at = p.partial + s * stride + row * p.ldp + n;
+            sum[0] += *reinterpret_cast<const f32x4 *>(at);
+            if constexpr (MODE == FORWARD) sum[1] += *reinterpret_cast<const f32x4 *>(at + width);
+        }
+        const int part = MODE == WEIGHT_GRAD && row >= p.rows;
+        const int64_t m = row - part * p.rows;
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+            if (n + q >= p.cols) break;
+            if constexpr (MODE == FORWARD) {
+                store_one<DT>(p.out[0], m * p.ldo + n + q, act<ACT>(sum[0][q]) * sum[1][q]);
+                if (p.out[1]) {
+                    store_one<DT>(p.out[1], m * p.ldo + n + q, sum[0][q]);
+                    store_one<DT>(p.out[2], m * p.ldo + n + q, sum[1][q]);
+                }
+            } else {
+                store_one<DT>(p.out[part], m * p.ldo + n + q, sum[0][q]);
+            }
+        }
+    }
+}
+
+// dg | du, side by side in a row of the workspace: [tokens][2][width], width = hidden rounded up to a piece, zeros in between.  Rounded to
+// the weights' type, which is what the matrix cores take.
+template <int DT, int ACT>
+__global__ __launch_bounds__(256) void k_slopes(const void *dh, const void *gate, const void *up, int64_t ld, int64_t tokens, int64_t hidden,
+                                                int64_t width, void *out) {
+    const int64_t f = ((int64_t)blockIdx.x * 256 + threadIdx.x) * 8;
+    if (f >= width) return;
+    for (int64_t m = blockIdx.y; m < tokens; m += gridDim.y) {
+        float d[8] = {}, g[8] = {}, u[8] = {}, dg[8], du[8];
+        const int64_t at = m * ld + f;
+        if (f + 8 <= hidden) {
+            unpack<DT>(load_piece<DT>(dh, at), d);
+            unpack<DT>(load_piece<DT>(gate, at), g);
+            unpack<DT>(load_piece<DT>(up, at), u);
+        } else {
+            for (int e = 0; e < 8; ++e)
+                if (f + e < hidden) {
+                    d[e] = load_one<DT>(dh, at + e);
+                    g[e] = load_one<DT>(gate, at + e);
+                    u[e] = load_one<DT>(up, at + e);
+                }
+        }
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            float a, da;
+            act_and_slope<ACT>(g[e], a, da);
+            dg[e] = d[e] * u[e] * da;
+            du[e] = d[e] * a;
+        }
+        store_piece<DT>(out, m * 2 * width + f, pack<DT>(dg));
+        store_piece<DT>(out, m * 2 * width + width + f, pack<DT>(du));
+    }
+}
+
+// Rows that the fills cannot take - a row or the distance between two is no multiple of 16 bytes - copied to where they can, zeros behind.
+__global__ __launch_bounds__(256) void k_align(const void *from, int64_t ld, int64_t rows, int64_t cols, int64_t width, void *to) {
+    const int64_t c = ((int64_t)blockIdx.x * 256 + threadIdx.x) * 8;
+    if (c >= width) return;
+    for (int64_t r = blockIdx.y; r < rows; r += gridDim.y) {
+        u32x4 v{0, 0, 0, 0};
+        if (c + 8 <= cols) {
+            v = load_piece<PARO_BF16>(from, r * ld + c);
+        } else {
+            for (int e = 0; e < 8; ++e)
+                if (c + e < cols) v[e / 2] |= (unsigned)static_cast<const unsigned short *>(from)[r * ld + c + e] << (16 * (e & 1));
+        }
+        store_piece<PARO_BF16>(to, r * width + c, v);
+    }
+}
+
+// ---------------------------------------------------------------- host
+int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
+int64_t up_to(int64_t a, int64_t b) { return ceil_div(a, b) * b; }
+constexpr int COMPUTE_UNITS = 256;
+
+bool fills_take(const void *p, int64_t ld, int64_t cols) { return !(reinterpret_cast<uintptr_t>(p) & 15) && ld % 8 == 0 && cols % 8 == 0; }
+
+struct Shape {                           // of a product's launch
+    bool large;                          // tiles of 256 x 256, else 128 x 128
+    int64_t tiles_m, tiles_n;
+    int splits;
+};
+// rows and columns: of the result (of WEIGHT_GRAD of one part, of FORWARD of both parts)
+Shape shape_of(int mode, int64_t rows, int64_t cols, int64_t inner) {
+    const auto tiles = [&](int64_t side, int64_t &m, int64_t &n) {
+        m = ceil_div(rows, side) * (mode == WEIGHT_GRAD ? 2 : 1);
+        n = mode == FORWARD ? ceil_div(cols, side / 2) : ceil_div(cols, side);
+        return m * n;
+    };
+    Shape s;
+    const int64_t n256 = tiles(256, s.tiles_m, s.tiles_n);
+    s.large = n256 >= COMPUTE_UNITS / 2;
+    const int64_t n = s.large ? n256 : tiles(128, s.tiles_m, s.tiles_n);
+    const int64_t at_once = s.large ? COMPUTE_UNITS : 2 * COMPUTE_UNITS;
+    const int64_t stages = ceil_div(inner, STEPS) * (mode == INPUT_GRAD ? 2 : 1);
+    // few tiles: the inner dimension is split, into parts of at least eight stages
+    s.splits = (int)std::max<int64_t>(1, std::min<int64_t>({at_once / std::max<int64_t>(n, 1), stages / 8, 16}));
+    return s;
+}
+int64_t partial_bytes(int mode, const Shape &s, int64_t rows, int64_t cols) {
+    if (s.splits == 1) return 0;
+    return s.splits * rows * up_to(cols, 4) * 4 * (mode == INPUT_GRAD ? 1 : 2);
+}
+
+template <int DT, int MODE, int ACT, int BM, int BN, int WAVES_M, int WAVES_N>
+int launch_tiles(const Product &p, hipStream_t st) {
+    constexpr unsigned LDS_BYTES = 2 * (BM + BN) * ROW_BYTES;
+    const auto kernel = k_product<DT, MODE, ACT, BM, BN, WAVES_M, WAVES_N>;
+    if (LDS_BYTES > 65536) {
+        const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void *>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, (int)LDS_BYTES);
+        if (e != hipSuccess) return fail(PARO_EHIP, std::string("shared memory: ") + hipGetErrorString(e));
+    }
+    hipLaunchKernelGGL(kernel, dim3((unsigned)(p.tiles_m * p.tiles_n), (unsigned)p.splits), dim3(64 * WAVES_M * WAVES_N), LDS_BYTES, st, p);
+    return PARO_OK;
+}
+
+template <int DT, int MODE, int ACT>
+int launch_product(Product p, const Shape &s, float *partial, hipStream_t st) {
+    p.tiles_m = (int)s.tiles_m;
+    p.tiles_n = (int)s.tiles_n;
+    p.splits = s.splits;
+    p.partial = partial;
+    p.ldp = up_to(p.cols, 4) * (MODE == FORWARD ? 2 : 1);
+    const int rc = s.large ? launch_tiles<DT, MODE, ACT, 256, 256, 2, 4>(p, st) : launch_tiles<DT, MODE, ACT, 128, 128, 2, 2>(p, st);
+    if (rc) return rc;
+    if (s.splits > 1) {
+        const int64_t threads = (MODE == WEIGHT_GRAD ? 2 : 1) * p.rows * (up_to(p.cols, 4) / 4);
+        hipLaunchKernelGGL((k_join_splits<DT, MODE, ACT>), dim3((unsigned)std::min<int64_t>(ceil_div(threads, 256), 8192)), dim3(256), 0, st, p);
+    }
+    return PARO_OK;
+}
+
+struct Room {                            // parts of the workspace, in bytes
+    int64_t x, wg, wu, slopes, partial, all;
+};
+Room room_of(const paro_gated_t &d, bool grad) {
+    const int64_t width = up_to(d.dim, 8), up256 = 256;
+    Room r{};
+    int64_t at = 0;
+    const auto take = [&](int64_t bytes) {
+        const int64_t here = at;
+        at += up_to(bytes, up256);
+        return here;
+    };
+    // whether the rows have to be copied depends on addresses as well: there is always room for it
+    r.x = take(d.n * width * 2);
+    r.wg = take(d.hidden * width * 2);
+    r.wu = take(d.hidden * width * 2);
+    int64_t partial = 0;
+    if (grad) {
+        r.slopes = take(d.n * 2 * up_to(d.hidden, 8) * 2);
+        partial = std::max(partial_bytes(INPUT_GRAD, shape_of(INPUT_GRAD, d.n, d.dim, d.hidden), d.n, d.dim),
+                           partial_bytes(WEIGHT_GRAD, shape_of(WEIGHT_GRAD, d.hidden, d.dim, d.n), d.hidden, d.dim));
+    } else {
+        partial = partial_bytes(FORWARD, shape_of(FORWARD, d.n, d.hidden, d.dim), d.n, d.hidden);
+    }
+    r.partial = take(partial);
+    r.all = std::max<int64_t>(at, 16);
+    return r;
+}
+
+// The rows as they are, or in a copy that the fills take.
+const char *taken(const void *rows, int64_t &ld, int64_t n, int64_t cols, bool as_they_are, char *copy, hipStream_t st) {
+    if (as_they_are) return static_cast<const char *>(rows);
+    const int64_t width = up_to(cols, 8);
+    hipLaunchKernelGGL(k_align, dim3((unsigned)ceil_div(width, 8 * 256), (unsigned)std::min<int64_t>(n, 65535)), dim3(256), 0, st, rows, ld, n, cols, width,
+                       copy);
+    ld = width;
+    return copy;
+}
+
+int check(const std::string &f, const paro_gated_t *d) {
+    if (!d) return fail(PARO_EINVAL, f + "d is NULL");
+    if (d->dtype != PARO_BF16 && d->dtype != PARO_F16) return fail(PARO_EINVAL, f + "dtype must be PARO_BF16 or PARO_F16");
+    if (d->act != PARO_SILU && d->act != PARO_GELU) return fail(PARO_EINVAL, f + "act must be PARO_SILU or PARO_GELU");
+    if (d->n < 0 || d->n > (1 << 24)) return fail(PARO_EINVAL, f + "n must be in [0, 2^24]");
+    if (d->dim < 1 || d->dim > (1 << 20) || d->hidden < 1 || d->hidden > (1 << 20)) return fail(PARO_EINVAL, f + "dim and hidden must be in [1, 2^20]");
+    if ((d->ld_x && d->ld_x < d->dim) || (d->ld_h && d->ld_h < d->hidden)) return fail(PARO_EINVAL, f + "a row is longer than its distance to the next");
+    if (d->ld_x > (1 << 21) || d->ld_h > (1 << 21)) return fail(PARO_EINVAL, f + "ld_x and ld_h are at most 2^21");
+    return PARO_OK;
+}
+int check_room(const std::string &f, const Room &r, const void *workspace, int64_t bytes) {
+    const int rc = check_array(workspace, 16, f + "workspace");
+    if (rc) return rc;
+    return bytes < r.all ? fail(PARO_ERANGE, f + "the workspace is smaller than paro_gated_workspace says") : PARO_OK;
+}
+
+// x and the weights as operands; both weights lie alike.
+struct Inputs {
+    const char *x, *wg, *wu;
+    int64_t ldx, ldw;
+};
+Inputs inputs_of(const paro_gated_t &d, const void *x, const void *wg, const void *wu, char *ws, const Room &r, hipStream_t st) {
+    Inputs in;
+    in.ldx = d.ld_x ? d.ld_x : d.dim;
+    in.x = taken(x, in.ldx, d.n, d.dim, fills_take(x, in.ldx, d.dim), ws + r.x, st);
+    const bool as_they_are = fills_take(wg, d.dim, d.dim) && fills_take(wu, d.dim, d.dim);
+    in.ldw = d.dim;
+    in.wg = taken(wg, in.ldw, d.hidden, d.dim, as_they_are, ws + r.wg, st);
+    in.ldw = d.dim;
+    in.wu = taken(wu, in.ldw, d.hidden, d.dim, as_they_are, ws + r.wu, st);
+    return in;
+}
+
+template <int DT, int ACT>
+int forward(const paro_gated_t &d, const void *x, const void *wg, const void *wu, void *h, void *gate, void *up, char *ws, const Room &r,
+            hipStream_t st) {
+    const Inputs in = inputs_of(d, x, wg, wu, ws, r, st);
+    Product p{};
+    p.a[0] = in.x;
+    p.b[0] = in.wg;
+    p.b[1] = in.wu;
+    p.lda = in.ldx * 2;
+    p.ldb = in.ldw * 2;
+    p.rows = d.n;
+    p.cols = d.hidden;
+    p.inner = up_to(d.dim, 8);
+    p.out[0] = static_cast<char *>(h);
+    p.out[1] = static_cast<char *>(gate);
+    p.out[2] = static_cast<char *>(up);
+    p.ldo = d.ld_h ? d.ld_h : d.hidden;
+    return launch_product<DT, FORWARD, ACT>(p, shape_of(FORWARD, d.n, d.hidden, d.dim), reinterpret_cast<float *>(ws + r.partial), st);
+}
+
+template <int DT, int ACT>
+int backward(const paro_gated_t &d, const void *dh, const void *gate, const void *up, const void *x, const void *wg, const void *wu, void *dx,
+             void *dwg, void *dwu, char *ws, const Room &r, hipStream_t st) {
+    Product p{};
+    if (d.n == 0) {                                         // no token, no stage: the tiles of dWg and dWu are zeros
+        p.rows = d.hidden;
+        p.cols = p.ldo = d.dim;
+        p.out[0] = static_cast<char *>(dwg);
+        p.out[1] = static_cast<char *>(dwu);
+        return launch_product<DT, WEIGHT_GRAD, PARO_SILU>(p, shape_of(WEIGHT_GRAD, d.hidden, d.dim, 0), nullptr, st);
+    }
+    const Inputs in = inputs_of(d, x, wg, wu, ws, r, st);
+    const int64_t width = up_to(d.hidden, 8);
+    char *slopes = ws + r.slopes;
+    float *partial = reinterpret_cast<float *>(ws + r.partial);
+    hipLaunchKernelGGL((k_slopes<DT, ACT>), dim3((unsigned)ceil_div(width, 8 * 256), (unsigned)std::min<int64_t>(d.n, 65535)), dim3(256), 0, st, dh, gate, up,
+                       d.ld_h ? d.ld_h : d.hidden, d.n, d.hidden, width, slopes);
+    p.a[0] = slopes;
+    p.a[1] = slopes + width * 2;
+    p.lda = 2 * width * 2;
+    p.b[0] = in.wg;
+    p.b[1] = in.wu;
+    p.ldb = in.ldw * 2;
+    p.rows = d.n;
+    p.cols = d.dim;
+    p.inner = width;
+    p.inner_b = d.hidden;
+    p.out[0] = static_cast<char *>(dx);
+    p.ldo = d.ld_x ? d.ld_x : d.dim;
+    int rc = launch_product<DT, INPUT_GRAD, PARO_SILU>(p, shape_of(INPUT_GRAD, d.n, d.dim, d.hidden), partial, st);
+    if (rc) return rc;
+    p.b[0] = in.x;
+    p.b[1] = nullptr;
+    p.ldb = in.ldx * 2;
+    p.rows = d.hidden;
+    p.inner = p.inner_b = d.n;
+    p.out[0] = static_cast<char *>(dwg);
+    p.out[1] = static_cast<char *>(dwu);
+    p.ldo = d.dim;
+    return launch_product<DT, WEIGHT_GRAD, PARO_SILU>(p, shape_of(WEIGHT_GRAD, d.hidden, d.dim, d.n), partial, st);
+}
+
+#define PARO_BY_TYPE(CALL)                                            \
+    (d->dtype == PARO_BF16 ? d->act == PARO_SILU ? CALL(PARO_BF16, PARO_SILU) : CALL(PARO_BF16, PARO_GELU) \
+                           : d->act == PARO_SILU ? CALL(PARO_F16, PARO_SILU) : CALL(PARO_F16, PARO_GELU))
+
+}  // namespace
+
+extern "C" {
+
+int64_t paro_gated_workspace(const paro_gated_t *d, int grad) {
+    int64_t bytes = 0;
+    const int rc = guarded([&]() -> int {
+        const int bad = check("paro_gated_workspace: ", d);
+        if (!bad) bytes = room_of(*d, grad != 0).all;
+        return bad;
+    });
+    return rc ? rc : bytes;
+}
+
+int paro_gated(const paro_gated_t *d, const void *x, const void *w_gate, const void *w_up, void *h, void *gate, void *up, void *workspace,
+               int64_t workspace_bytes, void *stream) {
+    return guarded([&]() -> int {
+        const std::string f = "paro_gated: ";
+        int rc;
+        if ((rc = check(f, d)) || d->n == 0) return rc;
+        if ((rc = check_array(x, 2, f + "x")) || (rc = check_array(w_gate, 2, f + "w_gate")) || (rc = check_array(w_up, 2, f + "w_up")) ||
+            (rc = check_array(h, 2, f + "h")))
+            return rc;
+        if (!gate != !up) return fail(PARO_EINVAL, f + "gate and up are stored both or neither");
+        if (gate && ((rc = check_array(gate, 2, f + "gate")) || (rc = check_array(up, 2, f + "up")))) return rc;
+        const Room r = room_of(*d, false);
+        if ((rc = check_room(f, r, workspace, workspace_bytes))) return rc;
+        hipStream_t st = static_cast<hipStream_t>(stream);
+        char *ws = static_cast<char *>(workspace);
+#define PARO_FORWARD(DT, ACT) forward<DT, ACT>(*d, x, w_gate, w_up, h, gate, up, ws, r, st)
+        if ((rc = PARO_BY_TYPE(PARO_FORWARD))) return rc;
+#undef PARO_FORWARD
+        PARO_LAUNCHED("paro_gated");
+        return PARO_OK;
+    });
+}
+
+int paro_gated_grad(const paro_gated_t *d, const void *dh, const void *gate, const void *up, const void *x, const void *w_gate, const void *w_up,
+                    void *dx, void *dw_gate, void *dw_up, void *workspace, int64_t workspace_bytes, void *stream) {
+    return guarded([&]() -> int {
+        const std::string f = "paro_gated_grad: ";
+        int rc;
+        if ((rc = check(f, d))) return rc;
+        if ((rc = check_array(w_gate, 2, f + "w_gate")) || (rc = check_array(w_up, 2, f + "w_up")) || (rc = check_array(dw_gate, 2, f + "dw_gate")) ||
+            (rc = check_array(dw_up, 2, f + "dw_up")))
+            return rc;
+        if (d->n && ((rc = check_array(dh, 2, f + "dh")) || (rc = check_array(gate, 2, f + "gate")) || (rc = check_array(up, 2, f + "up")) ||
+                     (rc = check_array(x, 2, f + "x")) || (rc = check_array(dx, 2, f + "dx"))))
+            return rc;
+        const Room r = room_of(*d, true);
+        if ((rc = check_room(f, r, workspace, workspace_bytes))) return rc;
+        hipStream_t st = static_cast<hipStream_t>(stream);
+        char *ws = static_cast<char *>(workspace);
+#define PARO_BACKWARD(DT, ACT) backward<DT, ACT>(*d, dh, gate, up, x, w_gate, w_up, dx, dw_gate, dw_up, ws, r, st)
+        if ((rc = PARO_BY_TYPE(PARO_BACKWARD))) return rc;
+#undef PARO_BACKWARD
+        PARO_LAUNCHED("paro_gated_grad");
+        return PARO_OK;
+    });
+}
+
+}  // extern "C"
