@@ -9,6 +9,8 @@
 // the same hidden elements, so that one wave has both and the activation and the product happen in its registers.
 // An operand whose inner dimension lies along memory (x, W forward; dg | du of dx) is read from shared memory in pieces of eight steps; one
 // whose inner dimension goes from row to row (W of dx; both of dW) is staged as it lies and transposed by the reading instruction.
+#include <type_traits>
+
 #include "operators.hpp"
 
 namespace {
@@ -54,18 +56,20 @@ __device__ __forceinline__ void act_and_slope(float g, float &a, float &da) {
 __device__ __forceinline__ int wave_of() { return __builtin_amdgcn_readfirstlane(threadIdx.x >> 6); }
 
 // 16 bytes a lane from memory to shared memory at `to` + 16 * lane, past the registers; out of range: zeros.  In assembly because
-// the compiler, which cannot tell the stages apart, would wait for it before every read of shared memory; end_stage() waits.
+// the compiler, which cannot tell the stages apart, would wait for it before every read of shared memory; all_waves() waits.
 // There is no register that it writes.
 __device__ __forceinline__ void fill(u32x4 from, unsigned offset, unsigned to) {
     asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(to), "v"(offset), "s"(from) : "memory");
 }
-// All of the wave's fills have arrived, all its reads are done; then those of all waves.
-__device__ __forceinline__ void end_stage() { asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory"); }
+// All but the wave's last `IN_FLIGHT` fills have arrived, all its reads are done; then those of all waves.
+template <int IN_FLIGHT>
+__device__ __forceinline__ void all_waves() { asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"i"(IN_FLIGHT) : "memory"); }
 
 // A buffer descriptor of the bytes from `base` on; beyond them the hardware reads zeros.
 __device__ __forceinline__ u32x4 range(const char *base, int64_t bytes) {
     const uint64_t at = (uint64_t)(uintptr_t)base;
-    return u32x4{(unsigned)at, (unsigned)(at >> 32) & 0xFFFFu, bytes < 0 ? 0u : bytes > 0x7FFFFFF0 ? 0x7FFFFFF0u : (unsigned)bytes, 0x00020000u};
+    const int over = (int)(bytes >> 31);
+    return u32x4{(unsigned)at, (unsigned)(at >> 32) & 0xFFFFu, over < 0 ? 0u : over > 0 ? 0x7FFFFFF0u : (unsigned)bytes, 0x00020000u};
 }
 constexpr unsigned NOWHERE = 0x80000000u;
 
@@ -158,35 +162,47 @@ __global__ __launch_bounds__(64 * WAVES_M * WAVES_N) void k_product(Product p) {
     const int stages_all = per_part * parts;
     const int from = (int)((int64_t)stages_all * blockIdx.y / p.splits), to = (int)((int64_t)stages_all * (blockIdx.y + 1) / p.splits);
 
-    const auto fill_stage = [&](int t, unsigned lds) {
-        const int part = parts == 2 && t >= per_part, k0 = (t - part * per_part) * STEPS;
-        const bool tail = k0 + STEPS > p.inner;
-        u32x4 ra, rb;
+    // What the next stage is filled from.
+    int part = parts == 2 && from >= per_part, left = (int)p.inner - (from - part * per_part) * STEPS;      // steps left of the part
+    const char *a_from, *b_from;
+    int64_t a_bytes, b_bytes;
+    const int64_t a_stage = A_ACROSS ? STEPS * p.lda : ROW_BYTES, b_stage = B_ACROSS ? STEPS * p.ldb : ROW_BYTES;
+    const auto begin_part = [&]() {
+        const int64_t k0 = p.inner - left;
         if constexpr (A_ACROSS) {
             const int64_t shift = k0 * p.lda + row0 * 2;
-            ra = range(p.a[out_part] + shift, p.inner * p.lda - out_part * (p.lda / 2) - shift);
+            a_from = p.a[out_part] + shift;
+            a_bytes = p.inner * p.lda - out_part * (p.lda / 2) - shift;
         } else {
-            const char *base = p.a[part] + row0 * p.lda + k0 * 2;
-            ra = range(base, (rows_left - 1) * p.lda + (p.inner - k0) * 2);
+            a_from = p.a[part] + row0 * p.lda + k0 * 2;
+            a_bytes = (rows_left - 1) * p.lda + left * 2;
         }
         if constexpr (B_ACROSS) {
             const int64_t shift = k0 * p.ldb + col0 * 2;
-            rb = range(p.b[part] + shift, (p.inner_b - 1) * p.ldb + (p.cols + 7) / 8 * 16 - shift);       // whole pieces: the rows have them, or their copy
+            b_from = p.b[part] + shift;
+            b_bytes = (p.inner_b - 1) * p.ldb + (p.cols + 7) / 8 * 16 - shift;       // whole pieces: the rows have them, or their copy
         } else {
-            const int64_t left = p.cols - b_row0 < 32 ? p.cols - b_row0 : 32;
-            rb = range(p.b[b_part] + b_row0 * p.ldb + k0 * 2, left <= 0 ? 0 : (left - 1) * p.ldb + (p.inner - k0) * 2);
+            const int64_t b_rows = p.cols - b_row0 < 32 ? p.cols - b_row0 : 32;
+            b_from = p.b[b_part] + b_row0 * p.ldb + k0 * 2;
+            b_bytes = b_rows <= 0 ? -1 : (b_rows - 1) * p.ldb + left * 2;
         }
+    };
+    begin_part();
+    const auto fill_stage = [&](unsigned lds) {
+        const u32x4 ra = range(a_from, a_bytes), rb = range(b_from, b_bytes);
 #pragma unroll
-        for (int i = 0; i < A_FILLS; ++i) {
-            unsigned at = a_at[i];
-            if (!A_ACROSS && tail) at = k0 + a_step[i] < p.inner ? at : NOWHERE;
-            fill(ra, at, lds + (w * A_FILLS + i) * 1024);
-        }
+        for (int i = 0; i < A_FILLS; ++i) fill(ra, A_ACROSS || a_step[i] < left ? a_at[i] : NOWHERE, lds + (w * A_FILLS + i) * 1024);
 #pragma unroll
-        for (int i = 0; i < B_FILLS; ++i) {
-            unsigned at = b_at[i];
-            if (!B_ACROSS && tail) at = k0 + b_step[i] < p.inner ? at : NOWHERE;
-            fill(rb, at, lds + A_BYTES + (w * B_FILLS + i) * 1024);
+        for (int i = 0; i < B_FILLS; ++i) fill(rb, B_ACROSS || b_step[i] < left ? b_at[i] : NOWHERE, lds + A_BYTES + (w * B_FILLS + i) * 1024);
+        a_from += a_stage;
+        a_bytes -= a_stage;
+        b_from += b_stage;
+        b_bytes -= b_stage;
+        left -= STEPS;
+        if (parts == 2 && left <= 0 && part == 0) {
+            part = 1;
+            left = (int)p.inner;
+            begin_part();
         }
     };
 
@@ -205,33 +221,55 @@ __global__ __launch_bounds__(64 * WAVES_M * WAVES_N) void k_product(Product p) {
     };
 
     f32x4 acc[TM][TN] = {};
-    const auto compute = [&](const char *stage) {
+    short8_t fa[2][TM], fb[2][TN];                  // fragments of the two halves of a stage
+    const auto read_b = [&](const char *stage, int half, int j) {
+        if constexpr (B_ACROSS) return read_across(stage + A_BYTES, wn * TN + j, half, BN);
+        else return read_along(stage + A_BYTES + wn * TN * 16 * ROW_BYTES, j, half);
+    };
+    const auto read_a = [&](const char *stage, int half, int i) {
+        if constexpr (A_ACROSS) return read_across(stage, wm * TM + i, half, BM);
+        else return read_along(stage + wm * TM * 16 * ROW_BYTES, i, half);
+    };
+    // The products of one half; meanwhile the fragments of the other are read.
+    const auto multiply = [&](auto half_, auto read_, const char *next) {
+        constexpr int half = half_, other = half ^ 1;
+        constexpr bool read = read_;
 #pragma unroll
-        for (int half = 0; half < 2; ++half) {
-            short8_t fa[TM], fb[TN];
-#pragma unroll
-            for (int j = 0; j < TN; ++j) {
-                if constexpr (B_ACROSS) fb[j] = read_across(stage + A_BYTES, wn * TN + j, half, BN);
-                else fb[j] = read_along(stage + A_BYTES + wn * TN * 16 * ROW_BYTES, j, half);
+        for (int i = 0; i < TM; ++i) {
+            if constexpr (read) {
+                if (i < TN) fb[other][i] = read_b(next, other, i);
+                fa[other][i] = read_a(next, other, i);
             }
 #pragma unroll
-            for (int i = 0; i < TM; ++i) {
-                if constexpr (A_ACROSS) fa[i] = read_across(stage, wm * TM + i, half, BM);
-                else fa[i] = read_along(stage + wm * TM * 16 * ROW_BYTES, i, half);
-            }
-#pragma unroll
-            for (int i = 0; i < TM; ++i)
-#pragma unroll
-                for (int j = 0; j < TN; ++j) acc[i][j] = mfma<DT>(fb[j], fa[i], acc[i][j]);
+            for (int j = 0; j < TN; ++j) acc[i][j] = mfma<DT>(fb[half][j], fa[half][i], acc[i][j]);
         }
     };
+    constexpr std::integral_constant<int, 0> FIRST;
+    constexpr std::integral_constant<int, 1> SECOND;
 
-    if (from < to) fill_stage(from, lds0);
-    for (int t = from; t < to; ++t) {
-        const int which = (t - from) & 1;
-        end_stage();
-        if (t + 1 < to) fill_stage(t + 1, lds0 + (which ^ 1) * STAGE);
-        compute(stages + which * STAGE);
+    if (from < to) {
+        fill_stage(lds0);
+        if (from + 1 < to) {
+            fill_stage(lds0 + STAGE);
+            all_waves<A_FILLS + B_FILLS>();
+        } else {
+            all_waves<0>();
+        }
+#pragma unroll
+        for (int j = 0; j < TN; ++j) fb[0][j] = read_b(stages, 0, j);
+#pragma unroll
+        for (int i = 0; i < TM; ++i) fa[0][i] = read_a(stages, 0, i);
+        // The second half's products run beside the reads of the next stage's first: by then every wave has read all of this stage, which
+        // is filled again, and the next one, filled a whole stage's time ago, has arrived.
+        unsigned which = 0;
+        for (int t = from; t < to - 1; ++t, which ^= STAGE) {
+            multiply(FIRST, std::true_type{}, stages + which);
+            all_waves<0>();
+            if (t + 2 < to) fill_stage(lds0 + which);
+            multiply(SECOND, std::true_type{}, stages + (which ^ STAGE));
+        }
+        multiply(FIRST, std::true_type{}, stages + which);
+        multiply(SECOND, std::false_type{}, stages);
     }
 
     // Of each 16x16 tile a lane holds four columns, 4 * (lane / 16) on, of row lane % 16.
