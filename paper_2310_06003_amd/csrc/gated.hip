@@ -4,8 +4,8 @@
 //   dg = dh u act'(g),  du = dh act(g);   dx = dg Wg + du Wu,  dWg = dg' x,  dWu = du' x
 //
 // Bound by the matrix cores for many tokens, by reading the weights for few.  Three products of one kernel: a block computes
-// a tile of the result with 16x16x32 matrix instructions in fp32, its waves side by side on it, from two stages of 64 steps of the inner
-// dimension in shared memory that are filled past the registers.  Forward, a tile holds the gate's and the up projection's columns of
+// a tile of the result with 16x16x32 matrix instructions in fp32, its waves side by side on it, from a ring of five parts of shared memory,
+// each 64 steps of the inner dimension of one operand, that are filled past the registers.  Forward, a tile holds the gate's and the up projection's columns of
 // the same hidden elements, so that one wave has both and the activation and the product happen in its registers.
 // An operand whose inner dimension lies along memory (x, W forward; dg | du of dx) is read from shared memory in pieces of eight steps; one
 // whose inner dimension goes from row to row (W of dx; both of dW) is staged as it lies and transposed by the reading instruction.
@@ -15,7 +15,7 @@
 
 namespace {
 
-constexpr int STEPS = 64;                // of the inner dimension, a stage
+constexpr int STEPS = 64;                // of the inner dimension, a stage: a part of the ring for each operand
 constexpr int ROW_BYTES = STEPS * 2;     // of an operand that lies along it
 enum { FORWARD = 0, INPUT_GRAD = 1, WEIGHT_GRAD = 2 };
 
@@ -58,18 +58,20 @@ __device__ __forceinline__ int wave_of() { return __builtin_amdgcn_readfirstlane
 // 16 bytes a lane from memory to shared memory at `to` + 16 * lane, past the registers; out of range: zeros.  In assembly because
 // the compiler, which cannot tell the stages apart, would wait for it before every read of shared memory; all_waves() waits.
 // There is no register that it writes.
+template <int AT>
 __device__ __forceinline__ void fill(u32x4 from, unsigned offset, unsigned to) {
-    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(to), "v"(offset), "s"(from) : "memory");
+    asm volatile("s_add_u32 m0, %0, %3\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(to), "v"(offset), "s"(from), "i"(AT)
+                 : "memory", "scc");
 }
 // All but the wave's last `IN_FLIGHT` fills have arrived, all its reads are done; then those of all waves.
 template <int IN_FLIGHT>
 __device__ __forceinline__ void all_waves() { asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"i"(IN_FLIGHT) : "memory"); }
 
-// A buffer descriptor of the bytes from `base` on; beyond them the hardware reads zeros.
-__device__ __forceinline__ u32x4 range(const char *base, int64_t bytes) {
+// A buffer descriptor of the memory from `base` on.  Lanes without a piece are sent NOWHERE, beyond it, where the hardware reads zeros: all
+// others stay inside their operand.
+__device__ __forceinline__ u32x4 descriptor(const char *base) {
     const uint64_t at = (uint64_t)(uintptr_t)base;
-    const int over = (int)(bytes >> 31);
-    return u32x4{(unsigned)at, (unsigned)(at >> 32) & 0xFFFFu, over < 0 ? 0u : over > 0 ? 0x7FFFFFF0u : (unsigned)bytes, 0x00020000u};
+    return u32x4{(unsigned)at, (unsigned)(at >> 32) & 0xFFFFu, 0x7FFFFFF0u, 0x00020000u};
 }
 constexpr unsigned NOWHERE = 0x80000000u;
 
@@ -79,7 +81,7 @@ struct Product {
     const char *a[2], *b[2];
     int64_t lda, ldb;                    // bytes
     int64_t rows, cols, inner;           // inner: of one part, in whole pieces where an operand lies along it
-    int64_t inner_b;                     // across: rows that b has
+    int64_t inner_b;                     // steps that b has (across: rows)
     char *out[3];                        // h, g, u; dx; dWg, dWu
     int64_t ldo;                         // elements
     float *partial;                      // splits > 1: [split][rows][cols of all parts], fp32
@@ -103,12 +105,12 @@ template <int DT, int MODE, int ACT, int BM, int BN, int WAVES_M, int WAVES_N>
 __global__ __launch_bounds__(64 * WAVES_M * WAVES_N) void k_product(Product p) {
     constexpr int THREADS_ = 64 * WAVES_M * WAVES_N;
     constexpr int TM = BM / WAVES_M / 16, TN = BN / WAVES_N / 16;             // 16x16 tiles of a wave
-    constexpr int A_BYTES = BM * ROW_BYTES, B_BYTES = BN * ROW_BYTES, STAGE = A_BYTES + B_BYTES;
-    constexpr int A_FILLS = A_BYTES / (THREADS_ * 16), B_FILLS = B_BYTES / (THREADS_ * 16);
+    constexpr int A_BYTES = BM * ROW_BYTES, B_BYTES = BN * ROW_BYTES, PART = A_BYTES;
+    constexpr int FILLS = A_BYTES / (THREADS_ * 16);           // of a part, by each wave
     constexpr bool A_ACROSS = MODE == WEIGHT_GRAD, B_ACROSS = MODE != FORWARD;
-    static_assert(TN == 4, "a wave's columns are two pairs of tiles");
-    extern __shared__ __attribute__((aligned(1024))) char stages[];
-    const unsigned lds0 = (unsigned)(uintptr_t)(lds_char *)stages;
+    static_assert(TN == 4 && A_BYTES == B_BYTES, "a wave's columns are two pairs of tiles, and a part of the ring takes either operand");
+    extern __shared__ __attribute__((aligned(1024))) char ring[];
+    const unsigned lds0 = (unsigned)(uintptr_t)(lds_char *)ring;
     const int w = wave_of(), lane = threadIdx.x & 63, wm = w / WAVES_N, wn = w % WAVES_N;
     int tm, tn;
     tile_of(blockIdx.x, p.tiles_m, p.tiles_n, tm, tn);
@@ -120,91 +122,103 @@ __global__ __launch_bounds__(64 * WAVES_M * WAVES_N) void k_product(Product p) {
     const int out_part = MODE == WEIGHT_GRAD ? tm >= n_tiles_part : 0;
     const int64_t row0 = MODE == WEIGHT_GRAD ? m0 - out_part * n_tiles_part * BM : m0;
     const int64_t col0 = (int64_t)tn * (MODE == FORWARD ? HALF_N : BN);
-    const int64_t rows_left = p.rows - row0 < BM ? p.rows - row0 : BM;
 
-    unsigned a_at[A_FILLS], b_at[B_FILLS];          // a lane's offsets from the operand's beginning
-    int a_step[A_FILLS], b_step[B_FILLS];           // along: the step that its piece begins with
-    const auto along = [&](int row, unsigned &at, int &step, int64_t memory_row, int64_t ld) {
+    // A lane's pieces: their offsets from where the stage begins, and the step (along: the first of eight) of each.  The pieces of a
+    // stage are exchanged within 256 bytes such that the lanes that read at a time meet all banks.  Pieces of rows or columns that the operand
+    // does not have are nowhere.
+    unsigned a_at[FILLS], b_at[FILLS];
+    int a_step[FILLS], b_step[FILLS];
+    const auto along = [&](int row, bool there, int64_t memory_row, int64_t ld, unsigned &at, int &step) {
         const int piece = (lane & 7) ^ ((row >> 1) & 7);
-        at = (unsigned)(memory_row * ld) + piece * 16;
+        at = there ? (unsigned)(memory_row * ld) + piece * 16 : NOWHERE;
         step = piece * 8;
     };
-    const auto across = [&](int k, int piece, unsigned &at, int64_t ld) {
-        const int block = (piece >> 1) ^ ((k & 3) | ((k >> 1) & 4));
-        at = (unsigned)(k * ld) + (block * 2 + (piece & 1)) * 16;
+    const auto across = [&](int k, int piece, int64_t columns_left, int64_t ld, unsigned &at, int &step) {
+        const int block = (piece >> 1) ^ ((k & 3) | ((k >> 1) & 4)), column = (block * 2 + (piece & 1)) * 8;
+        at = column < columns_left ? (unsigned)(k * ld) + column * 2 : NOWHERE;
+        step = k;
     };
-#pragma unroll
-    for (int i = 0; i < A_FILLS; ++i) {
-        if constexpr (A_ACROSS) {
-            constexpr int PIECES = BM / 8;
-            across((w * A_FILLS + i) * (64 / PIECES) + lane / PIECES, lane % PIECES, a_at[i], p.lda);
-        } else {
-            const int r = (w * A_FILLS + i) * 8 + lane / 8;
-            along(r, a_at[i], a_step[i], r, p.lda);
-        }
-    }
-#pragma unroll
-    for (int i = 0; i < B_FILLS; ++i) {
-        if constexpr (B_ACROSS) {
-            constexpr int PIECES = BN / 8;
-            across((w * B_FILLS + i) * (64 / PIECES) + lane / PIECES, lane % PIECES, b_at[i], p.ldb);
-        } else {                                    // 32 rows of the gate's, then 32 of the up projection's, for each wave's 64 columns
-            static_assert(B_ACROSS || B_FILLS == 4, "a wave fills 32 rows of b");
-            const int r = (w * B_FILLS + i) * 8 + lane / 8;
-            along(r, b_at[i], b_step[i], i * 8 + lane / 8, p.ldb);
-        }
-    }
-    // Forward: this wave's rows of b are the gate's (even waves) or the up projection's, from this row on.
+    // Forward: this wave fills rows of b that are the gate's (even waves) or the up projection's, from this row on.
     const int b_part = MODE == FORWARD ? w & 1 : 0;
     const int64_t b_row0 = MODE == FORWARD ? col0 + (w >> 1) * 32 : 0;
+#pragma unroll
+    for (int i = 0; i < FILLS; ++i) {
+        if constexpr (A_ACROSS) {
+            constexpr int PIECES = BM / 8;
+            across((w * FILLS + i) * (64 / PIECES) + lane / PIECES, lane % PIECES, p.rows - row0, p.lda, a_at[i], a_step[i]);
+        } else {
+            const int r = (w * FILLS + i) * 8 + lane / 8;
+            along(r, r < p.rows - row0, r, p.lda, a_at[i], a_step[i]);
+        }
+    }
+#pragma unroll
+    for (int i = 0; i < FILLS; ++i) {
+        if constexpr (B_ACROSS) {
+            constexpr int PIECES = BN / 8;
+            across((w * FILLS + i) * (64 / PIECES) + lane / PIECES, lane % PIECES, p.cols - col0, p.ldb, b_at[i], b_step[i]);
+        } else {                                    // 32 rows of the gate's, then 32 of the up projection's, for each wave's 64 columns
+            static_assert(B_ACROSS || FILLS == 4, "a wave fills 32 rows of b");
+            const int r = i * 8 + lane / 8;
+            along((w * FILLS + i) * 8 + lane / 8, b_row0 + r < p.cols, r, p.ldb, b_at[i], b_step[i]);
+        }
+    }
 
     const int per_part = (int)((p.inner + STEPS - 1) / STEPS), parts = MODE == INPUT_GRAD ? 2 : 1;
     const int stages_all = per_part * parts;
     const int from = (int)((int64_t)stages_all * blockIdx.y / p.splits), to = (int)((int64_t)stages_all * (blockIdx.y + 1) / p.splits);
 
     // What the next stage is filled from.
-    int part = parts == 2 && from >= per_part, left = (int)p.inner - (from - part * per_part) * STEPS;      // steps left of the part
-    const char *a_from, *b_from;
-    int64_t a_bytes, b_bytes;
+    u32x4 a_from, b_from;
+    int a_left, b_left, a_until, b_until;           // steps left of the part; stages until the part ends, or the block's share of it
     const int64_t a_stage = A_ACROSS ? STEPS * p.lda : ROW_BYTES, b_stage = B_ACROSS ? STEPS * p.ldb : ROW_BYTES;
-    const auto begin_part = [&]() {
-        const int64_t k0 = p.inner - left;
-        if constexpr (A_ACROSS) {
-            const int64_t shift = k0 * p.lda + row0 * 2;
-            a_from = p.a[out_part] + shift;
-            a_bytes = p.inner * p.lda - out_part * (p.lda / 2) - shift;
-        } else {
-            a_from = p.a[part] + row0 * p.lda + k0 * 2;
-            a_bytes = (rows_left - 1) * p.lda + left * 2;
-        }
-        if constexpr (B_ACROSS) {
-            const int64_t shift = k0 * p.ldb + col0 * 2;
-            b_from = p.b[part] + shift;
-            b_bytes = (p.inner_b - 1) * p.ldb + (p.cols + 7) / 8 * 16 - shift;       // whole pieces: the rows have them, or their copy
-        } else {
-            const int64_t b_rows = p.cols - b_row0 < 32 ? p.cols - b_row0 : 32;
-            b_from = p.b[b_part] + b_row0 * p.ldb + k0 * 2;
-            b_bytes = b_rows <= 0 ? -1 : (b_rows - 1) * p.ldb + left * 2;
+    const auto begin_a = [&](int part, int stage) {
+        const int64_t k0 = (int64_t)stage * STEPS;
+        a_from = descriptor(A_ACROSS ? p.a[out_part] + k0 * p.lda + row0 * 2 : p.a[part] + row0 * p.lda + k0 * 2);
+        a_left = (int)(p.inner - k0);
+        a_until = (to < (part + 1) * per_part ? to - part * per_part : per_part) - stage;
+    };
+    const auto begin_b = [&](int part, int stage) {
+        const int64_t k0 = (int64_t)stage * STEPS;
+        b_from = descriptor(B_ACROSS ? p.b[part] + k0 * p.ldb + col0 * 2 : p.b[b_part] + b_row0 * p.ldb + k0 * 2);
+        b_left = (int)(p.inner_b - k0);
+        b_until = (to < (part + 1) * per_part ? to - part * per_part : per_part) - stage;
+    };
+    const auto advance = [](u32x4 &d, int64_t bytes) {
+        const uint64_t at = ((uint64_t)d[1] << 32 | d[0]) + (uint64_t)bytes;
+        d[0] = (unsigned)at;
+        d[1] = (unsigned)(at >> 32);
+    };
+    // Past the last stage they go on with zeros from nowhere: the waits count on as many fills each time.
+    bool second_a = from >= per_part, second_b = second_a;
+    begin_a(second_a, from - (second_a ? per_part : 0));
+    begin_b(second_b, from - (second_b ? per_part : 0));
+    const auto next_a = [&]() {
+        advance(a_from, a_stage);
+        a_left -= STEPS;
+        if (--a_until == 0) {
+            if (MODE == INPUT_GRAD && !second_a && to > per_part) {
+                second_a = true;
+                begin_a(1, 0);
+            } else {
+                a_left = INT32_MIN / 2;
+            }
         }
     };
-    begin_part();
-    const auto fill_stage = [&](unsigned lds) {
-        const u32x4 ra = range(a_from, a_bytes), rb = range(b_from, b_bytes);
-#pragma unroll
-        for (int i = 0; i < A_FILLS; ++i) fill(ra, A_ACROSS || a_step[i] < left ? a_at[i] : NOWHERE, lds + (w * A_FILLS + i) * 1024);
-#pragma unroll
-        for (int i = 0; i < B_FILLS; ++i) fill(rb, B_ACROSS || b_step[i] < left ? b_at[i] : NOWHERE, lds + A_BYTES + (w * B_FILLS + i) * 1024);
-        a_from += a_stage;
-        a_bytes -= a_stage;
-        b_from += b_stage;
-        b_bytes -= b_stage;
-        left -= STEPS;
-        if (parts == 2 && left <= 0 && part == 0) {
-            part = 1;
-            left = (int)p.inner;
-            begin_part();
+    const auto next_b = [&]() {
+        advance(b_from, b_stage);
+        b_left -= STEPS;
+        if (--b_until == 0) {
+            if (MODE == INPUT_GRAD && !second_b && to > per_part) {
+                second_b = true;
+                begin_b(1, 0);
+            } else {
+                b_left = INT32_MIN / 2;
+            }
         }
     };
+    const unsigned lds_wave = lds0 + w * FILLS * 1024;
+    const auto fill_a = [&](auto i, unsigned to_part) { fill<i * 1024>(a_from, a_step[i] < a_left ? a_at[i] : NOWHERE, lds_wave + to_part); };
+    const auto fill_b = [&](auto i, unsigned to_part) { fill<i * 1024>(b_from, b_step[i] < b_left ? b_at[i] : NOWHERE, lds_wave + to_part); };
 
     // Where a lane reads a fragment: rows lane % 16 of a tile, steps 8 * (lane / 16) on.
     const int quad = lane >> 4, of16 = lane & 15;
@@ -222,54 +236,72 @@ __global__ __launch_bounds__(64 * WAVES_M * WAVES_N) void k_product(Product p) {
 
     f32x4 acc[TM][TN] = {};
     short8_t fa[2][TM], fb[2][TN];                  // fragments of the two halves of a stage
-    const auto read_b = [&](const char *stage, int half, int j) {
-        if constexpr (B_ACROSS) return read_across(stage + A_BYTES, wn * TN + j, half, BN);
-        else return read_along(stage + A_BYTES + wn * TN * 16 * ROW_BYTES, j, half);
+    const auto read_b = [&](unsigned at, int half, int j) {
+        if constexpr (B_ACROSS) return read_across(ring + at, wn * TN + j, half, BN);
+        else return read_along(ring + at + wn * TN * 16 * ROW_BYTES, j, half);
     };
-    const auto read_a = [&](const char *stage, int half, int i) {
-        if constexpr (A_ACROSS) return read_across(stage, wm * TM + i, half, BM);
-        else return read_along(stage + wm * TM * 16 * ROW_BYTES, i, half);
+    const auto read_a = [&](unsigned at, int half, int i) {
+        if constexpr (A_ACROSS) return read_across(ring + at, wm * TM + i, half, BM);
+        else return read_along(ring + at + wm * TM * 16 * ROW_BYTES, i, half);
     };
-    // The products of one half; meanwhile the fragments of the other are read.
-    const auto multiply = [&](auto half_, auto read_, const char *next) {
+    // The products of one half of a stage, from the fragments, in groups of one tile of rows; before each group some of the other half's
+    // fragments are read (from parts a and b) and what `before` does, in this order.
+    const auto multiply = [&](auto half_, unsigned a, unsigned b, auto &&before) {
         constexpr int half = half_, other = half ^ 1;
-        constexpr bool read = read_;
-#pragma unroll
-        for (int i = 0; i < TM; ++i) {
-            if constexpr (read) {
-                if (i < TN) fb[other][i] = read_b(next, other, i);
-                fa[other][i] = read_a(next, other, i);
+        static_for<0, TM>([&](auto i_) {
+            constexpr int i = i_;
+            __builtin_amdgcn_sched_barrier(0);
+            before(i_);
+            if constexpr (2 * i < TN) {
+                fb[other][2 * i] = read_b(b, other, 2 * i);
+                fb[other][2 * i + 1] = read_b(b, other, 2 * i + 1);
+            } else if constexpr (2 * i - TN < TM) {
+                fa[other][2 * i - TN] = read_a(a, other, 2 * i - TN);
+                fa[other][2 * i - TN + 1] = read_a(a, other, 2 * i - TN + 1);
             }
 #pragma unroll
             for (int j = 0; j < TN; ++j) acc[i][j] = mfma<DT>(fb[half][j], fa[half][i], acc[i][j]);
-        }
+        });
+        __builtin_amdgcn_sched_barrier(0);
     };
-    constexpr std::integral_constant<int, 0> FIRST;
-    constexpr std::integral_constant<int, 1> SECOND;
+    const auto two_on = [](unsigned part) { return part >= 3 * PART ? part - 3 * PART : part + 2 * PART; };
 
     if (from < to) {
-        fill_stage(lds0);
-        if (from + 1 < to) {
-            fill_stage(lds0 + STAGE);
-            all_waves<A_FILLS + B_FILLS>();
-        } else {
-            all_waves<0>();
-        }
+        // a(0) b(0) a(1) b(1) a(2)
+        static_for<0, 5>([&](auto n) {
+            static_for<0, FILLS>([&](auto i) {
+                if constexpr (n % 2 == 0) fill_a(i, n * PART);
+                else fill_b(i, n * PART);
+            });
+            if constexpr (n % 2 == 0) next_a();
+            else next_b();
+        });
+        all_waves<3 * FILLS>();
 #pragma unroll
-        for (int j = 0; j < TN; ++j) fb[0][j] = read_b(stages, 0, j);
+        for (int j = 0; j < TN; ++j) fb[0][j] = read_b(PART, 0, j);
 #pragma unroll
-        for (int i = 0; i < TM; ++i) fa[0][i] = read_a(stages, 0, i);
-        // The second half's products run beside the reads of the next stage's first: by then every wave has read all of this stage, which
-        // is filled again, and the next one, filled a whole stage's time ago, has arrived.
-        unsigned which = 0;
-        for (int t = from; t < to - 1; ++t, which ^= STAGE) {
-            multiply(FIRST, std::true_type{}, stages + which);
-            all_waves<0>();
-            if (t + 2 < to) fill_stage(lds0 + which);
-            multiply(SECOND, std::true_type{}, stages + (which ^ STAGE));
+        for (int i = 0; i < TM; ++i) fa[0][i] = read_a(0, 0, i);
+        // In the middle of stage t all waves have read its parts: they are filled with b(t + 2) and a(t + 3), beside the second half's products;
+        // and stage t + 1 has arrived, whose b was filled a stage's time ago and whose a two.
+        unsigned a = 0, b = PART;
+        for (int t = from; t < to; ++t) {
+            multiply(std::integral_constant<int, 0>{}, a, b, [](auto) {});
+            all_waves<FILLS>();
+            const unsigned a_free = a, b_free = b;
+            a = two_on(a);
+            b = two_on(b);
+            multiply(std::integral_constant<int, 1>{}, a, b, [&](auto i) {
+                constexpr int each = 2 * FILLS / TM;            // 1 or 2
+                static_for<0, each>([&](auto e) {
+                    constexpr std::integral_constant<int, (i * each + e) % FILLS> k;
+                    if constexpr (i * each + e < FILLS) fill_b(k, a_free);
+                    else fill_a(k, b_free);
+                });
+            });
+            next_b();
+            next_a();
         }
-        multiply(FIRST, std::true_type{}, stages + which);
-        multiply(SECOND, std::false_type{}, stages);
+        all_waves<0>();                             // nothing is on its way into the shared memory of the block that comes next
     }
 
     // Of each 16x16 tile a lane holds four columns, 4 * (lane / 16) on, of row lane % 16.
@@ -444,7 +476,7 @@ int64_t partial_bytes(int mode, const Shape &s, int64_t rows, int64_t cols) {
 
 template <int DT, int MODE, int ACT, int BM, int BN, int WAVES_M, int WAVES_N>
 int launch_tiles(const Product &p, hipStream_t st) {
-    constexpr unsigned LDS_BYTES = 2 * (BM + BN) * ROW_BYTES;
+    constexpr unsigned LDS_BYTES = 5 * BM * ROW_BYTES;
     const auto kernel = k_product<DT, MODE, ACT, BM, BN, WAVES_M, WAVES_N>;
     if (LDS_BYTES > 65536) {
         const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void *>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, (int)LDS_BYTES);
@@ -554,7 +586,7 @@ int forward(const paro_gated_t &d, const void *x, const void *wg, const void *wu
     p.ldb = in.ldw * 2;
     p.rows = d.n;
     p.cols = d.hidden;
-    p.inner = up_to(d.dim, 8);
+    p.inner = p.inner_b = up_to(d.dim, 8);
     p.out[0] = static_cast<char *>(h);
     p.out[1] = static_cast<char *>(gate);
     p.out[2] = static_cast<char *>(up);

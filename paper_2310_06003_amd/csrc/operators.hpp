@@ -8,6 +8,7 @@
 #include <cstdint>
 #include <exception>
 #include <string>
+#include <type_traits>
 
 #include "plan.hpp"
 
@@ -23,6 +24,15 @@ typedef float f32x4 __attribute__((ext_vector_type(4)));
         const hipError_t e_ = hipGetLastError();                                                         \
         if (e_ != hipSuccess) return fail(PARO_EHIP, std::string(what ": ") + hipGetErrorString(e_));    \
     } while (0)
+
+// Compile-time loop: the body sees its index as a constant.
+template <int I, int N, class F>
+__device__ __forceinline__ void static_for(F &&f) {
+    if constexpr (I < N) {
+        f(std::integral_constant<int, I>{});
+        static_for<I + 1, N>(f);
+    }
+}
 
 // Nothing is thrown across the C boundary: fail() makes strings.
 template <class F>
