@@ -84,21 +84,71 @@ struct Product {
     int64_t inner_b;                     // steps that b has (across: rows)
     char *out[3];                        // h, g, u; dx; dWg, dWu
     int64_t ldo;                         // elements
-    float *partial;                      // splits > 1: [split][rows][cols of all parts], fp32
-    int64_t ldp;
-    int tiles_m, tiles_n, splits;
+    int tiles_m, tiles_n;
+    unsigned whole, splits;              // the first tiles are whole blocks' work; of the others each is split among so many blocks,
+    float *partial;                      // which leave their sums here: [tile][split][row of tiles][tile][thread][4]
 };
 
-// Which tile a block computes.  Blocks go to the eight XCDs in turn: each takes a run of tiles of its own, eight tiles of rows
-// wide, so that what its blocks read at a time stays in its L2.
-__device__ __forceinline__ void tile_of(unsigned block, int tiles_m, int tiles_n, int &tm, int &tn) {
-    const unsigned all = tiles_m * tiles_n, each = all / 8, more = all % 8, xcd = block % 8;
-    const unsigned t = xcd * each + (xcd < more ? xcd : more) + block / 8;
-    constexpr unsigned WIDE = 8;
-    const unsigned band = t / (WIDE * tiles_n), first = band * WIDE, in = t - band * WIDE * tiles_n;
-    const unsigned high = tiles_m - first < WIDE ? tiles_m - first : WIDE;
-    tm = first + in % high;
-    tn = in / high;
+// Blocks go to the eight XCDs in turn: each takes a run of tiles of its own.
+__device__ __forceinline__ unsigned in_runs(unsigned block, unsigned all) {
+    const unsigned each = all / 8, more = all % 8, xcd = block % 8;
+    return xcd * each + (xcd < more ? xcd : more) + block / 8;
+}
+// Where tile t of the result lies.  Runs go four tiles of rows wide, so that what an XCD's blocks read at a time stays in its L2 (eight wide:
+// 4096 tokens of 4096 x 11008 forward 603 us, so 593; 8192 backward 2395 and 2353).
+template <int MODE, int BM, int BN>
+struct Place {
+    int part;                            // dW: the first half of the tiles of rows is dWg
+    int64_t row0, col0;
+    __device__ __forceinline__ Place(const Product &p, unsigned t) {
+        constexpr unsigned WIDE = 4;
+        const unsigned band = t / (WIDE * p.tiles_n), first = band * WIDE, in = t - band * WIDE * p.tiles_n;
+        const unsigned high = p.tiles_m - first < WIDE ? p.tiles_m - first : WIDE;
+        const int tm = first + in % high, tn = in / high, of_part = p.tiles_m / 2;
+        part = MODE == WEIGHT_GRAD && tm >= of_part;
+        row0 = (int64_t)(tm - part * of_part) * BM;
+        col0 = (int64_t)tn * (MODE == FORWARD ? BN / 2 : BN);
+    }
+};
+
+// Of each 16x16 tile a lane holds four columns, 4 * (lane / 16) on, of row lane % 16.  Two tiles of columns side by side are stored
+// together: quads exchange halves, so that each lane has eight columns in a row.
+template <int DT>
+__device__ __forceinline__ void store8(const Product &p, char *out, int64_t m, int64_t n, const f32x4 &left, const f32x4 &right) {
+    const int quad = (threadIdx.x >> 4) & 3;
+    const u32x2_t a{pack2<DT>(left[0], left[1]), pack2<DT>(left[2], left[3])}, b{pack2<DT>(right[0], right[1]), pack2<DT>(right[2], right[3])};
+    const auto s0 = __builtin_amdgcn_permlane16_swap(a[0], b[0], false, false);
+    const auto s1 = __builtin_amdgcn_permlane16_swap(a[1], b[1], false, false);
+    const u32x4 v{s0[0], s1[0], s0[1], s1[1]};
+    n += (quad & 1) * 16 + (quad >> 1) * 8;
+    if (m >= p.rows || n >= p.cols) return;
+    if (n + 8 <= p.cols) {
+        store_piece<DT>(out, m * p.ldo + n, v);
+    } else {
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+            if (n + e < p.cols) reinterpret_cast<unsigned short *>(out)[m * p.ldo + n + e] = (unsigned short)(v[e / 2] >> (16 * (e & 1)));
+    }
+}
+// What a wave does with a finished row of its tiles.
+template <int DT, int MODE, int ACT, int BM, int BN>
+__device__ __forceinline__ void finish(const Product &p, const Place<MODE, BM, BN> &at, int64_t m, int wn, const f32x4 (&acc)[4]) {
+    if constexpr (MODE == FORWARD) {
+        f32x4 h[2];
+#pragma unroll
+        for (int j = 0; j < 2; ++j)
+#pragma unroll
+            for (int q = 0; q < 4; ++q) h[j][q] = act<ACT>(acc[j][q]) * acc[j + 2][q];
+        const int64_t n = at.col0 + wn * 32;
+        store8<DT>(p, p.out[0], m, n, h[0], h[1]);
+        if (p.out[1]) {
+            store8<DT>(p, p.out[1], m, n, acc[0], acc[1]);
+            store8<DT>(p, p.out[2], m, n, acc[2], acc[3]);
+        }
+    } else {
+#pragma unroll
+        for (int j = 0; j < 4; j += 2) store8<DT>(p, p.out[at.part], m, at.col0 + (wn * 4 + j) * 16, acc[j], acc[j + 1]);
+    }
 }
 
 template <int DT, int MODE, int ACT, int BM, int BN, int WAVES_M, int WAVES_N>
@@ -112,16 +162,14 @@ __global__ __launch_bounds__(64 * WAVES_M * WAVES_N) void k_product(Product p) {
     extern __shared__ __attribute__((aligned(1024))) char ring[];
     const unsigned lds0 = (unsigned)(uintptr_t)(lds_char *)ring;
     const int w = wave_of(), lane = threadIdx.x & 63, wm = w / WAVES_N, wn = w % WAVES_N;
-    int tm, tn;
-    tile_of(blockIdx.x, p.tiles_m, p.tiles_n, tm, tn);
-    const int64_t m0 = (int64_t)tm * BM;
-
-    // The tile's operands: where they begin, and how many bytes from there may be read at step 0.
-    constexpr int HALF_N = BN / 2;
-    const int64_t n_tiles_part = MODE == WEIGHT_GRAD ? p.tiles_m / 2 : 0;     // dW: the first half of the tiles of rows is dWg
-    const int out_part = MODE == WEIGHT_GRAD ? tm >= n_tiles_part : 0;
-    const int64_t row0 = MODE == WEIGHT_GRAD ? m0 - out_part * n_tiles_part * BM : m0;
-    const int64_t col0 = (int64_t)tn * (MODE == FORWARD ? HALF_N : BN);
+    // The block's tile, and its share of the inner dimension.
+    const bool is_whole = blockIdx.x < p.whole;
+    const unsigned others = is_whole ? 0 : (gridDim.x - p.whole) / p.splits, among = is_whole ? 0 : blockIdx.x - p.whole;
+    const unsigned split = is_whole ? 0 : among / others, split_tile = is_whole ? 0 : in_runs(among - split * others, others);
+    const unsigned splits = is_whole ? 1 : p.splits;
+    const Place<MODE, BM, BN> at(p, is_whole ? in_runs(blockIdx.x, p.whole) : p.whole + split_tile);
+    const int64_t row0 = at.row0, col0 = at.col0;
+    const int out_part = at.part;
 
     // A lane's pieces: their offsets from where the stage begins, and the step (along: the first of eight) of each.  The pieces of a
     // stage are exchanged within 256 bytes such that the lanes that read at a time meet all banks.  Pieces of rows or columns that the operand
@@ -165,7 +213,7 @@ __global__ __launch_bounds__(64 * WAVES_M * WAVES_N) void k_product(Product p) {
 
     const int per_part = (int)((p.inner + STEPS - 1) / STEPS), parts = MODE == INPUT_GRAD ? 2 : 1;
     const int stages_all = per_part * parts;
-    const int from = (int)((int64_t)stages_all * blockIdx.y / p.splits), to = (int)((int64_t)stages_all * (blockIdx.y + 1) / p.splits);
+    const int from = (int)((int64_t)stages_all * split / splits), to = (int)((int64_t)stages_all * (split + 1) / splits);
 
     // What the next stage is filled from.
     u32x4 a_from, b_from;
@@ -304,87 +352,133 @@ __global__ __launch_bounds__(64 * WAVES_M * WAVES_N) void k_product(Product p) {
         all_waves<0>();                             // nothing is on its way into the shared memory of the block that comes next
     }
 
-    // Of each 16x16 tile a lane holds four columns, 4 * (lane / 16) on, of row lane % 16.
-    if (p.splits > 1) {
-        float *to_part = p.partial + (int64_t)blockIdx.y * (MODE == WEIGHT_GRAD ? 2 : 1) * p.rows * p.ldp;
+    if (splits > 1) {
+        float *sums = p.partial + ((int64_t)(split_tile * splits + split) * (TM * TN) * THREADS_ + threadIdx.x) * 4;
 #pragma unroll
-        for (int i = 0; i < TM; ++i) {
-            const int64_t m = row0 + (wm * TM + i) * 16 + of16;
-            if (m >= p.rows) continue;
+        for (int i = 0; i < TM; ++i)
+            if (row0 + (wm * TM + i) * 16 + of16 < p.rows)
 #pragma unroll
-            for (int j = 0; j < TN; ++j) {
-                const int64_t in = MODE == FORWARD ? wn * 32 + (j & 1) * 16 + quad * 4 : (wn * TN + j) * 16 + quad * 4;
-                const int64_t n = col0 + in, width = p.ldp / (MODE == FORWARD ? 2 : 1);
-                if (n < width) *reinterpret_cast<f32x4 *>(to_part + (out_part * p.rows + m) * p.ldp + (MODE == FORWARD ? (j >> 1) * width : 0) + n) = acc[i][j];
-            }
-        }
+                for (int j = 0; j < TN; ++j) *reinterpret_cast<f32x4 *>(sums + (int64_t)(i * TN + j) * THREADS_ * 4) = acc[i][j];
         return;
     }
-    // Two tiles of columns side by side: quads exchange halves, so that each lane has eight columns in a row.
-    const auto store8 = [&](char *out, int64_t m, int64_t n, const f32x4 &left, const f32x4 &right) {
-        u32x2_t a{pack2<DT>(left[0], left[1]), pack2<DT>(left[2], left[3])}, b{pack2<DT>(right[0], right[1]), pack2<DT>(right[2], right[3])};
-        const auto s0 = __builtin_amdgcn_permlane16_swap(a[0], b[0], false, false);
-        const auto s1 = __builtin_amdgcn_permlane16_swap(a[1], b[1], false, false);
-        const u32x4 v{s0[0], s1[0], s0[1], s1[1]};
-        n += (quad & 1) * 16 + (quad >> 1) * 8;
-        if (m >= p.rows || n >= p.cols) return;
-        if (n + 8 <= p.cols) {
-            store_piece<DT>(out, m * p.ldo + n, v);
-        } else {
 #pragma unroll
-            for (int e = 0; e < 8; ++e)
-                if (n + e < p.cols) reinterpret_cast<unsigned short *>(out)[m * p.ldo + n + e] = (unsigned short)(v[e / 2] >> (16 * (e & 1)));
-        }
-    };
-#pragma unroll
-    for (int i = 0; i < TM; ++i) {
-        const int64_t m = row0 + (wm * TM + i) * 16 + of16;
-        if constexpr (MODE == FORWARD) {
-            f32x4 h[2];
-#pragma unroll
-            for (int j = 0; j < 2; ++j)
-#pragma unroll
-                for (int q = 0; q < 4; ++q) h[j][q] = act<ACT>(acc[i][j][q]) * acc[i][j + 2][q];
-            const int64_t n = col0 + wn * 32;
-            store8(p.out[0], m, n, h[0], h[1]);
-            if (p.out[1]) {
-                store8(p.out[1], m, n, acc[i][0], acc[i][1]);
-                store8(p.out[2], m, n, acc[i][2], acc[i][3]);
-            }
-        } else {
-#pragma unroll
-            for (int j = 0; j < TN; j += 2) store8(p.out[out_part], m, col0 + (wn * TN + j) * 16, acc[i][j], acc[i][j + 1]);
-        }
-    }
+    for (int i = 0; i < TM; ++i) finish<DT, MODE, ACT>(p, at, row0 + (wm * TM + i) * 16 + of16, wn, acc[i]);
 }
 
-// Sums of a split product's parts, in order, and what its epilogue does.  A thread for four columns.
-template <int DT, int MODE, int ACT>
-__global__ __launch_bounds__(256) void k_join_splits(Product p) {
-    const int parts = MODE == WEIGHT_GRAD ? 2 : 1;
-    const int64_t width = p.ldp / (MODE == FORWARD ? 2 : 1), per_row = width / 4, all = parts * p.rows * per_row;
-    const int64_t stride = (int64_t)parts * p.rows * p.ldp;
-    for (int64_t e = (int64_t)blockIdx.x * 256 + threadIdx.x; e < all; e += (int64_t)gridDim.x * 256) {
-        const int64_t row = e / per_row, n = (e - row * per_row) * 4;
-        f32x4 sum[2] = {};
-        for (int s = 0; s < p.splits; ++s) {
-            const float *at = p.partial + s * stride + row * p.ldp + n;
-            sum[0] += *reinterpret_cast<const f32x4 *>(at);
-            if constexpr (MODE == FORWARD) sum[1] += *reinterpret_cast<const f32x4 *>(at + width);
+// Adds up the sums of a split tile's blocks, in order: a block for each row of a wave's tiles.
+template <int DT, int MODE, int ACT, int BM, int BN, int WAVES_M, int WAVES_N>
+__global__ __launch_bounds__(64 * WAVES_M * WAVES_N) void k_join(Product p) {
+    constexpr int THREADS_ = 64 * WAVES_M * WAVES_N, TM = BM / WAVES_M / 16, TN = 4;
+    const int w = wave_of(), i = blockIdx.y;
+    const Place<MODE, BM, BN> at(p, p.whole + blockIdx.x);
+    const int64_t m = at.row0 + ((w / WAVES_N) * TM + i) * 16 + (threadIdx.x & 15);
+    f32x4 acc[TN] = {};
+    if (m < p.rows) {
+        const float *sums = p.partial + ((int64_t)blockIdx.x * p.splits * (TM * TN) * THREADS_ + (int64_t)i * TN * THREADS_ + threadIdx.x) * 4;
+#pragma unroll 4
+        for (unsigned s = 0; s < p.splits; ++s)
+#pragma unroll
+            for (int j = 0; j < TN; ++j) acc[j] += *reinterpret_cast<const f32x4 *>(sums + ((int64_t)s * TM * TN + j) * THREADS_ * 4);
+    }
+    finish<DT, MODE, ACT>(p, at, m, w % WAVES_N, acc);
+}
+
+// Forward for few tokens: the weights are read once, straight into registers as fragments, and nothing else counts.  A block takes F_TILES x
+// 16 hidden elements; its waves share the inner dimension, 128 steps at a time in turn, and join their sums in shared memory.  Rows need no
+// alignment.  Rows of weights and tokens past the last one are read as the last one, and not stored.
+constexpr int FEW_WAVES = 4, FEW_STEPS = 128;
+
+template <int DT>
+__device__ __forceinline__ short8_t piece_or_zeros(const void *row, int64_t k, int64_t dim) {
+    if (k + 8 <= dim) return __builtin_bit_cast(short8_t, load_piece<DT>(row, k));
+    u32x4 v{0, 0, 0, 0};
+#pragma unroll
+    for (int e = 0; e < 8; ++e)
+        if (k + e < dim) v[e / 2] |= (unsigned)static_cast<const unsigned short *>(row)[k + e] << (16 * (e & 1));
+    return __builtin_bit_cast(short8_t, v);
+}
+
+template <int DT, int ACT, int F_TILES, int N_TILES>
+__global__ __launch_bounds__(64 * FEW_WAVES) void k_few(const char *x, const char *wg, const char *wu, int64_t n, int64_t dim, int64_t hidden, int64_t ldx,
+                                                        int64_t ldh, char *h, char *gate, char *up) {
+    __shared__ f32x4 sums[FEW_WAVES][F_TILES * 2 * N_TILES][64];
+    const int w = wave_of(), lane = threadIdx.x & 63, quad = lane >> 4, of16 = lane & 15;
+    const int64_t f0 = (int64_t)blockIdx.x * (F_TILES * 16);
+    const char *weights[F_TILES][2], *tokens[N_TILES];
+#pragma unroll
+    for (int i = 0; i < F_TILES; ++i) {
+        const int64_t f = f0 + i * 16 + of16 < hidden ? f0 + i * 16 + of16 : hidden - 1;
+        weights[i][0] = wg + f * dim * 2;
+        weights[i][1] = wu + f * dim * 2;
+    }
+#pragma unroll
+    for (int t = 0; t < N_TILES; ++t) tokens[t] = x + (t * 16 + of16 < n ? t * 16 + of16 : n - 1) * ldx * 2;
+
+    f32x4 acc[F_TILES][2][N_TILES] = {};
+    for (int64_t k0 = (int64_t)w * FEW_STEPS; k0 < dim; k0 += FEW_WAVES * FEW_STEPS) {
+        constexpr int PIECES = FEW_STEPS / 32;
+        if (k0 + FEW_STEPS <= dim) {
+            short8_t a[PIECES][F_TILES][2], b[PIECES][N_TILES];
+#pragma unroll
+            for (int c = 0; c < PIECES; ++c) {
+                const int64_t k = k0 + c * 32 + quad * 8;
+#pragma unroll
+                for (int i = 0; i < F_TILES; ++i)
+#pragma unroll
+                    for (int of = 0; of < 2; ++of) a[c][i][of] = __builtin_bit_cast(short8_t, load_piece<DT>(weights[i][of], k));
+#pragma unroll
+                for (int t = 0; t < N_TILES; ++t) b[c][t] = __builtin_bit_cast(short8_t, load_piece<DT>(tokens[t], k));
+            }
+#pragma unroll
+            for (int c = 0; c < PIECES; ++c)
+#pragma unroll
+                for (int i = 0; i < F_TILES; ++i)
+#pragma unroll
+                    for (int of = 0; of < 2; ++of)
+#pragma unroll
+                        for (int t = 0; t < N_TILES; ++t) acc[i][of][t] = mfma<DT>(a[c][i][of], b[c][t], acc[i][of][t]);
+        } else {
+            for (int64_t k1 = k0; k1 < dim; k1 += 32) {
+                const int64_t k = k1 + quad * 8;
+                short8_t b[N_TILES];
+#pragma unroll
+                for (int t = 0; t < N_TILES; ++t) b[t] = piece_or_zeros<DT>(tokens[t], k, dim);
+#pragma unroll
+                for (int i = 0; i < F_TILES; ++i)
+#pragma unroll
+                    for (int of = 0; of < 2; ++of) {
+                        const short8_t a = piece_or_zeros<DT>(weights[i][of], k, dim);
+#pragma unroll
+                        for (int t = 0; t < N_TILES; ++t) acc[i][of][t] = mfma<DT>(a, b[t], acc[i][of][t]);
+                    }
+            }
         }
-        const int part = MODE == WEIGHT_GRAD && row >= p.rows;
-        const int64_t m = row - part * p.rows;
+    }
+#pragma unroll
+    for (int i = 0; i < F_TILES; ++i)
+#pragma unroll
+        for (int of = 0; of < 2; ++of)
+#pragma unroll
+            for (int t = 0; t < N_TILES; ++t) sums[w][(i * 2 + of) * N_TILES + t][lane] = acc[i][of][t];
+    __syncthreads();
+    // A lane holds four hidden elements, 4 * (lane / 16) on, of token lane % 16 of each pair of tiles.
+    for (int pair = w; pair < F_TILES * N_TILES; pair += FEW_WAVES) {
+        const int i = pair / N_TILES, t = pair - i * N_TILES;
+        f32x4 g{}, u{};
+#pragma unroll
+        for (int k = 0; k < FEW_WAVES; ++k) {
+            g += sums[k][(i * 2) * N_TILES + t][lane];
+            u += sums[k][(i * 2 + 1) * N_TILES + t][lane];
+        }
+        const int64_t m = t * 16 + of16, f = f0 + i * 16 + quad * 4;
+        if (m >= n) continue;
 #pragma unroll
         for (int q = 0; q < 4; ++q) {
-            if (n + q >= p.cols) break;
-            if constexpr (MODE == FORWARD) {
-                store_one<DT>(p.out[0], m * p.ldo + n + q, act<ACT>(sum[0][q]) * sum[1][q]);
-                if (p.out[1]) {
-                    store_one<DT>(p.out[1], m * p.ldo + n + q, sum[0][q]);
-                    store_one<DT>(p.out[2], m * p.ldo + n + q, sum[1][q]);
-                }
-            } else {
-                store_one<DT>(p.out[part], m * p.ldo + n + q, sum[0][q]);
+            if (f + q >= hidden) break;
+            store_one<DT>(h, m * ldh + f + q, act<ACT>(g[q]) * u[q]);
+            if (gate) {
+                store_one<DT>(gate, m * ldh + f + q, g[q]);
+                store_one<DT>(up, m * ldh + f + q, u[q]);
             }
         }
     }
@@ -444,13 +538,15 @@ __global__ __launch_bounds__(256) void k_align(const void *from, int64_t ld, int
 int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 int64_t up_to(int64_t a, int64_t b) { return ceil_div(a, b) * b; }
 constexpr int COMPUTE_UNITS = 256;
+constexpr int64_t MIN_SAVED = 16;        // stages
 
 bool fills_take(const void *p, int64_t ld, int64_t cols) { return !(reinterpret_cast<uintptr_t>(p) & 15) && ld % 8 == 0 && cols % 8 == 0; }
 
 struct Shape {                           // of a product's launch
     bool large;                          // tiles of 256 x 256, else 128 x 128
-    int64_t tiles_m, tiles_n;
-    int splits;
+    int64_t tiles_m, tiles_n, whole, splits;
+    int64_t blocks() const { return whole + (tiles_m * tiles_n - whole) * splits; }
+    int64_t partial_bytes() const { return splits > 1 ? (tiles_m * tiles_n - whole) * splits * (large ? 256 * 256 : 128 * 128) * 4 : 0; }
 };
 // rows and columns: of the result (of WEIGHT_GRAD of one part, of FORWARD of both parts)
 Shape shape_of(int mode, int64_t rows, int64_t cols, int64_t inner) {
@@ -465,24 +561,27 @@ Shape shape_of(int mode, int64_t rows, int64_t cols, int64_t inner) {
     const int64_t n = s.large ? n256 : tiles(128, s.tiles_m, s.tiles_n);
     const int64_t at_once = s.large ? COMPUTE_UNITS : 2 * COMPUTE_UNITS;
     const int64_t stages = ceil_div(inner, STEPS) * (mode == INPUT_GRAD ? 2 : 1);
-    // few tiles: the inner dimension is split, into parts of at least eight stages
-    s.splits = (int)std::max<int64_t>(1, std::min<int64_t>({at_once / std::max<int64_t>(n, 1), stages / 8, 16}));
+    // The tiles beyond whole rounds are split, so that their blocks fill the chip once: into shares of at least eight stages, and where
+    // that saves more than the joining costs.
+    s.whole = n / at_once * at_once;
+    s.splits = n > s.whole ? std::max<int64_t>(1, std::min<int64_t>({at_once / (n - s.whole), stages / 8, 16})) : 1;
+    if (stages - stages / s.splits < MIN_SAVED) s.splits = 1;
+    if (s.splits == 1) s.whole = n;
     return s;
-}
-int64_t partial_bytes(int mode, const Shape &s, int64_t rows, int64_t cols) {
-    if (s.splits == 1) return 0;
-    return s.splits * rows * up_to(cols, 4) * 4 * (mode == INPUT_GRAD ? 1 : 2);
 }
 
 template <int DT, int MODE, int ACT, int BM, int BN, int WAVES_M, int WAVES_N>
-int launch_tiles(const Product &p, hipStream_t st) {
-    constexpr unsigned LDS_BYTES = 5 * BM * ROW_BYTES;
+int launch_tiles(const Product &p, const Shape &s, hipStream_t st) {
+    constexpr unsigned LDS_BYTES = 5 * BM * ROW_BYTES, THREADS_ = 64 * WAVES_M * WAVES_N;
     const auto kernel = k_product<DT, MODE, ACT, BM, BN, WAVES_M, WAVES_N>;
     if (LDS_BYTES > 65536) {
         const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void *>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, (int)LDS_BYTES);
         if (e != hipSuccess) return fail(PARO_EHIP, std::string("shared memory: ") + hipGetErrorString(e));
     }
-    hipLaunchKernelGGL(kernel, dim3((unsigned)(p.tiles_m * p.tiles_n), (unsigned)p.splits), dim3(64 * WAVES_M * WAVES_N), LDS_BYTES, st, p);
+    hipLaunchKernelGGL(kernel, dim3((unsigned)s.blocks()), dim3(THREADS_), LDS_BYTES, st, p);
+    if (s.splits > 1)
+        hipLaunchKernelGGL((k_join<DT, MODE, ACT, BM, BN, WAVES_M, WAVES_N>), dim3((unsigned)(s.tiles_m * s.tiles_n - s.whole), BM / WAVES_M / 16),
+                           dim3(THREADS_), 0, st, p);
     return PARO_OK;
 }
 
@@ -490,16 +589,10 @@ template <int DT, int MODE, int ACT>
 int launch_product(Product p, const Shape &s, float *partial, hipStream_t st) {
     p.tiles_m = (int)s.tiles_m;
     p.tiles_n = (int)s.tiles_n;
-    p.splits = s.splits;
+    p.whole = (unsigned)s.whole;
+    p.splits = (unsigned)s.splits;
     p.partial = partial;
-    p.ldp = up_to(p.cols, 4) * (MODE == FORWARD ? 2 : 1);
-    const int rc = s.large ? launch_tiles<DT, MODE, ACT, 256, 256, 2, 4>(p, st) : launch_tiles<DT, MODE, ACT, 128, 128, 2, 2>(p, st);
-    if (rc) return rc;
-    if (s.splits > 1) {
-        const int64_t threads = (MODE == WEIGHT_GRAD ? 2 : 1) * p.rows * (up_to(p.cols, 4) / 4);
-        hipLaunchKernelGGL((k_join_splits<DT, MODE, ACT>), dim3((unsigned)std::min<int64_t>(ceil_div(threads, 256), 8192)), dim3(256), 0, st, p);
-    }
-    return PARO_OK;
+    return s.large ? launch_tiles<DT, MODE, ACT, 256, 256, 2, 4>(p, s, st) : launch_tiles<DT, MODE, ACT, 128, 128, 2, 2>(p, s, st);
 }
 
 struct Room {                            // parts of the workspace, in bytes
@@ -521,10 +614,9 @@ Room room_of(const paro_gated_t &d, bool grad) {
     int64_t partial = 0;
     if (grad) {
         r.slopes = take(d.n * 2 * up_to(d.hidden, 8) * 2);
-        partial = std::max(partial_bytes(INPUT_GRAD, shape_of(INPUT_GRAD, d.n, d.dim, d.hidden), d.n, d.dim),
-                           partial_bytes(WEIGHT_GRAD, shape_of(WEIGHT_GRAD, d.hidden, d.dim, d.n), d.hidden, d.dim));
+        partial = std::max(shape_of(INPUT_GRAD, d.n, d.dim, d.hidden).partial_bytes(), shape_of(WEIGHT_GRAD, d.hidden, d.dim, d.n).partial_bytes());
     } else {
-        partial = partial_bytes(FORWARD, shape_of(FORWARD, d.n, d.hidden, d.dim), d.n, d.hidden);
+        partial = shape_of(FORWARD, d.n, d.hidden, d.dim).partial_bytes();
     }
     r.partial = take(partial);
     r.all = std::max<int64_t>(at, 16);
@@ -574,9 +666,26 @@ Inputs inputs_of(const paro_gated_t &d, const void *x, const void *wg, const voi
     return in;
 }
 
+// Which forward passes k_few takes (otherwise tiles of 128 rows, most of them empty, in us): up to 16 tokens, 4096 x 11008 with 1 token 38 (44), 8 44
+// (48), 12 47 (47), 4096 x 4096 with 16 19 (21), 4099 x 11003 with 16 90 (127); up to 64 over small weights, 1024 x 4096 with 32 12 (17), 768 x 2048 with
+// 64 12 (15), but 2048 x 5632 with 32 21 (19), 4096 x 11008 with 32 63 (50): beyond, the tokens that every block reads again outweigh.
+bool few_tokens(int64_t n, int64_t dim, int64_t hidden) { return n <= 16 || (n <= 64 && dim * hidden <= (int64_t)4 << 20); }
+
 template <int DT, int ACT>
 int forward(const paro_gated_t &d, const void *x, const void *wg, const void *wu, void *h, void *gate, void *up, char *ws, const Room &r,
             hipStream_t st) {
+    if (few_tokens(d.n, d.dim, d.hidden)) {
+#define PARO_FEW(F_TILES, N_TILES)                                                                                                         \
+    hipLaunchKernelGGL((k_few<DT, ACT, F_TILES, N_TILES>), dim3((unsigned)ceil_div(d.hidden, 16 * F_TILES)), dim3(64 * FEW_WAVES), 0, st,          \
+                       static_cast<const char *>(x), static_cast<const char *>(wg), static_cast<const char *>(wu), d.n, d.dim, d.hidden,   \
+                       d.ld_x ? d.ld_x : d.dim, d.ld_h ? d.ld_h : d.hidden, static_cast<char *>(h), static_cast<char *>(gate),             \
+                       static_cast<char *>(up))
+        if (d.n <= 16) PARO_FEW(1, 1);
+        else if (d.n <= 32) PARO_FEW(1, 2);
+        else PARO_FEW(1, 4);
+#undef PARO_FEW
+        return PARO_OK;
+    }
     const Inputs in = inputs_of(d, x, wg, wu, ws, r, st);
     Product p{};
     p.a[0] = in.x;
