@@ -384,7 +384,8 @@ int paro_distill_step(const paro_distill_t *d, const void *logits, const void *t
 
 /* The gated projections of a feed-forward block (the product that follows, with the down projection, is a plain one):
  *   g = x Wg', u = x Wu', h = act(g) * u        act: silu(g) = g / (1 + exp(-g)), or gelu(g) = g/2 (1 + erf(g / sqrt 2))
- * x: [n][dim], ld_x apart; Wg, Wu: [hidden][dim]; h, g, u: [n][hidden], ld_h apart.  dtype: PARO_BF16 or PARO_F16.  g and u are
+ * x: [n][dim], ld_x apart; Wg, Wu: [hidden][dim]; h, g, u: [n][hidden], ld_h apart.  dtype: PARO_BF16 or PARO_F16.  Where dim (and
+ * ld_x) are multiples of 8, x and the weights are 16-byte aligned; otherwise their rows are copied into the workspace.  g and u are
  * stored for the backward pass, or NULL both; h is formed from their fp32 values.  n == 0 is nothing to do. */
 enum { PARO_SILU = 0, PARO_GELU = 1 };
 typedef struct {

@@ -518,19 +518,28 @@ __global__ __launch_bounds__(256) void k_slopes(const void *dh, const void *gate
     }
 }
 
-// Rows that the fills cannot take - a row or the distance between two is no multiple of 16 bytes - copied to where they can, zeros behind.
-__global__ __launch_bounds__(256) void k_align(const void *from, int64_t ld, int64_t rows, int64_t cols, int64_t width, void *to) {
+// Rows that the fills cannot take - a row or the distance between two is no multiple of 16 bytes - copied to where they can, zeros behind:
+// up to three arrays of one width in a launch.
+struct Copies {
+    const void *from[3];
+    void *to[3];
+    int64_t ld[3], rows[3];
+    int64_t cols, width;
+};
+__global__ __launch_bounds__(256) void k_align(Copies a) {
+    const int which = blockIdx.z;
+    const void *from = a.from[which];
     const int64_t c = ((int64_t)blockIdx.x * 256 + threadIdx.x) * 8;
-    if (c >= width) return;
-    for (int64_t r = blockIdx.y; r < rows; r += gridDim.y) {
+    if (c >= a.width) return;
+    for (int64_t r = blockIdx.y; r < a.rows[which]; r += gridDim.y) {
         u32x4 v{0, 0, 0, 0};
-        if (c + 8 <= cols) {
-            v = load_piece<PARO_BF16>(from, r * ld + c);
+        if (c + 8 <= a.cols) {
+            v = load_piece<PARO_BF16>(from, r * a.ld[which] + c);
         } else {
             for (int e = 0; e < 8; ++e)
-                if (c + e < cols) v[e / 2] |= (unsigned)static_cast<const unsigned short *>(from)[r * ld + c + e] << (16 * (e & 1));
+                if (c + e < a.cols) v[e / 2] |= (unsigned)static_cast<const unsigned short *>(from)[r * a.ld[which] + c + e] << (16 * (e & 1));
         }
-        store_piece<PARO_BF16>(to, r * width + c, v);
+        store_piece<PARO_BF16>(a.to[which], r * a.width + c, v);
     }
 }
 
@@ -540,7 +549,8 @@ int64_t up_to(int64_t a, int64_t b) { return ceil_div(a, b) * b; }
 constexpr int COMPUTE_UNITS = 256;
 constexpr int64_t MIN_SAVED = 16;        // stages
 
-bool fills_take(const void *p, int64_t ld, int64_t cols) { return !(reinterpret_cast<uintptr_t>(p) & 15) && ld % 8 == 0 && cols % 8 == 0; }
+// Whether rows can be filled as they are (their array is 16-byte aligned then: see check_inputs).
+bool fills_take(int64_t ld, int64_t cols) { return ld % 8 == 0 && cols % 8 == 0; }
 
 struct Shape {                           // of a product's launch
     bool large;                          // tiles of 256 x 256, else 128 x 128
@@ -598,19 +608,23 @@ int launch_product(Product p, const Shape &s, float *partial, hipStream_t st) {
 struct Room {                            // parts of the workspace, in bytes
     int64_t x, wg, wu, slopes, partial, all;
 };
+int64_t ld_x(const paro_gated_t &d) { return d.ld_x ? d.ld_x : d.dim; }
+int64_t ld_h(const paro_gated_t &d) { return d.ld_h ? d.ld_h : d.hidden; }
+
 Room room_of(const paro_gated_t &d, bool grad) {
-    const int64_t width = up_to(d.dim, 8), up256 = 256;
+    const int64_t width = up_to(d.dim, 8);
     Room r{};
     int64_t at = 0;
     const auto take = [&](int64_t bytes) {
         const int64_t here = at;
-        at += up_to(bytes, up256);
+        at += up_to(bytes, 256);
         return here;
     };
-    // whether the rows have to be copied depends on addresses as well: there is always room for it
-    r.x = take(d.n * width * 2);
-    r.wg = take(d.hidden * width * 2);
-    r.wu = take(d.hidden * width * 2);
+    if (!fills_take(ld_x(d), d.dim)) r.x = take(d.n * width * 2);
+    if (!fills_take(d.dim, d.dim)) {
+        r.wg = take(d.hidden * width * 2);
+        r.wu = take(d.hidden * width * 2);
+    }
     int64_t partial = 0;
     if (grad) {
         r.slopes = take(d.n * 2 * up_to(d.hidden, 8) * 2);
@@ -623,16 +637,6 @@ Room room_of(const paro_gated_t &d, bool grad) {
     return r;
 }
 
-// The rows as they are, or in a copy that the fills take.
-const char *taken(const void *rows, int64_t &ld, int64_t n, int64_t cols, bool as_they_are, char *copy, hipStream_t st) {
-    if (as_they_are) return static_cast<const char *>(rows);
-    const int64_t width = up_to(cols, 8);
-    hipLaunchKernelGGL(k_align, dim3((unsigned)ceil_div(width, 8 * 256), (unsigned)std::min<int64_t>(n, 65535)), dim3(256), 0, st, rows, ld, n, cols, width,
-                       copy);
-    ld = width;
-    return copy;
-}
-
 int check(const std::string &f, const paro_gated_t *d) {
     if (!d) return fail(PARO_EINVAL, f + "d is NULL");
     if (d->dtype != PARO_BF16 && d->dtype != PARO_F16) return fail(PARO_EINVAL, f + "dtype must be PARO_BF16 or PARO_F16");
@@ -643,26 +647,56 @@ int check(const std::string &f, const paro_gated_t *d) {
     if (d->ld_x > (1 << 21) || d->ld_h > (1 << 21)) return fail(PARO_EINVAL, f + "ld_x and ld_h are at most 2^21");
     return PARO_OK;
 }
+// Where rows of x or of the weights lie on multiples of 16 bytes, so does their array.
+int check_inputs(const std::string &f, const paro_gated_t *d, const void *x, const void *w_gate, const void *w_up) {
+    const int64_t of_w = fills_take(d->dim, d->dim) ? 16 : 2, of_x = fills_take(ld_x(*d), d->dim) ? 16 : 2;
+    int rc = PARO_OK;
+    const auto check_one = [&](const void *p, int64_t size, const char *name) {
+        if (rc) return;
+        rc = check_array(p, 2, f + name);
+        if (!rc && (reinterpret_cast<uintptr_t>(p) & (uintptr_t)(size - 1))) rc = fail(PARO_EALIGN, f + name + " is not 16-byte aligned, as its rows are");
+    };
+    check_one(w_gate, of_w, "w_gate");
+    check_one(w_up, of_w, "w_up");
+    if (d->n) check_one(x, of_x, "x");
+    return rc;
+}
 int check_room(const std::string &f, const Room &r, const void *workspace, int64_t bytes) {
     const int rc = check_array(workspace, 16, f + "workspace");
     if (rc) return rc;
     return bytes < r.all ? fail(PARO_ERANGE, f + "the workspace is smaller than paro_gated_workspace says") : PARO_OK;
 }
 
-// x and the weights as operands; both weights lie alike.
+// x and the weights as operands: as they are, or copies that the fills take.
 struct Inputs {
     const char *x, *wg, *wu;
     int64_t ldx, ldw;
 };
 Inputs inputs_of(const paro_gated_t &d, const void *x, const void *wg, const void *wu, char *ws, const Room &r, hipStream_t st) {
-    Inputs in;
-    in.ldx = d.ld_x ? d.ld_x : d.dim;
-    in.x = taken(x, in.ldx, d.n, d.dim, fills_take(x, in.ldx, d.dim), ws + r.x, st);
-    const bool as_they_are = fills_take(wg, d.dim, d.dim) && fills_take(wu, d.dim, d.dim);
-    in.ldw = d.dim;
-    in.wg = taken(wg, in.ldw, d.hidden, d.dim, as_they_are, ws + r.wg, st);
-    in.ldw = d.dim;
-    in.wu = taken(wu, in.ldw, d.hidden, d.dim, as_they_are, ws + r.wu, st);
+    Inputs in{static_cast<const char *>(x), static_cast<const char *>(wg), static_cast<const char *>(wu), ld_x(d), d.dim};
+    Copies c{};
+    c.cols = d.dim;
+    c.width = up_to(d.dim, 8);
+    unsigned copies = 0;
+    const auto copy = [&](const char *&rows, int64_t ld, int64_t n, int64_t room) {
+        c.from[copies] = rows;
+        c.ld[copies] = ld;
+        c.rows[copies] = n;
+        c.to[copies++] = ws + room;
+        rows = ws + room;
+    };
+    if (!fills_take(d.dim, d.dim)) {
+        copy(in.wg, d.dim, d.hidden, r.wg);
+        copy(in.wu, d.dim, d.hidden, r.wu);
+        in.ldw = c.width;
+    }
+    if (!fills_take(in.ldx, d.dim)) {
+        copy(in.x, in.ldx, d.n, r.x);
+        in.ldx = c.width;
+    }
+    if (copies)
+        hipLaunchKernelGGL(k_align, dim3((unsigned)ceil_div(c.width, 8 * 256), (unsigned)std::min<int64_t>(std::max(d.n, d.hidden), 65535), copies), dim3(256), 0,
+                           st, c);
     return in;
 }
 
@@ -678,7 +712,7 @@ int forward(const paro_gated_t &d, const void *x, const void *wg, const void *wu
 #define PARO_FEW(F_TILES, N_TILES)                                                                                                         \
     hipLaunchKernelGGL((k_few<DT, ACT, F_TILES, N_TILES>), dim3((unsigned)ceil_div(d.hidden, 16 * F_TILES)), dim3(64 * FEW_WAVES), 0, st,          \
                        static_cast<const char *>(x), static_cast<const char *>(wg), static_cast<const char *>(wu), d.n, d.dim, d.hidden,   \
-                       d.ld_x ? d.ld_x : d.dim, d.ld_h ? d.ld_h : d.hidden, static_cast<char *>(h), static_cast<char *>(gate),             \
+                       ld_x(d), ld_h(d), static_cast<char *>(h), static_cast<char *>(gate),             \
                        static_cast<char *>(up))
         if (d.n <= 16) PARO_FEW(1, 1);
         else if (d.n <= 32) PARO_FEW(1, 2);
@@ -699,7 +733,7 @@ int forward(const paro_gated_t &d, const void *x, const void *wg, const void *wu
     p.out[0] = static_cast<char *>(h);
     p.out[1] = static_cast<char *>(gate);
     p.out[2] = static_cast<char *>(up);
-    p.ldo = d.ld_h ? d.ld_h : d.hidden;
+    p.ldo = ld_h(d);
     return launch_product<DT, FORWARD, ACT>(p, shape_of(FORWARD, d.n, d.hidden, d.dim), reinterpret_cast<float *>(ws + r.partial), st);
 }
 
@@ -719,7 +753,7 @@ int backward(const paro_gated_t &d, const void *dh, const void *gate, const void
     char *slopes = ws + r.slopes;
     float *partial = reinterpret_cast<float *>(ws + r.partial);
     hipLaunchKernelGGL((k_slopes<DT, ACT>), dim3((unsigned)ceil_div(width, 8 * 256), (unsigned)std::min<int64_t>(d.n, 65535)), dim3(256), 0, st, dh, gate, up,
-                       d.ld_h ? d.ld_h : d.hidden, d.n, d.hidden, width, slopes);
+                       ld_h(d), d.n, d.hidden, width, slopes);
     p.a[0] = slopes;
     p.a[1] = slopes + width * 2;
     p.lda = 2 * width * 2;
@@ -731,7 +765,7 @@ int backward(const paro_gated_t &d, const void *dh, const void *gate, const void
     p.inner = width;
     p.inner_b = d.hidden;
     p.out[0] = static_cast<char *>(dx);
-    p.ldo = d.ld_x ? d.ld_x : d.dim;
+    p.ldo = ld_x(d);
     int rc = launch_product<DT, INPUT_GRAD, PARO_SILU>(p, shape_of(INPUT_GRAD, d.n, d.dim, d.hidden), partial, st);
     if (rc) return rc;
     p.b[0] = in.x;
@@ -769,9 +803,7 @@ int paro_gated(const paro_gated_t *d, const void *x, const void *w_gate, const v
         const std::string f = "paro_gated: ";
         int rc;
         if ((rc = check(f, d)) || d->n == 0) return rc;
-        if ((rc = check_array(x, 2, f + "x")) || (rc = check_array(w_gate, 2, f + "w_gate")) || (rc = check_array(w_up, 2, f + "w_up")) ||
-            (rc = check_array(h, 2, f + "h")))
-            return rc;
+        if ((rc = check_inputs(f, d, x, w_gate, w_up)) || (rc = check_array(h, 2, f + "h"))) return rc;
         if (!gate != !up) return fail(PARO_EINVAL, f + "gate and up are stored both or neither");
         if (gate && ((rc = check_array(gate, 2, f + "gate")) || (rc = check_array(up, 2, f + "up")))) return rc;
         const Room r = room_of(*d, false);
@@ -792,11 +824,10 @@ int paro_gated_grad(const paro_gated_t *d, const void *dh, const void *gate, con
         const std::string f = "paro_gated_grad: ";
         int rc;
         if ((rc = check(f, d))) return rc;
-        if ((rc = check_array(w_gate, 2, f + "w_gate")) || (rc = check_array(w_up, 2, f + "w_up")) || (rc = check_array(dw_gate, 2, f + "dw_gate")) ||
-            (rc = check_array(dw_up, 2, f + "dw_up")))
+        if ((rc = check_inputs(f, d, x, w_gate, w_up)) || (rc = check_array(dw_gate, 2, f + "dw_gate")) || (rc = check_array(dw_up, 2, f + "dw_up")))
             return rc;
         if (d->n && ((rc = check_array(dh, 2, f + "dh")) || (rc = check_array(gate, 2, f + "gate")) || (rc = check_array(up, 2, f + "up")) ||
-                     (rc = check_array(x, 2, f + "x")) || (rc = check_array(dx, 2, f + "dx"))))
+                     (rc = check_array(dx, 2, f + "dx"))))
             return rc;
         const Room r = room_of(*d, true);
         if ((rc = check_room(f, r, workspace, workspace_bytes))) return rc;
