@@ -18,18 +18,21 @@
 
 namespace {
 
-PyObject *g_plan_type, *g_handle_type, *g_adam_type, *g_check;      // the binding's classes, and its check of a status code
+PyObject *g_plan_type, *g_handle_type, *g_adam_type, *g_distill_type, *g_gated_type, *g_check;     // the binding's classes, and its check of a status code
 PyObject *g_handle_name;
 
 // One argument of a call.
 union Arg {
     void *ptr;
     int64_t num;
+    float real;
 };
 struct Args {
-    Arg a[14];
+    Arg a[16];
     const void *contrib[PARO_MAX_RANKS];
     paro_adam_t hp;
+    paro_distill_t distill;
+    paro_gated_t gated;
 };
 
 // Copies `bytes` from an object that lies in memory as its C type does.
@@ -65,6 +68,12 @@ bool number(PyObject *o, int64_t lo, int64_t hi, int64_t *to) {
     return true;
 }
 
+bool real(PyObject *o, float *to) {
+    if (!PyFloat_CheckExact(o)) return false;
+    *to = (float)PyFloat_AS_DOUBLE(o);
+    return true;
+}
+
 bool addresses(PyObject *o, const void **to) {
     const bool list = PyList_CheckExact(o);
     if (!list && !PyTuple_CheckExact(o)) return false;
@@ -91,7 +100,7 @@ bool plan_of(PyObject *o, void **to) {
     return ok;
 }
 
-// kinds: P plan, i int, n int64_t, c contribution (or buffer) addresses, h hyper-parameters, p address
+// kinds: P plan, i int, n int64_t, f float, c contribution (or buffer) addresses, h hyper-parameters, D distillation, G gated projections, p address
 bool parse(const char *kinds, PyObject *const *args, Py_ssize_t n, Args *out) {
     for (Py_ssize_t k = 0; kinds[k]; ++k) {
         Arg *a = &out->a[k];
@@ -103,6 +112,9 @@ bool parse(const char *kinds, PyObject *const *args, Py_ssize_t n, Args *out) {
             case 'P': ok = plan_of(o, &a->ptr); break;
             case 'i': ok = number(o, INT_MIN, INT_MAX, &a->num); break;
             case 'n': ok = number(o, INT64_MIN, INT64_MAX, &a->num); break;
+            case 'f': ok = real(o, &a->real); break;
+            case 'D': ok = (PyObject *)Py_TYPE(o) == g_distill_type && copy_out(o, &out->distill, sizeof(out->distill)); break;
+            case 'G': ok = (PyObject *)Py_TYPE(o) == g_gated_type && copy_out(o, &out->gated, sizeof(out->gated)); break;
             case 'c': ok = addresses(o, out->contrib); break;
             case 'h': ok = (PyObject *)Py_TYPE(o) == g_adam_type && copy_out(o, &out->hp, sizeof(out->hp)); break;
             case 'p': ok = address(o, &a->ptr); break;
@@ -151,6 +163,36 @@ int64_t call_collective(void *fn, Args &x) {
                                                                  const_cast<void *const *>(x.contrib), x.a[8].ptr);
 }
 
+int64_t call_embed(void *fn, Args &x) {
+    return reinterpret_cast<decltype(&paro_embed)>(fn)(x.a[0].ptr, (int)x.a[1].num, x.a[2].num, x.a[3].num, x.a[4].ptr, (int)x.a[5].num, x.a[6].num,
+                                                       x.a[7].num, x.a[8].real, x.a[9].ptr, x.a[10].num, x.a[11].ptr);
+}
+int64_t call_embed_grad(void *fn, Args &x) {
+    return reinterpret_cast<decltype(&paro_embed_grad)>(fn)(x.a[0].ptr, (int)x.a[1].num, x.a[2].num, x.a[3].ptr, (int)x.a[4].num, x.a[5].num, x.a[6].num,
+                                                            x.a[7].real, x.a[8].ptr, (int)x.a[9].num, x.a[10].num, x.a[11].num, x.a[12].ptr, x.a[13].num,
+                                                            x.a[14].ptr);
+}
+int64_t call_distill_loss(void *fn, Args &x) {
+    return reinterpret_cast<decltype(&paro_distill_loss)>(fn)(&x.distill, x.a[1].ptr, x.a[2].ptr, at<int32_t>(x.a[3]), at<float>(x.a[4]), at<float>(x.a[5]),
+                                                              x.a[6].ptr);
+}
+int64_t call_distill_grad(void *fn, Args &x) {
+    return reinterpret_cast<decltype(&paro_distill_grad)>(fn)(&x.distill, x.a[1].ptr, x.a[2].ptr, at<int32_t>(x.a[3]), at<float>(x.a[4]), at<float>(x.a[5]),
+                                                              x.a[6].ptr, x.a[7].ptr);
+}
+int64_t call_distill_step(void *fn, Args &x) {
+    return reinterpret_cast<decltype(&paro_distill_step)>(fn)(&x.distill, x.a[1].ptr, x.a[2].ptr, at<int32_t>(x.a[3]), at<float>(x.a[4]), at<float>(x.a[5]),
+                                                              x.a[6].ptr, x.a[7].ptr);
+}
+int64_t call_gated(void *fn, Args &x) {
+    return reinterpret_cast<decltype(&paro_gated)>(fn)(&x.gated, x.a[1].ptr, x.a[2].ptr, x.a[3].ptr, x.a[4].ptr, x.a[5].ptr, x.a[6].ptr, x.a[7].ptr,
+                                                       x.a[8].num, x.a[9].ptr);
+}
+int64_t call_gated_grad(void *fn, Args &x) {
+    return reinterpret_cast<decltype(&paro_gated_grad)>(fn)(&x.gated, x.a[1].ptr, x.a[2].ptr, x.a[3].ptr, x.a[4].ptr, x.a[5].ptr, x.a[6].ptr, x.a[7].ptr,
+                                                            x.a[8].ptr, x.a[9].ptr, x.a[10].ptr, x.a[11].num, x.a[12].ptr);
+}
+
 struct Call {
     const char *name, *kinds, *doc;
     int least;                        // arguments without a default
@@ -170,6 +212,17 @@ constexpr Call CALLS[] = {
     {"paro_ring_hop", "Ppipipnp", "paro_ring_hop(plan, partial_in, in_dtype, local, local_dtype, out, n, stream=0)\n--\n\n", 7, call_hop, false},
     {"paro_collective_step", "Piiiiiicp", "paro_collective_step(plan, rank, sched, collective, phase, ring, step, bufs, stream=0)\n--\n\n", 8,
      call_collective, true},
+    {"paro_embed", "pinnpinnfpnp",
+     "paro_embed(table, dtype, rows, dim, tokens, token_dtype, n, first_token, scale, out, ld_out=0, stream=0)\n--\n\n", 10, call_embed, false},
+    {"paro_embed_grad", "pinpinnfpinnpnp",
+     "paro_embed_grad(dout, dtype, ld_dout, tokens, token_dtype, n, first_token, scale, grad, grad_dtype, rows, dim, workspace, workspace_bytes, "
+     "stream=0)\n--\n\n", 14, call_embed_grad, false},
+    {"paro_distill_loss", "Dpppppp", "paro_distill_loss(d, logits, teacher, ids, loss, lse=0, stream=0)\n--\n\n", 5, call_distill_loss, false},
+    {"paro_distill_grad", "Dppppppp", "paro_distill_grad(d, logits, teacher, ids, lse, dloss, dlogits, stream=0)\n--\n\n", 7, call_distill_grad, false},
+    {"paro_distill_step", "Dppppppp", "paro_distill_step(d, logits, teacher, ids, dloss, loss, dlogits, stream=0)\n--\n\n", 7, call_distill_step, false},
+    {"paro_gated", "Gpppppppnp", "paro_gated(d, x, w_gate, w_up, h, gate, up, workspace, workspace_bytes, stream=0)\n--\n\n", 9, call_gated, false},
+    {"paro_gated_grad", "Gppppppppppnp",
+     "paro_gated_grad(d, dh, gate, up, x, w_gate, w_up, dx, dw_gate, dw_up, workspace, workspace_bytes, stream=0)\n--\n\n", 12, call_gated_grad, false},
 };
 constexpr int N_CALLS = sizeof(CALLS) / sizeof(CALLS[0]);
 void *g_fn[N_CALLS];
@@ -263,19 +316,25 @@ PyObject *setup(PyObject *, PyObject *args) {
             return nullptr;
         }
     }
-    PyObject *types[] = {PyObject_GetAttrString(module, "Plan"), PyObject_GetAttrString(module, "c_void_p"),
-                         PyObject_GetAttrString(module, "paro_adam_t"), PyObject_GetAttrString(module, "_check")};
+    PyObject *types[] = {PyObject_GetAttrString(module, "Plan"),        PyObject_GetAttrString(module, "c_void_p"),
+                         PyObject_GetAttrString(module, "paro_adam_t"), PyObject_GetAttrString(module, "_check"),
+                         PyObject_GetAttrString(module, "paro_distill_t"), PyObject_GetAttrString(module, "paro_gated_t")};
     for (PyObject *t : types)
         if (!t) return nullptr;
-    PyObject *hp = PyObject_CallNoArgs(types[2]), *out = PyDict_New(), *doc_name = PyUnicode_FromString("paper_2310_06003_amd");
-    paro_adam_t probe;
-    if (!hp || !out || !doc_name) return nullptr;
-    const bool fits = copy_out(hp, &probe, sizeof(probe));
-    Py_DECREF(hp);
-    if (!fits) {
-        PyErr_SetString(PyExc_RuntimeError, "paro_adam_t has another size here than in paro.h");
+    PyObject *out = PyDict_New(), *doc_name = PyUnicode_FromString("paper_2310_06003_amd");
+    if (!out || !doc_name) return nullptr;
+    const auto fits = [](PyObject *type, void *to, size_t bytes, const char *name) {
+        PyObject *o = PyObject_CallNoArgs(type);
+        if (!o) return false;
+        const bool same = copy_out(o, to, bytes);
+        Py_DECREF(o);
+        if (!same) PyErr_Format(PyExc_RuntimeError, "%s has another size here than in paro.h", name);
+        return same;
+    };
+    Args probe;
+    if (!fits(types[2], &probe.hp, sizeof(probe.hp), "paro_adam_t") || !fits(types[4], &probe.distill, sizeof(probe.distill), "paro_distill_t") ||
+        !fits(types[5], &probe.gated, sizeof(probe.gated), "paro_gated_t"))
         return nullptr;
-    }
     define<0>();
     g_defs[N_CALLS] = {"make_adam", (PyCFunction)(void (*)())make_adam, METH_FASTCALL | METH_KEYWORDS,
                        "make_adam(*, lr, beta1, beta2, eps, weight_decay, grad_scale, max_norm=0.0, step=1, adamw=True, "
@@ -293,6 +352,8 @@ PyObject *setup(PyObject *, PyObject *args) {
     g_handle_type = types[1];
     g_adam_type = types[2];
     g_check = types[3];
+    g_distill_type = types[4];
+    g_gated_type = types[5];
     g_plan_type = types[0];
     return out;
 }
