@@ -547,7 +547,6 @@ __global__ __launch_bounds__(256) void k_align(Copies a) {
 int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 int64_t up_to(int64_t a, int64_t b) { return ceil_div(a, b) * b; }
 constexpr int COMPUTE_UNITS = 256;
-constexpr int64_t MIN_SAVED = 16;        // stages
 
 // Whether rows can be filled as they are (their array is 16-byte aligned then: see check_inputs).
 bool fills_take(int64_t ld, int64_t cols) { return ld % 8 == 0 && cols % 8 == 0; }
@@ -558,26 +557,33 @@ struct Shape {                           // of a product's launch
     int64_t blocks() const { return whole + (tiles_m * tiles_n - whole) * splits; }
     int64_t partial_bytes() const { return splits > 1 ? (tiles_m * tiles_n - whole) * splits * (large ? 256 * 256 : 128 * 128) * 4 : 0; }
 };
+// Which tiles, and how the inner dimension is split: what is quickest by this reckoning, in us.  A round of tiles takes its stages, 1.55 each of
+// a 256 x 256 tile, one a compute unit, 1.2 of two of 128 x 128.  The tiles beyond whole rounds may be split so that their blocks fill the chip
+// once, into shares of at least eight stages; then their sums are written and read at 2.5 TB/s, with a launch of 5.  Against measured
+// times (bf16, silu, forward with the projections stored), large tiles | small ones: 300 tokens of 2048 x 5632 40 | 38, reckoned 38 | 38; 512 of 4096 x 11008 108 | 133, 99 | 124;
+// 2000 of 4096 x 512 43 | 35, 44 | 36; 4000 of 1024 x 4096 77 | 109, 50 | 77 (it leaves out the stores of the result, alike in both).
 // rows and columns: of the result (of WEIGHT_GRAD of one part, of FORWARD of both parts)
 Shape shape_of(int mode, int64_t rows, int64_t cols, int64_t inner) {
-    const auto tiles = [&](int64_t side, int64_t &m, int64_t &n) {
-        m = ceil_div(rows, side) * (mode == WEIGHT_GRAD ? 2 : 1);
-        n = mode == FORWARD ? ceil_div(cols, side / 2) : ceil_div(cols, side);
-        return m * n;
-    };
-    Shape s;
-    const int64_t n256 = tiles(256, s.tiles_m, s.tiles_n);
-    s.large = n256 >= COMPUTE_UNITS / 2;
-    const int64_t n = s.large ? n256 : tiles(128, s.tiles_m, s.tiles_n);
-    const int64_t at_once = s.large ? COMPUTE_UNITS : 2 * COMPUTE_UNITS;
     const int64_t stages = ceil_div(inner, STEPS) * (mode == INPUT_GRAD ? 2 : 1);
-    // The tiles beyond whole rounds are split, so that their blocks fill the chip once: into shares of at least eight stages, and where
-    // that saves more than the joining costs.
-    s.whole = n / at_once * at_once;
-    s.splits = n > s.whole ? std::max<int64_t>(1, std::min<int64_t>({at_once / (n - s.whole), stages / 8, 16})) : 1;
-    if (stages - stages / s.splits < MIN_SAVED) s.splits = 1;
-    if (s.splits == 1) s.whole = n;
-    return s;
+    Shape best{};
+    double least = -1.0;
+    for (const bool large : {true, false}) {
+        const int64_t side = large ? 256 : 128, at_once = large ? COMPUTE_UNITS : 2 * COMPUTE_UNITS;
+        Shape s{large, ceil_div(rows, side) * (mode == WEIGHT_GRAD ? 2 : 1), ceil_div(cols, mode == FORWARD ? side / 2 : side), 0, 1};
+        const int64_t tiles = s.tiles_m * s.tiles_n, rest = tiles % at_once;
+        const double filled = (double)rows / (double)(ceil_div(rows, side) * side), stage = large ? 1.55 : 1.2;
+        for (int64_t splits = 1; splits == 1 || (rest && rest * splits <= at_once && splits <= 16 && stages / splits >= 8); ++splits) {
+            s.splits = splits;
+            s.whole = splits == 1 ? tiles : tiles - rest;
+            const int64_t in_turn = splits == 1 ? ceil_div(tiles, at_once) * stages : tiles / at_once * stages + ceil_div(stages, splits);
+            const double cost = (double)in_turn * stage + (splits == 1 ? 0.0 : 5.0 + (double)s.partial_bytes() * filled / 2.5e6);
+            if (least < 0.0 || cost < least) {
+                least = cost;
+                best = s;
+            }
+        }
+    }
+    return best;
 }
 
 template <int DT, int MODE, int ACT, int BM, int BN, int WAVES_M, int WAVES_N>
