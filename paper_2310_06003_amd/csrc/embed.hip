@@ -99,8 +99,16 @@ __global__ __launch_bounds__(SORT_THREADS) void k_sort_tokens(const Token *token
     const int64_t begin = from_token + w * part, end = begin + part < to_token ? begin + part : to_token;
     const uint64_t before = ((uint64_t)1 << lane) - 1;
 
+    uint64_t next[SORT_AHEAD];
+    const auto load = [&](int64_t from) {
+#pragma unroll
+        for (int u = 0; u < SORT_AHEAD; ++u) {
+            const int64_t i = from + u * 64 + lane;
+            next[u] = i < end ? (uint64_t)(int64_t)tokens[i] - (uint64_t)first : ~(uint64_t)0;
+        }
+    };
     // visit(row, i, place) for the tokens of the block's rows, in order; place counts on from what the wave's counter of the row holds.
-    // Returns how many tokens lie in rows before the block's.
+    // Returns how many tokens lie in rows before the block's.  The first tokens are loaded before it is called.
     const auto walk = [&](auto &&visit) {
         int below = 0, held = 0, head = 0;
         const auto number = [&](int of) {
@@ -115,20 +123,11 @@ __global__ __launch_bounds__(SORT_THREADS) void k_sort_tokens(const Token *token
             head += of;
             held -= of;
         };
-        uint64_t next[SORT_AHEAD];
-        const auto load = [&](int64_t from) {
-#pragma unroll
-            for (int u = 0; u < SORT_AHEAD; ++u) {
-                const int64_t i = from + u * 64 + lane;
-                next[u] = i < end ? (uint64_t)(int64_t)tokens[i] - (uint64_t)first : ~(uint64_t)0;
-            }
-        };
-        load(begin);
         for (int64_t from = begin; from < end; from += SORT_AHEAD * 64) {
             uint64_t now[SORT_AHEAD];
 #pragma unroll
             for (int u = 0; u < SORT_AHEAD; ++u) now[u] = next[u];
-            load(from + SORT_AHEAD * 64);
+            if (from + SORT_AHEAD * 64 < end) load(from + SORT_AHEAD * 64);
 #pragma unroll
             for (int u = 0; u < SORT_AHEAD; ++u) {
                 below += __popcll(__ballot(now[u] < (uint64_t)lo));
@@ -148,8 +147,10 @@ __global__ __launch_bounds__(SORT_THREADS) void k_sort_tokens(const Token *token
         return below;
     };
 
+    load(begin);
     for (int r = lane; r < SORT_ROWS; r += 64) count[w][r] = 0;
     const int below = walk([](int, int, int) {});
+    if constexpr (!COUNT) load(begin);              // for the second walk, on their way during the scan
     if (lane == 0) below_of[w] = below;
     __syncthreads();
 
@@ -241,25 +242,33 @@ struct RowPiece {
     }
 };
 
-// acc += dout[order[a .. b)], in order, for the lane's pieces of a tile of columns.
+// acc += dout[order[a .. b)], in order, for the lane's pieces of a tile of columns.  The places of 64 tokens are loaded at once, one a lane
+// (each by a scalar load that its row waits for: GPT-2's table 64 us, so 47; 32768 tokens of 4096 155 and 138).
 template <int DT, int GT, int C>
 __device__ __forceinline__ void add_rows(float (&acc)[C][Elem<GT>::E], const void *dout, int64_t ld, const int *order, int a, int b,
                                          const int64_t (&col)[C], int64_t dim) {
-    constexpr int U = C >= 8 ? 1 : 8 / C;           // 8 loads in flight
-    for (int k = a; k < b; k += U) {
-        RowPiece<DT, GT> piece[U][C];
+    constexpr int U = 4;                            // rows in flight; 2: 52 and 149 us, 6: 46 and 145
+    for (int k0 = a; k0 < b; k0 += 64) {
+        const int mine = k0 + lane_of() < b ? order[k0 + lane_of()] : 0, all = b - k0 < 64 ? b - k0 : 64;
+        const auto add = [&](int k, auto count_) {
+            constexpr int count = count_;
+            RowPiece<DT, GT> piece[count][C];
 #pragma unroll
-        for (int u = 0; u < U; ++u) {
-            const int64_t row = (int64_t)order[k + u < b ? k + u : b - 1] * ld;
+            for (int u = 0; u < count; ++u) {
+                const int64_t row = (int64_t)__builtin_amdgcn_readlane(mine, k + u) * ld;
 #pragma unroll
-            for (int c = 0; c < C; ++c)
-                if (k + u < b && col[c] < dim) piece[u][c].load(dout, row + col[c]);
-        }
+                for (int c = 0; c < C; ++c)
+                    if (col[c] < dim) piece[u][c].load(dout, row + col[c]);
+            }
 #pragma unroll
-        for (int u = 0; u < U; ++u)
+            for (int u = 0; u < count; ++u)
 #pragma unroll
-            for (int c = 0; c < C; ++c)
-                if (k + u < b && col[c] < dim) piece[u][c].add_to(acc[c]);
+                for (int c = 0; c < C; ++c)
+                    if (col[c] < dim) piece[u][c].add_to(acc[c]);
+        };
+        int k = 0;
+        for (; k + U <= all; k += U) add(k, std::integral_constant<int, U>{});
+        for (; k < all; ++k) add(k, std::integral_constant<int, 1>{});
     }
 }
 
@@ -284,12 +293,15 @@ __device__ __forceinline__ void store_row(float (&acc)[C][Elem<GT>::E], void *gr
     }
 }
 
-// A wave of the first blocks takes a segment of the sorted tokens: runs of more than `seg` are summed segment by segment, in parallel.
-// Of one segment such a run holds the beginning (slot 0), or the end and not the beginning (slot 1).  A wave of the others takes a
-// row of the table's gradient: it writes a short run's sum, or zeros where no token is.
+// Three kinds of blocks, in the order in which they start: what reads goes before what only writes, since a read that waits behind a stream of
+// stores takes microseconds (GPT-2's table 52 us with the rows in their own order, so 47; 32768 tokens of 4096 141 and 138).
+//   segments   a wave takes a segment of the sorted tokens: runs of more than `seg` are summed segment by segment, in parallel.  Of one
+//              segment such a run holds the beginning (slot 0), or the end and not the beginning (slot 1)
+//   runs       a wave takes a place among the sorted tokens, and sums the run that begins there, if a short one does
+//   the rest   a wave takes a row of the table's gradient and writes zeros, if no token is of that row
 template <int DT, int GT, int C>
 __global__ __launch_bounds__(THREADS) void k_sums(const void *dout, int64_t ld, const int *start, const int *order, const int *row_at, int64_t rows,
-                                                  int64_t dim, int seg, unsigned seg_blocks, float scale, float *partial, void *grad) {
+                                                  int64_t dim, int seg, unsigned seg_blocks, unsigned run_blocks, float scale, float *partial, void *grad) {
     constexpr int E = Elem<GT>::E;
     int64_t col[C];
     columns<E>(col, dim);
@@ -310,49 +322,60 @@ __global__ __launch_bounds__(THREADS) void k_sums(const void *dout, int64_t ld, 
 #pragma unroll
                     for (int j = 0; j < E; j += 4) store_piece<PARO_F32>(partial, (2 * s + slot) * dim + col[c] + j, pack<PARO_F32>(&acc[c][j]));
         }
-        return;
-    }
-    for (int64_t v = (int64_t)(blockIdx.x - seg_blocks) * WAVES + wave_of(); v < rows; v += (int64_t)(gridDim.x - seg_blocks) * WAVES) {
-        const int a = start[v], b = start[v + 1];
-        if (b - a > seg) continue;
-        float acc[C][E] = {};
-        add_rows<DT, GT>(acc, dout, ld, order, a, b, col, dim);
-        store_row<GT>(acc, grad, v, col, dim, scale);
+    } else if (blockIdx.x < seg_blocks + run_blocks) {
+        const int held = start[rows];
+        for (int64_t a = (int64_t)(blockIdx.x - seg_blocks) * WAVES + wave_of(); a < held; a += (int64_t)run_blocks * WAVES) {
+            const int v = row_at[a], b = start[v + 1];
+            if (start[v] != a || b - a > seg) continue;
+            float acc[C][E] = {};
+            add_rows<DT, GT>(acc, dout, ld, order, (int)a, b, col, dim);
+            store_row<GT>(acc, grad, v, col, dim, scale);
+        }
+    } else {
+        const unsigned first = seg_blocks + run_blocks;
+        for (int64_t v = (int64_t)(blockIdx.x - first) * WAVES + wave_of(); v < rows; v += (int64_t)(gridDim.x - first) * WAVES) {
+            if (start[v] != start[v + 1]) continue;
+#pragma unroll
+            for (int c = 0; c < C; ++c)
+                if (col[c] < dim) store_stream<GT>(grad, v * dim + col[c], u32x4{0, 0, 0, 0});
+        }
     }
 }
 
-// A wave adds up the segments of the long run that begins in its segment, if one does: the last one there.
+// A wave adds up the segments of the long run that begins in its segment, if one does: the last one there.  Four columns a lane and 16
+// segments in flight: few waves have anything to do, and the longest run, which many segments hold, decides.
 template <int GT>
 __global__ __launch_bounds__(THREADS) void k_join(const int *start, const int *row_at, int64_t rows, int64_t dim, int seg, float scale,
                                                   const float *partial, void *grad) {
-    constexpr int E = Elem<GT>::E, U = 8;
+    constexpr int U = 16;
     int64_t col[1];
-    columns<E>(col, dim);
+    columns<4>(col, dim);
     const int64_t s0 = (int64_t)blockIdx.x * WAVES + wave_of();
     const int held = start[rows], a = (int)(s0 * seg), end = a + seg < held ? a + seg : held;
     if (a >= end) return;
     const int v = row_at[end - 1], from = start[v], to = start[v + 1];
     if (from < a || to - from <= seg || col[0] >= dim) return;
-    float acc[1][E] = {};
+    float acc[4] = {};
     for (int64_t s = s0; s * seg < to; s += U) {
-        u32x4 raw[U][E / 4];
+        u32x4 raw[U];
 #pragma unroll
         for (int u = 0; u < U; ++u)
-#pragma unroll
-            for (int j = 0; j < E / 4; ++j)
-                if ((s + u) * seg < to) raw[u][j] = load_piece<PARO_F32>(partial, (2 * (s + u) + ((s + u) * seg < from ? 1 : 0)) * dim + col[0] + 4 * j);
+            if ((s + u) * seg < to) raw[u] = load_piece<PARO_F32>(partial, (2 * (s + u) + ((s + u) * seg < from ? 1 : 0)) * dim + col[0]);
 #pragma unroll
         for (int u = 0; u < U; ++u)
+            if ((s + u) * seg < to) {
+                float x[4];
+                unpack<PARO_F32>(raw[u], x);
 #pragma unroll
-            for (int j = 0; j < E / 4; ++j)
-                if ((s + u) * seg < to) {
-                    float x[4];
-                    unpack<PARO_F32>(raw[u][j], x);
-#pragma unroll
-                    for (int q = 0; q < 4; ++q) acc[0][4 * j + q] += x[q];
-                }
+                for (int q = 0; q < 4; ++q) acc[q] += x[q];
+            }
     }
-    store_row<GT>(acc, grad, v, col, dim, scale);
+#pragma unroll
+    for (int q = 0; q < 4; ++q) acc[q] *= scale;
+    if constexpr (GT == PARO_F32) store_piece<GT>(grad, v * dim + col[0], pack<GT>(acc));
+    else
+#pragma unroll
+        for (int q = 0; q < 4; ++q) store_one<GT>(grad, v * dim + col[0] + q, acc[q]);
 }
 
 // Rows narrower than a piece: a thread for each element.
@@ -383,7 +406,7 @@ int segment_of(int64_t n) {
     while (n / seg > MAX_SEGMENTS) seg *= 2;
     return seg;
 }
-constexpr int GRAD_PIECES = 4;           // pieces a lane of the sums: 32768 tokens of 4096, 139 us with one, 133 with two, 114
+constexpr int GRAD_PIECES = 4;           // pieces a lane of the sums (2: GPT-2's table 51 us, not 47, 32768 tokens of 4096 179, not 138)
 
 // Tokens of a slice of the sort.
 int64_t slice_of(int64_t n) { return std::max(SLICE, ceil_div(ceil_div(n, MAX_SLICES), SORT_THREADS) * SORT_THREADS); }
@@ -435,12 +458,12 @@ void launch_sums(const void *dout, int64_t ld, int64_t n, float scale, void *gra
     const int seg = segment_of(n), *row_at = reinterpret_cast<int *>(ws + g.row_at);
     float *partial = reinterpret_cast<float *>(ws + g.partial);
     const unsigned seg_blocks = n > seg ? (unsigned)ceil_div(ceil_div(n, seg), WAVES) : 0;
-    dim3 grid = grid_for(rows, ceil_div(dim, 64 * GRAD_PIECES * Elem<GT>::E));
-    grid.x += seg_blocks;
-    hipLaunchKernelGGL((k_sums<DT, GT, GRAD_PIECES>), grid, dim3(THREADS), 0, st, dout, ld, start, order, row_at, rows, dim, seg, seg_blocks, scale,
-                       partial, grad);
+    const int64_t tiles = ceil_div(dim, 64 * GRAD_PIECES * Elem<GT>::E);
+    const unsigned run_blocks = n ? grid_for(n, 2 * tiles).x : 0;
+    hipLaunchKernelGGL((k_sums<DT, GT, GRAD_PIECES>), dim3(seg_blocks + run_blocks + grid_for(rows, 2 * tiles).x, (unsigned)tiles), dim3(THREADS), 0, st, dout,
+                       ld, start, order, row_at, rows, dim, seg, seg_blocks, run_blocks, scale, partial, grad);
     if (seg_blocks)
-        hipLaunchKernelGGL((k_join<GT>), dim3(seg_blocks, (unsigned)ceil_div(dim, 64 * Elem<GT>::E)), dim3(THREADS), 0, st, start, row_at, rows, dim, seg,
+        hipLaunchKernelGGL((k_join<GT>), dim3(seg_blocks, (unsigned)ceil_div(dim, 64 * 4)), dim3(THREADS), 0, st, start, row_at, rows, dim, seg,
                            scale, partial, grad);
 }
 
