@@ -77,9 +77,9 @@ constexpr unsigned NOWHERE = 0x80000000u;
 
 struct Product {
     // Operand a: [rows][inner] (along) or [inner][rows] (across), operand b: [cols][inner] or [inner][cols].  Two parts: forward, the
-    // columns of b (gate, up); of dx, the inner dimension (of a the left and the right half, of b two matrices).
+    // columns of b (gate, up); of dx, the inner dimension (dg and du, Wg and Wu); of dW, the rows of a.  dg and du lie in panels (see k_slopes).
     const char *a[2], *b[2];
-    int64_t lda, ldb;                    // bytes
+    int64_t lda, ldb, panel;             // bytes from row to row, and from panel to panel
     int64_t rows, cols, inner;           // inner: of one part, in whole pieces where an operand lies along it
     int64_t inner_b;                     // steps that b has (across: rows)
     char *out[3];                        // h, g, u; dx; dWg, dWu
@@ -157,7 +157,7 @@ __global__ __launch_bounds__(64 * WAVES_M * WAVES_N) void k_product(Product p) {
     constexpr int TM = BM / WAVES_M / 16, TN = BN / WAVES_N / 16;             // 16x16 tiles of a wave
     constexpr int A_BYTES = BM * ROW_BYTES, B_BYTES = BN * ROW_BYTES, PART = A_BYTES;
     constexpr int FILLS = A_BYTES / (THREADS_ * 16);           // of a part, by each wave
-    constexpr bool A_ACROSS = MODE == WEIGHT_GRAD, B_ACROSS = MODE != FORWARD;
+    constexpr bool A_ACROSS = MODE == WEIGHT_GRAD, A_PANELS = MODE != FORWARD, B_ACROSS = MODE != FORWARD;
     static_assert(TN == 4 && A_BYTES == B_BYTES, "a wave's columns are two pairs of tiles, and a part of the ring takes either operand");
     extern __shared__ __attribute__((aligned(1024))) char ring[];
     const unsigned lds0 = (unsigned)(uintptr_t)(lds_char *)ring;
@@ -181,9 +181,10 @@ __global__ __launch_bounds__(64 * WAVES_M * WAVES_N) void k_product(Product p) {
         at = there ? (unsigned)(memory_row * ld) + piece * 16 : NOWHERE;
         step = piece * 8;
     };
-    const auto across = [&](int k, int piece, int64_t columns_left, int64_t ld, unsigned &at, int &step) {
+    // in_panels: the columns lie in panels of 64, `panel` bytes apart
+    const auto across = [&](int k, int piece, int64_t columns_left, int64_t ld, bool in_panels, unsigned &at, int &step) {
         const int block = (piece >> 1) ^ ((k & 3) | ((k >> 1) & 4)), column = (block * 2 + (piece & 1)) * 8;
-        at = column < columns_left ? (unsigned)(k * ld) + column * 2 : NOWHERE;
+        at = column < columns_left ? (unsigned)(k * ld) + (in_panels ? (unsigned)((column >> 6) * p.panel) + (column & 63) * 2 : column * 2) : NOWHERE;
         step = k;
     };
     // Forward: this wave fills rows of b that are the gate's (even waves) or the up projection's, from this row on.
@@ -193,17 +194,17 @@ __global__ __launch_bounds__(64 * WAVES_M * WAVES_N) void k_product(Product p) {
     for (int i = 0; i < FILLS; ++i) {
         if constexpr (A_ACROSS) {
             constexpr int PIECES = BM / 8;
-            across((w * FILLS + i) * (64 / PIECES) + lane / PIECES, lane % PIECES, p.rows - row0, p.lda, a_at[i], a_step[i]);
+            across((w * FILLS + i) * (64 / PIECES) + lane / PIECES, lane % PIECES, p.rows - row0, ROW_BYTES, true, a_at[i], a_step[i]);
         } else {
             const int r = (w * FILLS + i) * 8 + lane / 8;
-            along(r, r < p.rows - row0, r, p.lda, a_at[i], a_step[i]);
+            along(r, r < p.rows - row0, r, A_PANELS ? ROW_BYTES : p.lda, a_at[i], a_step[i]);
         }
     }
 #pragma unroll
     for (int i = 0; i < FILLS; ++i) {
         if constexpr (B_ACROSS) {
             constexpr int PIECES = BN / 8;
-            across((w * FILLS + i) * (64 / PIECES) + lane / PIECES, lane % PIECES, p.cols - col0, p.ldb, b_at[i], b_step[i]);
+            across((w * FILLS + i) * (64 / PIECES) + lane / PIECES, lane % PIECES, p.cols - col0, p.ldb, false, b_at[i], b_step[i]);
         } else {                                    // 32 rows of the gate's, then 32 of the up projection's, for each wave's 64 columns
             static_assert(B_ACROSS || FILLS == 4, "a wave fills 32 rows of b");
             const int r = i * 8 + lane / 8;
@@ -218,10 +219,12 @@ __global__ __launch_bounds__(64 * WAVES_M * WAVES_N) void k_product(Product p) {
     // What the next stage is filled from.
     u32x4 a_from, b_from;
     int a_left, b_left, a_until, b_until;           // steps left of the part; stages until the part ends, or the block's share of it
-    const int64_t a_stage = A_ACROSS ? STEPS * p.lda : ROW_BYTES, b_stage = B_ACROSS ? STEPS * p.ldb : ROW_BYTES;
+    const int64_t a_stage = A_ACROSS ? STEPS * ROW_BYTES : A_PANELS ? p.panel : ROW_BYTES, b_stage = B_ACROSS ? STEPS * p.ldb : ROW_BYTES;
     const auto begin_a = [&](int part, int stage) {
         const int64_t k0 = (int64_t)stage * STEPS;
-        a_from = descriptor(A_ACROSS ? p.a[out_part] + k0 * p.lda + row0 * 2 : p.a[part] + row0 * p.lda + k0 * 2);
+        a_from = descriptor(A_ACROSS   ? p.a[out_part] + row0 / 64 * p.panel + k0 * ROW_BYTES
+                            : A_PANELS ? p.a[part] + (k0 / 64) * p.panel + row0 * ROW_BYTES
+                                       : p.a[part] + row0 * p.lda + k0 * 2);
         a_left = (int)(p.inner - k0);
         a_until = (to < (part + 1) * per_part ? to - part * per_part : per_part) - stage;
     };
@@ -484,20 +487,23 @@ __global__ __launch_bounds__(64 * FEW_WAVES) void k_few(const char *x, const cha
     }
 }
 
-// dg | du, side by side in a row of the workspace: [tokens][2][width], width = hidden rounded up to a piece, zeros in between.  Rounded to
-// the weights' type, which is what the matrix cores take.
+// dg, then du, each in panels of 64 hidden elements: [panel][tokens][64], zeros past the last element.  What a tile's stage reads of them is then a
+// run of memory, for dx (256 tokens of a panel) as for dW (64 tokens of four), where rows of 11008 would be 22 KB apart
+// (8192 tokens of 4096 x 11008 2302 us, so 2285; this kernel 150 and 141).  Rounded to the
+// weights' type, which is what the matrix cores take.  A wave takes eight tokens of a panel.
 template <int DT, int ACT>
 __global__ __launch_bounds__(256) void k_slopes(const void *dh, const void *gate, const void *up, int64_t ld, int64_t tokens, int64_t hidden,
-                                                int64_t width, void *out) {
-    const int64_t f = ((int64_t)blockIdx.x * 256 + threadIdx.x) * 8;
-    if (f >= width) return;
-    for (int64_t m = blockIdx.y; m < tokens; m += gridDim.y) {
+                                                int64_t panels, char *out) {
+    const int lane = threadIdx.x & 63;
+    const int64_t panel = (int64_t)blockIdx.x * 4 + wave_of(), f = panel * 64 + (lane & 7) * 8;
+    if (panel >= panels) return;
+    for (int64_t m = (int64_t)blockIdx.y * 8 + lane / 8; m < tokens; m += (int64_t)gridDim.y * 8) {
         float d[8] = {}, g[8] = {}, u[8] = {}, dg[8], du[8];
         const int64_t at = m * ld + f;
         if (f + 8 <= hidden) {
-            unpack<DT>(load_piece<DT>(dh, at), d);
-            unpack<DT>(load_piece<DT>(gate, at), g);
-            unpack<DT>(load_piece<DT>(up, at), u);
+            unpack<DT>(load_stream<DT>(dh, at), d);
+            unpack<DT>(load_stream<DT>(gate, at), g);
+            unpack<DT>(load_stream<DT>(up, at), u);
         } else {
             for (int e = 0; e < 8; ++e)
                 if (f + e < hidden) {
@@ -513,8 +519,9 @@ __global__ __launch_bounds__(256) void k_slopes(const void *dh, const void *gate
             dg[e] = d[e] * u[e] * da;
             du[e] = d[e] * a;
         }
-        store_piece<DT>(out, m * 2 * width + f, pack<DT>(dg));
-        store_piece<DT>(out, m * 2 * width + width + f, pack<DT>(du));
+        const int64_t to = (panel * tokens + m) * 64 + (lane & 7) * 8;
+        store_piece<DT>(out, to, pack<DT>(dg));
+        store_piece<DT>(out, panels * tokens * 64 + to, pack<DT>(du));
     }
 }
 
@@ -633,7 +640,7 @@ Room room_of(const paro_gated_t &d, bool grad) {
     }
     int64_t partial = 0;
     if (grad) {
-        r.slopes = take(d.n * 2 * up_to(d.hidden, 8) * 2);
+        r.slopes = take(2 * up_to(d.hidden, 64) * d.n * 2);
         partial = std::max(shape_of(INPUT_GRAD, d.n, d.dim, d.hidden).partial_bytes(), shape_of(WEIGHT_GRAD, d.hidden, d.dim, d.n).partial_bytes());
     } else {
         partial = shape_of(FORWARD, d.n, d.hidden, d.dim).partial_bytes();
@@ -647,7 +654,7 @@ int check(const std::string &f, const paro_gated_t *d) {
     if (!d) return fail(PARO_EINVAL, f + "d is NULL");
     if (d->dtype != PARO_BF16 && d->dtype != PARO_F16) return fail(PARO_EINVAL, f + "dtype must be PARO_BF16 or PARO_F16");
     if (d->act != PARO_SILU && d->act != PARO_GELU) return fail(PARO_EINVAL, f + "act must be PARO_SILU or PARO_GELU");
-    if (d->n < 0 || d->n > (1 << 24)) return fail(PARO_EINVAL, f + "n must be in [0, 2^24]");
+    if (d->n < 0 || d->n > (1 << 22)) return fail(PARO_EINVAL, f + "n must be in [0, 2^22]");
     if (d->dim < 1 || d->dim > (1 << 20) || d->hidden < 1 || d->hidden > (1 << 20)) return fail(PARO_EINVAL, f + "dim and hidden must be in [1, 2^20]");
     if ((d->ld_x && d->ld_x < d->dim) || (d->ld_h && d->ld_h < d->hidden)) return fail(PARO_EINVAL, f + "a row is longer than its distance to the next");
     if (d->ld_x > (1 << 21) || d->ld_h > (1 << 21)) return fail(PARO_EINVAL, f + "ld_x and ld_h are at most 2^21");
@@ -755,20 +762,20 @@ int backward(const paro_gated_t &d, const void *dh, const void *gate, const void
         return launch_product<DT, WEIGHT_GRAD, PARO_SILU>(p, shape_of(WEIGHT_GRAD, d.hidden, d.dim, 0), nullptr, st);
     }
     const Inputs in = inputs_of(d, x, wg, wu, ws, r, st);
-    const int64_t width = up_to(d.hidden, 8);
+    const int64_t panels = ceil_div(d.hidden, 64);
     char *slopes = ws + r.slopes;
     float *partial = reinterpret_cast<float *>(ws + r.partial);
-    hipLaunchKernelGGL((k_slopes<DT, ACT>), dim3((unsigned)ceil_div(width, 8 * 256), (unsigned)std::min<int64_t>(d.n, 65535)), dim3(256), 0, st, dh, gate, up,
-                       ld_h(d), d.n, d.hidden, width, slopes);
+    hipLaunchKernelGGL((k_slopes<DT, ACT>), dim3((unsigned)ceil_div(panels, 4), (unsigned)std::min<int64_t>(ceil_div(d.n, 8), 65535)), dim3(256), 0, st, dh, gate,
+                       up, ld_h(d), d.n, d.hidden, panels, slopes);
+    p.panel = d.n * ROW_BYTES;
     p.a[0] = slopes;
-    p.a[1] = slopes + width * 2;
-    p.lda = 2 * width * 2;
+    p.a[1] = slopes + panels * p.panel;
     p.b[0] = in.wg;
     p.b[1] = in.wu;
     p.ldb = in.ldw * 2;
     p.rows = d.n;
     p.cols = d.dim;
-    p.inner = width;
+    p.inner = panels * 64;
     p.inner_b = d.hidden;
     p.out[0] = static_cast<char *>(dx);
     p.ldo = ld_x(d);
