@@ -430,7 +430,7 @@ GradRoom grad_room(int64_t n, int64_t rows, int64_t dim) {
 
 int check_embed(const std::string &f, int64_t n, int64_t rows, int64_t dim) {
     if (n < 0 || n > INT32_MAX) return fail(PARO_EINVAL, f + "n must be in [0, 2^31)");
-    if (rows < 1 || rows >= INT32_MAX) return fail(PARO_EINVAL, f + "rows must be in [1, 2^31 - 1)");
+    if (rows < 1 || rows > (1 << 30)) return fail(PARO_EINVAL, f + "rows must be in [1, 2^30]");
     if (dim < 1 || dim > (1 << 24)) return fail(PARO_EINVAL, f + "dim must be in [1, 2^24]");
     return PARO_OK;
 }

@@ -57,7 +57,7 @@ __device__ __forceinline__ int wave_of() { return __builtin_amdgcn_readfirstlane
 
 // 16 bytes a lane from memory to shared memory at `to` + 16 * lane, past the registers; out of range: zeros.  In assembly because
 // the compiler, which cannot tell the stages apart, would wait for it before every read of shared memory; all_waves() waits.
-// There is no register that it writes.
+// There is no vector register that it writes; m0, which nothing else in these kernels uses, cannot be named as written.
 template <int AT>
 __device__ __forceinline__ void fill(u32x4 from, unsigned offset, unsigned to) {
     asm volatile("s_add_u32 m0, %0, %3\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(to), "v"(offset), "s"(from), "i"(AT)
