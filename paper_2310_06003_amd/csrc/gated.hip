@@ -487,6 +487,130 @@ __global__ __launch_bounds__(64 * FEW_WAVES) void k_few(const char *x, const cha
     }
 }
 
+// Backward for few tokens: each weight is read once, each of its gradients written once, in one launch, and nothing else counts.  A block takes
+// a share of the hidden elements and 512 columns (256): a lane holds its eight columns (four) of every token's x and dx, the sums in fp32, and walks down
+// the rows of the weights; dg and du are formed in fp32, and not rounded, by the block.  Rows need no alignment; the last piece of a row starts early, and some elements
+// are computed and stored twice, alike.  The shares' dx are added up, in order, by k_few_join.
+constexpr int FEW_ROWS = 64;             // hidden elements whose dg and du a block holds at a time
+constexpr int few_columns(int64_t n) { return n <= 8 ? 8 : 4; }      // of a lane: registers
+
+// COLUMNS elements of a two-byte type at any element: 4 or 8.
+template <int COLUMNS>
+__device__ __forceinline__ u32x4 load_columns(const void *base, int64_t elem) {
+    if constexpr (COLUMNS == 8) return load_piece<PARO_BF16>(base, elem);
+    const u32x2 v = load_half_piece(base, elem);
+    return u32x4{v[0], v[1], 0, 0};
+}
+template <int COLUMNS>
+__device__ __forceinline__ void store_columns(void *base, int64_t elem, u32x4 v) {
+    if constexpr (COLUMNS == 8) store_piece<PARO_BF16>(base, elem, v);
+    else store_half_piece(base, elem, u32x2{v[0], v[1]});
+}
+
+template <int DT, int ACT, int N>
+__global__ __launch_bounds__(64 * FEW_WAVES) void k_few_grad(const void *dh, const void *gate, const void *up, const void *x, const void *wg, const void *wu,
+                                                             int n, int64_t dim, int64_t hidden, int64_t ldx, int64_t ldh, int64_t share, void *dwg, void *dwu,
+                                                             float *partial) {
+    constexpr int COLUMNS = few_columns(N);
+    __shared__ __attribute__((aligned(16))) float slopes[2][FEW_ROWS][N];
+    __shared__ f32x4 sums[N][COLUMNS / 4][64];
+    const int w = wave_of(), lane = threadIdx.x & 63;
+    const int64_t first = (int64_t)blockIdx.x * share, last = first + share < hidden ? first + share : hidden;
+    const int64_t column = ((int64_t)blockIdx.y * 64 + lane) * COLUMNS;
+    const bool there = column < dim;
+    const int64_t c = column + COLUMNS <= dim ? column : dim - COLUMNS;
+    u32x4 xs[N];
+    float acc[N][COLUMNS] = {};
+#pragma unroll
+    for (int t = 0; t < N; ++t) {
+        xs[t] = u32x4{0, 0, 0, 0};
+        if (there && t < n) xs[t] = load_columns<COLUMNS>(x, t * ldx + c);
+    }
+    for (int64_t f0 = first; f0 < last; f0 += FEW_ROWS) {
+        const int rows = (int)(last - f0 < FEW_ROWS ? last - f0 : FEW_ROWS);
+        __syncthreads();
+        for (int e = threadIdx.x; e < FEW_ROWS * N; e += 64 * FEW_WAVES) {
+            const int r = e % FEW_ROWS, t = e / FEW_ROWS;           // neighbours read neighbours
+            float dg = 0.0f, du = 0.0f;
+            if (r < rows && t < n) {
+                const int64_t at = t * ldh + f0 + r;
+                const float d = load_one<DT>(dh, at);
+                float a, da;
+                act_and_slope<ACT>(load_one<DT>(gate, at), a, da);
+                dg = d * load_one<DT>(up, at) * da;
+                du = d * a;
+            }
+            slopes[0][r][t] = dg;
+            slopes[1][r][t] = du;
+        }
+        __syncthreads();
+        if (!there) continue;
+        u32x4 next[2];
+        const auto load = [&](int r) {
+            next[0] = load_columns<COLUMNS>(wg, (f0 + r) * dim + c);
+            next[1] = load_columns<COLUMNS>(wu, (f0 + r) * dim + c);
+        };
+        if (w < rows) load(w);
+        for (int r = w; r < rows; r += FEW_WAVES) {
+            const u32x4 now[2] = {next[0], next[1]};
+            if (r + FEW_WAVES < rows) load(r + FEW_WAVES);
+#pragma unroll
+            for (int of = 0; of < 2; ++of) {
+                float weight[8], dw[8] = {};
+                unpack<DT>(now[of], weight);
+#pragma unroll
+                for (int t = 0; t < N; ++t) {
+                    const float s = slopes[of][r][t];
+                    float xt[8];
+                    unpack<DT>(xs[t], xt);
+#pragma unroll
+                    for (int e = 0; e < COLUMNS; ++e) {
+                        acc[t][e] = fmaf(s, weight[e], acc[t][e]);
+                        dw[e] = fmaf(s, xt[e], dw[e]);
+                    }
+                }
+                store_columns<COLUMNS>(of ? dwu : dwg, (f0 + r) * dim + c, pack<DT>(dw));
+            }
+        }
+    }
+    // the waves' dx, one after the other
+    for (int k = 0; k < FEW_WAVES; ++k) {
+        __syncthreads();
+        if (k != w || !there) continue;
+#pragma unroll
+        for (int t = 0; t < N; ++t)
+#pragma unroll
+            for (int q = 0; q < COLUMNS / 4; ++q) {
+                f32x4 v{acc[t][4 * q], acc[t][4 * q + 1], acc[t][4 * q + 2], acc[t][4 * q + 3]};
+                if (k) v += sums[t][q][lane];
+                if (k == FEW_WAVES - 1) {
+                    if (t < n) store_piece<PARO_F32>(partial, ((int64_t)blockIdx.x * n + t) * dim + c + 4 * q, __builtin_bit_cast(u32x4, v));
+                } else {
+                    sums[t][q][lane] = v;
+                }
+            }
+    }
+}
+
+// Adds up the shares' dx: a block for 64 columns of a token, its waves each a part of the shares.
+template <int DT>
+__global__ __launch_bounds__(512) void k_few_join(const float *partial, int n, int64_t dim, int shares, int64_t ldx, void *dx) {
+    __shared__ float sums[8][64];
+    const int w = wave_of(), lane = threadIdx.x & 63;
+    const int64_t column = (int64_t)blockIdx.x * 64 + lane, t = blockIdx.y;
+    const int each = (shares + 7) / 8, from = w * each, to = from + each < shares ? from + each : shares;
+    float sum = 0.0f;
+    if (column < dim)
+#pragma unroll 8
+        for (int s = from; s < to; ++s) sum += partial[((int64_t)s * n + t) * dim + column];
+    sums[w][lane] = sum;
+    __syncthreads();
+    if (w != 0 || column >= dim) return;
+#pragma unroll
+    for (int k = 1; k < 8; ++k) sum += sums[k][lane];
+    store_one<DT>(dx, t * ldx + column, sum);
+}
+
 // dg, then du, each in panels of 64 hidden elements: [panel][tokens][64], zeros past the last element.  What a tile's stage reads of them is then a
 // run of memory, for dx (256 tokens of a panel) as for dW (64 tokens of four), where rows of 11008 would be 22 KB apart
 // (8192 tokens of 4096 x 11008 2302 us, so 2285; this kernel 150 and 141).  Rounded to the
@@ -624,9 +748,25 @@ struct Room {                            // parts of the workspace, in bytes
 int64_t ld_x(const paro_gated_t &d) { return d.ld_x ? d.ld_x : d.dim; }
 int64_t ld_h(const paro_gated_t &d) { return d.ld_h ? d.ld_h : d.hidden; }
 
+// Which backward passes k_few_grad takes (otherwise tiles, of which few rows are filled, in us, 4096 x 11008 where no size is named): 1 token 84
+// (123), 2665 x 16768, whose rows have to be copied, 116 (250), 4 85 (121), 8 94 (117); 9 122 (123), 16 129 (117), 1024 x 1024 23 (22), so with more than 8 only
+// where rows have to be copied, 16 of 1601 x 4099 38 (56), 12 of 2665 x 16768 139 (249), or are short, 512 x 22016 41 (64), 384 x 384 17 (21); and into how many
+// shares of the hidden elements.
+bool few_tokens_grad(const paro_gated_t &d) {
+    return d.n >= 1 && d.dim >= 8 && (d.n <= 8 || (d.n <= 16 && (!fills_take(d.dim, d.dim) || d.dim <= 512)));
+}
+int64_t few_shares(const paro_gated_t &d) {
+    const int64_t wanted = std::min<int64_t>(256, std::max<int64_t>(16, 1024 / ceil_div(d.dim, 64 * few_columns(d.n))));
+    return ceil_div(d.hidden, std::max<int64_t>(FEW_WAVES, ceil_div(d.hidden, wanted)));
+}
+
 Room room_of(const paro_gated_t &d, bool grad) {
     const int64_t width = up_to(d.dim, 8);
     Room r{};
+    if (grad && few_tokens_grad(d)) {
+        r.all = few_shares(d) * d.n * d.dim * 4;
+        return r;
+    }
     int64_t at = 0;
     const auto take = [&](int64_t bytes) {
         const int64_t here = at;
@@ -760,6 +900,20 @@ int backward(const paro_gated_t &d, const void *dh, const void *gate, const void
         p.out[0] = static_cast<char *>(dwg);
         p.out[1] = static_cast<char *>(dwu);
         return launch_product<DT, WEIGHT_GRAD, PARO_SILU>(p, shape_of(WEIGHT_GRAD, d.hidden, d.dim, 0), nullptr, st);
+    }
+    if (few_tokens_grad(d)) {
+        const int64_t shares = few_shares(d);
+        float *sums = reinterpret_cast<float *>(ws + r.partial);
+#define PARO_FEW_GRAD(N)                                                                                                                  \
+    hipLaunchKernelGGL((k_few_grad<DT, ACT, N>), dim3((unsigned)shares, (unsigned)ceil_div(d.dim, 64 * few_columns(N))), dim3(64 * FEW_WAVES), 0, st, dh, gate, up, x, \
+                       wg, wu, (int)d.n, d.dim, d.hidden, ld_x(d), ld_h(d), ceil_div(d.hidden, shares), dwg, dwu, sums)
+        if (d.n <= 1) PARO_FEW_GRAD(1);
+        else if (d.n <= 4) PARO_FEW_GRAD(4);
+        else if (d.n <= 8) PARO_FEW_GRAD(8);
+        else PARO_FEW_GRAD(16);
+#undef PARO_FEW_GRAD
+        hipLaunchKernelGGL((k_few_join<DT>), dim3((unsigned)ceil_div(d.dim, 64), (unsigned)d.n), dim3(512), 0, st, sums, (int)d.n, d.dim, (int)shares, ld_x(d), dx);
+        return PARO_OK;
     }
     const Inputs in = inputs_of(d, x, wg, wu, ws, r, st);
     const int64_t panels = ceil_div(d.hidden, 64);

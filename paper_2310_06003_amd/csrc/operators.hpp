@@ -141,6 +141,12 @@ typedef u32x2 half_piece_at2 __attribute__((aligned(2)));
 __device__ __forceinline__ u32x2 load_half_piece_stream(const void *base, int64_t elem) {
     return __builtin_nontemporal_load(reinterpret_cast<const half_piece_at2 *>(static_cast<const char *>(base) + elem * 2));
 }
+__device__ __forceinline__ u32x2 load_half_piece(const void *base, int64_t elem) {
+    return *reinterpret_cast<const half_piece_at2 *>(static_cast<const char *>(base) + elem * 2);
+}
+__device__ __forceinline__ void store_half_piece(void *base, int64_t elem, u32x2 v) {
+    *reinterpret_cast<half_piece_at2 *>(static_cast<char *>(base) + elem * 2) = v;
+}
 template <int DT>
 __device__ __forceinline__ float load_one(const void *base, int64_t elem) {
     if constexpr (DT == PARO_F32) return static_cast<const float *>(base)[elem];
