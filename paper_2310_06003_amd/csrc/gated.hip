@@ -763,10 +763,6 @@ int64_t few_shares(const paro_gated_t &d) {
 Room room_of(const paro_gated_t &d, bool grad) {
     const int64_t width = up_to(d.dim, 8);
     Room r{};
-    if (grad && few_tokens_grad(d)) {
-        r.all = few_shares(d) * d.n * d.dim * 4;
-        return r;
-    }
     int64_t at = 0;
     const auto take = [&](int64_t bytes) {
         const int64_t here = at;
@@ -787,6 +783,10 @@ Room room_of(const paro_gated_t &d, bool grad) {
     }
     r.partial = take(partial);
     r.all = std::max<int64_t>(at, 16);
+    if (grad && few_tokens_grad(d)) {                       // its shares from the start on, in no less room than tiles would take: at odd
+        r.partial = 0;                                      // sizes no less than the forward pass's, so that one workspace has one size
+        r.all = std::max(r.all, few_shares(d) * d.n * d.dim * 4);
+    }
     return r;
 }
 
