@@ -12,6 +12,7 @@ namespace {
 
 constexpr int WAVES = 4;                 // waves of a block: each works for itself
 constexpr int THREADS = 64 * WAVES;
+constexpr int COMPUTE_UNITS = 256;
 constexpr int64_t MAX_BLOCKS = 1 << 22;  // of a launch (tiles counted); beyond, waves take several rows
 
 __device__ __forceinline__ int wave_of() { return __builtin_amdgcn_readfirstlane(threadIdx.x >> 6); }
@@ -170,13 +171,15 @@ __global__ __launch_bounds__(SORT_THREADS) void k_sort_tokens(const Token *token
             return;
         }
         if (gridDim.y > 1) {
+            int of_slice[MAX_SLICES];               // all on their way at once
+#pragma unroll
+            for (unsigned s = 0; s < MAX_SLICES; ++s) of_slice[s] = s < gridDim.y && mine < in_range ? counts.of_row[s * rows + lo + mine] : 0;
             total = 0;
-            if (mine < in_range)
-                for (unsigned s = 0; s < gridDim.y; ++s) {
-                    const int c = counts.of_row[s * rows + lo + mine];
-                    total += c;
-                    if (s < blockIdx.y) before_slice += c;
-                }
+#pragma unroll
+            for (unsigned s = 0; s < MAX_SLICES; ++s) {
+                total += of_slice[s];
+                before_slice += s < blockIdx.y ? of_slice[s] : 0;
+            }
         }
         sum = total;
 #pragma unroll
@@ -192,7 +195,11 @@ __global__ __launch_bounds__(SORT_THREADS) void k_sort_tokens(const Token *token
         int at = sum - total;
         for (int k = 0; k < w; ++k) at += wave_total[k];
         if (gridDim.y > 1) {
-            for (unsigned s = 0; s < gridDim.y; ++s) at += counts.below[s * gridDim.x + blockIdx.x];
+            int below_in[MAX_SLICES];
+#pragma unroll
+            for (unsigned s = 0; s < MAX_SLICES; ++s) below_in[s] = s < gridDim.y ? counts.below[s * gridDim.x + blockIdx.x] : 0;
+#pragma unroll
+            for (unsigned s = 0; s < MAX_SLICES; ++s) at += below_in[s];
         } else {
 #pragma unroll
             for (int k = 0; k < SORT_WAVES; ++k) at += below_of[k];
@@ -408,15 +415,21 @@ int segment_of(int64_t n) {
 }
 constexpr int GRAD_PIECES = 4;           // pieces a lane of the sums (2: GPT-2's table 51 us, not 47, 32768 tokens of 4096 179, not 138)
 
-// Tokens of a slice of the sort.
-int64_t slice_of(int64_t n) { return std::max(SLICE, ceil_div(ceil_div(n, MAX_SLICES), SORT_THREADS) * SORT_THREADS); }
+// Tokens of a slice of the sort: all of them, or SLICE, or fewer where the table has so few rows that a block for each slice of SLICE would
+// leave most of the chip idle (20000 tokens, 5000 rows in slices of 8192 56 us, of 2048 49; but 32768 tokens, 32000 rows 134 and 142).
+int64_t slice_of(int64_t n, int64_t rows) {
+    if (n <= SLICE) return SLICE;
+    const int64_t to_fill = COMPUTE_UNITS / ceil_div(rows, SORT_ROWS);
+    const int64_t slices = std::min<int64_t>(MAX_SLICES, std::max(ceil_div(n, SLICE), to_fill));
+    return std::max<int64_t>(SLICE / 4, ceil_div(ceil_div(n, slices), SORT_THREADS) * SORT_THREADS);
+}
 
 struct GradRoom {                        // parts of the workspace, in bytes
     int64_t start, order, row_at, of_row, below, partial, all;
 };
 GradRoom grad_room(int64_t n, int64_t rows, int64_t dim) {
     const auto up = [](int64_t x) { return (x + 255) / 256 * 256; };
-    const int64_t slices = n > SLICE ? ceil_div(n, slice_of(n)) : 0;
+    const int64_t slices = n > SLICE ? ceil_div(n, slice_of(n, rows)) : 0;
     GradRoom g;
     g.start = 0;
     g.order = up((rows + 1) * 4);
@@ -530,7 +543,7 @@ int paro_embed_grad(const void *dout, int dtype, int64_t ld_dout, const void *to
         char *ws = static_cast<char *>(workspace);
         int *start = reinterpret_cast<int *>(ws + g.start), *order = reinterpret_cast<int *>(ws + g.order);
         int *row_at = reinterpret_cast<int *>(ws + g.row_at);
-        const int64_t slice = slice_of(n);
+        const int64_t slice = slice_of(n, rows);
         const dim3 sort_grid((unsigned)ceil_div(rows, SORT_ROWS), (unsigned)std::max<int64_t>(1, ceil_div(n, slice)));
         const SliceCounts counts{reinterpret_cast<int *>(ws + g.of_row), reinterpret_cast<int *>(ws + g.below)};
 #define PARO_SORT(TOKEN, COUNT)                                                                                                        \
