@@ -300,12 +300,51 @@ __device__ __forceinline__ void store_row(float (&acc)[C][Elem<GT>::E], void *gr
     }
 }
 
+// Zeros for the rows without a token, in a span of the gradient as it lies in memory: aligned pieces, whatever the rows' width, and all lanes
+// have some, however narrow the rows are (a wave for each row: 35224 rows of 7443 fp32 elements 277 us, so 188; 87603 of 128 24 and 15).  A
+// piece that a row with tokens shares goes element by element.
+template <int GT, int C>
+__device__ __forceinline__ void zeros_of_span(void *grad, const int *start, int64_t from, int64_t rows, int64_t dim) {
+    constexpr int E = Elem<GT>::E;
+    const int64_t row0 = (from > 0 ? from : 0) / dim, all = rows * dim;
+    if (from + 64 * C * E <= (row0 + 1) * dim) {    // of one row: nothing to find out by lane (32768 tokens of 4096 145 us without, 133)
+        if (start[row0] != start[row0 + 1]) return;
+        if (from >= 0) {
+#pragma unroll
+            for (int c = 0; c < C; ++c) store_stream<GT>(grad, from + c * 64 * E + lane_of() * E, u32x4{0, 0, 0, 0});
+            return;
+        }
+    }
+    unsigned empty[C];                              // bit 0: the row of the piece's first element has no token, bit 1: the next one
+    int64_t elem[C], left[C];
+#pragma unroll
+    for (int c = 0; c < C; ++c) {
+        elem[c] = from + c * 64 * E + lane_of() * E;
+        const int64_t at = elem[c] > 0 ? elem[c] : 0;
+        const int64_t v = row0 + (unsigned)(at - row0 * dim) / (unsigned)dim;
+        left[c] = (v + 1) * dim - elem[c];
+        const int64_t v0 = v < rows ? v : rows, v1 = v + 1 < rows ? v + 1 : rows, v2 = v + 2 < rows ? v + 2 : rows;
+        const int s0 = start[v0], s1 = start[v1], s2 = start[v2];
+        empty[c] = (s0 == s1 ? 1 : 0) | (s1 == s2 ? 2 : 0);
+    }
+#pragma unroll
+    for (int c = 0; c < C; ++c) {
+        if (elem[c] >= 0 && elem[c] + E <= all && (empty[c] & 1) && (left[c] >= E || (empty[c] & 2))) {
+            store_stream<GT>(grad, elem[c], u32x4{0, 0, 0, 0});
+        } else {
+#pragma unroll
+            for (int j = 0; j < E; ++j)
+                if (elem[c] + j >= 0 && elem[c] + j < all && (empty[c] & (j < left[c] ? 1 : 2))) store_one<GT>(grad, elem[c] + j, 0.0f);
+        }
+    }
+}
+
 // Three kinds of blocks, in the order in which they start: what reads goes before what only writes, since a read that waits behind a stream of
 // stores takes microseconds (GPT-2's table 52 us with the rows in their own order, so 47; 32768 tokens of 4096 141 and 138).
 //   segments   a wave takes a segment of the sorted tokens: runs of more than `seg` are summed segment by segment, in parallel.  Of one
 //              segment such a run holds the beginning (slot 0), or the end and not the beginning (slot 1)
 //   runs       a wave takes a place among the sorted tokens, and sums the run that begins there, if a short one does
-//   the rest   a wave takes a row of the table's gradient and writes zeros, if no token is of that row
+//   the rest   a wave takes a span of the table's gradient and writes zeros where no token is of the row
 template <int DT, int GT, int C>
 __global__ __launch_bounds__(THREADS) void k_sums(const void *dout, int64_t ld, const int *start, const int *order, const int *row_at, int64_t rows,
                                                   int64_t dim, int seg, unsigned seg_blocks, unsigned run_blocks, float scale, float *partial, void *grad) {
@@ -339,13 +378,11 @@ __global__ __launch_bounds__(THREADS) void k_sums(const void *dout, int64_t ld, 
             store_row<GT>(acc, grad, v, col, dim, scale);
         }
     } else {
-        const unsigned first = seg_blocks + run_blocks;
-        for (int64_t v = (int64_t)(blockIdx.x - first) * WAVES + wave_of(); v < rows; v += (int64_t)(gridDim.x - first) * WAVES) {
-            if (start[v] != start[v + 1]) continue;
-#pragma unroll
-            for (int c = 0; c < C; ++c)
-                if (col[c] < dim) store_stream<GT>(grad, v * dim + col[c], u32x4{0, 0, 0, 0});
-        }
+        const unsigned first = seg_blocks + run_blocks, blocks = gridDim.x - first;
+        const int64_t lead = (reinterpret_cast<uintptr_t>(grad) & 127) / Elem<GT>::BYTES, all = rows * dim;
+        for (int64_t s = ((int64_t)blockIdx.y * blocks + (blockIdx.x - first)) * WAVES + wave_of(); s * (64 * C * E) - lead < all;
+             s += (int64_t)blocks * gridDim.y * WAVES)
+            zeros_of_span<GT, C>(grad, start, s * (64 * C * E) - lead, rows, dim);
     }
 }
 
@@ -473,7 +510,9 @@ void launch_sums(const void *dout, int64_t ld, int64_t n, float scale, void *gra
     const unsigned seg_blocks = n > seg ? (unsigned)ceil_div(ceil_div(n, seg), WAVES) : 0;
     const int64_t tiles = ceil_div(dim, 64 * GRAD_PIECES * Elem<GT>::E);
     const unsigned run_blocks = n ? grid_for(n, 2 * tiles).x : 0;
-    hipLaunchKernelGGL((k_sums<DT, GT, GRAD_PIECES>), dim3(seg_blocks + run_blocks + grid_for(rows, 2 * tiles).x, (unsigned)tiles), dim3(THREADS), 0, st, dout,
+    const int64_t spans = rows * dim / (64 * GRAD_PIECES * Elem<GT>::E) + 2;
+    const unsigned zero_blocks = (unsigned)std::max<int64_t>(1, std::min(MAX_BLOCKS / 2 / tiles, ceil_div(spans, tiles * WAVES)));
+    hipLaunchKernelGGL((k_sums<DT, GT, GRAD_PIECES>), dim3(seg_blocks + run_blocks + zero_blocks, (unsigned)tiles), dim3(THREADS), 0, st, dout,
                        ld, start, order, row_at, rows, dim, seg, seg_blocks, run_blocks, scale, partial, grad);
     if (seg_blocks)
         hipLaunchKernelGGL((k_join<GT>), dim3(seg_blocks, (unsigned)ceil_div(dim, 64 * 4)), dim3(THREADS), 0, st, start, row_at, rows, dim, seg,
