@@ -224,6 +224,9 @@ __global__ __launch_bounds__(SORT_THREADS) void k_sort_tokens(const Token *token
     });
 }
 
+// Pieces a lane of the sums takes: as many as a row has for it (16 rows' pieces in flight in any case), at most (2: GPT-2's table 51 us, not
+// 47, 32768 tokens of 4096 179, not 138).  4 whatever the width: 60000 tokens of 640 90 us, so 84; of 64 fp32 elements 66, so 60.
+constexpr int GRAD_PIECES = 4;
 // ---------------------------------------------------------------- sums over the sorted tokens
 // What a lane loads of a row of dout: as many elements as a piece of the gradient has, so that every store instruction of a wave covers
 // whole cache lines (fp32 gradients of two-byte rows in pieces of dout, 32 bytes a lane: GPT-2's table 56 us, so 40).
@@ -254,7 +257,7 @@ struct RowPiece {
 template <int DT, int GT, int C>
 __device__ __forceinline__ void add_rows(float (&acc)[C][Elem<GT>::E], const void *dout, int64_t ld, const int *order, int a, int b,
                                          const int64_t (&col)[C], int64_t dim) {
-    constexpr int U = 4;                            // rows in flight; 2: 52 and 149 us, 6: 46 and 145
+    constexpr int U = 16 / C;                       // rows in flight; for four pieces 2: 52 and 149 us, 6: 46 and 145
     for (int k0 = a; k0 < b; k0 += 64) {
         const int mine = k0 + lane_of() < b ? order[k0 + lane_of()] : 0, all = b - k0 < 64 ? b - k0 : 64;
         const auto add = [&](int k, auto count_) {
@@ -275,7 +278,14 @@ __device__ __forceinline__ void add_rows(float (&acc)[C][Elem<GT>::E], const voi
         };
         int k = 0;
         for (; k + U <= all; k += U) add(k, std::integral_constant<int, U>{});
-        for (; k < all; ++k) add(k, std::integral_constant<int, 1>{});
+        static_for<1, 5>([&](auto i) {              // the rest in halves; row by row 30000 tokens of 128 43 us, so 38
+            constexpr int fewer = U >> i;
+            if constexpr (fewer > 0)
+                if (k + fewer <= all) {
+                    add(k, std::integral_constant<int, fewer>{});
+                    k += fewer;
+                }
+        });
     }
 }
 
@@ -380,9 +390,9 @@ __global__ __launch_bounds__(THREADS) void k_sums(const void *dout, int64_t ld, 
     } else {
         const unsigned first = seg_blocks + run_blocks, blocks = gridDim.x - first;
         const int64_t lead = (reinterpret_cast<uintptr_t>(grad) & 127) / Elem<GT>::BYTES, all = rows * dim;
-        for (int64_t s = ((int64_t)blockIdx.y * blocks + (blockIdx.x - first)) * WAVES + wave_of(); s * (64 * C * E) - lead < all;
+        for (int64_t s = ((int64_t)blockIdx.y * blocks + (blockIdx.x - first)) * WAVES + wave_of(); s * (64 * GRAD_PIECES * E) - lead < all;
              s += (int64_t)blocks * gridDim.y * WAVES)
-            zeros_of_span<GT, C>(grad, start, s * (64 * C * E) - lead, rows, dim);
+            zeros_of_span<GT, GRAD_PIECES>(grad, start, s * (64 * GRAD_PIECES * E) - lead, rows, dim);
     }
 }
 
@@ -450,7 +460,6 @@ int segment_of(int64_t n) {
     while (n / seg > MAX_SEGMENTS) seg *= 2;
     return seg;
 }
-constexpr int GRAD_PIECES = 4;           // pieces a lane of the sums (2: GPT-2's table 51 us, not 47, 32768 tokens of 4096 179, not 138)
 
 // Tokens of a slice of the sort: all of them, or SLICE, or fewer where the table has so few rows that a block for each slice of SLICE would
 // leave most of the chip idle (20000 tokens, 5000 rows in slices of 8192 56 us, of 2048 49; but 32768 tokens, 32000 rows 134 and 142).
@@ -496,7 +505,7 @@ void launch_embed(const void *table, const void *tokens, int64_t n, int64_t firs
                        static_cast<const Token *>(tokens), n, first, rows, dim, scale, out, ld);
 }
 
-template <int DT, int GT>
+template <int DT, int GT, int C>
 void launch_sums(const void *dout, int64_t ld, int64_t n, float scale, void *grad, int64_t rows, int64_t dim, char *ws, const GradRoom &g,
                  hipStream_t st) {
     const int *start = reinterpret_cast<int *>(ws + g.start), *order = reinterpret_cast<int *>(ws + g.order);
@@ -508,11 +517,11 @@ void launch_sums(const void *dout, int64_t ld, int64_t n, float scale, void *gra
     const int seg = segment_of(n), *row_at = reinterpret_cast<int *>(ws + g.row_at);
     float *partial = reinterpret_cast<float *>(ws + g.partial);
     const unsigned seg_blocks = n > seg ? (unsigned)ceil_div(ceil_div(n, seg), WAVES) : 0;
-    const int64_t tiles = ceil_div(dim, 64 * GRAD_PIECES * Elem<GT>::E);
+    const int64_t tiles = ceil_div(dim, 64 * C * Elem<GT>::E);
     const unsigned run_blocks = n ? grid_for(n, 2 * tiles).x : 0;
     const int64_t spans = rows * dim / (64 * GRAD_PIECES * Elem<GT>::E) + 2;
     const unsigned zero_blocks = (unsigned)std::max<int64_t>(1, std::min(MAX_BLOCKS / 2 / tiles, ceil_div(spans, tiles * WAVES)));
-    hipLaunchKernelGGL((k_sums<DT, GT, GRAD_PIECES>), dim3(seg_blocks + run_blocks + zero_blocks, (unsigned)tiles), dim3(THREADS), 0, st, dout,
+    hipLaunchKernelGGL((k_sums<DT, GT, C>), dim3(seg_blocks + run_blocks + zero_blocks, (unsigned)tiles), dim3(THREADS), 0, st, dout,
                        ld, start, order, row_at, rows, dim, seg, seg_blocks, run_blocks, scale, partial, grad);
     if (seg_blocks)
         hipLaunchKernelGGL((k_join<GT>), dim3(seg_blocks, (unsigned)ceil_div(dim, 64 * 4)), dim3(THREADS), 0, st, start, row_at, rows, dim, seg,
@@ -597,7 +606,10 @@ int paro_embed_grad(const void *dout, int dtype, int64_t ld_dout, const void *to
         }
 #undef PARO_SORT
         PARO_LAUNCHED("paro_embed_grad");
-#define PARO_SUMS(DT, GT) launch_sums<DT, GT>(dout, ld_dout, n, scale, grad, rows, dim, ws, g, st)
+#define PARO_SUMS(DT, GT)                                                                                                              \
+    (dim <= 64 * Elem<GT>::E    ? launch_sums<DT, GT, 1>                                                                               \
+     : dim <= 128 * Elem<GT>::E ? launch_sums<DT, GT, 2>                                                                               \
+                                : launch_sums<DT, GT, GRAD_PIECES>)(dout, ld_dout, n, scale, grad, rows, dim, ws, g, st)
         if (dtype == PARO_F32) PARO_SUMS(PARO_F32, PARO_F32);
         else if (dtype == PARO_F16 && grad_dtype == PARO_F16) PARO_SUMS(PARO_F16, PARO_F16);
         else if (dtype == PARO_F16) PARO_SUMS(PARO_F16, PARO_F32);
