@@ -650,27 +650,46 @@ __global__ __launch_bounds__(256) void k_slopes(const void *dh, const void *gate
 }
 
 // Rows that the fills cannot take - a row or the distance between two is no multiple of 16 bytes - copied to where they can, zeros behind:
-// up to three arrays of one width in a launch.
+// up to three arrays of one width in a launch.  A thread takes pieces as they lie in the copy (a row for each block: 197 tokens of 231 x 8576
+// 30 us, so 21).  A piece that ends past its row is loaded whole where the array goes on, and masked.
 struct Copies {
     const void *from[3];
     void *to[3];
     int64_t ld[3], rows[3];
     int64_t cols, width;
 };
+constexpr int ALIGN_PIECES = 4;
 __global__ __launch_bounds__(256) void k_align(Copies a) {
-    const int which = blockIdx.z;
+    const int which = blockIdx.y;
     const void *from = a.from[which];
-    const int64_t c = ((int64_t)blockIdx.x * 256 + threadIdx.x) * 8;
-    if (c >= a.width) return;
-    for (int64_t r = blockIdx.y; r < a.rows[which]; r += gridDim.y) {
-        u32x4 v{0, 0, 0, 0};
-        if (c + 8 <= a.cols) {
-            v = load_piece<PARO_BF16>(from, r * a.ld[which] + c);
-        } else {
-            for (int e = 0; e < 8; ++e)
-                if (c + e < a.cols) v[e / 2] |= (unsigned)static_cast<const unsigned short *>(from)[r * a.ld[which] + c + e] << (16 * (e & 1));
+    const int64_t ld = a.ld[which], rows = a.rows[which], all = rows * (a.width / 8), end = (rows - 1) * ld + a.cols;
+    const unsigned of_row = (unsigned)(a.width / 8);
+    for (int64_t first = (int64_t)blockIdx.x * (256 * ALIGN_PIECES); first < all; first += (int64_t)gridDim.x * (256 * ALIGN_PIECES)) {
+        const int64_t row0 = first / of_row;
+        const unsigned past = (unsigned)(first - row0 * of_row) + threadIdx.x;
+        u32x4 v[ALIGN_PIECES];
+        int left[ALIGN_PIECES];
+#pragma unroll
+        for (int i = 0; i < ALIGN_PIECES; ++i) {
+            const unsigned down = (past + i * 256) / of_row;
+            const int64_t r = row0 + down, c = (int64_t)(past + i * 256 - down * of_row) * 8;
+            left[i] = (int)(a.cols - c);
+            v[i] = u32x4{0, 0, 0, 0};
+            if (r >= rows) continue;
+            if (r * ld + c + 8 <= end) {
+                v[i] = load_piece<PARO_BF16>(from, r * ld + c);
+            } else {
+                for (int e = 0; e < 8; ++e)
+                    if (e < left[i]) v[i][e / 2] |= (unsigned)static_cast<const unsigned short *>(from)[r * ld + c + e] << (16 * (e & 1));
+            }
         }
-        store_piece<PARO_BF16>(a.to[which], r * a.width + c, v);
+#pragma unroll
+        for (int i = 0; i < ALIGN_PIECES; ++i) {
+            const int64_t to = first + threadIdx.x + i * 256;
+#pragma unroll
+            for (int q = 0; q < 4; ++q) v[i][q] &= left[i] >= 2 * q + 2 ? 0xFFFFFFFFu : left[i] == 2 * q + 1 ? 0xFFFFu : 0u;
+            if (to < all) store_piece<PARO_BF16>(a.to[which], to * 8, v[i]);
+        }
     }
 }
 
@@ -690,7 +709,7 @@ struct Shape {                           // of a product's launch
 };
 // Which tiles, and how the inner dimension is split: what is quickest by this reckoning, in us.  A round of tiles takes its stages, 1.55 each of
 // a 256 x 256 tile, one a compute unit, 1.2 of two of 128 x 128.  The tiles beyond whole rounds may be split so that their blocks fill the chip
-// once, into shares of at least eight stages; then their sums are written and read at 2.5 TB/s, with a launch of 5.  Against measured
+// once, into at most 32 shares (488 tokens of 128 x 17536 backward 61 us, with 16 66, with 64 69) of at least eight stages; then their sums are written and read at 2.5 TB/s, with a launch of 5.  Against measured
 // times (bf16, silu, forward with the projections stored), large tiles | small ones: 300 tokens of 2048 x 5632 40 | 38, reckoned 38 | 38; 512 of 4096 x 11008 108 | 133, 99 | 124;
 // 2000 of 4096 x 512 43 | 35, 44 | 36; 4000 of 1024 x 4096 77 | 109, 50 | 77 (it leaves out the stores of the result, alike in both).
 // rows and columns: of the result (of WEIGHT_GRAD of one part, of FORWARD of both parts)
@@ -703,7 +722,7 @@ Shape shape_of(int mode, int64_t rows, int64_t cols, int64_t inner) {
         Shape s{large, ceil_div(rows, side) * (mode == WEIGHT_GRAD ? 2 : 1), ceil_div(cols, mode == FORWARD ? side / 2 : side), 0, 1};
         const int64_t tiles = s.tiles_m * s.tiles_n, rest = tiles % at_once;
         const double filled = (double)rows / (double)(ceil_div(rows, side) * side), stage = large ? 1.55 : 1.2;
-        for (int64_t splits = 1; splits == 1 || (rest && rest * splits <= at_once && splits <= 16 && stages / splits >= 8); ++splits) {
+        for (int64_t splits = 1; splits == 1 || (rest && rest * splits <= at_once && splits <= 32 && stages / splits >= 8); ++splits) {
             s.splits = splits;
             s.whole = splits == 1 ? tiles : tiles - rest;
             const int64_t in_turn = splits == 1 ? ceil_div(tiles, at_once) * stages : tiles / at_once * stages + ceil_div(stages, splits);
@@ -831,10 +850,12 @@ Inputs inputs_of(const paro_gated_t &d, const void *x, const void *wg, const voi
     c.cols = d.dim;
     c.width = up_to(d.dim, 8);
     unsigned copies = 0;
+    int64_t most = 0;
     const auto copy = [&](const char *&rows, int64_t ld, int64_t n, int64_t room) {
         c.from[copies] = rows;
         c.ld[copies] = ld;
         c.rows[copies] = n;
+        most = std::max(most, n);
         c.to[copies++] = ws + room;
         rows = ws + room;
     };
@@ -848,7 +869,7 @@ Inputs inputs_of(const paro_gated_t &d, const void *x, const void *wg, const voi
         in.ldx = c.width;
     }
     if (copies)
-        hipLaunchKernelGGL(k_align, dim3((unsigned)ceil_div(c.width, 8 * 256), (unsigned)std::min<int64_t>(std::max(d.n, d.hidden), 65535), copies), dim3(256), 0,
+        hipLaunchKernelGGL(k_align, dim3((unsigned)std::min<int64_t>(ceil_div(most * (c.width / 8), 256 * ALIGN_PIECES), 1 << 20), copies), dim3(256), 0,
                            st, c);
     return in;
 }
