@@ -71,17 +71,17 @@ __device__ __forceinline__ float teacher_of(const void *t, int64_t at, int dtype
 template <int DT, int THREADS, int HELD, bool LOSS, bool GRAD>
 __global__ __launch_bounds__(THREADS, HELD == 16 ? 4 : 1) void k_distill(const void *logits, const void *teacher, const int32_t *ids, const float *dloss, float *loss,
                                                      float *lse, void *dlogits, Row d) {
-    constexpr int E = Elem<DT>::E;
+    constexpr int E = Elem<DT>::E, ROOM = 4 * THREADS < MAX_K ? 4 * THREADS : MAX_K;      // for entries
     constexpr unsigned MINUS_INF = DT == PARO_F32 ? 0xFF800000u : DT == PARO_F16 ? 0xFC00FC00u : 0xFF80FF80u;
-    __shared__ __attribute__((aligned(16))) int s_id[MAX_K];
-    __shared__ float s_p[MAX_K];
+    __shared__ __attribute__((aligned(16))) int s_id[ROOM];
+    __shared__ float s_p[ROOM];
     __shared__ MaxSum s_teacher[THREADS / 64], s_student[THREADS / 64];
     __shared__ float s_loss[THREADS / 64];
     constexpr int LISTS = GRAD && HELD ? HELD * THREADS + 1 : 1;
     __shared__ int s_list[LISTS];                                // of each piece, and of the short one: an entry + 1, or none
-    __shared__ short s_next[GRAD && HELD ? MAX_K : 1];           // the entry + 1 after an entry
+    __shared__ short s_next[GRAD && HELD ? ROOM : 1];           // the entry + 1 after an entry
     const int64_t row = blockIdx.x;
-    const int tid = threadIdx.x;
+    const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid & ~63);
     const int k = (int)d.k;
     const char *z = static_cast<const char *>(logits) + row * d.ld_logits * Elem<DT>::BYTES;
     char *dz = GRAD ? static_cast<char *>(dlogits) + row * d.ld_dlogits * Elem<DT>::BYTES : nullptr;
@@ -100,7 +100,7 @@ __global__ __launch_bounds__(THREADS, HELD == 16 ? 4 : 1) void k_distill(const v
         s_p[j] = t;
         if (held) top = join(top, MaxSum{t, 1.0f}, c);
     }
-    if (tid < 4 && k + tid < MAX_K) s_id[k + tid] = -1;
+    if (tid < 4 && k + tid < ROOM) s_id[k + tid] = -1;
     top = block_join<THREADS>(top, s_teacher, c);
     const bool some = top.s != 0.0f;                             // NaN counts as something
 
@@ -133,7 +133,7 @@ __global__ __launch_bounds__(THREADS, HELD == 16 ? 4 : 1) void k_distill(const v
     }
     if (tid < rest) last = load_one<DT>(z, pieces * E + tid);
     // The student's logits at the teacher's places, before anything is overwritten.
-    constexpr int OWN = MAX_K / THREADS > 0 ? MAX_K / THREADS : 1;
+    constexpr int OWN = ROOM / THREADS;
     float at_id[OWN];
 #pragma unroll
     for (int o = 0; o < OWN; ++o) {
@@ -159,7 +159,7 @@ __global__ __launch_bounds__(THREADS, HELD == 16 ? 4 : 1) void k_distill(const v
         if constexpr (HELD > 0) {
 #pragma unroll
             for (int h = 0; h < HELD; ++h) {
-                take(held[h]);
+                if (h * THREADS + wave < pieces) take(held[h]);     // 4000 rows of 17000 60 us without, 53
                 apart(held[h]);
             }
         } else {
@@ -248,7 +248,7 @@ __global__ __launch_bounds__(THREADS, HELD == 16 ? 4 : 1) void k_distill(const v
                     for (int j = second; j && 4 * count * count <= k; j = s_next[j - 1]) ++count;
                     if (4 * count * count <= k) {
                         for (int before = 0; count > 0; --count) {
-                            int next = MAX_K + 1;
+                            int next = ROOM + 1;
                             for (int j = entry; j; j = s_next[j - 1]) next = j > before && j < next ? j : next;
                             add(s_id[next - 1], s_p[next - 1]);
                             before = next;
@@ -265,11 +265,11 @@ __global__ __launch_bounds__(THREADS, HELD == 16 ? 4 : 1) void k_distill(const v
 #pragma unroll
             for (int h = 0; h < HELD; ++h) {
                 const int i = h * THREADS + tid;
-                float x[E];
-                unpack<DT>(held[h], x);
-#pragma unroll
-                for (int e = 0; e < E; ++e) x[e] = q(x[e]) * w;
                 if (i < pieces) {
+                    float x[E];
+                    unpack<DT>(held[h], x);
+#pragma unroll
+                    for (int e = 0; e < E; ++e) x[e] = q(x[e]) * w;
                     take_off(i, x);
                     store_stream<DT>(dz, (int64_t)i * E, pack<DT>(x));      // 2047 rows of 50257 in fp32 148 us, so 141
                 }
@@ -328,8 +328,15 @@ void launch(const paro_distill_t &d, const void *logits, const void *teacher, co
 #define PARO_DISTILL(THREADS, HELD)                                                                                                        \
     hipLaunchKernelGGL((k_distill<DT, THREADS, HELD, LOSS, GRAD>), dim3((unsigned)d.n), dim3(THREADS), 0, st, logits, teacher, ids, dloss, \
                        loss, lse, dlogits, r)
-    if (pieces <= 256 * 4) PARO_DISTILL(256, 4);
-    else if (pieces <= 256 * 16) PARO_DISTILL(256, 16);             // 16384 rows of 32000 by 512 threads 409 us, by 256 380
+    // Few threads a row, so that many rows are under way and each thread has work: 12008 rows of 1717, loss alone, by 256 threads 31 us, by 64 15;
+    // 6000 of 6000 by 256 23, by 128 18; 5602 of 12509 in fp16 in 16 pieces a thread 73, in 8 63; 16384 of 32000 by 512 threads 409, by 256
+    // 380.  But entries enough for a thread, four: 30 rows of 2000 with 1000 entries by 64 threads 22, by 256 10.
+    if (pieces <= 64 * 4 && d.k <= 4 * 64) PARO_DISTILL(64, 4);
+    else if (pieces <= 128 * 4 && d.k <= 4 * 128) PARO_DISTILL(128, 4);
+    else if (pieces <= 128 * 8 && d.k <= 4 * 128) PARO_DISTILL(128, 8);
+    else if (pieces <= 256 * 4) PARO_DISTILL(256, 4);
+    else if (pieces <= 256 * 8) PARO_DISTILL(256, 8);
+    else if (pieces <= 256 * 16) PARO_DISTILL(256, 16);
     else if (pieces <= 512 * 16) PARO_DISTILL(512, 16);
     else if (pieces <= 1024 * 16) PARO_DISTILL(1024, 16);
     else PARO_DISTILL(1024, 0);
