@@ -221,3 +221,28 @@ def test_in_a_graph_and_on_another_stream(paro):
         step(*ref)
         torch.cuda.synchronize()
         assert all(torch.equal(a, b) for a, b in zip(ref, got))
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("v,span,k", [(1500, 1500, 250), (1500, 40, 250), (4000, 90, 512), (4000, 30, 40), (8000, 200, 300), (8000, 8000, 1024), (16000, 500, 600),
+                                      (16003, 64, 24), (30000, 3000, 1024), (60000, 16, 16)])
+def test_several_entries_in_a_piece(paro, v, span, k, dtype):
+    """Places that are named often and lie side by side, few of them and many; twice, with the same bits."""
+    z, t, _ = some_inputs(4, v, k, v + k, masked=False)
+    ids = torch.randint(0, span, (4, k), generator=rng(k)) + torch.tensor([[0], [v - span], [(v - span) // 2], [0]])
+    ids[3, ::3] = -1
+    z.scatter_(1, ids.clamp(0, v - 1), t + 4)
+    run_all(paro, z, t, ids, 2.0, dtype, "f32")
+    d = paro.make_distill(n=4, vocab=v, k=k, temperature=2.0, dtype=code(paro, dtype), teacher_dtype=paro.PARO_F32)
+    zd, td, idd = z.to(DEV, TORCH[dtype]), t.to(DEV), ids.int().to(DEV)
+    loss, got = torch.empty(4, device=DEV), [torch.empty(4, v, dtype=TORCH[dtype], device=DEV) for _ in range(3)]
+    for dz in got:
+        paro.paro_distill_step(d, zd.data_ptr(), td.data_ptr(), idd.data_ptr(), 0, loss.data_ptr(), dz.data_ptr(), stream())
+    assert torch.equal(got[0], got[1]) and torch.equal(got[0], got[2])
+
+
+@pytest.mark.parametrize("dtype,v", [("bf16", v) for v in (2047, 2048, 2049, 2055, 2056, 4103, 4104, 8191, 8199, 8200, 16384, 16391, 16392, 24577)]
+                         + [("f32", v) for v in (1023, 1024, 1027, 1028, 2051, 2052, 4099, 8195, 8196, 16383)])
+def test_row_lengths_between_two_launches(paro, dtype, v):
+    z, t, ids = some_inputs(3, v, 7, v)
+    run_all(paro, z, t, ids, 2.0, dtype, "bf16", pad=v % 3)

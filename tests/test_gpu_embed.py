@@ -164,3 +164,24 @@ def test_offsets_beyond_32_bits(paro, dtype):
     paro.paro_embed_grad(out.data_ptr(), code(paro, dtype), 0, tokens.data_ptr(), paro.PARO_I32, v, 0, 0.5, table.data_ptr(), code(paro, dtype), v, dim,
                          ws.data_ptr(), ws.numel(), stream())
     assert bool((table[-1] == 3.0).all()) and float(table.sum()) == 3.0 * dim
+
+
+@pytest.mark.parametrize("grad_dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("offset", [0, 1, 7, 31, 64, 77])
+@pytest.mark.parametrize("v,dim", [(1, 8), (2, 9), (700, 8), (300, 33), (513, 100), (40, 1031), (9, 5003)])
+def test_rows_without_a_token_are_zeros_wherever_the_table_lies(paro, v, dim, offset, grad_dtype):
+    """A gradient that begins at any element, few tokens or none: zeros in all other rows, nothing before and nothing behind."""
+    for tokens in (torch.tensor([v // 2, v - 1, v // 2]), torch.tensor([v]), torch.arange(0, v, 2)):
+        n, guard = tokens.numel(), 200
+        whole = torch.full((guard + offset + v * dim + guard,), 9.0, dtype=TORCH[grad_dtype], device=DEV)
+        grad = whole[guard - guard % 8 + offset:][:v * dim].view(v, dim)
+        dout = torch.randn(n, dim, generator=rng(v)).to(torch.bfloat16)
+        ws, dev, dout_dev = workspace(paro.paro_embed_grad_workspace(n, v, dim)), tokens.to(DEV), dout.to(DEV)
+        paro.paro_embed_grad(dout_dev.data_ptr(), paro.PARO_BF16, dim, dev.data_ptr(), paro.PARO_I64, n, 0, 1.0, grad.data_ptr(),
+                             code(paro, grad_dtype), v, dim, ws.data_ptr(), ws.numel(), stream())
+        held = tokens < v
+        ref = torch.zeros(v, dim, dtype=torch.float64).index_add_(0, tokens[held], dout[held].double())
+        check(grad, ref, rounding(ref, grad_dtype, 4 * EPS32 * ref.abs() + 8 * EPS32), "gradient")     # at most two summands of size below 8
+        assert bool((grad[ref.to(DEV).abs().sum(dim=1) == 0] == 0).all()), "a row without a token is not zeros"
+        grad.fill_(9.0)
+        assert bool((whole == 9.0).all()), "wrote beside the gradient"
