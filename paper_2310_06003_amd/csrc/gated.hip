@@ -147,12 +147,12 @@ __device__ __forceinline__ void finish(const Product &p, const Place<MODE, BM, B
         }
     } else {
 #pragma unroll
-        for (int j = 0; j < 4; j += 2) store8<DT>(p, p.out[at.part], m, at.col0 + (wn * 4 + j) * 16, acc[j], acc[j + 1]);
+        for (int j = 0; j < 4; j += 2) store8<DT>(p, at.part ? p.out[1] : p.out[0], m, at.col0 + (wn * 4 + j) * 16, acc[j], acc[j + 1]);
     }
 }
 
 template <int DT, int MODE, int ACT, int BM, int BN, int WAVES_M, int WAVES_N>
-__global__ __launch_bounds__(64 * WAVES_M * WAVES_N) void k_product(Product p) {
+__device__ __forceinline__ void product(const Product p, unsigned block, unsigned blocks) {
     constexpr int THREADS_ = 64 * WAVES_M * WAVES_N;
     constexpr int TM = BM / WAVES_M / 16, TN = BN / WAVES_N / 16;             // 16x16 tiles of a wave
     constexpr int A_BYTES = BM * ROW_BYTES, B_BYTES = BN * ROW_BYTES, PART = A_BYTES;
@@ -163,11 +163,11 @@ __global__ __launch_bounds__(64 * WAVES_M * WAVES_N) void k_product(Product p) {
     const unsigned lds0 = (unsigned)(uintptr_t)(lds_char *)ring;
     const int w = wave_of(), lane = threadIdx.x & 63, wm = w / WAVES_N, wn = w % WAVES_N;
     // The block's tile, and its share of the inner dimension.
-    const bool is_whole = blockIdx.x < p.whole;
-    const unsigned others = is_whole ? 0 : (gridDim.x - p.whole) / p.splits, among = is_whole ? 0 : blockIdx.x - p.whole;
+    const bool is_whole = block < p.whole;
+    const unsigned others = is_whole ? 0 : (blocks - p.whole) / p.splits, among = is_whole ? 0 : block - p.whole;
     const unsigned split = is_whole ? 0 : among / others, split_tile = is_whole ? 0 : in_runs(among - split * others, others);
     const unsigned splits = is_whole ? 1 : p.splits;
-    const Place<MODE, BM, BN> at(p, is_whole ? in_runs(blockIdx.x, p.whole) : p.whole + split_tile);
+    const Place<MODE, BM, BN> at(p, is_whole ? in_runs(block, p.whole) : p.whole + split_tile);
     const int64_t row0 = at.row0, col0 = at.col0;
     const int out_part = at.part;
 
@@ -222,15 +222,15 @@ __global__ __launch_bounds__(64 * WAVES_M * WAVES_N) void k_product(Product p) {
     const int64_t a_stage = A_ACROSS ? STEPS * ROW_BYTES : A_PANELS ? p.panel : ROW_BYTES, b_stage = B_ACROSS ? STEPS * p.ldb : ROW_BYTES;
     const auto begin_a = [&](int part, int stage) {
         const int64_t k0 = (int64_t)stage * STEPS;
-        a_from = descriptor(A_ACROSS   ? p.a[out_part] + row0 / 64 * p.panel + k0 * ROW_BYTES
-                            : A_PANELS ? p.a[part] + (k0 / 64) * p.panel + row0 * ROW_BYTES
-                                       : p.a[part] + row0 * p.lda + k0 * 2);
+        a_from = descriptor(A_ACROSS   ? (out_part ? p.a[1] : p.a[0]) + row0 / 64 * p.panel + k0 * ROW_BYTES
+                            : A_PANELS ? (part ? p.a[1] : p.a[0]) + (k0 / 64) * p.panel + row0 * ROW_BYTES
+                                       : (part ? p.a[1] : p.a[0]) + row0 * p.lda + k0 * 2);
         a_left = (int)(p.inner - k0);
         a_until = (to < (part + 1) * per_part ? to - part * per_part : per_part) - stage;
     };
     const auto begin_b = [&](int part, int stage) {
         const int64_t k0 = (int64_t)stage * STEPS;
-        b_from = descriptor(B_ACROSS ? p.b[part] + k0 * p.ldb + col0 * 2 : p.b[b_part] + b_row0 * p.ldb + k0 * 2);
+        b_from = descriptor(B_ACROSS ? (part ? p.b[1] : p.b[0]) + k0 * p.ldb + col0 * 2 : (b_part ? p.b[1] : p.b[0]) + b_row0 * p.ldb + k0 * 2);
         b_left = (int)(p.inner_b - k0);
         b_until = (to < (part + 1) * per_part ? to - part * per_part : per_part) - stage;
     };
@@ -366,6 +366,18 @@ __global__ __launch_bounds__(64 * WAVES_M * WAVES_N) void k_product(Product p) {
     }
 #pragma unroll
     for (int i = 0; i < TM; ++i) finish<DT, MODE, ACT>(p, at, row0 + (wm * TM + i) * 16 + of16, wn, acc[i]);
+}
+
+template <int DT, int MODE, int ACT, int BM, int BN, int WAVES_M, int WAVES_N>
+__global__ __launch_bounds__(64 * WAVES_M * WAVES_N) void k_product(Product p) {
+    product<DT, MODE, ACT, BM, BN, WAVES_M, WAVES_N>(p, blockIdx.x, gridDim.x);
+}
+
+// Both products of the backward pass in one launch: neither fills the chip on its own, or not to the end.
+template <int DT, int BM, int BN, int WAVES_M, int WAVES_N>
+__global__ __launch_bounds__(64 * WAVES_M * WAVES_N) void k_products(Product dx, Product dw, unsigned of_dx) {
+    if (blockIdx.x < of_dx) product<DT, INPUT_GRAD, PARO_SILU, BM, BN, WAVES_M, WAVES_N>(dx, blockIdx.x, of_dx);
+    else product<DT, WEIGHT_GRAD, PARO_SILU, BM, BN, WAVES_M, WAVES_N>(dw, blockIdx.x - of_dx, gridDim.x - of_dx);
 }
 
 // Adds up the sums of a split tile's blocks, in order: a block for each row of a wave's tiles.
@@ -704,6 +716,7 @@ bool fills_take(int64_t ld, int64_t cols) { return ld % 8 == 0 && cols % 8 == 0;
 struct Shape {                           // of a product's launch
     bool large;                          // tiles of 256 x 256, else 128 x 128
     int64_t tiles_m, tiles_n, whole, splits;
+    double cost;
     int64_t blocks() const { return whole + (tiles_m * tiles_n - whole) * splits; }
     int64_t partial_bytes() const { return splits > 1 ? (tiles_m * tiles_n - whole) * splits * (large ? 256 * 256 : 128 * 128) * 4 : 0; }
 };
@@ -716,49 +729,108 @@ struct Shape {                           // of a product's launch
 Shape shape_of(int mode, int64_t rows, int64_t cols, int64_t inner) {
     const int64_t stages = ceil_div(inner, STEPS) * (mode == INPUT_GRAD ? 2 : 1);
     Shape best{};
-    double least = -1.0;
+    best.cost = -1.0;
     for (const bool large : {true, false}) {
         const int64_t side = large ? 256 : 128, at_once = large ? COMPUTE_UNITS : 2 * COMPUTE_UNITS;
-        Shape s{large, ceil_div(rows, side) * (mode == WEIGHT_GRAD ? 2 : 1), ceil_div(cols, mode == FORWARD ? side / 2 : side), 0, 1};
+        Shape s{large, ceil_div(rows, side) * (mode == WEIGHT_GRAD ? 2 : 1), ceil_div(cols, mode == FORWARD ? side / 2 : side), 0, 1, 0.0};
         const int64_t tiles = s.tiles_m * s.tiles_n, rest = tiles % at_once;
         const double filled = (double)rows / (double)(ceil_div(rows, side) * side), stage = large ? 1.55 : 1.2;
         for (int64_t splits = 1; splits == 1 || (rest && rest * splits <= at_once && splits <= 32 && stages / splits >= 8); ++splits) {
             s.splits = splits;
             s.whole = splits == 1 ? tiles : tiles - rest;
             const int64_t in_turn = splits == 1 ? ceil_div(tiles, at_once) * stages : tiles / at_once * stages + ceil_div(stages, splits);
-            const double cost = (double)in_turn * stage + (splits == 1 ? 0.0 : 5.0 + (double)s.partial_bytes() * filled / 2.5e6);
-            if (least < 0.0 || cost < least) {
+            s.cost = (double)in_turn * stage + (splits == 1 ? 0.0 : 5.0 + (double)s.partial_bytes() * filled / 2.5e6);
+            if (best.cost < 0.0 || s.cost < best.cost) best = s;
+        }
+    }
+    return best;
+}
+
+// The backward pass's two products: each for itself, or both in one launch of small tiles, all tiles of a product in equal shares.  Then the blocks take
+// what all stages take on a full chip and half a short block's more, or the longest block's; by themselves there is a launch more, 5 us.  Kernel times of the
+// whole pass (bf16), by themselves | together: 100 tokens of 768 x 2048 25 | 20, 474 of 384 x 896 30 | 20, 500 of 1024 x 2816 43 | 34, 1000 of 2048 x 2048
+// 62 | 54, 128 of 4096 x 4096 64 | 55, 4000 of 512 x 1024 60 | 46; but 600 of 4096 x 11008 281 | 345, 3740 of 640 x 5504 188 | 193.
+struct Shapes {
+    Shape dx, dw;
+    bool together;
+    int64_t dw_partial() const { return together ? up_to(dx.partial_bytes(), 256) : 0; }
+    int64_t partial_bytes() const { return std::max(dx.partial_bytes(), dw_partial() + dw.partial_bytes()); }
+};
+Shapes shapes_of(int64_t n, int64_t dim, int64_t hidden) {
+    Shapes best{shape_of(INPUT_GRAD, n, dim, hidden), shape_of(WEIGHT_GRAD, hidden, dim, n), false};
+    double least = best.dx.cost + best.dw.cost + 5.0;
+    const auto small = [](int64_t tiles_m, int64_t tiles_n, int64_t splits) {
+        return Shape{false, tiles_m, tiles_n, splits == 1 ? tiles_m * tiles_n : 0, splits, 0.0};
+    };
+    const int64_t of_dx = ceil_div(hidden, STEPS) * 2, of_dw = ceil_div(n, STEPS), side_m = ceil_div(n, 128), side_h = ceil_div(hidden, 128) * 2,
+                  side_d = ceil_div(dim, 128);
+    const double filled = (double)n / (double)(side_m * 128);
+    const double all = (double)(side_m * side_d * of_dx + side_h * side_d * of_dw) / (2 * COMPUTE_UNITS);
+    for (const int64_t dw_splits : {1, 2, 4, 8, 16}) {
+        if (dw_splits > 1 && of_dw / dw_splits < 8) break;
+        const Shape dw = small(side_h, side_d, dw_splits);
+        for (const int64_t dx_splits : {1, 2, 3, 4, 6, 8, 11, 16, 23, 32}) {
+            if (dx_splits > 1 && of_dx / dx_splits < 8) break;
+            const Shape dx = small(side_m, side_d, dx_splits);
+            const int64_t a = ceil_div(of_dx, dx_splits), b = ceil_div(of_dw, dw_splits);
+            const double cost = 1.2 * std::max((double)std::max(a, b), all + 0.5 * (double)std::min(a, b)) + (dx_splits > 1 ? 5.0 : 0.0) +
+                                (dw_splits > 1 ? 5.0 : 0.0) + ((double)dx.partial_bytes() * filled + (double)dw.partial_bytes()) / 2.5e6;
+            if (cost < least) {
                 least = cost;
-                best = s;
+                best = Shapes{dx, dw, true};
             }
         }
     }
     return best;
 }
 
-template <int DT, int MODE, int ACT, int BM, int BN, int WAVES_M, int WAVES_N>
-int launch_tiles(const Product &p, const Shape &s, hipStream_t st) {
-    constexpr unsigned LDS_BYTES = 5 * BM * ROW_BYTES, THREADS_ = 64 * WAVES_M * WAVES_N;
-    const auto kernel = k_product<DT, MODE, ACT, BM, BN, WAVES_M, WAVES_N>;
-    if (LDS_BYTES > 65536) {
-        const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void *>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, (int)LDS_BYTES);
-        if (e != hipSuccess) return fail(PARO_EHIP, std::string("shared memory: ") + hipGetErrorString(e));
-    }
-    hipLaunchKernelGGL(kernel, dim3((unsigned)s.blocks()), dim3(THREADS_), LDS_BYTES, st, p);
-    if (s.splits > 1)
-        hipLaunchKernelGGL((k_join<DT, MODE, ACT, BM, BN, WAVES_M, WAVES_N>), dim3((unsigned)(s.tiles_m * s.tiles_n - s.whole), BM / WAVES_M / 16),
-                           dim3(THREADS_), 0, st, p);
-    return PARO_OK;
+template <class Kernel>
+int room_for(Kernel kernel, unsigned lds_bytes) {
+    if (lds_bytes <= 65536) return PARO_OK;
+    const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void *>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds_bytes);
+    return e == hipSuccess ? PARO_OK : fail(PARO_EHIP, std::string("shared memory: ") + hipGetErrorString(e));
 }
-
-template <int DT, int MODE, int ACT>
-int launch_product(Product p, const Shape &s, float *partial, hipStream_t st) {
+void place(Product &p, const Shape &s, float *partial) {
     p.tiles_m = (int)s.tiles_m;
     p.tiles_n = (int)s.tiles_n;
     p.whole = (unsigned)s.whole;
     p.splits = (unsigned)s.splits;
     p.partial = partial;
+}
+template <int DT, int MODE, int ACT, int BM, int BN, int WAVES_M, int WAVES_N>
+void launch_join(const Product &p, const Shape &s, hipStream_t st) {
+    if (s.splits > 1)
+        hipLaunchKernelGGL((k_join<DT, MODE, ACT, BM, BN, WAVES_M, WAVES_N>), dim3((unsigned)(s.tiles_m * s.tiles_n - s.whole), BM / WAVES_M / 16),
+                           dim3(64 * WAVES_M * WAVES_N), 0, st, p);
+}
+
+template <int DT, int MODE, int ACT, int BM, int BN, int WAVES_M, int WAVES_N>
+int launch_tiles(const Product &p, const Shape &s, hipStream_t st) {
+    constexpr unsigned LDS_BYTES = 5 * BM * ROW_BYTES;
+    const auto kernel = k_product<DT, MODE, ACT, BM, BN, WAVES_M, WAVES_N>;
+    if (const int rc = room_for(kernel, LDS_BYTES)) return rc;
+    hipLaunchKernelGGL(kernel, dim3((unsigned)s.blocks()), dim3(64 * WAVES_M * WAVES_N), LDS_BYTES, st, p);
+    launch_join<DT, MODE, ACT, BM, BN, WAVES_M, WAVES_N>(p, s, st);
+    return PARO_OK;
+}
+
+template <int DT, int MODE, int ACT>
+int launch_product(Product p, const Shape &s, float *partial, hipStream_t st) {
+    place(p, s, partial);
     return s.large ? launch_tiles<DT, MODE, ACT, 256, 256, 2, 4>(p, s, st) : launch_tiles<DT, MODE, ACT, 128, 128, 2, 2>(p, s, st);
+}
+
+template <int DT>
+int launch_products(Product dx, Product dw, const Shapes &s, float *partial, hipStream_t st) {
+    constexpr unsigned LDS_BYTES = 5 * 128 * ROW_BYTES;
+    place(dx, s.dx, partial);
+    place(dw, s.dw, partial + s.dw_partial() / 4);
+    const auto kernel = k_products<DT, 128, 128, 2, 2>;
+    if (const int rc = room_for(kernel, LDS_BYTES)) return rc;
+    hipLaunchKernelGGL(kernel, dim3((unsigned)(s.dx.blocks() + s.dw.blocks())), dim3(64 * 2 * 2), LDS_BYTES, st, dx, dw, (unsigned)s.dx.blocks());
+    launch_join<DT, INPUT_GRAD, PARO_SILU, 128, 128, 2, 2>(dx, s.dx, st);
+    launch_join<DT, WEIGHT_GRAD, PARO_SILU, 128, 128, 2, 2>(dw, s.dw, st);
+    return PARO_OK;
 }
 
 struct Room {                            // parts of the workspace, in bytes
@@ -796,7 +868,7 @@ Room room_of(const paro_gated_t &d, bool grad) {
     int64_t partial = 0;
     if (grad) {
         r.slopes = take(2 * up_to(d.hidden, 64) * d.n * 2);
-        partial = std::max(shape_of(INPUT_GRAD, d.n, d.dim, d.hidden).partial_bytes(), shape_of(WEIGHT_GRAD, d.hidden, d.dim, d.n).partial_bytes());
+        partial = shapes_of(d.n, d.dim, d.hidden).partial_bytes();
     } else {
         partial = shape_of(FORWARD, d.n, d.hidden, d.dim).partial_bytes();
     }
@@ -954,17 +1026,19 @@ int backward(const paro_gated_t &d, const void *dh, const void *gate, const void
     p.inner_b = d.hidden;
     p.out[0] = static_cast<char *>(dx);
     p.ldo = ld_x(d);
-    int rc = launch_product<DT, INPUT_GRAD, PARO_SILU>(p, shape_of(INPUT_GRAD, d.n, d.dim, d.hidden), partial, st);
-    if (rc) return rc;
-    p.b[0] = in.x;
-    p.b[1] = nullptr;
-    p.ldb = in.ldx * 2;
-    p.rows = d.hidden;
-    p.inner = p.inner_b = d.n;
-    p.out[0] = static_cast<char *>(dwg);
-    p.out[1] = static_cast<char *>(dwu);
-    p.ldo = d.dim;
-    return launch_product<DT, WEIGHT_GRAD, PARO_SILU>(p, shape_of(WEIGHT_GRAD, d.hidden, d.dim, d.n), partial, st);
+    Product q = p;
+    q.b[0] = in.x;
+    q.b[1] = nullptr;
+    q.ldb = in.ldx * 2;
+    q.rows = d.hidden;
+    q.inner = q.inner_b = d.n;
+    q.out[0] = static_cast<char *>(dwg);
+    q.out[1] = static_cast<char *>(dwu);
+    q.ldo = d.dim;
+    const Shapes s = shapes_of(d.n, d.dim, d.hidden);
+    if (s.together) return launch_products<DT>(p, q, s, partial, st);
+    const int rc = launch_product<DT, INPUT_GRAD, PARO_SILU>(p, s.dx, partial, st);
+    return rc ? rc : launch_product<DT, WEIGHT_GRAD, PARO_SILU>(q, s.dw, partial, st);
 }
 
 #define PARO_BY_TYPE(CALL)                                            \

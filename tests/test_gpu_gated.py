@@ -254,3 +254,10 @@ def test_in_a_graph_and_on_another_stream(paro):
         both(ref)
         torch.cuda.synchronize()
         assert all(torch.equal(a, b) for a, b in zip(ref, got))
+
+
+@pytest.mark.parametrize("n,dim,hidden,dtype,act,pad", [(474, 384, 896, "bf16", "silu", 8), (1000, 768, 2999, "bf16", "gelu", 0), (4544, 640, 640, "bf16", "silu", 0),
+                                                        (321, 81, 865, "f16", "gelu", 3), (1861, 2176, 128, "bf16", "silu", 0), (293, 121, 5000, "f16", "silu", 0),
+                                                        (4000, 512, 1024, "f16", "gelu", 0), (129, 130, 131, "bf16", "silu", 0)])
+def test_backward_of_middling_sizes(paro, n, dim, hidden, dtype, act, pad):
+    backward(paro, n, dim, hidden, dtype, act, pad=pad)
