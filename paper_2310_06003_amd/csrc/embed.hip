@@ -252,41 +252,45 @@ struct RowPiece {
     }
 };
 
-// acc += dout[order[a .. b)], in order, for the lane's pieces of a tile of columns.  The places of 64 tokens are loaded at once, one a lane
-// (each by a scalar load that its row waits for: GPT-2's table 64 us, so 47; 32768 tokens of 4096 155 and 138).
+// acc += dout's rows in the first `all` lanes of `mine`, in order, for the lane's pieces of a tile of columns.
+template <int DT, int GT, int C>
+__device__ __forceinline__ void add_listed(float (&acc)[C][Elem<GT>::E], const void *dout, int64_t ld, int mine, int all, const int64_t (&col)[C], int64_t dim) {
+    constexpr int U = 16 / C;                       // rows in flight; for four pieces 2: 52 and 149 us, 6: 46 and 145
+    const auto add = [&](int k, auto count_) {
+        constexpr int count = count_;
+        RowPiece<DT, GT> piece[count][C];
+#pragma unroll
+        for (int u = 0; u < count; ++u) {
+            const int64_t row = (int64_t)__builtin_amdgcn_readlane(mine, k + u) * ld;
+#pragma unroll
+            for (int c = 0; c < C; ++c)
+                if (col[c] < dim) piece[u][c].load(dout, row + col[c]);
+        }
+#pragma unroll
+        for (int u = 0; u < count; ++u)
+#pragma unroll
+            for (int c = 0; c < C; ++c)
+                if (col[c] < dim) piece[u][c].add_to(acc[c]);
+    };
+    int k = 0;
+    for (; k + U <= all; k += U) add(k, std::integral_constant<int, U>{});
+    static_for<1, 5>([&](auto i) {                  // the rest in halves; row by row 30000 tokens of 128 43 us, so 38
+        constexpr int fewer = U >> i;
+        if constexpr (fewer > 0)
+            if (k + fewer <= all) {
+                add(k, std::integral_constant<int, fewer>{});
+                k += fewer;
+            }
+    });
+}
+
+// acc += dout[order[a .. b)], in order.  The places of 64 tokens are loaded at once, one a lane (each by a scalar load that its row waits for:
+// GPT-2's table 64 us, so 47; 32768 tokens of 4096 155 and 138).
 template <int DT, int GT, int C>
 __device__ __forceinline__ void add_rows(float (&acc)[C][Elem<GT>::E], const void *dout, int64_t ld, const int *order, int a, int b,
                                          const int64_t (&col)[C], int64_t dim) {
-    constexpr int U = 16 / C;                       // rows in flight; for four pieces 2: 52 and 149 us, 6: 46 and 145
-    for (int k0 = a; k0 < b; k0 += 64) {
-        const int mine = k0 + lane_of() < b ? order[k0 + lane_of()] : 0, all = b - k0 < 64 ? b - k0 : 64;
-        const auto add = [&](int k, auto count_) {
-            constexpr int count = count_;
-            RowPiece<DT, GT> piece[count][C];
-#pragma unroll
-            for (int u = 0; u < count; ++u) {
-                const int64_t row = (int64_t)__builtin_amdgcn_readlane(mine, k + u) * ld;
-#pragma unroll
-                for (int c = 0; c < C; ++c)
-                    if (col[c] < dim) piece[u][c].load(dout, row + col[c]);
-            }
-#pragma unroll
-            for (int u = 0; u < count; ++u)
-#pragma unroll
-                for (int c = 0; c < C; ++c)
-                    if (col[c] < dim) piece[u][c].add_to(acc[c]);
-        };
-        int k = 0;
-        for (; k + U <= all; k += U) add(k, std::integral_constant<int, U>{});
-        static_for<1, 5>([&](auto i) {              // the rest in halves; row by row 30000 tokens of 128 43 us, so 38
-            constexpr int fewer = U >> i;
-            if constexpr (fewer > 0)
-                if (k + fewer <= all) {
-                    add(k, std::integral_constant<int, fewer>{});
-                    k += fewer;
-                }
-        });
-    }
+    for (int k0 = a; k0 < b; k0 += 64)
+        add_listed<DT, GT>(acc, dout, ld, k0 + lane_of() < b ? order[k0 + lane_of()] : 0, b - k0 < 64 ? b - k0 : 64, col, dim);
 }
 
 // Columns of a lane's pieces; the last piece of a row starts early, past the row: dim.
@@ -310,43 +314,61 @@ __device__ __forceinline__ void store_row(float (&acc)[C][Elem<GT>::E], void *gr
     }
 }
 
+// A lane's pieces of a span of the gradient as it lies in memory, `step` elements apart.
+template <int C>
+struct SpanPieces {
+    int64_t elem[C], row[C], left[C];               // first element, its row, what that row has from it on
+    unsigned empty[C];                              // bit 0: the row has no token, bit 1: the next one has none
+    __device__ __forceinline__ void place(int64_t from, int step, int piece, int64_t row0, int64_t dim) {
+#pragma unroll
+        for (int c = 0; c < C; ++c) {
+            elem[c] = from + c * step + lane_of() * piece;
+            const int64_t at = elem[c] > 0 ? elem[c] : 0;
+            row[c] = row0 + (unsigned)(at - row0 * dim) / (unsigned)dim;
+            left[c] = (row[c] + 1) * dim - elem[c];
+        }
+    }
+    // Zeros where the row is empty.  A piece that a row with tokens shares goes element by element.
+    template <int GT>
+    __device__ __forceinline__ void store(void *grad, int64_t all) const {
+        constexpr int E = Elem<GT>::E;
+#pragma unroll
+        for (int c = 0; c < C; ++c) {
+            if (elem[c] >= 0 && elem[c] + E <= all && (empty[c] & 1) && (left[c] >= E || (empty[c] & 2))) {
+                store_stream<GT>(grad, elem[c], u32x4{0, 0, 0, 0});
+            } else {
+#pragma unroll
+                for (int j = 0; j < E; ++j)
+                    if (elem[c] + j >= 0 && elem[c] + j < all && (empty[c] & (j < left[c] ? 1 : 2))) store_one<GT>(grad, elem[c] + j, 0.0f);
+            }
+        }
+    }
+};
+template <int GT, int C>
+__device__ __forceinline__ void store_zeros(void *grad, int64_t from) {
+#pragma unroll
+    for (int c = 0; c < C; ++c) store_stream<GT>(grad, from + (c * 64 + lane_of()) * Elem<GT>::E, u32x4{0, 0, 0, 0});
+}
+
 // Zeros for the rows without a token, in a span of the gradient as it lies in memory: aligned pieces, whatever the rows' width, and all lanes
-// have some, however narrow the rows are (a wave for each row: 35224 rows of 7443 fp32 elements 277 us, so 188; 87603 of 128 24 and 15).  A
-// piece that a row with tokens shares goes element by element.
+// have some, however narrow the rows are (a wave for each row: 35224 rows of 7443 fp32 elements 277 us, so 188; 87603 of 128 24 and 15). 
 template <int GT, int C>
 __device__ __forceinline__ void zeros_of_span(void *grad, const int *start, int64_t from, int64_t rows, int64_t dim) {
     constexpr int E = Elem<GT>::E;
     const int64_t row0 = (from > 0 ? from : 0) / dim, all = rows * dim;
     if (from + 64 * C * E <= (row0 + 1) * dim) {    // of one row: nothing to find out by lane (32768 tokens of 4096 145 us without, 133)
         if (start[row0] != start[row0 + 1]) return;
-        if (from >= 0) {
-#pragma unroll
-            for (int c = 0; c < C; ++c) store_stream<GT>(grad, from + c * 64 * E + lane_of() * E, u32x4{0, 0, 0, 0});
-            return;
-        }
+        if (from >= 0) return store_zeros<GT, C>(grad, from);
     }
-    unsigned empty[C];                              // bit 0: the row of the piece's first element has no token, bit 1: the next one
-    int64_t elem[C], left[C];
+    SpanPieces<C> at;
+    at.place(from, 64 * E, E, row0, dim);
 #pragma unroll
     for (int c = 0; c < C; ++c) {
-        elem[c] = from + c * 64 * E + lane_of() * E;
-        const int64_t at = elem[c] > 0 ? elem[c] : 0;
-        const int64_t v = row0 + (unsigned)(at - row0 * dim) / (unsigned)dim;
-        left[c] = (v + 1) * dim - elem[c];
-        const int64_t v0 = v < rows ? v : rows, v1 = v + 1 < rows ? v + 1 : rows, v2 = v + 2 < rows ? v + 2 : rows;
+        const int64_t v = at.row[c], v0 = v < rows ? v : rows, v1 = v + 1 < rows ? v + 1 : rows, v2 = v + 2 < rows ? v + 2 : rows;
         const int s0 = start[v0], s1 = start[v1], s2 = start[v2];
-        empty[c] = (s0 == s1 ? 1 : 0) | (s1 == s2 ? 2 : 0);
+        at.empty[c] = (s0 == s1 ? 1 : 0) | (s1 == s2 ? 2 : 0);
     }
-#pragma unroll
-    for (int c = 0; c < C; ++c) {
-        if (elem[c] >= 0 && elem[c] + E <= all && (empty[c] & 1) && (left[c] >= E || (empty[c] & 2))) {
-            store_stream<GT>(grad, elem[c], u32x4{0, 0, 0, 0});
-        } else {
-#pragma unroll
-            for (int j = 0; j < E; ++j)
-                if (elem[c] + j >= 0 && elem[c] + j < all && (empty[c] & (j < left[c] ? 1 : 2))) store_one<GT>(grad, elem[c] + j, 0.0f);
-        }
-    }
+    at.template store<GT>(grad, all);
 }
 
 // Three kinds of blocks, in the order in which they start: what reads goes before what only writes, since a read that waits behind a stream of
@@ -432,6 +454,54 @@ __global__ __launch_bounds__(THREADS) void k_join(const int *start, const int *r
         for (int q = 0; q < 4; ++q) store_one<GT>(grad, v * dim + col[0] + q, acc[q]);
 }
 
+// Up to 64 tokens: each wave has all of them, one a lane, and needs neither the sort nor its launch.  A wave takes a token, and sums its row if it is the row's
+// first; the others write zeros as above.  With the sort: 64 tokens of 3200, 2828 rows 16 us, so 9.6; 64 of 64, 100000 rows 13 and 8.7; 60 of 4096,
+// 32000 rows 52 and 46.
+constexpr int FEW_TOKENS = 64;
+template <int DT, int GT, int C>
+__global__ __launch_bounds__(THREADS) void k_few_tokens(const void *dout, int64_t ld, const void *tokens, bool wide, int n, int64_t first, int64_t rows, int64_t dim,
+                                                        unsigned token_blocks, float scale, void *grad) {
+    constexpr int E = Elem<GT>::E, SPAN = 64 * C * E;
+    const int lane = lane_of();
+    int mine = -1;                                  // the row of the lane's token
+    if (lane < n) mine = (int)(wide ? row_of(static_cast<const int64_t *>(tokens), lane, first, rows) : row_of(static_cast<const int32_t *>(tokens), lane, first, rows));
+    if (blockIdx.x < token_blocks) {
+        const int i = blockIdx.x * WAVES + wave_of();
+        if (i >= n) return;
+        const int v = __builtin_amdgcn_readlane(mine, i);
+        const uint64_t same = __ballot(mine == v), before = ((uint64_t)1 << lane) - 1;
+        if (v < 0 || __builtin_ctzll(same) != i) return;
+        const int to = same >> lane & 1 ? __popcll(same & before) : __popcll(same) + __popcll(~same & before);
+        int64_t col[C];
+        columns<E>(col, dim);
+        float acc[C][E] = {};
+        add_listed<DT, GT>(acc, dout, ld, __builtin_amdgcn_ds_permute(to * 4, lane), __popcll(same), col, dim);
+        store_row<GT>(acc, grad, v, col, dim, scale);
+        return;
+    }
+    const unsigned blocks = gridDim.x - token_blocks;
+    const int64_t lead = (reinterpret_cast<uintptr_t>(grad) & 127) / Elem<GT>::BYTES, all = rows * dim;
+    for (int64_t s = ((int64_t)blockIdx.y * blocks + (blockIdx.x - token_blocks)) * WAVES + wave_of(); s * SPAN - lead < all; s += (int64_t)blocks * gridDim.y * WAVES) {
+        const int64_t from = s * SPAN - lead, row0 = (from > 0 ? from : 0) / dim;
+        const int64_t past = row0 + (unsigned)(from + SPAN - row0 * dim) / (unsigned)dim;       // no element of the span is of a later row
+        uint64_t inside = __ballot(mine >= row0 && mine <= past);
+        if (!inside && from >= 0 && from + SPAN <= all) {
+            store_zeros<GT, C>(grad, from);
+            continue;
+        }
+        SpanPieces<C> at;
+        at.place(from, 64 * E, E, row0, dim);
+#pragma unroll
+        for (int c = 0; c < C; ++c) at.empty[c] = 3;
+        for (; inside; inside &= inside - 1) {
+            const int v = __builtin_amdgcn_readlane(mine, __builtin_ctzll(inside));
+#pragma unroll
+            for (int c = 0; c < C; ++c) at.empty[c] &= ~((v == at.row[c] ? 1 : 0) | (v == at.row[c] + 1 ? 2 : 0));
+        }
+        at.template store<GT>(grad, all);
+    }
+}
+
 // Rows narrower than a piece: a thread for each element.
 template <int DT, int GT>
 __global__ __launch_bounds__(THREADS) void k_narrow_sums(const void *dout, int64_t ld, const int *start, const int *order, int64_t rows,
@@ -505,6 +575,22 @@ void launch_embed(const void *table, const void *tokens, int64_t n, int64_t firs
                        static_cast<const Token *>(tokens), n, first, rows, dim, scale, out, ld);
 }
 
+// Blocks that write the zeros, of `tiles` rows of blocks.
+template <int GT>
+unsigned zero_blocks(int64_t rows, int64_t dim, int64_t tiles) {
+    const int64_t spans = rows * dim / (64 * GRAD_PIECES * Elem<GT>::E) + 2;
+    return (unsigned)std::max<int64_t>(1, std::min(MAX_BLOCKS / 2 / tiles, ceil_div(spans, tiles * WAVES)));
+}
+
+template <int DT, int GT>
+void launch_few(const void *dout, int64_t ld, const void *tokens, int token_dtype, int64_t n, int64_t first, float scale, void *grad, int64_t rows,
+                int64_t dim, hipStream_t st) {
+    const int64_t tiles = ceil_div(dim, 64 * GRAD_PIECES * Elem<GT>::E);
+    const unsigned token_blocks = (unsigned)ceil_div(n, WAVES);
+    hipLaunchKernelGGL((k_few_tokens<DT, GT, GRAD_PIECES>), dim3(token_blocks + zero_blocks<GT>(rows, dim, tiles), (unsigned)tiles), dim3(THREADS), 0, st, dout, ld,
+                       tokens, token_dtype == PARO_I64, (int)n, first, rows, dim, token_blocks, scale, grad);
+}
+
 template <int DT, int GT, int C>
 void launch_sums(const void *dout, int64_t ld, int64_t n, float scale, void *grad, int64_t rows, int64_t dim, char *ws, const GradRoom &g,
                  hipStream_t st) {
@@ -519,9 +605,7 @@ void launch_sums(const void *dout, int64_t ld, int64_t n, float scale, void *gra
     const unsigned seg_blocks = n > seg ? (unsigned)ceil_div(ceil_div(n, seg), WAVES) : 0;
     const int64_t tiles = ceil_div(dim, 64 * C * Elem<GT>::E);
     const unsigned run_blocks = n ? grid_for(n, 2 * tiles).x : 0;
-    const int64_t spans = rows * dim / (64 * GRAD_PIECES * Elem<GT>::E) + 2;
-    const unsigned zero_blocks = (unsigned)std::max<int64_t>(1, std::min(MAX_BLOCKS / 2 / tiles, ceil_div(spans, tiles * WAVES)));
-    hipLaunchKernelGGL((k_sums<DT, GT, C>), dim3(seg_blocks + run_blocks + zero_blocks, (unsigned)tiles), dim3(THREADS), 0, st, dout,
+    hipLaunchKernelGGL((k_sums<DT, GT, C>), dim3(seg_blocks + run_blocks + zero_blocks<GT>(rows, dim, tiles), (unsigned)tiles), dim3(THREADS), 0, st, dout,
                        ld, start, order, row_at, rows, dim, seg, seg_blocks, run_blocks, scale, partial, grad);
     if (seg_blocks)
         hipLaunchKernelGGL((k_join<GT>), dim3(seg_blocks, (unsigned)ceil_div(dim, 64 * 4)), dim3(THREADS), 0, st, start, row_at, rows, dim, seg,
@@ -588,6 +672,17 @@ int paro_embed_grad(const void *dout, int dtype, int64_t ld_dout, const void *to
         const GradRoom g = grad_room(n, rows, dim);
         if (workspace_bytes < g.all) return fail(PARO_ERANGE, f + "the workspace is smaller than paro_embed_grad_workspace says");
         hipStream_t st = static_cast<hipStream_t>(stream);
+        if (n <= FEW_TOKENS && dim * size_of(dtype) >= 16) {
+#define PARO_FEW(DT, GT) launch_few<DT, GT>(dout, ld_dout, tokens, token_dtype, n, first_token, scale, grad, rows, dim, st)
+            if (dtype == PARO_F32) PARO_FEW(PARO_F32, PARO_F32);
+            else if (dtype == PARO_F16 && grad_dtype == PARO_F16) PARO_FEW(PARO_F16, PARO_F16);
+            else if (dtype == PARO_F16) PARO_FEW(PARO_F16, PARO_F32);
+            else if (grad_dtype == PARO_BF16) PARO_FEW(PARO_BF16, PARO_BF16);
+            else PARO_FEW(PARO_BF16, PARO_F32);
+#undef PARO_FEW
+            PARO_LAUNCHED("paro_embed_grad");
+            return PARO_OK;
+        }
         char *ws = static_cast<char *>(workspace);
         int *start = reinterpret_cast<int *>(ws + g.start), *order = reinterpret_cast<int *>(ws + g.order);
         int *row_at = reinterpret_cast<int *>(ws + g.row_at);

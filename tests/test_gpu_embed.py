@@ -185,3 +185,11 @@ def test_rows_without_a_token_are_zeros_wherever_the_table_lies(paro, v, dim, of
         assert bool((grad[ref.to(DEV).abs().sum(dim=1) == 0] == 0).all()), "a row without a token is not zeros"
         grad.fill_(9.0)
         assert bool((whole == 9.0).all()), "wrote beside the gradient"
+
+
+@pytest.mark.parametrize("token", [torch.int32, torch.int64])
+@pytest.mark.parametrize("dtype,grad_dtype", [("bf16", "f32"), ("f16", "f16"), ("f32", "f32")])
+@pytest.mark.parametrize("n,dim,v", [(1, 5000, 3), (7, 8, 1000), (32, 100, 31), (33, 2049, 9), (63, 4100, 40), (64, 64, 3000), (64, 1030, 1), (65, 1030, 1)])
+def test_gradient_of_few_tokens(paro, n, dim, v, dtype, grad_dtype, token):
+    tokens = torch.randint(-2, v + 2, (n,), generator=rng(n * dim)).to(token)
+    gradient(paro, tokens + 11, dim, v, dtype, grad_dtype, first=11, pad=n % 3)
