@@ -591,6 +591,14 @@ void launch_few(const void *dout, int64_t ld, const void *tokens, int token_dtyp
                        tokens, token_dtype == PARO_I64, (int)n, first, rows, dim, token_blocks, scale, grad);
 }
 
+// Whether the tokens' waves, of GRAD_PIECES a lane, would be too few to keep the memory busy: up to six a SIMD.  Then one piece a lane and more waves
+// (four | one: 2000 tokens of 2048, 2000 rows 29 us | 20, 803 of 6519 33 | 26, 5157 of 896 in fp32 31 | 27; but 8191 of 768 to fp32 45 | 47, 20000 of
+// 2048 49 | 59).
+template <int GT>
+bool few_waves(int64_t n, int64_t dim) {
+    return n * ceil_div(dim, 64 * GRAD_PIECES * Elem<GT>::E) <= 6 * 4 * COMPUTE_UNITS;
+}
+
 template <int DT, int GT, int C>
 void launch_sums(const void *dout, int64_t ld, int64_t n, float scale, void *grad, int64_t rows, int64_t dim, char *ws, const GradRoom &g,
                  hipStream_t st) {
@@ -702,9 +710,9 @@ int paro_embed_grad(const void *dout, int dtype, int64_t ld_dout, const void *to
 #undef PARO_SORT
         PARO_LAUNCHED("paro_embed_grad");
 #define PARO_SUMS(DT, GT)                                                                                                              \
-    (dim <= 64 * Elem<GT>::E    ? launch_sums<DT, GT, 1>                                                                               \
-     : dim <= 128 * Elem<GT>::E ? launch_sums<DT, GT, 2>                                                                               \
-                                : launch_sums<DT, GT, GRAD_PIECES>)(dout, ld_dout, n, scale, grad, rows, dim, ws, g, st)
+    (dim <= 64 * Elem<GT>::E || few_waves<GT>(n, dim) ? launch_sums<DT, GT, 1>                                                         \
+     : dim <= 128 * Elem<GT>::E                       ? launch_sums<DT, GT, 2>                                                         \
+                                                      : launch_sums<DT, GT, GRAD_PIECES>)(dout, ld_dout, n, scale, grad, rows, dim, ws, g, st)
         if (dtype == PARO_F32) PARO_SUMS(PARO_F32, PARO_F32);
         else if (dtype == PARO_F16 && grad_dtype == PARO_F16) PARO_SUMS(PARO_F16, PARO_F16);
         else if (dtype == PARO_F16) PARO_SUMS(PARO_F16, PARO_F32);
