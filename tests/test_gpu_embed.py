@@ -193,3 +193,22 @@ def test_rows_without_a_token_are_zeros_wherever_the_table_lies(paro, v, dim, of
 def test_gradient_of_few_tokens(paro, n, dim, v, dtype, grad_dtype, token):
     tokens = torch.randint(-2, v + 2, (n,), generator=rng(n * dim)).to(token)
     gradient(paro, tokens + 11, dim, v, dtype, grad_dtype, first=11, pad=n % 3)
+
+
+def test_as_many_tokens_as_the_call_takes(paro):
+    """2^31 - 1 tokens: places among them, and 64 or a segment of 2^20 beyond, count in more than 32 bits.  One row's run ends in the last
+    segment, the other's is the last 100 tokens; small whole numbers here and there make the sums exact."""
+    n, dim, v = 2 ** 31 - 1, 8, 3
+    tokens = torch.zeros(n, dtype=torch.int32, device=DEV)
+    tokens[-100:] = 2
+    dout = torch.zeros(n, dim, dtype=torch.bfloat16, device=DEV)
+    ref = torch.zeros(v, dim)
+    seg = 2 ** 20
+    for i in (0, 5, seg - 1, seg, 700 * seg + 3, 2047 * seg - 1, 2047 * seg, 2047 * seg + 77, n - 101, n - 100, n - 64, n - 63, n - 37, n - 36, n - 1):
+        dout[i, i % dim] = 1 + i % 5
+        ref[2 if i >= n - 100 else 0, i % dim] += 1 + i % 5
+    grad = torch.full((v, dim), 7.0, device=DEV)
+    ws = workspace(paro.paro_embed_grad_workspace(n, v, dim))
+    paro.paro_embed_grad(dout.data_ptr(), paro.PARO_BF16, 0, tokens.data_ptr(), paro.PARO_I32, n, 0, 1.0, grad.data_ptr(), paro.PARO_F32, v, dim,
+                         ws.data_ptr(), ws.numel(), stream())
+    assert torch.equal(grad.cpu(), ref)
