@@ -287,10 +287,11 @@ __device__ __forceinline__ void add_listed(float (&acc)[C][Elem<GT>::E], const v
 // acc += dout[order[a .. b)], in order.  The places of 64 tokens are loaded at once, one a lane (each by a scalar load that its row waits for:
 // GPT-2's table 64 us, so 47; 32768 tokens of 4096 155 and 138).
 template <int DT, int GT, int C>
-__device__ __forceinline__ void add_rows(float (&acc)[C][Elem<GT>::E], const void *dout, int64_t ld, const int *order, int64_t a, int64_t b,
+__device__ __forceinline__ void add_rows(float (&acc)[C][Elem<GT>::E], const void *dout, int64_t ld, const int *order, int a, int b,
                                          const int64_t (&col)[C], int64_t dim) {
-    for (int64_t k0 = a; k0 < b; k0 += 64)              // in 64 bits: 64 more than a place among 2^31 - 1 tokens
-        add_listed<DT, GT>(acc, dout, ld, k0 + lane_of() < b ? order[k0 + lane_of()] : 0, b - k0 < 64 ? (int)(b - k0) : 64, col, dim);
+    const int *at = order + a, *end = order + b;        // addresses: 64 beyond the last place may take more than 32 bits
+    for (; at < end; at += 64)
+        add_listed<DT, GT>(acc, dout, ld, at + lane_of() < end ? at[lane_of()] : 0, end - at < 64 ? (int)(end - at) : 64, col, dim);
 }
 
 // Columns of a lane's pieces; the last piece of a row starts early, past the row: dim.
@@ -385,12 +386,13 @@ __global__ __launch_bounds__(THREADS) void k_sums(const void *dout, int64_t ld, 
     columns<E>(col, dim);
     if (blockIdx.x < seg_blocks) {
         const int64_t s = (int64_t)blockIdx.x * WAVES + wave_of();
-        const int64_t held = start[rows], a = s * seg, b = a + seg < held ? a + seg : held;
-        if (a >= b) return;
+        const int held = start[rows];
+        if (s * seg >= held) return;
+        const int a = (int)(s * seg), b = held - a > seg ? a + seg : held;      // the last segment's full end may take more than 32 bits
         const int rows_of[2] = {row_at[a], row_at[b - 1]};
         for (int slot = 0; slot < 2; ++slot) {
             if (slot == 1 && rows_of[1] == rows_of[0]) break;
-            const int64_t from = start[rows_of[slot]], to = start[rows_of[slot] + 1];
+            const int from = start[rows_of[slot]], to = start[rows_of[slot] + 1];
             if (to - from <= seg) continue;
             float acc[C][E] = {};
             add_rows<DT, GT>(acc, dout, ld, order, from > a ? from : a, to < b ? to : b, col, dim);
@@ -406,7 +408,7 @@ __global__ __launch_bounds__(THREADS) void k_sums(const void *dout, int64_t ld, 
             const int v = row_at[a], b = start[v + 1];
             if (start[v] != a || b - a > seg) continue;
             float acc[C][E] = {};
-            add_rows<DT, GT>(acc, dout, ld, order, a, b, col, dim);
+            add_rows<DT, GT>(acc, dout, ld, order, (int)a, b, col, dim);
             store_row<GT>(acc, grad, v, col, dim, scale);
         }
     } else {
@@ -427,10 +429,10 @@ __global__ __launch_bounds__(THREADS) void k_join(const int *start, const int *r
     int64_t col[1];
     columns<4>(col, dim);
     const int64_t s0 = (int64_t)blockIdx.x * WAVES + wave_of();
-    const int64_t held = start[rows], a = s0 * seg, end = a + seg < held ? a + seg : held;
-    if (a >= end) return;
-    const int v = row_at[end - 1];
-    const int64_t from = start[v], to = start[v + 1];
+    const int held = start[rows];
+    if (s0 * seg >= held) return;
+    const int a = (int)(s0 * seg), end = held - a > seg ? a + seg : held;
+    const int v = row_at[end - 1], from = start[v], to = start[v + 1];
     if (from < a || to - from <= seg || col[0] >= dim) return;
     float acc[4] = {};
     for (int64_t s = s0; s * seg < to; s += U) {
