@@ -372,7 +372,8 @@ typedef struct {
     int32_t reserved_;                          /* 0 */
 } paro_distill_t;
 
-/* loss: fp32 [n].  lse: NULL, or fp32 [n] = log of the sum of exp(logits / T), for paro_distill_grad. */
+/* loss: fp32 [n].  lse: NULL, or fp32 [n] = log of the sum of exp(logits / T), for paro_distill_grad (which forms a row's
+ * own again where the stored one is 1024 or more in size, and so no longer says enough of the row). */
 int paro_distill_loss(const paro_distill_t *d, const void *logits, const void *teacher, const int32_t *ids, float *loss,
                       float *lse, void *stream);
 /* dlogits = dloss[row] * the gradient above.  dloss: fp32 [n], NULL = ones.  dlogits may be logits. */

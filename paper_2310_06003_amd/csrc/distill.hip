@@ -19,6 +19,11 @@ constexpr float LOG2E = 1.44269504088896340736f, LN2 = 0.69314718055994530942f;
 __device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }      // 1 ulp; flushes below 2^-126
 constexpr float NOTHING = -__builtin_inff();
 
+// A stored log-sum L is off by up to 2^-24 L, which is what q = exp(z / T - L) is off by, relative.  From this size on (6e-5) the gradient forms
+// the row's own maximum and sum again, as the step does: at the lowest numbers of a type, which programs mask whole rows with, the stored one
+// holds nothing of the sum, or is infinite.
+constexpr float STORED_SERVES = 1024.0f;
+
 // Running maximum m of the logits and sum s of exp((x - m) / T), c = log2(e) / T.  m stays a logit, undivided: the lowest number of
 // a type, which programs mask with, does not overflow.  Nothing yet: m = -inf, s = 0.  fmaxf passes a NaN over; it reaches s.
 struct MaxSum {
@@ -86,6 +91,8 @@ __global__ __launch_bounds__(THREADS, HELD == 16 ? 4 : 1) void k_distill(const v
     const char *z = static_cast<const char *>(logits) + row * d.ld_logits * Elem<DT>::BYTES;
     char *dz = GRAD ? static_cast<char *>(dlogits) + row * d.ld_dlogits * Elem<DT>::BYTES : nullptr;
     const float inverse_t = 1.0f / d.temperature, c = LOG2E * inverse_t;
+    float stored = 0.0f;                                         // the row's log-sum, on its way beside the teacher's entries
+    if constexpr (!LOSS) stored = lse[row];
 
     if constexpr (GRAD && HELD > 0)
         for (int i = tid; i < LISTS; i += THREADS) s_list[i] = 0;
@@ -141,7 +148,7 @@ __global__ __launch_bounds__(THREADS, HELD == 16 ? 4 : 1) void k_distill(const v
         at_id[o] = j < k && s_id[j] >= 0 ? load_one<DT>(z, s_id[j]) : 0.0f;
     }
 
-    float most = 0.0f, norm;                                     // q = 2^((z - most) c - norm)
+    float most, norm;                                            // q = 2^((z - most) c - norm)
     if constexpr (LOSS) {
         MaxSum mine{NOTHING, 0.0f};
         const auto take = [&](u32x4 raw) {
@@ -179,7 +186,22 @@ __global__ __launch_bounds__(THREADS, HELD == 16 ? 4 : 1) void k_distill(const v
         norm = all.s == 0.0f ? 0.0f : __log2f(all.s);            // a row of -inf alone: q = 0
         if (lse && tid == 0) lse[row] = all.s == 0.0f ? NOTHING : most * inverse_t + norm * LN2;
     } else {
-        norm = lse[row] == NOTHING ? 0.0f : lse[row] * LOG2E;
+        // The stored log-sum as a logit, subtracted before anything is scaled: scaled first, both sides are rounded at their full size.  What that
+        // logit is off by, from 1 / T in two parts, goes into norm.
+        if (fabsf(stored) >= STORED_SERVES) {                    // NaN stays NaN
+            MaxSum mine{NOTHING, 0.0f};                          // element by element: seldom, and so without registers of its own
+#pragma unroll 1
+            for (int64_t i = tid; i < d.vocab; i += THREADS) {
+                const float x = load_one<DT>(z, i);
+                if (x != NOTHING) mine = join(mine, MaxSum{x, 1.0f}, c);
+            }
+            const MaxSum all = block_join<THREADS>(mine, s_student, c);
+            most = all.m == NOTHING ? 0.0f : all.m;
+            norm = all.s == 0.0f ? 0.0f : __log2f(all.s);
+        } else {
+            most = stored * d.temperature;
+            norm = (fmaf(-most, inverse_t, stored) - most * (fmaf(-d.temperature, inverse_t, 1.0f) * inverse_t)) * LOG2E;
+        }
     }
 
     // p, and this row's loss
