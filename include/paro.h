@@ -398,7 +398,8 @@ int64_t paro_gated_workspace(const paro_gated_t *d, int grad); /* bytes: of paro
 int paro_gated(const paro_gated_t *d, const void *x, const void *w_gate, const void *w_up, void *h, void *gate, void *up,
                void *workspace, int64_t workspace_bytes, void *stream);
 /* From dh (as h) and the stored projections: dg = dh * u * act'(g), du = dh * act(g), rounded to dtype where
- * the matrix cores take them (of a few tokens they stay fp32), and
+ * the matrix cores take them (of a few tokens they stay fp32; those of fp16 are scaled by a power of two where the largest would leave
+ * its range: what one loses is half an ulp, or 2^-25 of the largest), and
  *   dx = dg Wg + du Wu  (as x),   dWg = dg' x,   dWu = du' x  (dense; zeros for n == 0). */
 int paro_gated_grad(const paro_gated_t *d, const void *dh, const void *gate, const void *up, const void *x,
                     const void *w_gate, const void *w_up, void *dx, void *dw_gate, void *dw_up, void *workspace,

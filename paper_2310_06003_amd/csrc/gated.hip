@@ -87,6 +87,8 @@ struct Product {
     int tiles_m, tiles_n;
     unsigned whole, splits;              // the first tiles are whole blocks' work; of the others each is split among so many blocks,
     float *partial;                      // which leave their sums here: [tile][split][row of tiles][tile][thread][4]
+    const float *back;                   // of fp16 slopes: what the results are multiplied by (see k_slopes); or NULL
+    __device__ __forceinline__ float scale() const { return back ? *back : 1.0f; }
 };
 
 // Blocks go to the eight XCDs in turn: each takes a run of tiles of its own.
@@ -132,7 +134,7 @@ __device__ __forceinline__ void store8(const Product &p, char *out, int64_t m, i
 }
 // What a wave does with a finished row of its tiles.
 template <int DT, int MODE, int ACT, int BM, int BN>
-__device__ __forceinline__ void finish(const Product &p, const Place<MODE, BM, BN> &at, int64_t m, int wn, const f32x4 (&acc)[4]) {
+__device__ __forceinline__ void finish(const Product &p, const Place<MODE, BM, BN> &at, int64_t m, int wn, float scale, f32x4 (&acc)[4]) {
     if constexpr (MODE == FORWARD) {
         f32x4 h[2];
 #pragma unroll
@@ -146,6 +148,10 @@ __device__ __forceinline__ void finish(const Product &p, const Place<MODE, BM, B
             store8<DT>(p, p.out[2], m, n, acc[2], acc[3]);
         }
     } else {
+        if constexpr (DT == PARO_F16) {
+#pragma unroll
+            for (int j = 0; j < 4; ++j) acc[j] *= scale;
+        }
 #pragma unroll
         for (int j = 0; j < 4; j += 2) store8<DT>(p, at.part ? p.out[1] : p.out[0], m, at.col0 + (wn * 4 + j) * 16, acc[j], acc[j + 1]);
     }
@@ -170,6 +176,7 @@ __device__ __forceinline__ void product(const Product p, unsigned block, unsigne
     const Place<MODE, BM, BN> at(p, is_whole ? in_runs(block, p.whole) : p.whole + split_tile);
     const int64_t row0 = at.row0, col0 = at.col0;
     const int out_part = at.part;
+    const float scale = DT == PARO_F16 && MODE != FORWARD ? p.scale() : 1.0f;       // loaded long before it is needed
 
     // A lane's pieces: their offsets from where the stage begins, and the step (along: the first of eight) of each.  The pieces of a
     // stage are exchanged within 256 bytes such that the lanes that read at a time meet all banks.  Pieces of rows or columns that the operand
@@ -365,7 +372,7 @@ __device__ __forceinline__ void product(const Product p, unsigned block, unsigne
         return;
     }
 #pragma unroll
-    for (int i = 0; i < TM; ++i) finish<DT, MODE, ACT>(p, at, row0 + (wm * TM + i) * 16 + of16, wn, acc[i]);
+    for (int i = 0; i < TM; ++i) finish<DT, MODE, ACT>(p, at, row0 + (wm * TM + i) * 16 + of16, wn, scale, acc[i]);
 }
 
 template <int DT, int MODE, int ACT, int BM, int BN, int WAVES_M, int WAVES_N>
@@ -387,6 +394,7 @@ __global__ __launch_bounds__(64 * WAVES_M * WAVES_N) void k_join(Product p) {
     const int w = wave_of(), i = blockIdx.y;
     const Place<MODE, BM, BN> at(p, p.whole + blockIdx.x);
     const int64_t m = at.row0 + ((w / WAVES_N) * TM + i) * 16 + (threadIdx.x & 15);
+    const float scale = DT == PARO_F16 && MODE != FORWARD ? p.scale() : 1.0f;
     constexpr unsigned U = 4;                       // shares in flight, the last ones too (one by one: 26 tokens of 1231 x 16256 backward 107 us, so 99; 16: 98)
     f32x4 acc[TN] = {};
     if (m < p.rows) {
@@ -405,7 +413,7 @@ __global__ __launch_bounds__(64 * WAVES_M * WAVES_N) void k_join(Product p) {
                     for (int j = 0; j < TN; ++j) acc[j] += part[u][j];
         }
     }
-    finish<DT, MODE, ACT>(p, at, m, w % WAVES_N, acc);
+    finish<DT, MODE, ACT>(p, at, m, w % WAVES_N, scale, acc);
 }
 
 // Forward for few tokens: the weights are read once, straight into registers as fragments, and nothing else counts.  A block takes F_TILES x
@@ -637,25 +645,64 @@ __global__ __launch_bounds__(512) void k_few_join(const float *partial, int n, i
 // run of memory, for dx (256 tokens of a panel) as for dW (64 tokens of four), where rows of 11008 would be 22 KB apart
 // (8192 tokens of 4096 x 11008 2302 us, so 2285; this kernel 150 and 141).  Rounded to the
 // weights' type, which is what the matrix cores take.  A wave takes eight tokens of a panel.
-template <int DT, int ACT>
-__global__ __launch_bounds__(256) void k_slopes(const void *dh, const void *gate, const void *up, int64_t ld, int64_t tokens, int64_t hidden,
-                                                int64_t panels, char *out) {
+//
+// The product of three fp16 numbers may lie beyond 65504, or where fp16 keeps a binary place or two.  So each block writes down its largest dg or du, of
+// the finite ones, and a second launch looks at them: if the largest is below 1 or above 65504 it forms all slopes again, times the power of two that
+// brings the largest to between 2^14 and 2^15, and the products' results are multiplied by its inverse.  Either way what a slope loses
+// is half an ulp, or 2^-25 of the largest.
+struct Slopes {
+    const void *dh, *gate, *up;
+    int64_t ld, tokens, hidden, panels;
+    char *out;
+    float *back, *largest;               // of fp16: what the results are multiplied by; of each block of the first launch
+    int blocks;
+};
+__device__ __forceinline__ float block_most(float v, float *room) {
+#pragma unroll
+    for (int step = 32; step >= 1; step /= 2) v = fmaxf(v, __shfl_xor(v, step));
+    if ((threadIdx.x & 63) == 0) room[threadIdx.x >> 6] = v;
+    __syncthreads();
+    return fmaxf(fmaxf(room[0], room[1]), fmaxf(room[2], room[3]));
+}
+
+template <int DT, int ACT, bool AGAIN>
+__global__ __launch_bounds__(256) void k_slopes(Slopes s) {
+    constexpr bool WATCHED = DT == PARO_F16;
+    static_assert(WATCHED || !AGAIN, "other types have the range");
+    __shared__ float room[4];
     const int lane = threadIdx.x & 63;
     const int64_t panel = (int64_t)blockIdx.x * 4 + wave_of(), f = panel * 64 + (lane & 7) * 8;
-    if (panel >= panels) return;
-    for (int64_t m = (int64_t)blockIdx.y * 8 + lane / 8; m < tokens; m += (int64_t)gridDim.y * 8) {
+    float factor = 1.0f, most = 0.0f;
+    if constexpr (AGAIN) {
+        constexpr int U = 8;                        // all of a launch of 2048 blocks at once
+        for (int i = threadIdx.x; i < s.blocks; i += U * 256) {
+            float of[U];
+#pragma unroll
+            for (int k = 0; k < U; ++k) of[k] = i + k * 256 < s.blocks ? s.largest[i + k * 256] : 0.0f;
+#pragma unroll
+            for (int k = 0; k < U; ++k) most = fmaxf(most, of[k]);
+        }
+        most = block_most(most, room);
+        const bool fits = most == 0.0f || (most >= 1.0f && most <= 65504.0f);
+        const int exponent = (int)(__float_as_uint(most) >> 23) - 127;      // at least -80: three times 2^-24, and a slope's own smallness
+        const int up = fits ? 0 : 14 - (exponent > -100 ? exponent : -100);
+        if (blockIdx.x == 0 && blockIdx.y == 0 && threadIdx.x == 0) *s.back = __uint_as_float((unsigned)(127 - up) << 23);
+        if (fits) return;
+        factor = __uint_as_float((unsigned)(127 + up) << 23);
+    }
+    for (int64_t m = (int64_t)blockIdx.y * 8 + lane / 8; panel < s.panels && m < s.tokens; m += (int64_t)gridDim.y * 8) {
         float d[8] = {}, g[8] = {}, u[8] = {}, dg[8], du[8];
-        const int64_t at = m * ld + f;
-        if (f + 8 <= hidden) {
-            unpack<DT>(load_stream<DT>(dh, at), d);
-            unpack<DT>(load_stream<DT>(gate, at), g);
-            unpack<DT>(load_stream<DT>(up, at), u);
+        const int64_t at = m * s.ld + f;
+        if (f + 8 <= s.hidden) {
+            unpack<DT>(load_stream<DT>(s.dh, at), d);
+            unpack<DT>(load_stream<DT>(s.gate, at), g);
+            unpack<DT>(load_stream<DT>(s.up, at), u);
         } else {
             for (int e = 0; e < 8; ++e)
-                if (f + e < hidden) {
-                    d[e] = load_one<DT>(dh, at + e);
-                    g[e] = load_one<DT>(gate, at + e);
-                    u[e] = load_one<DT>(up, at + e);
+                if (f + e < s.hidden) {
+                    d[e] = load_one<DT>(s.dh, at + e);
+                    g[e] = load_one<DT>(s.gate, at + e);
+                    u[e] = load_one<DT>(s.up, at + e);
                 }
         }
 #pragma unroll
@@ -664,11 +711,29 @@ __global__ __launch_bounds__(256) void k_slopes(const void *dh, const void *gate
             act_and_slope<ACT>(g[e], a, da);
             dg[e] = d[e] * u[e] * da;
             du[e] = d[e] * a;
+            if constexpr (AGAIN) {
+                dg[e] *= factor;
+                du[e] *= factor;
+            } else if constexpr (WATCHED) {
+                most = fmaxf(most, fabsf(dg[e]) <= 3.4e38f ? fabsf(dg[e]) : 0.0f);
+                most = fmaxf(most, fabsf(du[e]) <= 3.4e38f ? fabsf(du[e]) : 0.0f);
+            }
         }
-        const int64_t to = (panel * tokens + m) * 64 + (lane & 7) * 8;
-        store_piece<DT>(out, to, pack<DT>(dg));
-        store_piece<DT>(out, panels * tokens * 64 + to, pack<DT>(du));
+        const int64_t to = (panel * s.tokens + m) * 64 + (lane & 7) * 8;
+        store_piece<DT>(s.out, to, pack<DT>(dg));
+        store_piece<DT>(s.out, s.panels * s.tokens * 64 + to, pack<DT>(du));
     }
+    if constexpr (WATCHED && !AGAIN) {
+        most = block_most(most, room);
+        if (threadIdx.x == 0) s.largest[blockIdx.y * gridDim.x + blockIdx.x] = most;
+    }
+}
+// At most so many blocks, in whole columns of them: of fp16 few enough that each of the second launch reads the largest of all, and of that one, which
+// mostly ends there, as few as fill the chip (2048: 4000 tokens of 512 x 1024 backward 50 us, so 47; in a type that needs none of this 43).
+constexpr int64_t WATCHED_BLOCKS = 2048, AGAIN_BLOCKS = 512;
+dim3 slopes_grid(const paro_gated_t &d, int64_t panels, int64_t blocks) {
+    const int64_t x = (panels + 3) / 4, y = (d.n + 7) / 8;
+    return dim3((unsigned)x, (unsigned)std::min(y, std::max<int64_t>(1, blocks / x)));
 }
 
 // Rows that the fills cannot take - a row or the distance between two is no multiple of 16 bytes - copied to where they can, zeros behind:
@@ -844,7 +909,7 @@ int launch_products(Product dx, Product dw, const Shapes &s, float *partial, hip
 }
 
 struct Room {                            // parts of the workspace, in bytes
-    int64_t x, wg, wu, slopes, partial, all;
+    int64_t x, wg, wu, slopes, largest, partial, all;
 };
 int64_t ld_x(const paro_gated_t &d) { return d.ld_x ? d.ld_x : d.dim; }
 int64_t ld_h(const paro_gated_t &d) { return d.ld_h ? d.ld_h : d.hidden; }
@@ -878,6 +943,10 @@ Room room_of(const paro_gated_t &d, bool grad) {
     int64_t partial = 0;
     if (grad) {
         r.slopes = take(2 * up_to(d.hidden, 64) * d.n * 2);
+        if (d.dtype == PARO_F16) {
+            const dim3 grid = slopes_grid(d, ceil_div(d.hidden, 64), WATCHED_BLOCKS);
+            r.largest = take((1 + (int64_t)grid.x * grid.y) * 4);
+        }
         partial = shapes_of(d.n, d.dim, d.hidden).partial_bytes();
     } else {
         partial = shape_of(FORWARD, d.n, d.hidden, d.dim).partial_bytes();
@@ -1022,8 +1091,14 @@ int backward(const paro_gated_t &d, const void *dh, const void *gate, const void
     const int64_t panels = ceil_div(d.hidden, 64);
     char *slopes = ws + r.slopes;
     float *partial = reinterpret_cast<float *>(ws + r.partial);
-    hipLaunchKernelGGL((k_slopes<DT, ACT>), dim3((unsigned)ceil_div(panels, 4), (unsigned)std::min<int64_t>(ceil_div(d.n, 8), 65535)), dim3(256), 0, st, dh, gate,
-                       up, ld_h(d), d.n, d.hidden, panels, slopes);
+    const dim3 grid = DT == PARO_F16 ? slopes_grid(d, panels, WATCHED_BLOCKS) : dim3((unsigned)ceil_div(panels, 4), (unsigned)std::min<int64_t>(ceil_div(d.n, 8), 65535));
+    float *largest = reinterpret_cast<float *>(ws + r.largest);
+    const Slopes of{dh, gate, up, ld_h(d), d.n, d.hidden, panels, slopes, largest, largest + 1, (int)(grid.x * grid.y)};
+    hipLaunchKernelGGL((k_slopes<DT, ACT, false>), grid, dim3(256), 0, st, of);
+    if constexpr (DT == PARO_F16) {
+        hipLaunchKernelGGL((k_slopes<DT, ACT, true>), slopes_grid(d, panels, AGAIN_BLOCKS), dim3(256), 0, st, of);
+        p.back = largest;
+    }
     p.panel = d.n * ROW_BYTES;
     p.a[0] = slopes;
     p.a[1] = slopes + panels * p.panel;
