@@ -57,11 +57,11 @@ __device__ __forceinline__ int wave_of() { return __builtin_amdgcn_readfirstlane
 
 // 16 bytes a lane from memory to shared memory at `to` + 16 * lane, past the registers; out of range: zeros.  In assembly because
 // the compiler, which cannot tell the stages apart, would wait for it before every read of shared memory; all_waves() waits.
-// There is no vector register that it writes; m0, which nothing else in these kernels uses, cannot be named as written.
+// It writes no register.  m0, which holds the place in shared memory, is an operand, so that the compiler knows what is in it; one instruction has to
+// stand between its write and its use.
 template <int AT>
 __device__ __forceinline__ void fill(u32x4 from, unsigned offset, unsigned to) {
-    asm volatile("s_add_u32 m0, %0, %3\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(to), "v"(offset), "s"(from), "i"(AT)
-                 : "memory", "scc");
+    asm volatile("s_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"{m0}"(to + AT), "v"(offset), "s"(from) : "memory");
 }
 // All but the wave's last `IN_FLIGHT` fills have arrived, all its reads are done; then those of all waves.
 template <int IN_FLIGHT>
