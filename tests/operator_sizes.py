@@ -1,0 +1,28 @@
+"""Sizes by which the tests on the GPU reach the forms of the operators' kernels that only larger calls take, each with the form it is there for.
+test_operator_launches.py holds the library to these."""
+
+# n, dim, hidden, dtype, act, pad: what the products of the forward pass are (tiles of 256 or 128, and whether the tiles of a last, partly
+# filled round are split over the inner dimension: all of them, those beyond whole rounds, or none)
+FORWARD = {
+    (7406, 1056, 1136, "bf16", "silu", 0): "256 rest split",
+    (1500, 2048, 4096, "f16", "silu", 8): "256 unsplit",
+    (137, 2542, 4432, "f16", "gelu", 3): "256 all split",
+    (908, 95, 4239, "bf16", "gelu", 1): "256 unsplit",
+    (3389, 3552, 1159, "bf16", "silu", 0): "128 rest split",
+    (138, 1056, 116, "f16", "silu", 0): "128 all split",
+    (163, 96, 108, "bf16", "gelu", 5): "128 unsplit",
+}
+# ... and of dx, and of dWg and dWu, each in a launch of its own
+BACKWARD = {
+    (1500, 2048, 4096, "bf16", "silu", 0): ("256 all split", "256 unsplit"),
+    (1999, 1601, 4099, "f16", "gelu", 3): ("256 all split", "256 unsplit"),
+    (1485, 1200, 6591, "bf16", "gelu", 8): ("256 all split", "256 rest split"),
+    (9387, 1552, 940, "f16", "silu", 0): ("256 rest split", "256 all split"),
+    (7300, 1776, 143, "bf16", "silu", 0): ("256 unsplit", "128 all split"),
+    (4878, 2791, 145, "bf16", "gelu", 1): ("256 unsplit", "256 all split"),
+    (3943, 670, 5651, "f16", "silu", 0): ("256 all split", "128 rest split"),
+    (1355, 1104, 3472, "bf16", "silu", 0): ("128 all split", "128 unsplit"),
+    (6257, 144, 4773, "bf16", "silu", 8): ("128 all split", "256 all split"),
+    (9340, 767, 647, "f16", "gelu", 0): ("128 unsplit", "128 all split"),
+    (5560, 1464, 2130, "bf16", "gelu", 0): ("128 rest split", "256 all split"),
+}
