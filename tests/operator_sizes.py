@@ -26,3 +26,16 @@ BACKWARD = {
     (9340, 767, 647, "f16", "gelu", 0): ("128 unsplit", "128 all split"),
     (5560, 1464, 2130, "bf16", "gelu", 0): ("128 rest split", "256 all split"),
 }
+# n, dim, hidden, dtype, act, pad of passes of few tokens backward: blocks of columns, and hidden elements of a share
+FEW_BACKWARD = {
+    (1, 4096, 11008, "bf16", "silu", 0): (8, 86),
+    (1, 9, 17000, "f16", "gelu", 1): (1, 67),
+    (3, 513, 1000, "f16", "silu", 0): (2, 4),
+    (4, 1601, 17000, "bf16", "gelu", 3): (4, 67),
+    (8, 4099, 2500, "bf16", "silu", 0): (9, 23),
+    (8, 2056, 3333, "f16", "silu", 8): (5, 17),
+    (9, 512, 17024, "bf16", "gelu", 0): (2, 67),
+    (12, 4100, 5000, "f16", "gelu", 5): (17, 84),
+    (16, 1601, 8199, "bf16", "silu", 0): (7, 57),
+    (16, 257, 17000, "f16", "silu", 1): (2, 67),
+}

@@ -141,3 +141,11 @@ def test_every_form_of_every_product_has_a_size():
     forms = {f"{side} {how}" for side in (256, 128) for how in ("unsplit", "rest split", "all split")}
     assert set(sizes.FORWARD.values()) == forms
     assert {dx for dx, _ in sizes.BACKWARD.values()} == forms and {dw for _, dw in sizes.BACKWARD.values()} == forms
+
+
+@pytest.mark.parametrize("size", list(sizes.FEW_BACKWARD))
+def test_forms_of_few_tokens_backward(launches, size):
+    n, dim, hidden, dtype, act, pad = size
+    grad, join = launches("gated_grad", n, dim, hidden, DTYPES[dtype], ACTS[act], pad)
+    assert (grad.kernel, join.kernel) == ("k_few_grad", "k_few_join")
+    assert (grad.y, -(-hidden // grad.x)) == sizes.FEW_BACKWARD[size]
