@@ -39,3 +39,22 @@ FEW_BACKWARD = {
     (16, 1601, 8199, "bf16", "silu", 0): (7, 57),
     (16, 257, 17000, "f16", "silu", 1): (2, 67),
 }
+# dtype, grad dtype, n, rows of the table, dim of table gradients: 16-byte pieces of a row that a lane of the sums takes
+TABLE_GRADIENT = {
+    ("bf16", "bf16", 6500, 57, 520): 2,
+    ("bf16", "bf16", 7000, 900, 1023): 2,
+    ("bf16", "bf16", 7001, 57, 1030): 4,
+    ("bf16", "bf16", 3100, 900, 2056): 4,
+    ("bf16", "bf16", 2100, 40, 4099): 4,
+    ("f16", "f16", 9000, 2000, 1024): 2,
+    ("f16", "f16", 6200, 900, 1531): 4,
+    ("bf16", "f32", 6700, 57, 301): 2,
+    ("bf16", "f32", 7000, 900, 1030): 4,
+    ("f16", "f32", 6500, 900, 512): 2,
+    ("f16", "f32", 8191, 3000, 768): 4,
+    ("f16", "f32", 2500, 40, 2051): 4,
+    ("f32", "f32", 6500, 57, 260): 2,
+    ("f32", "f32", 9000, 900, 511): 2,
+    ("f32", "f32", 6600, 57, 515): 4,
+    ("f32", "f32", 3300, 900, 1029): 4,
+}

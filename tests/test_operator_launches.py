@@ -149,3 +149,10 @@ def test_forms_of_few_tokens_backward(launches, size):
     grad, join = launches("gated_grad", n, dim, hidden, DTYPES[dtype], ACTS[act], pad)
     assert (grad.kernel, join.kernel) == ("k_few_grad", "k_few_join")
     assert (grad.y, -(-hidden // grad.x)) == sizes.FEW_BACKWARD[size]
+
+
+@pytest.mark.parametrize("size", list(sizes.TABLE_GRADIENT))
+def test_pieces_of_the_table_gradient(launches, size):
+    dtype, grad_dtype, n, rows, dim = size
+    sums, = [x for x in launches("embed_grad", n, rows, dim, DTYPES[dtype], DTYPES[grad_dtype]) if x.kernel == "k_sums"]
+    assert int(sums.flags[2]) == sizes.TABLE_GRADIENT[size]
