@@ -1,0 +1,55 @@
+"""Outputs of the distillation calls that the definition's tests leave open: the step's own loss where rows hold NaN, and the gradient written
+over the logits by paro_distill_grad."""
+import math
+
+import pytest
+import torch
+
+from operators_ref import DEV, TORCH, code, put, rng, rows, stream
+
+pytestmark = pytest.mark.gpu
+
+
+def some(n, v, k, seed):
+    g = rng(seed)
+    z, t = torch.randn(n, v, generator=g) * 2, torch.randn(n, k, generator=g)
+    ids = torch.randint(-1, v, (n, k), generator=g)
+    ids[n // 2] = -1
+    return z, t, ids
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("v", [7, 500, 5000, 30011, 140003])
+def test_loss_of_the_step_is_the_loss(paro, v, dtype):
+    """Bit for bit, row by row, NaN where the loss is NaN and nowhere else."""
+    z, t, ids = some(7, v, 6, v)
+    ids[1, 0] = ids[2, 0] = 0
+    z[1, v // 2], z[2, 0] = math.nan, -math.inf
+    z[3] = math.nan                                         # a row that holds no entry
+    d = paro.make_distill(n=7, vocab=v, k=6, temperature=2.0, dtype=code(paro, dtype), teacher_dtype=paro.PARO_F32)
+    zd, td, idd = z.to(DEV, TORCH[dtype]), t.to(DEV), ids.int().to(DEV)
+    loss, step = (torch.full((7,), 77.0, device=DEV) for _ in range(2))
+    dz = torch.empty(7, v, dtype=TORCH[dtype], device=DEV)
+    paro.paro_distill_loss(d, zd.data_ptr(), td.data_ptr(), idd.data_ptr(), loss.data_ptr(), 0, stream())
+    paro.paro_distill_step(d, zd.data_ptr(), td.data_ptr(), idd.data_ptr(), 0, step.data_ptr(), dz.data_ptr(), stream())
+    assert loss.isnan().tolist() == [False, True] + [False] * 5 and bool(loss[2].isposinf()) and float(loss[3]) == 0.0
+    assert bool(((loss == step) | (loss.isnan() & step.isnan())).all())
+
+
+@pytest.mark.parametrize("pad", [0, 3])
+@pytest.mark.parametrize("dtype,v", [(d, v) for d in ("bf16", "f16", "f32") for v in (5, 1000, 9001, 50257)] + [("f32", 65541), ("bf16", 131081)])
+def test_gradient_over_the_logits(paro, dtype, v, pad):
+    """The same bits as into an array of its own, nothing written between the rows."""
+    z, t, ids = some(5, v, 9, v)
+    d = paro.make_distill(n=5, vocab=v, k=9, temperature=2.0, dtype=code(paro, dtype), teacher_dtype=paro.PARO_F32, ld_logits=v + pad, ld_dlogits=v + pad)
+    whole, zd = rows(5, v, pad, dtype, fill=5.0)
+    zd.copy_(z.to(TORCH[dtype]))
+    td, idd, w = t.to(DEV), ids.int().to(DEV), torch.rand(5, generator=rng(1)).to(DEV)
+    loss, lse = torch.empty(5, device=DEV), torch.empty(5, device=DEV)
+    paro.paro_distill_loss(d, zd.data_ptr(), td.data_ptr(), idd.data_ptr(), loss.data_ptr(), lse.data_ptr(), stream())
+    apart = rows(5, v, pad, dtype)[1]
+    for target in (apart, zd):
+        paro.paro_distill_grad(d, zd.data_ptr(), td.data_ptr(), idd.data_ptr(), lse.data_ptr(), w.data_ptr(), target.data_ptr(), stream())
+    assert torch.equal(apart, zd)
+    zd.fill_(5.0)
+    assert bool((whole == 5.0).all())
