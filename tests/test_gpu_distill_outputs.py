@@ -5,7 +5,8 @@ import math
 import pytest
 import torch
 
-from operators_ref import DEV, TORCH, code, put, rng, rows, stream
+from operators_ref import DEV, TORCH, code, rng, rows, stream
+from test_gpu_distill import run_all, some_inputs
 
 pytestmark = pytest.mark.gpu
 
@@ -53,3 +54,11 @@ def test_gradient_over_the_logits(paro, dtype, v, pad):
     assert torch.equal(apart, zd)
     zd.fill_(5.0)
     assert bool((whole == 5.0).all())
+
+
+@pytest.mark.parametrize("dtype", ["f16", "f32"])
+@pytest.mark.parametrize("v,k", [(900, 1024), (1500, 600), (4096, 513)])
+def test_many_entries_in_short_rows(paro, dtype, v, k):
+    """More entries than the few threads of a short row would have taken: more threads."""
+    z, t, ids = some_inputs(3, v, k, v + k)
+    run_all(paro, z, t, ids, 2.0, dtype, "f32", pad=v % 3)
