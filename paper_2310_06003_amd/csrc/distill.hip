@@ -204,14 +204,14 @@ __global__ __launch_bounds__(THREADS, HELD == 16 ? 4 : 1) void k_distill(const v
         }
     }
 
-    // p, and this row's loss
-    const float top_norm = __log2f(top.s) * LN2;
+    // p, and this row's loss.  p is divided by its sum itself, not in the exponent, where the sum's logarithm would be rounded at its size.
+    const float top_norm = __log2f(top.s) * LN2, share = 1.0f / top.s;
     float sum = 0.0f;
 #pragma unroll
     for (int o = 0; o < OWN; ++o) {
         const int j = o * THREADS + tid;
         if (j < k) {
-            const float lp = (s_p[j] - top.m) * inverse_t - top_norm, p = s_id[j] >= 0 ? exp2_fast(lp * LOG2E) : 0.0f;
+            const float below = s_p[j] - top.m, lp = below * inverse_t - top_norm, p = s_id[j] >= 0 ? exp2_fast(below * c) * share : 0.0f;
             s_p[j] = p;
             if (LOSS && p != 0.0f) sum += p * (lp - ((at_id[o] - most) * inverse_t - norm * LN2));
         }

@@ -89,3 +89,25 @@ def test_log_sums_that_32_bits_do_not_resolve(paro, v, T, around):
     err = wT * (q * (4 * TINY + EPS32 * torch.where(lse.abs() < STORED, lse.abs(), 0.0)[:, None]) + 8 * TINY * P) + 2.0 ** -120
     check(step, ref, rounding(ref, "f32", err), "step")
     check(grad, ref, rounding(ref, "f32", err), "gradient")
+
+
+@pytest.mark.parametrize("which", ["grad", "step"])
+def test_the_teachers_share_is_as_exact_as_its_roundings(paro, which):
+    """Named words that the student masks: their gradient is -T w p alone.  Over many rows p is off, in the mean square, by what its own roundings
+    make up: the exponent's (at a size of 3 about 5e-8), the exponential's (7e-8), the sum's, its reciprocal's and the product's (4 to 5e-8
+    each), 1.2e-7 together.  Divided by its sum through a logarithm it would be off by that logarithm's rounding too, at its size."""
+    n, v, k, T = 512, 2000, 100, 2.0
+    g = rng(5)
+    t, ids = torch.randn(n, k, generator=g) * 2, torch.stack([torch.randperm(v, generator=g)[:k] for _ in range(n)])
+    z = torch.randn(n, v, generator=g).scatter_(1, ids, float("-inf"))
+    zd, td, idd = z.to(DEV), t.to(DEV), ids.int().to(DEV)
+    d = paro.make_distill(n=n, vocab=v, k=k, temperature=T, dtype=paro.PARO_F32, teacher_dtype=paro.PARO_F32)
+    loss, lse, dz = torch.empty(n, device=DEV), torch.empty(n, device=DEV), torch.empty(n, v, device=DEV)
+    args = zd.data_ptr(), td.data_ptr(), idd.data_ptr()
+    paro.paro_distill_loss(d, *args, loss.data_ptr(), lse.data_ptr(), stream())
+    if which == "grad":
+        paro.paro_distill_grad(d, *args, lse.data_ptr(), 0, dz.data_ptr(), stream())
+    else:
+        paro.paro_distill_step(d, *args, 0, loss.data_ptr(), dz.data_ptr(), stream())
+    got, ref = -dz.cpu().double().gather(1, ids) / T, torch.softmax(t.double() / T, dim=1)
+    assert float((got - ref).norm() / ref.norm()) < 1.5e-7
