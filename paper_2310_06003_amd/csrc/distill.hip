@@ -28,6 +28,16 @@ constexpr float STORED_SERVES = 1024.0f;
 // a type, which programs mask with, does not overflow.  Nothing yet: m = -inf, s = 0.  fmaxf passes a NaN over; it reaches s.
 struct MaxSum {
     float m, s;
+    template <int N>
+    __device__ __forceinline__ void take(const float (&x)[N], float c) {
+        const float before = m;
+#pragma unroll
+        for (int e = 0; e < N; ++e) m = fmaxf(m, x[e]);
+        const float from = m == NOTHING ? 0.0f : m;
+        s *= before == NOTHING ? 1.0f : exp2_fast((before - from) * c);
+#pragma unroll
+        for (int e = 0; e < N; ++e) s += exp2_fast((x[e] - from) * c);
+    }
 };
 __device__ __forceinline__ MaxSum join(MaxSum a, MaxSum b, float c) {
     MaxSum r;
@@ -72,9 +82,9 @@ __device__ __forceinline__ float teacher_of(const void *t, int64_t at, int dtype
 }
 
 // HELD pieces of the row a thread, in registers; 0: the row is read again for the gradient.  Of 16, no more than 128 registers (two
-// more, and so one block of 512 threads a compute unit: 666 rows of 60179 43 us, so 38).
+// more, and so one block of 512 threads a compute unit: 666 rows of 60179 43 us, so 38); of 8 in the gradient alone no more than 72, seven waves a SIMD.
 template <int DT, int THREADS, int HELD, bool LOSS, bool GRAD>
-__global__ __launch_bounds__(THREADS, HELD == 16 ? 4 : 1) void k_distill(const void *logits, const void *teacher, const int32_t *ids, const float *dloss, float *loss,
+__global__ __launch_bounds__(THREADS, HELD == 16 ? 4 : HELD == 8 && !LOSS ? 7 : 1) void k_distill(const void *logits, const void *teacher, const int32_t *ids, const float *dloss, float *loss,
                                                      float *lse, void *dlogits, Row d) {
     constexpr int E = Elem<DT>::E, ROOM = 4 * THREADS < MAX_K ? 4 * THREADS : MAX_K;      // for entries
     constexpr unsigned MINUS_INF = DT == PARO_F32 ? 0xFF800000u : DT == PARO_F16 ? 0xFC00FC00u : 0xFF80FF80u;
@@ -148,26 +158,27 @@ __global__ __launch_bounds__(THREADS, HELD == 16 ? 4 : 1) void k_distill(const v
         at_id[o] = j < k && s_id[j] >= 0 ? load_one<DT>(z, s_id[j]) : 0.0f;
     }
 
-    float most, norm;                                            // q = 2^((z - most) c - norm)
-    if constexpr (LOSS) {
+    // Maximum and sum of the row.
+    const auto of_row = [&]() {
         MaxSum mine{NOTHING, 0.0f};
         const auto take = [&](u32x4 raw) {
             float x[E];
             unpack<DT>(raw, x);
-            float m = mine.m;
-#pragma unroll
-            for (int e = 0; e < E; ++e) m = fmaxf(m, x[e]);
-            const float from = m == NOTHING ? 0.0f : m;
-            float s = mine.s * (mine.m == NOTHING ? 1.0f : exp2_fast((mine.m - from) * c));
-#pragma unroll
-            for (int e = 0; e < E; ++e) s += exp2_fast((x[e] - from) * c);
-            mine = MaxSum{m, s};
+            mine.take(x, c);
         };
-        if constexpr (HELD > 0) {
+        if constexpr (HELD > 0 && LOSS) {
 #pragma unroll
             for (int h = 0; h < HELD; ++h) {
                 if (h * THREADS + wave < pieces) take(held[h]);     // 4000 rows of 17000 60 us without, 53
                 apart(held[h]);
+            }
+        } else if constexpr (HELD > 0) {
+#pragma unroll
+            for (int h = 0; h < HELD; ++h) {        // of copies: what is unpacked here, by few rows, is not kept for all of them
+                u32x4 piece = held[h];
+                if constexpr (DT != PARO_F32) apart(piece);
+                take(piece);
+                __builtin_amdgcn_sched_barrier(0);
             }
         } else {
             for (int64_t i = tid; i < pieces; i += 4 * THREADS) {
@@ -181,27 +192,19 @@ __global__ __launch_bounds__(THREADS, HELD == 16 ? 4 : 1) void k_distill(const v
             }
         }
         if (tid < rest && last != NOTHING) mine = join(mine, MaxSum{last, 1.0f}, c);
-        const MaxSum all = block_join<THREADS>(mine, s_student, c);
+        return block_join<THREADS>(mine, s_student, c);
+    };
+    float most, norm;                                            // q = 2^((z - most) c - norm)
+    if (LOSS || fabsf(stored) >= STORED_SERVES) {                // a stored NaN stays NaN
+        const MaxSum all = of_row();
         most = all.m == NOTHING ? 0.0f : all.m;
         norm = all.s == 0.0f ? 0.0f : __log2f(all.s);            // a row of -inf alone: q = 0
-        if (lse && tid == 0) lse[row] = all.s == 0.0f ? NOTHING : most * inverse_t + norm * LN2;
+        if (LOSS && lse && tid == 0) lse[row] = all.s == 0.0f ? NOTHING : most * inverse_t + norm * LN2;
     } else {
         // The stored log-sum as a logit, subtracted before anything is scaled: scaled first, both sides are rounded at their full size.  What that
         // logit is off by, from 1 / T in two parts, goes into norm.
-        if (fabsf(stored) >= STORED_SERVES) {                    // NaN stays NaN
-            MaxSum mine{NOTHING, 0.0f};                          // element by element: seldom, and so without registers of its own
-#pragma unroll 1
-            for (int64_t i = tid; i < d.vocab; i += THREADS) {
-                const float x = load_one<DT>(z, i);
-                if (x != NOTHING) mine = join(mine, MaxSum{x, 1.0f}, c);
-            }
-            const MaxSum all = block_join<THREADS>(mine, s_student, c);
-            most = all.m == NOTHING ? 0.0f : all.m;
-            norm = all.s == 0.0f ? 0.0f : __log2f(all.s);
-        } else {
-            most = stored * d.temperature;
-            norm = (fmaf(-most, inverse_t, stored) - most * (fmaf(-d.temperature, inverse_t, 1.0f) * inverse_t)) * LOG2E;
-        }
+        most = stored * d.temperature;
+        norm = (fmaf(-most, inverse_t, stored) - most * (fmaf(-d.temperature, inverse_t, 1.0f) * inverse_t)) * LOG2E;
     }
 
     // p, and this row's loss.  p is divided by its sum itself, not in the exponent, where the sum's logarithm would be rounded at its size.
