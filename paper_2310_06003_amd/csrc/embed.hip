@@ -224,8 +224,9 @@ __global__ __launch_bounds__(SORT_THREADS) void k_sort_tokens(const Token *token
     });
 }
 
-// Pieces a lane of the sums takes: as many as a row has for it (16 rows' pieces in flight in any case), at most (2: GPT-2's table 51 us, not
-// 47, 32768 tokens of 4096 179, not 138).  4 whatever the width: 60000 tokens of 640 90 us, so 84; of 64 fp32 elements 66, so 60.
+// Pieces a lane of the sums takes at most (2: GPT-2's table 51 us, not 47, 32768 tokens of 4096 179, not 138); one where that would leave too few
+// waves (few_waves, below), and no more than a row has for it (4 whatever the width: 60000 tokens of 640 90 us, so 84; of 64 fp32 elements 66, so 60).
+// 16 rows' pieces are in flight in any case.
 constexpr int GRAD_PIECES = 4;
 // ---------------------------------------------------------------- sums over the sorted tokens
 // What a lane loads of a row of dout: as many elements as a piece of the gradient has, so that every store instruction of a wave covers

@@ -798,7 +798,7 @@ struct Shape {                           // of a product's launch
 // Which tiles, and how the inner dimension is split: what is quickest by this reckoning, in us.  A round of tiles takes its stages, 1.55 each of
 // a 256 x 256 tile, one a compute unit, 1.2 of two of 128 x 128.  The tiles beyond whole rounds may be split so that their blocks fill the chip
 // once, into at most 32 shares (488 tokens of 128 x 17536 backward 61 us, with 16 66, with 64 69) of at least eight stages; then their sums are written and read at 2.5 TB/s, with a launch of 5.  Against measured
-// times (bf16, silu, forward with the projections stored), large tiles | small ones: 300 tokens of 2048 x 5632 40 | 38, reckoned 38 | 38; 512 of 4096 x 11008 108 | 133, 99 | 124;
+// times (bf16, silu, forward with the projections stored), large tiles | small ones: 300 tokens of 2048 x 5632 40 | 38, reckoned 38 | 38; 512 of 4096 x 11008 108 (by now 99) | 133, 99 | 124;
 // 2000 of 4096 x 512 43 | 35, 44 | 36; 4000 of 1024 x 4096 77 | 109, 50 | 77 (it leaves out the stores of the result, alike in both).
 // rows and columns: of the result (of WEIGHT_GRAD of one part, of FORWARD of both parts)
 Shape shape_of(int mode, int64_t rows, int64_t cols, int64_t inner) {
