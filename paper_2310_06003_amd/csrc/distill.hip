@@ -208,15 +208,16 @@ __global__ __launch_bounds__(THREADS, HELD == 16 ? 4 : HELD == 8 && !LOSS ? 7 : 
     }
 
     // p, and this row's loss.  p is divided by its sum itself, not in the exponent, where the sum's logarithm would be rounded at its size.
-    const float top_norm = __log2f(top.s) * LN2, share = 1.0f / top.s;
+    // loss = T sum p (T log p - T log q) in logits, undivided: a named word that the student masks with the lowest number is not infinite at T < 1.
+    const float share = 1.0f / top.s, norms = (norm - __log2f(top.s)) * LN2 * d.temperature;
     float sum = 0.0f;
 #pragma unroll
     for (int o = 0; o < OWN; ++o) {
         const int j = o * THREADS + tid;
         if (j < k) {
-            const float below = s_p[j] - top.m, lp = below * inverse_t - top_norm, p = s_id[j] >= 0 ? exp2_fast(below * c) * share : 0.0f;
+            const float below = s_p[j] - top.m, p = s_id[j] >= 0 ? exp2_fast(below * c) * share : 0.0f;
             s_p[j] = p;
-            if (LOSS && p != 0.0f) sum += p * (lp - ((at_id[o] - most) * inverse_t - norm * LN2));
+            if (LOSS && p != 0.0f) sum += p * (below - (at_id[o] - most) + norms);
         }
     }
     if constexpr (LOSS) {
@@ -227,7 +228,7 @@ __global__ __launch_bounds__(THREADS, HELD == 16 ? 4 : HELD == 8 && !LOSS ? 7 : 
         if (tid == 0) {
             float all = 0.0f;
             for (int w = 0; w < THREADS / 64; ++w) all += s_loss[w];
-            loss[row] = all * d.temperature * d.temperature;
+            loss[row] = all * d.temperature;
         }
     } else {
         __syncthreads();

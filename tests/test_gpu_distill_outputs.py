@@ -62,3 +62,31 @@ def test_many_entries_in_short_rows(paro, dtype, v, k):
     """More entries than the few threads of a short row would have taken: more threads."""
     z, t, ids = some_inputs(3, v, k, v + k)
     run_all(paro, z, t, ids, 2.0, dtype, "f32", pad=v % 3)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16", "f32"])
+@pytest.mark.parametrize("T", [0.05, 0.25, 0.5, 1.0, 2.0])
+@pytest.mark.parametrize("v", [40, 5000, 140003])
+def test_loss_of_a_named_word_at_the_lowest_number(paro, v, T, dtype):
+    """The student masks a word that the teacher names with the lowest number of a type: the loss, about T p times that, mostly is a number of fp32,
+    although the logit by T may be none.  Where it is beyond them it is infinite."""
+    n, k = 6, 5
+    z, t, ids = torch.randn(n, v, generator=rng(v)), torch.randn(n, k, generator=rng(v + 1)) * T, torch.stack([torch.randperm(v, generator=rng(i))[:k] for i in range(n)])
+    for row in range(1, n):
+        z[row, ids[row, row - 1]] = torch.finfo(TORCH[dtype]).min
+    t[:, 0] += 2 * T                        # the others' shares are small
+    z[1, ids[1, 0]], z[1, ids[1, 1]] = z[0, 0], torch.finfo(TORCH[dtype]).min
+    d = paro.make_distill(n=n, vocab=v, k=k, temperature=T, dtype=code(paro, dtype), teacher_dtype=paro.PARO_F32)
+    zd, td, idd = z.to(DEV, TORCH[dtype]), t.to(DEV), ids.int().to(DEV)
+    loss, step, dz = torch.empty(n, device=DEV), torch.empty(n, device=DEV), torch.empty(n, v, dtype=TORCH[dtype], device=DEV)
+    paro.paro_distill_loss(d, zd.data_ptr(), td.data_ptr(), idd.data_ptr(), loss.data_ptr(), 0, stream())
+    paro.paro_distill_step(d, zd.data_ptr(), td.data_ptr(), idd.data_ptr(), 0, step.data_ptr(), dz.data_ptr(), stream())
+    assert torch.equal(loss, step)
+    T64 = float(torch.tensor(T, dtype=torch.float32))
+    log_p, log_q = torch.log_softmax(t.double() / T64, dim=1), torch.log_softmax(z.to(TORCH[dtype]).double() / T64, dim=1).gather(1, ids)
+    terms = log_p.exp() * (log_p - log_q)
+    ref, size = T64 * T64 * terms.sum(dim=1), T64 * T64 * (log_p.exp() * (log_p.abs() + log_q.abs() + 2)).sum(dim=1)
+    ref = ref.float().double()
+    # as in the tests of the operator: an exponent carries its own size in roundings
+    got = loss.cpu().double()
+    assert bool(((got == ref) | ((got - ref).abs() <= 2.0 ** -20 * size * (1 + log_p.abs().amax(dim=1) / 2)) & ref.isfinite()).all()), (loss, ref)
