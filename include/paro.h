@@ -405,6 +405,48 @@ int paro_gated_grad(const paro_gated_t *d, const void *dh, const void *gate, con
                     const void *w_gate, const void *w_up, void *dx, void *dw_gate, void *dw_up, void *workspace,
                     int64_t workspace_bytes, void *stream);
 
+/* Attention over sequences of queries and keys, with a sliding window, sinks (first tokens that stay visible) and a relative position bias
+ * by buckets that is learned.  The last query of a sequence stands where its last key stands: of nq queries and nk keys, query i has the place
+ * p = nk - nq + i, and sees key j where
+ *   0 <= j <= p  and  (window == 0  or  p - j < window  or  j < sinks);
+ *   s_ij = scale q_i . k_j + table[bucket(p - j)][head],  out_i = sum_j softmax(s_i)_j v_j
+ * (training and prompts: as many queries as keys; new tokens over a cache: fewer).  A query that sees no key (more queries than keys, or none) gets zeros.  Head h
+ * reads key head h / (heads / kv_heads).  dtype: PARO_BF16 or PARO_F16.
+ * Rows: an array's token t, head h begins at element t * ld + h * head (0: heads side by side; tokens dense).  Sequence b has the queries
+ *   [b len_q, (b + 1) len_q), or [q_starts[b], q_starts[b + 1]) where q_starts is not NULL, and the keys from row b len_k, or k_starts[b], on:
+ *   len_k, or k_lens[b], or (k_starts and no k_lens) k_starts[b + 1] - k_starts[b].
+ * These are DEVICE int32 arrays of batch (+ 1 where a difference is taken) numbers; no sequence is longer than len_q and len_k, nor reaches past rows_q and rows_k
+ * (0: batch * len), and what such an array says beyond that is cut off.  q and out, k and v have the same rows.  Rows of no sequence are neither read nor written, nor are
+ * keys read that lie between the sinks and the first window of 128 queries; what is not finite there is of no account.
+ * Bias: bucket(d) is the last b with first[b] <= d, first: DEVICE int32 [buckets], ascending from 0 (paro_rel_buckets); table: [buckets][heads] of table_dtype, dtype or
+ * PARO_F32.  A bias of -inf hides; a row of a type's lowest number is one like others.  buckets == 0: none, table and first are not looked at.
+ * stats: NULL, or fp32 [rows_q][heads][2] = the largest score and the log of the sum of exp(score - largest); -inf and 0 where no key is seen. */
+typedef struct {
+    int64_t batch, heads, kv_heads, head_dim;       /* kv_heads divides heads; head_dim <= 128 */
+    int64_t len_q, len_k;                           /* of the longest sequence */
+    int64_t rows_q, rows_k;                         /* of the arrays, 0 = batch * len */
+    int64_t ld_q, ld_k, ld_v, ld_out;               /* elements from token to token, 0 = dense */
+    int64_t head_q, head_k, head_v, head_out;       /* from head to head, 0 = head_dim */
+    int64_t window, sinks;
+    float scale;
+    int32_t dtype, buckets, table_dtype;
+} paro_attn_t;
+int64_t paro_attn_workspace(const paro_attn_t *d, int grad); /* bytes: of paro_attn, or of paro_attn_grad; 0: may be NULL */
+int paro_attn(const paro_attn_t *d, const void *q, const void *k, const void *v, const int32_t *q_starts, const int32_t *k_starts,
+              const int32_t *k_lens, const void *table, const int32_t *first, void *out, float *stats, void *workspace,
+              int64_t workspace_bytes, void *stream);
+/* From dout (as out) and what paro_attn left, with P = softmax and dS_ij = P_ij (dout_i . v_j - dout_i . out_i):
+ *   dv_j = sum P_ij dout_i,  dk_j = scale sum dS_ij q_i  (over queries and the heads that share them; as v, k),  dq_i = scale sum_j dS_ij k_j  (as q),
+ *   dtable[b][head] = sum of dS_ij over bucket(p - j) = b  (as table; NULL = not wanted).
+ * P and dS are rounded to dtype for the products (of dtable they are not), fp16 scaled by powers of two such that nothing overflows.  Sequences do not
+ * share rows.  Rows of a sequence are all written, others stay as they are. */
+int paro_attn_grad(const paro_attn_t *d, const void *dout, const void *q, const void *k, const void *v, const void *out, const float *stats,
+                   const int32_t *q_starts, const int32_t *k_starts, const int32_t *k_lens, const void *table, const int32_t *first,
+                   void *dq, void *dk, void *dv, void *dtable, void *workspace, int64_t workspace_bytes, void *stream);
+/* Host only: first[b] for b < buckets in [1, 256]: the first half of the buckets ((buckets + 1) / 2) hold one distance each, the others grow by
+ * a ratio, so that the last would end at max_distance: first[h + k] = ceil(h (max_distance / h)^(k / (buckets - h))).  max_distance >= h, < 2^30. */
+int paro_rel_buckets(int buckets, int64_t max_distance, int32_t *first);
+
 /* text of the calling thread's last error ("" if none); valid until that
  * thread's next failing call */
 const char *paro_last_error(void);

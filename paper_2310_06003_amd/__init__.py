@@ -88,6 +88,12 @@ class paro_gated_t(Structure):
                 ("act", c_int32)]
 
 
+class paro_attn_t(Structure):
+    _fields_ = [(k, c_int64) for k in ("batch", "heads", "kv_heads", "head_dim", "len_q", "len_k", "rows_q", "rows_k", "ld_q", "ld_k", "ld_v",
+                                       "ld_out", "head_q", "head_k", "head_v", "head_out", "window", "sinks")] + \
+               [("scale", c_float), ("dtype", c_int32), ("buckets", c_int32), ("table_dtype", c_int32)]
+
+
 EXPORTS = {
     "paro_strategy_legal": (c_int, [c_char_p]),
     "paro_plan": (c_int, [c_int, c_int, c_char_p, POINTER(c_int64), c_int64, POINTER(paro_plan_opts_t),
@@ -128,6 +134,10 @@ EXPORTS = {
     "paro_gated_workspace": (c_int64, [POINTER(paro_gated_t), c_int]),
     "paro_gated": (c_int, [POINTER(paro_gated_t)] + [c_void_p] * 7 + [c_int64, c_void_p]),
     "paro_gated_grad": (c_int, [POINTER(paro_gated_t)] + [c_void_p] * 10 + [c_int64, c_void_p]),
+    "paro_attn_workspace": (c_int64, [POINTER(paro_attn_t), c_int]),
+    "paro_attn": (c_int, [POINTER(paro_attn_t)] + [c_void_p] * 11 + [c_int64, c_void_p]),
+    "paro_attn_grad": (c_int, [POINTER(paro_attn_t)] + [c_void_p] * 16 + [c_int64, c_void_p]),
+    "paro_rel_buckets": (c_int, [c_int, c_int64, POINTER(c_int32)]),
     "paro_last_error": (c_char_p, []),
 }
 for _name, (_res, _args) in EXPORTS.items():
@@ -359,6 +369,37 @@ def paro_gated(d: paro_gated_t, x: int, w_gate: int, w_up: int, h: int, gate: in
 def paro_gated_grad(d: paro_gated_t, dh: int, gate: int, up: int, x: int, w_gate: int, w_up: int, dx: int, dw_gate: int, dw_up: int,
                     workspace: int, workspace_bytes: int, stream: int = 0) -> None:
     _check(_lib.paro_gated_grad(byref(d), dh, gate, up, x, w_gate, w_up, dx, dw_gate, dw_up, workspace, workspace_bytes, stream))
+
+
+def make_attn(*, batch, heads, head_dim, len_q, dtype, kv_heads=0, len_k=-1, rows_q=0, rows_k=0, ld_q=0, ld_k=0, ld_v=0, ld_out=0, head_q=0, head_k=0,
+              head_v=0, head_out=0, window=0, sinks=0, scale=0.0, buckets=0, table_dtype=PARO_F32) -> paro_attn_t:
+    """kv_heads 0: as many as heads; len_k -1: as len_q; scale 0: 1 / sqrt(head_dim)."""
+    return paro_attn_t(batch, heads, kv_heads or heads, head_dim, len_q, len_q if len_k == -1 else len_k, rows_q, rows_k, ld_q, ld_k, ld_v, ld_out,
+                       head_q, head_k, head_v, head_out, window, sinks, scale or max(head_dim, 1) ** -0.5, dtype, buckets, table_dtype)
+
+
+def paro_attn_workspace(d: paro_attn_t, grad: bool) -> int:
+    """Bytes."""
+    rc = _lib.paro_attn_workspace(byref(d), 1 if grad else 0)
+    return rc if rc >= 0 else _check(rc)
+
+
+def paro_attn(d: paro_attn_t, q: int, k: int, v: int, q_starts: int, k_starts: int, k_lens: int, table: int, first: int, out: int, stats: int,
+              workspace: int, workspace_bytes: int, stream: int = 0) -> None:
+    _check(_lib.paro_attn(byref(d), q, k, v, q_starts, k_starts, k_lens, table, first, out, stats, workspace, workspace_bytes, stream))
+
+
+def paro_attn_grad(d: paro_attn_t, dout: int, q: int, k: int, v: int, out: int, stats: int, q_starts: int, k_starts: int, k_lens: int, table: int,
+                   first: int, dq: int, dk: int, dv: int, dtable: int, workspace: int, workspace_bytes: int, stream: int = 0) -> None:
+    _check(_lib.paro_attn_grad(byref(d), dout, q, k, v, out, stats, q_starts, k_starts, k_lens, table, first, dq, dk, dv, dtable, workspace,
+                               workspace_bytes, stream))
+
+
+def paro_rel_buckets(buckets: int, max_distance: int) -> List[int]:
+    """The first distance of each bucket."""
+    first = (c_int32 * max(1, min(buckets, 256)))()
+    _check(_lib.paro_rel_buckets(buckets, max_distance, first))
+    return list(first)
 
 
 # The device calls and make_adam, which a training program makes every step, take their usual arguments through

@@ -11,11 +11,11 @@ from concurrent.futures import ThreadPoolExecutor
 HERE = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(HERE)
 SO = os.path.join(HERE, "libparo.so")
-SOURCES = [os.path.join(HERE, "csrc", f) for f in ("plan.cpp", "kernels.hip", "embed.hip", "distill.hip", "gated.hip")]
+SOURCES = [os.path.join(HERE, "csrc", f) for f in ("plan.cpp", "kernels.hip", "embed.hip", "distill.hip", "gated.hip", "attn.hip", "attn_grad.hip")]
 # the extension reads CPython's own structures: its name carries the interpreter that it was built for, so that no other loads it
 MARSHAL_SO = os.path.join(HERE, "_marshal" + sysconfig.get_config_var("EXT_SUFFIX"))
 MARSHAL_SOURCE = os.path.join(HERE, "csrc", "marshal.cpp")
-HEADERS = [os.path.join(HERE, "csrc", h) for h in ("plan.hpp", "device_util.hpp", "loaders.hpp", "operators.hpp")] + \
+HEADERS = [os.path.join(HERE, "csrc", h) for h in ("plan.hpp", "device_util.hpp", "loaders.hpp", "operators.hpp", "attn.hpp")] + \
           [os.path.join(ROOT, "include", "paro.h")]
 
 # -ffp-contract=off: every fp32 operation of the fold and of Adam is rounded on its own, so

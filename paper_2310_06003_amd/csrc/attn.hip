@@ -1,0 +1,534 @@
+// Attention with a sliding window, sinks and a relative position bias by buckets, forward (gfx950):
+//
+//   s_ij = scale q_i . k_j + table[bucket(p_i - j)][head],  out_i = sum_j softmax(s_i)_j v_j   over the keys j that query i sees
+//
+// in one pass over the keys: a row keeps its largest score m, l = sum exp(s - m) and the sum of exp(s - m) v in fp32; where m grows by more than a factor of
+// 2^8 in exp(m), l and the sum are scaled down (until then exp(s - m) is above one, which costs nothing).  The products run on the matrix cores
+// with the scores transposed: a lane has a query's scores of 16 keys of 32, rounded to 16 bits they are the operand of the second product as they
+// stand, and maximum and sum of a row need one exchange between the two halves of a wave.  fp16 shares are multiplied by 2^7 (divided out at the end), so that
+// those below 2^-14 of the largest keep their bits.
+#include "attn.hpp"
+
+namespace {
+
+constexpr int QUERIES = 128, KEYS = 64;      // of a block, of a tile
+constexpr float GROWS = 8.0f;                // powers of two that a row's shares may exceed one by
+template <int DT>
+constexpr float SHIFT = DT == PARO_F16 ? 7.0f : 0.0f;
+
+template <int DT, int HD, bool BIAS>
+__global__ __launch_bounds__(256, 2) void k_attend(Attn a) {
+    using T = Tile<HD>;
+    constexpr int BYTES = KEYS * T::ROW, PASSES = KEYS * T::PIECES / 256, STEPS = HD / 16;
+    __shared__ __attribute__((aligned(1024))) char tiles[2][2][BYTES];       // [buffer][keys, values]
+    __shared__ Bias bias;
+    __shared__ float by_distance[2][QUERIES + KEYS];
+    const unsigned work = in_runs(blockIdx.x, gridDim.x), of_head = work / a.tiles;
+    const int head = of_head % a.heads, b = of_head / a.heads, i0 = (int)(a.tiles - 1 - work % a.tiles) * QUERIES;     // the longest first
+    const Sequence seq(a, b);
+    if (i0 >= seq.nq) return;
+    const int lane = threadIdx.x & 63, w = wave_of(), h = lane >> 5;
+    const int off = seq.nk - seq.nq, first = i0 + off, last = (i0 + QUERIES < seq.nq ? i0 + QUERIES : seq.nq) - 1 + off;
+    const Seen<KEYS> seen(a, first, last);
+    const int of_wave = first + w * 32, place = of_wave + (lane & 31), i = i0 + w * 32 + (lane & 31);     // of the lane's query
+    const int kv = head / (a.heads / a.kv_heads);
+
+    // Each thread stages pieces of the same column.
+    const int piece = threadIdx.x % T::PIECES, row = threadIdx.x / T::PIECES;
+    constexpr int APART = 256 / T::PIECES;
+    u32x4 from_k[PASSES], from_v[PASSES];
+    const auto load = [&](int t) {
+        const int k0 = seen.tile(t) * KEYS;
+#pragma unroll
+        for (int n = 0; n < PASSES; ++n) {
+            const int j = k0 + row + n * APART;
+            from_k[n] = from_v[n] = u32x4{0, 0, 0, 0};
+            if (seen.holds(j)) {
+                from_k[n] = piece_of_head(a.k.of((int64_t)seq.k0 + j, kv), piece * 8, a.hd);
+                from_v[n] = piece_of_head(a.v.of((int64_t)seq.k0 + j, kv), piece * 8, a.hd);
+            }
+        }
+    };
+    int far_from = 0;                       // distances from here on have the last bucket's bias
+    float far_bias = 0.0f;
+    const auto is_far = [&](int k0) { return BIAS && first - (k0 + KEYS - 1) >= far_from; };
+    const auto stage = [&](int t, int buffer) {
+#pragma unroll
+        for (int n = 0; n < PASSES; ++n) {
+            const int at = T::at(row + n * APART, piece);
+            *reinterpret_cast<u32x4 *>(tiles[buffer][0] + at) = from_k[n];
+            *reinterpret_cast<u32x4 *>(tiles[buffer][1] + at) = from_v[n];
+        }
+        if constexpr (BIAS) {
+            const int k0 = seen.tile(t) * KEYS;
+            if (!is_far(k0) && threadIdx.x < QUERIES + KEYS - 1) by_distance[buffer][threadIdx.x] = bias.of(first - k0 + QUERIES - 1 - (int)threadIdx.x, a.buckets);
+        }
+    };
+
+    if (seen.tiles) load(0);
+    if constexpr (BIAS) {
+        bias.load(a, head);
+        __syncthreads();
+        far_from = bias.first[a.buckets - 1];
+        far_bias = bias.column[a.buckets - 1];
+    }
+    short8_t q[STEPS];
+#pragma unroll
+    for (int s = 0; s < STEPS; ++s) {
+        u32x4 v{0, 0, 0, 0};
+        if (i < seq.nq) v = piece_of_head(a.q.of((int64_t)seq.q0 + i, head), s * 16 + h * 8, a.hd);
+        q[s] = __builtin_bit_cast(short8_t, v);
+    }
+    // Scores are kept as they are without a bias (units of `unit` powers of two), and scaled, in natural units, with one: a table may hold a type's lowest
+    // number, whose multiple by LOG2E does not exist.
+    const float unit = BIAS ? LOG2E : a.scale * LOG2E, grows = GROWS / unit;
+    f32x16 out[HD / 32] = {};
+    float most = -INFINITY, used = -INFINITY, sum = 0.0f;
+    if (seen.tiles) stage(0, 0);
+    for (int t = 0; t < seen.tiles; ++t) {
+        const int k0 = seen.tile(t) * KEYS, buffer = t & 1;
+        if (t + 1 < seen.tiles) load(t + 1);
+        __syncthreads();
+        const char *const keys = tiles[buffer][0], *const values = tiles[buffer][1];
+        // what this wave's queries see of the tile: nothing, all, or some
+        const bool none = k0 > of_wave + 31 || (k0 + KEYS <= of_wave - a.window + 1 && k0 >= a.sinks);
+        if (!none) {
+            f32x16 s[2];
+#pragma unroll
+            for (int n = 0; n < 2; ++n) {
+                s[n] = f32x16{};
+#pragma unroll
+                for (int c = 0; c < STEPS; ++c) s[n] = mfma32<DT>(T::rows(keys, n * 32, c, lane), q[c], s[n]);
+            }
+            if constexpr (BIAS) {
+                const bool far = is_far(k0);
+                const float *const at = by_distance[buffer] + QUERIES - 1 - (w * 32 + (lane & 31)) + 4 * h;
+#pragma unroll
+                for (int n = 0; n < 2; ++n)
+#pragma unroll
+                    for (int e = 0; e < 16; ++e) s[n][e] = s[n][e] * a.scale + (far ? far_bias : at[n * 32 + 8 * (e / 4) + e % 4]);
+            }
+            const bool all = k0 + KEYS - 1 <= of_wave && (k0 > of_wave + 31 - a.window || k0 + KEYS <= a.sinks);
+            if (!all) {
+#pragma unroll
+                for (int n = 0; n < 2; ++n)
+#pragma unroll
+                    for (int e = 0; e < 16; ++e)
+                        if (!sees(place, k0 + n * 32 + 8 * (e / 4) + 4 * h + e % 4, a.window, a.sinks)) s[n][e] = -INFINITY;
+            }
+            float now = most;
+#pragma unroll
+            for (int n = 0; n < 2; ++n)
+#pragma unroll
+                for (int e = 0; e < 16; ++e) now = fmaxf(now, s[n][e]);
+            most = max_of_halves(now);
+            if (__any(most > used + grows || (used == -INFINITY && most > -INFINITY))) {
+                const float times = used == -INFINITY ? 0.0f : exp2_((used - most) * unit);
+                used = most;
+                sum *= times;
+#pragma unroll
+                for (int d = 0; d < HD / 32; ++d) out[d] *= times;
+            }
+            const float from = used == -INFINITY ? 0.0f : used, shift = SHIFT<DT> - from * unit;
+#pragma unroll
+            for (int n = 0; n < 2; ++n)
+#pragma unroll
+                for (int e = 0; e < 16; ++e) {
+                    s[n][e] = exp2_(BIAS ? __builtin_fmaf(s[n][e] - from, unit, SHIFT<DT>) : __builtin_fmaf(s[n][e], unit, shift));
+                    sum += s[n][e];
+                }
+#pragma unroll
+            for (int n = 0; n < 2; ++n)
+#pragma unroll
+                for (int k = 0; k < 2; ++k) {
+                    const short8_t p = pack8<DT>(s[n], 8 * k);
+#pragma unroll
+                    for (int d = 0; d < HD / 32; ++d) out[d] = mfma32<DT>(T::columns(values, n * 32 + k * 16, d, lane), p, out[d]);
+                }
+        }
+        if (t + 1 < seen.tiles) stage(t + 1, buffer ^ 1);
+    }
+    sum = sum_of_halves(sum);
+    const bool there = i < seq.nq;
+    const float times = sum > 0.0f ? 1.0f / sum : sum == 0.0f ? 0.0f : sum;       // NaN stays
+    char *const to = a.out.of((int64_t)seq.q0 + i, head);
+#pragma unroll
+    for (int d = 0; d < HD / 32; ++d) store_row32<DT>(to, d * 32, a.hd, out[d], times, there);
+    if (a.stats && there && h == 0) {
+        float *const at = a.stats + (((int64_t)seq.q0 + i) * a.heads + head) * 2;
+        const bool empty = most == -INFINITY;
+        at[0] = BIAS ? most : empty ? most : most * a.scale;
+        at[1] = empty ? 0.0f : (__builtin_amdgcn_logf(sum) - SHIFT<DT> + (used - most) * unit) * LN2;
+    }
+}
+
+// ---------------------------------------------------------------- few queries
+// Up to 16 queries a sequence: the keys and values are read once for all queries and heads that share them, and nothing else counts.  A block's waves take 32 keys
+// at a time in turn: keys straight into registers as operands, values through shared memory of the wave's own, to be transposed.  The rows of
+// the products are the heads of a group, query by query, ROWS in all.  Long sequences are shared out among blocks, whose sums k_attend_join adds.
+constexpr int FEW = 16, FEW_KEYS = 32, FEW_WAVES = 4;
+constexpr int MOST_SHARES = 256;
+
+struct Few {
+    int shares, row_tiles;
+    float *sums, *stats;              // of a share: [block][ROWS][HD], and [block][ROWS][2]: largest score in powers of two, sum
+};
+
+__device__ __forceinline__ float max_of_quads(float x) {
+    const auto both = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    return max_of_halves(fmaxf(__uint_as_float(both[0]), __uint_as_float(both[1])));
+}
+__device__ __forceinline__ float sum_of_quads(float x) {
+    const auto both = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    return sum_of_halves(__uint_as_float(both[0]) + __uint_as_float(both[1]));
+}
+
+// What is written of a finished row: largest score `most` (in units), sum of shares, the result's elements.
+template <int DT, bool BIAS>
+__device__ __forceinline__ void store_stats(const Attn &a, int64_t row, int head, float most, float sum) {
+    float *const at = a.stats + (row * a.heads + head) * 2;
+    const bool empty = most == -INFINITY;
+    at[0] = BIAS || empty ? most : most * a.scale;
+    at[1] = empty ? 0.0f : (__builtin_amdgcn_logf(sum) - SHIFT<DT>) * LN2;
+}
+
+template <int DT, int HD, bool BIAS, int NT>
+__global__ __launch_bounds__(64 * FEW_WAVES, NT == 1 ? 2 : 1) void k_attend_few(Attn a, Few f) {
+    using T = Tile<HD>;
+    constexpr int ROWS = 16 * NT, STEPS = HD / 32, PASSES = FEW_KEYS * T::PIECES / 64;
+    static_assert(FEW_WAVES * FEW_KEYS * T::ROW >= ROWS * HD * 4, "the waves' sums take the place of the values");
+    __shared__ __attribute__((aligned(1024))) char values[FEW_WAVES][FEW_KEYS * T::ROW];
+    __shared__ float of_waves[FEW_WAVES][ROWS][2];
+    __shared__ int first_of[MAX_BUCKETS];
+    const int lane = threadIdx.x & 63, w = wave_of(), g = lane >> 4, of16 = lane & 15;
+    const int share = blockIdx.x % f.shares, row_tile = blockIdx.x / f.shares % f.row_tiles;
+    const int of_kv = blockIdx.x / f.shares / f.row_tiles, kv = of_kv % a.kv_heads, b = of_kv / a.kv_heads;
+    const int group = a.heads / a.kv_heads, rows_before = row_tile * ROWS;
+    const Sequence seq(a, b);
+    const int off = seq.nk - seq.nq, rows = seq.nq * group;
+    if (rows_before >= rows) return;
+    const Seen<FEW_KEYS> seen(a, off, seq.nk - 1);
+    const int from = (int)((int64_t)seen.tiles * share / f.shares), to = (int)((int64_t)seen.tiles * (share + 1) / f.shares);
+
+    int place[NT], head[NT];
+    bool there[NT];
+    short8_t q[NT][STEPS];
+#pragma unroll
+    for (int n = 0; n < NT; ++n) {
+        const int r = rows_before + n * 16 + of16;
+        there[n] = r < rows;
+        place[n] = off + r / group;
+        head[n] = kv * group + r % group;
+#pragma unroll
+        for (int s = 0; s < STEPS; ++s) {
+            u32x4 v{0, 0, 0, 0};
+            if (there[n]) v = piece_of_head(a.q.of((int64_t)seq.q0 + r / group, head[n]), s * 32 + g * 8, a.hd);
+            q[n][s] = __builtin_bit_cast(short8_t, v);
+        }
+    }
+    u32x4 from_k[2][STEPS], from_v[PASSES];
+    const int piece = lane % T::PIECES, of_pass = lane / T::PIECES;
+    constexpr int APART = 64 / T::PIECES;
+    const auto load = [&](int t) {
+        const int k0 = seen.tile(t) * FEW_KEYS;
+#pragma unroll
+        for (int n = 0; n < 2; ++n) {
+            const int j = k0 + n * 16 + of16;
+            const bool held = seen.holds(j);
+            const char *const key = a.k.of((int64_t)seq.k0 + j, kv);
+#pragma unroll
+            for (int s = 0; s < STEPS; ++s) {
+                from_k[n][s] = u32x4{0, 0, 0, 0};
+                if (held) from_k[n][s] = piece_of_head(key, s * 32 + g * 8, a.hd);
+            }
+        }
+#pragma unroll
+        for (int n = 0; n < PASSES; ++n) {
+            const int j = k0 + of_pass + n * APART;
+            from_v[n] = u32x4{0, 0, 0, 0};
+            if (seen.holds(j)) from_v[n] = piece_of_head(a.v.of((int64_t)seq.k0 + j, kv), piece * 8, a.hd);
+        }
+    };
+    int far_from = 0;
+    float far_bias[NT] = {};
+    if (from + w < to) load(from + w);
+    if constexpr (BIAS) {
+        for (int i = threadIdx.x; i < a.buckets; i += 64 * FEW_WAVES) first_of[i] = a.first[i];
+#pragma unroll
+        for (int n = 0; n < NT; ++n)
+            if (there[n]) far_bias[n] = table_value(a, a.buckets - 1, head[n]);
+        __syncthreads();
+        far_from = first_of[a.buckets - 1];
+    }
+    const float unit = BIAS ? LOG2E : a.scale * LOG2E;
+    f32x4 out[NT][HD / 16] = {};
+    float most[NT], sum[NT];
+#pragma unroll
+    for (int n = 0; n < NT; ++n) {
+        most[n] = -INFINITY;
+        sum[n] = 0.0f;
+    }
+    char *const mine = values[w];
+    for (int t = from + w; t < to; t += FEW_WAVES) {
+        const int k0 = seen.tile(t) * FEW_KEYS;
+        short8_t keys[2][STEPS];
+#pragma unroll
+        for (int n = 0; n < 2; ++n)
+#pragma unroll
+            for (int s = 0; s < STEPS; ++s) keys[n][s] = __builtin_bit_cast(short8_t, from_k[n][s]);
+        asm volatile("" ::: "memory");                  // the last tile's values have been read
+#pragma unroll
+        for (int n = 0; n < PASSES; ++n) *reinterpret_cast<u32x4 *>(mine + T::at(of_pass + n * APART, piece)) = from_v[n];
+        asm volatile("" ::: "memory");                  // a wave's accesses of shared memory go in their order
+        if (t + FEW_WAVES < to) load(t + FEW_WAVES);
+        f32x4 s[NT][2];
+#pragma unroll
+        for (int n = 0; n < NT; ++n)
+#pragma unroll
+            for (int k = 0; k < 2; ++k) {
+                s[n][k] = f32x4{};
+#pragma unroll
+                for (int c = 0; c < STEPS; ++c) s[n][k] = mfma16<DT>(keys[k][c], q[n][c], s[n][k]);
+            }
+        if constexpr (BIAS) {
+            const bool far = off - (k0 + FEW_KEYS - 1) >= far_from;
+            // distances off - (k0 + 31) + lane: up to 16 queries' places, 32 keys
+            const int lowest = off - (k0 + FEW_KEYS - 1);
+            int bucket = 0;
+            if (!far) {
+                const int d = lowest + lane < 0 ? 0 : lowest + lane;
+                int some = a.buckets;
+                while (some > 1) {
+                    const int half = some >> 1;
+                    const bool up = first_of[bucket + half] <= d;
+                    bucket = up ? bucket + half : bucket;
+                    some = up ? some - half : half;
+                }
+            }
+#pragma unroll
+            for (int n = 0; n < NT; ++n)
+#pragma unroll
+                for (int k = 0; k < 2; ++k)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        float value = far_bias[n];
+                        if (!far) {
+                            const int of = __shfl(bucket, (place[n] - (k0 + k * 16 + 4 * g + e) - lowest) & 63);
+                            value = there[n] ? table_value(a, of, head[n]) : 0.0f;
+                        }
+                        s[n][k][e] = s[n][k][e] * a.scale + value;
+                    }
+        }
+#pragma unroll
+        for (int n = 0; n < NT; ++n) {
+            float now = most[n];
+#pragma unroll
+            for (int k = 0; k < 2; ++k)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const int j = k0 + k * 16 + 4 * g + e;
+                    if (j >= seq.nk || !sees(place[n], j, a.window, a.sinks)) s[n][k][e] = -INFINITY;
+                    now = fmaxf(now, s[n][k][e]);
+                }
+            now = max_of_quads(now);
+            const float was = most[n], base = now == -INFINITY ? 0.0f : now;
+            const float times = was == -INFINITY ? 0.0f : exp2_((was - base) * unit);
+            most[n] = now;
+            float added = 0.0f;
+            const float shift = SHIFT<DT> - base * unit;
+#pragma unroll
+            for (int k = 0; k < 2; ++k)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    s[n][k][e] = exp2_(BIAS ? __builtin_fmaf(s[n][k][e] - base, unit, SHIFT<DT>) : __builtin_fmaf(s[n][k][e], unit, shift));
+                    added += s[n][k][e];
+                }
+            sum[n] = sum[n] * times + added;
+            u32x4 packed;
+#pragma unroll
+            for (int k = 0; k < 2; ++k) {
+                packed[2 * k] = pack2<DT>(s[n][k][0], s[n][k][1]);
+                packed[2 * k + 1] = pack2<DT>(s[n][k][2], s[n][k][3]);
+            }
+            const short8_t p = __builtin_bit_cast(short8_t, packed);
+#pragma unroll
+            for (int d = 0; d < HD / 16; ++d) out[n][d] = mfma16<DT>(T::columns16(mine, d, lane), p, out[n][d] * times);
+        }
+    }
+    // The waves' sums, one after the other, relative to the block's largest score.
+#pragma unroll
+    for (int n = 0; n < NT; ++n) {
+        sum[n] = sum_of_quads(sum[n]);
+        if (g == 0) {
+            of_waves[w][n * 16 + of16][0] = most[n];
+            of_waves[w][n * 16 + of16][1] = sum[n];
+        }
+    }
+    __syncthreads();
+    float *const sums = reinterpret_cast<float *>(values[0]);            // [ROWS][HD]
+    float all_most[NT], all_sum[NT];
+#pragma unroll
+    for (int n = 0; n < NT; ++n) {
+        const int r = n * 16 + of16;
+        all_most[n] = -INFINITY;
+        all_sum[n] = 0.0f;
+        for (int v = 0; v < FEW_WAVES; ++v) all_most[n] = fmaxf(all_most[n], of_waves[v][r][0]);
+        const float base = all_most[n] == -INFINITY ? 0.0f : all_most[n];
+        for (int v = 0; v < FEW_WAVES; ++v) all_sum[n] += of_waves[v][r][1] * exp2_((of_waves[v][r][0] - base) * unit);
+        const float times = exp2_((most[n] - base) * unit);              // 0 where this wave saw nothing
+#pragma unroll
+        for (int d = 0; d < HD / 16; ++d) out[n][d] *= times;
+    }
+    for (int v = 0; v < FEW_WAVES; ++v) {
+        if (v == w) {
+#pragma unroll
+            for (int n = 0; n < NT; ++n)
+#pragma unroll
+                for (int d = 0; d < HD / 16; ++d) {
+                    f32x4 *const at = reinterpret_cast<f32x4 *>(sums + (n * 16 + of16) * HD + d * 16 + 4 * g);
+                    *at = v ? *at + out[n][d] : out[n][d];
+                }
+        }
+        __syncthreads();
+    }
+    if (f.shares > 1) {
+        float *const part = f.sums + (int64_t)blockIdx.x * (ROWS * HD);
+        for (int x = threadIdx.x; x < ROWS * HD / 4; x += 64 * FEW_WAVES) reinterpret_cast<f32x4 *>(part)[x] = reinterpret_cast<const f32x4 *>(sums)[x];
+        if (w == 0 && g == 0)
+#pragma unroll
+            for (int n = 0; n < NT; ++n) {
+                f.stats[((int64_t)blockIdx.x * ROWS + n * 16 + of16) * 2] = all_most[n];
+                f.stats[((int64_t)blockIdx.x * ROWS + n * 16 + of16) * 2 + 1] = all_sum[n];
+            }
+        return;
+    }
+    if (w == 0 && g == 0)
+#pragma unroll
+        for (int n = 0; n < NT; ++n) of_waves[0][n * 16 + of16][1] = all_sum[n];
+    __syncthreads();
+    for (int x = threadIdx.x; x < ROWS * T::PIECES; x += 64 * FEW_WAVES) {
+        const int r = x / T::PIECES, c = x % T::PIECES * 8, of_rows = rows_before + r;
+        if (of_rows >= rows || c >= a.hd) continue;
+        const float all = of_waves[0][r][1], times = all > 0.0f ? 1.0f / all : all;
+        float v[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[e] = sums[r * HD + c + e] * times;
+        store_piece_of_head(a.out.of((int64_t)seq.q0 + of_rows / group, kv * group + of_rows % group), c, a.hd, pack<DT>(v));
+    }
+    if (a.stats && w == 0 && g == 0)
+#pragma unroll
+        for (int n = 0; n < NT; ++n)
+            if (there[n]) store_stats<DT, BIAS>(a, (int64_t)seq.q0 + (rows_before + n * 16 + of16) / group, head[n], all_most[n], all_sum[n]);
+}
+
+// Adds the shares of a row, in order: a wave a row.
+template <int DT, int HD, bool BIAS, int NT>
+__global__ __launch_bounds__(256) void k_attend_join(Attn a, Few f) {
+    constexpr int ROWS = 16 * NT, EACH = HD / 64;
+    const int lane = threadIdx.x & 63;
+    const int64_t work = (int64_t)blockIdx.x * 4 + wave_of();                // [sequence, key head][row tile][row]
+    const int r = (int)(work % ROWS), row_tile = (int)(work / ROWS % f.row_tiles);
+    const int64_t of_kv = work / ROWS / f.row_tiles;
+    const int kv = (int)(of_kv % a.kv_heads), group = a.heads / a.kv_heads, of_rows = row_tile * ROWS + r;
+    if (of_kv / a.kv_heads >= a.batch) return;
+    const Sequence seq(a, (int)(of_kv / a.kv_heads));
+    if (of_rows >= seq.nq * group) return;
+    const float unit = BIAS ? LOG2E : a.scale * LOG2E;
+    const int64_t block = (of_kv * f.row_tiles + row_tile) * f.shares;
+    const float *const stats = f.stats + (block * ROWS + r) * 2, *const sums = f.sums + (block * ROWS + r) * HD + lane * EACH;
+    float most = -INFINITY, sum = 0.0f, out[EACH] = {};
+    for (int s = 0; s < f.shares; ++s) most = fmaxf(most, stats[(int64_t)s * ROWS * 2]);
+    const float base = most == -INFINITY ? 0.0f : most;
+#pragma unroll 8
+    for (int s = 0; s < f.shares; ++s) {
+        const float times = exp2_((stats[(int64_t)s * ROWS * 2] - base) * unit);
+        sum += stats[(int64_t)s * ROWS * 2 + 1] * times;
+#pragma unroll
+        for (int e = 0; e < EACH; ++e) out[e] += sums[(int64_t)s * ROWS * HD + e] * times;
+    }
+    const float times = sum > 0.0f ? 1.0f / sum : sum;
+    const int head = kv * group + of_rows % group;
+    const int64_t row = (int64_t)seq.q0 + of_rows / group;
+#pragma unroll
+    for (int e = 0; e < EACH; ++e)
+        if (lane * EACH + e < a.hd) store_one<DT>(a.out.of(row, head), lane * EACH + e, out[e] * times);
+    if (a.stats && lane == 0) store_stats<DT, BIAS>(a, row, head, most, sum);
+}
+
+// ---------------------------------------------------------------- host
+struct Plan {
+    bool few;
+    int tiles_of_rows, row_tiles, shares;            // few: 16-row tiles of a block, row tiles, shares
+    int64_t blocks, stats, bytes;
+};
+
+Plan plan_of(const paro_attn_t &d) {
+    Plan p{};
+    const int64_t group = d.heads / d.kv_heads;
+    p.few = d.len_q <= FEW;
+    if (!p.few) {
+        p.blocks = ceil_div(d.len_q, QUERIES) * d.heads * d.batch;
+        return p;
+    }
+    const int64_t rows = std::max<int64_t>(1, d.len_q * group), head_dim = d.head_dim <= 64 ? 64 : 128;
+    p.tiles_of_rows = rows <= 16 ? 1 : 2;
+    p.row_tiles = (int)ceil_div(rows, 16 * p.tiles_of_rows);
+    const int64_t whole = d.batch * d.kv_heads * p.row_tiles;
+    const int64_t span = d.window ? std::min<int64_t>(d.len_k, std::min<int64_t>(d.window, d.len_k) + d.len_q + std::min<int64_t>(d.sinks, d.len_k)) : d.len_k;
+    p.shares = (int)std::max<int64_t>(1, std::min<int64_t>(std::min<int64_t>(ceil_div(512, whole), ceil_div(span, 2 * FEW_WAVES * FEW_KEYS)), MOST_SHARES));
+    p.blocks = whole * p.shares;
+    if (p.shares > 1) {
+        p.stats = p.blocks * 16 * p.tiles_of_rows * head_dim * 4;
+        p.bytes = p.stats + p.blocks * 16 * p.tiles_of_rows * 8;
+    }
+    return p;
+}
+
+template <int DT, int HD, bool BIAS>
+void launch(const Attn &a, const Plan &p, char *workspace, hipStream_t st) {
+    if (!p.few) {
+        hipLaunchKernelGGL((k_attend<DT, HD, BIAS>), dim3((unsigned)p.blocks), dim3(256), 0, st, a);
+        return;
+    }
+    const Few f{p.shares, p.row_tiles, reinterpret_cast<float *>(workspace), reinterpret_cast<float *>(workspace + p.stats)};
+    const unsigned joins = (unsigned)(p.blocks / p.shares * 4 * p.tiles_of_rows);
+    if (p.tiles_of_rows == 1) {
+        hipLaunchKernelGGL((k_attend_few<DT, HD, BIAS, 1>), dim3((unsigned)p.blocks), dim3(64 * FEW_WAVES), 0, st, a, f);
+        if (p.shares > 1) hipLaunchKernelGGL((k_attend_join<DT, HD, BIAS, 1>), dim3(joins), dim3(256), 0, st, a, f);
+    } else {
+        hipLaunchKernelGGL((k_attend_few<DT, HD, BIAS, 2>), dim3((unsigned)p.blocks), dim3(64 * FEW_WAVES), 0, st, a, f);
+        if (p.shares > 1) hipLaunchKernelGGL((k_attend_join<DT, HD, BIAS, 2>), dim3(joins), dim3(256), 0, st, a, f);
+    }
+}
+
+}  // namespace
+
+int64_t paro::attn_forward_workspace(const paro_attn_t &d) { return plan_of(d).bytes; }
+
+extern "C" {
+
+int paro_attn(const paro_attn_t *d, const void *q, const void *k, const void *v, const int32_t *q_starts, const int32_t *k_starts, const int32_t *k_lens,
+              const void *table, const int32_t *first, void *out, float *stats, void *workspace, int64_t workspace_bytes, void *stream) {
+    return guarded([&]() -> int {
+        const std::string f = "paro_attn: ";
+        int rc;
+        if ((rc = check_attn(f, d)) || (rc = check_rows(f, *d, q_starts, k_starts)) || d->batch == 0 || d->len_q == 0) return rc;
+        if ((rc = check_inputs(f, *d, q, k, v, q_starts, k_starts, k_lens, table, first)) || (rc = check_array(out, 2, f + "out"))) return rc;
+        if (stats && (rc = check_array(stats, 4, f + "stats"))) return rc;
+        const Plan p = plan_of(*d);
+        if ((rc = check_room(f, p.bytes, workspace, workspace_bytes))) return rc;
+        Attn a = attn_of(*d, q, k, v, q_starts, k_starts, k_lens, table, first);
+        a.out.at = static_cast<char *>(out);
+        a.stats = stats;
+        a.tiles = (int)ceil_div(d->len_q, QUERIES);
+        hipStream_t st = static_cast<hipStream_t>(stream);
+        char *ws = static_cast<char *>(workspace);
+#define PARO_FORWARD(DT, HD, BIAS) launch<DT, HD, BIAS>(a, p, ws, st)
+        PARO_BY_FORM(PARO_FORWARD);
+#undef PARO_FORWARD
+        PARO_LAUNCHED("paro_attn");
+        return PARO_OK;
+    });
+}
+
+}  // extern "C"

@@ -1,0 +1,316 @@
+// What the attention's forward and backward kernels share (attn.hip, attn_grad.hip): where a sequence lies, which keys a tile of queries sees, tiles
+// of rows in shared memory and how the matrix instructions read them, the relative position bias.
+//
+// With off = keys - queries of a sequence, query i stands at place p = off + i and sees key j where 0 <= j <= p and (p - j < window or j < sinks).
+#pragma once
+
+#include <cmath>
+
+#include "operators.hpp"
+
+namespace {
+
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+typedef short short4_t __attribute__((ext_vector_type(4)));
+typedef short short8_t __attribute__((ext_vector_type(8)));
+typedef __bf16 bf16x8_t __attribute__((ext_vector_type(8)));
+typedef _Float16 f16x8_t __attribute__((ext_vector_type(8)));
+
+constexpr float LOG2E = 1.44269504088896340736f, LN2 = 0.69314718055994530942f;
+constexpr int MAX_BUCKETS = 256, MAX_HEAD = 128;
+constexpr int FAR_AWAY = 1 << 30;        // a window that holds every key: lengths are at most this
+
+template <int DT>
+__device__ __forceinline__ f32x16 mfma32(short8_t a, short8_t b, f32x16 c) {
+    if constexpr (DT == PARO_F16)
+        return __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(f16x8_t, a), __builtin_bit_cast(f16x8_t, b), c, 0, 0, 0);
+    else
+        return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8_t, a), __builtin_bit_cast(bf16x8_t, b), c, 0, 0, 0);
+}
+template <int DT>
+__device__ __forceinline__ f32x4 mfma16(short8_t a, short8_t b, f32x4 c) {
+    if constexpr (DT == PARO_F16)
+        return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8_t, a), __builtin_bit_cast(f16x8_t, b), c, 0, 0, 0);
+    else
+        return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, a), __builtin_bit_cast(bf16x8_t, b), c, 0, 0, 0);
+}
+__device__ __forceinline__ float exp2_(float x) { return __builtin_amdgcn_exp2f(x); }
+__device__ __forceinline__ int wave_of() { return __builtin_amdgcn_readfirstlane(threadIdx.x >> 6); }
+
+// A value of the lane 32 on (modulo 64) joined with a lane's own: both halves of a wave then have the same.
+__device__ __forceinline__ float max_of_halves(float x) {
+    const auto both = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    return fmaxf(__uint_as_float(both[0]), __uint_as_float(both[1]));
+}
+__device__ __forceinline__ float sum_of_halves(float x) {
+    const auto both = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    return __uint_as_float(both[0]) + __uint_as_float(both[1]);
+}
+
+// Blocks go to the eight XCDs in turn: each takes a run of the work of its own, so that the tiles of a head, which read the same keys, meet in its L2.
+__device__ __forceinline__ unsigned in_runs(unsigned block, unsigned all) {
+    const unsigned each = all / 8, more = all % 8, xcd = block % 8;
+    return xcd * each + (xcd < more ? xcd : more) + block / 8;
+}
+
+// Rows of an array of heads: elements from token to token, and from head to head.
+struct Rows {
+    char *at;
+    int64_t ld, head;
+    __device__ __forceinline__ char *of(int64_t row, int h) const { return at + (row * ld + h * head) * 2; }
+};
+
+struct Attn {
+    Rows q, k, v, out;
+    const int32_t *q_starts, *k_starts, *k_lens;
+    float *stats;
+    const void *table;
+    const int32_t *first;
+    int batch, heads, kv_heads, hd, len_q, len_k, rows_q, rows_k, window, sinks, buckets, table_dtype, tiles;
+    float scale;
+};
+
+// Where a sequence's rows lie.  Whatever the arrays on the device hold, the rows stay inside [0, rows_q) and [0, rows_k), and are no more than len_q and len_k.
+struct Sequence {
+    int q0, nq, k0, nk;
+    __device__ __forceinline__ Sequence(const Attn &a, int b) {
+        const auto inside = [](int64_t x, int64_t most) { return (int)(x < 0 ? 0 : x > most ? most : x); };
+        const int64_t qs = a.q_starts ? a.q_starts[b] : (int64_t)b * a.len_q, ks = a.k_starts ? a.k_starts[b] : (int64_t)b * a.len_k;
+        q0 = inside(qs, a.rows_q);
+        k0 = inside(ks, a.rows_k);
+        const int64_t q = a.q_starts ? a.q_starts[b + 1] - qs : a.len_q;
+        const int64_t k = a.k_lens ? a.k_lens[b] : a.k_starts ? a.k_starts[b + 1] - ks : a.len_k;
+        const int room_q = a.rows_q - q0, room_k = a.rows_k - k0;
+        nq = inside(q, a.len_q < room_q ? a.len_q : room_q);
+        nk = inside(k, a.len_k < room_k ? a.len_k : room_k);
+    }
+};
+
+// The tiles of KEYS keys that queries at the places [first, last] see: those with sinks, then those of the windows.  Keys that none of the queries sees are
+// not read (others': behind the end, between the sinks and the first window).
+template <int KEYS>
+struct Seen {
+    int end, low, sinks;              // keys [0, sinks) and [low, end)
+    int sink_tiles, first_tile, tiles;
+    __device__ __forceinline__ Seen(const Attn &a, int first, int last) {
+        end = last + 1 > 0 ? last + 1 : 0;
+        low = first - a.window + 1 > 0 ? first - a.window + 1 : 0;
+        if (low > end) low = end;
+        sinks = a.sinks < end ? a.sinks : end;
+        first_tile = low / KEYS;
+        const int of_sinks = (sinks + KEYS - 1) / KEYS;
+        sink_tiles = of_sinks < first_tile ? of_sinks : first_tile;
+        tiles = sink_tiles + (end + KEYS - 1) / KEYS - first_tile;
+        if (end == 0) tiles = 0;
+    }
+    __device__ __forceinline__ int tile(int t) const { return t < sink_tiles ? t : first_tile + t - sink_tiles; }
+    __device__ __forceinline__ bool holds(int j) const { return j < end && (j >= low || j < sinks); }
+};
+__device__ __forceinline__ bool sees(int p, int j, int window, int sinks) {
+    const int far = p - j;
+    return (unsigned)far < (unsigned)window || (far >= 0 && j < sinks);
+}
+
+// ---------------------------------------------------------------- tiles of rows in shared memory
+// HD (64 or 128) elements of 16 bits a row, whatever lies behind the head's own as zeros, in pieces of eight.  The pieces of a row are exchanged by its number such
+// that the lanes that read at a time meet all banks, both where they read the same piece of 16 rows and where they read 64 bytes of 4 rows (transposed).
+template <int HD>
+struct Tile {
+    static constexpr int ROW = HD * 2, PIECES = HD / 8;
+    static __device__ __forceinline__ int key(int row) {
+        if constexpr (HD == 128) return ((row & 3) << 2) | ((row >> 2) & 3);
+        else return ((row & 2) << 1) | ((row >> 2) & 3);
+    }
+    static __device__ __forceinline__ int at(int row, int piece) { return row * ROW + ((piece ^ key(row)) << 4); }
+
+    // Operand with 32 rows of the tile as its rows (or columns), step s of 16 elements: a lane has row lane % 32, elements 8 * (lane / 32) on.
+    static __device__ __forceinline__ short8_t rows(const char *tile, int row0, int s, int lane) {
+        return *reinterpret_cast<const short8_t *>(tile + row0 * ROW + at(lane & 31, 2 * s + (lane >> 5)));
+    }
+    // Operand with the elements [32 * d, 32 * d + 32) as its rows and 16 rows of the tile, row0 on, as its steps: lane / 32 = h has of these the rows
+    // 4h .. 4h + 3 and 8 + 4h .. 8 + 4h + 3, which is the order in which the result of a product has them.
+    static __device__ __forceinline__ short8_t columns(const char *tile, int row0, int d, int lane) {
+        const int h = lane >> 5, of16 = lane & 15, row = 4 * h + (of16 >> 2), piece = d * 4 + ((lane >> 4) & 1) * 2 + ((of16 & 3) >> 1);
+        const char *lo = tile + row0 * ROW + at(row, piece) + (of16 & 1) * 8, *hi = tile + row0 * ROW + at(row + 8, piece) + (of16 & 1) * 8;
+        return joined(lo, hi);
+    }
+    // The same for elements [16 * d, 16 * d + 16) and 32 rows of the tile: lane / 16 = g has the rows 4g .. 4g + 3 and 16 + 4g .. 16 + 4g + 3.
+    static __device__ __forceinline__ short8_t columns16(const char *tile, int d, int lane) {
+        const int g = lane >> 4, of16 = lane & 15, row = 4 * g + (of16 >> 2), piece = d * 2 + ((of16 & 3) >> 1);
+        const char *lo = tile + at(row, piece) + (of16 & 1) * 8;
+        return joined(lo, lo + 16 * ROW);               // rows 16 apart have the same key
+    }
+    static __device__ __forceinline__ short8_t joined(const char *lo, const char *hi) {
+        const short4_t a = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) short4_t *)lo);
+        const short4_t b = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) short4_t *)hi);
+        return __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7);
+    }
+};
+
+// Eight elements of a head's row, from `column` on; what lies behind the head: zeros.
+__device__ __forceinline__ u32x4 piece_of_head(const char *row, int column, int hd) {
+    if (column + 8 <= hd) return load_piece<PARO_BF16>(row, column);
+    u32x4 v{0, 0, 0, 0};
+#pragma unroll
+    for (int e = 0; e < 8; ++e)
+        if (column + e < hd) v[e / 2] |= (unsigned)reinterpret_cast<const unsigned short *>(row)[column + e] << (16 * (e & 1));
+    return v;
+}
+__device__ __forceinline__ void store_piece_of_head(char *row, int column, int hd, u32x4 v) {
+    if (column + 8 <= hd) {
+        store_piece<PARO_BF16>(row, column, v);
+        return;
+    }
+#pragma unroll
+    for (int e = 0; e < 8; ++e)
+        if (column + e < hd) reinterpret_cast<unsigned short *>(row)[column + e] = (unsigned short)(v[e / 2] >> (16 * (e & 1)));
+}
+// A row of 32 of the result of 32 x 32 products: a lane has of its row (lane % 32) the elements 8 * (i / 4) + 4 * (lane / 32) + i % 4.  Both halves of a
+// wave exchange, so that each stores eight in a row.
+template <int DT>
+__device__ __forceinline__ void store_row32(char *row, int column, int hd, const f32x16 &x, float times, bool there) {
+    const int h = (threadIdx.x >> 5) & 1;
+#pragma unroll
+    for (int i = 0; i < 16; i += 8) {
+        const unsigned a0 = pack2<DT>(x[i] * times, x[i + 1] * times), a1 = pack2<DT>(x[i + 2] * times, x[i + 3] * times);
+        const unsigned b0 = pack2<DT>(x[i + 4] * times, x[i + 5] * times), b1 = pack2<DT>(x[i + 6] * times, x[i + 7] * times);
+        const auto s0 = __builtin_amdgcn_permlane32_swap(a0, b0, false, false), s1 = __builtin_amdgcn_permlane32_swap(a1, b1, false, false);
+        if (there) store_piece_of_head(row, column + 2 * i + 8 * h, hd, u32x4{s0[0], s1[0], s0[1], s1[1]});
+    }
+}
+template <int DT>
+__device__ __forceinline__ short8_t pack8(const f32x16 &x, int from) {
+    u32x4 v;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) v[i] = pack2<DT>(x[from + 2 * i], x[from + 2 * i + 1]);
+    return __builtin_bit_cast(short8_t, v);
+}
+
+// ---------------------------------------------------------------- the bias
+__device__ __forceinline__ float table_value(const Attn &a, int bucket, int head) {
+    const int64_t at = (int64_t)bucket * a.heads + head;
+    return a.table_dtype == PARO_F32 ? static_cast<const float *>(a.table)[at] : bits16_to_f32(a.table_dtype, static_cast<const unsigned short *>(a.table)[at]);
+}
+// A head's column of the table and the first distances in shared memory, and the values by distance that a tile needs.
+struct Bias {
+    int first[MAX_BUCKETS];
+    float column[MAX_BUCKETS];
+
+    __device__ __forceinline__ void load(const Attn &a, int head) {         // then a barrier
+        for (int b = threadIdx.x; b < a.buckets; b += blockDim.x) {
+            first[b] = a.first[b];
+            column[b] = table_value(a, b, head);
+        }
+    }
+    // The last bucket that begins at `far` or before; the first where none does.
+    __device__ __forceinline__ int bucket(int far, int buckets) const {
+        int lo = 0, n = buckets;
+        while (n > 1) {                                                     // the answer lies in [lo, lo + n)
+            const int half = n >> 1;
+            const bool up = first[lo + half] <= far;
+            lo = up ? lo + half : lo;
+            n = up ? n - half : half;
+        }
+        return lo;
+    }
+    __device__ __forceinline__ float of(int far, int buckets) const { return column[bucket(far < 0 ? 0 : far, buckets)]; }
+};
+
+// ---------------------------------------------------------------- host
+inline int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
+
+inline int check_attn(const std::string &f, const paro_attn_t *d) {
+    if (!d) return fail(PARO_EINVAL, f + "d is NULL");
+    const auto bad = [&](const char *text) { return fail(PARO_EINVAL, f + text); };
+    if (d->dtype != PARO_BF16 && d->dtype != PARO_F16) return bad("dtype must be PARO_BF16 or PARO_F16");
+    if (d->batch < 0 || d->batch > (1 << 20)) return bad("batch must be in [0, 2^20]");
+    if (d->heads < 1 || d->heads > 1024 || d->kv_heads < 1 || d->heads % d->kv_heads) return bad("heads must be in [1, 1024] and a multiple of kv_heads");
+    if (d->head_dim < 1 || d->head_dim > MAX_HEAD) return bad("head_dim must be in [1, 128]");
+    if (d->len_q < 0 || d->len_q > FAR_AWAY || d->len_k < 0 || d->len_k > FAR_AWAY) return bad("len_q and len_k must be in [0, 2^30]");
+    if (d->rows_q < 0 || d->rows_q > INT32_MAX || d->rows_k < 0 || d->rows_k > INT32_MAX) return bad("rows_q and rows_k must be in [0, 2^31)");
+    if (d->batch * d->len_q > INT32_MAX && !d->rows_q) return bad("more than 2^31 - 1 rows of queries");
+    if (d->batch * d->len_k > INT32_MAX && !d->rows_k) return bad("more than 2^31 - 1 rows of keys");
+    if (d->window < 0 || d->sinks < 0) return bad("window and sinks must not be negative");
+    if (!(d->scale > 0.0f) || !(d->scale <= 3.0e38f)) return bad("scale must be positive and finite");
+    if (d->buckets < 0 || d->buckets > MAX_BUCKETS) return bad("buckets must be in [0, 256]");
+    if (d->buckets && d->table_dtype != PARO_F32 && d->table_dtype != d->dtype) return bad("table_dtype must be PARO_F32 or dtype");
+    // a head's distance is that between neighbours in a row, or that between whole planes: each row of each head ends before the next one's begins
+    const int64_t hd = d->head_dim, kv = d->kv_heads;
+    const int64_t lds[4] = {d->ld_q, d->ld_k, d->ld_v, d->ld_out}, heads[4] = {d->head_q, d->head_k, d->head_v, d->head_out};
+    for (int i = 0; i < 4; ++i) {
+        const int64_t count = i == 0 || i == 3 ? d->heads : kv;
+        const int64_t head = heads[i] ? heads[i] : hd, ld = lds[i] ? lds[i] : count * hd;
+        if (head < hd || ld < hd) return bad("a head is longer than its distance to the next");
+        if (head < ld && ld < (count - 1) * head + hd) return bad("a row is longer than its distance to the next");
+        if (ld > ((int64_t)1 << 40) || head > ((int64_t)1 << 50)) return bad("distances between rows are at most 2^40, between heads 2^50");
+    }
+    if (ceil_div(std::max(d->len_q, d->len_k), 16) * d->heads > INT32_MAX / std::max<int64_t>(1, d->batch))
+        return bad("batch * heads * length is at most 2^35");
+    return PARO_OK;
+}
+// Without arrays that say where sequences lie, they lie one behind the other.
+inline int check_rows(const std::string &f, const paro_attn_t &d, const void *q_starts, const void *k_starts) {
+    if (!q_starts && d.rows_q && d.rows_q < d.batch * d.len_q) return fail(PARO_EINVAL, f + "rows_q holds fewer than batch * len_q rows");
+    if (!k_starts && d.rows_k && d.rows_k < d.batch * d.len_k) return fail(PARO_EINVAL, f + "rows_k holds fewer than batch * len_k rows");
+    return PARO_OK;
+}
+inline int check_inputs(const std::string &f, const paro_attn_t &d, const void *q, const void *k, const void *v, const int32_t *q_starts, const int32_t *k_starts,
+                        const int32_t *k_lens, const void *table, const int32_t *first) {
+    int rc = check_array(q, 2, f + "q");
+    if (!rc && d.len_k) rc = check_array(k, 2, f + "k");
+    if (!rc && d.len_k) rc = check_array(v, 2, f + "v");
+    if (!rc && q_starts) rc = check_array(q_starts, 4, f + "q_starts");
+    if (!rc && k_starts) rc = check_array(k_starts, 4, f + "k_starts");
+    if (!rc && k_lens) rc = check_array(k_lens, 4, f + "k_lens");
+    if (!rc && d.buckets) rc = check_array(table, size_of(d.table_dtype), f + "table");
+    if (!rc && d.buckets) rc = check_array(first, 4, f + "first");
+    return rc;
+}
+inline int check_room(const std::string &f, int64_t needed, const void *workspace, int64_t bytes) {
+    if (!needed) return PARO_OK;
+    const int rc = check_array(workspace, 16, f + "workspace");
+    if (rc) return rc;
+    return bytes < needed ? fail(PARO_ERANGE, f + "the workspace is smaller than paro_attn_workspace says") : PARO_OK;
+}
+inline Attn attn_of(const paro_attn_t &d, const void *q, const void *k, const void *v, const int32_t *q_starts, const int32_t *k_starts, const int32_t *k_lens,
+                    const void *table, const int32_t *first) {
+    const auto rows = [&](const void *at, int64_t heads, int64_t ld, int64_t head) {
+        return Rows{static_cast<char *>(const_cast<void *>(at)), ld ? ld : heads * d.head_dim, head ? head : d.head_dim};
+    };
+    Attn a{};
+    a.q = rows(q, d.heads, d.ld_q, d.head_q);
+    a.k = rows(k, d.kv_heads, d.ld_k, d.head_k);
+    a.v = rows(v, d.kv_heads, d.ld_v, d.head_v);
+    a.out = rows(nullptr, d.heads, d.ld_out, d.head_out);
+    a.q_starts = q_starts;
+    a.k_starts = k_starts;
+    a.k_lens = k_lens;
+    a.table = table;
+    a.first = first;
+    a.batch = (int)d.batch;
+    a.heads = (int)d.heads;
+    a.kv_heads = (int)d.kv_heads;
+    a.hd = (int)d.head_dim;
+    a.len_q = (int)d.len_q;
+    a.len_k = (int)d.len_k;
+    a.rows_q = (int)(d.rows_q ? d.rows_q : d.batch * d.len_q);
+    a.rows_k = (int)(d.rows_k ? d.rows_k : d.batch * d.len_k);
+    a.window = d.window && d.window < FAR_AWAY ? (int)d.window : FAR_AWAY;
+    a.sinks = (int)std::min<int64_t>(d.sinks, FAR_AWAY);
+    a.buckets = d.buckets;
+    a.table_dtype = d.table_dtype;
+    a.scale = d.scale;
+    return a;
+}
+
+#define PARO_BY_FORM(CALL)                                                                                                            \
+    (d->dtype == PARO_BF16 ? d->head_dim <= 64 ? d->buckets ? CALL(PARO_BF16, 64, true) : CALL(PARO_BF16, 64, false)                    \
+                                               : d->buckets ? CALL(PARO_BF16, 128, true) : CALL(PARO_BF16, 128, false)                  \
+                           : d->head_dim <= 64 ? d->buckets ? CALL(PARO_F16, 64, true) : CALL(PARO_F16, 64, false)                      \
+                                               : d->buckets ? CALL(PARO_F16, 128, true) : CALL(PARO_F16, 128, false))
+
+}  // namespace
+
+namespace paro {
+int64_t attn_forward_workspace(const paro_attn_t &d);
+}

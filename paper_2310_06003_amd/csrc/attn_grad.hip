@@ -1,0 +1,683 @@
+// Gradient of the attention with a sliding window, sinks and a relative position bias (gfx950).  With P = softmax(s), from dout and the stored out and
+// statistics of the rows:
+//
+//   D_i = dout_i . out_i,  dP_ij = dout_i . v_j,  dS_ij = P_ij (dP_ij - D_i)
+//   dv_j = sum_i P_ij dout_i,  dk_j = scale sum_i dS_ij q_i,  dq_i = scale sum_j dS_ij k_j,  dtable[b] = sum of dS_ij over bucket(p_i - j) = b
+//
+// Two passes over the pairs that see each other, each of which forms P and dP again: k_grad_kv goes over the queries and keeps dk and dv of 128 keys in registers,
+// k_grad_q over the keys and keeps dq of 128 queries.  That is seven products where five would do, but every sum has one place and one order: no atomics on
+// results, the same call gives the same bits.  P and dS are rounded to 16 bits for the products; as in the forward pass, a product's result is
+// the next one's operand as it stands.  fp16: P is multiplied by 2^15; dS by a power of two that brings twice the largest |dout_i| |v_j| to at most 2^15, so that none
+// overflows and the small ones keep their bits.
+#include "attn.hpp"
+
+namespace {
+
+constexpr int BLOCK = 128;                   // keys of a k_grad_kv block, queries of a k_grad_q block: 32 a wave
+constexpr int Q_STEP = 32, K_STEP = 64;      // queries, keys of a tile
+constexpr int MOST_SHARES = 64;
+template <int DT>
+constexpr float SHIFT = DT == PARO_F16 ? 15.0f : 0.0f;
+
+struct Grad {
+    Attn a;
+    Rows dout, dq, dk, dv;
+    // [head][rows_q]: without a bias, P = exp2(q . k * scale * LOG2E - base); with one, exp2((s - base) * LOG2E - log_sum); D
+    float *base, *log_sum, *dots;
+    float *largest;                          // of fp16: the largest |dout_i|^2 and |v_j|^2 of each block of k_dots
+    float *times;                            // of fp16: what dS is multiplied by, and the inverse
+    float *partial;                          // of shared key tiles: [slot][dk, dv][128][HD]
+    float *of_table;                         // [head][sequence][tile of queries][bucket]
+    char *dtable;
+    int blocks_q, blocks_v;                  // of k_dots
+    int key_tiles, sink_tiles, shares, sink_shares, slots;      // of a sequence's key head; sink_tiles: the first ones, whose keys are sinks
+};
+
+// ---------------------------------------------------------------- statistics of the rows
+constexpr int DOT_ROWS = 16;
+
+template <int HD>
+__device__ __forceinline__ float over_lanes(float x) {       // of HD / 8 lanes side by side
+#pragma unroll
+    for (int n = 1; n < HD / 8; n *= 2) x += __shfl_xor(x, n);
+    return x;
+}
+// D, and what P is formed from; blocks behind those of the queries: the values' largest row.
+template <int DT, int HD>
+__global__ __launch_bounds__(256) void k_dots(Grad g) {
+    const Attn &a = g.a;
+    constexpr int LANES = HD / 8, AT_ONCE = 256 / LANES;
+    const bool of_values = (int)blockIdx.x >= g.blocks_q;
+    const unsigned tiles = of_values ? g.blocks_v / a.batch : g.blocks_q / a.batch, block = of_values ? blockIdx.x - g.blocks_q : blockIdx.x;
+    const int b = block / tiles, row0 = block % tiles * DOT_ROWS, piece = threadIdx.x % LANES;
+    const Sequence seq(a, b);
+    const int heads = of_values ? a.kv_heads : a.heads, n = of_values ? seq.nk : seq.nq;
+    const int rows = n - row0 < DOT_ROWS ? n - row0 : DOT_ROWS;
+    float largest = 0.0f;
+    for (int x = threadIdx.x / LANES; x < rows * heads; x += AT_ONCE) {
+        const int i = row0 + x / heads, head = x % heads;
+        float u[8], o[8];
+        float squares = 0.0f, dot = 0.0f;
+        if (of_values) {
+            unpack<DT>(piece_of_head(a.v.of((int64_t)seq.k0 + i, head), piece * 8, a.hd), u);
+        } else {
+            unpack<DT>(piece_of_head(g.dout.of((int64_t)seq.q0 + i, head), piece * 8, a.hd), u);
+            unpack<DT>(piece_of_head(a.out.of((int64_t)seq.q0 + i, head), piece * 8, a.hd), o);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) dot += u[e] * o[e];
+        }
+#pragma unroll
+        for (int e = 0; e < 8; ++e) squares += u[e] * u[e];
+        if constexpr (DT == PARO_F16) {
+            squares = over_lanes<HD>(squares);
+            if (squares < INFINITY) largest = fmaxf(largest, squares);          // a row that is not finite leaves the others' scale alone
+        }
+        if (of_values) continue;
+        dot = over_lanes<HD>(dot);
+        if (piece == 0) {
+            const float *const stats = a.stats + (((int64_t)seq.q0 + i) * a.heads + head) * 2;
+            const float most = stats[0], log_sum = stats[1];
+            const int64_t at = (int64_t)head * a.rows_q + seq.q0 + i;
+            const bool empty = most == -INFINITY;
+            g.dots[at] = dot;
+            if (a.buckets) {
+                g.base[at] = empty ? INFINITY : most;
+                g.log_sum[at] = empty ? 0.0f : log_sum * LOG2E - SHIFT<DT>;
+            } else {
+                g.base[at] = empty ? INFINITY : __builtin_fmaf(most, LOG2E, log_sum * LOG2E) - SHIFT<DT>;
+            }
+        }
+    }
+    if constexpr (DT == PARO_F16) {
+        __shared__ float of_waves[4];
+#pragma unroll
+        for (int x = 1; x < 64; x *= 2) largest = fmaxf(largest, __shfl_xor(largest, x));
+        if ((threadIdx.x & 63) == 0) of_waves[wave_of()] = largest;
+        __syncthreads();
+        if (threadIdx.x == 0) g.largest[blockIdx.x] = fmaxf(fmaxf(of_waves[0], of_waves[1]), fmaxf(of_waves[2], of_waves[3]));
+    }
+}
+// |dP - D| is at most twice the largest |dout_i| |v_j|, as out is a mean of values.
+__global__ __launch_bounds__(256) void k_times(Grad g) {
+    __shared__ float of_waves[2][4];
+    float most[2] = {0.0f, 0.0f};
+    for (int x = threadIdx.x; x < g.blocks_q + g.blocks_v; x += 256) {
+        const float v = g.largest[x];
+        if (x < g.blocks_q) most[0] = fmaxf(most[0], v);
+        else most[1] = fmaxf(most[1], v);
+    }
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
+#pragma unroll
+        for (int x = 1; x < 64; x *= 2) most[k] = fmaxf(most[k], __shfl_xor(most[k], x));
+        if ((threadIdx.x & 63) == 0) of_waves[k][wave_of()] = most[k];
+    }
+    __syncthreads();
+    if (threadIdx.x == 0) {
+#pragma unroll
+        for (int k = 0; k < 2; ++k) most[k] = fmaxf(fmaxf(of_waves[k][0], of_waves[k][1]), fmaxf(of_waves[k][2], of_waves[k][3]));
+        const bool usual = most[0] > 0.0f && most[1] > 0.0f;       // of zeros nothing is scaled
+        int power = 0;
+        if (usual) {
+            int e0, e1;
+            frexpf(most[0], &e0);                    // most <= 2^e
+            frexpf(most[1], &e1);
+            power = 14 - (e0 + 1) / 2 - (e1 + 1) / 2 - 1;
+            power = power < -100 ? -100 : power > 100 ? 100 : power;
+        }
+        g.times[0] = ldexpf(1.0f, power);
+        g.times[1] = ldexpf(1.0f, -power);
+    }
+}
+
+// ---------------------------------------------------------------- dk and dv
+struct Share {
+    int tile, share, shares, slot;           // slot < 0: the block has the tile to itself
+};
+__device__ __forceinline__ Share share_of(const Grad &g, int block, int of_kv) {
+    Share s;
+    const int of_sinks = g.sink_tiles * g.sink_shares;
+    if (block < of_sinks) {
+        s.shares = g.sink_shares;
+        s.tile = block / g.sink_shares;
+        s.share = block % g.sink_shares;
+    } else {
+        s.shares = g.shares;
+        s.tile = g.sink_tiles + (block - of_sinks) / g.shares;
+        s.share = (block - of_sinks) % g.shares;
+    }
+    s.slot = s.shares > 1 ? of_kv * g.slots + block : -1;
+    return s;
+}
+
+template <int DT, int HD, bool BIAS>
+__global__ __launch_bounds__(256, 1) void k_grad_kv(Grad g) {
+    using T = Tile<HD>;
+    const Attn &a = g.a;
+    constexpr int BYTES = Q_STEP * T::ROW, PASSES = Q_STEP * T::PIECES / 256, STEPS = HD / 16, APART = 256 / T::PIECES;
+    static_assert(PASSES >= 1, "every thread stages a piece");
+    __shared__ __attribute__((aligned(1024))) char tiles[2][2][BYTES];         // [buffer][queries, dout]
+    __shared__ float rows[2][3][Q_STEP];                                       // [buffer][base, log_sum, dots]
+    __shared__ Bias bias;
+    __shared__ float by_distance[2][BLOCK + Q_STEP];
+    const int per_kv = g.sink_tiles * g.sink_shares + (g.key_tiles - g.sink_tiles) * g.shares;
+    const unsigned work = in_runs(blockIdx.x, gridDim.x);
+    const int of_kv = work / per_kv, kv = of_kv % a.kv_heads, b = of_kv / a.kv_heads;
+    const Share share = share_of(g, work % per_kv, of_kv);
+    const Sequence seq(a, b);
+    const int k0 = share.tile * BLOCK;
+    if (k0 >= seq.nk) return;
+    const int lane = threadIdx.x & 63, w = wave_of(), h = lane >> 5, off = seq.nk - seq.nq, group = a.heads / a.kv_heads;
+    const int of_wave = k0 + w * 32, j = of_wave + (lane & 31);                // the lane's key
+    // The tiles of queries that see any of the keys, for each head of the group; and this share of them.
+    const int last_key = k0 + BLOCK < seq.nk ? k0 + BLOCK - 1 : seq.nk - 1;
+    const int64_t until = k0 < a.sinks ? seq.nq : (int64_t)last_key + a.window - off;
+    const int lo = k0 - off > 0 ? k0 - off : 0, hi = until < seq.nq ? (int)until : seq.nq;
+    const int tile0 = lo / Q_STEP, per_head = hi > lo ? (hi + Q_STEP - 1) / Q_STEP - tile0 : 0;
+    const int64_t all = (int64_t)per_head * group;
+    const int from = (int)(all * share.share / share.shares), to = (int)(all * (share.share + 1) / share.shares);
+
+    const int piece = threadIdx.x % T::PIECES, row = threadIdx.x / T::PIECES;
+    u32x4 from_q[PASSES], from_o[PASSES];
+    float from_row = 0.0f;
+    const auto load = [&](int u) {
+        const int head = kv * group + u / per_head, i0 = (tile0 + u % per_head) * Q_STEP;
+#pragma unroll
+        for (int n = 0; n < PASSES; ++n) {
+            const int i = i0 + row + n * APART;
+            from_q[n] = from_o[n] = u32x4{0, 0, 0, 0};
+            if (i < seq.nq) {
+                from_q[n] = piece_of_head(a.q.of((int64_t)seq.q0 + i, head), piece * 8, a.hd);
+                from_o[n] = piece_of_head(g.dout.of((int64_t)seq.q0 + i, head), piece * 8, a.hd);
+            }
+        }
+        if (threadIdx.x < 3 * Q_STEP && (BIAS || threadIdx.x < Q_STEP || threadIdx.x >= 2 * Q_STEP)) {
+            const int i = i0 + threadIdx.x % Q_STEP, which = threadIdx.x / Q_STEP;
+            const float *const of = which == 0 ? g.base : which == 1 ? g.log_sum : g.dots;
+            from_row = i < seq.nq ? of[(int64_t)head * a.rows_q + seq.q0 + i] : which == 0 ? INFINITY : 0.0f;
+        }
+    };
+    int far_from = 0, of_head = -1;
+    float far_bias = 0.0f, next_far_bias = 0.0f;
+    const auto is_far = [&](int i0) { return BIAS && off + i0 - (k0 + BLOCK - 1) >= far_from; };
+    const auto stage = [&](int u, int buffer) {
+#pragma unroll
+        for (int n = 0; n < PASSES; ++n) {
+            const int at = T::at(row + n * APART, piece);
+            *reinterpret_cast<u32x4 *>(tiles[buffer][0] + at) = from_q[n];
+            *reinterpret_cast<u32x4 *>(tiles[buffer][1] + at) = from_o[n];
+        }
+        if (threadIdx.x < 3 * Q_STEP) rows[buffer][threadIdx.x / Q_STEP][threadIdx.x % Q_STEP] = from_row;
+        if constexpr (BIAS) {
+            const int head = kv * group + u / per_head, i0 = (tile0 + u % per_head) * Q_STEP;
+            if (head != of_head) {
+                __syncthreads();
+                bias.load(a, head);
+                __syncthreads();
+                of_head = head;
+                far_from = bias.first[a.buckets - 1];
+                next_far_bias = bias.column[a.buckets - 1];
+            }
+            if (!is_far(i0) && threadIdx.x < BLOCK + Q_STEP - 1) by_distance[buffer][threadIdx.x] = bias.of(off + i0 - (k0 + BLOCK - 1) + (int)threadIdx.x, a.buckets);
+        }
+    };
+
+    short8_t keys[STEPS], values[STEPS];
+#pragma unroll
+    for (int s = 0; s < STEPS; ++s) {
+        u32x4 x{0, 0, 0, 0}, y{0, 0, 0, 0};
+        if (j < seq.nk) {
+            x = piece_of_head(a.k.of((int64_t)seq.k0 + j, kv), s * 16 + h * 8, a.hd);
+            y = piece_of_head(a.v.of((int64_t)seq.k0 + j, kv), s * 16 + h * 8, a.hd);
+        }
+        keys[s] = __builtin_bit_cast(short8_t, x);
+        values[s] = __builtin_bit_cast(short8_t, y);
+    }
+    const float unit = a.scale * LOG2E, times = DT == PARO_F16 ? g.times[0] * 0x1p-15f : 1.0f;
+    f32x16 dk[HD / 32] = {}, dv[HD / 32] = {};
+    if (from < to) {
+        load(from);
+        stage(from, 0);
+    }
+    for (int u = from; u < to; ++u) {
+        const int i0 = (tile0 + u % per_head) * Q_STEP, buffer = (u - from) & 1, first = off + i0;
+        far_bias = next_far_bias;
+        if (u + 1 < to) load(u + 1);
+        __syncthreads();
+        const char *const queries = tiles[buffer][0], *const douts = tiles[buffer][1];
+        const bool none = first + Q_STEP - 1 < of_wave || (first - (of_wave + 31) >= a.window && of_wave >= a.sinks);
+        if (!none) {
+            f32x16 s = {}, dp = {};
+#pragma unroll
+            for (int c = 0; c < STEPS; ++c) s = mfma32<DT>(T::rows(queries, 0, c, lane), keys[c], s);
+#pragma unroll
+            for (int c = 0; c < STEPS; ++c) dp = mfma32<DT>(T::rows(douts, 0, c, lane), values[c], dp);
+            const bool every = first >= of_wave + 31 && (first + Q_STEP - 1 - of_wave < a.window || of_wave + 31 < a.sinks);
+            if constexpr (BIAS) {
+                const bool far = is_far(i0);
+                const float *const at = by_distance[buffer] + BLOCK - 1 - (w * 32 + (lane & 31)) + 4 * h;
+#pragma unroll
+                for (int e = 0; e < 16; ++e) s[e] = s[e] * a.scale + (far ? far_bias : at[8 * (e / 4) + e % 4]);
+            }
+            if (!every) {
+#pragma unroll
+                for (int e = 0; e < 16; ++e)
+                    if (!sees(first + 8 * (e / 4) + 4 * h + e % 4, j, a.window, a.sinks)) s[e] = -INFINITY;
+            }
+#pragma unroll
+            for (int e = 0; e < 16; e += 4) {
+                const f32x4 base = *reinterpret_cast<const f32x4 *>(rows[buffer][0] + 2 * e + 4 * h);
+                const f32x4 dot = *reinterpret_cast<const f32x4 *>(rows[buffer][2] + 2 * e + 4 * h);
+                f32x4 log_sum = {};
+                if constexpr (BIAS) log_sum = *reinterpret_cast<const f32x4 *>(rows[buffer][1] + 2 * e + 4 * h);
+#pragma unroll
+                for (int x = 0; x < 4; ++x) {
+                    s[e + x] = exp2_(BIAS ? __builtin_fmaf(s[e + x] - base[x], LOG2E, -log_sum[x]) : __builtin_fmaf(s[e + x], unit, -base[x]));
+                    dp[e + x] = s[e + x] * (DT == PARO_F16 ? (dp[e + x] - dot[x]) * times : dp[e + x] - dot[x]);
+                }
+            }
+#pragma unroll
+            for (int k = 0; k < 2; ++k) {
+                const short8_t p = pack8<DT>(s, 8 * k), ds = pack8<DT>(dp, 8 * k);
+#pragma unroll
+                for (int d = 0; d < HD / 32; ++d) {
+                    dv[d] = mfma32<DT>(T::columns(douts, k * 16, d, lane), p, dv[d]);
+                    dk[d] = mfma32<DT>(T::columns(queries, k * 16, d, lane), ds, dk[d]);
+                }
+            }
+        }
+        if (u + 1 < to) stage(u + 1, buffer ^ 1);
+    }
+    if (share.slot >= 0) {
+        float *const at = g.partial + ((int64_t)share.slot * 2 * BLOCK + w * 32 + (lane & 31)) * HD + 4 * h;
+#pragma unroll
+        for (int d = 0; d < HD / 32; ++d)
+#pragma unroll
+            for (int e = 0; e < 16; e += 4) {
+                *reinterpret_cast<f32x4 *>(at + d * 32 + 2 * e) = f32x4{dk[d][e], dk[d][e + 1], dk[d][e + 2], dk[d][e + 3]};
+                *reinterpret_cast<f32x4 *>(at + BLOCK * HD + d * 32 + 2 * e) = f32x4{dv[d][e], dv[d][e + 1], dv[d][e + 2], dv[d][e + 3]};
+            }
+        return;
+    }
+    const float of_dk = DT == PARO_F16 ? a.scale * g.times[1] : a.scale, of_dv = DT == PARO_F16 ? 0x1p-15f : 1.0f;
+    char *const to_k = g.dk.of((int64_t)seq.k0 + j, kv), *const to_v = g.dv.of((int64_t)seq.k0 + j, kv);
+#pragma unroll
+    for (int d = 0; d < HD / 32; ++d) {
+        store_row32<DT>(to_k, d * 32, a.hd, dk[d], of_dk, j < seq.nk);
+        store_row32<DT>(to_v, d * 32, a.hd, dv[d], of_dv, j < seq.nk);
+    }
+}
+
+// Adds the shares of a tile of keys, in order: eight rows of dk or dv a block.
+template <int DT, int HD>
+__global__ __launch_bounds__(256) void k_grad_join(Grad g) {
+    const Attn &a = g.a;
+    constexpr int ROWS = 256 / (HD / 4);
+    const int joined = g.shares > 1 ? g.key_tiles : g.sink_tiles;
+    const int of_kv = blockIdx.x / joined, tile = blockIdx.x % joined, kv = of_kv % a.kv_heads, b = of_kv / a.kv_heads;
+    const Sequence seq(a, b);
+    const int r = blockIdx.y * ROWS + threadIdx.x / (HD / 4), c = threadIdx.x % (HD / 4) * 4, j = tile * BLOCK + r;
+    const bool of_v = blockIdx.z;
+    if (j >= seq.nk) return;
+    const bool sinks = tile < g.sink_tiles;
+    const int shares = sinks ? g.sink_shares : g.shares;
+    const int64_t slot = (int64_t)of_kv * g.slots + (sinks ? tile * g.sink_shares : g.sink_tiles * g.sink_shares + (tile - g.sink_tiles) * g.shares);
+    const float *at = g.partial + ((slot * 2 + of_v) * BLOCK + r) * HD + c;
+    f32x4 sum = {};
+#pragma unroll 8
+    for (int s = 0; s < shares; ++s) sum += *reinterpret_cast<const f32x4 *>(at + (int64_t)s * (2 * BLOCK * HD));
+    sum *= of_v ? (DT == PARO_F16 ? 0x1p-15f : 1.0f) : DT == PARO_F16 ? a.scale * g.times[1] : a.scale;
+    char *const to = (of_v ? g.dv : g.dk).of((int64_t)seq.k0 + j, kv);
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+        if (c + e < a.hd) store_one<DT>(to, c + e, sum[e]);
+}
+
+// ---------------------------------------------------------------- dq, and the table's gradient
+template <int DT, int HD, bool BIAS>
+__global__ __launch_bounds__(256, 2) void k_grad_q(Grad g) {
+    using T = Tile<HD>;
+    const Attn &a = g.a;
+    constexpr int BYTES = K_STEP * T::ROW, PASSES = K_STEP * T::PIECES / 256, STEPS = HD / 16, APART = 256 / T::PIECES, DISTANCES = 32 + K_STEP;
+    __shared__ __attribute__((aligned(1024))) char tiles[2][2][BYTES];          // [buffer][keys, values]
+    __shared__ Bias bias;
+    __shared__ float by_distance[2][BLOCK + K_STEP];
+    __shared__ float diagonals[BIAS ? 4 : 1][2][DISTANCES];                     // [wave][half]: sums of dS along a distance, of one tile
+    __shared__ float of_buckets[BIAS ? 4 : 1][BIAS ? MAX_BUCKETS : 1], far_sums[4];
+    const unsigned work = in_runs(blockIdx.x, gridDim.x), of_head = work / a.tiles;
+    const int head = of_head % a.heads, b = of_head / a.heads, tile = a.tiles - 1 - work % a.tiles, i0 = tile * BLOCK;
+    const bool want = BIAS && g.dtable;
+    float *const of_table = g.of_table + (((int64_t)head * a.batch + b) * a.tiles + tile) * a.buckets;
+    const Sequence seq(a, b);
+    if (i0 >= seq.nq) {
+        if (want)
+            for (int x = threadIdx.x; x < a.buckets; x += 256) of_table[x] = 0.0f;
+        return;
+    }
+    const int lane = threadIdx.x & 63, w = wave_of(), h = lane >> 5;
+    const int off = seq.nk - seq.nq, first = i0 + off, last = (i0 + BLOCK < seq.nq ? i0 + BLOCK : seq.nq) - 1 + off;
+    const Seen<K_STEP> seen(a, first, last);
+    const int of_wave = first + w * 32, place = of_wave + (lane & 31), i = i0 + w * 32 + (lane & 31);
+    const int kv = head / (a.heads / a.kv_heads);
+    const int piece = threadIdx.x % T::PIECES, row = threadIdx.x / T::PIECES;
+    u32x4 from_k[PASSES], from_v[PASSES];
+    const auto load = [&](int t) {
+        const int k0 = seen.tile(t) * K_STEP;
+#pragma unroll
+        for (int n = 0; n < PASSES; ++n) {
+            const int j = k0 + row + n * APART;
+            from_k[n] = from_v[n] = u32x4{0, 0, 0, 0};
+            if (seen.holds(j)) {
+                from_k[n] = piece_of_head(a.k.of((int64_t)seq.k0 + j, kv), piece * 8, a.hd);
+                from_v[n] = piece_of_head(a.v.of((int64_t)seq.k0 + j, kv), piece * 8, a.hd);
+            }
+        }
+    };
+    int far_from = 0;
+    float far_bias = 0.0f, far_sum = 0.0f;
+    const auto is_far = [&](int k0) { return BIAS && first - (k0 + K_STEP - 1) >= far_from; };
+    const auto stage = [&](int t, int buffer) {
+#pragma unroll
+        for (int n = 0; n < PASSES; ++n) {
+            const int at = T::at(row + n * APART, piece);
+            *reinterpret_cast<u32x4 *>(tiles[buffer][0] + at) = from_k[n];
+            *reinterpret_cast<u32x4 *>(tiles[buffer][1] + at) = from_v[n];
+        }
+        if constexpr (BIAS) {
+            const int k0 = seen.tile(t) * K_STEP;
+            if (!is_far(k0) && threadIdx.x < BLOCK + K_STEP - 1) by_distance[buffer][threadIdx.x] = bias.of(first - k0 + BLOCK - 1 - (int)threadIdx.x, a.buckets);
+        }
+    };
+    if (seen.tiles) load(0);
+    if constexpr (BIAS) {
+        bias.load(a, head);
+        for (int x = threadIdx.x; x < 4 * MAX_BUCKETS; x += 256) of_buckets[x / MAX_BUCKETS][x % MAX_BUCKETS] = 0.0f;
+        __syncthreads();
+        far_from = bias.first[a.buckets - 1];
+        far_bias = bias.column[a.buckets - 1];
+    }
+    short8_t q[STEPS], dout[STEPS];
+    float base = INFINITY, log_sum = 0.0f, dot = 0.0f;
+    if (i < seq.nq) {
+        const int64_t at = (int64_t)head * a.rows_q + seq.q0 + i;
+        base = g.base[at];
+        dot = g.dots[at];
+        if constexpr (BIAS) log_sum = g.log_sum[at];
+    }
+#pragma unroll
+    for (int s = 0; s < STEPS; ++s) {
+        u32x4 x{0, 0, 0, 0}, y{0, 0, 0, 0};
+        if (i < seq.nq) {
+            x = piece_of_head(a.q.of((int64_t)seq.q0 + i, head), s * 16 + h * 8, a.hd);
+            y = piece_of_head(g.dout.of((int64_t)seq.q0 + i, head), s * 16 + h * 8, a.hd);
+        }
+        q[s] = __builtin_bit_cast(short8_t, x);
+        dout[s] = __builtin_bit_cast(short8_t, y);
+    }
+    const float unit = a.scale * LOG2E, times = DT == PARO_F16 ? g.times[0] * 0x1p-15f : 1.0f;
+    f32x16 dq[HD / 32] = {};
+    if (seen.tiles) stage(0, 0);
+    for (int t = 0; t < seen.tiles; ++t) {
+        const int k0 = seen.tile(t) * K_STEP, buffer = t & 1;
+        if (t + 1 < seen.tiles) load(t + 1);
+        __syncthreads();
+        const char *const keys = tiles[buffer][0], *const values = tiles[buffer][1];
+        const bool none = k0 > of_wave + 31 || (k0 + K_STEP <= of_wave - a.window + 1 && k0 >= a.sinks), far = is_far(k0);
+        if (want && !far) {
+#pragma unroll
+            for (int x = 0; x < 2 * DISTANCES; x += 64) (&diagonals[BIAS ? w : 0][0][0])[x + lane] = 0.0f;
+        }
+        if (!none) {
+            const bool every = k0 + K_STEP - 1 <= of_wave && (k0 > of_wave + 31 - a.window || k0 + K_STEP <= a.sinks);
+#pragma unroll
+            for (int n = 0; n < 2; ++n) {
+                f32x16 s = {}, dp = {};
+#pragma unroll
+                for (int c = 0; c < STEPS; ++c) s = mfma32<DT>(T::rows(keys, n * 32, c, lane), q[c], s);
+#pragma unroll
+                for (int c = 0; c < STEPS; ++c) dp = mfma32<DT>(T::rows(values, n * 32, c, lane), dout[c], dp);
+                if constexpr (BIAS) {
+                    const float *const at = by_distance[buffer] + BLOCK - 1 - (w * 32 + (lane & 31)) + 4 * h + n * 32;
+#pragma unroll
+                    for (int e = 0; e < 16; ++e) s[e] = s[e] * a.scale + (far ? far_bias : at[8 * (e / 4) + e % 4]);
+                }
+                if (!every) {
+#pragma unroll
+                    for (int e = 0; e < 16; ++e)
+                        if (!sees(place, k0 + n * 32 + 8 * (e / 4) + 4 * h + e % 4, a.window, a.sinks)) s[e] = -INFINITY;
+                }
+#pragma unroll
+                for (int e = 0; e < 16; ++e) {
+                    const float p = exp2_(BIAS ? __builtin_fmaf(s[e] - base, LOG2E, -log_sum) : __builtin_fmaf(s[e], unit, -base));
+                    dp[e] = p * (DT == PARO_F16 ? (dp[e] - dot) * times : dp[e] - dot);
+                }
+                if constexpr (BIAS) {
+                    if (want && far) {
+#pragma unroll
+                        for (int e = 0; e < 16; ++e) far_sum += dp[e];
+                    } else if (want) {
+                        // the lanes of a half have 32 different distances each time, and halves an array each: every place is added to in the order of e and n
+                        float *const at = diagonals[w][h] + K_STEP - 1 + (lane & 31) - (n * 32 + 4 * h);
+#pragma unroll
+                        for (int e = 0; e < 16; ++e) __hip_atomic_fetch_add(at - (8 * (e / 4) + e % 4), dp[e], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP);
+                    }
+                }
+#pragma unroll
+                for (int k = 0; k < 2; ++k) {
+                    const short8_t ds = pack8<DT>(dp, 8 * k);
+#pragma unroll
+                    for (int d = 0; d < HD / 32; ++d) dq[d] = mfma32<DT>(T::columns(keys, n * 32 + k * 16, d, lane), ds, dq[d]);
+                }
+            }
+        }
+        if constexpr (BIAS) {
+            if (want && !far) {
+                __syncthreads();
+                // thread x has the distance first - (k0 + K_STEP - 1) + x of the tile; buckets are runs of distances, whose sums the last lane of a run adds
+                const int x = threadIdx.x, d = first - (k0 + K_STEP - 1) + x;
+                float sum = 0.0f;
+#pragma unroll
+                for (int v = 0; v < 4; ++v)
+                    if (x >= v * 32 && x < v * 32 + DISTANCES) sum += diagonals[v][0][x - v * 32] + diagonals[v][1][x - v * 32];
+                const int bucket = d < 0 || x >= BLOCK + K_STEP ? -1 : bias.bucket(d, a.buckets);
+#pragma unroll
+                for (int n = 1; n < 64; n *= 2) {
+                    const float before = __shfl_up(sum, n);
+                    const int of = __shfl_up(bucket, n);
+                    if (lane >= n && of == bucket) sum += before;
+                }
+                const int next = __shfl_down(bucket, 1);
+                if (bucket >= 0 && (lane == 63 || next != bucket)) of_buckets[w][bucket] += sum;
+            }
+        }
+        if (t + 1 < seen.tiles) stage(t + 1, buffer ^ 1);
+    }
+    const float of_dq = DT == PARO_F16 ? a.scale * g.times[1] : a.scale;
+    char *const to = g.dq.of((int64_t)seq.q0 + i, head);
+#pragma unroll
+    for (int d = 0; d < HD / 32; ++d) store_row32<DT>(to, d * 32, a.hd, dq[d], of_dq, i < seq.nq);
+    if constexpr (BIAS) {
+        if (want) {
+#pragma unroll
+            for (int x = 1; x < 64; x *= 2) far_sum += __shfl_xor(far_sum, x);
+            if (lane == 0) far_sums[w] = far_sum;
+            __syncthreads();
+            for (int x = threadIdx.x; x < a.buckets; x += 256) {
+                float sum = 0.0f;
+#pragma unroll
+                for (int v = 0; v < 4; ++v) sum += of_buckets[v][x] + (x == a.buckets - 1 ? far_sums[v] : 0.0f);
+                of_table[x] = DT == PARO_F16 ? sum * g.times[1] : sum;
+            }
+        }
+    }
+}
+
+// Adds the blocks' sums of a head, in order: a thread has every `parts`-th of a bucket.
+template <int DT>
+__global__ __launch_bounds__(256) void k_table_grad(Grad g) {
+    const Attn &a = g.a;
+    __shared__ float sums[256];
+    const int head = blockIdx.x, parts = 256 / a.buckets, bucket = threadIdx.x % a.buckets, part = threadIdx.x / a.buckets;
+    const int64_t blocks = (int64_t)a.batch * a.tiles;
+    const float *const at = g.of_table + (int64_t)head * blocks * a.buckets + bucket;
+    float sum = 0.0f;
+    if (part < parts) {
+#pragma unroll 8
+        for (int64_t x = part; x < blocks; x += parts) sum += at[x * a.buckets];
+    }
+    sums[threadIdx.x] = sum;
+    __syncthreads();
+    if (part) return;
+    for (int x = 1; x < parts; ++x) sum += sums[x * a.buckets + bucket];
+    const int64_t to = (int64_t)bucket * a.heads + head;
+    if (a.table_dtype == PARO_F32) reinterpret_cast<float *>(g.dtable)[to] = sum;
+    else store_one<DT>(g.dtable, to, sum);
+}
+
+// ---------------------------------------------------------------- host
+struct Plan {
+    int blocks_q, blocks_v, tiles, key_tiles, sink_tiles, shares, sink_shares, slots;
+    int64_t kv_blocks, log_sum, dots, largest, times, partial, of_table, bytes;
+};
+
+Plan plan_of(const paro_attn_t &d) {
+    Plan p{};
+    const int64_t group = d.heads / d.kv_heads, hd = d.head_dim <= 64 ? 64 : 128, rows_q = d.rows_q ? d.rows_q : d.batch * d.len_q;
+    const int64_t window = d.window && d.window < d.len_k ? d.window : d.len_k;
+    p.blocks_q = (int)(ceil_div(d.len_q, DOT_ROWS) * d.batch);
+    p.blocks_v = d.dtype == PARO_F16 ? (int)(ceil_div(d.len_k, DOT_ROWS) * d.batch) : 0;
+    p.tiles = (int)ceil_div(d.len_q, BLOCK);
+    p.key_tiles = (int)ceil_div(d.len_k, BLOCK);
+    // Tiles of keys are shared out where there are few of them; those with sinks, which every later query sees, by how many more see them than see others.
+    const int64_t whole = std::max<int64_t>(1, (int64_t)p.key_tiles * d.kv_heads * d.batch);
+    const int64_t others = std::min<int64_t>(d.len_q, window + BLOCK);
+    const int64_t steps = std::max<int64_t>(1, ceil_div(others, Q_STEP) * group);
+    p.shares = (int)std::max<int64_t>(1, std::min<int64_t>(std::min<int64_t>(ceil_div(512, whole), ceil_div(steps, 8)), MOST_SHARES));
+    p.sink_tiles = window < d.len_k ? (int)std::min<int64_t>(ceil_div(std::min<int64_t>(d.sinks, d.len_k), BLOCK), p.key_tiles) : 0;
+    // (a share's sums take 128 KiB of the workspace)
+    p.sink_shares = p.shares;
+    if (p.sink_tiles) {
+        const int64_t most = std::min<int64_t>(MOST_SHARES, std::max<int64_t>(p.shares, 1024 / (p.sink_tiles * d.kv_heads * d.batch)));
+        p.sink_shares = (int)std::min<int64_t>(p.shares * ceil_div(d.len_q, std::max<int64_t>(1, others)), most);
+    }
+    const int64_t per_kv = (int64_t)p.sink_tiles * p.sink_shares + (int64_t)(p.key_tiles - p.sink_tiles) * p.shares;
+    p.slots = p.shares > 1 ? (int)per_kv : p.sink_shares > 1 ? p.sink_tiles * p.sink_shares : 0;
+    p.kv_blocks = per_kv * d.kv_heads * d.batch;
+    int64_t at = 0;
+    const auto room = [&](int64_t floats) {
+        const int64_t was = at;
+        at += ceil_div(floats * 4, 256) * 256;
+        return was;
+    };
+    room(rows_q * d.heads);                                                     // base
+    p.log_sum = room(d.buckets ? rows_q * d.heads : 0);
+    p.dots = room(rows_q * d.heads);
+    p.largest = room((int64_t)p.blocks_q + p.blocks_v);
+    p.times = room(2);
+    p.partial = room((int64_t)p.slots * d.kv_heads * d.batch * 2 * BLOCK * hd);
+    p.of_table = room((int64_t)d.heads * d.batch * p.tiles * d.buckets);
+    p.bytes = at;
+    return p;
+}
+
+template <int DT, int HD, bool BIAS>
+void launch(const Grad &g, const Plan &p, hipStream_t st) {
+    if (p.blocks_q + p.blocks_v) hipLaunchKernelGGL((k_dots<DT, HD>), dim3((unsigned)(p.blocks_q + p.blocks_v)), dim3(256), 0, st, g);
+    if constexpr (DT == PARO_F16) hipLaunchKernelGGL(k_times, dim3(1), dim3(256), 0, st, g);
+    if (p.kv_blocks) {
+        hipLaunchKernelGGL((k_grad_kv<DT, HD, BIAS>), dim3((unsigned)p.kv_blocks), dim3(256), 0, st, g);
+        const int joined = p.shares > 1 ? p.key_tiles : p.sink_shares > 1 ? p.sink_tiles : 0;
+        if (joined)
+            hipLaunchKernelGGL((k_grad_join<DT, HD>), dim3((unsigned)(joined * g.a.kv_heads * g.a.batch), BLOCK / (1024 / HD), 2), dim3(256), 0, st, g);
+    }
+    if (p.tiles) hipLaunchKernelGGL((k_grad_q<DT, HD, BIAS>), dim3((unsigned)((int64_t)p.tiles * g.a.heads * g.a.batch)), dim3(256), 0, st, g);
+    if (BIAS && g.dtable) hipLaunchKernelGGL((k_table_grad<DT>), dim3((unsigned)g.a.heads), dim3(256), 0, st, g);
+}
+
+}  // namespace
+
+extern "C" {
+
+int64_t paro_attn_workspace(const paro_attn_t *d, int grad) {
+    int64_t bytes = 0;
+    const int rc = guarded([&]() -> int {
+        const int bad = check_attn("paro_attn_workspace: ", d);
+        if (!bad) bytes = d->batch == 0 ? 0 : grad ? plan_of(*d).bytes : paro::attn_forward_workspace(*d);
+        return bad;
+    });
+    return rc ? rc : bytes;
+}
+
+int paro_attn_grad(const paro_attn_t *d, const void *dout, const void *q, const void *k, const void *v, const void *out, const float *stats,
+                   const int32_t *q_starts, const int32_t *k_starts, const int32_t *k_lens, const void *table, const int32_t *first, void *dq, void *dk, void *dv,
+                   void *dtable, void *workspace, int64_t workspace_bytes, void *stream) {
+    return guarded([&]() -> int {
+        const std::string f = "paro_attn_grad: ";
+        int rc;
+        if ((rc = check_attn(f, d)) || (rc = check_rows(f, *d, q_starts, k_starts))) return rc;
+        if (d->batch == 0 && !(d->buckets && dtable)) return PARO_OK;
+        if (d->batch && d->len_q &&
+            ((rc = check_array(dout, 2, f + "dout")) || (rc = check_array(out, 2, f + "out")) || (rc = check_array(stats, 4, f + "stats")) || (rc = check_array(dq, 2, f + "dq"))))
+            return rc;
+        if (d->batch && (rc = check_inputs(f, *d, q, k, v, q_starts, k_starts, k_lens, table, first))) return rc;
+        if (d->batch && d->len_k && ((rc = check_array(dk, 2, f + "dk")) || (rc = check_array(dv, 2, f + "dv")))) return rc;
+        if (d->buckets && dtable && (rc = check_array(dtable, size_of(d->table_dtype), f + "dtable"))) return rc;
+        const Plan p = plan_of(*d);
+        if ((rc = check_room(f, p.bytes, workspace, workspace_bytes))) return rc;
+        char *ws = static_cast<char *>(workspace);
+        const auto floats = [&](int64_t at) { return reinterpret_cast<float *>(ws + at); };
+        Grad g{};
+        g.a = attn_of(*d, q, k, v, q_starts, k_starts, k_lens, table, first);
+        g.a.out.at = static_cast<char *>(const_cast<void *>(out));
+        g.a.stats = const_cast<float *>(stats);
+        g.a.tiles = p.tiles;
+        const auto as = [](Rows like, const void *at) {
+            like.at = static_cast<char *>(const_cast<void *>(at));
+            return like;
+        };
+        g.dout = as(g.a.out, dout);
+        g.dq = as(g.a.q, dq);
+        g.dk = as(g.a.k, dk);
+        g.dv = as(g.a.v, dv);
+        g.base = floats(0);
+        g.log_sum = floats(p.log_sum);
+        g.dots = floats(p.dots);
+        g.largest = floats(p.largest);
+        g.times = floats(p.times);
+        g.partial = floats(p.partial);
+        g.of_table = floats(p.of_table);
+        g.dtable = static_cast<char *>(dtable);
+        g.blocks_q = p.blocks_q;
+        g.blocks_v = p.blocks_v;
+        g.key_tiles = p.key_tiles;
+        g.sink_tiles = p.sink_tiles;
+        g.shares = p.shares;
+        g.sink_shares = p.sink_shares;
+        g.slots = p.slots;
+        hipStream_t st = static_cast<hipStream_t>(stream);
+#define PARO_BACKWARD(DT, HD, BIAS) launch<DT, HD, BIAS>(g, p, st)
+        PARO_BY_FORM(PARO_BACKWARD);
+#undef PARO_BACKWARD
+        PARO_LAUNCHED("paro_attn_grad");
+        return PARO_OK;
+    });
+}
+
+int paro_rel_buckets(int buckets, int64_t max_distance, int32_t *first) {
+    return guarded([&]() -> int {
+        const std::string f = "paro_rel_buckets: ";
+        if (buckets < 1 || buckets > MAX_BUCKETS) return fail(PARO_EINVAL, f + "buckets must be in [1, 256]");
+        const int single = (buckets + 1) / 2, more = buckets - single;
+        if (max_distance < single || max_distance >= FAR_AWAY) return fail(PARO_EINVAL, f + "max_distance must be in [(buckets + 1) / 2, 2^30)");
+        if (!first) return fail(PARO_EINVAL, f + "first is NULL");
+        for (int b = 0; b < single; ++b) first[b] = b;
+        // h (D / h)^(k / m), rounded up; where it is a whole number the power in 64 bits may lie to either side of it
+        for (int k = 0; k < more; ++k) {
+            const long double x = single * std::pow((long double)max_distance / single, (long double)k / more), whole = std::nearbyint(x);
+            first[single + k] = (int32_t)(std::fabs(x - whole) < 1e-12L * x ? whole : std::ceil(x));
+        }
+        return PARO_OK;
+    });
+}
+
+}  // extern "C"

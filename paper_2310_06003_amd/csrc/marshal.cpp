@@ -18,7 +18,7 @@
 
 namespace {
 
-PyObject *g_plan_type, *g_handle_type, *g_adam_type, *g_distill_type, *g_gated_type, *g_check;     // the binding's classes, and its check of a status code
+PyObject *g_plan_type, *g_handle_type, *g_adam_type, *g_distill_type, *g_gated_type, *g_attn_type, *g_check;     // the binding's classes, and its check of a status code
 PyObject *g_handle_name;
 
 // One argument of a call.
@@ -28,11 +28,12 @@ union Arg {
     float real;
 };
 struct Args {
-    Arg a[16];
+    Arg a[20];
     const void *contrib[PARO_MAX_RANKS];
     paro_adam_t hp;
     paro_distill_t distill;
     paro_gated_t gated;
+    paro_attn_t attn;
 };
 
 // Copies `bytes` from an object that lies in memory as its C type does.
@@ -100,7 +101,7 @@ bool plan_of(PyObject *o, void **to) {
     return ok;
 }
 
-// kinds: P plan, i int, n int64_t, f float, c contribution (or buffer) addresses, h hyper-parameters, D distillation, G gated projections, p address
+// kinds: P plan, i int, n int64_t, f float, c contribution (or buffer) addresses, h hyper-parameters, D distillation, G gated projections, A attention, p address
 bool parse(const char *kinds, PyObject *const *args, Py_ssize_t n, Args *out) {
     for (Py_ssize_t k = 0; kinds[k]; ++k) {
         Arg *a = &out->a[k];
@@ -115,6 +116,7 @@ bool parse(const char *kinds, PyObject *const *args, Py_ssize_t n, Args *out) {
             case 'f': ok = real(o, &a->real); break;
             case 'D': ok = (PyObject *)Py_TYPE(o) == g_distill_type && copy_out(o, &out->distill, sizeof(out->distill)); break;
             case 'G': ok = (PyObject *)Py_TYPE(o) == g_gated_type && copy_out(o, &out->gated, sizeof(out->gated)); break;
+            case 'A': ok = (PyObject *)Py_TYPE(o) == g_attn_type && copy_out(o, &out->attn, sizeof(out->attn)); break;
             case 'c': ok = addresses(o, out->contrib); break;
             case 'h': ok = (PyObject *)Py_TYPE(o) == g_adam_type && copy_out(o, &out->hp, sizeof(out->hp)); break;
             case 'p': ok = address(o, &a->ptr); break;
@@ -192,6 +194,15 @@ int64_t call_gated_grad(void *fn, Args &x) {
     return reinterpret_cast<decltype(&paro_gated_grad)>(fn)(&x.gated, x.a[1].ptr, x.a[2].ptr, x.a[3].ptr, x.a[4].ptr, x.a[5].ptr, x.a[6].ptr, x.a[7].ptr,
                                                             x.a[8].ptr, x.a[9].ptr, x.a[10].ptr, x.a[11].num, x.a[12].ptr);
 }
+int64_t call_attn(void *fn, Args &x) {
+    return reinterpret_cast<decltype(&paro_attn)>(fn)(&x.attn, x.a[1].ptr, x.a[2].ptr, x.a[3].ptr, at<int32_t>(x.a[4]), at<int32_t>(x.a[5]), at<int32_t>(x.a[6]),
+                                                      x.a[7].ptr, at<int32_t>(x.a[8]), x.a[9].ptr, at<float>(x.a[10]), x.a[11].ptr, x.a[12].num, x.a[13].ptr);
+}
+int64_t call_attn_grad(void *fn, Args &x) {
+    return reinterpret_cast<decltype(&paro_attn_grad)>(fn)(&x.attn, x.a[1].ptr, x.a[2].ptr, x.a[3].ptr, x.a[4].ptr, x.a[5].ptr, at<float>(x.a[6]), at<int32_t>(x.a[7]),
+                                                           at<int32_t>(x.a[8]), at<int32_t>(x.a[9]), x.a[10].ptr, at<int32_t>(x.a[11]), x.a[12].ptr, x.a[13].ptr,
+                                                           x.a[14].ptr, x.a[15].ptr, x.a[16].ptr, x.a[17].num, x.a[18].ptr);
+}
 
 struct Call {
     const char *name, *kinds, *doc;
@@ -223,6 +234,11 @@ constexpr Call CALLS[] = {
     {"paro_gated", "Gpppppppnp", "paro_gated(d, x, w_gate, w_up, h, gate, up, workspace, workspace_bytes, stream=0)\n--\n\n", 9, call_gated, false},
     {"paro_gated_grad", "Gppppppppppnp",
      "paro_gated_grad(d, dh, gate, up, x, w_gate, w_up, dx, dw_gate, dw_up, workspace, workspace_bytes, stream=0)\n--\n\n", 12, call_gated_grad, false},
+    {"paro_attn", "Apppppppppppnp",
+     "paro_attn(d, q, k, v, q_starts, k_starts, k_lens, table, first, out, stats, workspace, workspace_bytes, stream=0)\n--\n\n", 13, call_attn, false},
+    {"paro_attn_grad", "Appppppppppppppppnp",
+     "paro_attn_grad(d, dout, q, k, v, out, stats, q_starts, k_starts, k_lens, table, first, dq, dk, dv, dtable, workspace, workspace_bytes, stream=0)\n--\n\n",
+     18, call_attn_grad, false},
 };
 constexpr int N_CALLS = sizeof(CALLS) / sizeof(CALLS[0]);
 void *g_fn[N_CALLS];
@@ -318,7 +334,8 @@ PyObject *setup(PyObject *, PyObject *args) {
     }
     PyObject *types[] = {PyObject_GetAttrString(module, "Plan"),        PyObject_GetAttrString(module, "c_void_p"),
                          PyObject_GetAttrString(module, "paro_adam_t"), PyObject_GetAttrString(module, "_check"),
-                         PyObject_GetAttrString(module, "paro_distill_t"), PyObject_GetAttrString(module, "paro_gated_t")};
+                         PyObject_GetAttrString(module, "paro_distill_t"), PyObject_GetAttrString(module, "paro_gated_t"),
+                         PyObject_GetAttrString(module, "paro_attn_t")};
     for (PyObject *t : types)
         if (!t) return nullptr;
     PyObject *out = PyDict_New(), *doc_name = PyUnicode_FromString("paper_2310_06003_amd");
@@ -333,7 +350,7 @@ PyObject *setup(PyObject *, PyObject *args) {
     };
     Args probe;
     if (!fits(types[2], &probe.hp, sizeof(probe.hp), "paro_adam_t") || !fits(types[4], &probe.distill, sizeof(probe.distill), "paro_distill_t") ||
-        !fits(types[5], &probe.gated, sizeof(probe.gated), "paro_gated_t"))
+        !fits(types[5], &probe.gated, sizeof(probe.gated), "paro_gated_t") || !fits(types[6], &probe.attn, sizeof(probe.attn), "paro_attn_t"))
         return nullptr;
     define<0>();
     g_defs[N_CALLS] = {"make_adam", (PyCFunction)(void (*)())make_adam, METH_FASTCALL | METH_KEYWORDS,
@@ -354,6 +371,7 @@ PyObject *setup(PyObject *, PyObject *args) {
     g_check = types[3];
     g_distill_type = types[4];
     g_gated_type = types[5];
+    g_attn_type = types[6];
     g_plan_type = types[0];
     return out;
 }
