@@ -19,7 +19,7 @@ constexpr float SHIFT = DT == PARO_F16 ? 7.0f : 0.0f;
 template <int DT, int HD, bool BIAS>
 __global__ __launch_bounds__(256, 2) void k_attend(Attn a) {
     using T = Tile<HD>;
-    constexpr int BYTES = KEYS * T::ROW, PASSES = KEYS * T::PIECES / 256, STEPS = HD / 16;
+    constexpr int BYTES = KEYS * T::ROW, STEPS = HD / 16;
     __shared__ __attribute__((aligned(1024))) char tiles[2][2][BYTES];       // [buffer][keys, values]
     __shared__ Bias bias;
     __shared__ float by_distance[2][QUERIES + KEYS];
@@ -33,32 +33,22 @@ __global__ __launch_bounds__(256, 2) void k_attend(Attn a) {
     const int of_wave = first + w * 32, place = of_wave + (lane & 31), i = i0 + w * 32 + (lane & 31);     // of the lane's query
     const int kv = head / (a.heads / a.kv_heads);
 
-    // Each thread stages pieces of the same column.
-    const int piece = threadIdx.x % T::PIECES, row = threadIdx.x / T::PIECES;
-    constexpr int APART = 256 / T::PIECES;
-    u32x4 from_k[PASSES], from_v[PASSES];
+    const char *const keys_at = a.k.of(seq.k0, kv), *const values_at = a.v.of(seq.k0, kv);
+    Staged<HD, KEYS> from_k, from_v;
     const auto load = [&](int t) {
         const int k0 = seen.tile(t) * KEYS;
-#pragma unroll
-        for (int n = 0; n < PASSES; ++n) {
-            const int j = k0 + row + n * APART;
-            from_k[n] = from_v[n] = u32x4{0, 0, 0, 0};
-            if (seen.holds(j)) {
-                from_k[n] = piece_of_head(a.k.of((int64_t)seq.k0 + j, kv), piece * 8, a.hd);
-                from_v[n] = piece_of_head(a.v.of((int64_t)seq.k0 + j, kv), piece * 8, a.hd);
-            }
-        }
+        from_k.load(keys_at, a.k.ld, k0, seq.nk, a.hd);
+        from_v.load(values_at, a.v.ld, k0, seq.nk, a.hd);
     };
     int far_from = 0;                       // distances from here on have the last bucket's bias
     float far_bias = 0.0f;
     const auto is_far = [&](int k0) { return BIAS && first - (k0 + KEYS - 1) >= far_from; };
     const auto stage = [&](int t, int buffer) {
-#pragma unroll
-        for (int n = 0; n < PASSES; ++n) {
-            const int at = T::at(row + n * APART, piece);
-            *reinterpret_cast<u32x4 *>(tiles[buffer][0] + at) = from_k[n];
-            *reinterpret_cast<u32x4 *>(tiles[buffer][1] + at) = from_v[n];
-        }
+        const int first_key = seen.tile(t) * KEYS;
+        const auto holds = [&](int r) { return seen.holds(first_key + r); };
+        const bool all = seen.holds_all(first_key);
+        from_k.store(tiles[buffer][0], a.hd, all, holds);
+        from_v.store(tiles[buffer][1], a.hd, all, holds);
         if constexpr (BIAS) {
             const int k0 = seen.tile(t) * KEYS;
             if (!is_far(k0) && threadIdx.x < QUERIES + KEYS - 1) by_distance[buffer][threadIdx.x] = bias.of(first - k0 + QUERIES - 1 - (int)threadIdx.x, a.buckets);
@@ -73,11 +63,10 @@ __global__ __launch_bounds__(256, 2) void k_attend(Attn a) {
         far_bias = bias.column[a.buckets - 1];
     }
     short8_t q[STEPS];
+    const char *const query = a.q.of((int64_t)seq.q0 + (i < seq.nq ? i : seq.nq - 1), head);
 #pragma unroll
     for (int s = 0; s < STEPS; ++s) {
-        u32x4 v{0, 0, 0, 0};
-        if (i < seq.nq) v = piece_of_head(a.q.of((int64_t)seq.q0 + i, head), s * 16 + h * 8, a.hd);
-        q[s] = __builtin_bit_cast(short8_t, v);
+        q[s] = __builtin_bit_cast(short8_t, piece_of_head(query, s * 16 + h * 8, a.hd, i < seq.nq));
     }
     // Scores are kept as they are without a bias (units of `unit` powers of two), and scaled, in natural units, with one: a table may hold a type's lowest
     // number, whose multiple by LOG2E does not exist.
@@ -103,10 +92,17 @@ __global__ __launch_bounds__(256, 2) void k_attend(Attn a) {
             if constexpr (BIAS) {
                 const bool far = is_far(k0);
                 const float *const at = by_distance[buffer] + QUERIES - 1 - (w * 32 + (lane & 31)) + 4 * h;
+                if (far) {
 #pragma unroll
-                for (int n = 0; n < 2; ++n)
+                    for (int n = 0; n < 2; ++n)
 #pragma unroll
-                    for (int e = 0; e < 16; ++e) s[n][e] = s[n][e] * a.scale + (far ? far_bias : at[n * 32 + 8 * (e / 4) + e % 4]);
+                        for (int e = 0; e < 16; ++e) s[n][e] = __builtin_fmaf(s[n][e], a.scale, far_bias);
+                } else {
+#pragma unroll
+                    for (int n = 0; n < 2; ++n)
+#pragma unroll
+                        for (int e = 0; e < 16; ++e) s[n][e] = __builtin_fmaf(s[n][e], a.scale, at[n * 32 + 8 * (e / 4) + e % 4]);
+                }
             }
             const bool all = k0 + KEYS - 1 <= of_wave && (k0 > of_wave + 31 - a.window || k0 + KEYS <= a.sinks);
             if (!all) {
@@ -219,35 +215,25 @@ __global__ __launch_bounds__(64 * FEW_WAVES, NT == 1 ? 2 : 1) void k_attend_few(
         there[n] = r < rows;
         place[n] = off + r / group;
         head[n] = kv * group + r % group;
+        const char *const query = a.q.of((int64_t)seq.q0 + (there[n] ? r / group : 0), kv * group + (there[n] ? r % group : 0));
 #pragma unroll
-        for (int s = 0; s < STEPS; ++s) {
-            u32x4 v{0, 0, 0, 0};
-            if (there[n]) v = piece_of_head(a.q.of((int64_t)seq.q0 + r / group, head[n]), s * 32 + g * 8, a.hd);
-            q[n][s] = __builtin_bit_cast(short8_t, v);
-        }
+        for (int s = 0; s < STEPS; ++s) q[n][s] = __builtin_bit_cast(short8_t, piece_of_head(query, s * 32 + g * 8, a.hd, there[n]));
     }
     u32x4 from_k[2][STEPS], from_v[PASSES];
     const int piece = lane % T::PIECES, of_pass = lane / T::PIECES;
     constexpr int APART = 64 / T::PIECES;
+    const char *const keys_at = a.k.of(seq.k0, kv), *const values_at = a.v.of(seq.k0, kv);
     const auto load = [&](int t) {
         const int k0 = seen.tile(t) * FEW_KEYS;
+        const auto row = [&](const char *at, int64_t ld, int j) { return at + (int64_t)(j < seq.nk ? j : seq.nk - 1) * (ld * 2); };
 #pragma unroll
         for (int n = 0; n < 2; ++n) {
-            const int j = k0 + n * 16 + of16;
-            const bool held = seen.holds(j);
-            const char *const key = a.k.of((int64_t)seq.k0 + j, kv);
+            const char *const key = row(keys_at, a.k.ld, k0 + n * 16 + of16);
 #pragma unroll
-            for (int s = 0; s < STEPS; ++s) {
-                from_k[n][s] = u32x4{0, 0, 0, 0};
-                if (held) from_k[n][s] = piece_of_head(key, s * 32 + g * 8, a.hd);
-            }
+            for (int s = 0; s < STEPS; ++s) from_k[n][s] = raw_piece(key, s * 32 + g * 8, a.hd);
         }
 #pragma unroll
-        for (int n = 0; n < PASSES; ++n) {
-            const int j = k0 + of_pass + n * APART;
-            from_v[n] = u32x4{0, 0, 0, 0};
-            if (seen.holds(j)) from_v[n] = piece_of_head(a.v.of((int64_t)seq.k0 + j, kv), piece * 8, a.hd);
-        }
+        for (int n = 0; n < PASSES; ++n) from_v[n] = raw_piece(row(values_at, a.v.ld, k0 + of_pass + n * APART), piece * 8, a.hd);
     };
     int far_from = 0;
     float far_bias[NT] = {};
@@ -271,6 +257,14 @@ __global__ __launch_bounds__(64 * FEW_WAVES, NT == 1 ? 2 : 1) void k_attend_few(
     char *const mine = values[w];
     for (int t = from + w; t < to; t += FEW_WAVES) {
         const int k0 = seen.tile(t) * FEW_KEYS;
+        if (!seen.holds_all(k0) || a.hd != HD) {
+#pragma unroll
+            for (int n = 0; n < 2; ++n)
+#pragma unroll
+                for (int s = 0; s < STEPS; ++s) from_k[n][s] = finished(from_k[n][s], s * 32 + g * 8, a.hd, seen.holds(k0 + n * 16 + of16));
+#pragma unroll
+            for (int n = 0; n < PASSES; ++n) from_v[n] = finished(from_v[n], piece * 8, a.hd, seen.holds(k0 + of_pass + n * APART));
+        }
         short8_t keys[2][STEPS];
 #pragma unroll
         for (int n = 0; n < 2; ++n)
@@ -316,7 +310,7 @@ __global__ __launch_bounds__(64 * FEW_WAVES, NT == 1 ? 2 : 1) void k_attend_few(
                             const int of = __shfl(bucket, (place[n] - (k0 + k * 16 + 4 * g + e) - lowest) & 63);
                             value = there[n] ? table_value(a, of, head[n]) : 0.0f;
                         }
-                        s[n][k][e] = s[n][k][e] * a.scale + value;
+                        s[n][k][e] = __builtin_fmaf(s[n][k][e], a.scale, value);
                     }
         }
 #pragma unroll
@@ -347,8 +341,8 @@ __global__ __launch_bounds__(64 * FEW_WAVES, NT == 1 ? 2 : 1) void k_attend_few(
             u32x4 packed;
 #pragma unroll
             for (int k = 0; k < 2; ++k) {
-                packed[2 * k] = pack2<DT>(s[n][k][0], s[n][k][1]);
-                packed[2 * k + 1] = pack2<DT>(s[n][k][2], s[n][k][3]);
+                packed[2 * k] = both<DT>(s[n][k][0], s[n][k][1]);
+                packed[2 * k + 1] = both<DT>(s[n][k][2], s[n][k][3]);
             }
             const short8_t p = __builtin_bit_cast(short8_t, packed);
 #pragma unroll

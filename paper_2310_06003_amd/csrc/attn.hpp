@@ -104,6 +104,7 @@ struct Seen {
         if (end == 0) tiles = 0;
     }
     __device__ __forceinline__ int tile(int t) const { return t < sink_tiles ? t : first_tile + t - sink_tiles; }
+    __device__ __forceinline__ bool holds_all(int k0) const { return k0 + KEYS <= end && (k0 >= low || k0 + KEYS <= sinks); }
     __device__ __forceinline__ bool holds(int j) const { return j < end && (j >= low || j < sinks); }
 };
 __device__ __forceinline__ bool sees(int p, int j, int window, int sinks) {
@@ -147,24 +148,95 @@ struct Tile {
     }
 };
 
-// Eight elements of a head's row, from `column` on; what lies behind the head: zeros.
-__device__ __forceinline__ u32x4 piece_of_head(const char *row, int column, int hd) {
-    if (column + 8 <= hd) return load_piece<PARO_BF16>(row, column);
-    u32x4 v{0, 0, 0, 0};
+// Eight elements of a head's row, from `column` on; what lies behind the head: zeros.  One load without a branch: a piece that reaches past the head's end is read
+// from eight elements in front of that, and shifted.  (Branches for each element cost more than the products: 1999 tokens of 10 heads of 77 forward 93 us.)
+// The row has to exist also where the piece is not wanted.
+__device__ __forceinline__ u32x4 shifted(u32x4 v, int elements) {          // towards the first, by 0 to 7
+    if (elements & 4) v = u32x4{v[2], v[3], 0, 0};
+    if (elements & 2) v = u32x4{v[1], v[2], v[3], 0};
+    if (elements & 1) {
 #pragma unroll
-    for (int e = 0; e < 8; ++e)
-        if (column + e < hd) v[e / 2] |= (unsigned)reinterpret_cast<const unsigned short *>(row)[column + e] << (16 * (e & 1));
+        for (int i = 0; i < 4; ++i) v[i] = __builtin_amdgcn_alignbit(i < 3 ? v[i + 1] : 0, v[i], 16);
+    }
     return v;
 }
+__device__ __forceinline__ u32x4 short_row(const char *row, int column, int hd) {          // heads of less than eight elements
+    uint64_t lo = 0, hi = 0;
+#pragma unroll 1
+    for (int e = 0; column + e < hd; ++e) {
+        const uint64_t x = reinterpret_cast<const unsigned short *>(row)[column + e];
+        if (e < 4) lo |= x << (16 * e);
+        else hi |= x << (16 * (e - 4));
+    }
+    return u32x4{(unsigned)lo, (unsigned)(lo >> 32), (unsigned)hi, (unsigned)(hi >> 32)};
+}
+__device__ __forceinline__ u32x4 raw_piece(const char *row, int column, int hd) {
+    if (hd < 8) return short_row(row, column, hd);
+    return load_piece<PARO_BF16>(row, column < hd - 8 ? column : hd - 8);
+}
+__device__ __forceinline__ u32x4 finished(u32x4 v, int column, int hd, bool there) {       // of raw_piece
+    if ((hd & 7) && hd >= 8 && column > hd - 8) v = shifted(v, (column - (hd - 8)) & 7);
+    there = there && column < hd;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) v[i] = there ? v[i] : 0;
+    return v;
+}
+__device__ __forceinline__ u32x4 piece_of_head(const char *row, int column, int hd, bool there) { return finished(raw_piece(row, column, hd), column, hd, there); }
 __device__ __forceinline__ void store_piece_of_head(char *row, int column, int hd, u32x4 v) {
     if (column + 8 <= hd) {
         store_piece<PARO_BF16>(row, column, v);
         return;
     }
-#pragma unroll
-    for (int e = 0; e < 8; ++e)
-        if (column + e < hd) reinterpret_cast<unsigned short *>(row)[column + e] = (unsigned short)(v[e / 2] >> (16 * (e & 1)));
+    uint64_t lo = (uint64_t)v[1] << 32 | v[0], hi = (uint64_t)v[3] << 32 | v[2];
+#pragma unroll 1
+    for (int e = column; e < hd; ++e) {
+        reinterpret_cast<unsigned short *>(row)[e] = (unsigned short)lo;
+        lo = lo >> 16 | hi << 48;
+        hi >>= 16;
+    }
 }
+
+// Two floats rounded to nearest even by one instruction.
+typedef float f32x2 __attribute__((ext_vector_type(2)));
+typedef __bf16 bf16x2_t __attribute__((ext_vector_type(2)));
+typedef _Float16 f16x2_t __attribute__((ext_vector_type(2)));
+template <int DT>
+__device__ __forceinline__ unsigned both(float a, float b) {
+    if constexpr (DT == PARO_F16) return __builtin_bit_cast(unsigned, __builtin_convertvector(f32x2{a, b}, f16x2_t));
+    else return __builtin_bit_cast(unsigned, __builtin_convertvector(f32x2{a, b}, bf16x2_t));
+}
+
+// A tile of rows on its way from memory to shared memory: each thread takes pieces of one column, PASSES rows.  Rows that the tile does not hold are read as others
+// of the sequence and staged as zeros.
+template <int HD, int ROWS>
+struct Staged {
+    using T = Tile<HD>;
+    static constexpr int APART = 256 / T::PIECES, PASSES = ROWS / APART;
+    static_assert(PASSES >= 1 && ROWS % APART == 0, "every thread takes a piece of every pass");
+    u32x4 v[PASSES];
+
+    static __device__ __forceinline__ int column() { return (int)threadIdx.x % T::PIECES * 8; }
+    static __device__ __forceinline__ int row(int n) { return (int)threadIdx.x / T::PIECES + n * APART; }
+    // row r of the tile is the sequence's row0 + r; `rows` of them exist (one at least)
+    __device__ __forceinline__ void load(const char *of_head, int64_t ld, int row0, int rows, int hd) {
+#pragma unroll
+        for (int n = 0; n < PASSES; ++n) {
+            const int r = row0 + row(n);
+            v[n] = raw_piece(of_head + (int64_t)(r < rows ? r : rows - 1) * (ld * 2), column(), hd);
+        }
+    }
+    // holds(row of the tile): whether it is there;  all: every row is
+    template <class F>
+    __device__ __forceinline__ void store(char *tile, int hd, bool all, F &&holds) {
+        if (!all || hd != HD) {
+#pragma unroll
+            for (int n = 0; n < PASSES; ++n) v[n] = finished(v[n], column(), hd, all || holds(row(n)));
+        }
+#pragma unroll
+        for (int n = 0; n < PASSES; ++n) *reinterpret_cast<u32x4 *>(tile + T::at(row(n), column() / 8)) = v[n];
+    }
+};
+
 // A row of 32 of the result of 32 x 32 products: a lane has of its row (lane % 32) the elements 8 * (i / 4) + 4 * (lane / 32) + i % 4.  Both halves of a
 // wave exchange, so that each stores eight in a row.
 template <int DT>
@@ -172,8 +244,8 @@ __device__ __forceinline__ void store_row32(char *row, int column, int hd, const
     const int h = (threadIdx.x >> 5) & 1;
 #pragma unroll
     for (int i = 0; i < 16; i += 8) {
-        const unsigned a0 = pack2<DT>(x[i] * times, x[i + 1] * times), a1 = pack2<DT>(x[i + 2] * times, x[i + 3] * times);
-        const unsigned b0 = pack2<DT>(x[i + 4] * times, x[i + 5] * times), b1 = pack2<DT>(x[i + 6] * times, x[i + 7] * times);
+        const unsigned a0 = both<DT>(x[i] * times, x[i + 1] * times), a1 = both<DT>(x[i + 2] * times, x[i + 3] * times);
+        const unsigned b0 = both<DT>(x[i + 4] * times, x[i + 5] * times), b1 = both<DT>(x[i + 6] * times, x[i + 7] * times);
         const auto s0 = __builtin_amdgcn_permlane32_swap(a0, b0, false, false), s1 = __builtin_amdgcn_permlane32_swap(a1, b1, false, false);
         if (there) store_piece_of_head(row, column + 2 * i + 8 * h, hd, u32x4{s0[0], s1[0], s0[1], s1[1]});
     }
@@ -182,7 +254,7 @@ template <int DT>
 __device__ __forceinline__ short8_t pack8(const f32x16 &x, int from) {
     u32x4 v;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) v[i] = pack2<DT>(x[from + 2 * i], x[from + 2 * i + 1]);
+    for (int i = 0; i < 4; ++i) v[i] = both<DT>(x[from + 2 * i], x[from + 2 * i + 1]);
     return __builtin_bit_cast(short8_t, v);
 }
 

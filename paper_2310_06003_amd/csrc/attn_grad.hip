@@ -14,7 +14,7 @@
 namespace {
 
 constexpr int BLOCK = 128;                   // keys of a k_grad_kv block, queries of a k_grad_q block: 32 a wave
-constexpr int Q_STEP = 32, K_STEP = 64;      // queries, keys of a tile
+constexpr int Q_STEP = 32;                   // queries of a tile
 constexpr int MOST_SHARES = 64;
 template <int DT>
 constexpr float SHIFT = DT == PARO_F16 ? 15.0f : 0.0f;
@@ -59,10 +59,10 @@ __global__ __launch_bounds__(256) void k_dots(Grad g) {
         float u[8], o[8];
         float squares = 0.0f, dot = 0.0f;
         if (of_values) {
-            unpack<DT>(piece_of_head(a.v.of((int64_t)seq.k0 + i, head), piece * 8, a.hd), u);
+            unpack<DT>(piece_of_head(a.v.of((int64_t)seq.k0 + i, head), piece * 8, a.hd, true), u);
         } else {
-            unpack<DT>(piece_of_head(g.dout.of((int64_t)seq.q0 + i, head), piece * 8, a.hd), u);
-            unpack<DT>(piece_of_head(a.out.of((int64_t)seq.q0 + i, head), piece * 8, a.hd), o);
+            unpack<DT>(piece_of_head(g.dout.of((int64_t)seq.q0 + i, head), piece * 8, a.hd, true), u);
+            unpack<DT>(piece_of_head(a.out.of((int64_t)seq.q0 + i, head), piece * 8, a.hd, true), o);
 #pragma unroll
             for (int e = 0; e < 8; ++e) dot += u[e] * o[e];
         }
@@ -151,12 +151,12 @@ __device__ __forceinline__ Share share_of(const Grad &g, int block, int of_kv) {
 }
 
 template <int DT, int HD, bool BIAS>
-__global__ __launch_bounds__(256, 1) void k_grad_kv(Grad g) {
+__global__ __launch_bounds__(256, 2) void k_grad_kv(Grad g) {
     using T = Tile<HD>;
     const Attn &a = g.a;
-    constexpr int BYTES = Q_STEP * T::ROW, PASSES = Q_STEP * T::PIECES / 256, STEPS = HD / 16, APART = 256 / T::PIECES;
-    static_assert(PASSES >= 1, "every thread stages a piece");
+    constexpr int BYTES = Q_STEP * T::ROW, STEPS = HD / 16;
     __shared__ __attribute__((aligned(1024))) char tiles[2][2][BYTES];         // [buffer][queries, dout]
+    __shared__ __attribute__((aligned(1024))) char values[BLOCK * T::ROW];
     __shared__ float rows[2][3][Q_STEP];                                       // [buffer][base, log_sum, dots]
     __shared__ Bias bias;
     __shared__ float by_distance[2][BLOCK + Q_STEP];
@@ -177,20 +177,14 @@ __global__ __launch_bounds__(256, 1) void k_grad_kv(Grad g) {
     const int64_t all = (int64_t)per_head * group;
     const int from = (int)(all * share.share / share.shares), to = (int)(all * (share.share + 1) / share.shares);
 
-    const int piece = threadIdx.x % T::PIECES, row = threadIdx.x / T::PIECES;
-    u32x4 from_q[PASSES], from_o[PASSES];
+    // The next step's head, and its first query.
+    Staged<HD, Q_STEP> from_q, from_o;
     float from_row = 0.0f;
-    const auto load = [&](int u) {
-        const int head = kv * group + u / per_head, i0 = (tile0 + u % per_head) * Q_STEP;
-#pragma unroll
-        for (int n = 0; n < PASSES; ++n) {
-            const int i = i0 + row + n * APART;
-            from_q[n] = from_o[n] = u32x4{0, 0, 0, 0};
-            if (i < seq.nq) {
-                from_q[n] = piece_of_head(a.q.of((int64_t)seq.q0 + i, head), piece * 8, a.hd);
-                from_o[n] = piece_of_head(g.dout.of((int64_t)seq.q0 + i, head), piece * 8, a.hd);
-            }
-        }
+    int next_head = 0, next_tile = 0;
+    const auto load = [&]() {
+        const int head = kv * group + next_head, i0 = (tile0 + next_tile) * Q_STEP;
+        from_q.load(a.q.of(seq.q0, head), a.q.ld, i0, seq.nq, a.hd);
+        from_o.load(g.dout.of(seq.q0, head), g.dout.ld, i0, seq.nq, a.hd);
         if (threadIdx.x < 3 * Q_STEP && (BIAS || threadIdx.x < Q_STEP || threadIdx.x >= 2 * Q_STEP)) {
             const int i = i0 + threadIdx.x % Q_STEP, which = threadIdx.x / Q_STEP;
             const float *const of = which == 0 ? g.base : which == 1 ? g.log_sum : g.dots;
@@ -200,16 +194,13 @@ __global__ __launch_bounds__(256, 1) void k_grad_kv(Grad g) {
     int far_from = 0, of_head = -1;
     float far_bias = 0.0f, next_far_bias = 0.0f;
     const auto is_far = [&](int i0) { return BIAS && off + i0 - (k0 + BLOCK - 1) >= far_from; };
-    const auto stage = [&](int u, int buffer) {
-#pragma unroll
-        for (int n = 0; n < PASSES; ++n) {
-            const int at = T::at(row + n * APART, piece);
-            *reinterpret_cast<u32x4 *>(tiles[buffer][0] + at) = from_q[n];
-            *reinterpret_cast<u32x4 *>(tiles[buffer][1] + at) = from_o[n];
-        }
+    const auto stage = [&](int buffer) {
+        const int head = kv * group + next_head, i0 = (tile0 + next_tile) * Q_STEP;
+        const auto holds = [&](int r) { return i0 + r < seq.nq; };
+        from_q.store(tiles[buffer][0], a.hd, i0 + Q_STEP <= seq.nq, holds);
+        from_o.store(tiles[buffer][1], a.hd, i0 + Q_STEP <= seq.nq, holds);
         if (threadIdx.x < 3 * Q_STEP) rows[buffer][threadIdx.x / Q_STEP][threadIdx.x % Q_STEP] = from_row;
         if constexpr (BIAS) {
-            const int head = kv * group + u / per_head, i0 = (tile0 + u % per_head) * Q_STEP;
             if (head != of_head) {
                 __syncthreads();
                 bias.load(a, head);
@@ -222,27 +213,33 @@ __global__ __launch_bounds__(256, 1) void k_grad_kv(Grad g) {
         }
     };
 
-    short8_t keys[STEPS], values[STEPS];
+    // The wave's keys stay in registers, its values (two blocks a compute unit leave no registers for them) in shared memory.
+    short8_t keys[STEPS];
+    {
+        const int at = j < seq.nk ? j : seq.nk - 1;
+        const char *const key = a.k.of((int64_t)seq.k0 + at, kv), *const value = a.v.of((int64_t)seq.k0 + at, kv);
 #pragma unroll
-    for (int s = 0; s < STEPS; ++s) {
-        u32x4 x{0, 0, 0, 0}, y{0, 0, 0, 0};
-        if (j < seq.nk) {
-            x = piece_of_head(a.k.of((int64_t)seq.k0 + j, kv), s * 16 + h * 8, a.hd);
-            y = piece_of_head(a.v.of((int64_t)seq.k0 + j, kv), s * 16 + h * 8, a.hd);
+        for (int s = 0; s < STEPS; ++s) {
+            keys[s] = __builtin_bit_cast(short8_t, piece_of_head(key, s * 16 + h * 8, a.hd, j < seq.nk));
+            *reinterpret_cast<u32x4 *>(values + w * 32 * T::ROW + T::at(lane & 31, 2 * s + h)) = piece_of_head(value, s * 16 + h * 8, a.hd, j < seq.nk);
         }
-        keys[s] = __builtin_bit_cast(short8_t, x);
-        values[s] = __builtin_bit_cast(short8_t, y);
     }
     const float unit = a.scale * LOG2E, times = DT == PARO_F16 ? g.times[0] * 0x1p-15f : 1.0f;
     f32x16 dk[HD / 32] = {}, dv[HD / 32] = {};
     if (from < to) {
-        load(from);
-        stage(from, 0);
+        next_head = from / per_head;
+        next_tile = from % per_head;
+        load();
+        stage(0);
     }
     for (int u = from; u < to; ++u) {
-        const int i0 = (tile0 + u % per_head) * Q_STEP, buffer = (u - from) & 1, first = off + i0;
+        const int i0 = (tile0 + next_tile) * Q_STEP, buffer = (u - from) & 1, first = off + i0;
         far_bias = next_far_bias;
-        if (u + 1 < to) load(u + 1);
+        if (++next_tile == per_head) {
+            next_tile = 0;
+            ++next_head;
+        }
+        if (u + 1 < to) load();
         __syncthreads();
         const char *const queries = tiles[buffer][0], *const douts = tiles[buffer][1];
         const bool none = first + Q_STEP - 1 < of_wave || (first - (of_wave + 31) >= a.window && of_wave >= a.sinks);
@@ -251,13 +248,18 @@ __global__ __launch_bounds__(256, 1) void k_grad_kv(Grad g) {
 #pragma unroll
             for (int c = 0; c < STEPS; ++c) s = mfma32<DT>(T::rows(queries, 0, c, lane), keys[c], s);
 #pragma unroll
-            for (int c = 0; c < STEPS; ++c) dp = mfma32<DT>(T::rows(douts, 0, c, lane), values[c], dp);
+            for (int c = 0; c < STEPS; ++c) dp = mfma32<DT>(T::rows(douts, 0, c, lane), T::rows(values, w * 32, c, lane), dp);
             const bool every = first >= of_wave + 31 && (first + Q_STEP - 1 - of_wave < a.window || of_wave + 31 < a.sinks);
             if constexpr (BIAS) {
                 const bool far = is_far(i0);
                 const float *const at = by_distance[buffer] + BLOCK - 1 - (w * 32 + (lane & 31)) + 4 * h;
+                if (far) {
 #pragma unroll
-                for (int e = 0; e < 16; ++e) s[e] = s[e] * a.scale + (far ? far_bias : at[8 * (e / 4) + e % 4]);
+                    for (int e = 0; e < 16; ++e) s[e] = __builtin_fmaf(s[e], a.scale, far_bias);
+                } else {
+#pragma unroll
+                    for (int e = 0; e < 16; ++e) s[e] = __builtin_fmaf(s[e], a.scale, at[8 * (e / 4) + e % 4]);
+                }
             }
             if (!every) {
 #pragma unroll
@@ -286,7 +288,7 @@ __global__ __launch_bounds__(256, 1) void k_grad_kv(Grad g) {
                 }
             }
         }
-        if (u + 1 < to) stage(u + 1, buffer ^ 1);
+        if (u + 1 < to) stage(buffer ^ 1);
     }
     if (share.slot >= 0) {
         float *const at = g.partial + ((int64_t)share.slot * 2 * BLOCK + w * 32 + (lane & 31)) * HD + 4 * h;
@@ -338,11 +340,13 @@ template <int DT, int HD, bool BIAS>
 __global__ __launch_bounds__(256, 2) void k_grad_q(Grad g) {
     using T = Tile<HD>;
     const Attn &a = g.a;
-    constexpr int BYTES = K_STEP * T::ROW, PASSES = K_STEP * T::PIECES / 256, STEPS = HD / 16, APART = 256 / T::PIECES, DISTANCES = 32 + K_STEP;
+    constexpr int KEYS = BIAS && HD == 128 ? 32 : 64;                           // of a tile: what lets two blocks into the shared memory
+    constexpr int BYTES = KEYS * T::ROW, STEPS = HD / 16, DISTANCES = 32 + KEYS, SQUARE = 36;
     __shared__ __attribute__((aligned(1024))) char tiles[2][2][BYTES];          // [buffer][keys, values]
     __shared__ Bias bias;
-    __shared__ float by_distance[2][BLOCK + K_STEP];
-    __shared__ float diagonals[BIAS ? 4 : 1][2][DISTANCES];                     // [wave][half]: sums of dS along a distance, of one tile
+    __shared__ float by_distance[2][BLOCK + KEYS];
+    __shared__ __attribute__((aligned(16))) float squares[BIAS ? 4 : 1][BIAS ? 32 * SQUARE : 4];     // [wave]: 32 x 32 of dS
+    __shared__ float diagonals[BIAS ? 4 : 1][DISTANCES];                        // [wave]: sums of dS along a distance, of one tile
     __shared__ float of_buckets[BIAS ? 4 : 1][BIAS ? MAX_BUCKETS : 1], far_sums[4];
     const unsigned work = in_runs(blockIdx.x, gridDim.x), of_head = work / a.tiles;
     const int head = of_head % a.heads, b = of_head / a.heads, tile = a.tiles - 1 - work % a.tiles, i0 = tile * BLOCK;
@@ -356,36 +360,28 @@ __global__ __launch_bounds__(256, 2) void k_grad_q(Grad g) {
     }
     const int lane = threadIdx.x & 63, w = wave_of(), h = lane >> 5;
     const int off = seq.nk - seq.nq, first = i0 + off, last = (i0 + BLOCK < seq.nq ? i0 + BLOCK : seq.nq) - 1 + off;
-    const Seen<K_STEP> seen(a, first, last);
+    const Seen<KEYS> seen(a, first, last);
     const int of_wave = first + w * 32, place = of_wave + (lane & 31), i = i0 + w * 32 + (lane & 31);
     const int kv = head / (a.heads / a.kv_heads);
-    const int piece = threadIdx.x % T::PIECES, row = threadIdx.x / T::PIECES;
-    u32x4 from_k[PASSES], from_v[PASSES];
+    const char *const keys_at = a.k.of(seq.k0, kv), *const values_at = a.v.of(seq.k0, kv);
+    Staged<HD, KEYS> from_k, from_v;
     const auto load = [&](int t) {
-        const int k0 = seen.tile(t) * K_STEP;
-#pragma unroll
-        for (int n = 0; n < PASSES; ++n) {
-            const int j = k0 + row + n * APART;
-            from_k[n] = from_v[n] = u32x4{0, 0, 0, 0};
-            if (seen.holds(j)) {
-                from_k[n] = piece_of_head(a.k.of((int64_t)seq.k0 + j, kv), piece * 8, a.hd);
-                from_v[n] = piece_of_head(a.v.of((int64_t)seq.k0 + j, kv), piece * 8, a.hd);
-            }
-        }
+        const int k0 = seen.tile(t) * KEYS;
+        from_k.load(keys_at, a.k.ld, k0, seq.nk, a.hd);
+        from_v.load(values_at, a.v.ld, k0, seq.nk, a.hd);
     };
     int far_from = 0;
     float far_bias = 0.0f, far_sum = 0.0f;
-    const auto is_far = [&](int k0) { return BIAS && first - (k0 + K_STEP - 1) >= far_from; };
+    const auto is_far = [&](int k0) { return BIAS && first - (k0 + KEYS - 1) >= far_from; };
     const auto stage = [&](int t, int buffer) {
-#pragma unroll
-        for (int n = 0; n < PASSES; ++n) {
-            const int at = T::at(row + n * APART, piece);
-            *reinterpret_cast<u32x4 *>(tiles[buffer][0] + at) = from_k[n];
-            *reinterpret_cast<u32x4 *>(tiles[buffer][1] + at) = from_v[n];
-        }
+        const int first_key = seen.tile(t) * KEYS;
+        const auto holds = [&](int r) { return seen.holds(first_key + r); };
+        const bool all = seen.holds_all(first_key);
+        from_k.store(tiles[buffer][0], a.hd, all, holds);
+        from_v.store(tiles[buffer][1], a.hd, all, holds);
         if constexpr (BIAS) {
-            const int k0 = seen.tile(t) * K_STEP;
-            if (!is_far(k0) && threadIdx.x < BLOCK + K_STEP - 1) by_distance[buffer][threadIdx.x] = bias.of(first - k0 + BLOCK - 1 - (int)threadIdx.x, a.buckets);
+            const int k0 = seen.tile(t) * KEYS;
+            if (!is_far(k0) && threadIdx.x < BLOCK + KEYS - 1) by_distance[buffer][threadIdx.x] = bias.of(first - k0 + BLOCK - 1 - (int)threadIdx.x, a.buckets);
         }
     };
     if (seen.tiles) load(0);
@@ -404,33 +400,31 @@ __global__ __launch_bounds__(256, 2) void k_grad_q(Grad g) {
         dot = g.dots[at];
         if constexpr (BIAS) log_sum = g.log_sum[at];
     }
+    {
+        const int at = i < seq.nq ? i : seq.nq - 1;
+        const char *const query = a.q.of((int64_t)seq.q0 + at, head), *const grad = g.dout.of((int64_t)seq.q0 + at, head);
 #pragma unroll
-    for (int s = 0; s < STEPS; ++s) {
-        u32x4 x{0, 0, 0, 0}, y{0, 0, 0, 0};
-        if (i < seq.nq) {
-            x = piece_of_head(a.q.of((int64_t)seq.q0 + i, head), s * 16 + h * 8, a.hd);
-            y = piece_of_head(g.dout.of((int64_t)seq.q0 + i, head), s * 16 + h * 8, a.hd);
+        for (int s = 0; s < STEPS; ++s) {
+            q[s] = __builtin_bit_cast(short8_t, piece_of_head(query, s * 16 + h * 8, a.hd, i < seq.nq));
+            dout[s] = __builtin_bit_cast(short8_t, piece_of_head(grad, s * 16 + h * 8, a.hd, i < seq.nq));
         }
-        q[s] = __builtin_bit_cast(short8_t, x);
-        dout[s] = __builtin_bit_cast(short8_t, y);
     }
     const float unit = a.scale * LOG2E, times = DT == PARO_F16 ? g.times[0] * 0x1p-15f : 1.0f;
     f32x16 dq[HD / 32] = {};
     if (seen.tiles) stage(0, 0);
     for (int t = 0; t < seen.tiles; ++t) {
-        const int k0 = seen.tile(t) * K_STEP, buffer = t & 1;
+        const int k0 = seen.tile(t) * KEYS, buffer = t & 1;
         if (t + 1 < seen.tiles) load(t + 1);
         __syncthreads();
         const char *const keys = tiles[buffer][0], *const values = tiles[buffer][1];
-        const bool none = k0 > of_wave + 31 || (k0 + K_STEP <= of_wave - a.window + 1 && k0 >= a.sinks), far = is_far(k0);
+        const bool none = k0 > of_wave + 31 || (k0 + KEYS <= of_wave - a.window + 1 && k0 >= a.sinks), far = is_far(k0);
         if (want && !far) {
-#pragma unroll
-            for (int x = 0; x < 2 * DISTANCES; x += 64) (&diagonals[BIAS ? w : 0][0][0])[x + lane] = 0.0f;
+            for (int x = lane; x < DISTANCES; x += 64) diagonals[BIAS ? w : 0][x] = 0.0f;
         }
         if (!none) {
-            const bool every = k0 + K_STEP - 1 <= of_wave && (k0 > of_wave + 31 - a.window || k0 + K_STEP <= a.sinks);
+            const bool every = k0 + KEYS - 1 <= of_wave && (k0 > of_wave + 31 - a.window || k0 + KEYS <= a.sinks);
 #pragma unroll
-            for (int n = 0; n < 2; ++n) {
+            for (int n = 0; n < KEYS / 32; ++n) {
                 f32x16 s = {}, dp = {};
 #pragma unroll
                 for (int c = 0; c < STEPS; ++c) s = mfma32<DT>(T::rows(keys, n * 32, c, lane), q[c], s);
@@ -438,8 +432,13 @@ __global__ __launch_bounds__(256, 2) void k_grad_q(Grad g) {
                 for (int c = 0; c < STEPS; ++c) dp = mfma32<DT>(T::rows(values, n * 32, c, lane), dout[c], dp);
                 if constexpr (BIAS) {
                     const float *const at = by_distance[buffer] + BLOCK - 1 - (w * 32 + (lane & 31)) + 4 * h + n * 32;
+                    if (far) {
 #pragma unroll
-                    for (int e = 0; e < 16; ++e) s[e] = s[e] * a.scale + (far ? far_bias : at[8 * (e / 4) + e % 4]);
+                        for (int e = 0; e < 16; ++e) s[e] = __builtin_fmaf(s[e], a.scale, far_bias);
+                    } else {
+#pragma unroll
+                        for (int e = 0; e < 16; ++e) s[e] = __builtin_fmaf(s[e], a.scale, at[8 * (e / 4) + e % 4]);
+                    }
                 }
                 if (!every) {
 #pragma unroll
@@ -456,10 +455,30 @@ __global__ __launch_bounds__(256, 2) void k_grad_q(Grad g) {
 #pragma unroll
                         for (int e = 0; e < 16; ++e) far_sum += dp[e];
                     } else if (want) {
-                        // the lanes of a half have 32 different distances each time, and halves an array each: every place is added to in the order of e and n
-                        float *const at = diagonals[w][h] + K_STEP - 1 + (lane & 31) - (n * 32 + 4 * h);
+                        // Through shared memory (the wave's own, whose accesses go in their order): lane r of a half has of each of its 16 rows the key r in front of
+                        // the row, modulo 32, which are two distances.  (LDS atomics instead: 8 x 1024 tokens of 12 heads of 64 this kernel 214 us.)
+                        float *const square = squares[w];
+                        asm volatile("" ::: "memory");
 #pragma unroll
-                        for (int e = 0; e < 16; ++e) __hip_atomic_fetch_add(at - (8 * (e / 4) + e % 4), dp[e], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP);
+                        for (int e = 0; e < 16; e += 4)
+                            *reinterpret_cast<f32x4 *>(square + (lane & 31) * SQUARE + 2 * e + 4 * h) = f32x4{dp[e], dp[e + 1], dp[e + 2], dp[e + 3]};
+                        asm volatile("" ::: "memory");
+                        float near = 0.0f, behind = 0.0f;                       // distances r, and r - 32, from the square's first row and key
+                        const int r = lane & 31;
+#pragma unroll
+                        for (int y = 0; y < 16; ++y) {
+                            const int row = h * 16 + y;
+                            const float x = square[row * SQUARE + ((row - r) & 31)];
+                            near += row >= r ? x : 0.0f;
+                            behind += row >= r ? 0.0f : x;
+                        }
+                        near = sum_of_halves(near);
+                        behind = sum_of_halves(behind);
+                        // place KEYS - 1 - n * 32 + distance; behind: of r = 0 there is none
+                        const int place_of = KEYS - 1 - n * 32 + (h ? r - 32 : r);
+                        asm volatile("" ::: "memory");
+                        if (!h || r) diagonals[w][place_of] += h ? behind : near;
+                        asm volatile("" ::: "memory");
                     }
                 }
 #pragma unroll
@@ -473,13 +492,13 @@ __global__ __launch_bounds__(256, 2) void k_grad_q(Grad g) {
         if constexpr (BIAS) {
             if (want && !far) {
                 __syncthreads();
-                // thread x has the distance first - (k0 + K_STEP - 1) + x of the tile; buckets are runs of distances, whose sums the last lane of a run adds
-                const int x = threadIdx.x, d = first - (k0 + K_STEP - 1) + x;
+                // thread x has the distance first - (k0 + KEYS - 1) + x of the tile; buckets are runs of distances, whose sums the last lane of a run adds
+                const int x = threadIdx.x, d = first - (k0 + KEYS - 1) + x;
                 float sum = 0.0f;
 #pragma unroll
                 for (int v = 0; v < 4; ++v)
-                    if (x >= v * 32 && x < v * 32 + DISTANCES) sum += diagonals[v][0][x - v * 32] + diagonals[v][1][x - v * 32];
-                const int bucket = d < 0 || x >= BLOCK + K_STEP ? -1 : bias.bucket(d, a.buckets);
+                    if (x >= v * 32 && x < v * 32 + DISTANCES) sum += diagonals[v][x - v * 32];
+                const int bucket = d < 0 || x >= BLOCK + KEYS ? -1 : bias.bucket(d, a.buckets);
 #pragma unroll
                 for (int n = 1; n < 64; n *= 2) {
                     const float before = __shfl_up(sum, n);
