@@ -422,10 +422,10 @@ int paro_gated_grad(const paro_gated_t *d, const void *dh, const void *gate, con
  * PARO_F32.  A bias of -inf hides; a row of a type's lowest number is one like others.  buckets == 0: none, table and first are not looked at.
  * stats: NULL, or fp32 [rows_q][heads][2] = the largest score and the log of the sum of exp(score - largest); -inf and 0 where no key is seen. */
 typedef struct {
-    int64_t batch, heads, kv_heads, head_dim;       /* kv_heads divides heads; head_dim <= 128 */
+    int64_t batch, heads, kv_heads, head_dim;       /* kv_heads divides heads; head_dim in [8, 128] */
     int64_t len_q, len_k;                           /* of the longest sequence */
     int64_t rows_q, rows_k;                         /* of the arrays, 0 = batch * len */
-    int64_t ld_q, ld_k, ld_v, ld_out;               /* elements from token to token, 0 = dense */
+    int64_t ld_q, ld_k, ld_v, ld_out;               /* elements from token to token, 0 = dense; at most 2^24 */
     int64_t head_q, head_k, head_v, head_out;       /* from head to head, 0 = head_dim */
     int64_t window, sinks;
     float scale;

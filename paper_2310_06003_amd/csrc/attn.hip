@@ -11,7 +11,7 @@
 
 namespace {
 
-constexpr int QUERIES = 128, KEYS = 64;      // of a block, of a tile
+constexpr int QUERIES = 128, KEYS = 32;      // of a block, of a tile
 constexpr float GROWS = 8.0f;                // powers of two that a row's shares may exceed one by
 template <int DT>
 constexpr float SHIFT = DT == PARO_F16 ? 7.0f : 0.0f;
@@ -19,10 +19,10 @@ constexpr float SHIFT = DT == PARO_F16 ? 7.0f : 0.0f;
 template <int DT, int HD, bool BIAS>
 __global__ __launch_bounds__(256, 2) void k_attend(Attn a) {
     using T = Tile<HD>;
-    constexpr int BYTES = KEYS * T::ROW, STEPS = HD / 16;
-    __shared__ __attribute__((aligned(1024))) char tiles[2][2][BYTES];       // [buffer][keys, values]
+    constexpr int BYTES = KEYS * T::ROW, STEPS = HD / 16, RING = 4;
+    __shared__ __attribute__((aligned(1024))) char tiles[RING][2][BYTES];    // [part of the ring][keys, values]
     __shared__ Bias bias;
-    __shared__ float by_distance[2][QUERIES + KEYS];
+    __shared__ float by_distance[RING][QUERIES + KEYS];
     const unsigned work = in_runs(blockIdx.x, gridDim.x), of_head = work / a.tiles;
     const int head = of_head % a.heads, b = of_head / a.heads, i0 = (int)(a.tiles - 1 - work % a.tiles) * QUERIES;     // the longest first
     const Sequence seq(a, b);
@@ -35,7 +35,7 @@ __global__ __launch_bounds__(256, 2) void k_attend(Attn a) {
 
     const char *const keys_at = a.k.of(seq.k0, kv), *const values_at = a.v.of(seq.k0, kv);
     Staged<HD, KEYS> from_k, from_v;
-    const auto load = [&](int t) {
+    const auto load = [&](int t) __attribute__((always_inline)) {
         const int k0 = seen.tile(t) * KEYS;
         from_k.load(keys_at, a.k.ld, k0, seq.nk, a.hd);
         from_v.load(values_at, a.v.ld, k0, seq.nk, a.hd);
@@ -43,16 +43,16 @@ __global__ __launch_bounds__(256, 2) void k_attend(Attn a) {
     int far_from = 0;                       // distances from here on have the last bucket's bias
     float far_bias = 0.0f;
     const auto is_far = [&](int k0) { return BIAS && first - (k0 + KEYS - 1) >= far_from; };
-    const auto stage = [&](int t, int buffer) {
+    const auto stage_bias = [&](int k0, int part) __attribute__((always_inline)) {
+        if (!is_far(k0) && threadIdx.x < QUERIES + KEYS - 1) by_distance[part][threadIdx.x] = bias.of(first - k0 + QUERIES - 1 - (int)threadIdx.x, a.buckets);
+    };
+    const auto stage = [&](int t, int part) __attribute__((always_inline)) {
         const int first_key = seen.tile(t) * KEYS;
         const auto holds = [&](int r) { return seen.holds(first_key + r); };
         const bool all = seen.holds_all(first_key);
-        from_k.store(tiles[buffer][0], a.hd, all, holds);
-        from_v.store(tiles[buffer][1], a.hd, all, holds);
-        if constexpr (BIAS) {
-            const int k0 = seen.tile(t) * KEYS;
-            if (!is_far(k0) && threadIdx.x < QUERIES + KEYS - 1) by_distance[buffer][threadIdx.x] = bias.of(first - k0 + QUERIES - 1 - (int)threadIdx.x, a.buckets);
-        }
+        from_k.store(tiles[part][0], a.hd, all, holds);
+        from_v.store(tiles[part][1], a.hd, all, holds);
+        if constexpr (BIAS) stage_bias(first_key, part);
     };
 
     if (seen.tiles) load(0);
@@ -65,84 +65,126 @@ __global__ __launch_bounds__(256, 2) void k_attend(Attn a) {
     short8_t q[STEPS];
     const char *const query = a.q.of((int64_t)seq.q0 + (i < seq.nq ? i : seq.nq - 1), head);
 #pragma unroll
-    for (int s = 0; s < STEPS; ++s) {
-        q[s] = __builtin_bit_cast(short8_t, piece_of_head(query, s * 16 + h * 8, a.hd, i < seq.nq));
-    }
+    for (int s = 0; s < STEPS; ++s) q[s] = __builtin_bit_cast(short8_t, piece_of_head(query, s * 16 + h * 8, a.hd, i < seq.nq));
     // Scores are kept as they are without a bias (units of `unit` powers of two), and scaled, in natural units, with one: a table may hold a type's lowest
     // number, whose multiple by LOG2E does not exist.
     const float unit = BIAS ? LOG2E : a.scale * LOG2E, grows = GROWS / unit;
-    f32x16 out[HD / 32] = {};
-    float most = -INFINITY, used = -INFINITY, sum = 0.0f;
-    if (seen.tiles) stage(0, 0);
-    for (int t = 0; t < seen.tiles; ++t) {
-        const int k0 = seen.tile(t) * KEYS, buffer = t & 1;
-        if (t + 1 < seen.tiles) load(t + 1);
-        __syncthreads();
-        const char *const keys = tiles[buffer][0], *const values = tiles[buffer][1];
-        // what this wave's queries see of the tile: nothing, all, or some
-        const bool none = k0 > of_wave + 31 || (k0 + KEYS <= of_wave - a.window + 1 && k0 >= a.sinks);
-        if (!none) {
-            f32x16 s[2];
+    f32x16 out[HD / 32] = {}, scores[2];
+    float most = -INFINITY, used = -INFINITY, from = 0.0f, shift = SHIFT<DT>, sum = 0.0f;
+    // What is left of a tile's scores: the bias, and -inf where a query does not see a key.
+    const auto add_bias = [&](f32x16 &s, int k0, int part) __attribute__((always_inline)) {
+        if constexpr (BIAS) {
+            if (is_far(k0)) {
 #pragma unroll
-            for (int n = 0; n < 2; ++n) {
-                s[n] = f32x16{};
+                for (int e = 0; e < 16; ++e) s[e] = __builtin_fmaf(s[e], a.scale, far_bias);
+            } else {
+                const float *const at = by_distance[part] + QUERIES - 1 - (w * 32 + (lane & 31)) + 4 * h;
 #pragma unroll
-                for (int c = 0; c < STEPS; ++c) s[n] = mfma32<DT>(T::rows(keys, n * 32, c, lane), q[c], s[n]);
+                for (int e = 0; e < 16; ++e) s[e] = __builtin_fmaf(s[e], a.scale, at[8 * (e / 4) + e % 4]);
             }
-            if constexpr (BIAS) {
-                const bool far = is_far(k0);
-                const float *const at = by_distance[buffer] + QUERIES - 1 - (w * 32 + (lane & 31)) + 4 * h;
-                if (far) {
-#pragma unroll
-                    for (int n = 0; n < 2; ++n)
-#pragma unroll
-                        for (int e = 0; e < 16; ++e) s[n][e] = __builtin_fmaf(s[n][e], a.scale, far_bias);
-                } else {
-#pragma unroll
-                    for (int n = 0; n < 2; ++n)
-#pragma unroll
-                        for (int e = 0; e < 16; ++e) s[n][e] = __builtin_fmaf(s[n][e], a.scale, at[n * 32 + 8 * (e / 4) + e % 4]);
-                }
-            }
-            const bool all = k0 + KEYS - 1 <= of_wave && (k0 > of_wave + 31 - a.window || k0 + KEYS <= a.sinks);
-            if (!all) {
-#pragma unroll
-                for (int n = 0; n < 2; ++n)
-#pragma unroll
-                    for (int e = 0; e < 16; ++e)
-                        if (!sees(place, k0 + n * 32 + 8 * (e / 4) + 4 * h + e % 4, a.window, a.sinks)) s[n][e] = -INFINITY;
-            }
-            float now = most;
-#pragma unroll
-            for (int n = 0; n < 2; ++n)
-#pragma unroll
-                for (int e = 0; e < 16; ++e) now = fmaxf(now, s[n][e]);
-            most = max_of_halves(now);
-            if (__any(most > used + grows || (used == -INFINITY && most > -INFINITY))) {
-                const float times = used == -INFINITY ? 0.0f : exp2_((used - most) * unit);
-                used = most;
-                sum *= times;
-#pragma unroll
-                for (int d = 0; d < HD / 32; ++d) out[d] *= times;
-            }
-            const float from = used == -INFINITY ? 0.0f : used, shift = SHIFT<DT> - from * unit;
-#pragma unroll
-            for (int n = 0; n < 2; ++n)
-#pragma unroll
-                for (int e = 0; e < 16; ++e) {
-                    s[n][e] = exp2_(BIAS ? __builtin_fmaf(s[n][e] - from, unit, SHIFT<DT>) : __builtin_fmaf(s[n][e], unit, shift));
-                    sum += s[n][e];
-                }
-#pragma unroll
-            for (int n = 0; n < 2; ++n)
-#pragma unroll
-                for (int k = 0; k < 2; ++k) {
-                    const short8_t p = pack8<DT>(s[n], 8 * k);
-#pragma unroll
-                    for (int d = 0; d < HD / 32; ++d) out[d] = mfma32<DT>(T::columns(values, n * 32 + k * 16, d, lane), p, out[d]);
-                }
         }
-        if (t + 1 < seen.tiles) stage(t + 1, buffer ^ 1);
+    };
+    const auto finish = [&](f32x16 &s, int k0, int part) __attribute__((always_inline)) {
+        add_bias(s, k0, part);
+        const bool all = k0 + KEYS - 1 <= of_wave && (k0 > of_wave + 31 - a.window || k0 + KEYS <= a.sinks);
+        if (!all) {
+#pragma unroll
+            for (int e = 0; e < 16; ++e)
+                if (!sees(place, k0 + 8 * (e / 4) + 4 * h + e % 4, a.window, a.sinks)) s[e] = -INFINITY;
+        }
+    };
+    // In step t the scores of tile t + 1 are formed beside the exponentials of tile t, the products with its values follow, and tile t + 2 goes to the part of the ring
+    // whose tile all waves have left.  Four steps a round, so that the parts of the ring are constants.
+    const auto products = [&](auto part_) __attribute__((always_inline)) {
+        constexpr int part = part_, after = (part + 1) % RING;
+        f32x16 &now = scores[part & 1], &next = scores[after & 1];
+        float largest = most;
+#pragma unroll
+        for (int e = 0; e < 16; ++e) largest = fmaxf(largest, now[e]);
+        most = max_of_halves(largest);
+        if (__any(most > used + grows)) {
+            const bool some = most > -INFINITY;
+            const float times = some ? exp2_((used - most) * unit) : 1.0f;          // 0 at first
+            used = most;
+            from = some ? most : 0.0f;
+            shift = SHIFT<DT> - from * unit;
+            sum *= times;
+#pragma unroll
+            for (int d = 0; d < HD / 32; ++d) out[d] *= times;
+        }
+        __syncthreads();
+        next = f32x16{};                    // behind the last tile: of whatever the ring holds, and not looked at
+#pragma unroll
+        for (int c = 0; c < STEPS; ++c) next = mfma32<DT>(T::rows(tiles[after][0], 0, c, lane), q[c], next);
+#pragma unroll
+        for (int e = 0; e < 16; ++e) {
+            now[e] = exp2_(BIAS ? __builtin_fmaf(now[e] - from, unit, SHIFT<DT>) : __builtin_fmaf(now[e], unit, shift));
+            sum += now[e];
+        }
+        asm volatile("" : "+v"(sum));       // beside the products, not behind them
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {
+            const short8_t p = pack8<DT>(now, 8 * k);
+#pragma unroll
+            for (int d = 0; d < HD / 32; ++d) out[d] = mfma32<DT>(T::columns(tiles[part][1], k * 16, d, lane), p, out[d]);
+        }
+    };
+    const auto step = [&](auto part_, int t) __attribute__((always_inline)) {
+        constexpr int part = part_, after = (part + 1) % RING, second = (part + 2) % RING;
+        products(part_);
+        if (t + 1 < seen.tiles) finish(scores[after & 1], seen.tile(t + 1) * KEYS, after);
+        if (t + 2 < seen.tiles) stage(t + 2, second);
+        if (t + 3 < seen.tiles) load(t + 3);
+    };
+    // Where every query sees the tiles t + 1 to t + 3 whole, nothing is asked; key: the first of tile t.
+    const auto plain_step = [&](auto part_, int key, const char *&k_at, const char *&v_at) __attribute__((always_inline)) {
+        constexpr int part = part_, after = (part + 1) % RING, second = (part + 2) % RING;
+        products(part_);
+        add_bias(scores[after & 1], key + KEYS, after);
+        from_k.store_whole(tiles[second][0], a.hd);
+        from_v.store_whole(tiles[second][1], a.hd);
+        if constexpr (BIAS) stage_bias(key + 2 * KEYS, second);
+        from_k.load_whole(k_at, a.k.ld, a.hd);
+        from_v.load_whole(v_at, a.v.ld, a.hd);
+        k_at += a.k.ld * (2 * KEYS);
+        v_at += a.v.ld * (2 * KEYS);
+    };
+    constexpr std::integral_constant<int, 0> p0{};
+    constexpr std::integral_constant<int, 1> p1{};
+    constexpr std::integral_constant<int, 2> p2{};
+    constexpr std::integral_constant<int, 3> p3{};
+    if (seen.tiles) {
+        int plain_from, plain_to;
+        seen.plain(a, first, last, plain_from, plain_to);
+        stage(0, 0);
+        if (seen.tiles > 1) load(1);
+        __syncthreads();
+        scores[0] = f32x16{};
+#pragma unroll
+        for (int c = 0; c < STEPS; ++c) scores[0] = mfma32<DT>(T::rows(tiles[0][0], 0, c, lane), q[c], scores[0]);
+        finish(scores[0], seen.tile(0) * KEYS, 0);
+        if (seen.tiles > 1) stage(1, 1);
+        if (seen.tiles > 2) load(2);
+        for (int t = 0;;) {
+            if (t >= plain_from && t + 6 < plain_to) {
+                int key = seen.tile(t) * KEYS;
+                const char *k_at = keys_at + (int64_t)(key + 3 * KEYS) * (a.k.ld * 2), *v_at = values_at + (int64_t)(key + 3 * KEYS) * (a.v.ld * 2);
+                for (; t + 6 < plain_to; t += 4, key += 4 * KEYS) {
+                    plain_step(p0, key, k_at, v_at);
+                    plain_step(p1, key + KEYS, k_at, v_at);
+                    plain_step(p2, key + 2 * KEYS, k_at, v_at);
+                    plain_step(p3, key + 3 * KEYS, k_at, v_at);
+                }
+            }
+            step(p0, t);
+            if (++t == seen.tiles) break;
+            step(p1, t);
+            if (++t == seen.tiles) break;
+            step(p2, t);
+            if (++t == seen.tiles) break;
+            step(p3, t);
+            if (++t == seen.tiles) break;
+        }
     }
     sum = sum_of_halves(sum);
     const bool there = i < seq.nq;
@@ -230,10 +272,10 @@ __global__ __launch_bounds__(64 * FEW_WAVES, NT == 1 ? 2 : 1) void k_attend_few(
         for (int n = 0; n < 2; ++n) {
             const char *const key = row(keys_at, a.k.ld, k0 + n * 16 + of16);
 #pragma unroll
-            for (int s = 0; s < STEPS; ++s) from_k[n][s] = raw_piece(key, s * 32 + g * 8, a.hd);
+            for (int s = 0; s < STEPS; ++s) from_k[n][s] = load_piece<DT>(key, column_of(s * 32 + g * 8, a.hd));
         }
 #pragma unroll
-        for (int n = 0; n < PASSES; ++n) from_v[n] = raw_piece(row(values_at, a.v.ld, k0 + of_pass + n * APART), piece * 8, a.hd);
+        for (int n = 0; n < PASSES; ++n) from_v[n] = load_piece<DT>(row(values_at, a.v.ld, k0 + of_pass + n * APART), column_of(piece * 8, a.hd));
     };
     int far_from = 0;
     float far_bias[NT] = {};

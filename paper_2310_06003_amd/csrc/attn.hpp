@@ -17,7 +17,7 @@ typedef __bf16 bf16x8_t __attribute__((ext_vector_type(8)));
 typedef _Float16 f16x8_t __attribute__((ext_vector_type(8)));
 
 constexpr float LOG2E = 1.44269504088896340736f, LN2 = 0.69314718055994530942f;
-constexpr int MAX_BUCKETS = 256, MAX_HEAD = 128;
+constexpr int MAX_BUCKETS = 256, MIN_HEAD = 8, MAX_HEAD = 128;
 constexpr int FAR_AWAY = 1 << 30;        // a window that holds every key: lengths are at most this
 
 template <int DT>
@@ -103,6 +103,12 @@ struct Seen {
         tiles = sink_tiles + (end + KEYS - 1) / KEYS - first_tile;
         if (end == 0) tiles = 0;
     }
+    // The tiles [from, to) of which every query sees every key.
+    __device__ __forceinline__ void plain(const Attn &a, int first, int last, int &from, int &to) const {
+        const int cut = last - a.window >= 0 ? (last - a.window) / KEYS + 1 : 0;        // the first tile in all windows
+        from = sink_tiles + (cut > first_tile ? cut - first_tile : 0);
+        to = first + 1 > 0 ? sink_tiles + (first + 1) / KEYS - first_tile : 0;
+    }
     __device__ __forceinline__ int tile(int t) const { return t < sink_tiles ? t : first_tile + t - sink_tiles; }
     __device__ __forceinline__ bool holds_all(int k0) const { return k0 + KEYS <= end && (k0 >= low || k0 + KEYS <= sinks); }
     __device__ __forceinline__ bool holds(int j) const { return j < end && (j >= low || j < sinks); }
@@ -149,8 +155,9 @@ struct Tile {
 };
 
 // Eight elements of a head's row, from `column` on; what lies behind the head: zeros.  One load without a branch: a piece that reaches past the head's end is read
-// from eight elements in front of that, and shifted.  (Branches for each element cost more than the products: 1999 tokens of 10 heads of 77 forward 93 us.)
+// from eight elements in front of that, and shifted.  (With branches for each element 1999 tokens of 10 heads of 77 took 78 us forward, so 47.)
 // The row has to exist also where the piece is not wanted.
+__device__ __forceinline__ int column_of(int column, int hd) { return column < hd - 8 ? column : hd - 8; }
 __device__ __forceinline__ u32x4 shifted(u32x4 v, int elements) {          // towards the first, by 0 to 7
     if (elements & 4) v = u32x4{v[2], v[3], 0, 0};
     if (elements & 2) v = u32x4{v[1], v[2], v[3], 0};
@@ -160,28 +167,16 @@ __device__ __forceinline__ u32x4 shifted(u32x4 v, int elements) {          // to
     }
     return v;
 }
-__device__ __forceinline__ u32x4 short_row(const char *row, int column, int hd) {          // heads of less than eight elements
-    uint64_t lo = 0, hi = 0;
-#pragma unroll 1
-    for (int e = 0; column + e < hd; ++e) {
-        const uint64_t x = reinterpret_cast<const unsigned short *>(row)[column + e];
-        if (e < 4) lo |= x << (16 * e);
-        else hi |= x << (16 * (e - 4));
-    }
-    return u32x4{(unsigned)lo, (unsigned)(lo >> 32), (unsigned)hi, (unsigned)(hi >> 32)};
-}
-__device__ __forceinline__ u32x4 raw_piece(const char *row, int column, int hd) {
-    if (hd < 8) return short_row(row, column, hd);
-    return load_piece<PARO_BF16>(row, column < hd - 8 ? column : hd - 8);
-}
-__device__ __forceinline__ u32x4 finished(u32x4 v, int column, int hd, bool there) {       // of raw_piece
-    if ((hd & 7) && hd >= 8 && column > hd - 8) v = shifted(v, (column - (hd - 8)) & 7);
+__device__ __forceinline__ u32x4 finished(u32x4 v, int column, int hd, bool there) {       // of what was loaded from column_of
+    if (hd & 7) v = shifted(v, (column - column_of(column, hd)) & 7);
     there = there && column < hd;
 #pragma unroll
     for (int i = 0; i < 4; ++i) v[i] = there ? v[i] : 0;
     return v;
 }
-__device__ __forceinline__ u32x4 piece_of_head(const char *row, int column, int hd, bool there) { return finished(raw_piece(row, column, hd), column, hd, there); }
+__device__ __forceinline__ u32x4 piece_of_head(const char *row, int column, int hd, bool there) {
+    return finished(load_piece<PARO_BF16>(row, column_of(column, hd)), column, hd, there);
+}
 __device__ __forceinline__ void store_piece_of_head(char *row, int column, int hd, u32x4 v) {
     if (column + 8 <= hd) {
         store_piece<PARO_BF16>(row, column, v);
@@ -207,7 +202,7 @@ __device__ __forceinline__ unsigned both(float a, float b) {
 }
 
 // A tile of rows on its way from memory to shared memory: each thread takes pieces of one column, PASSES rows.  Rows that the tile does not hold are read as others
-// of the sequence and staged as zeros.
+// of the sequence and staged as zeros.  A thread's place in a tile is a 32-bit offset that stays, the tile's a scalar address.
 template <int HD, int ROWS>
 struct Staged {
     using T = Tile<HD>;
@@ -217,13 +212,24 @@ struct Staged {
 
     static __device__ __forceinline__ int column() { return (int)threadIdx.x % T::PIECES * 8; }
     static __device__ __forceinline__ int row(int n) { return (int)threadIdx.x / T::PIECES + n * APART; }
-    // row r of the tile is the sequence's row0 + r; `rows` of them exist (one at least)
+    static __device__ __forceinline__ unsigned offset(int r, unsigned ld, int hd) { return (unsigned)r * (ld * 2) + column_of(column(), hd) * 2; }
+    // row r of the tile is the sequence's row0 + r; `rows` of them exist (one at least, and row0 is one)
     __device__ __forceinline__ void load(const char *of_head, int64_t ld, int row0, int rows, int hd) {
+        const char *const tile = of_head + (int64_t)row0 * (ld * 2);
+        const int last = rows - 1 - row0;
+        if (last >= ROWS - 1) {
+            load_whole(tile, ld, hd);
+        } else {
 #pragma unroll
-        for (int n = 0; n < PASSES; ++n) {
-            const int r = row0 + row(n);
-            v[n] = raw_piece(of_head + (int64_t)(r < rows ? r : rows - 1) * (ld * 2), column(), hd);
+            for (int n = 0; n < PASSES; ++n) v[n] = *reinterpret_cast<const piece_at2 *>(tile + offset(row(n) < last ? row(n) : last, (unsigned)ld, hd));
         }
+    }
+    __device__ __forceinline__ void load_whole(const char *tile, int64_t ld, int hd) {
+#pragma unroll
+        for (int n = 0; n < PASSES; ++n) v[n] = *reinterpret_cast<const piece_at2 *>(tile + offset(row(n), (unsigned)ld, hd));
+    }
+    __device__ __forceinline__ void store_whole(char *tile, int hd) {
+        store(tile, hd, true, [](int) { return true; });
     }
     // holds(row of the tile): whether it is there;  all: every row is
     template <class F>
@@ -297,7 +303,7 @@ inline int check_attn(const std::string &f, const paro_attn_t *d) {
     if (d->dtype != PARO_BF16 && d->dtype != PARO_F16) return bad("dtype must be PARO_BF16 or PARO_F16");
     if (d->batch < 0 || d->batch > (1 << 20)) return bad("batch must be in [0, 2^20]");
     if (d->heads < 1 || d->heads > 1024 || d->kv_heads < 1 || d->heads % d->kv_heads) return bad("heads must be in [1, 1024] and a multiple of kv_heads");
-    if (d->head_dim < 1 || d->head_dim > MAX_HEAD) return bad("head_dim must be in [1, 128]");
+    if (d->head_dim < MIN_HEAD || d->head_dim > MAX_HEAD) return bad("head_dim must be in [8, 128]");
     if (d->len_q < 0 || d->len_q > FAR_AWAY || d->len_k < 0 || d->len_k > FAR_AWAY) return bad("len_q and len_k must be in [0, 2^30]");
     if (d->rows_q < 0 || d->rows_q > INT32_MAX || d->rows_k < 0 || d->rows_k > INT32_MAX) return bad("rows_q and rows_k must be in [0, 2^31)");
     if (d->batch * d->len_q > INT32_MAX && !d->rows_q) return bad("more than 2^31 - 1 rows of queries");
@@ -314,7 +320,7 @@ inline int check_attn(const std::string &f, const paro_attn_t *d) {
         const int64_t head = heads[i] ? heads[i] : hd, ld = lds[i] ? lds[i] : count * hd;
         if (head < hd || ld < hd) return bad("a head is longer than its distance to the next");
         if (head < ld && ld < (count - 1) * head + hd) return bad("a row is longer than its distance to the next");
-        if (ld > ((int64_t)1 << 40) || head > ((int64_t)1 << 50)) return bad("distances between rows are at most 2^40, between heads 2^50");
+        if (ld > ((int64_t)1 << 24) || head > ((int64_t)1 << 50)) return bad("distances between rows are at most 2^24, between heads 2^50");
     }
     if (ceil_div(std::max(d->len_q, d->len_k), 16) * d->heads > INT32_MAX / std::max<int64_t>(1, d->batch))
         return bad("batch * heads * length is at most 2^35");

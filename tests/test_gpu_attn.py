@@ -24,7 +24,7 @@ def test_any_length(paro, n):
     forward(paro, [(n, n)], hd=128, dtype="f16", window=20, sinks=3, buckets=9, layout="dense", stats=False)
 
 
-@pytest.mark.parametrize("hd", [1, 3, 7, 8, 9, 16, 31, 32, 33, 56, 63, 64, 65, 72, 77, 80, 96, 120, 127, 128])
+@pytest.mark.parametrize("hd", [8, 9, 11, 16, 31, 32, 33, 56, 63, 64, 65, 72, 77, 80, 96, 120, 127, 128])
 def test_any_head_width(paro, hd):
     forward(paro, [(70, 70)], hd=hd, heads=3, pad=hd % 3)
     forward(paro, [(5, 150)], hd=hd, dtype="f16", pad=5, heads=4, kv=2)
