@@ -16,7 +16,8 @@ constexpr float GROWS = 8.0f;                // powers of two that a row's share
 template <int DT>
 constexpr float SHIFT = DT == PARO_F16 ? 7.0f : 0.0f;
 
-template <int DT, int HD, bool BIAS>
+// FILL: keys and values lie on 16 bytes and go to shared memory past the registers.
+template <int DT, int HD, bool BIAS, bool FILL>
 __global__ __launch_bounds__(256, 2) void k_attend(Attn a) {
     using T = Tile<HD>;
     constexpr int BYTES = KEYS * T::ROW, STEPS = HD / 16, RING = 4;
@@ -35,6 +36,8 @@ __global__ __launch_bounds__(256, 2) void k_attend(Attn a) {
 
     const char *const keys_at = a.k.of(seq.k0, kv), *const values_at = a.v.of(seq.k0, kv);
     Staged<HD, KEYS> from_k, from_v;
+    const Filled<HD, KEYS> fill_k(a.k.ld, a.hd), fill_v(a.v.ld, a.hd);
+    constexpr int FILLS = 2 * Filled<HD, KEYS>::FILLS;
     const auto load = [&](int t) __attribute__((always_inline)) {
         const int k0 = seen.tile(t) * KEYS;
         from_k.load(keys_at, a.k.ld, k0, seq.nk, a.hd);
@@ -48,14 +51,30 @@ __global__ __launch_bounds__(256, 2) void k_attend(Attn a) {
     };
     const auto stage = [&](int t, int part) __attribute__((always_inline)) {
         const int first_key = seen.tile(t) * KEYS;
+        if constexpr (BIAS) stage_bias(first_key, part);
         const auto holds = [&](int r) { return seen.holds(first_key + r); };
         const bool all = seen.holds_all(first_key);
         from_k.store(tiles[part][0], a.hd, all, holds);
         from_v.store(tiles[part][1], a.hd, all, holds);
+    };
+    const auto fill = [&](int t, int part) __attribute__((always_inline)) {
+        const int first_key = seen.tile(t) * KEYS;
         if constexpr (BIAS) stage_bias(first_key, part);
+        const u32x4 k_from = fill_k.descriptor(keys_at + (int64_t)first_key * (a.k.ld * 2)), v_from = fill_v.descriptor(values_at + (int64_t)first_key * (a.v.ld * 2));
+        const auto holds = [&](int r) { return seen.holds(first_key + r); };
+        fill_k.held(k_from, tiles[part][0], holds);
+        fill_v.held(v_from, tiles[part][1], holds);
+    };
+    // Nothing, in the place of a tile that is not there: the waits count on as many loads each time.
+    const auto fill_none = [&](int part) __attribute__((always_inline)) {
+        const auto holds = [](int) { return false; };
+        fill_k.held(fill_k.descriptor(keys_at), tiles[part][0], holds);
+        fill_v.held(fill_v.descriptor(values_at), tiles[part][1], holds);
     };
 
-    if (seen.tiles) load(0);
+    if constexpr (!FILL) {
+        if (seen.tiles) load(0);
+    }
     if constexpr (BIAS) {
         bias.load(a, head);
         __syncthreads();
@@ -93,9 +112,9 @@ __global__ __launch_bounds__(256, 2) void k_attend(Attn a) {
                 if (!sees(place, k0 + 8 * (e / 4) + 4 * h + e % 4, a.window, a.sinks)) s[e] = -INFINITY;
         }
     };
-    // In step t the scores of tile t + 1 are formed beside the exponentials of tile t, the products with its values follow, and tile t + 2 goes to the part of the ring
-    // whose tile all waves have left.  Four steps a round, so that the parts of the ring are constants.
-    const auto products = [&](auto part_) __attribute__((always_inline)) {
+    // In step t the scores of tile t + 1 are formed beside the exponentials of tile t, and the products with its values follow.  Meanwhile tile t + 3 (through
+    // registers: t + 2) goes to the part of the ring whose tile all waves have left.  Four steps a round, so that the parts of the ring are constants.
+    const auto products = [&](auto part_, auto &&between) __attribute__((always_inline)) {
         constexpr int part = part_, after = (part + 1) % RING;
         f32x16 &now = scores[part & 1], &next = scores[after & 1];
         float largest = most;
@@ -112,7 +131,9 @@ __global__ __launch_bounds__(256, 2) void k_attend(Attn a) {
 #pragma unroll
             for (int d = 0; d < HD / 32; ++d) out[d] *= times;
         }
-        __syncthreads();
+        if constexpr (FILL) arrived<FILLS>();           // tile t + 2 may be on its way
+        else __syncthreads();
+        between();
         next = f32x16{};                    // behind the last tile: of whatever the ring holds, and not looked at
 #pragma unroll
         for (int c = 0; c < STEPS; ++c) next = mfma32<DT>(T::rows(tiles[after][0], 0, c, lane), q[c], next);
@@ -130,22 +151,37 @@ __global__ __launch_bounds__(256, 2) void k_attend(Attn a) {
         }
     };
     const auto step = [&](auto part_, int t) __attribute__((always_inline)) {
-        constexpr int part = part_, after = (part + 1) % RING, second = (part + 2) % RING;
-        products(part_);
+        constexpr int part = part_, after = (part + 1) % RING;
+        products(part_, [&]() __attribute__((always_inline)) {
+            if constexpr (FILL) {
+                if (t + 3 < seen.tiles) fill(t + 3, (part + 3) % RING);
+                else fill_none((part + 3) % RING);
+            }
+        });
         if (t + 1 < seen.tiles) finish(scores[after & 1], seen.tile(t + 1) * KEYS, after);
-        if (t + 2 < seen.tiles) stage(t + 2, second);
-        if (t + 3 < seen.tiles) load(t + 3);
+        if constexpr (!FILL) {
+            if (t + 2 < seen.tiles) stage(t + 2, (part + 2) % RING);
+            if (t + 3 < seen.tiles) load(t + 3);
+        }
     };
-    // Where every query sees the tiles t + 1 to t + 3 whole, nothing is asked; key: the first of tile t.
-    const auto plain_step = [&](auto part_, int key, const char *&k_at, const char *&v_at) __attribute__((always_inline)) {
-        constexpr int part = part_, after = (part + 1) % RING, second = (part + 2) % RING;
-        products(part_);
-        add_bias(scores[after & 1], key + KEYS, after);
-        from_k.store_whole(tiles[second][0], a.hd);
-        from_v.store_whole(tiles[second][1], a.hd);
-        if constexpr (BIAS) stage_bias(key + 2 * KEYS, second);
-        from_k.load_whole(k_at, a.k.ld, a.hd);
-        from_v.load_whole(v_at, a.v.ld, a.hd);
+    // Where every query sees the tiles t + 1 to t + 3 whole, nothing is asked; key0: the first of tile t; k_at, v_at: of tile t + 3.
+    const auto plain_step = [&](auto part_, int key0, const char *&k_at, const char *&v_at) __attribute__((always_inline)) {
+        constexpr int part = part_, after = (part + 1) % RING, second = (part + 2) % RING, third = (part + 3) % RING;
+        products(part_, [&]() __attribute__((always_inline)) {
+            if constexpr (FILL) {
+                fill_k.whole(fill_k.descriptor(k_at), tiles[third][0]);
+                fill_v.whole(fill_v.descriptor(v_at), tiles[third][1]);
+                if constexpr (BIAS) stage_bias(key0 + 3 * KEYS, third);
+            }
+        });
+        add_bias(scores[after & 1], key0 + KEYS, after);
+        if constexpr (!FILL) {
+            from_k.store_whole(tiles[second][0], a.hd);
+            from_v.store_whole(tiles[second][1], a.hd);
+            if constexpr (BIAS) stage_bias(key0 + 2 * KEYS, second);
+            from_k.load_whole(k_at, a.k.ld, a.hd);
+            from_v.load_whole(v_at, a.v.ld, a.hd);
+        }
         k_at += a.k.ld * (2 * KEYS);
         v_at += a.v.ld * (2 * KEYS);
     };
@@ -156,24 +192,34 @@ __global__ __launch_bounds__(256, 2) void k_attend(Attn a) {
     if (seen.tiles) {
         int plain_from, plain_to;
         seen.plain(a, first, last, plain_from, plain_to);
-        stage(0, 0);
-        if (seen.tiles > 1) load(1);
-        __syncthreads();
+        if constexpr (FILL) {
+            for (int t = 0; t < 3; ++t) {
+                if (t < seen.tiles) fill(t, t);
+                else fill_none(t);
+            }
+            arrived<2 * FILLS>();
+        } else {
+            stage(0, 0);
+            if (seen.tiles > 1) load(1);
+            __syncthreads();
+        }
         scores[0] = f32x16{};
 #pragma unroll
         for (int c = 0; c < STEPS; ++c) scores[0] = mfma32<DT>(T::rows(tiles[0][0], 0, c, lane), q[c], scores[0]);
         finish(scores[0], seen.tile(0) * KEYS, 0);
-        if (seen.tiles > 1) stage(1, 1);
-        if (seen.tiles > 2) load(2);
+        if constexpr (!FILL) {
+            if (seen.tiles > 1) stage(1, 1);
+            if (seen.tiles > 2) load(2);
+        }
         for (int t = 0;;) {
             if (t >= plain_from && t + 6 < plain_to) {
-                int key = seen.tile(t) * KEYS;
-                const char *k_at = keys_at + (int64_t)(key + 3 * KEYS) * (a.k.ld * 2), *v_at = values_at + (int64_t)(key + 3 * KEYS) * (a.v.ld * 2);
-                for (; t + 6 < plain_to; t += 4, key += 4 * KEYS) {
-                    plain_step(p0, key, k_at, v_at);
-                    plain_step(p1, key + KEYS, k_at, v_at);
-                    plain_step(p2, key + 2 * KEYS, k_at, v_at);
-                    plain_step(p3, key + 3 * KEYS, k_at, v_at);
+                int key0 = seen.tile(t) * KEYS;
+                const char *k_at = keys_at + (int64_t)(key0 + 3 * KEYS) * (a.k.ld * 2), *v_at = values_at + (int64_t)(key0 + 3 * KEYS) * (a.v.ld * 2);
+                for (; t + 6 < plain_to; t += 4, key0 += 4 * KEYS) {
+                    plain_step(p0, key0, k_at, v_at);
+                    plain_step(p1, key0 + KEYS, k_at, v_at);
+                    plain_step(p2, key0 + 2 * KEYS, k_at, v_at);
+                    plain_step(p3, key0 + 3 * KEYS, k_at, v_at);
                 }
             }
             step(p0, t);
@@ -185,6 +231,7 @@ __global__ __launch_bounds__(256, 2) void k_attend(Attn a) {
             step(p3, t);
             if (++t == seen.tiles) break;
         }
+        if constexpr (FILL) arrived<0>();               // nothing is on its way into the shared memory of the block that comes next
     }
     sum = sum_of_halves(sum);
     const bool there = i < seq.nq;
@@ -520,10 +567,14 @@ Plan plan_of(const paro_attn_t &d) {
     return p;
 }
 
+// Rows that lie on 16 bytes and heads of whole pieces.
+bool fills_take(const Rows &r, int hd) { return hd % 8 == 0 && r.ld % 8 == 0 && r.head % 8 == 0 && reinterpret_cast<uintptr_t>(r.at) % 16 == 0; }
+
 template <int DT, int HD, bool BIAS>
 void launch(const Attn &a, const Plan &p, char *workspace, hipStream_t st) {
     if (!p.few) {
-        hipLaunchKernelGGL((k_attend<DT, HD, BIAS>), dim3((unsigned)p.blocks), dim3(256), 0, st, a);
+        if (fills_take(a.k, a.hd) && fills_take(a.v, a.hd)) hipLaunchKernelGGL((k_attend<DT, HD, BIAS, true>), dim3((unsigned)p.blocks), dim3(256), 0, st, a);
+        else hipLaunchKernelGGL((k_attend<DT, HD, BIAS, false>), dim3((unsigned)p.blocks), dim3(256), 0, st, a);
         return;
     }
     const Few f{p.shares, p.row_tiles, reinterpret_cast<float *>(workspace), reinterpret_cast<float *>(workspace + p.stats)};

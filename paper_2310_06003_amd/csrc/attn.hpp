@@ -243,6 +243,49 @@ struct Staged {
     }
 };
 
+// The same without registers: 16 bytes a lane from memory to shared memory at `to` + 16 * lane, past the registers; lanes without a piece are sent NOWHERE, where the
+// hardware reads zeros.  Rows have to lie on 16 bytes.  In assembly because the compiler, which cannot tell the tiles apart, would wait for it before every read
+// of shared memory; arrived() waits.  It writes no register; m0, which holds the place in shared memory, is an operand, and one instruction has to stand between
+// its write and its use.
+typedef __attribute__((address_space(3))) char lds_char;
+template <int AT>
+__device__ __forceinline__ void fill(u32x4 from, unsigned offset, unsigned to) {
+    asm volatile("s_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"{m0}"(to + AT), "v"(offset), "s"(from) : "memory");
+}
+// All but the wave's last `IN_FLIGHT` loads have arrived, all its accesses of shared memory are done; then those of all waves.
+template <int IN_FLIGHT>
+__device__ __forceinline__ void arrived() { asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"i"(IN_FLIGHT) : "memory"); }
+constexpr unsigned NOWHERE = 0x80000000u;
+
+template <int HD, int ROWS>
+struct Filled {
+    using T = Tile<HD>;
+    static constexpr int AT_ONCE = 64 / T::PIECES, FILLS = ROWS / AT_ONCE / 4;       // rows of an instruction; instructions of a wave of four
+    static_assert(FILLS >= 1 && ROWS % (AT_ONCE * 4) == 0, "every wave fills a part");
+    unsigned at[FILLS];              // of the lane's pieces, from the tile's first row
+
+    static __device__ __forceinline__ int row(int n) { return (wave_of() * FILLS + n) * AT_ONCE + (int)(threadIdx.x & 63) / T::PIECES; }
+    __device__ __forceinline__ Filled(int64_t ld, int hd) {
+#pragma unroll
+        for (int n = 0; n < FILLS; ++n) {
+            const int piece = (int)(threadIdx.x % T::PIECES) ^ T::key(row(n));
+            at[n] = piece * 8 < hd ? (unsigned)row(n) * (unsigned)(ld * 2) + piece * 16 : NOWHERE;
+        }
+    }
+    static __device__ __forceinline__ u32x4 descriptor(const char *tile) {
+        const uint64_t at = (uint64_t)(uintptr_t)tile;
+        return u32x4{(unsigned)at, (unsigned)(at >> 32) & 0xFFFFu, 0x7FFFFFF0u, 0x00020000u};
+    }
+    static __device__ __forceinline__ unsigned place(const char *tile) { return (unsigned)(uintptr_t)(const lds_char *)tile + wave_of() * FILLS * 1024; }
+    __device__ __forceinline__ void whole(u32x4 from, const char *tile) const {
+        static_for<0, FILLS>([&](auto n) { fill<n * 1024>(from, at[n], place(tile)); });
+    }
+    template <class F>
+    __device__ __forceinline__ void held(u32x4 from, const char *tile, F &&holds) const {
+        static_for<0, FILLS>([&](auto n) { fill<n * 1024>(from, holds(row(n)) ? at[n] : NOWHERE, place(tile)); });
+    }
+};
+
 // A row of 32 of the result of 32 x 32 products: a lane has of its row (lane % 32) the elements 8 * (i / 4) + 4 * (lane / 32) + i % 4.  Both halves of a
 // wave exchange, so that each stores eight in a row.
 template <int DT>
