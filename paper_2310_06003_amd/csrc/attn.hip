@@ -45,7 +45,8 @@ __global__ __launch_bounds__(256, 2) void k_attend(Attn a) {
     };
     int far_from = 0;                       // distances from here on have the last bucket's bias
     float far_bias = 0.0f;
-    const auto is_far = [&](int k0) { return BIAS && first - (k0 + KEYS - 1) >= far_from; };
+    bool usual = true;
+    const auto is_far = [&](int k0) { return BIAS && usual && first - (k0 + KEYS - 1) >= far_from; };
     const auto stage_bias = [&](int k0, int part) __attribute__((always_inline)) {
         if (!is_far(k0) && threadIdx.x < QUERIES + KEYS - 1) by_distance[part][threadIdx.x] = bias.of(first - k0 + QUERIES - 1 - (int)threadIdx.x, a.buckets);
     };
@@ -80,31 +81,33 @@ __global__ __launch_bounds__(256, 2) void k_attend(Attn a) {
         __syncthreads();
         far_from = bias.first[a.buckets - 1];
         far_bias = bias.column[a.buckets - 1];
+        usual = fabsf(far_bias) < USUAL;
     }
     short8_t q[STEPS];
     const char *const query = a.q.of((int64_t)seq.q0 + (i < seq.nq ? i : seq.nq - 1), head);
 #pragma unroll
     for (int s = 0; s < STEPS; ++s) q[s] = __builtin_bit_cast(short8_t, piece_of_head(query, s * 16 + h * 8, a.hd, i < seq.nq));
-    // Scores are kept as they are without a bias (units of `unit` powers of two), and scaled, in natural units, with one: a table may hold a type's lowest
-    // number, whose multiple by LOG2E does not exist.
+    // Scores are in units of `unit` powers of two: as the products give them without a bias, natural ones with one.  Of a tile whose keys all have the last bucket's
+    // bias (far) it is not added, but enters the largest score and the exponent as a whole.
     const float unit = BIAS ? LOG2E : a.scale * LOG2E, grows = GROWS / unit;
     f32x16 out[HD / 32] = {}, scores[2];
+    bool far[2] = {};
     float most = -INFINITY, used = -INFINITY, from = 0.0f, shift = SHIFT<DT>, sum = 0.0f;
+    // A query that has seen nothing but a table's lowest numbers sees no key of a far tile: all are -inf there.
+    const auto far_plus = [&](float from) { return from < -LOWEST ? -INFINITY : __builtin_fmaf(far_bias - from, LOG2E, SHIFT<DT>); };
     // What is left of a tile's scores: the bias, and -inf where a query does not see a key.
-    const auto add_bias = [&](f32x16 &s, int k0, int part) __attribute__((always_inline)) {
+    const auto add_bias = [&](f32x16 &s, bool &is, int k0, int part) __attribute__((always_inline)) {
         if constexpr (BIAS) {
-            if (is_far(k0)) {
-#pragma unroll
-                for (int e = 0; e < 16; ++e) s[e] = __builtin_fmaf(s[e], a.scale, far_bias);
-            } else {
+            is = is_far(k0);
+            if (!is) {
                 const float *const at = by_distance[part] + QUERIES - 1 - (w * 32 + (lane & 31)) + 4 * h;
 #pragma unroll
                 for (int e = 0; e < 16; ++e) s[e] = __builtin_fmaf(s[e], a.scale, at[8 * (e / 4) + e % 4]);
             }
         }
     };
-    const auto finish = [&](f32x16 &s, int k0, int part) __attribute__((always_inline)) {
-        add_bias(s, k0, part);
+    const auto finish = [&](f32x16 &s, bool &is, int k0, int part) __attribute__((always_inline)) {
+        add_bias(s, is, k0, part);
         const bool all = k0 + KEYS - 1 <= of_wave && (k0 > of_wave + 31 - a.window || k0 + KEYS <= a.sinks);
         if (!all) {
 #pragma unroll
@@ -117,16 +120,18 @@ __global__ __launch_bounds__(256, 2) void k_attend(Attn a) {
     const auto products = [&](auto part_, auto &&between) __attribute__((always_inline)) {
         constexpr int part = part_, after = (part + 1) % RING;
         f32x16 &now = scores[part & 1], &next = scores[after & 1];
-        float largest = most;
+        const bool &is = far[part & 1];
+        float largest = now[0];
 #pragma unroll
-        for (int e = 0; e < 16; ++e) largest = fmaxf(largest, now[e]);
-        most = max_of_halves(largest);
+        for (int e = 1; e < 16; ++e) largest = fmaxf(largest, now[e]);
+        if (BIAS && is) largest = __builtin_fmaf(largest, a.scale, far_bias);
+        most = max_of_halves(fmaxf(most, largest));
         if (__any(most > used + grows)) {
             const bool some = most > -INFINITY;
             const float times = some ? exp2_((used - most) * unit) : 1.0f;          // 0 at first
             used = most;
             from = some ? most : 0.0f;
-            shift = SHIFT<DT> - from * unit;
+            shift = BIAS && fabsf(from) > USUAL ? SHIFT<DT> : SHIFT<DT> - from * unit;
             sum *= times;
 #pragma unroll
             for (int d = 0; d < HD / 32; ++d) out[d] *= times;
@@ -134,12 +139,18 @@ __global__ __launch_bounds__(256, 2) void k_attend(Attn a) {
         if constexpr (FILL) arrived<FILLS>();           // tile t + 2 may be on its way
         else __syncthreads();
         between();
+        if (BIAS && !is && __any(fabsf(from) > USUAL)) {       // a table's lowest numbers, whose multiples by LOG2E do not exist
+#pragma unroll
+            for (int e = 0; e < 16; ++e) now[e] = fabsf(from) > USUAL ? now[e] - from : now[e];
+        }
+        const float times = BIAS && is ? a.scale * LOG2E : unit, plus = BIAS && is ? far_plus(from) : shift;
+        __builtin_amdgcn_s_setprio(1);
         next = f32x16{};                    // behind the last tile: of whatever the ring holds, and not looked at
 #pragma unroll
         for (int c = 0; c < STEPS; ++c) next = mfma32<DT>(T::rows(tiles[after][0], 0, c, lane), q[c], next);
 #pragma unroll
         for (int e = 0; e < 16; ++e) {
-            now[e] = exp2_(BIAS ? __builtin_fmaf(now[e] - from, unit, SHIFT<DT>) : __builtin_fmaf(now[e], unit, shift));
+            now[e] = exp2_(__builtin_fmaf(now[e], times, plus));
             sum += now[e];
         }
         asm volatile("" : "+v"(sum));       // beside the products, not behind them
@@ -149,6 +160,7 @@ __global__ __launch_bounds__(256, 2) void k_attend(Attn a) {
 #pragma unroll
             for (int d = 0; d < HD / 32; ++d) out[d] = mfma32<DT>(T::columns(tiles[part][1], k * 16, d, lane), p, out[d]);
         }
+        __builtin_amdgcn_s_setprio(0);
     };
     const auto step = [&](auto part_, int t) __attribute__((always_inline)) {
         constexpr int part = part_, after = (part + 1) % RING;
@@ -158,7 +170,7 @@ __global__ __launch_bounds__(256, 2) void k_attend(Attn a) {
                 else fill_none((part + 3) % RING);
             }
         });
-        if (t + 1 < seen.tiles) finish(scores[after & 1], seen.tile(t + 1) * KEYS, after);
+        if (t + 1 < seen.tiles) finish(scores[after & 1], far[after & 1], seen.tile(t + 1) * KEYS, after);
         if constexpr (!FILL) {
             if (t + 2 < seen.tiles) stage(t + 2, (part + 2) % RING);
             if (t + 3 < seen.tiles) load(t + 3);
@@ -174,7 +186,7 @@ __global__ __launch_bounds__(256, 2) void k_attend(Attn a) {
                 if constexpr (BIAS) stage_bias(key0 + 3 * KEYS, third);
             }
         });
-        add_bias(scores[after & 1], key0 + KEYS, after);
+        add_bias(scores[after & 1], far[after & 1], key0 + KEYS, after);
         if constexpr (!FILL) {
             from_k.store_whole(tiles[second][0], a.hd);
             from_v.store_whole(tiles[second][1], a.hd);
@@ -206,7 +218,7 @@ __global__ __launch_bounds__(256, 2) void k_attend(Attn a) {
         scores[0] = f32x16{};
 #pragma unroll
         for (int c = 0; c < STEPS; ++c) scores[0] = mfma32<DT>(T::rows(tiles[0][0], 0, c, lane), q[c], scores[0]);
-        finish(scores[0], seen.tile(0) * KEYS, 0);
+        finish(scores[0], far[0], seen.tile(0) * KEYS, 0);
         if constexpr (!FILL) {
             if (seen.tiles > 1) stage(1, 1);
             if (seen.tiles > 2) load(2);
@@ -566,9 +578,6 @@ Plan plan_of(const paro_attn_t &d) {
     }
     return p;
 }
-
-// Rows that lie on 16 bytes and heads of whole pieces.
-bool fills_take(const Rows &r, int hd) { return hd % 8 == 0 && r.ld % 8 == 0 && r.head % 8 == 0 && reinterpret_cast<uintptr_t>(r.at) % 16 == 0; }
 
 template <int DT, int HD, bool BIAS>
 void launch(const Attn &a, const Plan &p, char *workspace, hipStream_t st) {

@@ -18,6 +18,8 @@ typedef _Float16 f16x8_t __attribute__((ext_vector_type(8)));
 
 constexpr float LOG2E = 1.44269504088896340736f, LN2 = 0.69314718055994530942f;
 constexpr int MAX_BUCKETS = 256, MIN_HEAD = 8, MAX_HEAD = 128;
+constexpr float USUAL = 1e5f;            // a score in size, up to which LOG2E times it says enough of it
+constexpr float LOWEST = 1e38f;          // ... from which, below zero, it is a table's lowest number
 constexpr int FAR_AWAY = 1 << 30;        // a window that holds every key: lengths are at most this
 
 template <int DT>
@@ -114,8 +116,8 @@ struct Seen {
     __device__ __forceinline__ bool holds(int j) const { return j < end && (j >= low || j < sinks); }
 };
 __device__ __forceinline__ bool sees(int p, int j, int window, int sinks) {
-    const int far = p - j;
-    return (unsigned)far < (unsigned)window || (far >= 0 && j < sinks);
+    const int reach = j < sinks ? INT32_MAX : window;
+    return (unsigned)(p - j) < (unsigned)reach;
 }
 
 // ---------------------------------------------------------------- tiles of rows in shared memory
@@ -245,12 +247,13 @@ struct Staged {
 
 // The same without registers: 16 bytes a lane from memory to shared memory at `to` + 16 * lane, past the registers; lanes without a piece are sent NOWHERE, where the
 // hardware reads zeros.  Rows have to lie on 16 bytes.  In assembly because the compiler, which cannot tell the tiles apart, would wait for it before every read
-// of shared memory; arrived() waits.  It writes no register; m0, which holds the place in shared memory, is an operand, and one instruction has to stand between
-// its write and its use.
+// of shared memory; arrived() waits.  It writes no register; m0, which holds the place in shared memory, is an operand.  Five wait states have to stand between a
+// vector instruction that writes a scalar register (v_readlane, where the compiler has kept the descriptor in a lane) and its use by a load, one between a write of m0
+// and its use; inside the assembly the compiler does not see to it.
 typedef __attribute__((address_space(3))) char lds_char;
 template <int AT>
 __device__ __forceinline__ void fill(u32x4 from, unsigned offset, unsigned to) {
-    asm volatile("s_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"{m0}"(to + AT), "v"(offset), "s"(from) : "memory");
+    asm volatile("s_nop 4\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"{m0}"(to + AT), "v"(offset), "s"(from) : "memory");
 }
 // All but the wave's last `IN_FLIGHT` loads have arrived, all its accesses of shared memory are done; then those of all waves.
 template <int IN_FLIGHT>
@@ -393,6 +396,8 @@ inline int check_room(const std::string &f, int64_t needed, const void *workspac
     if (rc) return rc;
     return bytes < needed ? fail(PARO_ERANGE, f + "the workspace is smaller than paro_attn_workspace says") : PARO_OK;
 }
+// Rows that lie on 16 bytes and heads of whole pieces: what goes past the registers.
+inline bool fills_take(const Rows &r, int hd) { return hd % 8 == 0 && r.ld % 8 == 0 && r.head % 8 == 0 && reinterpret_cast<uintptr_t>(r.at) % 16 == 0; }
 inline Attn attn_of(const paro_attn_t &d, const void *q, const void *k, const void *v, const int32_t *q_starts, const int32_t *k_starts, const int32_t *k_lens,
                     const void *table, const int32_t *first) {
     const auto rows = [&](const void *at, int64_t heads, int64_t ld, int64_t head) {

@@ -22,19 +22,19 @@ constexpr float SHIFT = DT == PARO_F16 ? 15.0f : 0.0f;
 struct Grad {
     Attn a;
     Rows dout, dq, dk, dv;
-    // [head][rows_q]: without a bias, P = exp2(q . k * scale * LOG2E - base); with one, exp2((s - base) * LOG2E - log_sum); D
-    float *base, *log_sum, *dots;
+    // [head][rows_q]: P = exp2(s * LOG2E - base); D.  Of a bias, whose largest score may be a table's lowest number: P = exp2((s - peak) * LOG2E - log_sum)
+    float *base, *dots, *peak, *log_sum;
     float *largest;                          // of fp16: the largest |dout_i|^2 and |v_j|^2 of each block of k_dots
     float *times;                            // of fp16: what dS is multiplied by, and the inverse
     float *partial;                          // of shared key tiles: [slot][dk, dv][128][HD]
     float *of_table;                         // [head][sequence][tile of queries][bucket]
     char *dtable;
-    int blocks_q, blocks_v;                  // of k_dots
+    int blocks_q, blocks_v, blocks_heads;    // of k_dots
     int key_tiles, sink_tiles, shares, sink_shares, slots;      // of a sequence's key head; sink_tiles: the first ones, whose keys are sinks
 };
 
 // ---------------------------------------------------------------- statistics of the rows
-constexpr int DOT_ROWS = 16;
+constexpr int DOT_ROWS = 32, DOT_HEADS = 8;
 
 template <int HD>
 __device__ __forceinline__ float over_lanes(float x) {       // of HD / 8 lanes side by side
@@ -42,49 +42,64 @@ __device__ __forceinline__ float over_lanes(float x) {       // of HD / 8 lanes 
     for (int n = 1; n < HD / 8; n *= 2) x += __shfl_xor(x, n);
     return x;
 }
-// D, and what P is formed from; blocks behind those of the queries: the values' largest row.
+// D, and what P is formed from, of 32 rows of 8 heads; blocks behind those of the queries: the values' largest row.
 template <int DT, int HD>
 __global__ __launch_bounds__(256) void k_dots(Grad g) {
     const Attn &a = g.a;
-    constexpr int LANES = HD / 8, AT_ONCE = 256 / LANES;
+    constexpr int LANES = HD / 8, AT_ONCE = 256 / LANES, U = 4;
+    __shared__ float dots[DOT_HEADS][DOT_ROWS + 1];
     const bool of_values = (int)blockIdx.x >= g.blocks_q;
-    const unsigned tiles = of_values ? g.blocks_v / a.batch : g.blocks_q / a.batch, block = of_values ? blockIdx.x - g.blocks_q : blockIdx.x;
-    const int b = block / tiles, row0 = block % tiles * DOT_ROWS, piece = threadIdx.x % LANES;
+    const unsigned tiles = (of_values ? g.blocks_v : g.blocks_q) / a.batch, block = of_values ? blockIdx.x - g.blocks_q : blockIdx.x;
+    const int b = block / tiles, row0 = block % tiles * DOT_ROWS, column = threadIdx.x % LANES * 8, head0 = blockIdx.y * DOT_HEADS;
     const Sequence seq(a, b);
     const int heads = of_values ? a.kv_heads : a.heads, n = of_values ? seq.nk : seq.nq;
-    const int rows = n - row0 < DOT_ROWS ? n - row0 : DOT_ROWS;
+    const int rows = n - row0 < DOT_ROWS ? n - row0 : DOT_ROWS, items = rows > 0 && head0 < heads ? rows * DOT_HEADS : 0;
     float largest = 0.0f;
-    for (int x = threadIdx.x / LANES; x < rows * heads; x += AT_ONCE) {
-        const int i = row0 + x / heads, head = x % heads;
-        float u[8], o[8];
-        float squares = 0.0f, dot = 0.0f;
-        if (of_values) {
-            unpack<DT>(piece_of_head(a.v.of((int64_t)seq.k0 + i, head), piece * 8, a.hd, true), u);
-        } else {
-            unpack<DT>(piece_of_head(g.dout.of((int64_t)seq.q0 + i, head), piece * 8, a.hd, true), u);
-            unpack<DT>(piece_of_head(a.out.of((int64_t)seq.q0 + i, head), piece * 8, a.hd, true), o);
+    for (int x0 = threadIdx.x / LANES; x0 < items; x0 += U * AT_ONCE) {
+        u32x4 u_raw[U], o_raw[U];
+        int r[U], head[U];
 #pragma unroll
-            for (int e = 0; e < 8; ++e) dot += u[e] * o[e];
-        }
-#pragma unroll
-        for (int e = 0; e < 8; ++e) squares += u[e] * u[e];
-        if constexpr (DT == PARO_F16) {
-            squares = over_lanes<HD>(squares);
-            if (squares < INFINITY) largest = fmaxf(largest, squares);          // a row that is not finite leaves the others' scale alone
-        }
-        if (of_values) continue;
-        dot = over_lanes<HD>(dot);
-        if (piece == 0) {
-            const float *const stats = a.stats + (((int64_t)seq.q0 + i) * a.heads + head) * 2;
-            const float most = stats[0], log_sum = stats[1];
-            const int64_t at = (int64_t)head * a.rows_q + seq.q0 + i;
-            const bool empty = most == -INFINITY;
-            g.dots[at] = dot;
-            if (a.buckets) {
-                g.base[at] = empty ? INFINITY : most;
-                g.log_sum[at] = empty ? 0.0f : log_sum * LOG2E - SHIFT<DT>;
+        for (int u = 0; u < U; ++u) {
+            const int x = x0 + u * AT_ONCE, at = x < items ? x : items - 1;
+            r[u] = at / DOT_HEADS;
+            head[u] = head0 + at % DOT_HEADS < heads ? head0 + at % DOT_HEADS : heads - 1;
+            if (of_values) {
+                u_raw[u] = o_raw[u] = piece_of_head(a.v.of((int64_t)seq.k0 + row0 + r[u], head[u]), column, a.hd, true);
             } else {
-                g.base[at] = empty ? INFINITY : __builtin_fmaf(most, LOG2E, log_sum * LOG2E) - SHIFT<DT>;
+                u_raw[u] = piece_of_head(g.dout.of((int64_t)seq.q0 + row0 + r[u], head[u]), column, a.hd, true);
+                o_raw[u] = piece_of_head(a.out.of((int64_t)seq.q0 + row0 + r[u], head[u]), column, a.hd, true);
+            }
+        }
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            float x[8], o[8], dot = 0.0f, squares = 0.0f;
+            unpack<DT>(u_raw[u], x);
+            unpack<DT>(o_raw[u], o);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) dot += x[e] * o[e];
+            if constexpr (DT == PARO_F16) {
+#pragma unroll
+                for (int e = 0; e < 8; ++e) squares += x[e] * x[e];
+                squares = over_lanes<HD>(squares);
+                if (squares < INFINITY) largest = fmaxf(largest, squares);          // a row that is not finite leaves the others' scale alone
+            }
+            dot = over_lanes<HD>(dot);
+            if (column == 0) dots[head[u] - head0][r[u]] = dot;
+        }
+    }
+    __syncthreads();
+    if (!of_values) {
+        const int r = threadIdx.x % DOT_ROWS, head = head0 + threadIdx.x / DOT_ROWS;
+        if (r < rows && head < heads) {
+            const float *const stats = a.stats + (((int64_t)seq.q0 + row0 + r) * a.heads + head) * 2;
+            const float most = stats[0], log_sum = stats[1];
+            const int64_t at = (int64_t)head * a.rows_q + seq.q0 + row0 + r;
+            const bool empty = most == -INFINITY;
+            g.dots[at] = dots[threadIdx.x / DOT_ROWS][r];
+            g.base[at] = empty ? INFINITY : __builtin_fmaf(most, LOG2E, log_sum * LOG2E) - SHIFT<DT>;
+            if (a.buckets) {
+                g.peak[at] = empty ? INFINITY : most;
+                g.log_sum[at] = empty ? 0.0f : log_sum * LOG2E - SHIFT<DT>;
             }
         }
     }
@@ -94,18 +109,21 @@ __global__ __launch_bounds__(256) void k_dots(Grad g) {
         for (int x = 1; x < 64; x *= 2) largest = fmaxf(largest, __shfl_xor(largest, x));
         if ((threadIdx.x & 63) == 0) of_waves[wave_of()] = largest;
         __syncthreads();
-        if (threadIdx.x == 0) g.largest[blockIdx.x] = fmaxf(fmaxf(of_waves[0], of_waves[1]), fmaxf(of_waves[2], of_waves[3]));
+        if (threadIdx.x == 0) g.largest[(int64_t)blockIdx.y * gridDim.x + blockIdx.x] = fmaxf(fmaxf(of_waves[0], of_waves[1]), fmaxf(of_waves[2], of_waves[3]));
     }
 }
 // |dP - D| is at most twice the largest |dout_i| |v_j|, as out is a mean of values.
 __global__ __launch_bounds__(256) void k_times(Grad g) {
     __shared__ float of_waves[2][4];
     float most[2] = {0.0f, 0.0f};
-    for (int x = threadIdx.x; x < g.blocks_q + g.blocks_v; x += 256) {
-        const float v = g.largest[x];
-        if (x < g.blocks_q) most[0] = fmaxf(most[0], v);
-        else most[1] = fmaxf(most[1], v);
-    }
+    const int blocks = g.blocks_q + g.blocks_v;
+    for (int y = 0; y < g.blocks_heads; ++y)
+#pragma unroll 4
+        for (int x = threadIdx.x; x < blocks; x += 256) {
+            const float v = g.largest[(int64_t)y * blocks + x];
+            if (x < g.blocks_q) most[0] = fmaxf(most[0], v);
+            else most[1] = fmaxf(most[1], v);
+        }
 #pragma unroll
     for (int k = 0; k < 2; ++k) {
 #pragma unroll
@@ -150,14 +168,16 @@ __device__ __forceinline__ Share share_of(const Grad &g, int block, int of_kv) {
     return s;
 }
 
-template <int DT, int HD, bool BIAS>
+// FILL: queries and dout lie on 16 bytes and go to shared memory past the registers.
+template <int DT, int HD, bool BIAS, bool FILL>
 __global__ __launch_bounds__(256, 2) void k_grad_kv(Grad g) {
     using T = Tile<HD>;
     const Attn &a = g.a;
     constexpr int BYTES = Q_STEP * T::ROW, STEPS = HD / 16;
     __shared__ __attribute__((aligned(1024))) char tiles[2][2][BYTES];         // [buffer][queries, dout]
     __shared__ __attribute__((aligned(1024))) char values[BLOCK * T::ROW];
-    __shared__ float rows[2][3][Q_STEP];                                       // [buffer][base, log_sum, dots]
+    __shared__ __attribute__((aligned(16))) float rows[2][4][Q_STEP];          // [buffer][base, dots, peak, log_sum]
+    __shared__ int lowest[2];                                                  // whether the base of any row says too little
     __shared__ Bias bias;
     __shared__ float by_distance[2][BLOCK + Q_STEP];
     const int per_kv = g.sink_tiles * g.sink_shares + (g.key_tiles - g.sink_tiles) * g.shares;
@@ -179,27 +199,48 @@ __global__ __launch_bounds__(256, 2) void k_grad_kv(Grad g) {
 
     // The next step's head, and its first query.
     Staged<HD, Q_STEP> from_q, from_o;
+    const Filled<HD, Q_STEP> fill_q(a.q.ld, a.hd), fill_o(g.dout.ld, a.hd);
     float from_row = 0.0f;
     int next_head = 0, next_tile = 0;
-    const auto load = [&]() {
-        const int head = kv * group + next_head, i0 = (tile0 + next_tile) * Q_STEP;
-        from_q.load(a.q.of(seq.q0, head), a.q.ld, i0, seq.nq, a.hd);
-        from_o.load(g.dout.of(seq.q0, head), g.dout.ld, i0, seq.nq, a.hd);
-        if (threadIdx.x < 3 * Q_STEP && (BIAS || threadIdx.x < Q_STEP || threadIdx.x >= 2 * Q_STEP)) {
-            const int i = i0 + threadIdx.x % Q_STEP, which = threadIdx.x / Q_STEP;
-            const float *const of = which == 0 ? g.base : which == 1 ? g.log_sum : g.dots;
-            from_row = i < seq.nq ? of[(int64_t)head * a.rows_q + seq.q0 + i] : which == 0 ? INFINITY : 0.0f;
+    const auto load = [&](int buffer) __attribute__((always_inline)) {
+        const int head = kv * group + next_head, i0 = (tile0 + next_tile) * Q_STEP, which = threadIdx.x / Q_STEP, i = i0 + threadIdx.x % Q_STEP;
+        if (which < (BIAS ? 4 : 2)) {
+            const float *const of = which == 0 ? g.base : which == 1 ? g.dots : which == 2 ? g.peak : g.log_sum;
+            const float x = of[(int64_t)head * a.rows_q + seq.q0 + (i < seq.nq ? i : seq.nq - 1)];
+            from_row = i < seq.nq ? x : which % 2 == 0 ? INFINITY : 0.0f;
+        }
+        if constexpr (FILL) {
+            const u32x4 q_from = fill_q.descriptor(a.q.of((int64_t)seq.q0 + i0, head)), o_from = fill_o.descriptor(g.dout.of((int64_t)seq.q0 + i0, head));
+            if (i0 + Q_STEP <= seq.nq) {
+                fill_q.whole(q_from, tiles[buffer][0]);
+                fill_o.whole(o_from, tiles[buffer][1]);
+            } else {
+                const auto holds = [&](int r) { return i0 + r < seq.nq; };
+                fill_q.held(q_from, tiles[buffer][0], holds);
+                fill_o.held(o_from, tiles[buffer][1], holds);
+            }
+        } else {
+            from_q.load(a.q.of(seq.q0, head), a.q.ld, i0, seq.nq, a.hd);
+            from_o.load(g.dout.of(seq.q0, head), g.dout.ld, i0, seq.nq, a.hd);
         }
     };
     int far_from = 0, of_head = -1;
     float far_bias = 0.0f, next_far_bias = 0.0f;
-    const auto is_far = [&](int i0) { return BIAS && off + i0 - (k0 + BLOCK - 1) >= far_from; };
-    const auto stage = [&](int buffer) {
+    const auto is_far = [&](int i0, float last) { return BIAS && fabsf(last) < USUAL && off + i0 - (k0 + BLOCK - 1) >= far_from; };
+    const auto stage = [&](int buffer) __attribute__((always_inline)) {
         const int head = kv * group + next_head, i0 = (tile0 + next_tile) * Q_STEP;
-        const auto holds = [&](int r) { return i0 + r < seq.nq; };
-        from_q.store(tiles[buffer][0], a.hd, i0 + Q_STEP <= seq.nq, holds);
-        from_o.store(tiles[buffer][1], a.hd, i0 + Q_STEP <= seq.nq, holds);
-        if (threadIdx.x < 3 * Q_STEP) rows[buffer][threadIdx.x / Q_STEP][threadIdx.x % Q_STEP] = from_row;
+        if constexpr (!FILL) {
+            const auto holds = [&](int r) { return i0 + r < seq.nq; };
+            from_q.store(tiles[buffer][0], a.hd, i0 + Q_STEP <= seq.nq, holds);
+            from_o.store(tiles[buffer][1], a.hd, i0 + Q_STEP <= seq.nq, holds);
+        }
+        if (threadIdx.x < (BIAS ? 4 : 2) * Q_STEP) rows[buffer][threadIdx.x / Q_STEP][threadIdx.x % Q_STEP] = from_row;
+        if constexpr (BIAS) {
+            if (w == 1) {                                       // whose first half has the peaks
+                const bool any = __any(lane < 32 && fabsf(from_row) > USUAL && fabsf(from_row) < INFINITY);
+                if (lane == 0) lowest[buffer] = any;
+            }
+        }
         if constexpr (BIAS) {
             if (head != of_head) {
                 __syncthreads();
@@ -209,7 +250,7 @@ __global__ __launch_bounds__(256, 2) void k_grad_kv(Grad g) {
                 far_from = bias.first[a.buckets - 1];
                 next_far_bias = bias.column[a.buckets - 1];
             }
-            if (!is_far(i0) && threadIdx.x < BLOCK + Q_STEP - 1) by_distance[buffer][threadIdx.x] = bias.of(off + i0 - (k0 + BLOCK - 1) + (int)threadIdx.x, a.buckets);
+            if (!is_far(i0, next_far_bias) && threadIdx.x < BLOCK + Q_STEP - 1) by_distance[buffer][threadIdx.x] = bias.of(off + i0 - (k0 + BLOCK - 1) + (int)threadIdx.x, a.buckets);
         }
     };
 
@@ -229,7 +270,7 @@ __global__ __launch_bounds__(256, 2) void k_grad_kv(Grad g) {
     if (from < to) {
         next_head = from / per_head;
         next_tile = from % per_head;
-        load();
+        load(0);
         stage(0);
     }
     for (int u = from; u < to; ++u) {
@@ -239,8 +280,13 @@ __global__ __launch_bounds__(256, 2) void k_grad_kv(Grad g) {
             next_tile = 0;
             ++next_head;
         }
-        if (u + 1 < to) load();
-        __syncthreads();
+        if constexpr (FILL) {
+            arrived<0>();                    // this step's tiles; and all waves have left the last step's
+            if (u + 1 < to) load(buffer ^ 1);
+        } else {
+            if (u + 1 < to) load(buffer ^ 1);
+            __syncthreads();
+        }
         const char *const queries = tiles[buffer][0], *const douts = tiles[buffer][1];
         const bool none = first + Q_STEP - 1 < of_wave || (first - (of_wave + 31) >= a.window && of_wave >= a.sinks);
         if (!none) {
@@ -250,13 +296,10 @@ __global__ __launch_bounds__(256, 2) void k_grad_kv(Grad g) {
 #pragma unroll
             for (int c = 0; c < STEPS; ++c) dp = mfma32<DT>(T::rows(douts, 0, c, lane), T::rows(values, w * 32, c, lane), dp);
             const bool every = first >= of_wave + 31 && (first + Q_STEP - 1 - of_wave < a.window || of_wave + 31 < a.sinks);
+            const bool far = is_far(i0, far_bias);
             if constexpr (BIAS) {
-                const bool far = is_far(i0);
-                const float *const at = by_distance[buffer] + BLOCK - 1 - (w * 32 + (lane & 31)) + 4 * h;
-                if (far) {
-#pragma unroll
-                    for (int e = 0; e < 16; ++e) s[e] = __builtin_fmaf(s[e], a.scale, far_bias);
-                } else {
+                if (!far) {
+                    const float *const at = by_distance[buffer] + BLOCK - 1 - (w * 32 + (lane & 31)) + 4 * h;
 #pragma unroll
                     for (int e = 0; e < 16; ++e) s[e] = __builtin_fmaf(s[e], a.scale, at[8 * (e / 4) + e % 4]);
                 }
@@ -266,17 +309,27 @@ __global__ __launch_bounds__(256, 2) void k_grad_kv(Grad g) {
                 for (int e = 0; e < 16; ++e)
                     if (!sees(first + 8 * (e / 4) + 4 * h + e % 4, j, a.window, a.sinks)) s[e] = -INFINITY;
             }
+            const float by = BIAS && !far ? LOG2E : unit, plus = BIAS && far ? far_bias * LOG2E : 0.0f;
+            if (BIAS && lowest[buffer]) {                // a row's largest score may be a table's lowest number: P from the difference
+#pragma unroll
+                for (int e = 0; e < 16; ++e) {
+                    const int r = 8 * (e / 4) + 4 * h + e % 4;
+                    const float score = far ? __builtin_fmaf(s[e], a.scale, far_bias) : s[e], peak = rows[buffer][2][r];
+                    s[e] = peak < INFINITY ? exp2_(__builtin_fmaf(score - peak, LOG2E, -rows[buffer][3][r])) : 0.0f;
+                }
+            } else {
+#pragma unroll
+                for (int e = 0; e < 16; e += 4) {
+                    const f32x4 base = *reinterpret_cast<const f32x4 *>(rows[buffer][0] + 2 * e + 4 * h);
+#pragma unroll
+                    for (int x = 0; x < 4; ++x) s[e + x] = exp2_(__builtin_fmaf(s[e + x], by, BIAS ? plus - base[x] : -base[x]));
+                }
+            }
 #pragma unroll
             for (int e = 0; e < 16; e += 4) {
-                const f32x4 base = *reinterpret_cast<const f32x4 *>(rows[buffer][0] + 2 * e + 4 * h);
-                const f32x4 dot = *reinterpret_cast<const f32x4 *>(rows[buffer][2] + 2 * e + 4 * h);
-                f32x4 log_sum = {};
-                if constexpr (BIAS) log_sum = *reinterpret_cast<const f32x4 *>(rows[buffer][1] + 2 * e + 4 * h);
+                const f32x4 dot = *reinterpret_cast<const f32x4 *>(rows[buffer][1] + 2 * e + 4 * h);
 #pragma unroll
-                for (int x = 0; x < 4; ++x) {
-                    s[e + x] = exp2_(BIAS ? __builtin_fmaf(s[e + x] - base[x], LOG2E, -log_sum[x]) : __builtin_fmaf(s[e + x], unit, -base[x]));
-                    dp[e + x] = s[e + x] * (DT == PARO_F16 ? (dp[e + x] - dot[x]) * times : dp[e + x] - dot[x]);
-                }
+                for (int x = 0; x < 4; ++x) dp[e + x] = s[e + x] * (DT == PARO_F16 ? (dp[e + x] - dot[x]) * times : dp[e + x] - dot[x]);
             }
 #pragma unroll
             for (int k = 0; k < 2; ++k) {
@@ -336,15 +389,16 @@ __global__ __launch_bounds__(256) void k_grad_join(Grad g) {
 }
 
 // ---------------------------------------------------------------- dq, and the table's gradient
-template <int DT, int HD, bool BIAS>
+// FILL: keys and values lie on 16 bytes and go to shared memory past the registers.
+template <int DT, int HD, bool BIAS, bool FILL>
 __global__ __launch_bounds__(256, 2) void k_grad_q(Grad g) {
     using T = Tile<HD>;
     const Attn &a = g.a;
-    constexpr int KEYS = BIAS && HD == 128 ? 32 : 64;                           // of a tile: what lets two blocks into the shared memory
+    constexpr int KEYS = 32, RING = BIAS && HD == 128 ? 3 : 4;                  // so that two blocks go into the shared memory
     constexpr int BYTES = KEYS * T::ROW, STEPS = HD / 16, DISTANCES = 32 + KEYS, SQUARE = 36;
-    __shared__ __attribute__((aligned(1024))) char tiles[2][2][BYTES];          // [buffer][keys, values]
+    __shared__ __attribute__((aligned(1024))) char tiles[RING][2][BYTES];       // [part of the ring][keys, values]
     __shared__ Bias bias;
-    __shared__ float by_distance[2][BLOCK + KEYS];
+    __shared__ float by_distance[RING][BLOCK + KEYS];
     __shared__ __attribute__((aligned(16))) float squares[BIAS ? 4 : 1][BIAS ? 32 * SQUARE : 4];     // [wave]: 32 x 32 of dS
     __shared__ float diagonals[BIAS ? 4 : 1][DISTANCES];                        // [wave]: sums of dS along a distance, of one tile
     __shared__ float of_buckets[BIAS ? 4 : 1][BIAS ? MAX_BUCKETS : 1], far_sums[4];
@@ -365,40 +419,68 @@ __global__ __launch_bounds__(256, 2) void k_grad_q(Grad g) {
     const int kv = head / (a.heads / a.kv_heads);
     const char *const keys_at = a.k.of(seq.k0, kv), *const values_at = a.v.of(seq.k0, kv);
     Staged<HD, KEYS> from_k, from_v;
-    const auto load = [&](int t) {
+    const Filled<HD, KEYS> fill_k(a.k.ld, a.hd), fill_v(a.v.ld, a.hd);
+    constexpr int FILLS = 2 * Filled<HD, KEYS>::FILLS;
+    int far_from = 0;
+    float far_bias = 0.0f, far_sum = 0.0f;
+    bool usual = true;
+    const auto is_far = [&](int k0) { return BIAS && usual && first - (k0 + KEYS - 1) >= far_from; };
+    const auto stage_bias = [&](int k0, int part) __attribute__((always_inline)) {
+        if (!is_far(k0) && threadIdx.x < BLOCK + KEYS - 1) by_distance[part][threadIdx.x] = bias.of(first - k0 + BLOCK - 1 - (int)threadIdx.x, a.buckets);
+    };
+    const auto load = [&](int t) __attribute__((always_inline)) {
         const int k0 = seen.tile(t) * KEYS;
         from_k.load(keys_at, a.k.ld, k0, seq.nk, a.hd);
         from_v.load(values_at, a.v.ld, k0, seq.nk, a.hd);
     };
-    int far_from = 0;
-    float far_bias = 0.0f, far_sum = 0.0f;
-    const auto is_far = [&](int k0) { return BIAS && first - (k0 + KEYS - 1) >= far_from; };
-    const auto stage = [&](int t, int buffer) {
+    const auto stage = [&](int t, int part) __attribute__((always_inline)) {
         const int first_key = seen.tile(t) * KEYS;
+        if constexpr (BIAS) stage_bias(first_key, part);
         const auto holds = [&](int r) { return seen.holds(first_key + r); };
         const bool all = seen.holds_all(first_key);
-        from_k.store(tiles[buffer][0], a.hd, all, holds);
-        from_v.store(tiles[buffer][1], a.hd, all, holds);
-        if constexpr (BIAS) {
-            const int k0 = seen.tile(t) * KEYS;
-            if (!is_far(k0) && threadIdx.x < BLOCK + KEYS - 1) by_distance[buffer][threadIdx.x] = bias.of(first - k0 + BLOCK - 1 - (int)threadIdx.x, a.buckets);
+        from_k.store(tiles[part][0], a.hd, all, holds);
+        from_v.store(tiles[part][1], a.hd, all, holds);
+    };
+    const auto fill = [&](int t, int part) __attribute__((always_inline)) {
+        const int first_key = seen.tile(t) * KEYS;
+        if constexpr (BIAS) stage_bias(first_key, part);
+        const u32x4 k_from = fill_k.descriptor(keys_at + (int64_t)first_key * (a.k.ld * 2)), v_from = fill_v.descriptor(values_at + (int64_t)first_key * (a.v.ld * 2));
+        if (seen.holds_all(first_key)) {
+            fill_k.whole(k_from, tiles[part][0]);
+            fill_v.whole(v_from, tiles[part][1]);
+        } else {
+            const auto holds = [&](int r) { return seen.holds(first_key + r); };
+            fill_k.held(k_from, tiles[part][0], holds);
+            fill_v.held(v_from, tiles[part][1], holds);
         }
     };
-    if (seen.tiles) load(0);
+    // Nothing, in the place of a tile that is not there: the waits count on as many loads each time.
+    const auto fill_none = [&](int part) __attribute__((always_inline)) {
+        const auto holds = [](int) { return false; };
+        fill_k.held(fill_k.descriptor(keys_at), tiles[part][0], holds);
+        fill_v.held(fill_v.descriptor(values_at), tiles[part][1], holds);
+    };
+    if constexpr (!FILL) {
+        if (seen.tiles) load(0);
+    }
     if constexpr (BIAS) {
         bias.load(a, head);
         for (int x = threadIdx.x; x < 4 * MAX_BUCKETS; x += 256) of_buckets[x / MAX_BUCKETS][x % MAX_BUCKETS] = 0.0f;
         __syncthreads();
         far_from = bias.first[a.buckets - 1];
         far_bias = bias.column[a.buckets - 1];
+        usual = fabsf(far_bias) < USUAL;
     }
     short8_t q[STEPS], dout[STEPS];
-    float base = INFINITY, log_sum = 0.0f, dot = 0.0f;
+    float base = INFINITY, peak = INFINITY, log_sum = 0.0f, dot = 0.0f;
     if (i < seq.nq) {
         const int64_t at = (int64_t)head * a.rows_q + seq.q0 + i;
         base = g.base[at];
         dot = g.dots[at];
-        if constexpr (BIAS) log_sum = g.log_sum[at];
+        if constexpr (BIAS) {
+            peak = g.peak[at];
+            log_sum = g.log_sum[at];
+        }
     }
     {
         const int at = i < seq.nq ? i : seq.nq - 1;
@@ -411,82 +493,95 @@ __global__ __launch_bounds__(256, 2) void k_grad_q(Grad g) {
     }
     const float unit = a.scale * LOG2E, times = DT == PARO_F16 ? g.times[0] * 0x1p-15f : 1.0f;
     f32x16 dq[HD / 32] = {};
-    if (seen.tiles) stage(0, 0);
-    for (int t = 0; t < seen.tiles; ++t) {
-        const int k0 = seen.tile(t) * KEYS, buffer = t & 1;
-        if (t + 1 < seen.tiles) load(t + 1);
-        __syncthreads();
-        const char *const keys = tiles[buffer][0], *const values = tiles[buffer][1];
-        const bool none = k0 > of_wave + 31 || (k0 + KEYS <= of_wave - a.window + 1 && k0 >= a.sinks), far = is_far(k0);
+    const bool lowest = BIAS && __any(fabsf(peak) > USUAL && fabsf(peak) < INFINITY);       // a row's largest score may be a table's lowest number
+    const float far_plus = peak < -LOWEST ? -INFINITY : far_bias * LOG2E - base;            // (which sees no key with another bias)
+    // In step t tile t + RING - 1 (through registers: t + 1) goes to the part of the ring whose tile all waves have left.  As many steps a round as the ring has parts, so
+    // that these are constants.  PLAIN: every query sees the tile whole, and the tile that is brought is there whole.
+    const auto step = [&](auto part_, auto plain_, int t, int k0, const char *k_at, const char *v_at) __attribute__((always_inline)) {
+        constexpr int part = part_, PLAIN = plain_, coming = (part + RING - 1) % RING;
+        if constexpr (FILL) {
+            arrived<(RING - 2) * FILLS>();
+            if constexpr (PLAIN) {
+                fill_k.whole(fill_k.descriptor(k_at), tiles[coming][0]);
+                fill_v.whole(fill_v.descriptor(v_at), tiles[coming][1]);
+                if constexpr (BIAS) stage_bias(k0 + (RING - 1) * KEYS, coming);
+            } else {
+                if (t + RING - 1 < seen.tiles) fill(t + RING - 1, coming);
+                else fill_none(coming);
+            }
+        } else {
+            __syncthreads();
+        }
+        const char *const keys = tiles[part][0], *const values = tiles[part][1];
+        const bool none = !PLAIN && (k0 > of_wave + 31 || (k0 + KEYS <= of_wave - a.window + 1 && k0 >= a.sinks)), far = is_far(k0);
         if (want && !far) {
             for (int x = lane; x < DISTANCES; x += 64) diagonals[BIAS ? w : 0][x] = 0.0f;
         }
         if (!none) {
-            const bool every = k0 + KEYS - 1 <= of_wave && (k0 > of_wave + 31 - a.window || k0 + KEYS <= a.sinks);
+            f32x16 s = {}, dp = {};
 #pragma unroll
-            for (int n = 0; n < KEYS / 32; ++n) {
-                f32x16 s = {}, dp = {};
+            for (int c = 0; c < STEPS; ++c) s = mfma32<DT>(T::rows(keys, 0, c, lane), q[c], s);
 #pragma unroll
-                for (int c = 0; c < STEPS; ++c) s = mfma32<DT>(T::rows(keys, n * 32, c, lane), q[c], s);
+            for (int c = 0; c < STEPS; ++c) dp = mfma32<DT>(T::rows(values, 0, c, lane), dout[c], dp);
+            if constexpr (BIAS) {
+                if (!far) {
+                    const float *const at = by_distance[part] + BLOCK - 1 - (w * 32 + (lane & 31)) + 4 * h;
 #pragma unroll
-                for (int c = 0; c < STEPS; ++c) dp = mfma32<DT>(T::rows(values, n * 32, c, lane), dout[c], dp);
-                if constexpr (BIAS) {
-                    const float *const at = by_distance[buffer] + BLOCK - 1 - (w * 32 + (lane & 31)) + 4 * h + n * 32;
-                    if (far) {
-#pragma unroll
-                        for (int e = 0; e < 16; ++e) s[e] = __builtin_fmaf(s[e], a.scale, far_bias);
-                    } else {
-#pragma unroll
-                        for (int e = 0; e < 16; ++e) s[e] = __builtin_fmaf(s[e], a.scale, at[8 * (e / 4) + e % 4]);
-                    }
+                    for (int e = 0; e < 16; ++e) s[e] = __builtin_fmaf(s[e], a.scale, at[8 * (e / 4) + e % 4]);
                 }
-                if (!every) {
+            }
+            const bool every = PLAIN || (k0 + KEYS - 1 <= of_wave && (k0 > of_wave + 31 - a.window || k0 + KEYS <= a.sinks));
+            if (!every) {
 #pragma unroll
-                    for (int e = 0; e < 16; ++e)
-                        if (!sees(place, k0 + n * 32 + 8 * (e / 4) + 4 * h + e % 4, a.window, a.sinks)) s[e] = -INFINITY;
+                for (int e = 0; e < 16; ++e)
+                    if (!sees(place, k0 + 8 * (e / 4) + 4 * h + e % 4, a.window, a.sinks)) s[e] = -INFINITY;
+            }
+            if (BIAS && !far && lowest) {
+#pragma unroll
+                for (int e = 0; e < 16; ++e) s[e] = peak < INFINITY ? exp2_(__builtin_fmaf(s[e] - peak, LOG2E, -log_sum)) : 0.0f;
+            } else {
+                const float by = BIAS && !far ? LOG2E : unit, plus = BIAS && far ? far_plus : -base;
+#pragma unroll
+                for (int e = 0; e < 16; ++e) s[e] = exp2_(__builtin_fmaf(s[e], by, plus));
+            }
+#pragma unroll
+            for (int e = 0; e < 16; ++e) dp[e] = s[e] * (DT == PARO_F16 ? (dp[e] - dot) * times : dp[e] - dot);
+            if constexpr (BIAS) {
+                if (want && far) {
+#pragma unroll
+                    for (int e = 0; e < 16; ++e) far_sum += dp[e];
+                } else if (want) {
+                // Through shared memory (the wave's own, whose accesses go in their order): lane r of a half has of each of its 16 rows the key r in front of
+                // the row, modulo 32, which are two distances.  (LDS atomics instead: 8 x 1024 tokens of 12 heads of 64 this kernel 214 us.)
+                float *const square = squares[w];
+                asm volatile("" ::: "memory");
+#pragma unroll
+                for (int e = 0; e < 16; e += 4)
+                    *reinterpret_cast<f32x4 *>(square + (lane & 31) * SQUARE + 2 * e + 4 * h) = f32x4{dp[e], dp[e + 1], dp[e + 2], dp[e + 3]};
+                asm volatile("" ::: "memory");
+                float near = 0.0f, behind = 0.0f;                       // distances r, and r - 32, from the square's first row and key
+                const int r = lane & 31;
+#pragma unroll
+                for (int y = 0; y < 16; ++y) {
+                    const int row = h * 16 + y;
+                    const float x = square[row * SQUARE + ((row - r) & 31)];
+                    near += row >= r ? x : 0.0f;
+                    behind += row >= r ? 0.0f : x;
                 }
-#pragma unroll
-                for (int e = 0; e < 16; ++e) {
-                    const float p = exp2_(BIAS ? __builtin_fmaf(s[e] - base, LOG2E, -log_sum) : __builtin_fmaf(s[e], unit, -base));
-                    dp[e] = p * (DT == PARO_F16 ? (dp[e] - dot) * times : dp[e] - dot);
+                near = sum_of_halves(near);
+                behind = sum_of_halves(behind);
+                // place KEYS - 1 + distance; behind: of r = 0 there is none
+                const int place_of = KEYS - 1 + (h ? r - 32 : r);
+                asm volatile("" ::: "memory");
+                if (!h || r) diagonals[w][place_of] += h ? behind : near;
+                asm volatile("" ::: "memory");
                 }
-                if constexpr (BIAS) {
-                    if (want && far) {
+            }
 #pragma unroll
-                        for (int e = 0; e < 16; ++e) far_sum += dp[e];
-                    } else if (want) {
-                        // Through shared memory (the wave's own, whose accesses go in their order): lane r of a half has of each of its 16 rows the key r in front of
-                        // the row, modulo 32, which are two distances.  (LDS atomics instead: 8 x 1024 tokens of 12 heads of 64 this kernel 214 us.)
-                        float *const square = squares[w];
-                        asm volatile("" ::: "memory");
+            for (int k = 0; k < 2; ++k) {
+                const short8_t ds = pack8<DT>(dp, 8 * k);
 #pragma unroll
-                        for (int e = 0; e < 16; e += 4)
-                            *reinterpret_cast<f32x4 *>(square + (lane & 31) * SQUARE + 2 * e + 4 * h) = f32x4{dp[e], dp[e + 1], dp[e + 2], dp[e + 3]};
-                        asm volatile("" ::: "memory");
-                        float near = 0.0f, behind = 0.0f;                       // distances r, and r - 32, from the square's first row and key
-                        const int r = lane & 31;
-#pragma unroll
-                        for (int y = 0; y < 16; ++y) {
-                            const int row = h * 16 + y;
-                            const float x = square[row * SQUARE + ((row - r) & 31)];
-                            near += row >= r ? x : 0.0f;
-                            behind += row >= r ? 0.0f : x;
-                        }
-                        near = sum_of_halves(near);
-                        behind = sum_of_halves(behind);
-                        // place KEYS - 1 - n * 32 + distance; behind: of r = 0 there is none
-                        const int place_of = KEYS - 1 - n * 32 + (h ? r - 32 : r);
-                        asm volatile("" ::: "memory");
-                        if (!h || r) diagonals[w][place_of] += h ? behind : near;
-                        asm volatile("" ::: "memory");
-                    }
-                }
-#pragma unroll
-                for (int k = 0; k < 2; ++k) {
-                    const short8_t ds = pack8<DT>(dp, 8 * k);
-#pragma unroll
-                    for (int d = 0; d < HD / 32; ++d) dq[d] = mfma32<DT>(T::columns(keys, n * 32 + k * 16, d, lane), ds, dq[d]);
-                }
+                for (int d = 0; d < HD / 32; ++d) dq[d] = mfma32<DT>(T::columns(keys, k * 16, d, lane), ds, dq[d]);
             }
         }
         if constexpr (BIAS) {
@@ -509,7 +604,42 @@ __global__ __launch_bounds__(256, 2) void k_grad_q(Grad g) {
                 if (bucket >= 0 && (lane == 63 || next != bucket)) of_buckets[w][bucket] += sum;
             }
         }
-        if (t + 1 < seen.tiles) stage(t + 1, buffer ^ 1);
+        if constexpr (!FILL) {
+            if (t + 1 < seen.tiles) stage(t + 1, (part + 1) % RING);
+            if (t + 2 < seen.tiles) load(t + 2);
+        }
+    };
+    if (seen.tiles) {
+        int plain_from, plain_to;
+        seen.plain(a, first, last, plain_from, plain_to);
+        if constexpr (FILL) {
+            for (int t = 0; t < RING - 1; ++t) {
+                if (t < seen.tiles) fill(t, t);
+                else fill_none(t);
+            }
+        } else {
+            stage(0, 0);
+            if (seen.tiles > 1) load(1);
+        }
+        for (int t = 0; t < seen.tiles;) {
+            if (FILL && t >= plain_from && t + 2 * RING - 2 < plain_to) {
+                int k0 = seen.tile(t) * KEYS;
+                const int64_t k_step = a.k.ld * (2 * KEYS), v_step = a.v.ld * (2 * KEYS);
+                const char *k_at = keys_at + (int64_t)(seen.tile(t) + RING - 1) * k_step, *v_at = values_at + (int64_t)(seen.tile(t) + RING - 1) * v_step;
+                for (; t + 2 * RING - 2 < plain_to; t += RING)
+                    static_for<0, RING>([&](auto part) __attribute__((always_inline)) {
+                        step(part, std::integral_constant<int, 1>{}, 0, k0, k_at, v_at);
+                        k0 += KEYS;
+                        k_at += k_step;
+                        v_at += v_step;
+                    });
+            }
+            static_for<0, RING>([&](auto part) __attribute__((always_inline)) {
+                if (t < seen.tiles) step(part, std::integral_constant<int, 0>{}, t, seen.tile(t) * KEYS, nullptr, nullptr);
+                ++t;
+            });
+        }
+        if constexpr (FILL) arrived<0>();                       // nothing is on its way into the shared memory of the block that comes next
     }
     const float of_dq = DT == PARO_F16 ? a.scale * g.times[1] : a.scale;
     char *const to = g.dq.of((int64_t)seq.q0 + i, head);
@@ -555,8 +685,8 @@ __global__ __launch_bounds__(256) void k_table_grad(Grad g) {
 
 // ---------------------------------------------------------------- host
 struct Plan {
-    int blocks_q, blocks_v, tiles, key_tiles, sink_tiles, shares, sink_shares, slots;
-    int64_t kv_blocks, log_sum, dots, largest, times, partial, of_table, bytes;
+    int blocks_q, blocks_v, blocks_heads, tiles, key_tiles, sink_tiles, shares, sink_shares, slots;
+    int64_t kv_blocks, dots, peak, log_sum, largest, times, partial, of_table, bytes;
 };
 
 Plan plan_of(const paro_attn_t &d) {
@@ -565,6 +695,7 @@ Plan plan_of(const paro_attn_t &d) {
     const int64_t window = d.window && d.window < d.len_k ? d.window : d.len_k;
     p.blocks_q = (int)(ceil_div(d.len_q, DOT_ROWS) * d.batch);
     p.blocks_v = d.dtype == PARO_F16 ? (int)(ceil_div(d.len_k, DOT_ROWS) * d.batch) : 0;
+    p.blocks_heads = (int)ceil_div(d.heads, DOT_HEADS);
     p.tiles = (int)ceil_div(d.len_q, BLOCK);
     p.key_tiles = (int)ceil_div(d.len_k, BLOCK);
     // Tiles of keys are shared out where there are few of them; those with sinks, which every later query sees, by how many more see them than see others.
@@ -589,9 +720,10 @@ Plan plan_of(const paro_attn_t &d) {
         return was;
     };
     room(rows_q * d.heads);                                                     // base
-    p.log_sum = room(d.buckets ? rows_q * d.heads : 0);
     p.dots = room(rows_q * d.heads);
-    p.largest = room((int64_t)p.blocks_q + p.blocks_v);
+    p.peak = room(d.buckets ? rows_q * d.heads : 0);
+    p.log_sum = room(d.buckets ? rows_q * d.heads : 0);
+    p.largest = room(d.dtype == PARO_F16 ? ((int64_t)p.blocks_q + p.blocks_v) * p.blocks_heads : 0);
     p.times = room(2);
     p.partial = room((int64_t)p.slots * d.kv_heads * d.batch * 2 * BLOCK * hd);
     p.of_table = room((int64_t)d.heads * d.batch * p.tiles * d.buckets);
@@ -601,15 +733,20 @@ Plan plan_of(const paro_attn_t &d) {
 
 template <int DT, int HD, bool BIAS>
 void launch(const Grad &g, const Plan &p, hipStream_t st) {
-    if (p.blocks_q + p.blocks_v) hipLaunchKernelGGL((k_dots<DT, HD>), dim3((unsigned)(p.blocks_q + p.blocks_v)), dim3(256), 0, st, g);
+    if (p.blocks_q + p.blocks_v) hipLaunchKernelGGL((k_dots<DT, HD>), dim3((unsigned)(p.blocks_q + p.blocks_v), (unsigned)p.blocks_heads), dim3(256), 0, st, g);
     if constexpr (DT == PARO_F16) hipLaunchKernelGGL(k_times, dim3(1), dim3(256), 0, st, g);
     if (p.kv_blocks) {
-        hipLaunchKernelGGL((k_grad_kv<DT, HD, BIAS>), dim3((unsigned)p.kv_blocks), dim3(256), 0, st, g);
+        if (fills_take(g.a.q, g.a.hd) && fills_take(g.dout, g.a.hd)) hipLaunchKernelGGL((k_grad_kv<DT, HD, BIAS, true>), dim3((unsigned)p.kv_blocks), dim3(256), 0, st, g);
+        else hipLaunchKernelGGL((k_grad_kv<DT, HD, BIAS, false>), dim3((unsigned)p.kv_blocks), dim3(256), 0, st, g);
         const int joined = p.shares > 1 ? p.key_tiles : p.sink_shares > 1 ? p.sink_tiles : 0;
         if (joined)
             hipLaunchKernelGGL((k_grad_join<DT, HD>), dim3((unsigned)(joined * g.a.kv_heads * g.a.batch), BLOCK / (1024 / HD), 2), dim3(256), 0, st, g);
     }
-    if (p.tiles) hipLaunchKernelGGL((k_grad_q<DT, HD, BIAS>), dim3((unsigned)((int64_t)p.tiles * g.a.heads * g.a.batch)), dim3(256), 0, st, g);
+    const unsigned q_blocks = (unsigned)((int64_t)p.tiles * g.a.heads * g.a.batch);
+    if (q_blocks) {
+        if (fills_take(g.a.k, g.a.hd) && fills_take(g.a.v, g.a.hd)) hipLaunchKernelGGL((k_grad_q<DT, HD, BIAS, true>), dim3(q_blocks), dim3(256), 0, st, g);
+        else hipLaunchKernelGGL((k_grad_q<DT, HD, BIAS, false>), dim3(q_blocks), dim3(256), 0, st, g);
+    }
     if (BIAS && g.dtable) hipLaunchKernelGGL((k_table_grad<DT>), dim3((unsigned)g.a.heads), dim3(256), 0, st, g);
 }
 
@@ -659,8 +796,9 @@ int paro_attn_grad(const paro_attn_t *d, const void *dout, const void *q, const 
         g.dk = as(g.a.k, dk);
         g.dv = as(g.a.v, dv);
         g.base = floats(0);
-        g.log_sum = floats(p.log_sum);
         g.dots = floats(p.dots);
+        g.peak = floats(p.peak);
+        g.log_sum = floats(p.log_sum);
         g.largest = floats(p.largest);
         g.times = floats(p.times);
         g.partial = floats(p.partial);
@@ -668,6 +806,7 @@ int paro_attn_grad(const paro_attn_t *d, const void *dout, const void *q, const 
         g.dtable = static_cast<char *>(dtable);
         g.blocks_q = p.blocks_q;
         g.blocks_v = p.blocks_v;
+        g.blocks_heads = p.blocks_heads;
         g.key_tiles = p.key_tiles;
         g.sink_tiles = p.sink_tiles;
         g.shares = p.shares;
