@@ -24,15 +24,16 @@ __global__ __launch_bounds__(256, 2) void k_attend(Attn a) {
     __shared__ __attribute__((aligned(1024))) char tiles[RING][2][BYTES];    // [part of the ring][keys, values]
     __shared__ Bias bias;
     __shared__ float by_distance[RING][QUERIES + KEYS];
-    const unsigned work = in_runs(blockIdx.x, gridDim.x), of_head = work / a.tiles;
-    const int head = of_head % a.heads, b = of_head / a.heads, i0 = (int)(a.tiles - 1 - work % a.tiles) * QUERIES;     // the longest first
+    const int group = a.heads / a.kv_heads;
+    const Work work(blockIdx.x, a.batch * a.kv_heads, a.tiles * group);
+    const int kv = work.unit % a.kv_heads, b = work.unit / a.kv_heads, head = kv * group + work.within % group;
+    const int i0 = (a.tiles - 1 - work.within / group) * QUERIES;                      // the longest first
     const Sequence seq(a, b);
     if (i0 >= seq.nq) return;
     const int lane = threadIdx.x & 63, w = wave_of(), h = lane >> 5;
     const int off = seq.nk - seq.nq, first = i0 + off, last = (i0 + QUERIES < seq.nq ? i0 + QUERIES : seq.nq) - 1 + off;
     const Seen<KEYS> seen(a, first, last);
     const int of_wave = first + w * 32, place = of_wave + (lane & 31), i = i0 + w * 32 + (lane & 31);     // of the lane's query
-    const int kv = head / (a.heads / a.kv_heads);
 
     const char *const keys_at = a.k.of(seq.k0, kv), *const values_at = a.v.of(seq.k0, kv);
     Staged<HD, KEYS> from_k, from_v;
@@ -62,9 +63,14 @@ __global__ __launch_bounds__(256, 2) void k_attend(Attn a) {
         const int first_key = seen.tile(t) * KEYS;
         if constexpr (BIAS) stage_bias(first_key, part);
         const u32x4 k_from = fill_k.descriptor(keys_at + (int64_t)first_key * (a.k.ld * 2)), v_from = fill_v.descriptor(values_at + (int64_t)first_key * (a.v.ld * 2));
-        const auto holds = [&](int r) { return seen.holds(first_key + r); };
-        fill_k.held(k_from, tiles[part][0], holds);
-        fill_v.held(v_from, tiles[part][1], holds);
+        if (seen.holds_all(first_key)) {
+            fill_k.whole(k_from, tiles[part][0]);
+            fill_v.whole(v_from, tiles[part][1]);
+        } else {
+            const auto holds = [&](int r) { return seen.holds(first_key + r); };
+            fill_k.held(k_from, tiles[part][0], holds);
+            fill_v.held(v_from, tiles[part][1], holds);
+        }
     };
     // Nothing, in the place of a tile that is not there: the waits count on as many loads each time.
     const auto fill_none = [&](int part) __attribute__((always_inline)) {
@@ -117,60 +123,69 @@ __global__ __launch_bounds__(256, 2) void k_attend(Attn a) {
     };
     // In step t the scores of tile t + 1 are formed beside the exponentials of tile t, and the products with its values follow.  Meanwhile tile t + 3 (through
     // registers: t + 2) goes to the part of the ring whose tile all waves have left.  Four steps a round, so that the parts of the ring are constants.
-    const auto products = [&](auto part_, auto &&between) __attribute__((always_inline)) {
+    // What this wave's queries see of a tile: nothing?
+    const auto none = [&](int k0) { return k0 > of_wave + 31 || (k0 + KEYS <= of_wave - a.window + 1 && k0 >= a.sinks); };
+    const auto products = [&](auto part_, bool sees_now, bool sees_next, auto &&between) __attribute__((always_inline)) {
         constexpr int part = part_, after = (part + 1) % RING;
         f32x16 &now = scores[part & 1], &next = scores[after & 1];
         const bool &is = far[part & 1];
-        float largest = now[0];
+        if (sees_now) {
+            float largest = now[0];
 #pragma unroll
-        for (int e = 1; e < 16; ++e) largest = fmaxf(largest, now[e]);
-        if (BIAS && is) largest = __builtin_fmaf(largest, a.scale, far_bias);
-        most = max_of_halves(fmaxf(most, largest));
-        if (__any(most > used + grows)) {
-            const bool some = most > -INFINITY;
-            const float times = some ? exp2_((used - most) * unit) : 1.0f;          // 0 at first
-            used = most;
-            from = some ? most : 0.0f;
-            shift = BIAS && fabsf(from) > USUAL ? SHIFT<DT> : SHIFT<DT> - from * unit;
-            sum *= times;
+            for (int e = 1; e < 16; ++e) largest = fmaxf(largest, now[e]);
+            if (BIAS && is) largest = __builtin_fmaf(largest, a.scale, far_bias);
+            most = max_of_halves(fmaxf(most, largest));
+            if (__any(most > used + grows)) {
+                const bool some = most > -INFINITY;
+                const float times = some ? exp2_((used - most) * unit) : 1.0f;          // 0 at first
+                used = most;
+                from = some ? most : 0.0f;
+                shift = BIAS && fabsf(from) > USUAL ? SHIFT<DT> : SHIFT<DT> - from * unit;
+                sum *= times;
 #pragma unroll
-            for (int d = 0; d < HD / 32; ++d) out[d] *= times;
+                for (int d = 0; d < HD / 32; ++d) out[d] *= times;
+            }
         }
         if constexpr (FILL) arrived<FILLS>();           // tile t + 2 may be on its way
         else __syncthreads();
         between();
-        if (BIAS && !is && __any(fabsf(from) > USUAL)) {       // a table's lowest numbers, whose multiples by LOG2E do not exist
+        if (BIAS && sees_now && !is && __any(fabsf(from) > USUAL)) {       // a table's lowest numbers, whose multiples by LOG2E do not exist
 #pragma unroll
             for (int e = 0; e < 16; ++e) now[e] = fabsf(from) > USUAL ? now[e] - from : now[e];
         }
         const float times = BIAS && is ? a.scale * LOG2E : unit, plus = BIAS && is ? far_plus(from) : shift;
         __builtin_amdgcn_s_setprio(1);
-        next = f32x16{};                    // behind the last tile: of whatever the ring holds, and not looked at
+        if (sees_next) {                    // behind the last tile: of whatever the ring holds, and not looked at
+            next = f32x16{};
 #pragma unroll
-        for (int c = 0; c < STEPS; ++c) next = mfma32<DT>(T::rows(tiles[after][0], 0, c, lane), q[c], next);
-#pragma unroll
-        for (int e = 0; e < 16; ++e) {
-            now[e] = exp2_(__builtin_fmaf(now[e], times, plus));
-            sum += now[e];
+            for (int c = 0; c < STEPS; ++c) next = mfma32<DT>(T::rows(tiles[after][0], 0, c, lane), q[c], next);
         }
-        asm volatile("" : "+v"(sum));       // beside the products, not behind them
+        if (sees_now) {
 #pragma unroll
-        for (int k = 0; k < 2; ++k) {
-            const short8_t p = pack8<DT>(now, 8 * k);
+            for (int e = 0; e < 16; ++e) {
+                now[e] = exp2_(__builtin_fmaf(now[e], times, plus));
+                sum += now[e];
+            }
+            asm volatile("" : "+v"(sum));       // beside the products, not behind them
 #pragma unroll
-            for (int d = 0; d < HD / 32; ++d) out[d] = mfma32<DT>(T::columns(tiles[part][1], k * 16, d, lane), p, out[d]);
+            for (int k = 0; k < 2; ++k) {
+                const short8_t p = pack8<DT>(now, 8 * k);
+#pragma unroll
+                for (int d = 0; d < HD / 32; ++d) out[d] = mfma32<DT>(T::columns(tiles[part][1], k * 16, d, lane), p, out[d]);
+            }
         }
         __builtin_amdgcn_s_setprio(0);
     };
     const auto step = [&](auto part_, int t) __attribute__((always_inline)) {
         constexpr int part = part_, after = (part + 1) % RING;
-        products(part_, [&]() __attribute__((always_inline)) {
+        const bool sees_next = t + 1 < seen.tiles && !none(seen.tile(t + 1) * KEYS);
+        products(part_, !none(seen.tile(t) * KEYS), sees_next, [&]() __attribute__((always_inline)) {
             if constexpr (FILL) {
                 if (t + 3 < seen.tiles) fill(t + 3, (part + 3) % RING);
                 else fill_none((part + 3) % RING);
             }
         });
-        if (t + 1 < seen.tiles) finish(scores[after & 1], far[after & 1], seen.tile(t + 1) * KEYS, after);
+        if (sees_next) finish(scores[after & 1], far[after & 1], seen.tile(t + 1) * KEYS, after);
         if constexpr (!FILL) {
             if (t + 2 < seen.tiles) stage(t + 2, (part + 2) % RING);
             if (t + 3 < seen.tiles) load(t + 3);
@@ -179,7 +194,7 @@ __global__ __launch_bounds__(256, 2) void k_attend(Attn a) {
     // Where every query sees the tiles t + 1 to t + 3 whole, nothing is asked; key0: the first of tile t; k_at, v_at: of tile t + 3.
     const auto plain_step = [&](auto part_, int key0, const char *&k_at, const char *&v_at) __attribute__((always_inline)) {
         constexpr int part = part_, after = (part + 1) % RING, second = (part + 2) % RING, third = (part + 3) % RING;
-        products(part_, [&]() __attribute__((always_inline)) {
+        products(part_, true, true, [&]() __attribute__((always_inline)) {
             if constexpr (FILL) {
                 fill_k.whole(fill_k.descriptor(k_at), tiles[third][0]);
                 fill_v.whole(fill_v.descriptor(v_at), tiles[third][1]);

@@ -49,11 +49,25 @@ __device__ __forceinline__ float sum_of_halves(float x) {
     return __uint_as_float(both[0]) + __uint_as_float(both[1]);
 }
 
-// Blocks go to the eight XCDs in turn: each takes a run of the work of its own, so that the tiles of a head, which read the same keys, meet in its L2.
-__device__ __forceinline__ unsigned in_runs(unsigned block, unsigned all) {
-    const unsigned each = all / 8, more = all % 8, xcd = block % 8;
-    return xcd * each + (xcd < more ? xcd : more) + block / 8;
-}
+// Blocks go to the eight XCDs in turn.  A unit is the work of a sequence's key head, which reads the same keys and values over and over: it stays on one XCD, to meet
+// in its L2, and units go to the XCDs in turn, so that sequences of different lengths even out (runs of a sequence each: packed sequences of 1024 to 2048 tokens
+// forward 295 us, so 2xx); what is left over in the end is shared by all.
+struct Work {
+    int unit, within;
+    __device__ __forceinline__ Work(unsigned block, unsigned units, unsigned of_unit) {
+        const unsigned whole = units / 8 * 8 * of_unit;
+        if (block < whole) {
+            const unsigned k = block / 8;
+            unit = (int)(k / of_unit * 8 + block % 8);
+            within = (int)(k % of_unit);
+        } else {
+            const unsigned rest = block - whole, all = (units % 8) * of_unit, each = all / 8, more = all % 8, xcd = rest % 8;
+            const unsigned at = xcd * each + (xcd < more ? xcd : more) + rest / 8;
+            unit = (int)(units / 8 * 8 + at / of_unit);
+            within = (int)(at % of_unit);
+        }
+    }
+};
 
 // Rows of an array of heads: elements from token to token, and from head to head.
 struct Rows {

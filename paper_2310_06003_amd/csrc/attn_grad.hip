@@ -181,9 +181,9 @@ __global__ __launch_bounds__(256, 2) void k_grad_kv(Grad g) {
     __shared__ Bias bias;
     __shared__ float by_distance[2][BLOCK + Q_STEP];
     const int per_kv = g.sink_tiles * g.sink_shares + (g.key_tiles - g.sink_tiles) * g.shares;
-    const unsigned work = in_runs(blockIdx.x, gridDim.x);
-    const int of_kv = work / per_kv, kv = of_kv % a.kv_heads, b = of_kv / a.kv_heads;
-    const Share share = share_of(g, work % per_kv, of_kv);
+    const Work work(blockIdx.x, a.batch * a.kv_heads, per_kv);
+    const int of_kv = work.unit, kv = of_kv % a.kv_heads, b = of_kv / a.kv_heads;
+    const Share share = share_of(g, work.within, of_kv);
     const Sequence seq(a, b);
     const int k0 = share.tile * BLOCK;
     if (k0 >= seq.nk) return;
@@ -402,8 +402,10 @@ __global__ __launch_bounds__(256, 2) void k_grad_q(Grad g) {
     __shared__ __attribute__((aligned(16))) float squares[BIAS ? 4 : 1][BIAS ? 32 * SQUARE : 4];     // [wave]: 32 x 32 of dS
     __shared__ float diagonals[BIAS ? 4 : 1][DISTANCES];                        // [wave]: sums of dS along a distance, of one tile
     __shared__ float of_buckets[BIAS ? 4 : 1][BIAS ? MAX_BUCKETS : 1], far_sums[4];
-    const unsigned work = in_runs(blockIdx.x, gridDim.x), of_head = work / a.tiles;
-    const int head = of_head % a.heads, b = of_head / a.heads, tile = a.tiles - 1 - work % a.tiles, i0 = tile * BLOCK;
+    const int group = a.heads / a.kv_heads;
+    const Work work(blockIdx.x, a.batch * a.kv_heads, a.tiles * group);
+    const int kv = work.unit % a.kv_heads, b = work.unit / a.kv_heads, head = kv * group + work.within % group;
+    const int tile = a.tiles - 1 - work.within / group, i0 = tile * BLOCK;             // the longest first
     const bool want = BIAS && g.dtable;
     float *const of_table = g.of_table + (((int64_t)head * a.batch + b) * a.tiles + tile) * a.buckets;
     const Sequence seq(a, b);
@@ -416,7 +418,6 @@ __global__ __launch_bounds__(256, 2) void k_grad_q(Grad g) {
     const int off = seq.nk - seq.nq, first = i0 + off, last = (i0 + BLOCK < seq.nq ? i0 + BLOCK : seq.nq) - 1 + off;
     const Seen<KEYS> seen(a, first, last);
     const int of_wave = first + w * 32, place = of_wave + (lane & 31), i = i0 + w * 32 + (lane & 31);
-    const int kv = head / (a.heads / a.kv_heads);
     const char *const keys_at = a.k.of(seq.k0, kv), *const values_at = a.v.of(seq.k0, kv);
     Staged<HD, KEYS> from_k, from_v;
     const Filled<HD, KEYS> fill_k(a.k.ld, a.hd), fill_v(a.v.ld, a.hd);
