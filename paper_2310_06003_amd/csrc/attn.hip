@@ -16,14 +16,12 @@ constexpr float GROWS = 8.0f;                // powers of two that a row's share
 template <int DT>
 constexpr float SHIFT = DT == PARO_F16 ? 7.0f : 0.0f;
 
-// FILL: keys and values lie on 16 bytes and go to shared memory past the registers.
-template <int DT, int HD, bool BIAS, bool FILL>
+template <int DT, int HD, bool BIAS>
 __global__ __launch_bounds__(256, 2) void k_attend(Attn a) {
     using T = Tile<HD>;
     constexpr int BYTES = KEYS * T::ROW, STEPS = HD / 16, RING = 4;
     __shared__ __attribute__((aligned(1024))) char tiles[RING][2][BYTES];    // [part of the ring][keys, values]
     __shared__ Bias bias;
-    __shared__ float by_distance[RING][QUERIES + KEYS];
     const int group = a.heads / a.kv_heads;
     const Work work(blockIdx.x, a.batch * a.kv_heads, a.tiles * group);
     const int kv = work.unit % a.kv_heads, b = work.unit / a.kv_heads, head = kv * group + work.within % group;
@@ -35,39 +33,23 @@ __global__ __launch_bounds__(256, 2) void k_attend(Attn a) {
     const Seen<KEYS> seen(a, first, last);
     const int of_wave = first + w * 32, place = of_wave + (lane & 31), i = i0 + w * 32 + (lane & 31);     // of the lane's query
 
-    const char *const keys_at = a.k.of(seq.k0, kv), *const values_at = a.v.of(seq.k0, kv);
-    Staged<HD, KEYS> from_k, from_v;
-    const Filled<HD, KEYS> fill_k(a.k.ld, a.hd), fill_v(a.v.ld, a.hd);
+    const int64_t row_k = a.copied_k ? (int64_t)b * a.len_k : seq.k0, row_v = a.copied_v ? (int64_t)b * a.len_k : seq.k0;
+    const char *const keys_at = a.keys.of(row_k, kv), *const values_at = a.values.of(row_v, kv);
+    const int64_t k_step = a.keys.ld * (2 * KEYS), v_step = a.values.ld * (2 * KEYS);
+    const Filled<HD, KEYS> fill_k(a.keys.ld, a.hd), fill_v(a.values.ld, a.hd);
     constexpr int FILLS = 2 * Filled<HD, KEYS>::FILLS;
-    const auto load = [&](int t) __attribute__((always_inline)) {
-        const int k0 = seen.tile(t) * KEYS;
-        from_k.load(keys_at, a.k.ld, k0, seq.nk, a.hd);
-        from_v.load(values_at, a.v.ld, k0, seq.nk, a.hd);
-    };
-    int far_from = 0;                       // distances from here on have the last bucket's bias
-    float far_bias = 0.0f;
-    bool usual = true;
-    const auto is_far = [&](int k0) { return BIAS && usual && first - (k0 + KEYS - 1) >= far_from; };
-    const auto stage_bias = [&](int k0, int part) __attribute__((always_inline)) {
-        if (!is_far(k0) && threadIdx.x < QUERIES + KEYS - 1) by_distance[part][threadIdx.x] = bias.of(first - k0 + QUERIES - 1 - (int)threadIdx.x, a.buckets);
-    };
-    const auto stage = [&](int t, int part) __attribute__((always_inline)) {
-        const int first_key = seen.tile(t) * KEYS;
-        if constexpr (BIAS) stage_bias(first_key, part);
-        const auto holds = [&](int r) { return seen.holds(first_key + r); };
-        const bool all = seen.holds_all(first_key);
-        from_k.store(tiles[part][0], a.hd, all, holds);
-        from_v.store(tiles[part][1], a.hd, all, holds);
-    };
+    Distances by_distance{};
+    const auto lowest = [&](int k0) { return first - (k0 + KEYS - 1); };
+    const auto is_far = [&](int k0) { return BIAS && by_distance.usual && by_distance.beyond(lowest(k0)); };
     const auto fill = [&](int t, int part) __attribute__((always_inline)) {
-        const int first_key = seen.tile(t) * KEYS;
-        if constexpr (BIAS) stage_bias(first_key, part);
-        const u32x4 k_from = fill_k.descriptor(keys_at + (int64_t)first_key * (a.k.ld * 2)), v_from = fill_v.descriptor(values_at + (int64_t)first_key * (a.v.ld * 2));
-        if (seen.holds_all(first_key)) {
+        const int tile = seen.tile(t), k0 = tile * KEYS;
+        if constexpr (BIAS) by_distance.look_up(bias, lowest(k0), part, a.buckets);
+        const u32x4 k_from = fill_k.descriptor(keys_at + tile * k_step), v_from = fill_v.descriptor(values_at + tile * v_step);
+        if (seen.holds_all(k0)) {
             fill_k.whole(k_from, tiles[part][0]);
             fill_v.whole(v_from, tiles[part][1]);
         } else {
-            const auto holds = [&](int r) { return seen.holds(first_key + r); };
+            const auto holds = [&](int r) { return seen.holds(k0 + r); };
             fill_k.held(k_from, tiles[part][0], holds);
             fill_v.held(v_from, tiles[part][1], holds);
         }
@@ -79,15 +61,11 @@ __global__ __launch_bounds__(256, 2) void k_attend(Attn a) {
         fill_v.held(fill_v.descriptor(values_at), tiles[part][1], holds);
     };
 
-    if constexpr (!FILL) {
-        if (seen.tiles) load(0);
-    }
     if constexpr (BIAS) {
         bias.load(a, head);
         __syncthreads();
-        far_from = bias.first[a.buckets - 1];
-        far_bias = bias.column[a.buckets - 1];
-        usual = fabsf(far_bias) < USUAL;
+        by_distance.begin(bias, a.buckets);
+        __syncthreads();
     }
     short8_t q[STEPS];
     const char *const query = a.q.of((int64_t)seq.q0 + (i < seq.nq ? i : seq.nq - 1), head);
@@ -100,15 +78,15 @@ __global__ __launch_bounds__(256, 2) void k_attend(Attn a) {
     bool far[2] = {};
     float most = -INFINITY, used = -INFINITY, from = 0.0f, shift = SHIFT<DT>, sum = 0.0f;
     // A query that has seen nothing but a table's lowest numbers sees no key of a far tile: all are -inf there.
-    const auto far_plus = [&](float from) { return from < -LOWEST ? -INFINITY : __builtin_fmaf(far_bias - from, LOG2E, SHIFT<DT>); };
+    const auto far_plus = [&](float from) { return from < -LOWEST ? -INFINITY : __builtin_fmaf(by_distance.far - from, LOG2E, SHIFT<DT>); };
     // What is left of a tile's scores: the bias, and -inf where a query does not see a key.
     const auto add_bias = [&](f32x16 &s, bool &is, int k0, int part) __attribute__((always_inline)) {
         if constexpr (BIAS) {
             is = is_far(k0);
             if (!is) {
-                const float *const at = by_distance[part] + QUERIES - 1 - (w * 32 + (lane & 31)) + 4 * h;
+                const float *const at = by_distance.values(bias, lowest(k0), part) + (place - first) + 4 - 4 * h;
 #pragma unroll
-                for (int e = 0; e < 16; ++e) s[e] = __builtin_fmaf(s[e], a.scale, at[8 * (e / 4) + e % 4]);
+                for (int e = 0; e < 16; ++e) s[e] = __builtin_fmaf(s[e], a.scale, at[27 - (8 * (e / 4) + e % 4)]);
             }
         }
     };
@@ -121,8 +99,8 @@ __global__ __launch_bounds__(256, 2) void k_attend(Attn a) {
                 if (!sees(place, k0 + 8 * (e / 4) + 4 * h + e % 4, a.window, a.sinks)) s[e] = -INFINITY;
         }
     };
-    // In step t the scores of tile t + 1 are formed beside the exponentials of tile t, and the products with its values follow.  Meanwhile tile t + 3 (through
-    // registers: t + 2) goes to the part of the ring whose tile all waves have left.  Four steps a round, so that the parts of the ring are constants.
+    // In step t the scores of tile t + 1 are formed beside the exponentials of tile t, and the products with its values follow.  Meanwhile tile t + 3 goes to the
+    // part of the ring whose tile all waves have left.  Four steps a round, so that the parts of the ring are constants.
     // What this wave's queries see of a tile: nothing?
     const auto none = [&](int k0) { return k0 > of_wave + 31 || (k0 + KEYS <= of_wave - a.window + 1 && k0 >= a.sinks); };
     const auto products = [&](auto part_, bool sees_now, bool sees_next, auto &&between) __attribute__((always_inline)) {
@@ -133,7 +111,7 @@ __global__ __launch_bounds__(256, 2) void k_attend(Attn a) {
             float largest = now[0];
 #pragma unroll
             for (int e = 1; e < 16; ++e) largest = fmaxf(largest, now[e]);
-            if (BIAS && is) largest = __builtin_fmaf(largest, a.scale, far_bias);
+            if (BIAS && is) largest = __builtin_fmaf(largest, a.scale, by_distance.far);
             most = max_of_halves(fmaxf(most, largest));
             if (__any(most > used + grows)) {
                 const bool some = most > -INFINITY;
@@ -146,8 +124,7 @@ __global__ __launch_bounds__(256, 2) void k_attend(Attn a) {
                 for (int d = 0; d < HD / 32; ++d) out[d] *= times;
             }
         }
-        if constexpr (FILL) arrived<FILLS>();           // tile t + 2 may be on its way
-        else __syncthreads();
+        arrived<FILLS>();                   // tile t + 2 may be on its way
         between();
         if (BIAS && sees_now && !is && __any(fabsf(from) > USUAL)) {       // a table's lowest numbers, whose multiples by LOG2E do not exist
 #pragma unroll
@@ -177,40 +154,25 @@ __global__ __launch_bounds__(256, 2) void k_attend(Attn a) {
         __builtin_amdgcn_s_setprio(0);
     };
     const auto step = [&](auto part_, int t) __attribute__((always_inline)) {
-        constexpr int part = part_, after = (part + 1) % RING;
+        constexpr int part = part_, after = (part + 1) % RING, third = (part + 3) % RING;
         const bool sees_next = t + 1 < seen.tiles && !none(seen.tile(t + 1) * KEYS);
         products(part_, !none(seen.tile(t) * KEYS), sees_next, [&]() __attribute__((always_inline)) {
-            if constexpr (FILL) {
-                if (t + 3 < seen.tiles) fill(t + 3, (part + 3) % RING);
-                else fill_none((part + 3) % RING);
-            }
+            if (t + 3 < seen.tiles) fill(t + 3, third);
+            else fill_none(third);
         });
         if (sees_next) finish(scores[after & 1], far[after & 1], seen.tile(t + 1) * KEYS, after);
-        if constexpr (!FILL) {
-            if (t + 2 < seen.tiles) stage(t + 2, (part + 2) % RING);
-            if (t + 3 < seen.tiles) load(t + 3);
-        }
     };
-    // Where every query sees the tiles t + 1 to t + 3 whole, nothing is asked; key0: the first of tile t; k_at, v_at: of tile t + 3.
-    const auto plain_step = [&](auto part_, int key0, const char *&k_at, const char *&v_at) __attribute__((always_inline)) {
-        constexpr int part = part_, after = (part + 1) % RING, second = (part + 2) % RING, third = (part + 3) % RING;
+    // Where every query sees the tiles t + 1 to t + 3 whole, nothing is asked; k0: the first key of tile t; k_at, v_at: tile t + 3.
+    const auto plain_step = [&](auto part_, int k0, const char *&k_at, const char *&v_at) __attribute__((always_inline)) {
+        constexpr int part = part_, after = (part + 1) % RING, third = (part + 3) % RING;
         products(part_, true, true, [&]() __attribute__((always_inline)) {
-            if constexpr (FILL) {
-                fill_k.whole(fill_k.descriptor(k_at), tiles[third][0]);
-                fill_v.whole(fill_v.descriptor(v_at), tiles[third][1]);
-                if constexpr (BIAS) stage_bias(key0 + 3 * KEYS, third);
-            }
+            fill_k.whole(fill_k.descriptor(k_at), tiles[third][0]);
+            fill_v.whole(fill_v.descriptor(v_at), tiles[third][1]);
+            if constexpr (BIAS) by_distance.look_up(bias, lowest(k0 + 3 * KEYS), third, a.buckets);
         });
-        add_bias(scores[after & 1], far[after & 1], key0 + KEYS, after);
-        if constexpr (!FILL) {
-            from_k.store_whole(tiles[second][0], a.hd);
-            from_v.store_whole(tiles[second][1], a.hd);
-            if constexpr (BIAS) stage_bias(key0 + 2 * KEYS, second);
-            from_k.load_whole(k_at, a.k.ld, a.hd);
-            from_v.load_whole(v_at, a.v.ld, a.hd);
-        }
-        k_at += a.k.ld * (2 * KEYS);
-        v_at += a.v.ld * (2 * KEYS);
+        add_bias(scores[after & 1], far[after & 1], k0 + KEYS, after);
+        k_at += k_step;
+        v_at += v_step;
     };
     constexpr std::integral_constant<int, 0> p0{};
     constexpr std::integral_constant<int, 1> p1{};
@@ -219,34 +181,24 @@ __global__ __launch_bounds__(256, 2) void k_attend(Attn a) {
     if (seen.tiles) {
         int plain_from, plain_to;
         seen.plain(a, first, last, plain_from, plain_to);
-        if constexpr (FILL) {
-            for (int t = 0; t < 3; ++t) {
-                if (t < seen.tiles) fill(t, t);
-                else fill_none(t);
-            }
-            arrived<2 * FILLS>();
-        } else {
-            stage(0, 0);
-            if (seen.tiles > 1) load(1);
-            __syncthreads();
+        for (int t = 0; t < 3; ++t) {
+            if (t < seen.tiles) fill(t, t);
+            else fill_none(t);
         }
+        arrived<2 * FILLS>();
         scores[0] = f32x16{};
 #pragma unroll
         for (int c = 0; c < STEPS; ++c) scores[0] = mfma32<DT>(T::rows(tiles[0][0], 0, c, lane), q[c], scores[0]);
         finish(scores[0], far[0], seen.tile(0) * KEYS, 0);
-        if constexpr (!FILL) {
-            if (seen.tiles > 1) stage(1, 1);
-            if (seen.tiles > 2) load(2);
-        }
         for (int t = 0;;) {
             if (t >= plain_from && t + 6 < plain_to) {
-                int key0 = seen.tile(t) * KEYS;
-                const char *k_at = keys_at + (int64_t)(key0 + 3 * KEYS) * (a.k.ld * 2), *v_at = values_at + (int64_t)(key0 + 3 * KEYS) * (a.v.ld * 2);
-                for (; t + 6 < plain_to; t += 4, key0 += 4 * KEYS) {
-                    plain_step(p0, key0, k_at, v_at);
-                    plain_step(p1, key0 + KEYS, k_at, v_at);
-                    plain_step(p2, key0 + 2 * KEYS, k_at, v_at);
-                    plain_step(p3, key0 + 3 * KEYS, k_at, v_at);
+                int k0 = seen.tile(t) * KEYS;
+                const char *k_at = keys_at + (seen.tile(t) + 3) * k_step, *v_at = values_at + (seen.tile(t) + 3) * v_step;
+                for (; t + 6 < plain_to; t += 4, k0 += 4 * KEYS) {
+                    plain_step(p0, k0, k_at, v_at);
+                    plain_step(p1, k0 + KEYS, k_at, v_at);
+                    plain_step(p2, k0 + 2 * KEYS, k_at, v_at);
+                    plain_step(p3, k0 + 3 * KEYS, k_at, v_at);
                 }
             }
             step(p0, t);
@@ -258,7 +210,7 @@ __global__ __launch_bounds__(256, 2) void k_attend(Attn a) {
             step(p3, t);
             if (++t == seen.tiles) break;
         }
-        if constexpr (FILL) arrived<0>();               // nothing is on its way into the shared memory of the block that comes next
+        arrived<0>();                       // nothing is on its way into the shared memory of the block that comes next
     }
     sum = sum_of_halves(sum);
     const bool there = i < seq.nq;
@@ -578,6 +530,11 @@ Plan plan_of(const paro_attn_t &d) {
     p.few = d.len_q <= FEW;
     if (!p.few) {
         p.blocks = ceil_div(d.len_q, QUERIES) * d.heads * d.batch;
+        const auto copy = [&](int64_t ld, int64_t head) {
+            if (!fills_take(ld ? ld : d.kv_heads * d.head_dim, head ? head : d.head_dim, d.head_dim)) p.bytes += copy_bytes(d, d.len_k, d.kv_heads);
+        };
+        copy(d.ld_k, d.head_k);
+        copy(d.ld_v, d.head_v);
         return p;
     }
     const int64_t rows = std::max<int64_t>(1, d.len_q * group), head_dim = d.head_dim <= 64 ? 64 : 128;
@@ -597,8 +554,7 @@ Plan plan_of(const paro_attn_t &d) {
 template <int DT, int HD, bool BIAS>
 void launch(const Attn &a, const Plan &p, char *workspace, hipStream_t st) {
     if (!p.few) {
-        if (fills_take(a.k, a.hd) && fills_take(a.v, a.hd)) hipLaunchKernelGGL((k_attend<DT, HD, BIAS, true>), dim3((unsigned)p.blocks), dim3(256), 0, st, a);
-        else hipLaunchKernelGGL((k_attend<DT, HD, BIAS, false>), dim3((unsigned)p.blocks), dim3(256), 0, st, a);
+        hipLaunchKernelGGL((k_attend<DT, HD, BIAS>), dim3((unsigned)p.blocks), dim3(256), 0, st, a);
         return;
     }
     const Few f{p.shares, p.row_tiles, reinterpret_cast<float *>(workspace), reinterpret_cast<float *>(workspace + p.stats)};
@@ -634,6 +590,13 @@ int paro_attn(const paro_attn_t *d, const void *q, const void *k, const void *v,
         a.tiles = (int)ceil_div(d->len_q, QUERIES);
         hipStream_t st = static_cast<hipStream_t>(stream);
         char *ws = static_cast<char *>(workspace);
+        if (!p.few) {
+            if ((rc = check_aligned(f, a.k, a.hd, "k")) || (rc = check_aligned(f, a.v, a.hd, "v"))) return rc;
+            Copying copying(ws, 0);
+            a.copied_k = copying.take(*d, a.keys, d->len_k, d->kv_heads, true);
+            a.copied_v = copying.take(*d, a.values, d->len_k, d->kv_heads, true);
+            copying.launch(a, st);
+        }
 #define PARO_FORWARD(DT, HD, BIAS) launch<DT, HD, BIAS>(a, p, ws, st)
         PARO_BY_FORM(PARO_FORWARD);
 #undef PARO_FORWARD

@@ -78,6 +78,8 @@ struct Rows {
 
 struct Attn {
     Rows q, k, v, out;
+    Rows keys, values;                 // k and v as the fills take them: themselves, or copies, of sequence b from row b len_k on
+    bool copied_k, copied_v;
     const int32_t *q_starts, *k_starts, *k_lens;
     float *stats;
     const void *table;
@@ -217,50 +219,8 @@ __device__ __forceinline__ unsigned both(float a, float b) {
     else return __builtin_bit_cast(unsigned, __builtin_convertvector(f32x2{a, b}, bf16x2_t));
 }
 
-// A tile of rows on its way from memory to shared memory: each thread takes pieces of one column, PASSES rows.  Rows that the tile does not hold are read as others
-// of the sequence and staged as zeros.  A thread's place in a tile is a 32-bit offset that stays, the tile's a scalar address.
-template <int HD, int ROWS>
-struct Staged {
-    using T = Tile<HD>;
-    static constexpr int APART = 256 / T::PIECES, PASSES = ROWS / APART;
-    static_assert(PASSES >= 1 && ROWS % APART == 0, "every thread takes a piece of every pass");
-    u32x4 v[PASSES];
-
-    static __device__ __forceinline__ int column() { return (int)threadIdx.x % T::PIECES * 8; }
-    static __device__ __forceinline__ int row(int n) { return (int)threadIdx.x / T::PIECES + n * APART; }
-    static __device__ __forceinline__ unsigned offset(int r, unsigned ld, int hd) { return (unsigned)r * (ld * 2) + column_of(column(), hd) * 2; }
-    // row r of the tile is the sequence's row0 + r; `rows` of them exist (one at least, and row0 is one)
-    __device__ __forceinline__ void load(const char *of_head, int64_t ld, int row0, int rows, int hd) {
-        const char *const tile = of_head + (int64_t)row0 * (ld * 2);
-        const int last = rows - 1 - row0;
-        if (last >= ROWS - 1) {
-            load_whole(tile, ld, hd);
-        } else {
-#pragma unroll
-            for (int n = 0; n < PASSES; ++n) v[n] = *reinterpret_cast<const piece_at2 *>(tile + offset(row(n) < last ? row(n) : last, (unsigned)ld, hd));
-        }
-    }
-    __device__ __forceinline__ void load_whole(const char *tile, int64_t ld, int hd) {
-#pragma unroll
-        for (int n = 0; n < PASSES; ++n) v[n] = *reinterpret_cast<const piece_at2 *>(tile + offset(row(n), (unsigned)ld, hd));
-    }
-    __device__ __forceinline__ void store_whole(char *tile, int hd) {
-        store(tile, hd, true, [](int) { return true; });
-    }
-    // holds(row of the tile): whether it is there;  all: every row is
-    template <class F>
-    __device__ __forceinline__ void store(char *tile, int hd, bool all, F &&holds) {
-        if (!all || hd != HD) {
-#pragma unroll
-            for (int n = 0; n < PASSES; ++n) v[n] = finished(v[n], column(), hd, all || holds(row(n)));
-        }
-#pragma unroll
-        for (int n = 0; n < PASSES; ++n) *reinterpret_cast<u32x4 *>(tile + T::at(row(n), column() / 8)) = v[n];
-    }
-};
-
-// The same without registers: 16 bytes a lane from memory to shared memory at `to` + 16 * lane, past the registers; lanes without a piece are sent NOWHERE, where the
-// hardware reads zeros.  Rows have to lie on 16 bytes.  In assembly because the compiler, which cannot tell the tiles apart, would wait for it before every read
+// A tile of rows on its way from memory to shared memory: 16 bytes a lane to `to` + 16 * lane, past the registers; lanes without a piece are sent NOWHERE, where the
+// hardware reads zeros.  Rows have to lie on 16 bytes.  (Through registers 8192 tokens of 32 heads of 128 took 520 us forward, so 457.)  In assembly because the compiler, which cannot tell the tiles apart, would wait for it before every read
 // of shared memory; arrived() waits.  It writes no register; m0, which holds the place in shared memory, is an operand.  Five wait states have to stand between a
 // vector instruction that writes a scalar register (v_readlane, where the compiler has kept the descriptor in a lane) and its use by a load, one between a write of m0
 // and its use; inside the assembly the compiler does not see to it.
@@ -329,13 +289,17 @@ __device__ __forceinline__ float table_value(const Attn &a, int bucket, int head
     const int64_t at = (int64_t)bucket * a.heads + head;
     return a.table_dtype == PARO_F32 ? static_cast<const float *>(a.table)[at] : bits16_to_f32(a.table_dtype, static_cast<const unsigned short *>(a.table)[at]);
 }
-// A head's column of the table and the first distances in shared memory, and the values by distance that a tile needs.
+// A head's bias in shared memory.  Where the last bucket begins within NEAR (far_from), its values are there for every distance from -EDGE to far_from + EDGE, so that a
+// tile reads them wherever it lies; otherwise each tile has a window of EDGE distances of its own looked up.  (Windows always, each a search of five steps: 8 x 1024
+// tokens of 12 heads of 64 forward 46 us.)
+constexpr int NEAR = 1024, EDGE = 160;
 struct Bias {
     int first[MAX_BUCKETS];
     float column[MAX_BUCKETS];
+    float by[EDGE + NEAR + EDGE];
 
     __device__ __forceinline__ void load(const Attn &a, int head) {         // then a barrier
-        for (int b = threadIdx.x; b < a.buckets; b += blockDim.x) {
+        for (int b = threadIdx.x; b < a.buckets; b += 256) {
             first[b] = a.first[b];
             column[b] = table_value(a, b, head);
         }
@@ -353,6 +317,54 @@ struct Bias {
     }
     __device__ __forceinline__ float of(int far, int buckets) const { return column[bucket(far < 0 ? 0 : far, buckets)]; }
 };
+struct Distances {                      // what a thread holds of it
+    int far_from;                       // distances from here on have the last bucket's bias
+    float far;
+    bool whole, usual;                  // whole: of every distance;  usual: LOG2E times the far bias says enough of it
+
+    // after load() and a barrier; then another
+    __device__ __forceinline__ void begin(Bias &bias, int buckets) {
+        far_from = __builtin_amdgcn_readfirstlane(bias.first[buckets - 1]);
+        if (far_from < 0) far_from = 0;
+        far = __uint_as_float(__builtin_amdgcn_readfirstlane(__float_as_uint(bias.column[buckets - 1])));
+        usual = fabsf(far) < USUAL;
+        whole = far_from <= NEAR;
+        if (whole)
+            for (int x = threadIdx.x; x < far_from + 2 * EDGE; x += 256) bias.by[x] = bias.of(x - EDGE, buckets);
+    }
+    __device__ __forceinline__ bool beyond(int lowest) const { return lowest >= far_from; }      // all of a tile, whose lowest distance this is
+    // the window of a tile, for its part of the ring; then a barrier
+    __device__ __forceinline__ void look_up(Bias &bias, int lowest, int part, int buckets) const {
+        if (!whole && !(usual && beyond(lowest)) && threadIdx.x < EDGE) bias.by[part * EDGE + threadIdx.x] = bias.of(lowest + (int)threadIdx.x, buckets);
+    }
+    // values by distance from `lowest` on
+    __device__ __forceinline__ const float *values(const Bias &bias, int lowest, int part) const {
+        return whole ? bias.by + EDGE + (lowest < far_from ? lowest : far_from) : bias.by + part * EDGE;
+    }
+};
+
+// ---------------------------------------------------------------- rows off 16 bytes
+// Copies of the sequences' rows, heads side by side, each in whole pieces (zeros behind its end): sequence b from row b len on.
+constexpr int ALIGN_ROWS = 32;
+struct Copies {
+    Rows from[4];
+    char *to[4];
+    int heads[4];
+    bool keys[4];                       // rows of keys, or of queries
+};
+__global__ __launch_bounds__(256) void k_align(Attn a, Copies c) {
+    const int which = blockIdx.y, tiles = gridDim.x / a.batch, b = blockIdx.x / tiles, row0 = blockIdx.x % tiles * ALIGN_ROWS;
+    const Sequence seq(a, b);
+    const bool keys = c.keys[which];
+    const int n = keys ? seq.nk : seq.nq, rows = n - row0 < ALIGN_ROWS ? n - row0 : ALIGN_ROWS, pieces = (a.hd + 7) / 8, of_row = c.heads[which] * pieces;
+    const int64_t to0 = (int64_t)b * (keys ? a.len_k : a.len_q) + row0, from0 = (int64_t)(keys ? seq.k0 : seq.q0) + row0;
+    const Rows from = c.from[which];
+    u32x4 *const to = reinterpret_cast<u32x4 *>(c.to[which]) + to0 * of_row;
+    for (int x = threadIdx.x; x < rows * of_row; x += 256) {
+        const int r = x / of_row, in = x % of_row;
+        to[x] = piece_of_head(from.of(from0 + r, in / pieces), in % pieces * 8, a.hd, true);
+    }
+}
 
 // ---------------------------------------------------------------- host
 inline int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
@@ -411,7 +423,36 @@ inline int check_room(const std::string &f, int64_t needed, const void *workspac
     return bytes < needed ? fail(PARO_ERANGE, f + "the workspace is smaller than paro_attn_workspace says") : PARO_OK;
 }
 // Rows that lie on 16 bytes and heads of whole pieces: what goes past the registers.
-inline bool fills_take(const Rows &r, int hd) { return hd % 8 == 0 && r.ld % 8 == 0 && r.head % 8 == 0 && reinterpret_cast<uintptr_t>(r.at) % 16 == 0; }
+inline bool fills_take(int64_t ld, int64_t head, int64_t hd) { return hd % 8 == 0 && ld % 8 == 0 && head % 8 == 0; }
+inline int64_t copy_bytes(const paro_attn_t &d, int64_t len, int64_t heads) { return ceil_div(d.batch * len * heads * ceil_div(d.head_dim, 8) * 16, 256) * 256; }
+inline int check_aligned(const std::string &f, const Rows &r, int hd, const char *name) {
+    return fills_take(r.ld, r.head, hd) && (reinterpret_cast<uintptr_t>(r.at) & 15) ? fail(PARO_EALIGN, f + name + " is not 16-byte aligned, as its rows are") : PARO_OK;
+}
+// Rows that the fills do not take are copied into the workspace.
+struct Copying {
+    Copies c{};
+    int arrays = 0;
+    int64_t most = 0;
+    char *ws;
+    int64_t at;
+    Copying(char *workspace, int64_t offset) : ws(workspace), at(offset) {}
+    bool take(const paro_attn_t &d, Rows &rows, int64_t len, int64_t heads, bool keys) {
+        if (fills_take(rows.ld, rows.head, d.head_dim)) return false;
+        const int64_t width = ceil_div(d.head_dim, 8) * 8;
+        c.from[arrays] = rows;
+        c.heads[arrays] = (int)heads;
+        c.keys[arrays] = keys;
+        rows = Rows{ws + at, heads * width, width};
+        c.to[arrays++] = rows.at;
+        at += copy_bytes(d, len, heads);
+        most = std::max(most, len);
+        return true;
+    }
+    void launch(const Attn &a, hipStream_t st) const {
+        if (arrays && most && a.batch)
+            hipLaunchKernelGGL(k_align, dim3((unsigned)(ceil_div(most, ALIGN_ROWS) * a.batch), (unsigned)arrays), dim3(256), 0, st, a, c);
+    }
+};
 inline Attn attn_of(const paro_attn_t &d, const void *q, const void *k, const void *v, const int32_t *q_starts, const int32_t *k_starts, const int32_t *k_lens,
                     const void *table, const int32_t *first) {
     const auto rows = [&](const void *at, int64_t heads, int64_t ld, int64_t head) {
@@ -422,6 +463,8 @@ inline Attn attn_of(const paro_attn_t &d, const void *q, const void *k, const vo
     a.k = rows(k, d.kv_heads, d.ld_k, d.head_k);
     a.v = rows(v, d.kv_heads, d.ld_v, d.head_v);
     a.out = rows(nullptr, d.heads, d.ld_out, d.head_out);
+    a.keys = a.k;
+    a.values = a.v;
     a.q_starts = q_starts;
     a.k_starts = k_starts;
     a.k_lens = k_lens;

@@ -22,6 +22,8 @@ constexpr float SHIFT = DT == PARO_F16 ? 15.0f : 0.0f;
 struct Grad {
     Attn a;
     Rows dout, dq, dk, dv;
+    Rows queries, douts;                     // q and dout as the fills take them: themselves, or copies, of sequence b from row b len_q on
+    bool copied_q, copied_o;
     // [head][rows_q]: P = exp2(s * LOG2E - base); D.  Of a bias, whose largest score may be a table's lowest number: P = exp2((s - peak) * LOG2E - log_sum)
     float *base, *dots, *peak, *log_sum;
     float *largest;                          // of fp16: the largest |dout_i|^2 and |v_j|^2 of each block of k_dots
@@ -168,8 +170,7 @@ __device__ __forceinline__ Share share_of(const Grad &g, int block, int of_kv) {
     return s;
 }
 
-// FILL: queries and dout lie on 16 bytes and go to shared memory past the registers.
-template <int DT, int HD, bool BIAS, bool FILL>
+template <int DT, int HD, bool BIAS>
 __global__ __launch_bounds__(256, 2) void k_grad_kv(Grad g) {
     using T = Tile<HD>;
     const Attn &a = g.a;
@@ -179,7 +180,6 @@ __global__ __launch_bounds__(256, 2) void k_grad_kv(Grad g) {
     __shared__ __attribute__((aligned(16))) float rows[2][4][Q_STEP];          // [buffer][base, dots, peak, log_sum]
     __shared__ int lowest[2];                                                  // whether the base of any row says too little
     __shared__ Bias bias;
-    __shared__ float by_distance[2][BLOCK + Q_STEP];
     const int per_kv = g.sink_tiles * g.sink_shares + (g.key_tiles - g.sink_tiles) * g.shares;
     const Work work(blockIdx.x, a.batch * a.kv_heads, per_kv);
     const int of_kv = work.unit, kv = of_kv % a.kv_heads, b = of_kv / a.kv_heads;
@@ -198,8 +198,8 @@ __global__ __launch_bounds__(256, 2) void k_grad_kv(Grad g) {
     const int from = (int)(all * share.share / share.shares), to = (int)(all * (share.share + 1) / share.shares);
 
     // The next step's head, and its first query.
-    Staged<HD, Q_STEP> from_q, from_o;
-    const Filled<HD, Q_STEP> fill_q(a.q.ld, a.hd), fill_o(g.dout.ld, a.hd);
+    const int64_t row_q = g.copied_q ? (int64_t)b * a.len_q : seq.q0, row_o = g.copied_o ? (int64_t)b * a.len_q : seq.q0;
+    const Filled<HD, Q_STEP> fill_q(g.queries.ld, a.hd), fill_o(g.douts.ld, a.hd);
     float from_row = 0.0f;
     int next_head = 0, next_tile = 0;
     const auto load = [&](int buffer) __attribute__((always_inline)) {
@@ -209,48 +209,36 @@ __global__ __launch_bounds__(256, 2) void k_grad_kv(Grad g) {
             const float x = of[(int64_t)head * a.rows_q + seq.q0 + (i < seq.nq ? i : seq.nq - 1)];
             from_row = i < seq.nq ? x : which % 2 == 0 ? INFINITY : 0.0f;
         }
-        if constexpr (FILL) {
-            const u32x4 q_from = fill_q.descriptor(a.q.of((int64_t)seq.q0 + i0, head)), o_from = fill_o.descriptor(g.dout.of((int64_t)seq.q0 + i0, head));
-            if (i0 + Q_STEP <= seq.nq) {
-                fill_q.whole(q_from, tiles[buffer][0]);
-                fill_o.whole(o_from, tiles[buffer][1]);
-            } else {
-                const auto holds = [&](int r) { return i0 + r < seq.nq; };
-                fill_q.held(q_from, tiles[buffer][0], holds);
-                fill_o.held(o_from, tiles[buffer][1], holds);
-            }
+        const u32x4 q_from = fill_q.descriptor(g.queries.of(row_q + i0, head)), o_from = fill_o.descriptor(g.douts.of(row_o + i0, head));
+        if (i0 + Q_STEP <= seq.nq) {
+            fill_q.whole(q_from, tiles[buffer][0]);
+            fill_o.whole(o_from, tiles[buffer][1]);
         } else {
-            from_q.load(a.q.of(seq.q0, head), a.q.ld, i0, seq.nq, a.hd);
-            from_o.load(g.dout.of(seq.q0, head), g.dout.ld, i0, seq.nq, a.hd);
+            const auto holds = [&](int r) { return i0 + r < seq.nq; };
+            fill_q.held(q_from, tiles[buffer][0], holds);
+            fill_o.held(o_from, tiles[buffer][1], holds);
         }
     };
-    int far_from = 0, of_head = -1;
-    float far_bias = 0.0f, next_far_bias = 0.0f;
-    const auto is_far = [&](int i0, float last) { return BIAS && fabsf(last) < USUAL && off + i0 - (k0 + BLOCK - 1) >= far_from; };
+    Distances by_distance{}, next_distance{};
+    int of_head = -1;
+    const auto lowest_of = [&](int i0) { return off + i0 - (k0 + BLOCK - 1); };
     const auto stage = [&](int buffer) __attribute__((always_inline)) {
-        const int head = kv * group + next_head, i0 = (tile0 + next_tile) * Q_STEP;
-        if constexpr (!FILL) {
-            const auto holds = [&](int r) { return i0 + r < seq.nq; };
-            from_q.store(tiles[buffer][0], a.hd, i0 + Q_STEP <= seq.nq, holds);
-            from_o.store(tiles[buffer][1], a.hd, i0 + Q_STEP <= seq.nq, holds);
-        }
         if (threadIdx.x < (BIAS ? 4 : 2) * Q_STEP) rows[buffer][threadIdx.x / Q_STEP][threadIdx.x % Q_STEP] = from_row;
         if constexpr (BIAS) {
             if (w == 1) {                                       // whose first half has the peaks
                 const bool any = __any(lane < 32 && fabsf(from_row) > USUAL && fabsf(from_row) < INFINITY);
                 if (lane == 0) lowest[buffer] = any;
             }
-        }
-        if constexpr (BIAS) {
+            const int head = kv * group + next_head, i0 = (tile0 + next_tile) * Q_STEP;
             if (head != of_head) {
-                __syncthreads();
+                __syncthreads();                                // the last head's tiles are done with its bias
                 bias.load(a, head);
                 __syncthreads();
                 of_head = head;
-                far_from = bias.first[a.buckets - 1];
-                next_far_bias = bias.column[a.buckets - 1];
+                next_distance.begin(bias, a.buckets);           // read behind the next step's barrier
+                __syncthreads();
             }
-            if (!is_far(i0, next_far_bias) && threadIdx.x < BLOCK + Q_STEP - 1) by_distance[buffer][threadIdx.x] = bias.of(off + i0 - (k0 + BLOCK - 1) + (int)threadIdx.x, a.buckets);
+            next_distance.look_up(bias, lowest_of(i0), buffer, a.buckets);
         }
     };
 
@@ -275,18 +263,13 @@ __global__ __launch_bounds__(256, 2) void k_grad_kv(Grad g) {
     }
     for (int u = from; u < to; ++u) {
         const int i0 = (tile0 + next_tile) * Q_STEP, buffer = (u - from) & 1, first = off + i0;
-        far_bias = next_far_bias;
+        by_distance = next_distance;
         if (++next_tile == per_head) {
             next_tile = 0;
             ++next_head;
         }
-        if constexpr (FILL) {
-            arrived<0>();                    // this step's tiles; and all waves have left the last step's
-            if (u + 1 < to) load(buffer ^ 1);
-        } else {
-            if (u + 1 < to) load(buffer ^ 1);
-            __syncthreads();
-        }
+        arrived<0>();                        // this step's tiles; and all waves have left the last step's
+        if (u + 1 < to) load(buffer ^ 1);
         const char *const queries = tiles[buffer][0], *const douts = tiles[buffer][1];
         const bool none = first + Q_STEP - 1 < of_wave || (first - (of_wave + 31) >= a.window && of_wave >= a.sinks);
         if (!none) {
@@ -296,10 +279,10 @@ __global__ __launch_bounds__(256, 2) void k_grad_kv(Grad g) {
 #pragma unroll
             for (int c = 0; c < STEPS; ++c) dp = mfma32<DT>(T::rows(douts, 0, c, lane), T::rows(values, w * 32, c, lane), dp);
             const bool every = first >= of_wave + 31 && (first + Q_STEP - 1 - of_wave < a.window || of_wave + 31 < a.sinks);
-            const bool far = is_far(i0, far_bias);
+            const bool far = BIAS && by_distance.usual && by_distance.beyond(lowest_of(i0));
             if constexpr (BIAS) {
                 if (!far) {
-                    const float *const at = by_distance[buffer] + BLOCK - 1 - (w * 32 + (lane & 31)) + 4 * h;
+                    const float *const at = by_distance.values(bias, lowest_of(i0), buffer) + BLOCK - 1 - (w * 32 + (lane & 31)) + 4 * h;
 #pragma unroll
                     for (int e = 0; e < 16; ++e) s[e] = __builtin_fmaf(s[e], a.scale, at[8 * (e / 4) + e % 4]);
                 }
@@ -309,12 +292,12 @@ __global__ __launch_bounds__(256, 2) void k_grad_kv(Grad g) {
                 for (int e = 0; e < 16; ++e)
                     if (!sees(first + 8 * (e / 4) + 4 * h + e % 4, j, a.window, a.sinks)) s[e] = -INFINITY;
             }
-            const float by = BIAS && !far ? LOG2E : unit, plus = BIAS && far ? far_bias * LOG2E : 0.0f;
+            const float by = BIAS && !far ? LOG2E : unit, plus = BIAS && far ? by_distance.far * LOG2E : 0.0f;
             if (BIAS && lowest[buffer]) {                // a row's largest score may be a table's lowest number: P from the difference
 #pragma unroll
                 for (int e = 0; e < 16; ++e) {
                     const int r = 8 * (e / 4) + 4 * h + e % 4;
-                    const float score = far ? __builtin_fmaf(s[e], a.scale, far_bias) : s[e], peak = rows[buffer][2][r];
+                    const float score = far ? __builtin_fmaf(s[e], a.scale, by_distance.far) : s[e], peak = rows[buffer][2][r];
                     s[e] = peak < INFINITY ? exp2_(__builtin_fmaf(score - peak, LOG2E, -rows[buffer][3][r])) : 0.0f;
                 }
             } else {
@@ -389,8 +372,7 @@ __global__ __launch_bounds__(256) void k_grad_join(Grad g) {
 }
 
 // ---------------------------------------------------------------- dq, and the table's gradient
-// FILL: keys and values lie on 16 bytes and go to shared memory past the registers.
-template <int DT, int HD, bool BIAS, bool FILL>
+template <int DT, int HD, bool BIAS>
 __global__ __launch_bounds__(256, 2) void k_grad_q(Grad g) {
     using T = Tile<HD>;
     const Attn &a = g.a;
@@ -398,10 +380,11 @@ __global__ __launch_bounds__(256, 2) void k_grad_q(Grad g) {
     constexpr int BYTES = KEYS * T::ROW, STEPS = HD / 16, DISTANCES = 32 + KEYS, SQUARE = 36;
     __shared__ __attribute__((aligned(1024))) char tiles[RING][2][BYTES];       // [part of the ring][keys, values]
     __shared__ Bias bias;
-    __shared__ float by_distance[RING][BLOCK + KEYS];
     __shared__ __attribute__((aligned(16))) float squares[BIAS ? 4 : 1][BIAS ? 32 * SQUARE : 4];     // [wave]: 32 x 32 of dS
     __shared__ float diagonals[BIAS ? 4 : 1][DISTANCES];                        // [wave]: sums of dS along a distance, of one tile
-    __shared__ float of_buckets[BIAS ? 4 : 1][BIAS ? MAX_BUCKETS : 1], far_sums[4];
+    // Of the block: by distance; where the bias is not there for every distance, [wave][bucket]
+    __shared__ float sums[BIAS ? NEAR + EDGE : 1], far_sums[4];
+    static_assert(NEAR + EDGE >= 4 * MAX_BUCKETS, "the waves' buckets take the place of the distances");
     const int group = a.heads / a.kv_heads;
     const Work work(blockIdx.x, a.batch * a.kv_heads, a.tiles * group);
     const int kv = work.unit % a.kv_heads, b = work.unit / a.kv_heads, head = kv * group + work.within % group;
@@ -418,39 +401,23 @@ __global__ __launch_bounds__(256, 2) void k_grad_q(Grad g) {
     const int off = seq.nk - seq.nq, first = i0 + off, last = (i0 + BLOCK < seq.nq ? i0 + BLOCK : seq.nq) - 1 + off;
     const Seen<KEYS> seen(a, first, last);
     const int of_wave = first + w * 32, place = of_wave + (lane & 31), i = i0 + w * 32 + (lane & 31);
-    const char *const keys_at = a.k.of(seq.k0, kv), *const values_at = a.v.of(seq.k0, kv);
-    Staged<HD, KEYS> from_k, from_v;
-    const Filled<HD, KEYS> fill_k(a.k.ld, a.hd), fill_v(a.v.ld, a.hd);
+    const int64_t row_k = a.copied_k ? (int64_t)b * a.len_k : seq.k0, row_v = a.copied_v ? (int64_t)b * a.len_k : seq.k0;
+    const char *const keys_at = a.keys.of(row_k, kv), *const values_at = a.values.of(row_v, kv);
+    const int64_t k_step = a.keys.ld * (2 * KEYS), v_step = a.values.ld * (2 * KEYS);
+    const Filled<HD, KEYS> fill_k(a.keys.ld, a.hd), fill_v(a.values.ld, a.hd);
     constexpr int FILLS = 2 * Filled<HD, KEYS>::FILLS;
-    int far_from = 0;
-    float far_bias = 0.0f, far_sum = 0.0f;
-    bool usual = true;
-    const auto is_far = [&](int k0) { return BIAS && usual && first - (k0 + KEYS - 1) >= far_from; };
-    const auto stage_bias = [&](int k0, int part) __attribute__((always_inline)) {
-        if (!is_far(k0) && threadIdx.x < BLOCK + KEYS - 1) by_distance[part][threadIdx.x] = bias.of(first - k0 + BLOCK - 1 - (int)threadIdx.x, a.buckets);
-    };
-    const auto load = [&](int t) __attribute__((always_inline)) {
-        const int k0 = seen.tile(t) * KEYS;
-        from_k.load(keys_at, a.k.ld, k0, seq.nk, a.hd);
-        from_v.load(values_at, a.v.ld, k0, seq.nk, a.hd);
-    };
-    const auto stage = [&](int t, int part) __attribute__((always_inline)) {
-        const int first_key = seen.tile(t) * KEYS;
-        if constexpr (BIAS) stage_bias(first_key, part);
-        const auto holds = [&](int r) { return seen.holds(first_key + r); };
-        const bool all = seen.holds_all(first_key);
-        from_k.store(tiles[part][0], a.hd, all, holds);
-        from_v.store(tiles[part][1], a.hd, all, holds);
-    };
+    Distances by_distance{};
+    float far_sum = 0.0f;
+    const auto lowest_of = [&](int k0) { return first - (k0 + KEYS - 1); };
     const auto fill = [&](int t, int part) __attribute__((always_inline)) {
-        const int first_key = seen.tile(t) * KEYS;
-        if constexpr (BIAS) stage_bias(first_key, part);
-        const u32x4 k_from = fill_k.descriptor(keys_at + (int64_t)first_key * (a.k.ld * 2)), v_from = fill_v.descriptor(values_at + (int64_t)first_key * (a.v.ld * 2));
-        if (seen.holds_all(first_key)) {
+        const int tile = seen.tile(t), k0 = tile * KEYS;
+        if constexpr (BIAS) by_distance.look_up(bias, lowest_of(k0), part, a.buckets);
+        const u32x4 k_from = fill_k.descriptor(keys_at + tile * k_step), v_from = fill_v.descriptor(values_at + tile * v_step);
+        if (seen.holds_all(k0)) {
             fill_k.whole(k_from, tiles[part][0]);
             fill_v.whole(v_from, tiles[part][1]);
         } else {
-            const auto holds = [&](int r) { return seen.holds(first_key + r); };
+            const auto holds = [&](int r) { return seen.holds(k0 + r); };
             fill_k.held(k_from, tiles[part][0], holds);
             fill_v.held(v_from, tiles[part][1], holds);
         }
@@ -461,16 +428,12 @@ __global__ __launch_bounds__(256, 2) void k_grad_q(Grad g) {
         fill_k.held(fill_k.descriptor(keys_at), tiles[part][0], holds);
         fill_v.held(fill_v.descriptor(values_at), tiles[part][1], holds);
     };
-    if constexpr (!FILL) {
-        if (seen.tiles) load(0);
-    }
     if constexpr (BIAS) {
         bias.load(a, head);
-        for (int x = threadIdx.x; x < 4 * MAX_BUCKETS; x += 256) of_buckets[x / MAX_BUCKETS][x % MAX_BUCKETS] = 0.0f;
+        for (int x = threadIdx.x; x < NEAR + EDGE; x += 256) sums[x] = 0.0f;
         __syncthreads();
-        far_from = bias.first[a.buckets - 1];
-        far_bias = bias.column[a.buckets - 1];
-        usual = fabsf(far_bias) < USUAL;
+        by_distance.begin(bias, a.buckets);
+        __syncthreads();
     }
     short8_t q[STEPS], dout[STEPS];
     float base = INFINITY, peak = INFINITY, log_sum = 0.0f, dot = 0.0f;
@@ -495,29 +458,25 @@ __global__ __launch_bounds__(256, 2) void k_grad_q(Grad g) {
     const float unit = a.scale * LOG2E, times = DT == PARO_F16 ? g.times[0] * 0x1p-15f : 1.0f;
     f32x16 dq[HD / 32] = {};
     const bool lowest = BIAS && __any(fabsf(peak) > USUAL && fabsf(peak) < INFINITY);       // a row's largest score may be a table's lowest number
-    const float far_plus = peak < -LOWEST ? -INFINITY : far_bias * LOG2E - base;            // (which sees no key with another bias)
-    // In step t tile t + RING - 1 (through registers: t + 1) goes to the part of the ring whose tile all waves have left.  As many steps a round as the ring has parts, so
+    const float far_plus = peak < -LOWEST ? -INFINITY : by_distance.far * LOG2E - base;            // (which sees no key with another bias)
+    // In step t tile t + RING - 1 goes to the part of the ring whose tile all waves have left.  As many steps a round as the ring has parts, so
     // that these are constants.  PLAIN: every query sees the tile whole, and the tile that is brought is there whole.
     const auto step = [&](auto part_, auto plain_, int t, int k0, const char *k_at, const char *v_at) __attribute__((always_inline)) {
         constexpr int part = part_, PLAIN = plain_, coming = (part + RING - 1) % RING;
-        if constexpr (FILL) {
-            arrived<(RING - 2) * FILLS>();
-            if constexpr (PLAIN) {
-                fill_k.whole(fill_k.descriptor(k_at), tiles[coming][0]);
-                fill_v.whole(fill_v.descriptor(v_at), tiles[coming][1]);
-                if constexpr (BIAS) stage_bias(k0 + (RING - 1) * KEYS, coming);
-            } else {
-                if (t + RING - 1 < seen.tiles) fill(t + RING - 1, coming);
-                else fill_none(coming);
-            }
+        arrived<(RING - 2) * FILLS>();
+        if constexpr (PLAIN) {
+            fill_k.whole(fill_k.descriptor(k_at), tiles[coming][0]);
+            fill_v.whole(fill_v.descriptor(v_at), tiles[coming][1]);
+            if constexpr (BIAS) by_distance.look_up(bias, lowest_of(k0 + (RING - 1) * KEYS), coming, a.buckets);
         } else {
-            __syncthreads();
+            if (t + RING - 1 < seen.tiles) fill(t + RING - 1, coming);
+            else fill_none(coming);
         }
         const char *const keys = tiles[part][0], *const values = tiles[part][1];
-        const bool none = !PLAIN && (k0 > of_wave + 31 || (k0 + KEYS <= of_wave - a.window + 1 && k0 >= a.sinks)), far = is_far(k0);
-        if (want && !far) {
+        const bool none = !PLAIN && (k0 > of_wave + 31 || (k0 + KEYS <= of_wave - a.window + 1 && k0 >= a.sinks));
+        const bool beyond = BIAS && by_distance.beyond(lowest_of(k0)), far = beyond && by_distance.usual;
+        if (want && !beyond)
             for (int x = lane; x < DISTANCES; x += 64) diagonals[BIAS ? w : 0][x] = 0.0f;
-        }
         if (!none) {
             f32x16 s = {}, dp = {};
 #pragma unroll
@@ -526,9 +485,9 @@ __global__ __launch_bounds__(256, 2) void k_grad_q(Grad g) {
             for (int c = 0; c < STEPS; ++c) dp = mfma32<DT>(T::rows(values, 0, c, lane), dout[c], dp);
             if constexpr (BIAS) {
                 if (!far) {
-                    const float *const at = by_distance[part] + BLOCK - 1 - (w * 32 + (lane & 31)) + 4 * h;
+                    const float *const at = by_distance.values(bias, lowest_of(k0), part) + (place - first) + 4 - 4 * h;
 #pragma unroll
-                    for (int e = 0; e < 16; ++e) s[e] = __builtin_fmaf(s[e], a.scale, at[8 * (e / 4) + e % 4]);
+                    for (int e = 0; e < 16; ++e) s[e] = __builtin_fmaf(s[e], a.scale, at[27 - (8 * (e / 4) + e % 4)]);
                 }
             }
             const bool every = PLAIN || (k0 + KEYS - 1 <= of_wave && (k0 > of_wave + 31 - a.window || k0 + KEYS <= a.sinks));
@@ -548,7 +507,7 @@ __global__ __launch_bounds__(256, 2) void k_grad_q(Grad g) {
 #pragma unroll
             for (int e = 0; e < 16; ++e) dp[e] = s[e] * (DT == PARO_F16 ? (dp[e] - dot) * times : dp[e] - dot);
             if constexpr (BIAS) {
-                if (want && far) {
+                if (want && beyond) {
 #pragma unroll
                     for (int e = 0; e < 16; ++e) far_sum += dp[e];
                 } else if (want) {
@@ -586,47 +545,42 @@ __global__ __launch_bounds__(256, 2) void k_grad_q(Grad g) {
             }
         }
         if constexpr (BIAS) {
-            if (want && !far) {
+            if (want && !beyond) {
                 __syncthreads();
-                // thread x has the distance first - (k0 + KEYS - 1) + x of the tile; buckets are runs of distances, whose sums the last lane of a run adds
-                const int x = threadIdx.x, d = first - (k0 + KEYS - 1) + x;
+                // thread x has the distance lowest + x of the tile
+                const int x = threadIdx.x, d = lowest_of(k0) + x;
                 float sum = 0.0f;
 #pragma unroll
                 for (int v = 0; v < 4; ++v)
                     if (x >= v * 32 && x < v * 32 + DISTANCES) sum += diagonals[v][x - v * 32];
-                const int bucket = d < 0 || x >= BLOCK + KEYS ? -1 : bias.bucket(d, a.buckets);
+                if (by_distance.whole) {
+                    if (d >= 0 && x < EDGE) sums[d] += sum;
+                } else {
+                    // buckets are runs of distances, whose sums the last lane of a run adds
+                    const int bucket = d < 0 || x >= EDGE ? -1 : bias.bucket(d, a.buckets);
 #pragma unroll
-                for (int n = 1; n < 64; n *= 2) {
-                    const float before = __shfl_up(sum, n);
-                    const int of = __shfl_up(bucket, n);
-                    if (lane >= n && of == bucket) sum += before;
+                    for (int n = 1; n < 64; n *= 2) {
+                        const float before = __shfl_up(sum, n);
+                        const int of = __shfl_up(bucket, n);
+                        if (lane >= n && of == bucket) sum += before;
+                    }
+                    const int next = __shfl_down(bucket, 1);
+                    if (bucket >= 0 && (lane == 63 || next != bucket)) sums[w * MAX_BUCKETS + bucket] += sum;
                 }
-                const int next = __shfl_down(bucket, 1);
-                if (bucket >= 0 && (lane == 63 || next != bucket)) of_buckets[w][bucket] += sum;
             }
-        }
-        if constexpr (!FILL) {
-            if (t + 1 < seen.tiles) stage(t + 1, (part + 1) % RING);
-            if (t + 2 < seen.tiles) load(t + 2);
         }
     };
     if (seen.tiles) {
         int plain_from, plain_to;
         seen.plain(a, first, last, plain_from, plain_to);
-        if constexpr (FILL) {
-            for (int t = 0; t < RING - 1; ++t) {
-                if (t < seen.tiles) fill(t, t);
-                else fill_none(t);
-            }
-        } else {
-            stage(0, 0);
-            if (seen.tiles > 1) load(1);
+        for (int t = 0; t < RING - 1; ++t) {
+            if (t < seen.tiles) fill(t, t);
+            else fill_none(t);
         }
         for (int t = 0; t < seen.tiles;) {
-            if (FILL && t >= plain_from && t + 2 * RING - 2 < plain_to) {
+            if (t >= plain_from && t + 2 * RING - 2 < plain_to) {
                 int k0 = seen.tile(t) * KEYS;
-                const int64_t k_step = a.k.ld * (2 * KEYS), v_step = a.v.ld * (2 * KEYS);
-                const char *k_at = keys_at + (int64_t)(seen.tile(t) + RING - 1) * k_step, *v_at = values_at + (int64_t)(seen.tile(t) + RING - 1) * v_step;
+                const char *k_at = keys_at + (seen.tile(t) + RING - 1) * k_step, *v_at = values_at + (seen.tile(t) + RING - 1) * v_step;
                 for (; t + 2 * RING - 2 < plain_to; t += RING)
                     static_for<0, RING>([&](auto part) __attribute__((always_inline)) {
                         step(part, std::integral_constant<int, 1>{}, 0, k0, k_at, v_at);
@@ -640,7 +594,7 @@ __global__ __launch_bounds__(256, 2) void k_grad_q(Grad g) {
                 ++t;
             });
         }
-        if constexpr (FILL) arrived<0>();                       // nothing is on its way into the shared memory of the block that comes next
+        arrived<0>();                                           // nothing is on its way into the shared memory of the block that comes next
     }
     const float of_dq = DT == PARO_F16 ? a.scale * g.times[1] : a.scale;
     char *const to = g.dq.of((int64_t)seq.q0 + i, head);
@@ -652,11 +606,24 @@ __global__ __launch_bounds__(256, 2) void k_grad_q(Grad g) {
             for (int x = 1; x < 64; x *= 2) far_sum += __shfl_xor(far_sum, x);
             if (lane == 0) far_sums[w] = far_sum;
             __syncthreads();
-            for (int x = threadIdx.x; x < a.buckets; x += 256) {
-                float sum = 0.0f;
+            const float back = DT == PARO_F16 ? g.times[1] : 1.0f;
+            if (by_distance.whole) {                            // a wave a bucket; the last has what lies beyond too
+                for (int x = w; x < a.buckets; x += 4) {
+                    const int all = by_distance.far_from + EDGE, from = bias.first[x], until = x + 1 < a.buckets ? bias.first[x + 1] : all;
+                    float sum = 0.0f;
+                    for (int d = (from > 0 ? from : 0) + lane; d < until && d < all; d += 64) sum += sums[d];
 #pragma unroll
-                for (int v = 0; v < 4; ++v) sum += of_buckets[v][x] + (x == a.buckets - 1 ? far_sums[v] : 0.0f);
-                of_table[x] = DT == PARO_F16 ? sum * g.times[1] : sum;
+                    for (int n = 1; n < 64; n *= 2) sum += __shfl_xor(sum, n);
+                    if (x == a.buckets - 1) sum += far_sums[0] + far_sums[1] + far_sums[2] + far_sums[3];
+                    if (lane == 0) of_table[x] = sum * back;
+                }
+            } else {
+                for (int x = threadIdx.x; x < a.buckets; x += 256) {
+                    float sum = 0.0f;
+#pragma unroll
+                    for (int v = 0; v < 4; ++v) sum += sums[v * MAX_BUCKETS + x] + (x == a.buckets - 1 ? far_sums[v] : 0.0f);
+                    of_table[x] = sum * back;
+                }
             }
         }
     }
@@ -687,7 +654,7 @@ __global__ __launch_bounds__(256) void k_table_grad(Grad g) {
 // ---------------------------------------------------------------- host
 struct Plan {
     int blocks_q, blocks_v, blocks_heads, tiles, key_tiles, sink_tiles, shares, sink_shares, slots;
-    int64_t kv_blocks, dots, peak, log_sum, largest, times, partial, of_table, bytes;
+    int64_t kv_blocks, copies, dots, peak, log_sum, largest, times, partial, of_table, bytes;
 };
 
 Plan plan_of(const paro_attn_t &d) {
@@ -728,6 +695,14 @@ Plan plan_of(const paro_attn_t &d) {
     p.times = room(2);
     p.partial = room((int64_t)p.slots * d.kv_heads * d.batch * 2 * BLOCK * hd);
     p.of_table = room((int64_t)d.heads * d.batch * p.tiles * d.buckets);
+    p.copies = at;
+    const auto copy = [&](int64_t ld, int64_t head, int64_t len, int64_t heads) {
+        if (!fills_take(ld ? ld : heads * d.head_dim, head ? head : d.head_dim, d.head_dim)) at += copy_bytes(d, len, heads);
+    };
+    copy(d.ld_q, d.head_q, d.len_q, d.heads);
+    copy(d.ld_out, d.head_out, d.len_q, d.heads);
+    copy(d.ld_k, d.head_k, d.len_k, d.kv_heads);
+    copy(d.ld_v, d.head_v, d.len_k, d.kv_heads);
     p.bytes = at;
     return p;
 }
@@ -737,17 +712,13 @@ void launch(const Grad &g, const Plan &p, hipStream_t st) {
     if (p.blocks_q + p.blocks_v) hipLaunchKernelGGL((k_dots<DT, HD>), dim3((unsigned)(p.blocks_q + p.blocks_v), (unsigned)p.blocks_heads), dim3(256), 0, st, g);
     if constexpr (DT == PARO_F16) hipLaunchKernelGGL(k_times, dim3(1), dim3(256), 0, st, g);
     if (p.kv_blocks) {
-        if (fills_take(g.a.q, g.a.hd) && fills_take(g.dout, g.a.hd)) hipLaunchKernelGGL((k_grad_kv<DT, HD, BIAS, true>), dim3((unsigned)p.kv_blocks), dim3(256), 0, st, g);
-        else hipLaunchKernelGGL((k_grad_kv<DT, HD, BIAS, false>), dim3((unsigned)p.kv_blocks), dim3(256), 0, st, g);
+        hipLaunchKernelGGL((k_grad_kv<DT, HD, BIAS>), dim3((unsigned)p.kv_blocks), dim3(256), 0, st, g);
         const int joined = p.shares > 1 ? p.key_tiles : p.sink_shares > 1 ? p.sink_tiles : 0;
         if (joined)
             hipLaunchKernelGGL((k_grad_join<DT, HD>), dim3((unsigned)(joined * g.a.kv_heads * g.a.batch), BLOCK / (1024 / HD), 2), dim3(256), 0, st, g);
     }
     const unsigned q_blocks = (unsigned)((int64_t)p.tiles * g.a.heads * g.a.batch);
-    if (q_blocks) {
-        if (fills_take(g.a.k, g.a.hd) && fills_take(g.a.v, g.a.hd)) hipLaunchKernelGGL((k_grad_q<DT, HD, BIAS, true>), dim3(q_blocks), dim3(256), 0, st, g);
-        else hipLaunchKernelGGL((k_grad_q<DT, HD, BIAS, false>), dim3(q_blocks), dim3(256), 0, st, g);
-    }
+    if (q_blocks) hipLaunchKernelGGL((k_grad_q<DT, HD, BIAS>), dim3(q_blocks), dim3(256), 0, st, g);
     if (BIAS && g.dtable) hipLaunchKernelGGL((k_table_grad<DT>), dim3((unsigned)g.a.heads), dim3(256), 0, st, g);
 }
 
@@ -814,6 +785,17 @@ int paro_attn_grad(const paro_attn_t *d, const void *dout, const void *q, const 
         g.sink_shares = p.sink_shares;
         g.slots = p.slots;
         hipStream_t st = static_cast<hipStream_t>(stream);
+        if ((rc = check_aligned(f, g.a.q, g.a.hd, "q")) || (rc = check_aligned(f, g.dout, g.a.hd, "dout")) || (rc = check_aligned(f, g.a.k, g.a.hd, "k")) ||
+            (rc = check_aligned(f, g.a.v, g.a.hd, "v")))
+            return rc;
+        g.queries = g.a.q;
+        g.douts = g.dout;
+        Copying copying(ws, p.copies);
+        g.copied_q = copying.take(*d, g.queries, d->len_q, d->heads, false);
+        g.copied_o = copying.take(*d, g.douts, d->len_q, d->heads, false);
+        g.a.copied_k = copying.take(*d, g.a.keys, d->len_k, d->kv_heads, true);
+        g.a.copied_v = copying.take(*d, g.a.values, d->len_k, d->kv_heads, true);
+        copying.launch(g.a, st);
 #define PARO_BACKWARD(DT, HD, BIAS) launch<DT, HD, BIAS>(g, p, st)
         PARO_BY_FORM(PARO_BACKWARD);
 #undef PARO_BACKWARD
