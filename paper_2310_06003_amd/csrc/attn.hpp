@@ -345,7 +345,7 @@ struct Distances {                      // what a thread holds of it
 
 // ---------------------------------------------------------------- rows off 16 bytes
 // Copies of the sequences' rows, heads side by side, each in whole pieces (zeros behind its end): sequence b from row b len on.
-constexpr int ALIGN_ROWS = 32;
+constexpr int ALIGN_ROWS = 8;
 struct Copies {
     Rows from[4];
     char *to[4];

@@ -171,7 +171,7 @@ __device__ __forceinline__ Share share_of(const Grad &g, int block, int of_kv) {
 }
 
 template <int DT, int HD, bool BIAS>
-__global__ __launch_bounds__(256, 2) void k_grad_kv(Grad g) {
+__global__ __launch_bounds__(256, HD == 64 ? 3 : 2) void k_grad_kv(Grad g) {
     using T = Tile<HD>;
     const Attn &a = g.a;
     constexpr int BYTES = Q_STEP * T::ROW, STEPS = HD / 16;
@@ -200,21 +200,33 @@ __global__ __launch_bounds__(256, 2) void k_grad_kv(Grad g) {
     // The next step's head, and its first query.
     const int64_t row_q = g.copied_q ? (int64_t)b * a.len_q : seq.q0, row_o = g.copied_o ? (int64_t)b * a.len_q : seq.q0;
     const Filled<HD, Q_STEP> fill_q(g.queries.ld, a.hd), fill_o(g.douts.ld, a.hd);
+    // What the next step takes: its head and tile of queries, where their rows are, and this thread's number of theirs.
+    const int which = threadIdx.x / Q_STEP;
+    const float *const of_rows = (which == 0 ? g.base : which == 1 ? g.dots : which == 2 ? g.peak : g.log_sum) + seq.q0 + threadIdx.x % Q_STEP;
+    const int64_t q_step = g.queries.ld * (2 * Q_STEP), o_step = g.douts.ld * (2 * Q_STEP);
+    const char *q_at = nullptr, *o_at = nullptr;
+    const float *row_at = nullptr;
     float from_row = 0.0f;
-    int next_head = 0, next_tile = 0;
-    const auto load = [&](int buffer) __attribute__((always_inline)) {
-        const int head = kv * group + next_head, i0 = (tile0 + next_tile) * Q_STEP, which = threadIdx.x / Q_STEP, i = i0 + threadIdx.x % Q_STEP;
+    int next_head = 0, next_tile = 0, next_i0 = 0;
+    const auto point = [&]() __attribute__((always_inline)) {
+        const int head = kv * group + next_head;
+        next_i0 = (tile0 + next_tile) * Q_STEP;
+        q_at = g.queries.of(row_q + next_i0, head);
+        o_at = g.douts.of(row_o + next_i0, head);
+        row_at = of_rows + (int64_t)head * a.rows_q + next_i0;
+    };
+    const auto load = [&](auto buffer) __attribute__((always_inline)) {
         if (which < (BIAS ? 4 : 2)) {
-            const float *const of = which == 0 ? g.base : which == 1 ? g.dots : which == 2 ? g.peak : g.log_sum;
-            const float x = of[(int64_t)head * a.rows_q + seq.q0 + (i < seq.nq ? i : seq.nq - 1)];
-            from_row = i < seq.nq ? x : which % 2 == 0 ? INFINITY : 0.0f;
+            const int left = seq.nq - 1 - next_i0 - (int)threadIdx.x % Q_STEP;           // rows behind this thread's
+            const float x = row_at[left < 0 ? left : 0];
+            from_row = left >= 0 ? x : which % 2 == 0 ? INFINITY : 0.0f;
         }
-        const u32x4 q_from = fill_q.descriptor(g.queries.of(row_q + i0, head)), o_from = fill_o.descriptor(g.douts.of(row_o + i0, head));
-        if (i0 + Q_STEP <= seq.nq) {
+        const u32x4 q_from = fill_q.descriptor(q_at), o_from = fill_o.descriptor(o_at);
+        if (next_i0 + Q_STEP <= seq.nq) {
             fill_q.whole(q_from, tiles[buffer][0]);
             fill_o.whole(o_from, tiles[buffer][1]);
         } else {
-            const auto holds = [&](int r) { return i0 + r < seq.nq; };
+            const auto holds = [&](int r) { return next_i0 + r < seq.nq; };
             fill_q.held(q_from, tiles[buffer][0], holds);
             fill_o.held(o_from, tiles[buffer][1], holds);
         }
@@ -222,14 +234,14 @@ __global__ __launch_bounds__(256, 2) void k_grad_kv(Grad g) {
     Distances by_distance{}, next_distance{};
     int of_head = -1;
     const auto lowest_of = [&](int i0) { return off + i0 - (k0 + BLOCK - 1); };
-    const auto stage = [&](int buffer) __attribute__((always_inline)) {
+    const auto stage = [&](auto buffer) __attribute__((always_inline)) {
         if (threadIdx.x < (BIAS ? 4 : 2) * Q_STEP) rows[buffer][threadIdx.x / Q_STEP][threadIdx.x % Q_STEP] = from_row;
         if constexpr (BIAS) {
             if (w == 1) {                                       // whose first half has the peaks
                 const bool any = __any(lane < 32 && fabsf(from_row) > USUAL && fabsf(from_row) < INFINITY);
                 if (lane == 0) lowest[buffer] = any;
             }
-            const int head = kv * group + next_head, i0 = (tile0 + next_tile) * Q_STEP;
+            const int head = kv * group + next_head;
             if (head != of_head) {
                 __syncthreads();                                // the last head's tiles are done with its bias
                 bias.load(a, head);
@@ -238,7 +250,7 @@ __global__ __launch_bounds__(256, 2) void k_grad_kv(Grad g) {
                 next_distance.begin(bias, a.buckets);           // read behind the next step's barrier
                 __syncthreads();
             }
-            next_distance.look_up(bias, lowest_of(i0), buffer, a.buckets);
+            next_distance.look_up(bias, lowest_of(next_i0), buffer, a.buckets);
         }
     };
 
@@ -255,21 +267,25 @@ __global__ __launch_bounds__(256, 2) void k_grad_kv(Grad g) {
     }
     const float unit = a.scale * LOG2E, times = DT == PARO_F16 ? g.times[0] * 0x1p-15f : 1.0f;
     f32x16 dk[HD / 32] = {}, dv[HD / 32] = {};
-    if (from < to) {
-        next_head = from / per_head;
-        next_tile = from % per_head;
-        load(0);
-        stage(0);
-    }
-    for (int u = from; u < to; ++u) {
-        const int i0 = (tile0 + next_tile) * Q_STEP, buffer = (u - from) & 1, first = off + i0;
+    constexpr std::integral_constant<int, 0> b0{};
+    constexpr std::integral_constant<int, 1> b1{};
+    int left = to - from;
+    const auto step = [&](auto buffer_, auto other) __attribute__((always_inline)) {
+        constexpr int buffer = buffer_;
+        const int i0 = next_i0, first = off + i0;
+        const bool more = --left > 0;
         by_distance = next_distance;
+        next_i0 += Q_STEP;
+        q_at += q_step;
+        o_at += o_step;
+        row_at += Q_STEP;
         if (++next_tile == per_head) {
             next_tile = 0;
             ++next_head;
+            point();
         }
         arrived<0>();                        // this step's tiles; and all waves have left the last step's
-        if (u + 1 < to) load(buffer ^ 1);
+        if (more) load(other);
         const char *const queries = tiles[buffer][0], *const douts = tiles[buffer][1];
         const bool none = first + Q_STEP - 1 < of_wave || (first - (of_wave + 31) >= a.window && of_wave >= a.sinks);
         if (!none) {
@@ -324,7 +340,18 @@ __global__ __launch_bounds__(256, 2) void k_grad_kv(Grad g) {
                 }
             }
         }
-        if (u + 1 < to) stage(buffer ^ 1);
+        if (more) stage(other);
+    };
+    if (from < to) {
+        next_head = from / per_head;
+        next_tile = from % per_head;
+        point();
+        load(b0);
+        stage(b0);
+        while (left > 0) {
+            step(b0, b1);
+            if (left > 0) step(b1, b0);
+        }
     }
     if (share.slot >= 0) {
         float *const at = g.partial + ((int64_t)share.slot * 2 * BLOCK + w * 32 + (lane & 31)) * HD + 4 * h;
@@ -373,10 +400,10 @@ __global__ __launch_bounds__(256) void k_grad_join(Grad g) {
 
 // ---------------------------------------------------------------- dq, and the table's gradient
 template <int DT, int HD, bool BIAS>
-__global__ __launch_bounds__(256, 2) void k_grad_q(Grad g) {
+__global__ __launch_bounds__(256, HD == 64 ? 3 : 2) void k_grad_q(Grad g) {
     using T = Tile<HD>;
     const Attn &a = g.a;
-    constexpr int KEYS = 32, RING = BIAS && HD == 128 ? 3 : 4;                  // so that two blocks go into the shared memory
+    constexpr int KEYS = 32, RING = !BIAS ? 4 : HD == 128 ? 3 : 2;      // so that two blocks (of short heads three) go into the shared memory
     constexpr int BYTES = KEYS * T::ROW, STEPS = HD / 16, DISTANCES = 32 + KEYS, SQUARE = 36;
     __shared__ __attribute__((aligned(1024))) char tiles[RING][2][BYTES];       // [part of the ring][keys, values]
     __shared__ Bias bias;
@@ -666,11 +693,21 @@ Plan plan_of(const paro_attn_t &d) {
     p.blocks_heads = (int)ceil_div(d.heads, DOT_HEADS);
     p.tiles = (int)ceil_div(d.len_q, BLOCK);
     p.key_tiles = (int)ceil_div(d.len_k, BLOCK);
-    // Tiles of keys are shared out where there are few of them; those with sinks, which every later query sees, by how many more see them than see others.
+    // Tiles of keys are shared out where there are few of them, by a reckoning of the time (us): a step of 32 queries takes 1.5 with one block on a compute unit, 2.3 with
+    // two, each share four more at its beginning and end; its sums are written and read again.  Those with sinks, which every later query sees, by how many more
+    // see them than see others.
     const int64_t whole = std::max<int64_t>(1, (int64_t)p.key_tiles * d.kv_heads * d.batch);
     const int64_t others = std::min<int64_t>(d.len_q, window + BLOCK);
-    const int64_t steps = std::max<int64_t>(1, ceil_div(others, Q_STEP) * group);
-    p.shares = (int)std::max<int64_t>(1, std::min<int64_t>(std::min<int64_t>(ceil_div(512, whole), ceil_div(steps, 8)), MOST_SHARES));
+    const double steps = std::max<double>(1.0, (double)ceil_div(others, Q_STEP) * group * (d.window ? 1.0 : 0.5));
+    double least = 0.0;
+    for (int shares = 1; shares <= MOST_SHARES; ++shares) {
+        const double blocks = (double)whole * shares, rounds = std::ceil(blocks / 512);
+        const double time = rounds * (steps / shares + 4) * (blocks > 256 ? 2.3 : 1.5) + (shares > 1 ? 5 + blocks * hd / 128 * 0.055 : 0.0);
+        if (shares == 1 || time < least) {
+            p.shares = shares;
+            least = time;
+        }
+    }
     p.sink_tiles = window < d.len_k ? (int)std::min<int64_t>(ceil_div(std::min<int64_t>(d.sinks, d.len_k), BLOCK), p.key_tiles) : 0;
     // (a share's sums take 128 KiB of the workspace)
     p.sink_shares = p.shares;
