@@ -230,8 +230,10 @@ __global__ __launch_bounds__(256, 2) void k_attend(Attn a) {
 // Up to 16 queries a sequence: the keys and values are read once for all queries and heads that share them, and nothing else counts.  A block's waves take 32 keys
 // at a time in turn: keys straight into registers as operands, values through shared memory of the wave's own, to be transposed.  The rows of
 // the products are the heads of a group, query by query, ROWS in all.  Long sequences are shared out among blocks, whose sums k_attend_join adds.
-constexpr int FEW = 16, FEW_KEYS = 32, FEW_WAVES = 4;
-constexpr int MOST_SHARES = 256;
+constexpr int FEW = 16, FEW_KEYS = 32, MOST_SHARES = 256;
+// Waves of a block: eight fill a compute unit's memory pipes without a second launch (four a block and twice the blocks, joined: 32 sequences with a window of 1024,
+// 8 key heads of 128, 36 us); wide heads with 32 rows leave registers for four.
+constexpr int few_waves(int hd, int nt) { return hd == 128 && nt == 2 ? 4 : 8; }
 
 struct Few {
     int shares, row_tiles;
@@ -256,13 +258,26 @@ __device__ __forceinline__ void store_stats(const Attn &a, int64_t row, int head
     at[1] = empty ? 0.0f : (__builtin_amdgcn_logf(sum) - SHIFT<DT>) * LN2;
 }
 
+// Four elements of a head's row.
+template <int DT>
+__device__ __forceinline__ void store4(char *row, int column, int hd, f32x4 v, float times) {
+    const u32x2 packed{both<DT>(v[0] * times, v[1] * times), both<DT>(v[2] * times, v[3] * times)};
+    if (column + 4 <= hd) {
+        store_half_piece(row, column, packed);
+        return;
+    }
+#pragma unroll
+    for (int e = 0; e < 3; ++e)
+        if (column + e < hd) reinterpret_cast<unsigned short *>(row)[column + e] = (unsigned short)(packed[e / 2] >> (16 * (e & 1)));
+}
+
 template <int DT, int HD, bool BIAS, int NT>
-__global__ __launch_bounds__(64 * FEW_WAVES, NT == 1 ? 2 : 1) void k_attend_few(Attn a, Few f) {
+__global__ __launch_bounds__((64 * few_waves(HD, NT))) void k_attend_few(Attn a, Few f) {
     using T = Tile<HD>;
-    constexpr int ROWS = 16 * NT, STEPS = HD / 32, PASSES = FEW_KEYS * T::PIECES / 64;
-    static_assert(FEW_WAVES * FEW_KEYS * T::ROW >= ROWS * HD * 4, "the waves' sums take the place of the values");
-    __shared__ __attribute__((aligned(1024))) char values[FEW_WAVES][FEW_KEYS * T::ROW];
-    __shared__ float of_waves[FEW_WAVES][ROWS][2];
+    constexpr int ROWS = 16 * NT, STEPS = HD / 32, PASSES = FEW_KEYS * T::PIECES / 64, WAVES = few_waves(HD, NT);
+    static_assert(FEW_KEYS * T::ROW == 16 * HD * 4, "a wave's sums of 16 rows take the place of its values");
+    __shared__ __attribute__((aligned(1024))) char values[WAVES][FEW_KEYS * T::ROW];
+    __shared__ float of_waves[WAVES][ROWS][2];
     __shared__ int first_of[MAX_BUCKETS];
     const int lane = threadIdx.x & 63, w = wave_of(), g = lane >> 4, of16 = lane & 15;
     const int share = blockIdx.x % f.shares, row_tile = blockIdx.x / f.shares % f.row_tiles;
@@ -307,7 +322,7 @@ __global__ __launch_bounds__(64 * FEW_WAVES, NT == 1 ? 2 : 1) void k_attend_few(
     float far_bias[NT] = {};
     if (from + w < to) load(from + w);
     if constexpr (BIAS) {
-        for (int i = threadIdx.x; i < a.buckets; i += 64 * FEW_WAVES) first_of[i] = a.first[i];
+        for (int i = threadIdx.x; i < a.buckets; i += 64 * WAVES) first_of[i] = a.first[i];
 #pragma unroll
         for (int n = 0; n < NT; ++n)
             if (there[n]) far_bias[n] = table_value(a, a.buckets - 1, head[n]);
@@ -323,7 +338,7 @@ __global__ __launch_bounds__(64 * FEW_WAVES, NT == 1 ? 2 : 1) void k_attend_few(
         sum[n] = 0.0f;
     }
     char *const mine = values[w];
-    for (int t = from + w; t < to; t += FEW_WAVES) {
+    for (int t = from + w; t < to; t += WAVES) {
         const int k0 = seen.tile(t) * FEW_KEYS;
         if (!seen.holds_all(k0) || a.hd != HD) {
 #pragma unroll
@@ -342,7 +357,7 @@ __global__ __launch_bounds__(64 * FEW_WAVES, NT == 1 ? 2 : 1) void k_attend_few(
 #pragma unroll
         for (int n = 0; n < PASSES; ++n) *reinterpret_cast<u32x4 *>(mine + T::at(of_pass + n * APART, piece)) = from_v[n];
         asm volatile("" ::: "memory");                  // a wave's accesses of shared memory go in their order
-        if (t + FEW_WAVES < to) load(t + FEW_WAVES);
+        if (t + WAVES < to) load(t + WAVES);
         f32x4 s[NT][2];
 #pragma unroll
         for (int n = 0; n < NT; ++n)
@@ -417,7 +432,7 @@ __global__ __launch_bounds__(64 * FEW_WAVES, NT == 1 ? 2 : 1) void k_attend_few(
             for (int d = 0; d < HD / 16; ++d) out[n][d] = mfma16<DT>(T::columns16(mine, d, lane), p, out[n][d] * times);
         }
     }
-    // The waves' sums, one after the other, relative to the block's largest score.
+    // The waves' sums, relative to the block's largest score: 16 rows at a time, each thread adds four elements of a row, wave by wave.
 #pragma unroll
     for (int n = 0; n < NT; ++n) {
         sum[n] = sum_of_quads(sum[n]);
@@ -427,60 +442,43 @@ __global__ __launch_bounds__(64 * FEW_WAVES, NT == 1 ? 2 : 1) void k_attend_few(
         }
     }
     __syncthreads();
-    float *const sums = reinterpret_cast<float *>(values[0]);            // [ROWS][HD]
-    float all_most[NT], all_sum[NT];
 #pragma unroll
     for (int n = 0; n < NT; ++n) {
-        const int r = n * 16 + of16;
-        all_most[n] = -INFINITY;
-        all_sum[n] = 0.0f;
-        for (int v = 0; v < FEW_WAVES; ++v) all_most[n] = fmaxf(all_most[n], of_waves[v][r][0]);
-        const float base = all_most[n] == -INFINITY ? 0.0f : all_most[n];
-        for (int v = 0; v < FEW_WAVES; ++v) all_sum[n] += of_waves[v][r][1] * exp2_((of_waves[v][r][0] - base) * unit);
+        const int r16 = n * 16 + of16;
+        float all_most = -INFINITY, all_sum = 0.0f;
+        for (int v = 0; v < WAVES; ++v) all_most = fmaxf(all_most, of_waves[v][r16][0]);
+        const float base = all_most == -INFINITY ? 0.0f : all_most;
+        for (int v = 0; v < WAVES; ++v) all_sum += of_waves[v][r16][1] * exp2_((of_waves[v][r16][0] - base) * unit);
         const float times = exp2_((most[n] - base) * unit);              // 0 where this wave saw nothing
+        float *const mine_out = reinterpret_cast<float *>(mine);
 #pragma unroll
-        for (int d = 0; d < HD / 16; ++d) out[n][d] *= times;
-    }
-    for (int v = 0; v < FEW_WAVES; ++v) {
-        if (v == w) {
-#pragma unroll
-            for (int n = 0; n < NT; ++n)
-#pragma unroll
-                for (int d = 0; d < HD / 16; ++d) {
-                    f32x4 *const at = reinterpret_cast<f32x4 *>(sums + (n * 16 + of16) * HD + d * 16 + 4 * g);
-                    *at = v ? *at + out[n][d] : out[n][d];
-                }
+        for (int d = 0; d < HD / 16; ++d) *reinterpret_cast<f32x4 *>(mine_out + of16 * HD + d * 16 + 4 * g) = out[n][d] * times;
+        if (w == 0 && g == 0) {
+            if (f.shares > 1) {
+                f.stats[((int64_t)blockIdx.x * ROWS + r16) * 2] = all_most;
+                f.stats[((int64_t)blockIdx.x * ROWS + r16) * 2 + 1] = all_sum;
+            } else if (a.stats && there[n]) {
+                store_stats<DT, BIAS>(a, (int64_t)seq.q0 + (rows_before + r16) / group, head[n], all_most, all_sum);
+            }
         }
         __syncthreads();
-    }
-    if (f.shares > 1) {
-        float *const part = f.sums + (int64_t)blockIdx.x * (ROWS * HD);
-        for (int x = threadIdx.x; x < ROWS * HD / 4; x += 64 * FEW_WAVES) reinterpret_cast<f32x4 *>(part)[x] = reinterpret_cast<const f32x4 *>(sums)[x];
-        if (w == 0 && g == 0)
+        for (int x = threadIdx.x; x < 16 * HD / 4; x += 64 * WAVES) {
+            const int row = x / (HD / 4), c = x % (HD / 4) * 4, of_rows = rows_before + n * 16 + row;
+            f32x4 all{};
 #pragma unroll
-            for (int n = 0; n < NT; ++n) {
-                f.stats[((int64_t)blockIdx.x * ROWS + n * 16 + of16) * 2] = all_most[n];
-                f.stats[((int64_t)blockIdx.x * ROWS + n * 16 + of16) * 2 + 1] = all_sum[n];
+            for (int v = 0; v < WAVES; ++v) all += *reinterpret_cast<const f32x4 *>(values[v] + x * 16);
+            if (f.shares > 1) {
+                *reinterpret_cast<f32x4 *>(f.sums + ((int64_t)blockIdx.x * ROWS + n * 16 + row) * HD + c) = all;
+            } else if (of_rows < rows && c < a.hd) {
+                float most_of = -INFINITY, sum_of = 0.0f;
+                for (int v = 0; v < WAVES; ++v) most_of = fmaxf(most_of, of_waves[v][n * 16 + row][0]);
+                const float base_of = most_of == -INFINITY ? 0.0f : most_of;
+                for (int v = 0; v < WAVES; ++v) sum_of += of_waves[v][n * 16 + row][1] * exp2_((of_waves[v][n * 16 + row][0] - base_of) * unit);
+                store4<DT>(a.out.of((int64_t)seq.q0 + of_rows / group, kv * group + of_rows % group), c, a.hd, all, sum_of > 0.0f ? 1.0f / sum_of : sum_of);
             }
-        return;
+        }
+        __syncthreads();                    // the next 16 rows come to the same place
     }
-    if (w == 0 && g == 0)
-#pragma unroll
-        for (int n = 0; n < NT; ++n) of_waves[0][n * 16 + of16][1] = all_sum[n];
-    __syncthreads();
-    for (int x = threadIdx.x; x < ROWS * T::PIECES; x += 64 * FEW_WAVES) {
-        const int r = x / T::PIECES, c = x % T::PIECES * 8, of_rows = rows_before + r;
-        if (of_rows >= rows || c >= a.hd) continue;
-        const float all = of_waves[0][r][1], times = all > 0.0f ? 1.0f / all : all;
-        float v[8];
-#pragma unroll
-        for (int e = 0; e < 8; ++e) v[e] = sums[r * HD + c + e] * times;
-        store_piece_of_head(a.out.of((int64_t)seq.q0 + of_rows / group, kv * group + of_rows % group), c, a.hd, pack<DT>(v));
-    }
-    if (a.stats && w == 0 && g == 0)
-#pragma unroll
-        for (int n = 0; n < NT; ++n)
-            if (there[n]) store_stats<DT, BIAS>(a, (int64_t)seq.q0 + (rows_before + n * 16 + of16) / group, head[n], all_most[n], all_sum[n]);
 }
 
 // Adds the shares of a row, in order: a wave a row.
@@ -498,15 +496,22 @@ __global__ __launch_bounds__(256) void k_attend_join(Attn a, Few f) {
     const float unit = BIAS ? LOG2E : a.scale * LOG2E;
     const int64_t block = (of_kv * f.row_tiles + row_tile) * f.shares;
     const float *const stats = f.stats + (block * ROWS + r) * 2, *const sums = f.sums + (block * ROWS + r) * HD + lane * EACH;
+    // a lane has every 64th share's part in the sum
     float most = -INFINITY, sum = 0.0f, out[EACH] = {};
-    for (int s = 0; s < f.shares; ++s) most = fmaxf(most, stats[(int64_t)s * ROWS * 2]);
-    const float base = most == -INFINITY ? 0.0f : most;
-#pragma unroll 8
-    for (int s = 0; s < f.shares; ++s) {
-        const float times = exp2_((stats[(int64_t)s * ROWS * 2] - base) * unit);
-        sum += stats[(int64_t)s * ROWS * 2 + 1] * times;
+    for (int s = lane; s < f.shares; s += 64) most = fmaxf(most, stats[(int64_t)s * ROWS * 2]);
 #pragma unroll
-        for (int e = 0; e < EACH; ++e) out[e] += sums[(int64_t)s * ROWS * HD + e] * times;
+    for (int n = 1; n < 64; n *= 2) most = fmaxf(most, __shfl_xor(most, n));
+    const float base = most == -INFINITY ? 0.0f : most;
+    for (int s0 = 0; s0 < f.shares; s0 += 64) {
+        const int mine = s0 + lane < f.shares ? s0 + lane : f.shares - 1, here = f.shares - s0 < 64 ? f.shares - s0 : 64;
+        const float of_share = exp2_((stats[(int64_t)mine * ROWS * 2] - base) * unit), total = stats[(int64_t)mine * ROWS * 2 + 1];
+#pragma unroll 8
+        for (int s = 0; s < here; ++s) {
+            const float times = __shfl(of_share, s);
+            sum += __shfl(total, s) * times;
+#pragma unroll
+            for (int e = 0; e < EACH; ++e) out[e] += sums[(int64_t)(s0 + s) * ROWS * HD + e] * times;
+        }
     }
     const float times = sum > 0.0f ? 1.0f / sum : sum;
     const int head = kv * group + of_rows % group;
@@ -540,9 +545,10 @@ Plan plan_of(const paro_attn_t &d) {
     const int64_t rows = std::max<int64_t>(1, d.len_q * group), head_dim = d.head_dim <= 64 ? 64 : 128;
     p.tiles_of_rows = rows <= 16 ? 1 : 2;
     p.row_tiles = (int)ceil_div(rows, 16 * p.tiles_of_rows);
-    const int64_t whole = d.batch * d.kv_heads * p.row_tiles;
+    const int64_t whole = d.batch * d.kv_heads * p.row_tiles, waves = few_waves((int)head_dim, p.tiles_of_rows);
     const int64_t span = d.window ? std::min<int64_t>(d.len_k, std::min<int64_t>(d.window, d.len_k) + d.len_q + std::min<int64_t>(d.sinks, d.len_k)) : d.len_k;
-    p.shares = (int)std::max<int64_t>(1, std::min<int64_t>(std::min<int64_t>(ceil_div(512, whole), ceil_div(span, 2 * FEW_WAVES * FEW_KEYS)), MOST_SHARES));
+    // Eight waves a compute unit; each has three tiles of keys at least, as a second launch costs what three take.
+    p.shares = (int)std::max<int64_t>(1, std::min<int64_t>(std::min<int64_t>(ceil_div(2048 / waves, whole), ceil_div(span, 3 * waves * FEW_KEYS)), MOST_SHARES));
     p.blocks = whole * p.shares;
     if (p.shares > 1) {
         p.stats = p.blocks * 16 * p.tiles_of_rows * head_dim * 4;
@@ -560,10 +566,10 @@ void launch(const Attn &a, const Plan &p, char *workspace, hipStream_t st) {
     const Few f{p.shares, p.row_tiles, reinterpret_cast<float *>(workspace), reinterpret_cast<float *>(workspace + p.stats)};
     const unsigned joins = (unsigned)(p.blocks / p.shares * 4 * p.tiles_of_rows);
     if (p.tiles_of_rows == 1) {
-        hipLaunchKernelGGL((k_attend_few<DT, HD, BIAS, 1>), dim3((unsigned)p.blocks), dim3(64 * FEW_WAVES), 0, st, a, f);
+        hipLaunchKernelGGL((k_attend_few<DT, HD, BIAS, 1>), dim3((unsigned)p.blocks), dim3(64 * few_waves(HD, 1)), 0, st, a, f);
         if (p.shares > 1) hipLaunchKernelGGL((k_attend_join<DT, HD, BIAS, 1>), dim3(joins), dim3(256), 0, st, a, f);
     } else {
-        hipLaunchKernelGGL((k_attend_few<DT, HD, BIAS, 2>), dim3((unsigned)p.blocks), dim3(64 * FEW_WAVES), 0, st, a, f);
+        hipLaunchKernelGGL((k_attend_few<DT, HD, BIAS, 2>), dim3((unsigned)p.blocks), dim3(64 * few_waves(HD, 2)), 0, st, a, f);
         if (p.shares > 1) hipLaunchKernelGGL((k_attend_join<DT, HD, BIAS, 2>), dim3(joins), dim3(256), 0, st, a, f);
     }
 }
