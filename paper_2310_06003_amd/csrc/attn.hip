@@ -505,12 +505,20 @@ __global__ __launch_bounds__(256) void k_attend_join(Attn a, Few f) {
     for (int s0 = 0; s0 < f.shares; s0 += 64) {
         const int mine = s0 + lane < f.shares ? s0 + lane : f.shares - 1, here = f.shares - s0 < 64 ? f.shares - s0 : 64;
         const float of_share = exp2_((stats[(int64_t)mine * ROWS * 2] - base) * unit), total = stats[(int64_t)mine * ROWS * 2 + 1];
-#pragma unroll 8
-        for (int s = 0; s < here; ++s) {
-            const float times = __shfl(of_share, s);
-            sum += __shfl(total, s) * times;
+        for (int s = 0; s < here; s += 8) {                 // eight shares in flight
+            float part[8][EACH];
 #pragma unroll
-            for (int e = 0; e < EACH; ++e) out[e] += sums[(int64_t)(s0 + s) * ROWS * HD + e] * times;
+            for (int u = 0; u < 8; ++u)
+#pragma unroll
+                for (int e = 0; e < EACH; ++e) part[u][e] = sums[(int64_t)(s0 + (s + u < here ? s + u : here - 1)) * ROWS * HD + e];
+#pragma unroll
+            for (int u = 0; u < 8; ++u) {
+                const int of = s + u < here ? s + u : here - 1;
+                const float times = s + u < here ? __shfl(of_share, of) : 0.0f;
+                sum += __shfl(total, of) * times;
+#pragma unroll
+                for (int e = 0; e < EACH; ++e) out[e] += part[u][e] * times;
+            }
         }
     }
     const float times = sum > 0.0f ? 1.0f / sum : sum;
@@ -547,8 +555,10 @@ Plan plan_of(const paro_attn_t &d) {
     p.row_tiles = (int)ceil_div(rows, 16 * p.tiles_of_rows);
     const int64_t whole = d.batch * d.kv_heads * p.row_tiles, waves = few_waves((int)head_dim, p.tiles_of_rows);
     const int64_t span = d.window ? std::min<int64_t>(d.len_k, std::min<int64_t>(d.window, d.len_k) + d.len_q + std::min<int64_t>(d.sinks, d.len_k)) : d.len_k;
-    // Eight waves a compute unit; each has three tiles of keys at least, as a second launch costs what three take.
-    p.shares = (int)std::max<int64_t>(1, std::min<int64_t>(std::min<int64_t>(ceil_div(2048 / waves, whole), ceil_div(span, 3 * waves * FEW_KEYS)), MOST_SHARES));
+    // Eight waves a compute unit, sixteen over long caches (4 of 50000 to 100000 keys, 8 key heads of 128: 265 us, so 242); each of eight has three tiles of keys at least, as a
+    // second launch costs what three take, each of sixteen twelve (32 sequences with a window of 1024 in 512 blocks 38 us, in 256 27).
+    const auto shares = [&](int64_t all, int64_t tiles) { return std::min<int64_t>(ceil_div(all / waves, whole), ceil_div(span, tiles * waves * FEW_KEYS)); };
+    p.shares = (int)std::max<int64_t>(1, std::min<int64_t>(std::max(shares(2048, 3), shares(4096, 12)), MOST_SHARES));
     p.blocks = whole * p.shares;
     if (p.shares > 1) {
         p.stats = p.blocks * 16 * p.tiles_of_rows * head_dim * 4;
