@@ -360,9 +360,17 @@ __global__ __launch_bounds__(256) void k_align(Attn a, Copies c) {
     const int64_t to0 = (int64_t)b * (keys ? a.len_k : a.len_q) + row0, from0 = (int64_t)(keys ? seq.k0 : seq.q0) + row0;
     const Rows from = c.from[which];
     u32x4 *const to = reinterpret_cast<u32x4 *>(c.to[which]) + to0 * of_row;
-    for (int x = threadIdx.x; x < rows * of_row; x += 256) {
-        const int r = x / of_row, in = x % of_row;
-        to[x] = piece_of_head(from.of(from0 + r, in / pieces), in % pieces * 8, a.hd, true);
+    const int all = rows > 0 ? rows * of_row : 0;
+    for (int x0 = threadIdx.x; x0 < all; x0 += 4 * 256) {                    // four pieces in flight
+        u32x4 v[4];
+#pragma unroll
+        for (int u = 0; u < 4; ++u) {
+            const int x = x0 + u * 256 < all ? x0 + u * 256 : all - 1, r = x / of_row, in = x % of_row;
+            v[u] = piece_of_head(from.of(from0 + r, in / pieces), in % pieces * 8, a.hd, true);
+        }
+#pragma unroll
+        for (int u = 0; u < 4; ++u)
+            if (x0 + u * 256 < all) to[x0 + u * 256] = v[u];
     }
 }
 

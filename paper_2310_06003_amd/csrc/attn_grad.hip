@@ -4,8 +4,8 @@
 //   D_i = dout_i . out_i,  dP_ij = dout_i . v_j,  dS_ij = P_ij (dP_ij - D_i)
 //   dv_j = sum_i P_ij dout_i,  dk_j = scale sum_i dS_ij q_i,  dq_i = scale sum_j dS_ij k_j,  dtable[b] = sum of dS_ij over bucket(p_i - j) = b
 //
-// Two passes over the pairs that see each other, each of which forms P and dP again: k_grad_kv goes over the queries and keeps dk and dv of 128 keys in registers,
-// k_grad_q over the keys and keeps dq of 128 queries.  That is seven products where five would do, but every sum has one place and one order: no atomics on
+// Two passes over the pairs that see each other, each of which forms P and dP again: grad_kv goes over the queries and keeps dk and dv of 128 keys in registers,
+// grad_q over the keys and keeps dq of 128 queries.  That is seven products where five would do, but every sum has one place and one order: no atomics on
 // results, the same call gives the same bits.  P and dS are rounded to 16 bits for the products; as in the forward pass, a product's result is
 // the next one's operand as it stands.  fp16: P is multiplied by 2^15; dS by a power of two that brings twice the largest |dout_i| |v_j| to at most 2^15, so that none
 // overflows and the small ones keep their bits.
@@ -13,7 +13,7 @@
 
 namespace {
 
-constexpr int BLOCK = 128;                   // keys of a k_grad_kv block, queries of a k_grad_q block: 32 a wave
+constexpr int BLOCK = 128;                   // keys of a grad_kv block, queries of a grad_q block: 32 a wave
 constexpr int Q_STEP = 32;                   // queries of a tile
 constexpr int MOST_SHARES = 64;
 template <int DT>
@@ -36,7 +36,7 @@ struct Grad {
 };
 
 // ---------------------------------------------------------------- statistics of the rows
-constexpr int DOT_ROWS = 32, DOT_HEADS = 8;
+constexpr int DOT_ROWS = 16, DOT_HEADS = 8;
 
 template <int HD>
 __device__ __forceinline__ float over_lanes(float x) {       // of HD / 8 lanes side by side
@@ -44,11 +44,11 @@ __device__ __forceinline__ float over_lanes(float x) {       // of HD / 8 lanes 
     for (int n = 1; n < HD / 8; n *= 2) x += __shfl_xor(x, n);
     return x;
 }
-// D, and what P is formed from, of 32 rows of 8 heads; blocks behind those of the queries: the values' largest row.
+// D, and what P is formed from, of 16 rows of 8 heads; blocks behind those of the queries: the values' largest row.
 template <int DT, int HD>
 __global__ __launch_bounds__(256) void k_dots(Grad g) {
     const Attn &a = g.a;
-    constexpr int LANES = HD / 8, AT_ONCE = 256 / LANES, U = 4;
+    constexpr int LANES = HD / 8, AT_ONCE = 256 / LANES, U = DOT_ROWS * DOT_HEADS / AT_ONCE;       // all of a block in flight
     __shared__ float dots[DOT_HEADS][DOT_ROWS + 1];
     const bool of_values = (int)blockIdx.x >= g.blocks_q;
     const unsigned tiles = (of_values ? g.blocks_v : g.blocks_q) / a.batch, block = of_values ? blockIdx.x - g.blocks_q : blockIdx.x;
@@ -92,7 +92,7 @@ __global__ __launch_bounds__(256) void k_dots(Grad g) {
     __syncthreads();
     if (!of_values) {
         const int r = threadIdx.x % DOT_ROWS, head = head0 + threadIdx.x / DOT_ROWS;
-        if (r < rows && head < heads) {
+        if (threadIdx.x < DOT_ROWS * DOT_HEADS && r < rows && head < heads) {
             const float *const stats = a.stats + (((int64_t)seq.q0 + row0 + r) * a.heads + head) * 2;
             const float most = stats[0], log_sum = stats[1];
             const int64_t at = (int64_t)head * a.rows_q + seq.q0 + row0 + r;
@@ -170,18 +170,27 @@ __device__ __forceinline__ Share share_of(const Grad &g, int block, int of_kv) {
     return s;
 }
 
+template <int HD, bool BIAS>
+struct SharedKv {
+    __attribute__((aligned(1024))) char tiles[2][2][Q_STEP * Tile<HD>::ROW];   // [buffer][queries, dout]
+    __attribute__((aligned(1024))) char values[BLOCK * Tile<HD>::ROW];
+    __attribute__((aligned(16))) float rows[2][4][Q_STEP];                     // [buffer][base, dots, peak, log_sum]
+    int lowest[2];                                                             // whether the base of any row says too little
+    std::conditional_t<BIAS, Bias, int> bias;
+};
 template <int DT, int HD, bool BIAS>
-__global__ __launch_bounds__(256, HD == 64 ? 3 : 2) void k_grad_kv(Grad g) {
+__device__ __forceinline__ void grad_kv(const Grad &g, unsigned block, SharedKv<HD, BIAS> &shared) {
     using T = Tile<HD>;
     const Attn &a = g.a;
-    constexpr int BYTES = Q_STEP * T::ROW, STEPS = HD / 16;
-    __shared__ __attribute__((aligned(1024))) char tiles[2][2][BYTES];         // [buffer][queries, dout]
-    __shared__ __attribute__((aligned(1024))) char values[BLOCK * T::ROW];
-    __shared__ __attribute__((aligned(16))) float rows[2][4][Q_STEP];          // [buffer][base, dots, peak, log_sum]
-    __shared__ int lowest[2];                                                  // whether the base of any row says too little
-    __shared__ Bias bias;
+    auto &tiles = shared.tiles;
+    auto &values = shared.values;
+    auto &rows = shared.rows;
+    auto &lowest = shared.lowest;
+    auto &bias = shared.bias;
+    constexpr int STEPS = HD / 16;
     const int per_kv = g.sink_tiles * g.sink_shares + (g.key_tiles - g.sink_tiles) * g.shares;
-    const Work work(blockIdx.x, a.batch * a.kv_heads, per_kv);
+    if (block >= (unsigned)(per_kv * a.batch * a.kv_heads)) return;
+    const Work work(block, a.batch * a.kv_heads, per_kv);
     const int of_kv = work.unit, kv = of_kv % a.kv_heads, b = of_kv / a.kv_heads;
     const Share share = share_of(g, work.within, of_kv);
     const Sequence seq(a, b);
@@ -399,21 +408,31 @@ __global__ __launch_bounds__(256) void k_grad_join(Grad g) {
 }
 
 // ---------------------------------------------------------------- dq, and the table's gradient
-template <int DT, int HD, bool BIAS>
-__global__ __launch_bounds__(256, HD == 64 ? 3 : 2) void k_grad_q(Grad g) {
-    using T = Tile<HD>;
-    const Attn &a = g.a;
-    constexpr int KEYS = 32, RING = !BIAS ? 4 : HD == 128 ? 3 : 2;      // so that two blocks (of short heads three) go into the shared memory
-    constexpr int BYTES = KEYS * T::ROW, STEPS = HD / 16, DISTANCES = 32 + KEYS, SQUARE = 36;
-    __shared__ __attribute__((aligned(1024))) char tiles[RING][2][BYTES];       // [part of the ring][keys, values]
-    __shared__ Bias bias;
-    __shared__ __attribute__((aligned(16))) float squares[BIAS ? 4 : 1][BIAS ? 32 * SQUARE : 4];     // [wave]: 32 x 32 of dS
-    __shared__ float diagonals[BIAS ? 4 : 1][DISTANCES];                        // [wave]: sums of dS along a distance, of one tile
-    // Of the block: by distance; where the bias is not there for every distance, [wave][bucket]
-    __shared__ float sums[BIAS ? NEAR + EDGE : 1], far_sums[4];
+template <int HD, bool BIAS>
+struct SharedQ {
+    static constexpr int KEYS = 32, RING = !BIAS ? 4 : HD == 128 ? 3 : 2;       // so that two blocks (of short heads three) go into the shared memory
+    static constexpr int DISTANCES = 32 + KEYS, SQUARE = 36;
     static_assert(NEAR + EDGE >= 4 * MAX_BUCKETS, "the waves' buckets take the place of the distances");
+    __attribute__((aligned(1024))) char tiles[RING][2][KEYS * Tile<HD>::ROW];   // [part of the ring][keys, values]
+    __attribute__((aligned(16))) float squares[BIAS ? 4 : 1][BIAS ? 32 * SQUARE : 4];      // [wave]: 32 x 32 of dS
+    float diagonals[BIAS ? 4 : 1][DISTANCES];                                   // [wave]: sums of dS along a distance, of one tile
+    float sums[BIAS ? NEAR + EDGE : 1], far_sums[4];                            // of the block: by distance; where the bias is not there for every one, [wave][bucket]
+    std::conditional_t<BIAS, Bias, int> bias;
+};
+template <int DT, int HD, bool BIAS>
+__device__ __forceinline__ void grad_q(const Grad &g, unsigned block, SharedQ<HD, BIAS> &shared) {
+    using T = Tile<HD>;
+    using S = SharedQ<HD, BIAS>;
+    const Attn &a = g.a;
+    constexpr int KEYS = S::KEYS, RING = S::RING, STEPS = HD / 16, DISTANCES = S::DISTANCES, SQUARE = S::SQUARE;
+    auto &tiles = shared.tiles;
+    auto &squares = shared.squares;
+    auto &diagonals = shared.diagonals;
+    auto &sums = shared.sums;
+    auto &far_sums = shared.far_sums;
+    auto &bias = shared.bias;
     const int group = a.heads / a.kv_heads;
-    const Work work(blockIdx.x, a.batch * a.kv_heads, a.tiles * group);
+    const Work work(block, a.batch * a.kv_heads, a.tiles * group);
     const int kv = work.unit % a.kv_heads, b = work.unit / a.kv_heads, head = kv * group + work.within % group;
     const int tile = a.tiles - 1 - work.within / group, i0 = tile * BLOCK;             // the longest first
     const bool want = BIAS && g.dtable;
@@ -656,6 +675,18 @@ __global__ __launch_bounds__(256, HD == 64 ? 3 : 2) void k_grad_q(Grad g) {
     }
 }
 
+// Both passes in one launch, as neither fills the chip to its end: the first of_kv blocks (a multiple of eight, so that what is one XCD's stays there) have keys,
+// the others queries.  (In launches of their own: 1999 tokens of 10 heads of 77 88 + 59 us.)
+template <int DT, int HD, bool BIAS>
+__global__ __launch_bounds__(256, HD == 64 ? 3 : 2) void k_grads(Grad g, unsigned of_kv) {
+    __shared__ union {
+        SharedKv<HD, BIAS> kv;
+        SharedQ<HD, BIAS> q;
+    } shared;
+    if (blockIdx.x < of_kv) grad_kv<DT, HD, BIAS>(g, blockIdx.x, shared.kv);
+    else grad_q<DT, HD, BIAS>(g, blockIdx.x - of_kv, shared.q);
+}
+
 // Adds the blocks' sums of a head, in order: a thread has every `parts`-th of a bucket.
 template <int DT>
 __global__ __launch_bounds__(256) void k_table_grad(Grad g) {
@@ -748,14 +779,10 @@ template <int DT, int HD, bool BIAS>
 void launch(const Grad &g, const Plan &p, hipStream_t st) {
     if (p.blocks_q + p.blocks_v) hipLaunchKernelGGL((k_dots<DT, HD>), dim3((unsigned)(p.blocks_q + p.blocks_v), (unsigned)p.blocks_heads), dim3(256), 0, st, g);
     if constexpr (DT == PARO_F16) hipLaunchKernelGGL(k_times, dim3(1), dim3(256), 0, st, g);
-    if (p.kv_blocks) {
-        hipLaunchKernelGGL((k_grad_kv<DT, HD, BIAS>), dim3((unsigned)p.kv_blocks), dim3(256), 0, st, g);
-        const int joined = p.shares > 1 ? p.key_tiles : p.sink_shares > 1 ? p.sink_tiles : 0;
-        if (joined)
-            hipLaunchKernelGGL((k_grad_join<DT, HD>), dim3((unsigned)(joined * g.a.kv_heads * g.a.batch), BLOCK / (1024 / HD), 2), dim3(256), 0, st, g);
-    }
-    const unsigned q_blocks = (unsigned)((int64_t)p.tiles * g.a.heads * g.a.batch);
-    if (q_blocks) hipLaunchKernelGGL((k_grad_q<DT, HD, BIAS>), dim3(q_blocks), dim3(256), 0, st, g);
+    const int64_t of_kv = ceil_div(p.kv_blocks, 8) * 8, of_q = (int64_t)p.tiles * g.a.heads * g.a.batch;
+    if (of_kv + of_q) hipLaunchKernelGGL((k_grads<DT, HD, BIAS>), dim3((unsigned)(of_kv + of_q)), dim3(256), 0, st, g, (unsigned)of_kv);
+    const int joined = p.shares > 1 ? p.key_tiles : p.sink_shares > 1 ? p.sink_tiles : 0;
+    if (joined) hipLaunchKernelGGL((k_grad_join<DT, HD>), dim3((unsigned)(joined * g.a.kv_heads * g.a.batch), BLOCK / (1024 / HD), 2), dim3(256), 0, st, g);
     if (BIAS && g.dtable) hipLaunchKernelGGL((k_table_grad<DT>), dim3((unsigned)g.a.heads), dim3(256), 0, st, g);
 }
 
