@@ -729,10 +729,11 @@ Plan plan_of(const paro_attn_t &d) {
     // see them than see others.
     const int64_t whole = std::max<int64_t>(1, (int64_t)p.key_tiles * d.kv_heads * d.batch);
     const int64_t others = std::min<int64_t>(d.len_q, window + BLOCK);
-    const double steps = std::max<double>(1.0, (double)ceil_div(others, Q_STEP) * group * (d.window ? 1.0 : 0.5));
+    const double longest = std::max<double>(1.0, (double)ceil_div(others, Q_STEP) * group), usual = d.window ? longest : longest / 2;       // steps
     double least = 0.0;
     for (int shares = 1; shares <= MOST_SHARES; ++shares) {
         const double blocks = (double)whole * shares, rounds = std::ceil(blocks / 512);
+        const double steps = rounds > 1 ? usual : longest;
         const double time = rounds * (steps / shares + 4) * (blocks > 256 ? 2.3 : 1.5) + (shares > 1 ? 5 + blocks * hd / 128 * 0.055 : 0.0);
         if (shares == 1 || time < least) {
             p.shares = shares;

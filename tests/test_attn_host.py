@@ -67,6 +67,26 @@ def test_refuses_pointers():
     assert paro._lib.paro_attn_grad(None, *[P] * 16, 0, 0) == paro.PARO_EINVAL
 
 
+def test_rows_on_sixteen_bytes_lie_there():
+    """Where a head and its distances are whole pieces, the arrays that go to shared memory as they are lie on 16 bytes; others are copied."""
+    d = paro.make_attn(**{**ATTN, "buckets": 0})
+    for which, name in enumerate(("q", "k", "v")):
+        args = [P] * 3
+        args[which] = P + 8
+        if name != "q":
+            refused(lambda: paro.paro_attn(d, *args, 0, 0, 0, 0, 0, P, P, P, ROOM), paro.PARO_EALIGN, "16-byte")
+        refused(lambda: paro.paro_attn_grad(d, P, *args, P, P, 0, 0, 0, 0, 0, P, P, P, 0, P, ROOM), paro.PARO_EALIGN, "16-byte")
+    refused(lambda: paro.paro_attn_grad(d, P + 2, P, P, P, P, P, 0, 0, 0, 0, 0, P, P, P, 0, P, ROOM), paro.PARO_EALIGN, "16-byte")
+    whole, odd = (paro.make_attn(**{**ATTN, **x}) for x in (dict(head_dim=72), dict(head_dim=70)))
+    copy_k, copy_q = (-(-2 * 100 * heads * 72 * 2 // 256) * 256 for heads in (2, 4))
+    assert paro.paro_attn_workspace(whole, False) == 0 and paro.paro_attn_workspace(odd, False) == 2 * copy_k
+    assert paro.paro_attn_workspace(odd, True) == paro.paro_attn_workspace(whole, True) + 2 * copy_k + 2 * copy_q
+    apart = paro.make_attn(**{**ATTN, "ld_k": 131})                      # one of the four
+    assert paro.paro_attn_workspace(apart, False) == -(-2 * 100 * 2 * 64 * 2 // 256) * 256
+    few = paro.make_attn(**{**ATTN, "head_dim": 70, "len_q": 3})         # few queries take rows as they lie
+    assert paro.paro_attn_workspace(few, False) == 0
+
+
 def test_nothing_to_do_needs_no_arrays():
     for change in (dict(batch=0), dict(len_q=0)):
         d = paro.make_attn(**{**ATTN, **change})

@@ -70,6 +70,8 @@ def test_long_sequences(paro):
     backward(paro, [(1100, 1100)], heads=1, hd=128, window=100, sinks=4)
     backward(paro, [(1500, 1500)], heads=2, kv=1, hd=64, window=200, sinks=140, buckets=32, far=128, dtype="f16")
     backward(paro, [(700, 1500)], heads=1, hd=64, buckets=32, far=128)
+    backward(paro, [(700, 700)], heads=6, window=40, sinks=4)
+    backward(paro, [(700, 700)], heads=6, window=40, sinks=140, dtype="f16", buckets=8)
 
 
 @pytest.mark.parametrize("spread", [1e-6, 3e4])
