@@ -389,7 +389,7 @@ inline int check_attn(const std::string &f, const paro_attn_t *d) {
     if (d->batch * d->len_q > INT32_MAX && !d->rows_q) return bad("more than 2^31 - 1 rows of queries");
     if (d->batch * d->len_k > INT32_MAX && !d->rows_k) return bad("more than 2^31 - 1 rows of keys");
     if (d->window < 0 || d->sinks < 0) return bad("window and sinks must not be negative");
-    if (!(d->scale > 0.0f) || !(d->scale <= 3.0e38f)) return bad("scale must be positive and finite");
+    if (!(d->scale >= 1e-18f) || !(d->scale <= 1e18f)) return bad("scale must be in [1e-18, 1e18]");
     if (d->buckets < 0 || d->buckets > MAX_BUCKETS) return bad("buckets must be in [0, 256]");
     if (d->buckets && d->table_dtype != PARO_F32 && d->table_dtype != d->dtype) return bad("table_dtype must be PARO_F32 or dtype");
     // a head's distance is that between neighbours in a row, or that between whole planes: each row of each head ends before the next one's begins
@@ -402,8 +402,8 @@ inline int check_attn(const std::string &f, const paro_attn_t *d) {
         if (head < ld && ld < (count - 1) * head + hd) return bad("a row is longer than its distance to the next");
         if (ld > ((int64_t)1 << 24) || head > ((int64_t)1 << 50)) return bad("distances between rows are at most 2^24, between heads 2^50");
     }
-    if (ceil_div(std::max(d->len_q, d->len_k), 16) * d->heads > INT32_MAX / std::max<int64_t>(1, d->batch))
-        return bad("batch * heads * length is at most 2^35");
+    if (ceil_div(std::max(d->len_q, d->len_k), 8) * d->heads > INT32_MAX / std::max<int64_t>(1, d->batch))
+        return bad("batch * heads * length is at most 2^34");
     return PARO_OK;
 }
 // Without arrays that say where sequences lie, they lie one behind the other.

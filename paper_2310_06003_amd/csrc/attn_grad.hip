@@ -339,6 +339,10 @@ __device__ __forceinline__ void grad_kv(const Grad &g, unsigned block, SharedKv<
 #pragma unroll
                 for (int x = 0; x < 4; ++x) dp[e + x] = s[e + x] * (DT == PARO_F16 ? (dp[e + x] - dot[x]) * times : dp[e + x] - dot[x]);
             }
+            if (!every) {                        // what a key that is not seen holds is of no account
+#pragma unroll
+                for (int e = 0; e < 16; ++e) dp[e] = s[e] == 0.0f ? 0.0f : dp[e];
+            }
 #pragma unroll
             for (int k = 0; k < 2; ++k) {
                 const short8_t p = pack8<DT>(s, 8 * k), ds = pack8<DT>(dp, 8 * k);
@@ -552,6 +556,10 @@ __device__ __forceinline__ void grad_q(const Grad &g, unsigned block, SharedQ<HD
             }
 #pragma unroll
             for (int e = 0; e < 16; ++e) dp[e] = s[e] * (DT == PARO_F16 ? (dp[e] - dot) * times : dp[e] - dot);
+            if (!every) {                        // what a key that is not seen holds is of no account
+#pragma unroll
+                for (int e = 0; e < 16; ++e) dp[e] = s[e] == 0.0f ? 0.0f : dp[e];
+            }
             if constexpr (BIAS) {
                 if (want && beyond) {
 #pragma unroll

@@ -26,10 +26,10 @@ def refused(call, code, text):
     (dict(heads=1026), "heads"), (dict(heads=5), "multiple of kv_heads"), (dict(kv_heads=-2), "heads"), (dict(head_dim=0), "head_dim"), (dict(head_dim=7), "head_dim"), (dict(head_dim=129), "head_dim"),
     (dict(len_q=-2), "len_q"), (dict(len_q=2**30 + 1), "len_q"), (dict(len_k=2**31), "len_q"), (dict(rows_q=-1), "rows_q"), (dict(rows_k=2**31), "rows_q"),
     (dict(batch=4, len_q=2**30), "rows of queries"), (dict(batch=4, len_k=2**30), "rows of keys"), (dict(window=-1), "window"), (dict(sinks=-1), "window"),
-    (dict(scale=-1.0), "scale"), (dict(scale=math.nan), "scale"), (dict(scale=math.inf), "scale"), (dict(buckets=-1), "buckets"), (dict(buckets=257), "buckets"),
+    (dict(scale=-1.0), "scale"), (dict(scale=1e-19), "scale"), (dict(scale=1e19), "scale"), (dict(scale=math.nan), "scale"), (dict(scale=math.inf), "scale"), (dict(buckets=-1), "buckets"), (dict(buckets=257), "buckets"),
     (dict(table_dtype=paro.PARO_F16), "table_dtype"), (dict(ld_q=255), "longer"), (dict(ld_k=127), "longer"), (dict(ld_v=1), "longer"), (dict(ld_out=-256), "longer"),
     (dict(head_q=63), "longer"), (dict(head_k=-64), "longer"), (dict(head_v=65, ld_v=128), "longer"), (dict(head_out=80, ld_out=300), "longer"),
-    (dict(ld_k=2**24 + 1), "2^24"), (dict(head_v=2**50 + 1), "2^50"), (dict(heads=1024, kv_heads=1, batch=2, len_q=2**29, len_k=1), "2^35"),
+    (dict(ld_k=2**24 + 1), "2^24"), (dict(head_v=2**50 + 1), "2^50"), (dict(heads=1024, kv_heads=1, batch=2, len_q=2**29, len_k=1), "2^34"),
     (dict(rows_q=199), "rows_q holds"), (dict(rows_k=199), "rows_k holds")])
 def test_refuses(change, text):
     d = paro.make_attn(**{**ATTN, **change})

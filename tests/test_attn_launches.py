@@ -102,4 +102,4 @@ def test_passes_of_the_gradient(launches, dtype, buckets):
                                          (dict(n=1500, heads=16, kv=1, hd=64), 12), (dict(n=1024, batch=8, heads=12), 0)])
 def test_shared_tiles_of_keys(launches, size, joined):
     got = [x for x in launches("grad", **size) if x.kernel == "k_grad_join"]
-    assert [x.x for x in got] == ([joined * size.get("batch", 1) * (size.get("kv") or size["heads"])] if joined else [])
+    assert [x.x for x in got] == ([joined * size.get("batch", 1) * (size.get("kv") or size.get("heads", 2))] if joined else [])

@@ -81,6 +81,22 @@ def test_small_and_large_gradients(paro, spread):
     backward(paro, [(140, 140)], spread=spread, hd=128, dtype="bf16")
 
 
+@pytest.mark.parametrize("hd", [64, 72])
+def test_keys_that_no_query_sees(paro, hd):
+    """Between the sinks and the first window: whatever they hold, their gradients are zeros and the others as they were."""
+    c = Case(paro, [(200, 500)], window=60, sinks=3, hd=hd, heads=2)
+    gone = slice(c.k_at[0] + 3, c.k_at[0] + 500 - 200 - 60 + 1)
+    c.set_forward()
+    c.backward()
+    c.check_backward()
+    want = [x.view.clone() for x in (c.dq, c.dk, c.dv)]
+    assert bool((want[1][gone] == 0).all()) and bool((want[2][gone] == 0).all())
+    c.k.view[gone] = torch.inf
+    c.v.view[gone] = torch.nan
+    c.backward()
+    assert all(torch.equal(x.view, y) for x, y in zip((c.dq, c.dk, c.dv), want))
+
+
 def test_without_the_tables_gradient(paro):
     c = backward(paro, [(150, 150)], want_table=False, buckets=8)
     assert bool((c.dtable == 7).all())
