@@ -51,7 +51,7 @@ __device__ __forceinline__ float sum_of_halves(float x) {
 
 // Blocks go to the eight XCDs in turn.  A unit is the work of a sequence's key head, which reads the same keys and values over and over: it stays on one XCD, to meet
 // in its L2, and units go to the XCDs in turn, so that sequences of different lengths even out (runs of a sequence each: packed sequences of 1024 to 2048 tokens
-// forward 295 us, so 2xx); what is left over in the end is shared by all.
+// forward 295 us, so 220); what is left over in the end is shared by all.
 struct Work {
     int unit, within;
     __device__ __forceinline__ Work(unsigned block, unsigned units, unsigned of_unit) {
