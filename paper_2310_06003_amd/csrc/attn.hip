@@ -23,7 +23,7 @@ __global__ __launch_bounds__(256, 2) void k_attend(Attn a) {
     __shared__ __attribute__((aligned(1024))) char tiles[RING][2][BYTES];    // [part of the ring][keys, values]
     __shared__ Bias bias;
     const int group = a.heads / a.kv_heads;
-    const Work work(blockIdx.x, a.batch * a.kv_heads, a.tiles * group);
+    const Work work(blockIdx.x, a.batch * a.kv_heads, a.tiles * group, a.bunch, group);
     const int kv = work.unit % a.kv_heads, b = work.unit / a.kv_heads, head = kv * group + work.within % group;
     const int i0 = (a.tiles - 1 - work.within / group) * QUERIES;                      // the longest first
     const Sequence seq(a, b);
@@ -604,6 +604,7 @@ int paro_attn(const paro_attn_t *d, const void *q, const void *k, const void *v,
         a.out.at = static_cast<char *>(out);
         a.stats = stats;
         a.tiles = (int)ceil_div(d->len_q, QUERIES);
+        a.bunch = bunch_of(a.tiles * (d->heads / d->kv_heads));
         hipStream_t st = static_cast<hipStream_t>(stream);
         char *ws = static_cast<char *>(workspace);
         if (!p.few) {

@@ -51,15 +51,18 @@ __device__ __forceinline__ float sum_of_halves(float x) {
 
 // Blocks go to the eight XCDs in turn.  A unit is the work of a sequence's key head, which reads the same keys and values over and over: it stays on one XCD, to meet
 // in its L2, and units go to the XCDs in turn, so that sequences of different lengths even out (runs of a sequence each: packed sequences of 1024 to 2048 tokens
-// forward 295 us, so 220); what is left over in the end is shared by all.
+// forward 295 us, so 220); what is left over in the end is shared by all.  An XCD takes its units a bunch at a time, the longest blocks of all of them first, `together`
+// (the heads that read a key head) side by side.  (Unit by unit: 8 x 1024 tokens of 12 heads of 64 forward 44 us, so 36, backward 137, so 108; 8192 of 32 heads of 128
+// 446 and 1820, so 430 and 1755.  All units at once: 32 x 2048 tokens of 32 heads with a window of 512 forward 1283, as their keys do not fit the L2, so 890.  Heads apart: packed sequences 235.)
 struct Work {
     int unit, within;
-    __device__ __forceinline__ Work(unsigned block, unsigned units, unsigned of_unit) {
+    __device__ __forceinline__ Work(unsigned block, unsigned units, unsigned of_unit, unsigned bunch, unsigned together) {
         const unsigned whole = units / 8 * 8 * of_unit;
         if (block < whole) {
-            const unsigned k = block / 8;
-            unit = (int)(k / of_unit * 8 + block % 8);
-            within = (int)(k % of_unit);
+            const unsigned k = block / 8, g = k / (of_unit * bunch), left = units / 8 - g * bunch, n = (left < bunch ? left : bunch) * together;
+            const unsigned r = k - g * (of_unit * bunch), x = r % n;
+            unit = (int)((g * bunch + x / together) * 8 + block % 8);
+            within = (int)(r / n * together + x % together);
         } else {
             const unsigned rest = block - whole, all = (units % 8) * of_unit, each = all / 8, more = all % 8, xcd = rest % 8;
             const unsigned at = xcd * each + (xcd < more ? xcd : more) + rest / 8;
@@ -68,6 +71,8 @@ struct Work {
         }
     }
 };
+// Units of a bunch: two rounds of blocks of an XCD's 32 compute units, four units at least.
+inline int bunch_of(int64_t of_unit) { return (int)std::max<int64_t>(4, 128 / std::max<int64_t>(1, of_unit)); }
 
 // Rows of an array of heads: elements from token to token, and from head to head.
 struct Rows {
@@ -84,7 +89,7 @@ struct Attn {
     float *stats;
     const void *table;
     const int32_t *first;
-    int batch, heads, kv_heads, hd, len_q, len_k, rows_q, rows_k, window, sinks, buckets, table_dtype, tiles;
+    int batch, heads, kv_heads, hd, len_q, len_k, rows_q, rows_k, window, sinks, buckets, table_dtype, tiles, bunch;
     float scale;
 };
 

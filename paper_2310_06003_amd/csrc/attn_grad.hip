@@ -32,7 +32,7 @@ struct Grad {
     float *of_table;                         // [head][sequence][tile of queries][bucket]
     char *dtable;
     int blocks_q, blocks_v, blocks_heads;    // of k_dots
-    int key_tiles, sink_tiles, shares, sink_shares, slots;      // of a sequence's key head; sink_tiles: the first ones, whose keys are sinks
+    int key_tiles, sink_tiles, shares, sink_shares, slots, bunch_kv;      // of a sequence's key head; sink_tiles: the first ones, whose keys are sinks
 };
 
 // ---------------------------------------------------------------- statistics of the rows
@@ -190,7 +190,7 @@ __device__ __forceinline__ void grad_kv(const Grad &g, unsigned block, SharedKv<
     constexpr int STEPS = HD / 16;
     const int per_kv = g.sink_tiles * g.sink_shares + (g.key_tiles - g.sink_tiles) * g.shares;
     if (block >= (unsigned)(per_kv * a.batch * a.kv_heads)) return;
-    const Work work(block, a.batch * a.kv_heads, per_kv);
+    const Work work(block, a.batch * a.kv_heads, per_kv, g.bunch_kv, 1);
     const int of_kv = work.unit, kv = of_kv % a.kv_heads, b = of_kv / a.kv_heads;
     const Share share = share_of(g, work.within, of_kv);
     const Sequence seq(a, b);
@@ -436,7 +436,7 @@ __device__ __forceinline__ void grad_q(const Grad &g, unsigned block, SharedQ<HD
     auto &far_sums = shared.far_sums;
     auto &bias = shared.bias;
     const int group = a.heads / a.kv_heads;
-    const Work work(block, a.batch * a.kv_heads, a.tiles * group);
+    const Work work(block, a.batch * a.kv_heads, a.tiles * group, a.bunch, group);
     const int kv = work.unit % a.kv_heads, b = work.unit / a.kv_heads, head = kv * group + work.within % group;
     const int tile = a.tiles - 1 - work.within / group, i0 = tile * BLOCK;             // the longest first
     const bool want = BIAS && g.dtable;
@@ -832,6 +832,8 @@ int paro_attn_grad(const paro_attn_t *d, const void *dout, const void *q, const 
         g.a.out.at = static_cast<char *>(const_cast<void *>(out));
         g.a.stats = const_cast<float *>(stats);
         g.a.tiles = p.tiles;
+        g.a.bunch = bunch_of(p.tiles * (d->heads / d->kv_heads));
+        g.bunch_kv = bunch_of(ceil_div(p.kv_blocks, d->kv_heads * std::max<int64_t>(1, d->batch)));
         const auto as = [](Rows like, const void *at) {
             like.at = static_cast<char *>(const_cast<void *>(at));
             return like;
