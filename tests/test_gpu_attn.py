@@ -131,3 +131,10 @@ def test_arrays_on_the_device_that_reach_too_far_are_cut_off(paro):
     c.k_starts[:] = torch.tensor([1 << 30, -7, 2**31 - 1], dtype=torch.int32)
     c.forward()
     torch.cuda.synchronize()
+
+
+@pytest.mark.parametrize("sequences,heads,kv,hd", [(43, 32, 1, 16), (70, 12, 12, 8)])
+def test_many_sequences(paro, sequences, heads, kv, hd):
+    """More than an XCD takes at a time, and some left over: few key heads of many blocks, many of two."""
+    n = [(7 * b % 160, 7 * b % 160) for b in range(sequences)]
+    forward(paro, n, heads=heads, kv=kv, hd=hd, window=90, sinks=3, buckets=6)

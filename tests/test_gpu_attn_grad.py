@@ -173,3 +173,10 @@ def test_a_row_that_is_not_finite_stays_in_its_place(paro, dtype):
     for x, y in zip(got, want):
         assert torch.equal(x[c.q_at[0]:, 1].nan_to_num(7), y[c.q_at[0]:, 1].nan_to_num(7)) and torch.equal(x[c.q_at[1]:].nan_to_num(7), y[c.q_at[1]:].nan_to_num(7))
         assert torch.equal(x[c.q_at[0] + 128:c.q_at[0] + 200], y[c.q_at[0] + 128:c.q_at[0] + 200])
+
+
+@pytest.mark.parametrize("sequences,heads,kv,hd", [(43, 32, 1, 16), (70, 12, 12, 8)])
+def test_many_sequences(paro, sequences, heads, kv, hd):
+    """More than an XCD takes at a time, and some left over: few key heads of many blocks, many of two."""
+    n = [(7 * b % 160, 7 * b % 160) for b in range(sequences)]
+    backward(paro, n, heads=heads, kv=kv, hd=hd, window=90, sinks=3, buckets=6)
