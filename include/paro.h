@@ -420,7 +420,8 @@ int paro_gated_grad(const paro_gated_t *d, const void *dh, const void *gate, con
  * keys read that lie between the sinks and the first window of 128 queries; what is not finite there is of no account.  A key that some query of its tile sees is read:
  * what is not finite in it spreads to the results of those that see it, and may spread to others of the tile (up to 128 queries and 64 keys).
  * For more than 16 queries (len_q) and for the gradient: an array whose distances and head_dim are multiples of 8 is 16-byte aligned; the rows of others are copied into the
- * workspace (k and v; for the gradient q and dout too).  scale is in [1e-18, 1e18]; batch * heads * len at most 2^34.
+ * workspace (k and v; for the gradient q and dout too).  scale is in [1e-18, 1e18]; batch * heads * len at most 2^34,
+ * less where that is more than 2^32 threads in a launch (PARO_ERANGE).
  * Bias: bucket(d) is the last b with first[b] <= d, first: DEVICE int32 [buckets], ascending from 0 (paro_rel_buckets); table: [buckets][heads] of table_dtype, dtype or
  * PARO_F32.  A bias of -inf hides; a row of a type's lowest number is one like others.  buckets == 0: none, table and first are not looked at.
  * stats: NULL, or fp32 [rows_q][heads][2] = the largest score and the log of the sum of exp(score - largest); -inf and 0 where no key is seen. */

@@ -599,7 +599,8 @@ int paro_attn(const paro_attn_t *d, const void *q, const void *k, const void *v,
         if ((rc = check_inputs(f, *d, q, k, v, q_starts, k_starts, k_lens, table, first)) || (rc = check_array(out, 2, f + "out"))) return rc;
         if (stats && (rc = check_array(stats, 4, f + "stats"))) return rc;
         const Plan p = plan_of(*d);
-        if ((rc = check_room(f, p.bytes, workspace, workspace_bytes))) return rc;
+        const int threads = p.few ? 64 * few_waves(d->head_dim <= 64 ? 64 : 128, p.tiles_of_rows) : 256;
+        if ((rc = check_room(f, p.bytes, workspace, workspace_bytes)) || (rc = check_launch(f, p.blocks, threads))) return rc;
         Attn a = attn_of(*d, q, k, v, q_starts, k_starts, k_lens, table, first);
         a.out.at = static_cast<char *>(out);
         a.stats = stats;
@@ -612,6 +613,7 @@ int paro_attn(const paro_attn_t *d, const void *q, const void *k, const void *v,
             Copying copying(ws, 0);
             a.copied_k = copying.take(*d, a.keys, d->len_k, d->kv_heads, true);
             a.copied_v = copying.take(*d, a.values, d->len_k, d->kv_heads, true);
+            if ((rc = check_launch(f, copying.blocks(a), 256))) return rc;
             copying.launch(a, st);
         }
 #define PARO_FORWARD(DT, HD, BIAS) launch<DT, HD, BIAS>(a, p, ws, st)

@@ -435,6 +435,10 @@ inline int check_room(const std::string &f, int64_t needed, const void *workspac
     if (rc) return rc;
     return bytes < needed ? fail(PARO_ERANGE, f + "the workspace is smaller than paro_attn_workspace says") : PARO_OK;
 }
+// A launch counts its threads in 32 bits.
+inline int check_launch(const std::string &f, int64_t blocks, int64_t threads) {
+    return blocks * threads > UINT32_MAX ? fail(PARO_ERANGE, f + "more sequences, heads and tokens than a launch takes") : PARO_OK;
+}
 // Rows that lie on 16 bytes and heads of whole pieces: what goes past the registers.
 inline bool fills_take(int64_t ld, int64_t head, int64_t hd) { return hd % 8 == 0 && ld % 8 == 0 && head % 8 == 0; }
 inline int64_t copy_bytes(const paro_attn_t &d, int64_t len, int64_t heads) { return ceil_div(d.batch * len * heads * ceil_div(d.head_dim, 8) * 16, 256) * 256; }
@@ -461,9 +465,10 @@ struct Copying {
         most = std::max(most, len);
         return true;
     }
+    int64_t blocks(const Attn &a) const { return ceil_div(most, ALIGN_ROWS) * a.batch; }
     void launch(const Attn &a, hipStream_t st) const {
         if (arrays && most && a.batch)
-            hipLaunchKernelGGL(k_align, dim3((unsigned)(ceil_div(most, ALIGN_ROWS) * a.batch), (unsigned)arrays), dim3(256), 0, st, a, c);
+            hipLaunchKernelGGL(k_align, dim3((unsigned)blocks(a), (unsigned)arrays), dim3(256), 0, st, a, c);
     }
 };
 inline Attn attn_of(const paro_attn_t &d, const void *q, const void *k, const void *v, const int32_t *q_starts, const int32_t *k_starts, const int32_t *k_lens,

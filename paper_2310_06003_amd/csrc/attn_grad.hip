@@ -870,6 +870,9 @@ int paro_attn_grad(const paro_attn_t *d, const void *dout, const void *q, const 
         g.copied_o = copying.take(*d, g.douts, d->len_q, d->heads, false);
         g.a.copied_k = copying.take(*d, g.a.keys, d->len_k, d->kv_heads, true);
         g.a.copied_v = copying.take(*d, g.a.values, d->len_k, d->kv_heads, true);
+        if ((rc = check_launch(f, copying.blocks(g.a), 256)) || (rc = check_launch(f, (int64_t)p.blocks_q + p.blocks_v, 256)) ||
+            (rc = check_launch(f, p.kv_blocks + 8 + (int64_t)p.tiles * d->heads * d->batch, 256)))
+            return rc;
         copying.launch(g.a, st);
 #define PARO_BACKWARD(DT, HD, BIAS) launch<DT, HD, BIAS>(g, p, st)
         PARO_BY_FORM(PARO_BACKWARD);

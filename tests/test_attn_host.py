@@ -67,6 +67,16 @@ def test_refuses_pointers():
     assert paro._lib.paro_attn_grad(None, *[P] * 16, 0, 0) == paro.PARO_EINVAL
 
 
+def test_refuses_more_than_a_launch_takes():
+    """Launches count their threads in 32 bits."""
+    room = 2**62
+    for change in (dict(batch=2**17, heads=256, kv_heads=256, head_dim=8, len_q=60, len_k=60), dict(batch=2**17, heads=128, kv_heads=128, head_dim=8, len_q=1, len_k=60),
+                   dict(batch=2**20, heads=1, kv_heads=1, head_dim=9, len_q=1000, len_k=1000)):
+        d = paro.make_attn(**{**ATTN, "buckets": 0, **change})
+        refused(lambda: paro.paro_attn(d, P, P, P, 0, 0, 0, 0, 0, P, P, P, room), paro.PARO_ERANGE, "a launch")
+        refused(lambda: paro.paro_attn_grad(d, P, P, P, P, P, P, 0, 0, 0, 0, 0, P, P, P, 0, P, room), paro.PARO_ERANGE, "a launch")
+
+
 def test_rows_on_sixteen_bytes_lie_there():
     """Where a head and its distances are whole pieces, the arrays that go to shared memory as they are lie on 16 bytes; others are copied."""
     d = paro.make_attn(**{**ATTN, "buckets": 0})
