@@ -53,7 +53,8 @@ __device__ __forceinline__ float sum_of_halves(float x) {
 // in its L2, and units go to the XCDs in turn, so that sequences of different lengths even out (runs of a sequence each: packed sequences of 1024 to 2048 tokens
 // forward 295 us, so 220); what is left over in the end is shared by all.  An XCD takes its units a bunch at a time, the longest blocks of all of them first, `together`
 // (the heads that read a key head) side by side.  (Unit by unit: 8 x 1024 tokens of 12 heads of 64 forward 44 us, so 36, backward 137, so 108; 8192 of 32 heads of 128
-// 446 and 1820, so 430 and 1755.  All units at once: 32 x 2048 tokens of 32 heads with a window of 512 forward 1283, as their keys do not fit the L2, so 890.  Heads apart: packed sequences 235.)
+// 446 and 1820, so 430 and 1755.  All units at once: 32 x 2048 tokens of 32 heads with a window of 512 forward 1283, as their keys do not fit the
+// L2, so 890.  Heads apart: packed sequences 235, so 213.)
 struct Work {
     int unit, within;
     __device__ __forceinline__ Work(unsigned block, unsigned units, unsigned of_unit, unsigned bunch, unsigned together) {
@@ -178,7 +179,7 @@ struct Tile {
 };
 
 // Eight elements of a head's row, from `column` on; what lies behind the head: zeros.  One load without a branch: a piece that reaches past the head's end is read
-// from eight elements in front of that, and shifted.  (With branches for each element 1999 tokens of 10 heads of 77 took 78 us forward, so 47.)
+// from eight elements in front of that, and shifted.  (With branches for each element 1999 tokens of 10 heads of 77 took 78 us forward, so 44.)
 // The row has to exist also where the piece is not wanted.
 __device__ __forceinline__ int column_of(int column, int hd) { return column < hd - 8 ? column : hd - 8; }
 __device__ __forceinline__ u32x4 shifted(u32x4 v, int elements) {          // towards the first, by 0 to 7
@@ -225,10 +226,10 @@ __device__ __forceinline__ unsigned both(float a, float b) {
 }
 
 // A tile of rows on its way from memory to shared memory: 16 bytes a lane to `to` + 16 * lane, past the registers; lanes without a piece are sent NOWHERE, where the
-// hardware reads zeros.  Rows have to lie on 16 bytes.  (Through registers 8192 tokens of 32 heads of 128 took 520 us forward, so 457.)  In assembly because the compiler, which cannot tell the tiles apart, would wait for it before every read
-// of shared memory; arrived() waits.  It writes no register; m0, which holds the place in shared memory, is an operand.  Five wait states have to stand between a
-// vector instruction that writes a scalar register (v_readlane, where the compiler has kept the descriptor in a lane) and its use by a load, one between a write of m0
-// and its use; inside the assembly the compiler does not see to it.
+// hardware reads zeros.  Rows have to lie on 16 bytes.  (Through registers, when it came in: 8192 tokens of 32 heads of 128 forward 520 us, so 457.)  In assembly because the
+// compiler, which cannot tell the tiles apart, would wait for it before every read of shared memory; arrived() waits.  It writes no register; m0, which holds the place in
+// shared memory, is an operand.  Five wait states have to stand between a vector instruction that writes a scalar register (v_readlane, where the compiler has kept
+// the descriptor in a lane) and its use by a load, one between a write of m0 and its use; inside the assembly the compiler does not see to it.
 typedef __attribute__((address_space(3))) char lds_char;
 template <int AT>
 __device__ __forceinline__ void fill(u32x4 from, unsigned offset, unsigned to) {
@@ -296,7 +297,7 @@ __device__ __forceinline__ float table_value(const Attn &a, int bucket, int head
 }
 // A head's bias in shared memory.  Where the last bucket begins within NEAR (far_from), its values are there for every distance from -EDGE to far_from + EDGE, so that a
 // tile reads them wherever it lies; otherwise each tile has a window of EDGE distances of its own looked up.  (Windows always, each a search of five steps: 8 x 1024
-// tokens of 12 heads of 64 forward 46 us.)
+// tokens of 12 heads of 64 forward 46 us, so 40.)
 constexpr int NEAR = 1024, EDGE = 160;
 struct Bias {
     int first[MAX_BUCKETS];
@@ -349,7 +350,8 @@ struct Distances {                      // what a thread holds of it
 };
 
 // ---------------------------------------------------------------- rows off 16 bytes
-// Copies of the sequences' rows, heads side by side, each in whole pieces (zeros behind its end): sequence b from row b len on.
+// Copies of the sequences' rows, heads side by side, each in whole pieces (zeros behind its end): sequence b from row b len on.  (3 x 1999 tokens, 10 heads of 77 over 5: 12 us
+// for 43 MiB of four arrays.  Each block through its registers, when it came in: 340 us backward, so 240.)
 constexpr int ALIGN_ROWS = 8;
 struct Copies {
     Rows from[4];
