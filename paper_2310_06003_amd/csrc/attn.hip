@@ -16,25 +16,45 @@
 namespace {
 
 constexpr int QUERIES = 128, KEYS = 32;      // of a block, of a tile
+constexpr int MOST_SHARES = 256;
 constexpr float GROWS = 8.0f;                // powers of two that a row's shares may exceed one by
 template <int DT>
 constexpr float SHIFT = DT == PARO_F16 ? 7.0f : 0.0f;
 
-template <int DT, int HD, bool BIAS>
-__global__ __launch_bounds__(256, 2) void k_attend(Attn a) {
+struct Few {                              // of blocks that share a tile's keys, whose sums k_attend_join adds
+    int shares, row_tiles;                // row_tiles: of a sequence's key head
+    float *sums, *stats;                  // of a share: [block][ROWS][HD], and [block][ROWS][2]: largest score, sum
+};
+
+// SHARED: the block has one share of its tile's keys.  (Unshared: 64 tokens over 100000 keys, 8 key heads of 128, 1750 us, so 220; 8192 tokens of one head of 64 117, so 39; 2048 of
+// four 35, so 30.)
+template <int DT, int HD, bool BIAS, bool SHARED>
+__global__ __launch_bounds__(256, 2) void k_attend(Attn a, Few f) {
     using T = Tile<HD>;
     constexpr int BYTES = KEYS * T::ROW, STEPS = HD / 16, RING = 4;
     __shared__ __attribute__((aligned(1024))) char tiles[RING][2][BYTES];    // [part of the ring][keys, values]
     __shared__ Bias bias;
     const int group = a.heads / a.kv_heads;
-    const Work work(blockIdx.x, a.batch * a.kv_heads, a.tiles * group, a.bunch, group);
-    const int kv = work.unit % a.kv_heads, b = work.unit / a.kv_heads, head = kv * group + work.within % group;
-    const int i0 = (a.tiles - 1 - work.within / group) * QUERIES;                      // the longest first
+    int unit_of, tile_of, of_group, share = 0;
+    if constexpr (SHARED) {                // shares of the same keys stay on one XCD where there are eight, or a multiple
+        const int block = blockIdx.x / f.shares;
+        share = blockIdx.x % f.shares;
+        unit_of = block / f.row_tiles;
+        tile_of = block % f.row_tiles / group;
+        of_group = block % f.row_tiles % group;
+    } else {
+        const Work work(blockIdx.x, a.batch * a.kv_heads, a.tiles * group, a.bunch, group);
+        unit_of = work.unit;
+        tile_of = a.tiles - 1 - work.within / group;                                   // the longest first
+        of_group = work.within % group;
+    }
+    const int kv = unit_of % a.kv_heads, b = unit_of / a.kv_heads, head = kv * group + of_group, i0 = tile_of * QUERIES;
     const Sequence seq(a, b);
     if (i0 >= seq.nq) return;
     const int lane = threadIdx.x & 63, w = wave_of(), h = lane >> 5;
     const int off = seq.nk - seq.nq, first = i0 + off, last = (i0 + QUERIES < seq.nq ? i0 + QUERIES : seq.nq) - 1 + off;
     const Seen<KEYS> seen(a, first, last);
+    const int from_tile = SHARED ? (int)((int64_t)seen.tiles * share / f.shares) : 0, to_tile = SHARED ? (int)((int64_t)seen.tiles * (share + 1) / f.shares) : seen.tiles;
     const int of_wave = first + w * 32, place = of_wave + (lane & 31), i = i0 + w * 32 + (lane & 31);     // of the lane's query
 
     const int64_t row_k = a.copied_k ? (int64_t)b * a.len_k : seq.k0, row_v = a.copied_v ? (int64_t)b * a.len_k : seq.k0;
@@ -159,9 +179,9 @@ __global__ __launch_bounds__(256, 2) void k_attend(Attn a) {
     };
     const auto step = [&](auto part_, int t) __attribute__((always_inline)) {
         constexpr int part = part_, after = (part + 1) % RING, third = (part + 3) % RING;
-        const bool sees_next = t + 1 < seen.tiles && !none(seen.tile(t + 1) * KEYS);
+        const bool sees_next = t + 1 < to_tile && !none(seen.tile(t + 1) * KEYS);
         products(part_, !none(seen.tile(t) * KEYS), sees_next, [&]() __attribute__((always_inline)) {
-            if (t + 3 < seen.tiles) fill(t + 3, third);
+            if (t + 3 < to_tile) fill(t + 3, third);
             else fill_none(third);
         });
         if (sees_next) finish(scores[after & 1], far[after & 1], seen.tile(t + 1) * KEYS, after);
@@ -182,19 +202,20 @@ __global__ __launch_bounds__(256, 2) void k_attend(Attn a) {
     constexpr std::integral_constant<int, 1> p1{};
     constexpr std::integral_constant<int, 2> p2{};
     constexpr std::integral_constant<int, 3> p3{};
-    if (seen.tiles) {
+    if (from_tile < to_tile) {
         int plain_from, plain_to;
         seen.plain(a, first, last, plain_from, plain_to);
+        if (SHARED && plain_to > to_tile) plain_to = to_tile;
         for (int t = 0; t < 3; ++t) {
-            if (t < seen.tiles) fill(t, t);
+            if (from_tile + t < to_tile) fill(from_tile + t, t);
             else fill_none(t);
         }
         arrived<2 * FILLS>();
         scores[0] = f32x16{};
 #pragma unroll
         for (int c = 0; c < STEPS; ++c) scores[0] = mfma32<DT>(T::rows(tiles[0][0], 0, c, lane), q[c], scores[0]);
-        finish(scores[0], far[0], seen.tile(0) * KEYS, 0);
-        for (int t = 0;;) {
+        finish(scores[0], far[0], seen.tile(from_tile) * KEYS, 0);
+        for (int t = from_tile;;) {
             if (t >= plain_from && t + 6 < plain_to) {
                 int k0 = seen.tile(t) * KEYS;
                 const char *k_at = keys_at + (seen.tile(t) + 3) * k_step, *v_at = values_at + (seen.tile(t) + 3) * v_step;
@@ -206,17 +227,31 @@ __global__ __launch_bounds__(256, 2) void k_attend(Attn a) {
                 }
             }
             step(p0, t);
-            if (++t == seen.tiles) break;
+            if (++t == to_tile) break;
             step(p1, t);
-            if (++t == seen.tiles) break;
+            if (++t == to_tile) break;
             step(p2, t);
-            if (++t == seen.tiles) break;
+            if (++t == to_tile) break;
             step(p3, t);
-            if (++t == seen.tiles) break;
+            if (++t == to_tile) break;
         }
         arrived<0>();                       // nothing is on its way into the shared memory of the block that comes next
     }
     sum = sum_of_halves(sum);
+    if constexpr (SHARED) {
+        const float times = most > -INFINITY ? exp2_((used - most) * unit) : 1.0f;
+        const int64_t row = (int64_t)blockIdx.x * QUERIES + w * 32 + (lane & 31);
+#pragma unroll
+        for (int d = 0; d < HD / 32; ++d)
+#pragma unroll
+            for (int e = 0; e < 16; e += 4)
+                *reinterpret_cast<f32x4 *>(f.sums + row * HD + d * 32 + 2 * e + 4 * h) = f32x4{out[d][e], out[d][e + 1], out[d][e + 2], out[d][e + 3]} * times;
+        if (h == 0) {
+            f.stats[row * 2] = most;
+            f.stats[row * 2 + 1] = sum * times;
+        }
+        return;
+    }
     const bool there = i < seq.nq;
     const float times = sum > 0.0f ? 1.0f / sum : sum == 0.0f ? 0.0f : sum;       // NaN stays
     char *const to = a.out.of((int64_t)seq.q0 + i, head);
@@ -234,15 +269,10 @@ __global__ __launch_bounds__(256, 2) void k_attend(Attn a) {
 // Up to 16 queries a sequence: the keys and values are read once for all queries and heads that share them, and nothing else counts.  A block's waves take 32 keys
 // at a time in turn: keys straight into registers as operands, values through shared memory of the wave's own, to be transposed.  The rows of
 // the products are the heads of a group, query by query, ROWS in all.  Long sequences are shared out among blocks, whose sums k_attend_join adds.
-constexpr int FEW = 16, FEW_KEYS = 32, MOST_SHARES = 256;
+constexpr int FEW = 16, FEW_KEYS = 32;
 // Waves of a block: eight fill a compute unit's memory pipes without a second launch (four a block and twice the blocks, joined: 32 sequences with a window of 1024,
 // 8 key heads of 128, 36 us); wide heads with 32 rows leave registers for four.
 constexpr int few_waves(int hd, int nt) { return hd == 128 && nt == 2 ? 4 : 8; }
-
-struct Few {
-    int shares, row_tiles;
-    float *sums, *stats;              // of a share: [block][ROWS][HD], and [block][ROWS][2]: largest score in powers of two, sum
-};
 
 __device__ __forceinline__ float max_of_quads(float x) {
     const auto both = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
@@ -494,9 +524,11 @@ __global__ __launch_bounds__(256) void k_attend_join(Attn a, Few f) {
     const int r = (int)(work % ROWS), row_tile = (int)(work / ROWS % f.row_tiles);
     const int64_t of_kv = work / ROWS / f.row_tiles;
     const int kv = (int)(of_kv % a.kv_heads), group = a.heads / a.kv_heads, of_rows = row_tile * ROWS + r;
+    // k_attend's rows are a head's tokens, k_attend_few's a token's heads
+    const int token = ROWS == QUERIES ? row_tile / group * QUERIES + r : of_rows / group, head = kv * group + (ROWS == QUERIES ? row_tile : of_rows) % group;
     if (of_kv / a.kv_heads >= a.batch) return;
     const Sequence seq(a, (int)(of_kv / a.kv_heads));
-    if (of_rows >= seq.nq * group) return;
+    if (token >= seq.nq) return;
     const float unit = BIAS ? LOG2E : a.scale * LOG2E;
     const int64_t block = (of_kv * f.row_tiles + row_tile) * f.shares;
     const float *const stats = f.stats + (block * ROWS + r) * 2, *const sums = f.sums + (block * ROWS + r) * HD + lane * EACH;
@@ -526,8 +558,7 @@ __global__ __launch_bounds__(256) void k_attend_join(Attn a, Few f) {
         }
     }
     const float times = sum > 0.0f ? 1.0f / sum : sum;
-    const int head = kv * group + of_rows % group;
-    const int64_t row = (int64_t)seq.q0 + of_rows / group;
+    const int64_t row = (int64_t)seq.q0 + token;
 #pragma unroll
     for (int e = 0; e < EACH; ++e)
         if (lane * EACH + e < a.hd) store_one<DT>(a.out.of(row, head), lane * EACH + e, out[e] * times);
@@ -537,8 +568,8 @@ __global__ __launch_bounds__(256) void k_attend_join(Attn a, Few f) {
 // ---------------------------------------------------------------- host
 struct Plan {
     bool few;
-    int tiles_of_rows, row_tiles, shares;            // few: 16-row tiles of a block, row tiles, shares
-    int64_t blocks, stats, bytes;
+    int tiles_of_rows, row_tiles, shares;            // few: 16-row tiles of a block; row tiles of a key head; shares of the keys
+    int64_t blocks, sums, stats, bytes;
 };
 
 Plan plan_of(const paro_attn_t &d) {
@@ -552,6 +583,17 @@ Plan plan_of(const paro_attn_t &d) {
         };
         copy(d.ld_k, d.head_k);
         copy(d.ld_v, d.head_v);
+        // Shares of 1024 keys and more, for two blocks a compute unit; by eights, where there are as many.
+        const int64_t span = d.window ? std::min<int64_t>(d.len_k, std::min<int64_t>(d.window, d.len_k) + QUERIES + std::min<int64_t>(d.sinks, d.len_k)) : d.len_k;
+        p.shares = (int)std::max<int64_t>(1, std::min<int64_t>(std::min<int64_t>(512 / std::max<int64_t>(1, p.blocks), span / (32 * KEYS)), MOST_SHARES));
+        if (p.shares > 8) p.shares = p.shares / 8 * 8;
+        p.row_tiles = (int)(ceil_div(d.len_q, QUERIES) * group);
+        p.blocks *= p.shares;
+        if (p.shares > 1) {
+            p.sums = p.bytes;
+            p.stats = p.sums + p.blocks * QUERIES * (d.head_dim <= 64 ? 64 : 128) * 4;
+            p.bytes = p.stats + p.blocks * QUERIES * 8;
+        }
         return p;
     }
     const int64_t rows = std::max<int64_t>(1, d.len_q * group), head_dim = d.head_dim <= 64 ? 64 : 128;
@@ -573,11 +615,16 @@ Plan plan_of(const paro_attn_t &d) {
 
 template <int DT, int HD, bool BIAS>
 void launch(const Attn &a, const Plan &p, char *workspace, hipStream_t st) {
+    const Few f{p.shares, p.row_tiles, reinterpret_cast<float *>(workspace + p.sums), reinterpret_cast<float *>(workspace + p.stats)};
     if (!p.few) {
-        hipLaunchKernelGGL((k_attend<DT, HD, BIAS>), dim3((unsigned)p.blocks), dim3(256), 0, st, a);
+        if (p.shares > 1) {
+            hipLaunchKernelGGL((k_attend<DT, HD, BIAS, true>), dim3((unsigned)p.blocks), dim3(256), 0, st, a, f);
+            hipLaunchKernelGGL((k_attend_join<DT, HD, BIAS, QUERIES / 16>), dim3((unsigned)(p.blocks / p.shares * (QUERIES / 4))), dim3(256), 0, st, a, f);
+        } else {
+            hipLaunchKernelGGL((k_attend<DT, HD, BIAS, false>), dim3((unsigned)p.blocks), dim3(256), 0, st, a, f);
+        }
         return;
     }
-    const Few f{p.shares, p.row_tiles, reinterpret_cast<float *>(workspace), reinterpret_cast<float *>(workspace + p.stats)};
     const unsigned joins = (unsigned)(p.blocks / p.shares * 4 * p.tiles_of_rows);
     if (p.tiles_of_rows == 1) {
         hipLaunchKernelGGL((k_attend_few<DT, HD, BIAS, 1>), dim3((unsigned)p.blocks), dim3(64 * few_waves(HD, 1)), 0, st, a, f);

@@ -59,7 +59,7 @@ def names(got):
     return [x.kernel for x in got]
 
 
-@pytest.mark.parametrize("n,kernel", [(1, "k_attend_few"), (16, "k_attend_few"), (17, "k_attend"), (5000, "k_attend")])
+@pytest.mark.parametrize("n,kernel", [(1, "k_attend_few"), (16, "k_attend_few"), (17, "k_attend"), (2047, "k_attend")])
 def test_few_queries_and_many(launches, n, kernel):
     assert names(launches("attn", n=n)) == [kernel]
 
@@ -77,6 +77,15 @@ def test_shares_of_long_caches(launches, size, shares):
     got = launches("attn", n=1, **size)
     whole = size.get("batch", 1) * (size.get("kv") or size["heads"])
     assert got[0].x == whole * shares and names(got) == ["k_attend_few"] + ["k_attend_join"] * (shares > 1)
+
+
+@pytest.mark.parametrize("size,blocks,shares", [(dict(n=64, m=5000), 2, 4), (dict(n=17, m=20500, batch=5, heads=3, kv=1), 15, 16), (dict(n=33, m=9000, batch=2, heads=4, kv=2, window=5001, sinks=40), 8, 5),
+                                                (dict(n=2200, heads=1), 18, 2), (dict(n=64, m=100000, heads=32, kv=8, hd=128), 32, 16), (dict(n=64, m=2047), 2, 1),
+                                                (dict(n=64, m=100000, window=1024, sinks=4), 2, 1), (dict(n=4096, m=4096, heads=12), 384, 1), (dict(n=8192, heads=4, hd=128), 256, 2)])
+def test_shares_of_keys(launches, size, blocks, shares):
+    got = launches("attn", **size)
+    assert got[0].x == blocks * shares and names(got) == ["k_attend"] + ["k_attend_join"] * (shares > 1)
+    assert shares == 1 or got[1].x == blocks * 32
 
 
 @pytest.mark.parametrize("change,arrays", [({}, 0), (dict(pad=8), 0), (dict(pad=4), 2), (dict(hd=72), 0), (dict(hd=70), 2)])

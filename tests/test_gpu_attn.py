@@ -138,3 +138,12 @@ def test_many_sequences(paro, sequences, heads, kv, hd):
     """More than an XCD takes at a time, and some left over: few key heads of many blocks, many of two."""
     n = [(7 * b % 160, 7 * b % 160) for b in range(sequences)]
     forward(paro, n, heads=heads, kv=kv, hd=hd, window=90, sinks=3, buckets=6)
+
+
+@pytest.mark.parametrize("hd,dtype,buckets", [(64, "bf16", 0), (128, "f16", 0), (40, "f16", 9), (128, "bf16", 32), (77, "bf16", 0)])
+def test_keys_shared_among_blocks(paro, hd, dtype, buckets):
+    """More than 16 queries over many keys, in fewer blocks than the chip has room for: a few shares, by eights, shares of nothing, sequences of few keys or none."""
+    forward(paro, [(64, 5000)], hd=hd, dtype=dtype, buckets=buckets, far=128)
+    forward(paro, [(17, 20500), (150, 3000), (40, 10), (30, 0), (0, 50)], heads=3, kv=1, hd=hd, dtype=dtype, buckets=buckets, pad=3, stats=False)
+    forward(paro, [(33, 9000), (20, 70)], heads=4, kv=2, hd=hd, dtype=dtype, buckets=buckets, window=5001, sinks=40, use_lens=True)
+    forward(paro, [(2200, 2200)], heads=1, hd=hd, dtype=dtype, buckets=buckets)
