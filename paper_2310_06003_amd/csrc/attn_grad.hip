@@ -755,7 +755,8 @@ Plan plan_of(const paro_attn_t &d) {
     p.sink_shares = p.shares;
     if (p.sink_tiles) {
         const int64_t most = std::min<int64_t>(MOST_SHARES, std::max<int64_t>(p.shares, 1024 / (p.sink_tiles * d.kv_heads * d.batch)));
-        p.sink_shares = (int)std::min<int64_t>(p.shares * ceil_div(d.len_q, std::max<int64_t>(1, others)), most);
+        // (no query, one share: a tile's block writes its zeros)
+        p.sink_shares = (int)std::min<int64_t>(p.shares * std::max<int64_t>(1, ceil_div(d.len_q, std::max<int64_t>(1, others))), most);
     }
     const int64_t per_kv = (int64_t)p.sink_tiles * p.sink_shares + (int64_t)(p.key_tiles - p.sink_tiles) * p.shares;
     p.slots = p.shares > 1 ? (int)per_kv : p.sink_shares > 1 ? p.sink_tiles * p.sink_shares : 0;
