@@ -787,6 +787,11 @@ Plan plan_of(const paro_attn_t &d) {
     return p;
 }
 
+void launch_table_grad(const Grad &g, int dtype, hipStream_t st) {
+    if (dtype == PARO_F16) hipLaunchKernelGGL((k_table_grad<PARO_F16>), dim3((unsigned)g.a.heads), dim3(256), 0, st, g);
+    else hipLaunchKernelGGL((k_table_grad<PARO_BF16>), dim3((unsigned)g.a.heads), dim3(256), 0, st, g);
+}
+
 template <int DT, int HD, bool BIAS>
 void launch(const Grad &g, const Plan &p, hipStream_t st) {
     if (p.blocks_q + p.blocks_v) hipLaunchKernelGGL((k_dots<DT, HD>), dim3((unsigned)(p.blocks_q + p.blocks_v), (unsigned)p.blocks_heads), dim3(256), 0, st, g);
@@ -795,7 +800,7 @@ void launch(const Grad &g, const Plan &p, hipStream_t st) {
     if (of_kv + of_q) hipLaunchKernelGGL((k_grads<DT, HD, BIAS>), dim3((unsigned)(of_kv + of_q)), dim3(256), 0, st, g, (unsigned)of_kv);
     const int joined = p.shares > 1 ? p.key_tiles : p.sink_shares > 1 ? p.sink_tiles : 0;
     if (joined) hipLaunchKernelGGL((k_grad_join<DT, HD>), dim3((unsigned)(joined * g.a.kv_heads * g.a.batch), BLOCK / (1024 / HD), 2), dim3(256), 0, st, g);
-    if (BIAS && g.dtable) hipLaunchKernelGGL((k_table_grad<DT>), dim3((unsigned)g.a.heads), dim3(256), 0, st, g);
+    if (BIAS && g.dtable) launch_table_grad(g, DT, st);
 }
 
 }  // namespace
@@ -826,6 +831,15 @@ int paro_attn_grad(const paro_attn_t *d, const void *dout, const void *q, const 
         if (d->batch && (rc = check_inputs(f, *d, q, k, v, q_starts, k_starts, k_lens, table, first))) return rc;
         if (d->batch && d->len_k && ((rc = check_array(dk, 2, f + "dk")) || (rc = check_array(dv, 2, f + "dv")))) return rc;
         if (d->buckets && dtable && (rc = check_array(dtable, size_of(d->table_dtype), f + "dtable"))) return rc;
+        hipStream_t st = static_cast<hipStream_t>(stream);
+        if (d->batch == 0) {                     // of a table that nothing has looked at: zeros
+            Grad none{};
+            none.a = attn_of(*d, q, k, v, q_starts, k_starts, k_lens, table, first);
+            none.dtable = static_cast<char *>(dtable);
+            launch_table_grad(none, d->dtype, st);
+            PARO_LAUNCHED("paro_attn_grad");
+            return PARO_OK;
+        }
         const Plan p = plan_of(*d);
         if ((rc = check_room(f, p.bytes, workspace, workspace_bytes))) return rc;
         char *ws = static_cast<char *>(workspace);
@@ -836,7 +850,7 @@ int paro_attn_grad(const paro_attn_t *d, const void *dout, const void *q, const 
         g.a.stats = const_cast<float *>(stats);
         g.a.tiles = p.tiles;
         g.a.bunch = bunch_of(p.tiles * (d->heads / d->kv_heads));
-        g.bunch_kv = bunch_of(ceil_div(p.kv_blocks, d->kv_heads * std::max<int64_t>(1, d->batch)));
+        g.bunch_kv = bunch_of(ceil_div(p.kv_blocks, d->kv_heads * d->batch));
         const auto as = [](Rows like, const void *at) {
             like.at = static_cast<char *>(const_cast<void *>(at));
             return like;
@@ -862,7 +876,6 @@ int paro_attn_grad(const paro_attn_t *d, const void *dout, const void *q, const 
         g.shares = p.shares;
         g.sink_shares = p.sink_shares;
         g.slots = p.slots;
-        hipStream_t st = static_cast<hipStream_t>(stream);
         if ((rc = check_aligned(f, g.a.q, g.a.hd, "q")) || (rc = check_aligned(f, g.dout, g.a.hd, "dout")) || (rc = check_aligned(f, g.a.k, g.a.hd, "k")) ||
             (rc = check_aligned(f, g.a.v, g.a.hd, "v")))
             return rc;

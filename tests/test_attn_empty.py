@@ -72,3 +72,14 @@ def test_keys_without_queries_have_gradients(launches, m, window, sinks, dtype):
     got = launches("grad", batch=3, n=0, m=m, window=window, sinks=sinks, dtype=dtype)
     blocks = [x.x for x in got if x.kernel == "k_grads"]
     assert len(blocks) == 1 and blocks[0] >= 3 * 2 * -(-m // 128)
+
+
+@pytest.mark.parametrize("dtype", [BF16, F16])
+@pytest.mark.parametrize("hd,m,window,sinks", [(64, 100, 0, 0), (128, 5000, 0, 0), (64, 300, 10, 4), (128, 5000, 200, 300)])
+def test_no_sequence_leaves_a_table_without_gradient(launches, hd, m, window, sinks, dtype):
+    """batch 0: no array but the table's gradient is needed, nor a workspace; its zeros are one launch."""
+    for n in (0, 1, 300):
+        got = launches("grad", batch=0, hd=hd, n=n, m=m, window=window, sinks=sinks, buckets=9, dtype=dtype, given=["dtable"])
+        assert [(x.kernel, x.x) for x in got] == [("k_table_grad", 2)]
+        assert launches("grad", batch=0, hd=hd, n=n, m=m, window=window, sinks=sinks, buckets=9, dtype=dtype, given=[]) == []
+        assert launches("grad", batch=0, hd=hd, n=n, m=m, window=window, sinks=sinks, dtype=dtype, given=["dtable"]) == []      # of no bucket

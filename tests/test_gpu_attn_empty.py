@@ -1,6 +1,8 @@
 """Attention and its gradient where there are no queries, no keys or no sequences, against the definition: what is there is written, nothing else."""
 import pytest
+import torch
 
+from operators_ref import DEV, TORCH, code, stream
 from test_gpu_attn_grad import backward
 
 pytestmark = pytest.mark.gpu
@@ -18,3 +20,27 @@ def test_keys_without_queries(paro, window, sinks, buckets, dtype):
 
 def test_sequences_without_queries_among_others(paro):
     backward(paro, [(0, 300), (200, 300), (0, 5), (40, 40)], heads=4, kv=2, window=30, sinks=5, buckets=6, dtype="f16")
+
+
+@pytest.mark.parametrize("dtype,table", [("bf16", "f32"), ("bf16", "bf16"), ("f16", "f16")])
+def test_no_sequence_leaves_a_table_without_gradient(paro, dtype, table):
+    """batch 0, at once and in a graph: zeros, without a workspace."""
+    kinds = dict(batch=0, heads=5, head_dim=64, len_q=300, dtype=code(paro, dtype), window=10, sinks=4, buckets=7, table_dtype=code(paro, table))
+    d = paro.make_attn(**kinds)
+    assert paro.paro_attn_workspace(d, True) == 0
+    whole = torch.full((40,), 7.0, dtype=TORCH[table], device=DEV)
+
+    def check():
+        assert bool((whole[:35] == 0).all()) and bool((whole[35:] == 7).all())
+        whole[:35] = 7.0
+    paro.paro_attn_grad(d, *[0] * 14, whole.data_ptr(), 0, 0, stream())
+    check()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        paro.paro_attn_grad(d, *[0] * 14, whole.data_ptr(), 0, 0, stream())
+    for _ in range(3):
+        graph.replay()
+        check()
+    paro.paro_attn_grad(d, *[0] * 15, 0, 0, stream())                          # not wanted
+    paro.paro_attn(d, *[0] * 10, 0, 0, stream())
+    assert bool((whole == 7).all())
