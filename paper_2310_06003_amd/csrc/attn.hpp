@@ -421,7 +421,7 @@ inline int check_rows(const std::string &f, const paro_attn_t &d, const void *q_
 }
 inline int check_inputs(const std::string &f, const paro_attn_t &d, const void *q, const void *k, const void *v, const int32_t *q_starts, const int32_t *k_starts,
                         const int32_t *k_lens, const void *table, const int32_t *first) {
-    int rc = check_array(q, 2, f + "q");
+    int rc = d.len_q ? check_array(q, 2, f + "q") : PARO_OK;
     if (!rc && d.len_k) rc = check_array(k, 2, f + "k");
     if (!rc && d.len_k) rc = check_array(v, 2, f + "v");
     if (!rc && q_starts) rc = check_array(q_starts, 4, f + "q_starts");

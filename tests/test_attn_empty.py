@@ -83,3 +83,17 @@ def test_no_sequence_leaves_a_table_without_gradient(launches, hd, m, window, si
         assert [(x.kernel, x.x) for x in got] == [("k_table_grad", 2)]
         assert launches("grad", batch=0, hd=hd, n=n, m=m, window=window, sinks=sinks, buckets=9, dtype=dtype, given=[]) == []
         assert launches("grad", batch=0, hd=hd, n=n, m=m, window=window, sinks=sinks, dtype=dtype, given=["dtable"]) == []      # of no bucket
+
+
+@pytest.mark.parametrize("buckets", [0, 9])
+@pytest.mark.parametrize("window,sinks", [(0, 0), (10, 4)])
+def test_arrays_without_rows_may_be_null(launches, window, sinks, buckets):
+    """An empty tensor's address is 0: arrays of queries are not looked at where len_q is 0, arrays of keys where len_k is."""
+    of_q, of_k, more = ["dout", "q", "out", "stats", "dq"], ["k", "v", "dk", "dv"], ["workspace"] + (["table", "first", "dtable"] if buckets else [])
+    size = dict(batch=3, window=window, sinks=sinks, buckets=buckets)
+    for n, m, given in ((0, 100, of_k), (50, 0, of_q), (1, 0, of_q), (0, 0, [])):
+        kernels = [x.kernel for x in launches("grad", n=n, m=m, given=given + more, **size)]
+        assert kernels == ["k_dots"] * (n > 0) + ["k_grads"] * (n + m > 0) + ["k_table_grad"] * (buckets > 0)
+    for n, m, given in ((0, 100, []), (50, 0, ["q", "out", "stats"]), (1, 0, ["q", "out"]), (0, 0, [])):
+        kernels = [x.kernel for x in launches("attn", n=n, m=m, given=given + more, **size)]
+        assert kernels == (["k_attend" if n > 16 else "k_attend_few"] if n else [])

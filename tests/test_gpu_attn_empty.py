@@ -2,6 +2,7 @@
 import pytest
 import torch
 
+from attn_ref import Case
 from operators_ref import DEV, TORCH, code, stream
 from test_gpu_attn_grad import backward
 
@@ -44,3 +45,24 @@ def test_no_sequence_leaves_a_table_without_gradient(paro, dtype, table):
     paro.paro_attn_grad(d, *[0] * 15, 0, 0, stream())                          # not wanted
     paro.paro_attn(d, *[0] * 10, 0, 0, stream())
     assert bool((whole == 7).all())
+
+
+@pytest.mark.parametrize("hd,dtype,buckets", [(64, "bf16", 0), (128, "f16", 5), (77, "bf16", 3)])
+def test_arrays_of_no_rows_are_null(paro, hd, dtype, buckets):
+    """What an empty tensor's address is, 0, in the place of the queries' arrays, and of the keys'."""
+    empty = torch.empty(0, 4, hd, dtype=TORCH[dtype], device=DEV)
+    assert empty.data_ptr() == 0
+    c = Case(paro, [(0, 100), (0, 40)], hd=hd, heads=4, kv=2, dtype=dtype, buckets=buckets, window=10, sinks=4)
+    for x in (c.q, c.dout, c.out, c.dq):
+        x.view = empty
+    c.stats = torch.empty(0, 4, 2, device=DEV)
+    c.forward()
+    c.backward()
+    c.check_backward()
+    c = Case(paro, [(40, 0), (100, 0)], hd=hd, heads=4, kv=2, dtype=dtype, buckets=buckets, window=10, sinks=4)
+    for x in (c.k, c.v, c.dk, c.dv):
+        x.view = empty[:, :2]
+    c.forward()
+    c.check_forward()
+    c.backward()
+    c.check_backward()
