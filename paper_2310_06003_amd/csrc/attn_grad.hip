@@ -26,7 +26,7 @@ struct Grad {
     bool copied_q, copied_o;
     // [head][rows_q]: P = exp2(s * LOG2E - base); D.  Of a bias, whose largest score may be a table's lowest number: P = exp2((s - peak) * LOG2E - log_sum)
     float *base, *dots, *peak, *log_sum;
-    float *largest;                          // of fp16: the largest |dout_i|^2 and |v_j|^2 of each block of k_dots
+    float *largest;                          // of fp16: the largest |dout_i|^2 and |v_j|^2 of each block of k_dots, of rows that see each other
     float *times;                            // of fp16: what dS is multiplied by, and the inverse
     float *partial;                          // of shared key tiles: [slot][dk, dv][128][HD]
     float *of_table;                         // [head][sequence][tile of queries][bucket]
@@ -44,20 +44,19 @@ __device__ __forceinline__ float over_lanes(float x) {       // of HD / 8 lanes 
     for (int n = 1; n < HD / 8; n *= 2) x += __shfl_xor(x, n);
     return x;
 }
-// D, and what P is formed from, of 16 rows of 8 heads; blocks behind those of the queries: the values' largest row.  Reads dout and out once: 8192 tokens of 32 heads of 128
+// D, and what P is formed from, of 16 rows of 8 heads; blocks behind those of the queries: the values' largest row, of those that some query sees.  Reads dout and out once: 8192 tokens of 32 heads of 128
 // 28 us, 4.9 TB/s.
 template <int DT, int HD>
 __global__ __launch_bounds__(256) void k_dots(Grad g) {
     const Attn &a = g.a;
     constexpr int LANES = HD / 8, AT_ONCE = 256 / LANES, U = DOT_ROWS * DOT_HEADS / AT_ONCE;       // all of a block in flight
-    __shared__ float dots[DOT_HEADS][DOT_ROWS + 1];
+    __shared__ float dots[DOT_HEADS][DOT_ROWS + 1], squares[DT == PARO_F16 ? DOT_HEADS : 1][DOT_ROWS + 1];
     const bool of_values = (int)blockIdx.x >= g.blocks_q;
     const unsigned tiles = (of_values ? g.blocks_v : g.blocks_q) / a.batch, block = of_values ? blockIdx.x - g.blocks_q : blockIdx.x;
     const int b = block / tiles, row0 = block % tiles * DOT_ROWS, column = threadIdx.x % LANES * 8, head0 = blockIdx.y * DOT_HEADS;
     const Sequence seq(a, b);
-    const int heads = of_values ? a.kv_heads : a.heads, n = of_values ? seq.nk : seq.nq;
+    const int heads = of_values ? a.kv_heads : a.heads, n = !of_values ? seq.nq : seq.nq ? seq.nk : 0;
     const int rows = n - row0 < DOT_ROWS ? n - row0 : DOT_ROWS, items = rows > 0 && head0 < heads ? rows * DOT_HEADS : 0;
-    float largest = 0.0f;
     for (int x0 = threadIdx.x / LANES; x0 < items; x0 += U * AT_ONCE) {
         u32x4 u_raw[U], o_raw[U];
         int r[U], head[U];
@@ -75,25 +74,30 @@ __global__ __launch_bounds__(256) void k_dots(Grad g) {
         }
 #pragma unroll
         for (int u = 0; u < U; ++u) {
-            float x[8], o[8], dot = 0.0f, squares = 0.0f;
+            float x[8], o[8], dot = 0.0f, square = 0.0f;
             unpack<DT>(u_raw[u], x);
             unpack<DT>(o_raw[u], o);
 #pragma unroll
             for (int e = 0; e < 8; ++e) dot += x[e] * o[e];
             if constexpr (DT == PARO_F16) {
 #pragma unroll
-                for (int e = 0; e < 8; ++e) squares += x[e] * x[e];
-                squares = over_lanes<HD>(squares);
-                if (squares < INFINITY) largest = fmaxf(largest, squares);          // a row that is not finite leaves the others' scale alone
+                for (int e = 0; e < 8; ++e) square += x[e] * x[e];
+                square = over_lanes<HD>(square);
+                if (column == 0) squares[head[u] - head0][r[u]] = square;
             }
             dot = over_lanes<HD>(dot);
             if (column == 0) dots[head[u] - head0][r[u]] = dot;
         }
     }
     __syncthreads();
-    if (!of_values) {
-        const int r = threadIdx.x % DOT_ROWS, head = head0 + threadIdx.x / DOT_ROWS;
-        if (threadIdx.x < DOT_ROWS * DOT_HEADS && r < rows && head < heads) {
+    const int r = threadIdx.x % DOT_ROWS, head = head0 + threadIdx.x / DOT_ROWS;
+    float largest = 0.0f;
+    if (threadIdx.x < DOT_ROWS * DOT_HEADS && r < rows && head < heads) {
+        bool counts;                         // P is zero in rows that see no key, and for keys that no row sees
+        if (of_values) {
+            const int j = row0 + r;
+            counts = j < a.sinks || j >= seq.nk - seq.nq - a.window + 1;
+        } else {
             const float *const stats = a.stats + (((int64_t)seq.q0 + row0 + r) * a.heads + head) * 2;
             const float most = stats[0], log_sum = stats[1];
             const int64_t at = (int64_t)head * a.rows_q + seq.q0 + row0 + r;
@@ -104,6 +108,11 @@ __global__ __launch_bounds__(256) void k_dots(Grad g) {
                 g.peak[at] = empty ? INFINITY : most;
                 g.log_sum[at] = empty ? 0.0f : log_sum * LOG2E - SHIFT<DT>;
             }
+            counts = !empty;
+        }
+        if constexpr (DT == PARO_F16) {
+            const float square = squares[threadIdx.x / DOT_ROWS][r];
+            if (counts && square < INFINITY) largest = square;          // a row that is not finite leaves the others' scale alone
         }
     }
     if constexpr (DT == PARO_F16) {
