@@ -241,11 +241,11 @@ __device__ __forceinline__ void grad_kv(const Grad &g, unsigned block, SharedKv<
             from_row = left >= 0 ? x : which % 2 == 0 ? INFINITY : 0.0f;
         }
         const u32x4 q_from = fill_q.descriptor(q_at), o_from = fill_o.descriptor(o_at);
-        if (next_i0 + Q_STEP <= seq.nq) {
+        if (next_i0 + Q_STEP <= seq.nq && next_i0 >= -off) {
             fill_q.whole(q_from, tiles[buffer][0]);
             fill_o.whole(o_from, tiles[buffer][1]);
         } else {
-            const auto holds = [&](int r) { return next_i0 + r < seq.nq; };
+            const auto holds = [&](int r) { return next_i0 + r < seq.nq && next_i0 + r >= -off; };       // what stands in front of the first key is of no account
             fill_q.held(q_from, tiles[buffer][0], holds);
             fill_o.held(o_from, tiles[buffer][1], holds);
         }

@@ -62,3 +62,24 @@ def test_large_gradients_of_queries_whose_keys_are_hidden(paro):
         c.dout.view[c.q_at[0]:, 2] = value
         got.append(gradients(c))
     assert same(*got)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+@pytest.mark.parametrize("hd,pad", [(64, 0), (128, 0), (77, 3)])
+def test_queries_that_see_no_key_hold_anything(paro, hd, pad, dtype):
+    """More queries than keys: NaN and infinities in those in front of the first key stay out of every other row, and their own results are zeros."""
+    for nq, nk in ((200, 50), (161, 1), (40, 39), (300, 0)):
+        c = Case(paro, [(nq, nk), (40, 40)], hd=hd, pad=pad, heads=4, kv=2, dtype=dtype, buckets=6, window=30, sinks=2)
+        rows = slice(c.q_at[0], c.q_at[0] + nq - nk)
+        got = []
+        for value in (0.0, torch.nan, torch.inf):
+            c.q.view[rows] = value
+            c.dout.view[rows] = value
+            c.forward()
+            c.backward()
+            got.append([x.clone() for x in (c.out.whole, c.stats, c.dq.whole, c.dk.whole, c.dv.whole, c.dtable)])
+            if value == 0.0:
+                c.check_forward()
+                c.check_backward()
+        assert same(got[0], got[1]) and same(got[0], got[2])
+        assert bool((c.out.view[rows] == 0).all()) and bool((c.dq.view[rows] == 0).all())
