@@ -94,7 +94,7 @@ struct Attn {
     float scale;
 };
 
-// Where a sequence's rows lie.  Whatever the arrays on the device hold, the rows stay inside [0, rows_q) and [0, rows_k), and are no more than len_q and len_k.
+// Where a sequence's rows lie.  Whatever the arrays on the device hold, its rows are those inside [0, rows_q) and [0, rows_k), and of these the first len_q and len_k.
 struct Sequence {
     int q0, nq, k0, nk;
     __device__ __forceinline__ Sequence(const Attn &a, int b) {
@@ -102,11 +102,10 @@ struct Sequence {
         const int64_t qs = a.q_starts ? a.q_starts[b] : (int64_t)b * a.len_q, ks = a.k_starts ? a.k_starts[b] : (int64_t)b * a.len_k;
         q0 = inside(qs, a.rows_q);
         k0 = inside(ks, a.rows_k);
-        const int64_t q = a.q_starts ? a.q_starts[b + 1] - qs : a.len_q;
-        const int64_t k = a.k_lens ? a.k_lens[b] : a.k_starts ? a.k_starts[b + 1] - ks : a.len_k;
-        const int room_q = a.rows_q - q0, room_k = a.rows_k - k0;
-        nq = inside(q, a.len_q < room_q ? a.len_q : room_q);
-        nk = inside(k, a.len_k < room_k ? a.len_k : room_k);
+        const int64_t q_end = a.q_starts ? a.q_starts[b + 1] : qs + a.len_q;
+        const int64_t k_end = a.k_lens ? ks + a.k_lens[b] : a.k_starts ? a.k_starts[b + 1] : ks + a.len_k;
+        nq = inside((int64_t)inside(q_end, a.rows_q) - q0, a.len_q);
+        nk = inside((int64_t)inside(k_end, a.rows_k) - k0, a.len_k);
     }
 };
 
