@@ -97,12 +97,13 @@ __global__ __launch_bounds__(256, 2) void k_attend(Attn a, Few f) {
     for (int s = 0; s < STEPS; ++s) q[s] = __builtin_bit_cast(short8_t, piece_of_head(query, s * 16 + h * 8, a.hd, i < seq.nq));
     // Scores are in units of `unit` powers of two: as the products give them without a bias, natural ones with one.  Of a tile whose keys all have the last bucket's
     // bias (far) it is not added, but enters the largest score and the exponent as a whole.
-    const float unit = BIAS ? LOG2E : a.scale * LOG2E, grows = GROWS / unit;
+    // Where a row's largest score is large in size (a table's lowest number, or large products), differences to it are formed before they are brought to powers of two: its multiple
+    // by LOG2E is off by its size times 2^-24, a factor of more than fp16 holds from 10^7 on.
+    const float unit = BIAS ? LOG2E : a.scale * LOG2E, grows = GROWS / unit, usual = BIAS ? USUAL : USUAL / a.scale;
+    bool large = false;                    // of some row of the wave
     f32x16 out[HD / 32] = {}, scores[2];
     bool far[2] = {};
     float most = -INFINITY, used = -INFINITY, from = 0.0f, shift = SHIFT<DT>, sum = 0.0f;
-    // A query that has seen nothing but a table's lowest numbers sees no key of a far tile: all are -inf there.
-    const auto far_plus = [&](float from) { return from < -LOWEST ? -INFINITY : __builtin_fmaf(by_distance.far - from, LOG2E, SHIFT<DT>); };
     // What is left of a tile's scores: the bias, and -inf where a query does not see a key.
     const auto add_bias = [&](f32x16 &s, bool &is, int k0, int part) __attribute__((always_inline)) {
         if constexpr (BIAS) {
@@ -142,19 +143,24 @@ __global__ __launch_bounds__(256, 2) void k_attend(Attn a, Few f) {
                 const float times = some ? exp2_((used - most) * unit) : 1.0f;          // 0 at first
                 used = most;
                 from = some ? most : 0.0f;
-                shift = BIAS && fabsf(from) > USUAL ? SHIFT<DT> : SHIFT<DT> - from * unit;
+                large = __any(fabsf(from) > usual);
+                shift = fabsf(from) > usual ? SHIFT<DT> : SHIFT<DT> - from * unit;
                 sum *= times;
 #pragma unroll
                 for (int d = 0; d < HD / 32; ++d) out[d] *= times;
             }
+            if (large) {
+#pragma unroll
+                for (int e = 0; e < 16; ++e) {
+                    const float score = BIAS && is ? __builtin_fmaf(now[e], a.scale, by_distance.far) : now[e];
+                    now[e] = fabsf(from) > usual ? score - from : score;
+                }
+            }
         }
         arrived<FILLS>();                   // tile t + 2 may be on its way
         between();
-        if (BIAS && sees_now && !is && __any(fabsf(from) > USUAL)) {       // a table's lowest numbers, whose multiples by LOG2E do not exist
-#pragma unroll
-            for (int e = 0; e < 16; ++e) now[e] = fabsf(from) > USUAL ? now[e] - from : now[e];
-        }
-        const float times = BIAS && is ? a.scale * LOG2E : unit, plus = BIAS && is ? far_plus(from) : shift;
+        const bool as_far = BIAS && is && !large;
+        const float times = as_far ? a.scale * LOG2E : unit, plus = as_far ? __builtin_fmaf(by_distance.far - from, LOG2E, SHIFT<DT>) : shift;
         __builtin_amdgcn_s_setprio(1);
         if (sees_next) {                    // behind the last tile: of whatever the ring holds, and not looked at
             next = f32x16{};
@@ -446,12 +452,11 @@ __global__ __launch_bounds__((64 * few_waves(HD, NT))) void k_attend_few(Attn a,
             const float times = was == -INFINITY ? 0.0f : exp2_((was - base) * unit);
             most[n] = now;
             float added = 0.0f;
-            const float shift = SHIFT<DT> - base * unit;
 #pragma unroll
             for (int k = 0; k < 2; ++k)
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
-                    s[n][k][e] = exp2_(BIAS ? __builtin_fmaf(s[n][k][e] - base, unit, SHIFT<DT>) : __builtin_fmaf(s[n][k][e], unit, shift));
+                    s[n][k][e] = exp2_(__builtin_fmaf(s[n][k][e] - base, unit, SHIFT<DT>));
                     added += s[n][k][e];
                 }
             sum[n] = sum[n] * times + added;
