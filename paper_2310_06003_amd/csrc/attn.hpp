@@ -19,7 +19,6 @@ typedef _Float16 f16x8_t __attribute__((ext_vector_type(8)));
 constexpr float LOG2E = 1.44269504088896340736f, LN2 = 0.69314718055994530942f;
 constexpr int MAX_BUCKETS = 256, MIN_HEAD = 8, MAX_HEAD = 128;
 constexpr float USUAL = 1e5f;            // a score in size, up to which LOG2E times it says enough of it
-constexpr float LOWEST = 1e38f;          // ... from which, below zero, it is a table's lowest number
 constexpr int FAR_AWAY = 1 << 30;        // a window that holds every key: lengths are at most this
 
 template <int DT>

@@ -24,8 +24,8 @@ struct Grad {
     Rows dout, dq, dk, dv;
     Rows queries, douts;                     // q and dout as the fills take them: themselves, or copies, of sequence b from row b len_q on
     bool copied_q, copied_o;
-    // [head][rows_q]: P = exp2(s * LOG2E - base); D.  Of a bias, whose largest score may be a table's lowest number: P = exp2((s - peak) * LOG2E - log_sum)
-    float *base, *dots, *peak, *log_sum;
+    float *base, *dots;                      // [head][rows_q]: P = exp2(s * LOG2E - base), or, where the base is large in size, from the statistics (see peak_of); D
+    int *large;                              // [4 heads][16 rows]: whether the base of one is
     float *largest;                          // of fp16: the largest |dout_i|^2 and |v_j|^2 of each block of k_dots, of rows that see each other
     float *times;                            // of fp16: what dS is multiplied by, and the inverse
     float *partial;                          // of shared key tiles: [slot][dk, dv][128][HD]
@@ -36,7 +36,7 @@ struct Grad {
 };
 
 // ---------------------------------------------------------------- statistics of the rows
-constexpr int DOT_ROWS = 16, DOT_HEADS = 8;
+constexpr int DOT_ROWS = 16, DOT_HEADS = 8, FLAG_HEADS = 64 / DOT_ROWS;      // heads of a wave, whose rows have one flag
 
 template <int HD>
 __device__ __forceinline__ float over_lanes(float x) {       // of HD / 8 lanes side by side
@@ -92,6 +92,7 @@ __global__ __launch_bounds__(256) void k_dots(Grad g) {
     __syncthreads();
     const int r = threadIdx.x % DOT_ROWS, head = head0 + threadIdx.x / DOT_ROWS;
     float largest = 0.0f;
+    bool large = false;
     if (threadIdx.x < DOT_ROWS * DOT_HEADS && r < rows && head < heads) {
         bool counts;                         // P is zero in rows that see no key, and for keys that no row sees
         if (of_values) {
@@ -104,17 +105,17 @@ __global__ __launch_bounds__(256) void k_dots(Grad g) {
             const bool empty = most == -INFINITY;
             g.dots[at] = dots[threadIdx.x / DOT_ROWS][r];
             g.base[at] = empty ? INFINITY : __builtin_fmaf(most, LOG2E, log_sum * LOG2E) - SHIFT<DT>;
-            if (a.buckets) {
-                g.peak[at] = empty ? INFINITY : most;
-                g.log_sum[at] = empty ? 0.0f : log_sum * LOG2E - SHIFT<DT>;
-            }
             counts = !empty;
+            large = counts && fabsf(most) > USUAL;
         }
         if constexpr (DT == PARO_F16) {
             const float square = squares[threadIdx.x / DOT_ROWS][r];
             if (counts && square < INFINITY) largest = square;          // a row that is not finite leaves the others' scale alone
         }
     }
+    large = __any(large);
+    if (!of_values && threadIdx.x < DOT_ROWS * DOT_HEADS && (threadIdx.x & 63) == 0)
+        g.large[(int64_t)(head / FLAG_HEADS) * g.blocks_q + blockIdx.x] = large;
     if constexpr (DT == PARO_F16) {
         __shared__ float of_waves[4];
 #pragma unroll
@@ -160,6 +161,12 @@ __global__ __launch_bounds__(256) void k_times(Grad g) {
     }
 }
 
+// Where scores are large in size (a table's lowest number, or large products), LOG2E times one says too little: P = exp2((s - peak) * LOG2E - log_sum), with s as the forward pass
+// had it.  Of a row that sees no key the peak is infinity.
+__device__ __forceinline__ float peak_of(float most) { return most == -INFINITY ? INFINITY : most; }
+template <int DT>
+__device__ __forceinline__ float log_sum_of(float log_sum) { return log_sum * LOG2E - SHIFT<DT>; }
+
 // ---------------------------------------------------------------- dk and dv
 struct Share {
     int tile, share, shares, slot;           // slot < 0: the block has the tile to itself
@@ -184,8 +191,7 @@ template <int HD, bool BIAS>
 struct SharedKv {
     __attribute__((aligned(1024))) char tiles[2][2][Q_STEP * Tile<HD>::ROW];   // [buffer][queries, dout]
     __attribute__((aligned(1024))) char values[BLOCK * Tile<HD>::ROW];
-    __attribute__((aligned(16))) float rows[2][4][Q_STEP];                     // [buffer][base, dots, peak, log_sum]
-    int lowest[2];                                                             // whether the base of any row says too little
+    __attribute__((aligned(16))) float rows[2][4][Q_STEP];                     // [buffer][base, dots, of large ones peak, log_sum]
     std::conditional_t<BIAS, Bias, int> bias;
 };
 template <int DT, int HD, bool BIAS>
@@ -195,7 +201,6 @@ __device__ __forceinline__ void grad_kv(const Grad &g, unsigned block, SharedKv<
     auto &tiles = shared.tiles;
     auto &values = shared.values;
     auto &rows = shared.rows;
-    auto &lowest = shared.lowest;
     auto &bias = shared.bias;
     constexpr int STEPS = HD / 16;
     const int per_kv = g.sink_tiles * g.sink_shares + (g.key_tiles - g.sink_tiles) * g.shares;
@@ -216,12 +221,19 @@ __device__ __forceinline__ void grad_kv(const Grad &g, unsigned block, SharedKv<
     const int64_t all = (int64_t)per_head * group;
     const int from = (int)(all * share.share / share.shares), to = (int)(all * (share.share + 1) / share.shares);
 
+    bool large = false;                       // whether the base of some row is
+    {
+        const int tiles16 = g.blocks_q / a.batch, first16 = lo / DOT_ROWS, some = hi > lo ? (hi + DOT_ROWS - 1) / DOT_ROWS - first16 : 0;
+        for (int y = kv * group / FLAG_HEADS; y <= (kv * group + group - 1) / FLAG_HEADS; ++y)
+            for (int x = threadIdx.x; x < some; x += 256) large |= g.large[(int64_t)y * g.blocks_q + b * tiles16 + first16 + x] != 0;
+        large = __syncthreads_or(large);
+    }
     // The next step's head, and its first query.
     const int64_t row_q = g.copied_q ? (int64_t)b * a.len_q : seq.q0, row_o = g.copied_o ? (int64_t)b * a.len_q : seq.q0;
     const Filled<HD, Q_STEP> fill_q(g.queries.ld, a.hd), fill_o(g.douts.ld, a.hd);
     // What the next step takes: its head and tile of queries, where their rows are, and this thread's number of theirs.
     const int which = threadIdx.x / Q_STEP;
-    const float *const of_rows = (which == 0 ? g.base : which == 1 ? g.dots : which == 2 ? g.peak : g.log_sum) + seq.q0 + threadIdx.x % Q_STEP;
+    const float *const of_rows = (which == 0 ? g.base : g.dots) + seq.q0 + threadIdx.x % Q_STEP;
     const int64_t q_step = g.queries.ld * (2 * Q_STEP), o_step = g.douts.ld * (2 * Q_STEP);
     const char *q_at = nullptr, *o_at = nullptr;
     const float *row_at = nullptr;
@@ -234,11 +246,15 @@ __device__ __forceinline__ void grad_kv(const Grad &g, unsigned block, SharedKv<
         o_at = g.douts.of(row_o + next_i0, head);
         row_at = of_rows + (int64_t)head * a.rows_q + next_i0;
     };
-    const auto load = [&](auto buffer) __attribute__((always_inline)) {
-        if (which < (BIAS ? 4 : 2)) {
-            const int left = seq.nq - 1 - next_i0 - (int)threadIdx.x % Q_STEP;           // rows behind this thread's
+    const auto load = [&](auto buffer, auto large_) __attribute__((always_inline)) {
+        const int left = seq.nq - 1 - next_i0 - (int)threadIdx.x % Q_STEP;               // rows behind this thread's
+        if (which < 2) {
             const float x = row_at[left < 0 ? left : 0];
-            from_row = left >= 0 ? x : which % 2 == 0 ? INFINITY : 0.0f;
+            from_row = left >= 0 ? x : which == 0 ? INFINITY : 0.0f;
+        } else if (large_ && which < 4) {
+            const int i = next_i0 + (int)threadIdx.x % Q_STEP;
+            const float x = a.stats[(((int64_t)seq.q0 + (left < 0 ? i + left : i)) * a.heads + kv * group + next_head) * 2 + which - 2];
+            from_row = which == 2 ? left >= 0 ? peak_of(x) : INFINITY : log_sum_of<DT>(x);
         }
         const u32x4 q_from = fill_q.descriptor(q_at), o_from = fill_o.descriptor(o_at);
         if (next_i0 + Q_STEP <= seq.nq && next_i0 >= -off) {
@@ -253,13 +269,9 @@ __device__ __forceinline__ void grad_kv(const Grad &g, unsigned block, SharedKv<
     Distances by_distance{}, next_distance{};
     int of_head = -1;
     const auto lowest_of = [&](int i0) { return off + i0 - (k0 + BLOCK - 1); };
-    const auto stage = [&](auto buffer) __attribute__((always_inline)) {
-        if (threadIdx.x < (BIAS ? 4 : 2) * Q_STEP) rows[buffer][threadIdx.x / Q_STEP][threadIdx.x % Q_STEP] = from_row;
+    const auto stage = [&](auto buffer, auto large_) __attribute__((always_inline)) {
+        if (threadIdx.x < (large_ ? 4 : 2) * Q_STEP) rows[buffer][threadIdx.x / Q_STEP][threadIdx.x % Q_STEP] = from_row;
         if constexpr (BIAS) {
-            if (w == 1) {                                       // whose first half has the peaks
-                const bool any = __any(lane < 32 && fabsf(from_row) > USUAL && fabsf(from_row) < INFINITY);
-                if (lane == 0) lowest[buffer] = any;
-            }
             const int head = kv * group + next_head;
             if (head != of_head) {
                 __syncthreads();                                // the last head's tiles are done with its bias
@@ -289,8 +301,9 @@ __device__ __forceinline__ void grad_kv(const Grad &g, unsigned block, SharedKv<
     constexpr std::integral_constant<int, 0> b0{};
     constexpr std::integral_constant<int, 1> b1{};
     int left = to - from;
-    const auto step = [&](auto buffer_, auto other) __attribute__((always_inline)) {
+    const auto step = [&](auto buffer_, auto other, auto large_) __attribute__((always_inline)) {
         constexpr int buffer = buffer_;
+        constexpr bool LARGE = large_;
         const int i0 = next_i0, first = off + i0;
         const bool more = --left > 0;
         by_distance = next_distance;
@@ -304,7 +317,7 @@ __device__ __forceinline__ void grad_kv(const Grad &g, unsigned block, SharedKv<
             point();
         }
         arrived<0>();                        // this step's tiles; and all waves have left the last step's
-        if (more) load(other);
+        if (more) load(other, large_);
         const char *const queries = tiles[buffer][0], *const douts = tiles[buffer][1];
         const bool none = first + Q_STEP - 1 < of_wave || (first - (of_wave + 31) >= a.window && of_wave >= a.sinks);
         if (!none) {
@@ -328,11 +341,11 @@ __device__ __forceinline__ void grad_kv(const Grad &g, unsigned block, SharedKv<
                     if (!sees(first + 8 * (e / 4) + 4 * h + e % 4, j, a.window, a.sinks)) s[e] = -INFINITY;
             }
             const float by = BIAS && !far ? LOG2E : unit, plus = BIAS && far ? by_distance.far * LOG2E : 0.0f;
-            if (BIAS && lowest[buffer]) {                // a row's largest score may be a table's lowest number: P from the difference
+            if constexpr (LARGE) {
 #pragma unroll
                 for (int e = 0; e < 16; ++e) {
                     const int r = 8 * (e / 4) + 4 * h + e % 4;
-                    const float score = far ? __builtin_fmaf(s[e], a.scale, by_distance.far) : s[e], peak = rows[buffer][2][r];
+                    const float score = !BIAS ? s[e] * a.scale : far ? __builtin_fmaf(s[e], a.scale, by_distance.far) : s[e], peak = rows[buffer][2][r];
                     s[e] = peak < INFINITY ? exp2_(__builtin_fmaf(score - peak, LOG2E, -rows[buffer][3][r])) : 0.0f;
                 }
             } else {
@@ -363,18 +376,22 @@ __device__ __forceinline__ void grad_kv(const Grad &g, unsigned block, SharedKv<
                 }
             }
         }
-        if (more) stage(other);
+        if (more) stage(other, large_);
     };
     if (from < to) {
         next_head = from / per_head;
         next_tile = from % per_head;
         point();
-        load(b0);
-        stage(b0);
-        while (left > 0) {
-            step(b0, b1);
-            if (left > 0) step(b1, b0);
-        }
+        const auto steps = [&](auto large_) __attribute__((always_inline)) {
+            load(b0, large_);
+            stage(b0, large_);
+            while (left > 0) {
+                step(b0, b1, large_);
+                if (left > 0) step(b1, b0, large_);
+            }
+        };
+        if (large) steps(std::true_type{});
+        else steps(std::false_type{});
     }
     if (share.slot >= 0) {
         float *const at = g.partial + ((int64_t)share.slot * 2 * BLOCK + w * 32 + (lane & 31)) * HD + 4 * h;
@@ -496,15 +513,13 @@ __device__ __forceinline__ void grad_q(const Grad &g, unsigned block, SharedQ<HD
         __syncthreads();
     }
     short8_t q[STEPS], dout[STEPS];
-    float base = INFINITY, peak = INFINITY, log_sum = 0.0f, dot = 0.0f;
-    if (i < seq.nq) {
-        const int64_t at = (int64_t)head * a.rows_q + seq.q0 + i;
-        base = g.base[at];
-        dot = g.dots[at];
-        if constexpr (BIAS) {
-            peak = g.peak[at];
-            log_sum = g.log_sum[at];
-        }
+    const int64_t row = (int64_t)seq.q0 + (i < seq.nq ? i : seq.nq - 1), of_row = (int64_t)head * a.rows_q + row;
+    const float base = i < seq.nq ? g.base[of_row] : INFINITY, dot = i < seq.nq ? g.dots[of_row] : 0.0f;
+    bool large = false;                       // whether the base of some row is
+    {
+        const int tiles16 = g.blocks_q / a.batch, x = i0 / DOT_ROWS + threadIdx.x;
+        if (threadIdx.x < BLOCK / DOT_ROWS && x < tiles16) large = g.large[(int64_t)(head / FLAG_HEADS) * g.blocks_q + b * tiles16 + x] != 0;
+        large = __syncthreads_or(large);
     }
     {
         const int at = i < seq.nq ? i : seq.nq - 1;
@@ -517,11 +532,11 @@ __device__ __forceinline__ void grad_q(const Grad &g, unsigned block, SharedQ<HD
     }
     const float unit = a.scale * LOG2E, times = DT == PARO_F16 ? g.times[0] * 0x1p-15f : 1.0f;
     f32x16 dq[HD / 32] = {};
-    const bool lowest = BIAS && __any(fabsf(peak) > USUAL && fabsf(peak) < INFINITY);       // a row's largest score may be a table's lowest number
-    const float far_plus = peak < -LOWEST ? -INFINITY : by_distance.far * LOG2E - base;            // (which sees no key with another bias)
+    const float far_plus = by_distance.far * LOG2E - base;
     // In step t tile t + RING - 1 goes to the part of the ring whose tile all waves have left.  As many steps a round as the ring has parts, so
     // that these are constants.  PLAIN: every query sees the tile whole, and the tile that is brought is there whole.
-    const auto step = [&](auto part_, auto plain_, int t, int k0, const char *k_at, const char *v_at) __attribute__((always_inline)) {
+    const auto step = [&](auto part_, auto plain_, auto large_, int t, int k0, const char *k_at, const char *v_at) __attribute__((always_inline)) {
+        constexpr bool LARGE = large_;
         constexpr int part = part_, PLAIN = plain_, coming = (part + RING - 1) % RING;
         arrived<(RING - 2) * FILLS>();
         if constexpr (PLAIN) {
@@ -556,9 +571,14 @@ __device__ __forceinline__ void grad_q(const Grad &g, unsigned block, SharedQ<HD
                 for (int e = 0; e < 16; ++e)
                     if (!sees(place, k0 + 8 * (e / 4) + 4 * h + e % 4, a.window, a.sinks)) s[e] = -INFINITY;
             }
-            if (BIAS && !far && lowest) {
+            if constexpr (LARGE) {               // the row's numbers are read again in each step, as registers are few
+                const float *const stats = a.stats + (row * a.heads + head) * 2;
+                const float peak = i < seq.nq ? peak_of(stats[0]) : INFINITY, log_sum = log_sum_of<DT>(stats[1]);
 #pragma unroll
-                for (int e = 0; e < 16; ++e) s[e] = peak < INFINITY ? exp2_(__builtin_fmaf(s[e] - peak, LOG2E, -log_sum)) : 0.0f;
+                for (int e = 0; e < 16; ++e) {
+                    const float score = !BIAS ? s[e] * a.scale : far ? __builtin_fmaf(s[e], a.scale, by_distance.far) : s[e];
+                    s[e] = peak < INFINITY ? exp2_(__builtin_fmaf(score - peak, LOG2E, -log_sum)) : 0.0f;
+                }
             } else {
                 const float by = BIAS && !far ? LOG2E : unit, plus = BIAS && far ? far_plus : -base;
 #pragma unroll
@@ -641,23 +661,27 @@ __device__ __forceinline__ void grad_q(const Grad &g, unsigned block, SharedQ<HD
             if (t < seen.tiles) fill(t, t);
             else fill_none(t);
         }
-        for (int t = 0; t < seen.tiles;) {
-            if (t >= plain_from && t + 2 * RING - 2 < plain_to) {
-                int k0 = seen.tile(t) * KEYS;
-                const char *k_at = keys_at + (seen.tile(t) + RING - 1) * k_step, *v_at = values_at + (seen.tile(t) + RING - 1) * v_step;
-                for (; t + 2 * RING - 2 < plain_to; t += RING)
-                    static_for<0, RING>([&](auto part) __attribute__((always_inline)) {
-                        step(part, std::integral_constant<int, 1>{}, 0, k0, k_at, v_at);
-                        k0 += KEYS;
-                        k_at += k_step;
-                        v_at += v_step;
-                    });
+        const auto steps = [&](auto large_) __attribute__((always_inline)) {
+            for (int t = 0; t < seen.tiles;) {
+                if (t >= plain_from && t + 2 * RING - 2 < plain_to) {
+                    int k0 = seen.tile(t) * KEYS;
+                    const char *k_at = keys_at + (seen.tile(t) + RING - 1) * k_step, *v_at = values_at + (seen.tile(t) + RING - 1) * v_step;
+                    for (; t + 2 * RING - 2 < plain_to; t += RING)
+                        static_for<0, RING>([&](auto part) __attribute__((always_inline)) {
+                            step(part, std::integral_constant<int, 1>{}, large_, 0, k0, k_at, v_at);
+                            k0 += KEYS;
+                            k_at += k_step;
+                            v_at += v_step;
+                        });
+                }
+                static_for<0, RING>([&](auto part) __attribute__((always_inline)) {
+                    if (t < seen.tiles) step(part, std::integral_constant<int, 0>{}, large_, t, seen.tile(t) * KEYS, nullptr, nullptr);
+                    ++t;
+                });
             }
-            static_for<0, RING>([&](auto part) __attribute__((always_inline)) {
-                if (t < seen.tiles) step(part, std::integral_constant<int, 0>{}, t, seen.tile(t) * KEYS, nullptr, nullptr);
-                ++t;
-            });
-        }
+        };
+        if (large) steps(std::true_type{});
+        else steps(std::false_type{});
         arrived<0>();                                           // nothing is on its way into the shared memory of the block that comes next
     }
     const float of_dq = DT == PARO_F16 ? a.scale * g.times[1] : a.scale;
@@ -731,7 +755,7 @@ __global__ __launch_bounds__(256) void k_table_grad(Grad g) {
 // ---------------------------------------------------------------- host
 struct Plan {
     int blocks_q, blocks_v, blocks_heads, tiles, key_tiles, sink_tiles, shares, sink_shares, slots;
-    int64_t kv_blocks, copies, dots, peak, log_sum, largest, times, partial, of_table, bytes;
+    int64_t kv_blocks, copies, dots, large, largest, times, partial, of_table, bytes;
 };
 
 Plan plan_of(const paro_attn_t &d) {
@@ -778,8 +802,7 @@ Plan plan_of(const paro_attn_t &d) {
     };
     room(rows_q * d.heads);                                                     // base
     p.dots = room(rows_q * d.heads);
-    p.peak = room(d.buckets ? rows_q * d.heads : 0);
-    p.log_sum = room(d.buckets ? rows_q * d.heads : 0);
+    p.large = room((int64_t)p.blocks_q * p.blocks_heads * (DOT_HEADS / FLAG_HEADS));
     p.largest = room(d.dtype == PARO_F16 ? ((int64_t)p.blocks_q + p.blocks_v) * p.blocks_heads : 0);
     p.times = room(2);
     p.partial = room((int64_t)p.slots * d.kv_heads * d.batch * 2 * BLOCK * hd);
@@ -870,8 +893,7 @@ int paro_attn_grad(const paro_attn_t *d, const void *dout, const void *q, const 
         g.dv = as(g.a.v, dv);
         g.base = floats(0);
         g.dots = floats(p.dots);
-        g.peak = floats(p.peak);
-        g.log_sum = floats(p.log_sum);
+        g.large = reinterpret_cast<int *>(ws + p.large);
         g.largest = floats(p.largest);
         g.times = floats(p.times);
         g.partial = floats(p.partial);

@@ -54,7 +54,7 @@ class Exact(Case):
             self.buckets, self.table = 0, None
 
 
-def both(paro, lengths, scale, high, backward=False, **kw):
+def both(paro, lengths, scale, high, backward=True, **kw):
     c = Exact(paro, lengths, scale, high, **kw)
     c.forward()
     c.check(c.check_forward)
@@ -98,4 +98,4 @@ def test_with_a_bias(paro, hd, dtype, far, scale, high):
     kw = dict(hd=hd, dtype=dtype, buckets=12, far=far, table="f32")
     both(paro, [(300, 300), (20, 5)], scale, high, heads=4, kv=2, **kw)
     both(paro, [(3, 300)], scale, high, **kw)
-    both(paro, [(64, 5000)], scale, high, backward=False, **kw)
+    both(paro, [(64, 5000)], scale, high, backward=True, **kw)
