@@ -417,11 +417,13 @@ int paro_gated_grad(const paro_gated_t *d, const void *dh, const void *gate, con
  *   len_k, or k_lens[b], or (k_starts and no k_lens) k_starts[b + 1] - k_starts[b].
  * These are DEVICE int32 arrays of batch (+ 1 where a difference is taken) numbers; no sequence is longer than len_q and len_k, nor reaches past rows_q and rows_k
  * (0: batch * len), and what such an array says beyond that is cut off.  q and out, k and v have the same rows.  Rows of no sequence are neither read nor written, nor are
- * keys read that lie between the sinks and the first window of 128 queries; what is not finite there is of no account.  A key that some query of its tile sees is read:
- * what is not finite in it spreads to the results of those that see it, and may spread to others of the tile (up to 128 queries and 64 keys).
+ * keys read that lie between the sinks and the first window of 128 queries; what is not finite there is of no account, nor in queries in front of the first key.  A key that some
+ * query of its tile sees is read: what is not finite in it spreads to the results of those that see it, and may spread to others of the tile (up to 128 queries and 64 keys).
+ * An array of queries may be NULL where len_q is 0, one of keys where len_k is.
  * For more than 16 queries (len_q) and for the gradient: an array whose distances and head_dim are multiples of 8 is 16-byte aligned; the rows of others are copied into the
  * workspace (k and v; for the gradient q and dout too).  scale is in [1e-18, 1e18]; batch * heads * len at most 2^34,
- * less where that is more than 2^32 threads in a launch (PARO_ERANGE).
+ * less where that is more than 2^32 threads in a launch (PARO_ERANGE).  Scores and their softmax are fp32, of any size that fp32 holds; the softmax' shares are rounded to dtype
+ * for the product with v (fp16 times 2^7), out once more.
  * Bias: bucket(d) is the last b with first[b] <= d, first: DEVICE int32 [buckets], ascending from 0 (paro_rel_buckets); table: [buckets][heads] of table_dtype, dtype or
  * PARO_F32.  A bias of -inf hides; a row of a type's lowest number is one like others.  buckets == 0: none, table and first are not looked at.
  * stats: NULL, or fp32 [rows_q][heads][2] = the largest score and the log of the sum of exp(score - largest); -inf and 0 where no key is seen. */
@@ -443,7 +445,8 @@ int paro_attn(const paro_attn_t *d, const void *q, const void *k, const void *v,
  *   dv_j = sum P_ij dout_i,  dk_j = scale sum dS_ij q_i  (over queries and the heads that share them; as v, k),  dq_i = scale sum_j dS_ij k_j  (as q),
  *   dtable[b][head] = sum of dS_ij over bucket(p - j) = b  (as table; NULL = not wanted).
  * P and dS are rounded to dtype for the products (of dtable they are not), fp16 scaled by powers of two such that nothing overflows.  Sequences do not
- * share rows.  Rows of a sequence are all written, others stay as they are. */
+ * share rows.  Rows of a sequence are all written, others stay as they are; no sequence (batch 0) leaves dtable zeros, without a workspace.  What is not finite in q or dout of a query
+ * with p >= 0 spreads to its dq, and to dk and dv of the keys that a query of its tile (32) sees. */
 int paro_attn_grad(const paro_attn_t *d, const void *dout, const void *q, const void *k, const void *v, const void *out, const float *stats,
                    const int32_t *q_starts, const int32_t *k_starts, const int32_t *k_lens, const void *table, const int32_t *first,
                    void *dq, void *dk, void *dv, void *dtable, void *workspace, int64_t workspace_bytes, void *stream);

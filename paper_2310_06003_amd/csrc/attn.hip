@@ -8,9 +8,10 @@
 // stand, and maximum and sum of a row need one exchange between the two halves of a wave.  fp16 shares are multiplied by 2^7 (divided out at the end), so that
 // those below 2^-14 of the largest keep their bits.
 //
-// k_attend: 8192 tokens of 32 heads of 128, window 4096, 430 us, 960 TF: the matrix cores are busy 49 % of the cycles, the vector unit (16 exponents, 84 other instructions
-// for 32 x 32 scores) a third, at the clock that power allows.  8 x 1024 tokens of 12 heads of 64 with bias 32 us: the vector unit and the way from score to product.
-// k_attend_few: 4 tokens over 50000 to 100000 keys, 8 key heads of 128, 259 us, 5.2 TB/s: memory.
+// k_attend: 8192 tokens of 32 heads of 128, window 4096, 437 us at best (945 TF), 479 in the middle: the matrix cores are busy 50 % of the cycles, the vector unit (16 exponents,
+// 84 other instructions for 32 x 32 scores) a third, at the clock that power allows (1.8 GHz).  8 x 1024 tokens of 12 heads of 64 with bias 35 us: the way from score to exponent to
+// product, with a barrier behind eight matrix instructions; waves wait 41 %, matrix cores are busy 13 %.  64 tokens over 100000 keys, 8 key heads of 128, shared: 203 us and 7 to join.
+// k_attend_few: 4 tokens over 50000 to 100000 keys, 8 key heads of 128, 271 us at best, 4.9 TB/s: memory.
 #include "attn.hpp"
 
 namespace {
@@ -26,8 +27,8 @@ struct Few {                              // of blocks that share a tile's keys,
     float *sums, *stats;                  // of a share: [block][ROWS][HD], and [block][ROWS][2]: largest score, sum
 };
 
-// SHARED: the block has one share of its tile's keys.  (Unshared: 64 tokens over 100000 keys, 8 key heads of 128, 1750 us, so 220; 8192 tokens of one head of 64 117, so 39; 2048 of
-// four 35, so 30.)
+// SHARED: the block has one share of its tile's keys.  (Unshared: 64 tokens over 100000 keys, 8 key heads of 128, 1793 us, so 221; 8192 tokens of one head of 64 123, so 37; 2048 of
+// four 37, so 29.)
 template <int DT, int HD, bool BIAS, bool SHARED>
 __global__ __launch_bounds__(256, 2) void k_attend(Attn a, Few f) {
     using T = Tile<HD>;

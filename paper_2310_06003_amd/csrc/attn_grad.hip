@@ -44,8 +44,8 @@ __device__ __forceinline__ float over_lanes(float x) {       // of HD / 8 lanes 
     for (int n = 1; n < HD / 8; n *= 2) x += __shfl_xor(x, n);
     return x;
 }
-// D, and what P is formed from, of 16 rows of 8 heads; blocks behind those of the queries: the values' largest row, of those that some query sees.  Reads dout and out once: 8192 tokens of 32 heads of 128
-// 28 us, 4.9 TB/s.
+// D, and what P is formed from, of 16 rows of 8 heads; blocks behind those of the queries: the values' largest row, of those that some query sees.  Reads dout and out once: 8192
+// tokens of 32 heads of 128 30 us at best, 4.6 TB/s.
 template <int DT, int HD>
 __global__ __launch_bounds__(256) void k_dots(Grad g) {
     const Attn &a = g.a;
@@ -718,8 +718,9 @@ __device__ __forceinline__ void grad_q(const Grad &g, unsigned block, SharedQ<HD
 }
 
 // Both passes in one launch, as neither fills the chip to its end: the first of_kv blocks (a multiple of eight, so that what is one XCD's stays there) have keys,
-// the others queries.  (In launches of their own: 1999 tokens of 10 heads of 77 88 + 59 us, so 114.)  8192 tokens of 32 heads of 128, all seen: 1750 us, 1100 TF of the seven
-// products; matrix cores busy 56 % of the cycles at 1.74 GHz, shared memory 37 %.  8 x 1024 of 12 heads of 64 with bias 96 us: waves wait half of their cycles, three a SIMD.
+// the others queries.  (In launches of their own: 1999 tokens of 10 heads of 77 88 + 59 us, so 114.)  8192 tokens of 32 heads of 128, all seen: 1777 us, 1080 TF of the seven
+// products; matrix cores busy 56 % of the cycles at 1.77 GHz, shared memory 36 %.  8 x 1024 of 12 heads of 64 with bias 96 us: waves wait half of their cycles, three a SIMD.
+// Steps for large scores (see peak_of) are loops of their own, as a question in each step costs registers: 8192 tokens 1862 us the call, so 1801, packed sequences 676, so 634.
 template <int DT, int HD, bool BIAS>
 __global__ __launch_bounds__(256, HD == 64 ? 3 : 2) void k_grads(Grad g, unsigned of_kv) {
     __shared__ union {
