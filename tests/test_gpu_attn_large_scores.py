@@ -99,3 +99,26 @@ def test_with_a_bias(paro, hd, dtype, far, scale, high):
     both(paro, [(300, 300), (20, 5)], scale, high, heads=4, kv=2, **kw)
     both(paro, [(3, 300)], scale, high, **kw)
     both(paro, [(64, 5000)], scale, high, backward=True, **kw)
+
+
+@pytest.mark.parametrize("lengths", [[(200, 200)], [(1, 300), (16, 300), (9, 9)], [(64, 5000)]])
+@pytest.mark.parametrize("hd,buckets", [(64, 0), (128, 0), (128, 12)])
+def test_shares_are_at_most_one(paro, hd, buckets, lengths):
+    """Scores of 10^8 to 10^9 whose sums round: the forward pass gives means of values all the same, and the gradient, which has to form the same scores to the bit (few queries take other products forward
+    than backward), a P of at most exp(-log_sum), which is at most one.  So |out| is at most the largest |v| and |dv_j| the sum of |dout_i| over queries and heads, each but for its roundings: of out by half a step, its
+    shares by another; of P and dv by half a step each; of sums by 2^-24 a term."""
+    for dtype, size in (("bf16", 3e4), ("f16", 1e4)):
+        c = Case(paro, lengths, heads=4, kv=2, hd=hd, dtype=dtype, buckets=buckets, size=size)
+        c.k.view.mul_(size).clamp_(-6e4, 6e4)
+        c.q.view.clamp_(-6e4, 6e4)
+        c.forward()
+        c.backward()
+        half = 2.0 ** -8 if dtype == "bf16" else 2.0 ** -11
+        for (nq, nk), q_at, k_at in zip(lengths, c.q_at, c.k_at):
+            out, dout = (x.view[q_at:q_at + nq].double() for x in (c.out, c.dout))
+            v, dv = (x.view[k_at:k_at + nk].double() for x in (c.v, c.dv))
+            assert bool((out.abs() <= v.abs().amax(0).repeat_interleave(2, 0) * (1 + half) * (1 + half) * (1 + 2 * nk * 2.0 ** -24) + 2.0 ** -25).all())
+            most = dout.abs().sum(0).unflatten(0, (2, 2)).sum(1)
+            assert bool((dv.abs() <= most * (1 + half) ** 2 * (1 + 4 * nq * 2.0 ** -24) + 2.0 ** -25).all()), float((dv.abs() / most).max())
+            if dtype == "bf16":
+                assert all(bool(x.view[at:at + n].isfinite().all()) for x, at, n in ((c.dq, q_at, nq), (c.dk, k_at, nk)))
